@@ -355,6 +355,113 @@ int32_t gnnco_embedding_update(gnnco_handle* h, int32_t feat_dtype, int32_t F, c
                                float* m, float* v, void* X, float lr, float beta1, float beta2, float eps,
                                int64_t step, void* stream);
 
+/* Input embeddings SHARED between nodes: every node carries a token (its degree class, its community, its type) and
+ * reads row tokens[i] of one table, so that few rows learn from many nodes (a table of its own per node is
+ * gnnco_embedding_update's variant).  Rows of table, out, dout and dtable are F consecutive elements, `*_ld`
+ * elements apart (>= F), so out may be a block of columns of X; any alignment works, 16-byte aligned rows are faster.
+ *
+ * gnnco_embedding_lookup: out[i,:] = scale * table[tokens[i],:] for i < rows, rounded once to out_dtype.  A negative
+ * token means "no token" and gives a row of zeros.  A token >= V gives a row of zeros too and makes
+ * gnnco_async_status report GNNCO_OUT_OF_RANGE.
+ *
+ * gnnco_embedding_plan: orders the rows by token (stable) into plan_ws (gnnco_embedding_plan_bytes bytes for the largest
+ * F it will be used with, 256-byte aligned, caller-owned); one plan serves every gradient with these tokens.  Tokens
+ * outside [0, V) are left out (>= V is reported as above).
+ *
+ * gnnco_embedding_grad: dtable[v,:] = scale * sum over rows i with token v of dout[i,:], for every v < V (zeros for a
+ * token that does not occur), summed in float32 in the plan's order (bit-identical from run to run, no
+ * floating-point atomics) and rounded once to table_dtype.  rows, V and F as given to the plan; partial sums use
+ * plan_ws, so gradients from one plan must not overlap on the GPU.
+ * All three are asynchronous on `stream`; 0 <= rows < 2^31 - 1, F <= 65536. */
+int32_t gnnco_embedding_lookup(gnnco_handle* h, int32_t table_dtype, int32_t out_dtype, int64_t rows, int32_t V, int32_t F,
+                               const int32_t* tokens, const void* table, int64_t table_ld, float scale, void* out,
+                               int64_t out_ld, void* stream);
+int32_t gnnco_embedding_plan_bytes(int64_t rows, int32_t V, int32_t F, size_t* bytes);
+int32_t gnnco_embedding_plan(gnnco_handle* h, const int32_t* tokens, int64_t rows, int32_t V, int32_t F, void* plan_ws,
+                             size_t plan_bytes, void* stream);
+int32_t gnnco_embedding_grad(gnnco_handle* h, int32_t grad_dtype, int32_t table_dtype, int64_t rows, int32_t V, int32_t F,
+                             const void* dout, int64_t dout_ld, float scale, void* plan_ws, size_t plan_bytes,
+                             void* dtable, int64_t dtable_ld, void* stream);
+
+/* Norms before and after a block of the network, fused with the block's gate and residual scale.  With
+ * r(v) = 1 / sqrt(mean_f v_f^2 + eps), row by row:
+ *   x_out = x + scale * gate .* (y * r(y)) .* w_post      (x: residual stream, y: the block's output)
+ *   h_out = (x_out * r(x_out)) .* w_pre                   (the next block's input)
+ * y == NULL: no block yet (the first norm of a network), x_out is x itself and must be NULL.  h_out == NULL: no further
+ * norm.  gate == NULL: 1;  gate_ld == 0: one float32 vector [F] shared by all rows;  gate_ld >= F: a row of its own
+ * per row, in feat_dtype.  w_pre, w_post: float32 [F] or NULL (= 1).  x, y, x_out, h_out: feat_dtype, rows `*_ld`
+ * elements apart; x_out may be x.  Statistics are float32; h_out is computed from x_out before it is rounded.  F <= 8192.
+ *
+ * gnnco_block_norm_backward: `d` as in the forward call except that d->x is the residual stream AFTER the block (x_out,
+ * or x where there was no block).  dx_out (gradient arriving on the stream) and dh (gradient of h_out) are inputs, either
+ * may be NULL but not both (without dh, d->x is not read); dx (required), dy (required iff y) are outputs; dx may be
+ * dx_out.  dw_pre, dw_post: float32 [F] or NULL; dgate: like the gate (float32 [F], or feat_dtype rows dgate_ld apart) or
+ * NULL.  Sums over rows are taken in a fixed order.  ws: gnnco_block_norm_workspace_bytes bytes, 256-byte aligned.
+ * Asynchronous on `stream`. */
+typedef struct {
+  int64_t rows;
+  int32_t F;
+  int32_t feat_dtype;            /* gnnco_dtype */
+  float eps;                     /* > 0 */
+  float scale;
+  const void* x;
+  int64_t x_ld;
+  const void* y;                 /* or NULL */
+  int64_t y_ld;
+  const void* gate;              /* or NULL */
+  int64_t gate_ld;
+  const float* w_pre;            /* [F] or NULL */
+  const float* w_post;           /* [F] or NULL */
+} gnnco_block_norm_desc;
+typedef struct {
+  const void* dx_out;
+  int64_t dx_out_ld;
+  const void* dh;
+  int64_t dh_ld;
+  void* dx;
+  int64_t dx_ld;
+  void* dy;
+  int64_t dy_ld;
+  void* dgate;
+  int64_t dgate_ld;
+  float* dw_pre;
+  float* dw_post;
+} gnnco_block_norm_grads;
+int32_t gnnco_block_norm(gnnco_handle* h, const gnnco_block_norm_desc* d, void* x_out, int64_t x_out_ld, void* h_out,
+                         int64_t h_out_ld, void* stream);
+int32_t gnnco_block_norm_workspace_bytes(const gnnco_handle* h, int32_t F, size_t* bytes);
+int32_t gnnco_block_norm_backward(gnnco_handle* h, const gnnco_block_norm_desc* d, const gnnco_block_norm_grads* g, void* ws,
+                                  size_t ws_bytes, void* stream);
+
+/* Weight updates orthogonalised by Newton-Schulz products (an alternative to Adam for the weights of the hidden layers),
+ * for `sets` matrices W [sets x rows x cols] at once:
+ *   m = momentum * m + dW;   u = dW + momentum * m (nesterov != 0) or m
+ *   X = u / (|u|_F + eps), transposed where rows > cols;   `steps` times:  A = X X^T,  X = (a I + b A + c A A) X
+ *   W = W (1 - lr * weight_decay) - lr * sqrt(max(1, cols / rows)) * X
+ * The usual coefficients are a = 3.4445, b = -4.7750, c = 2.0315 with 5 steps: singular values of u end near 1.
+ * Coefficients that carry a singular value in [0, 1] past 2 are refused; steps 1 .. 32.  Products are taken to float32
+ * accuracy (operands split into two float16 limbs, float32 accumulation); the norm is summed in float64.  A zero
+ * gradient gives a zero X; a matrix with an infinity or NaN in u gives NaN in its own set only.  `active` (device,
+ * [sets] uint8, or NULL = all): sets with active[s] == 0 keep W and m bit for bit.  Layers updated here are
+ * noticed by GNNCO_WEIGHTS_UNTOUCHED.
+ * gnnco_orthogonalise: O = X after the steps, in G's orientation, for G and O [sets x rows x cols] in float32 or bfloat16
+ * (lr, momentum, weight_decay and nesterov are not read; sets that are not active are not written; O may be G).
+ * ws: gnnco_muon_workspace_bytes bytes, 256-byte aligned.  Asynchronous on `stream`; results do not depend on `sets` or
+ * on timing. */
+typedef struct {
+  float lr, momentum, weight_decay;
+  int32_t nesterov;
+  int32_t steps;
+  float a, b, c;
+  float eps;                     /* > 0 */
+  const uint8_t* active;
+} gnnco_muon_params;
+int32_t gnnco_muon_workspace_bytes(const gnnco_handle* h, int64_t sets, int32_t rows, int32_t cols, size_t* bytes);
+int32_t gnnco_muon_update(gnnco_handle* h, int64_t sets, int32_t rows, int32_t cols, float* W, float* m, const float* dW,
+                          const gnnco_muon_params* p, void* ws, size_t ws_bytes, void* stream);
+int32_t gnnco_orthogonalise(gnnco_handle* h, int32_t in_dtype, int32_t out_dtype, int64_t sets, int32_t rows, int32_t cols,
+                            const void* G, void* O, const gnnco_muon_params* p, void* ws, size_t ws_bytes, void* stream);
+
 /* Objective only, for callers that cannot allocate device memory.  (The paper has no
  * counterpart to this call; it exists for the way the library is embedded.)
  *

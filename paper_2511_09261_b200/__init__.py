@@ -28,7 +28,9 @@ EXPORTS = [
     "gnnco_profile_begin", "gnnco_profile_end", "gnnco_objective_static", "gnnco_conflict_workspace_bytes",
     "gnnco_conflict_actions", "gnnco_apply_actions", "gnnco_gumbel_softmax", "gnnco_embedding_update",
     "gnnco_repair_boundary", "gnnco_partition_quality", "gnnco_active_plan_bytes", "gnnco_active_plan",
-    "gnnco_louvain_workspace_bytes", "gnnco_louvain",
+    "gnnco_louvain_workspace_bytes", "gnnco_louvain", "gnnco_embedding_lookup", "gnnco_embedding_plan_bytes",
+    "gnnco_embedding_plan", "gnnco_embedding_grad", "gnnco_block_norm", "gnnco_block_norm_workspace_bytes",
+    "gnnco_block_norm_backward", "gnnco_muon_workspace_bytes", "gnnco_muon_update", "gnnco_orthogonalise",
 ]
 
 _vp, _i32, _i64, _u32, _f32, _sz = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_float,
@@ -65,6 +67,22 @@ class TrainOut(ctypes.Structure):
 
 class ProfileEntry(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 32), ("calls", _i64), ("total_ms", ctypes.c_double)]
+
+
+class BlockNormDesc(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("F", _i32), ("feat_dtype", _i32), ("eps", _f32), ("scale", _f32), ("x", _vp),
+                ("x_ld", _i64), ("y", _vp), ("y_ld", _i64), ("gate", _vp), ("gate_ld", _i64), ("w_pre", _vp),
+                ("w_post", _vp)]
+
+
+class BlockNormGrads(ctypes.Structure):
+    _fields_ = [("dx_out", _vp), ("dx_out_ld", _i64), ("dh", _vp), ("dh_ld", _i64), ("dx", _vp), ("dx_ld", _i64),
+                ("dy", _vp), ("dy_ld", _i64), ("dgate", _vp), ("dgate_ld", _i64), ("dw_pre", _vp), ("dw_post", _vp)]
+
+
+class MuonParams(ctypes.Structure):
+    _fields_ = [("lr", _f32), ("momentum", _f32), ("weight_decay", _f32), ("nesterov", _i32), ("steps", _i32),
+                ("a", _f32), ("b", _f32), ("c", _f32), ("eps", _f32), ("active", _vp)]
 
 
 class GnncoError(RuntimeError):
@@ -123,6 +141,18 @@ def load_library(build_if_missing: bool = True):
     lib.gnnco_active_plan.argtypes = [_vp, _vp, _vp, _sz, _vp, ctypes.POINTER(_i32)]
     lib.gnnco_gumbel_softmax.argtypes = [_vp, _i32, _i32, _vp, _vp, _f32, _vp, _vp]
     lib.gnnco_embedding_update.argtypes = [_vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _f32, _f32, _f32, _f32, _i64, _vp]
+    lib.gnnco_embedding_lookup.argtypes = [_vp, _i32, _i32, _i64, _i32, _i32, _vp, _vp, _i64, _f32, _vp, _i64, _vp]
+    lib.gnnco_embedding_plan_bytes.argtypes = [_i64, _i32, _i32, ctypes.POINTER(_sz)]
+    lib.gnnco_embedding_plan.argtypes = [_vp, _vp, _i64, _i32, _i32, _vp, _sz, _vp]
+    lib.gnnco_embedding_grad.argtypes = [_vp, _i32, _i32, _i64, _i32, _i32, _vp, _i64, _f32, _vp, _sz, _vp, _i64, _vp]
+    lib.gnnco_block_norm.argtypes = [_vp, ctypes.POINTER(BlockNormDesc), _vp, _i64, _vp, _i64, _vp]
+    lib.gnnco_block_norm_workspace_bytes.argtypes = [_vp, _i32, ctypes.POINTER(_sz)]
+    lib.gnnco_block_norm_backward.argtypes = [_vp, ctypes.POINTER(BlockNormDesc), ctypes.POINTER(BlockNormGrads), _vp,
+                                              _sz, _vp]
+    lib.gnnco_muon_workspace_bytes.argtypes = [_vp, _i64, _i32, _i32, ctypes.POINTER(_sz)]
+    lib.gnnco_muon_update.argtypes = [_vp, _i64, _i32, _i32, _vp, _vp, _vp, ctypes.POINTER(MuonParams), _vp, _sz, _vp]
+    lib.gnnco_orthogonalise.argtypes = [_vp, _i32, _i32, _i64, _i32, _i32, _vp, _vp, ctypes.POINTER(MuonParams), _vp, _sz,
+                                        _vp]
     for name in EXPORTS:
         if name not in ("gnnco_status_string", "gnnco_launch_count"):
             getattr(lib, name).restype = _i32
@@ -154,6 +184,29 @@ def _require(t, dtype, what: str, device_type: str = "cuda"):
     if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_contiguous() or t.device.type != device_type:
         raise TypeError("%s must be a contiguous %s tensor of dtype %s" % (what, device_type, dtype))
     return t
+
+
+def _feat_code(t, what: str) -> int:
+    import torch
+    if isinstance(t, torch.Tensor):
+        if t.dtype == torch.float32:
+            return F32
+        if t.dtype == torch.bfloat16:
+            return BF16
+    raise TypeError("%s must be a float32 or bfloat16 tensor" % what)
+
+
+def _empty(shape, dtype, device, stream):
+    """A tensor for a call on ``stream``: its memory comes from that stream's pool, so that work still queued on
+    the current stream cannot own it."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+MUON_COEFS = (3.4445, -4.7750, 2.0315)
 
 
 class Model:
@@ -215,6 +268,27 @@ class Adam:
         a.active = _dptr(self.active)
         a.step_dev = _dptr(self.step_dev)
         return a
+
+
+class Muon:
+    """Momentum and hyper-parameters of orthogonalised updates (``gnnco_muon_params``) for every weight of a model;
+    ``PartitionedGraph.muon_step`` applies one.  (A layer of width 1 gets its normalised gradient: the one singular
+    vector there is.)"""
+
+    def __init__(self, model: Model, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True,
+                 weight_decay: float = 0.0, steps: int = 5, coefs: Sequence[float] = MUON_COEFS, eps: float = 1e-7):
+        import torch
+        self.lr, self.momentum, self.nesterov, self.weight_decay = lr, momentum, nesterov, weight_decay
+        self.steps, self.coefs, self.eps = steps, tuple(coefs), eps
+        self.active = None          # uint8 [weight_sets] device tensor: sets that are updated (None = all)
+        self.m = [torch.zeros_like(w) for w in model.W]
+
+
+class EmbeddingPlan:
+    """Rows ordered by token (``gnnco_embedding_plan``); serves every gradient with the same tokens and width <= F."""
+
+    def __init__(self, rows: int, V: int, F: int, ws):
+        self.rows, self.V, self.F, self.ws = rows, V, F, ws
 
 
 class PartitionedGraph:
@@ -493,6 +567,221 @@ class PartitionedGraph:
                                                 float(beta2), float(eps), int(step), _stream_ptr(stream)),
                "gnnco_embedding_update")
         return X
+
+    # ---- shared input embeddings, norms around a block, orthogonalised updates
+
+    def _rows(self, t, dtype, shape, what: str) -> int:
+        """Checks a [rows, F] tensor whose rows are consecutive elements; returns the distance between rows."""
+        import torch
+        if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != self.device or t.dim() != 2:
+            raise TypeError("%s must be a 2-D %s tensor on %s" % (what, dtype, self.device))
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError("%s must be %s" % (what, list(shape)))
+        if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+            raise ValueError("%s must have rows of consecutive elements that do not overlap" % what)
+        return t.stride(0) if t.shape[0] > 1 else max(int(t.shape[1]), 1)
+
+    def _tokens(self, tokens):
+        import torch
+        _require(tokens, torch.int32, "tokens")
+        if tokens.dim() != 1 or tokens.device != self.device:
+            raise ValueError("tokens must be one-dimensional and on %s" % self.device)
+        return int(tokens.shape[0])
+
+    def embedding_lookup(self, table, tokens, scale: float = 1.0, out=None, out_dtype=None, stream=None):
+        """``gnnco_embedding_lookup``: scale * table[tokens] for ``tokens`` int32 [rows]; a negative token gives zeros.
+        ``table`` [V, F] and ``out`` [rows, F] are float32 or bfloat16 (``out_dtype`` defaults to the table's) and
+        may be columns of wider tensors."""
+        td = _feat_code(table, "table")
+        rows = self._tokens(tokens)
+        if table.dim() != 2 or 0 in table.shape:
+            raise ValueError("table must be [V, F]")
+        V, F = table.shape
+        table_ld = self._rows(table, table.dtype, table.shape, "table")
+        if out is None:
+            out = _empty((rows, F), out_dtype or table.dtype, self.device, stream)
+        od = _feat_code(out, "out")
+        out_ld = self._rows(out, out.dtype, (rows, F), "out")
+        _check(self._lib.gnnco_embedding_lookup(self._handle, td, od, rows, V, F, tokens.data_ptr(), table.data_ptr(),
+                                                table_ld, scale, out.data_ptr(), out_ld, _stream_ptr(stream)),
+               "gnnco_embedding_lookup")
+        return out
+
+    def embedding_plan(self, tokens, V: int, F: int, stream=None) -> EmbeddingPlan:
+        """``gnnco_embedding_plan``: order of ``tokens`` (int32 [rows]) for gradients of tables [V, <= F].  No host
+        synchronisation."""
+        import torch
+        rows = self._tokens(tokens)
+        need = _sz(0)
+        _check(self._lib.gnnco_embedding_plan_bytes(rows, V, F, ctypes.byref(need)), "gnnco_embedding_plan_bytes")
+        ws = _empty(need.value, torch.uint8, self.device, stream)
+        _check(self._lib.gnnco_embedding_plan(self._handle, tokens.data_ptr(), rows, V, F, ws.data_ptr(), need.value,
+                                              _stream_ptr(stream)), "gnnco_embedding_plan")
+        return EmbeddingPlan(rows, V, F, ws)
+
+    def embedding_grad(self, plan: EmbeddingPlan, dout, scale: float = 1.0, out=None, out_dtype=None, stream=None):
+        """``gnnco_embedding_grad``: gradient [V, F] of the table of ``embedding_lookup`` for the plan's tokens, from
+        ``dout`` [rows, F] (float32 or bfloat16); float32 unless ``out`` or ``out_dtype`` says bfloat16."""
+        import torch
+        gd = _feat_code(dout, "dout")
+        if dout.dim() != 2 or not 1 <= dout.shape[1] <= plan.F:
+            raise ValueError("dout must be [rows, F] with F up to the plan's")
+        F = dout.shape[1]
+        dout_ld = self._rows(dout, dout.dtype, (plan.rows, F), "dout")
+        if out is None:
+            out = _empty((plan.V, F), out_dtype or torch.float32, self.device, stream)
+        od = _feat_code(out, "out")
+        out_ld = self._rows(out, out.dtype, (plan.V, F), "out")
+        _check(self._lib.gnnco_embedding_grad(self._handle, gd, od, plan.rows, plan.V, F, dout.data_ptr(), dout_ld,
+                                              scale, plan.ws.data_ptr(), plan.ws.numel(), out.data_ptr(), out_ld,
+                                              _stream_ptr(stream)), "gnnco_embedding_grad")
+        return out
+
+    def _weight(self, w, F, what: str):
+        import torch
+        if w is None:
+            return None
+        _require(w, torch.float32, what)
+        if tuple(w.shape) != (F,) or w.device != self.device:
+            raise ValueError("%s must be [F] on %s" % (what, self.device))
+        return w.data_ptr()
+
+    def _block_desc(self, x, w_pre, y, w_post, gate, scale, eps):
+        dt = _feat_code(x, "x")
+        if x.dim() != 2 or x.shape[1] < 1:
+            raise ValueError("x must be [rows, F]")
+        if y is None and (gate is not None or w_post is not None):
+            raise ValueError("gate and w_post belong to a block output y")
+        rows, F = x.shape
+        d = BlockNormDesc(rows, F, dt, eps, scale, x.data_ptr(), self._rows(x, x.dtype, (rows, F), "x"))
+        if y is not None:
+            d.y, d.y_ld = y.data_ptr(), self._rows(y, x.dtype, (rows, F), "y")
+        if gate is not None:
+            if gate.dim() == 1:
+                d.gate = self._weight(gate, F, "gate")
+            else:
+                d.gate, d.gate_ld = gate.data_ptr(), self._rows(gate, x.dtype, (rows, F), "gate")
+        d.w_pre, d.w_post = self._weight(w_pre, F, "w_pre"), self._weight(w_post, F, "w_post")
+        return d
+
+    def block_norm(self, x, w_pre=None, y=None, w_post=None, gate=None, scale: float = 1.0, eps: float = 1e-6, x_out=None,
+                   h_out=None, want_h: bool = True, stream=None):
+        """``gnnco_block_norm``: (x_out, h) with x_out = x + scale * gate * norm(y) * w_post and h = norm(x_out) * w_pre.
+        Without ``y`` x_out is x; with want_h=False h is None.  ``gate``: None, float32 [F] or [rows, F] like x."""
+        d = self._block_desc(x, w_pre, y, w_post, gate, scale, eps)
+        shape = (d.rows, d.F)
+        if y is None:
+            if x_out is not None:
+                raise ValueError("x_out belongs to a block output y")
+        elif x_out is None:
+            x_out = _empty(shape, x.dtype, self.device, stream)
+        if h_out is None and want_h:
+            h_out = _empty(shape, x.dtype, self.device, stream)
+        _check(self._lib.gnnco_block_norm(
+            self._handle, ctypes.byref(d), _dptr(x_out), 0 if x_out is None else self._rows(x_out, x.dtype, shape, "x_out"),
+            _dptr(h_out), 0 if h_out is None else self._rows(h_out, x.dtype, shape, "h_out"), _stream_ptr(stream)),
+            "gnnco_block_norm")
+        return (x if y is None else x_out), h_out
+
+    def block_norm_backward(self, x, dh=None, w_pre=None, dx_out=None, y=None, w_post=None, gate=None, scale: float = 1.0,
+                            eps: float = 1e-6, dx=None, dy=None, dgate=None, stream=None):
+        """``gnnco_block_norm_backward``: ``x`` is the stream after the block (the forward call's x_out).  Returns
+        dict(dx, dy, dgate, dw_pre, dw_post); entries whose input was not given are None."""
+        import torch
+        d = self._block_desc(x, w_pre, y, w_post, gate, scale, eps)
+        shape = (d.rows, d.F)
+        g = BlockNormGrads()
+        if dh is not None:
+            g.dh, g.dh_ld = dh.data_ptr(), self._rows(dh, x.dtype, shape, "dh")
+        if dx_out is not None:
+            g.dx_out, g.dx_out_ld = dx_out.data_ptr(), self._rows(dx_out, x.dtype, shape, "dx_out")
+        if dx is None:
+            dx = _empty(shape, x.dtype, self.device, stream)
+        g.dx, g.dx_ld = dx.data_ptr(), self._rows(dx, x.dtype, shape, "dx")
+        if y is not None:
+            if dy is None:
+                dy = _empty(shape, x.dtype, self.device, stream)
+            g.dy, g.dy_ld = dy.data_ptr(), self._rows(dy, x.dtype, shape, "dy")
+        if gate is not None:
+            if dgate is None:
+                dgate = _empty(tuple(gate.shape), gate.dtype, self.device, stream)
+            if gate.dim() == 1:
+                g.dgate = self._weight(dgate, d.F, "dgate")
+            else:
+                g.dgate, g.dgate_ld = dgate.data_ptr(), self._rows(dgate, x.dtype, shape, "dgate")
+        dw_pre = dw_post = None
+        if w_pre is not None:
+            dw_pre = _empty(d.F, torch.float32, self.device, stream)
+            g.dw_pre = dw_pre.data_ptr()
+        if w_post is not None:
+            dw_post = _empty(d.F, torch.float32, self.device, stream)
+            g.dw_post = dw_post.data_ptr()
+        need = _sz(0)
+        _check(self._lib.gnnco_block_norm_workspace_bytes(self._handle, d.F, ctypes.byref(need)),
+               "gnnco_block_norm_workspace_bytes")
+        ws = _empty(need.value, torch.uint8, self.device, stream)
+        _check(self._lib.gnnco_block_norm_backward(self._handle, ctypes.byref(d), ctypes.byref(g), ws.data_ptr(),
+                                                   need.value, _stream_ptr(stream)), "gnnco_block_norm_backward")
+        return dict(dx=dx, dy=dy, dgate=dgate, dw_pre=dw_pre, dw_post=dw_post)
+
+    def _muon_call(self, shape, active, stream, ws):
+        import torch
+        sets, r, c = (int(v) for v in shape)
+        if active is not None:
+            _require(active, torch.uint8, "active")
+            if tuple(active.shape) != (sets,) or active.device != self.device:
+                raise ValueError("active must be [sets]")
+        need = _sz(0)
+        _check(self._lib.gnnco_muon_workspace_bytes(self._handle, sets, r, c, ctypes.byref(need)),
+               "gnnco_muon_workspace_bytes")
+        if ws is None:
+            ws = _empty(max(256, need.value), torch.uint8, self.device, stream)
+        return sets, r, c, ws
+
+    def muon_update(self, W, m, dW, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True,
+                    weight_decay: float = 0.0, steps: int = 5, coefs: Sequence[float] = MUON_COEFS, eps: float = 1e-7,
+                    active=None, ws=None, stream=None):
+        """``gnnco_muon_update``: one orthogonalised update of ``W`` [sets, d_in, d_out] (float32, in place) with the
+        gradient ``dW`` and the momentum ``m`` (in place); ``active`` uint8 [sets] restricts it.  ``ws`` may be a
+        uint8 tensor kept between calls."""
+        import torch
+        for t, what in ((W, "W"), (m, "m"), (dW, "dW")):
+            _require(t, torch.float32, what)
+            if t.dim() != 3 or t.shape != W.shape or t.device != self.device:
+                raise ValueError("W, m and dW must be [sets, d_in, d_out] on %s" % self.device)
+        sets, r, c, ws = self._muon_call(W.shape, active, stream, ws)
+        p = MuonParams(lr, momentum, weight_decay, int(nesterov), steps, coefs[0], coefs[1], coefs[2], eps, _dptr(active))
+        _check(self._lib.gnnco_muon_update(self._handle, sets, r, c, W.data_ptr(), m.data_ptr(), dW.data_ptr(),
+                                           ctypes.byref(p), ws.data_ptr(), ws.numel(), _stream_ptr(stream)),
+               "gnnco_muon_update")
+        return W
+
+    def muon_step(self, model: Model, opt: Muon, dW: Sequence, stream=None) -> None:
+        """One ``muon_update`` of every layer of ``model`` with the gradients ``dW`` of a training step."""
+        for W, m, g in zip(model.W, opt.m, dW):
+            self.muon_update(W, m, g, opt.lr, opt.momentum, opt.nesterov, opt.weight_decay, opt.steps, opt.coefs, opt.eps,
+                             opt.active, stream=stream)
+
+    def orthogonalise(self, G, out=None, out_dtype=None, steps: int = 5, coefs: Sequence[float] = MUON_COEFS,
+                      eps: float = 1e-7, active=None, ws=None, stream=None):
+        """``gnnco_orthogonalise``: the Newton-Schulz iterate of every matrix of ``G`` [sets, rows, cols] (float32 or
+        bfloat16)."""
+        gd = _feat_code(G, "G")
+        _require(G, G.dtype, "G")
+        if G.dim() != 3 or 0 in G.shape or G.device != self.device:
+            raise ValueError("G must be [sets, rows, cols] on %s" % self.device)
+        if out is None:
+            out = _empty(tuple(G.shape), out_dtype or G.dtype, self.device, stream)
+        od = _feat_code(out, "out")
+        _require(out, out.dtype, "out")
+        if out.shape != G.shape or out.device != self.device:
+            raise ValueError("out must have the shape of G")
+        sets, r, c, ws = self._muon_call(G.shape, active, stream, ws)
+        p = MuonParams(0.0, 0.0, 0.0, 0, steps, coefs[0], coefs[1], coefs[2], eps, _dptr(active))
+        _check(self._lib.gnnco_orthogonalise(self._handle, gd, od, sets, r, c, G.data_ptr(), out.data_ptr(),
+                                             ctypes.byref(p), ws.data_ptr(), ws.numel(), _stream_ptr(stream)),
+               "gnnco_orthogonalise")
+        return out
 
     def objective_static(self, p, alpha: float, beta: float, lam: float = 0.0, pen=None, loss=None, stream=None):
         """``gnnco_objective_static``: per-subgraph objective of given probabilities, with no

@@ -10,7 +10,7 @@
 // value of u towards 1 and leaves the singular vectors alone.
 #include <math.h>
 
-#include "internal.cuh"
+#include "muon_internal.cuh"
 #include "vec_io.cuh"
 
 namespace {
@@ -139,18 +139,26 @@ __global__ void __launch_bounds__(256) muon_finish(const float* __restrict__ X, 
 struct NsLayout {
   float *x0, *x1, *a, *p;
   double* partial;
+  void* scratch;                                           // of the on-chip kernel, where that one runs
+  bool on_chip;
   int64_t chunk;                                           // matrices worked on at a time
   size_t bytes;
 };
-NsLayout ns_layout(void* ws, int64_t sets, int64_t r, int64_t c) {
-  const int64_t k = r < c ? r : c;
-  NsLayout L;
+NsLayout ns_layout(const gnnco_handle* h, void* ws, int64_t sets, int64_t r, int64_t c) {
+  const int64_t k = r < c ? r : c, n = r < c ? c : r;
+  NsLayout L = {};
+  Carver cv(ws, 0);
+  L.on_chip = ns_on_chip_supported(h, (int32_t)k, (int32_t)n);
+  if (L.on_chip) {
+    L.scratch = cv.take<char>(ns_on_chip_scratch_bytes(h, sets, (int32_t)k, (int32_t)n));
+    L.bytes = cv.off;
+    return L;
+  }
   const int64_t each = (2 * r * c + 2 * k * k) * 4;
   L.chunk = ((int64_t)256 << 20) / each;
   if (L.chunk < 1) L.chunk = 1;
   if (L.chunk > sets) L.chunk = sets;
   if (L.chunk > 32768) L.chunk = 32768;
-  Carver cv(ws, 0);
   L.x0 = cv.take<float>(L.chunk * r * c);
   L.x1 = cv.take<float>(L.chunk * r * c);
   L.a = cv.take<float>(L.chunk * k * k);
@@ -165,26 +173,44 @@ bool valid_sizes(int64_t sets, int32_t r, int32_t c) {
 }
 
 // The iteration must stay bounded on [0, 1], where the singular values start; what it reaches there also bounds every
-// intermediate value.  Sampled densely; a coefficient set whose values grow past 2 is refused.
-bool coefficients_bounded(float a, float b, float c, int steps) {
+// intermediate value.  Sampled densely; a coefficient set whose values grow past 2 is refused.  *p_max: the largest
+// |a + b s^2 + c s^4| over the values reached.
+bool coefficients_bounded(float a, float b, float c, int steps, double* p_max) {
+  double top = 1.0;
   for (int q = 0; q <= 4096; ++q) {
     double s = q / 4096.0;
     for (int t = 0; t < steps; ++t) {
       const double s2 = s * s;
       s = s * (a + s2 * (b + s2 * (double)c));
       if (!(fabs(s) <= 2.0)) return false;
+      if (fabs(s) > top) top = fabs(s);
     }
+  }
+  *p_max = 0.0;
+  for (int q = 0; q <= 4096; ++q) {
+    const double s = top * q / 4096.0, s2 = s * s, p = fabs(a + s2 * (b + s2 * (double)c));
+    if (p > *p_max) *p_max = p;
   }
   return true;
 }
 
-struct NsParams { int steps; float a, b, c, eps; };
+struct NsParams { int steps; float a, b, c, eps; float p_scale; };
 
 template <typename TG, typename TO>
 int32_t run_ns(gnnco_handle* h, int64_t sets, int32_t r, int32_t c, const TG* G, float* m, float* W, TO* O, float mu, int nesterov,
                float keep, float step, const uint8_t* active, const NsParams& P, const NsLayout& L, cudaStream_t st) {
   const bool tr = r > c;
   const int32_t k = tr ? c : r, n = tr ? r : c, count = r * c;
+  if (L.on_chip) {
+    NsJob J = {};
+    J.G = G; J.m = m; J.W = W; J.O = O; J.active = active; J.sets = sets;
+    J.r = r; J.c = c; J.k = k; J.n = n;
+    J.g_bf16 = sizeof(TG) == 2; J.o_bf16 = sizeof(TO) == 2; J.transpose = tr; J.nesterov = nesterov; J.steps = P.steps;
+    J.vec4 = !tr && c % 4 == 0 && sizeof(TG) == 4 && vec_ok(G, c, 4, 4) && (!m || vec_ok(m, c, 4, 4));
+    J.mu = mu; J.keep = keep; J.step = step; J.eps = P.eps; J.a = P.a; J.b = P.b; J.cc = P.c; J.p_scale = P.p_scale;
+    J.scratch = L.scratch; J.status = h->status;
+    return launch_ns_on_chip(h, J, st);
+  }
   int parts = (count + 4095) / 4096;
   if (parts > kPartials) parts = kPartials;
   for (int64_t s0 = 0; s0 < sets; s0 += L.chunk) {
@@ -206,26 +232,31 @@ int32_t run_ns(gnnco_handle* h, int64_t sets, int32_t r, int32_t c, const TG* G,
   return GNNCO_OK;
 }
 
-int32_t check_params(const NsParams& P) {
+int32_t check_params(NsParams& P) {
   if (P.steps < 1 || P.steps > 32 || !(P.eps > 0.0f)) return GNNCO_INVALID_ARGUMENT;
-  return coefficients_bounded(P.a, P.b, P.c, P.steps) ? GNNCO_OK : GNNCO_INVALID_ARGUMENT;
+  double p_max = 0.0;
+  if (!coefficients_bounded(P.a, P.b, P.c, P.steps, &p_max)) return GNNCO_INVALID_ARGUMENT;
+  // entries of P stay below 2^15 in float16
+  P.p_scale = 16384.0f;
+  while (P.p_scale * p_max > 32768.0) P.p_scale *= 0.5f;
+  return GNNCO_OK;
 }
 
 }  // namespace
 
 extern "C" int32_t gnnco_muon_workspace_bytes(const gnnco_handle* h, int64_t sets, int32_t rows, int32_t cols, size_t* bytes) {
   if (!h || !bytes || !valid_sizes(sets, rows, cols)) return GNNCO_INVALID_ARGUMENT;
-  *bytes = ns_layout(nullptr, sets, rows, cols).bytes;
+  *bytes = ns_layout(h, nullptr, sets, rows, cols).bytes;
   return GNNCO_OK;
 }
 
 extern "C" int32_t gnnco_muon_update(gnnco_handle* h, int64_t sets, int32_t rows, int32_t cols, float* W, float* m, const float* dW,
                                      const gnnco_muon_params* p, void* ws, size_t ws_bytes, void* stream) {
   if (!h || !W || !m || !dW || !p || !ws || ((uintptr_t)ws & 255) || !valid_sizes(sets, rows, cols)) return GNNCO_INVALID_ARGUMENT;
-  const NsParams P{p->steps, p->a, p->b, p->c, p->eps};
+  NsParams P{p->steps, p->a, p->b, p->c, p->eps, 1.0f};
   const int32_t rc = check_params(P);
   if (rc != GNNCO_OK) return rc;
-  const NsLayout L = ns_layout(ws, sets, rows, cols);
+  const NsLayout L = ns_layout(h, ws, sets, rows, cols);
   if (ws_bytes < L.bytes) return GNNCO_WORKSPACE_TOO_SMALL;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   ProfScope prof_(h, K_MUON, st);
@@ -243,10 +274,10 @@ extern "C" int32_t gnnco_orthogonalise(gnnco_handle* h, int32_t in_dtype, int32_
   if (!h || !G || !O || !p || !ws || ((uintptr_t)ws & 255) || !valid_sizes(sets, rows, cols)) return GNNCO_INVALID_ARGUMENT;
   if ((in_dtype != GNNCO_F32 && in_dtype != GNNCO_BF16) || (out_dtype != GNNCO_F32 && out_dtype != GNNCO_BF16))
     return GNNCO_UNSUPPORTED;
-  const NsParams P{p->steps, p->a, p->b, p->c, p->eps};
+  NsParams P{p->steps, p->a, p->b, p->c, p->eps, 1.0f};
   const int32_t rc = check_params(P);
   if (rc != GNNCO_OK) return rc;
-  const NsLayout L = ns_layout(ws, sets, rows, cols);
+  const NsLayout L = ns_layout(h, ws, sets, rows, cols);
   if (ws_bytes < L.bytes) return GNNCO_WORKSPACE_TOO_SMALL;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   ProfScope prof_(h, K_MUON, st);

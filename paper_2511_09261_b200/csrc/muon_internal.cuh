@@ -1,0 +1,24 @@
+// What the two halves of the orthogonalised update share (muon.cu: any size; muon_tc.cu: matrices that stay on chip).
+#pragma once
+
+#include "internal.cuh"
+
+struct NsJob {
+  const void* G;              // gradient (or the matrix to orthogonalise), [sets x r x c]
+  float *m, *W;               // momentum and weights, or NULL: write the iterate to O
+  void* O;
+  const uint8_t* active;
+  int64_t sets;
+  int32_t r, c, k, n;         // X is k x n, k <= n
+  int32_t g_bf16, o_bf16, transpose, nesterov, steps, vec4;
+  float mu, keep, step, eps;  // W = W * keep - step * X
+  float a, b, cc;             // the polynomial's coefficients
+  float p_scale;              // power of two that P = a I + b A + c A^2 is held at in float16
+  void* scratch;
+  int32_t* status;
+};
+
+// ---- muon_tc.cu: whole iterations on chip for k, n <= 256
+bool ns_on_chip_supported(const gnnco_handle* h, int32_t k, int32_t n);
+size_t ns_on_chip_scratch_bytes(const gnnco_handle* h, int64_t sets, int32_t k, int32_t n);
+int32_t launch_ns_on_chip(gnnco_handle* h, const NsJob& job, cudaStream_t st);

@@ -7,10 +7,10 @@
 //   X' = P X         P = a I + b A + c A A from tensor memory, X from shared memory (n-major: the same bytes)
 //
 // Accuracy.  Operands are float16 pairs (limbs): x = hi + lo with hi = fl16(x), lo = fl16(x - hi), 22 bits together, at
-// power-of-two scales that keep hi in range and lo normal; a product is hi hi + hi lo + lo hi (the dropped lo lo is
+// power-of-two scales that keep hi in range and lo's last bit small; a product is hi hi + hi lo + lo hi (the dropped lo lo is
 // 2^-24 of it) summed in the float32 accumulator.  The tensor core drops the bits below the accumulator's last place at
 // every instruction, so the small products of all k come first and the large ones meet the accumulator only k / 16
-// times (error of a 256 x 256 iterate after 5 steps: 8.1e-6 interleaved; see below for this order).  That is float32
+// times (error of a 256 x 256 iterate after 5 steps: 3.8e-6, 8.0e-6 when interleaved).  That is float32
 // accuracy at a third of the float16 rate; one float16 or bfloat16 product would put 2e-3 (1.5e-2) into the result, because errors in the direction of small singular values
 // grow by a = 3.4 per step.
 //
@@ -25,7 +25,7 @@
 // A and A A are worked on.  A's low limb does not fit next to X as a whole: its second half follows into the room of the
 // first as soon as the products that read the first are done (they are issued first).
 //
-// Roles: warp 16 issues MMAs and the exchange; warps 0-15 load, convert and store: warp w owns rows 32 (w % 4) .. +32 (its TMEM
+// Roles: warp 16 issues MMAs; warp 17 exchanges blocks and prefetches the next matrix into L2; warps 0-15 load, convert and store: warp w owns rows 32 (w % 4) .. +32 (its TMEM
 // lanes) and the 32-column items w / 4 and w / 4 + 4.  Barriers per 64-column panel let the next product start on the
 // first panels while the others are converted.  Every wait is bounded; a CTA that gives up raises the status word.
 #include <cuda_fp16.h>
@@ -37,10 +37,8 @@
 
 namespace {
 
-constexpr int kWorkWarps = 16, kThreads = 32 * (kWorkWarps + 1);
+constexpr int kWorkWarps = 16, kMmaWarp = 16, kSideWarp = 17, kThreads = 32 * (kWorkWarps + 2);
 constexpr uint32_t kPanel = 16384;                         // 128 rows x 64 float16
-constexpr float kXScale = 16384.0f;                        // |X| <= 2 on entry and by the bound on the coefficients
-constexpr float kAScale = 8192.0f;                         // |A| <= 4
 
 template <bool PAIR>
 struct Cfg {
@@ -58,8 +56,9 @@ struct Bars {
   uint64_t x[4], a[4], p[4];                               // panel ready (used in the even CTA)
   uint64_t m1, m2, m3, lofree;                             // products done (both CTAs)
   uint64_t l;                                              // second half of A's low limb ready (even CTA)
+  uint64_t own;                                            // this CTA's off-diagonal block written (by its workers)
   uint64_t g, s, s2;                                       // partner's block in scratch / copied here / copied there
-  uint64_t norm, norm2, loaded;                            // loader: sums ready, partner's sum ready, X written
+  uint64_t norm, norm2, again, loaded;                     // loader: sums ready, partner's sum ready, sums read, X written
 };
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
@@ -68,20 +67,40 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   return r;
 }
 __device__ __forceinline__ float2 unpack_f16(uint32_t v) { return __half22float2(*reinterpret_cast<__half2*>(&v)); }
-// x, y -> packed high limbs and packed low limbs
+// x, y -> packed high limbs and packed low limbs (x - hi in one mixed-precision operation per value)
 __device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t& lo) {
   hi = pack_f16(x, y);
-  const float2 f = unpack_f16(hi);
-  lo = pack_f16(x - f.x, y - f.y);
+  float a, b;
+  asm("{\n\t.reg .b16 h0, h1, minus_one;\n\tmov.b32 {h0, h1}, %2;\n\tmov.b16 minus_one, 0xBC00;\n\t"
+      "fma.rn.f32.f16 %0, h0, minus_one, %3;\n\tfma.rn.f32.f16 %1, h1, minus_one, %4;\n\t}"
+      : "=f"(a), "=f"(b) : "r"(hi), "f"(x), "f"(y));
+  lo = pack_f16(a, b);
+}
+// packed limbs -> the two values
+__device__ __forceinline__ float2 join2(uint32_t hi, uint32_t lo) {
+  const float2 h = unpack_f16(hi);
+  float2 v;
+  asm("{\n\t.reg .b16 l0, l1;\n\tmov.b32 {l0, l1}, %2;\n\tadd.rn.f32.f16 %0, l0, %3;\n\tadd.rn.f32.f16 %1, l1, %4;\n\t}"
+      : "=f"(v.x), "=f"(v.y) : "r"(lo), "f"(h.x), "f"(h.y));
+  return v;
+}
+__device__ __forceinline__ void st_shared8(uint32_t saddr, uint32_t a, uint32_t b) {
+  asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(saddr), "r"(a), "r"(b) : "memory");
+}
+__device__ __forceinline__ float2 ld_shared8(uint32_t saddr) {
+  float2 v;
+  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(saddr) : "memory");
+  return v;
 }
 // row r, 16-byte chunk c of a panel
 __device__ __forceinline__ uint32_t at_chunk(int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); }
 
-template <bool PAIR>
+// CLUSTER: what the other CTA of the pair wrote before it arrived is visible afterwards
 struct Waiter {
   volatile uint32_t* abort_flag;
-  __device__ __forceinline__ bool operator()(uint64_t* bar, uint32_t parity) const {
-    auto ready = [&]() { return PAIR ? tc::mbar_try_wait_cluster(bar, parity) : tc::mbar_try_wait(bar, parity); };
+  template <bool CLUSTER = false>
+  __device__ __forceinline__ bool on(uint64_t* bar, uint32_t parity) const {
+    auto ready = [&]() { return CLUSTER ? tc::mbar_try_wait_cluster(bar, parity) : tc::mbar_try_wait(bar, parity); };
     if (ready()) return true;
     const long long t0 = clock64();
     while (!ready()) {
@@ -95,7 +114,8 @@ struct Waiter {
   }
 };
 
-template <bool PAIR>
+// VEC4: float32 matrices whose rows are X's rows and multiples of 16 bytes; else any type, order and alignment.
+template <bool PAIR, bool VEC4>
 __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
   using C = Cfg<PAIR>;
   extern __shared__ uint8_t smem_raw[];
@@ -105,7 +125,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
   Bars* B = reinterpret_cast<Bars*>(gen + C::X_BYTES + C::A_BYTES);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(B + 1);
   volatile uint32_t* abort_flag = tmem_slot + 1;
-  double* sums = reinterpret_cast<double*>(gen + C::X_BYTES + C::A_BYTES + 512);   // [16] own warps, [16 + rank] per CTA
+  double* sums = reinterpret_cast<double*>(gen + C::X_BYTES + C::A_BYTES + 512);   // [16] own warps, [2] the partner's total
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = PAIR ? tc::cluster_ctarank() : 0u;
@@ -113,7 +133,9 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
   const int kc = (J.k + 15) / 16 * 16, nc = (J.n + 15) / 16 * 16;   // contraction lengths
   const int a_items = (kc + 31) / 32, x_items = (nc + 31) / 32;     // 32-column items of A / P and of X
   const int quarters = PAIR ? 4 : (J.k + 31) / 32;                  // row quarters that hold anything
-  const Waiter<PAIR> wait{abort_flag};
+  const Waiter waiter{abort_flag};
+  auto wait = [&](uint64_t* bar, uint32_t parity) { return waiter.on<false>(bar, parity); };
+  auto wait_both = [&](uint64_t* bar, uint32_t parity) { return waiter.on<PAIR>(bar, parity); };
 
   if (threadIdx.x == 0) {
     auto panel_items = [](int items, int p) { const int left = items - 2 * p; return left <= 0 ? 1 : left >= 2 ? 2 : left; };
@@ -124,11 +146,11 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
     }
     tc::mbar_init(&B->m1, 1); tc::mbar_init(&B->m2, 1); tc::mbar_init(&B->m3, 1); tc::mbar_init(&B->lofree, 1);
     tc::mbar_init(&B->l, 4 * (a_items > 4 ? a_items - 4 : 1) * C::CTAS);
-    // items of the partner's off-diagonal half: the odd CTA receives the even one's upper columns and vice versa
-    const int off_items = rank == 1 ? (x_items > 4 ? x_items - 4 : 1) : 4;
-    tc::mbar_init(&B->g, 4 * off_items);
+    // items of the off-diagonal half that this CTA writes: the upper columns in the even CTA, the lower ones in the odd
+    tc::mbar_init(&B->own, 4 * (rank == 0 ? (x_items > 4 ? x_items - 4 : 1) : 4));
+    tc::mbar_init(&B->g, 1);
     tc::mbar_init(&B->s, 1); tc::mbar_init(&B->s2, 1);
-    tc::mbar_init(&B->norm, kWorkWarps); tc::mbar_init(&B->norm2, 1); tc::mbar_init(&B->loaded, kWorkWarps);
+    tc::mbar_init(&B->norm, kWorkWarps); tc::mbar_init(&B->norm2, 1); tc::mbar_init(&B->again, kWorkWarps); tc::mbar_init(&B->loaded, kWorkWarps);
     *abort_flag = 0;
     tc::fence_mbar_init();
   }
@@ -144,102 +166,166 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
   // the exchange scratch of this pair: [CTA][limb][2 panels]
   uint8_t* const scratch = PAIR ? static_cast<uint8_t*>(J.scratch) + group * (2 * 4 * (int64_t)kPanel) : nullptr;
 
-  if (warp == kWorkWarps) {
-    // ------------------------------------------------------------------------------ MMA issue, exchange
-    if (lane == 0) {
+  if (warp == kMmaWarp) {
+    // ------------------------------------------------------------------------------ MMA issue
+    {
+      // the whole warp takes every step together (see mma_f16); one lane issues
+      const uint32_t leader = tc::elect_one();
+      auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, waiter.on<false>(bar, parity)) != 0; };
+      auto wait_both = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, waiter.on<PAIR>(bar, parity)) != 0; };
       const uint32_t i1 = tc::idesc_f16_f32(PAIR ? 256 : 128, PAIR ? 256 : kc, false);
       const uint32_t i3 = tc::idesc_f16_f32(PAIR ? 256 : 128, PAIR ? 256 : nc, true);
       auto commit = [&](uint64_t* bar) {
-        if constexpr (PAIR) tc::mma_commit_pair(bar, 3);
-        else tc::mma_commit(bar);
+        if (leader) {
+          if constexpr (PAIR) tc::mma_commit_pair(bar, 3);
+          else tc::mma_commit(bar);
+        }
+        __syncwarp();
       };
-      auto left = [&](int t, int limb) { return (uint64_t)(tmem + C::ACC1 + (t >> 1) * 32 + (t & 1) * 8 + limb * 16); };
-      auto kmajor = [&](uint32_t base, int t) { return tc::smem_desc_sw128(base + (t >> 2) * kPanel + (t & 3) * 32, 16, 1024); };
-      // rows 16 t .. of X: in a pair rows 128 .. are in panels 2 and 3
-      auto nmajor = [&](uint32_t base, int t) {
-        const uint32_t off = PAIR ? (uint32_t)(t >> 3) * 2 * kPanel + (uint32_t)(t & 7) * 2048u : (uint32_t)t * 2048u;
-        return tc::smem_desc_sw128(base + off, kPanel, 1024);
+      // Everything a product needs is a base plus constants, so that an MMA costs the issuing thread a few instructions:
+      // 16 of k are 32 bytes of a k-major row, 2,048 bytes of n-major rows and 8 columns of tensor memory.
+      const uint64_t xh = tc::smem_desc_sw128(sX, 16, 1024), xl = tc::smem_desc_sw128(sX + 4 * kPanel, 16, 1024);
+      const uint64_t ah = tc::smem_desc_sw128(sA, 16, 1024), al = tc::smem_desc_sw128(sA + C::A_HI * kPanel, 16, 1024);
+      const uint64_t nh = tc::smem_desc_sw128(sX, kPanel, 1024), nl = tc::smem_desc_sw128(sX + 4 * kPanel, kPanel, 1024);
+      constexpr uint64_t kDescPanel = kPanel >> 4;
+      auto n_off = [](int p) {                             // rows 64 p .. of X: in a pair rows 128 .. are in panels 2 and 3
+        return (uint64_t)((PAIR ? (p >> 1) * 2 * kPanel + (p & 1) * 8192u : (uint32_t)p * 8192u) >> 4);
       };
-      const uint32_t xh = sX, xl = sX + 4 * kPanel, ah = sA, al = sA + C::A_HI * kPanel;
       const int tk = kc / 16, tn = nc / 16;                // k-steps of 16
+      // k-steps of panel p: f(step inside the panel)
+      auto steps_of = [](int p, int t_end, auto f) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (4 * p + q < t_end) f(q);
+      };
+      const uint32_t tbase = __shfl_sync(0xffffffffu, tmem, 0);
+      const uint32_t acc1 = tbase + C::ACC1, acc2 = tbase + C::ACC2, acc3 = tbase + C::ACC3;
+      auto lefth = [&](int p, int q) { return (uint64_t)(acc1 + p * 64 + (q >> 1) * 32 + (q & 1) * 8); };
+      auto leftl = [&](int p, int q) { return lefth(p, q) + 16; };
       uint32_t it = 0;
-      for (int64_t s = group; s < J.sets && !*abort_flag; s += groups) {
+      for (int64_t s = group; s < J.sets; s += groups) {
         if (J.active && !J.active[s]) continue;
-        for (int step = 0; step < J.steps; ++step, ++it) {
+        bool ok = true;
+        for (int step = 0; step < J.steps && ok; ++step, ++it) {
           const uint32_t ph = it & 1;
-          if (rank == 0) {
-            for (int t = 0; t < tn; ++t) {                 // X X^T
-              if ((t & 3) == 0) {
-                if (!wait(&B->x[t >> 2], ph)) break;
-                tc::tc_fence_after_sync();
-              }
-              tc::mma_f16<PAIR, false>(tmem + C::ACC1, kmajor(xh, t), kmajor(xl, t), i1, t != 0);
-              tc::mma_f16<PAIR, false>(tmem + C::ACC1, kmajor(xl, t), kmajor(xh, t), i1, true);
+          if (rank == 0) {                                 // X X^T
+            for (int p = 0; 4 * p < tn && ok; ++p) {
+              ok = wait_both(&B->x[p], ph);
+              tc::tc_fence_after_sync();
+              if (ok) steps_of(p, tn, [&](int q) {
+                const uint64_t o = p * kDescPanel + 2 * q;
+                tc::mma_f16<PAIR, false>(leader, acc1, xh + o, xl + o, i1, p + q != 0);
+                tc::mma_f16<PAIR, false>(leader, acc1, xl + o, xh + o, i1, true);
+              });
             }
-            for (int t = 0; t < tn; ++t) tc::mma_f16<PAIR, false>(tmem + C::ACC1, kmajor(xh, t), kmajor(xh, t), i1, true);
+            if (!ok) break;
+            for (int p = 0; 4 * p < tn; ++p)
+              steps_of(p, tn, [&](int q) {
+                const uint64_t o = p * kDescPanel + 2 * q;
+                tc::mma_f16<PAIR, false>(leader, acc1, xh + o, xh + o, i1, true);
+              });
             commit(&B->m1);
           }
-          if constexpr (PAIR) {
-            // X X^T has read the rows; the off-diagonal block gives way to the partner's
-            if (!wait(&B->m1, ph) || !wait(&B->g, ph)) break;
-            tc::fence_proxy_async_all();
-            tc::mbar_arrive_expect_tx(&B->s, 4 * kPanel);
-            const uint8_t* from = scratch + (rank ^ 1u) * 4 * kPanel;
-            for (int limb = 0; limb < 2; ++limb)
-              tc::bulk_load((limb ? xl : xh) + (rank == 0 ? 2 : 0) * kPanel, from + limb * 2 * kPanel, 2 * kPanel, &B->s);
-            if (rank == 1) {
-              if (!wait(&B->s, ph)) break;
-              tc::mbar_arrive_release_cluster(tc::map_to_cta(tc::smem_u32(&B->s2), 0));
-            }
-          }
           if (rank == 0) {
-            bool ok = true;                                // A A
-            if constexpr (PAIR) {
-              for (int t = 0; t < 8 && ok; ++t) {          // what reads the first half of A's low limb comes first
-                if ((t & 3) == 0) {
-                  ok = wait(&B->a[t >> 2], ph);
-                  tc::tc_fence_after_sync();
-                }
-                if (ok) tc::mma_f16<true, true>(tmem + C::ACC2, left(t, 0), kmajor(al, t), i1, t != 0);
+            if constexpr (PAIR) {                          // A A: what reads the first half of A's low limb comes first
+              for (int p = 0; p < 2 && ok; ++p) {
+                ok = wait_both(&B->a[p], ph);
+                tc::tc_fence_after_sync();
+                if (ok) steps_of(p, 8, [&](int q) { tc::mma_f16<true, true>(leader, acc2, lefth(p, q), al + p * kDescPanel + 2 * q, i1, p + q != 0); });
               }
               if (!ok) break;
               commit(&B->lofree);
             }
-            for (int t = 0; t < tk && ok; ++t) {
-              if ((t & 3) == 0 && !(PAIR && t < 8)) {
-                ok = wait(&B->a[t >> 2], ph);
+            for (int p = 0; 4 * p < tk && ok; ++p) {
+              if (!PAIR || p >= 2) {
+                ok = wait_both(&B->a[p], ph);
                 tc::tc_fence_after_sync();
               }
-              if (!ok) break;
-              tc::mma_f16<PAIR, true>(tmem + C::ACC2, left(t, 1), kmajor(ah, t), i1, PAIR || t != 0);
-              if constexpr (!PAIR) tc::mma_f16<PAIR, true>(tmem + C::ACC2, left(t, 0), kmajor(al, t), i1, true);
+              if (ok) steps_of(p, tk, [&](int q) {
+                const uint64_t o = p * kDescPanel + 2 * q;
+                tc::mma_f16<PAIR, true>(leader, acc2, leftl(p, q), ah + o, i1, PAIR || p + q != 0);
+                if constexpr (!PAIR) tc::mma_f16<PAIR, true>(leader, acc2, lefth(p, q), al + o, i1, true);
+              });
             }
             if constexpr (PAIR) {
-              if (!ok || !wait(&B->l, ph)) break;
+              ok = ok && wait_both(&B->l, ph);
               tc::tc_fence_after_sync();
-              for (int t = 8; t < tk; ++t) tc::mma_f16<true, true>(tmem + C::ACC2, left(t, 0), kmajor(al, t - 8), i1, true);
+              for (int p = 2; 4 * p < tk && ok; ++p)
+                steps_of(p, tk, [&](int q) { tc::mma_f16<true, true>(leader, acc2, lefth(p, q), al + (p - 2) * kDescPanel + 2 * q, i1, true); });
             }
-            for (int t = 0; t < tk && ok; ++t) tc::mma_f16<PAIR, true>(tmem + C::ACC2, left(t, 0), kmajor(ah, t), i1, true);
             if (!ok) break;
+            for (int p = 0; 4 * p < tk; ++p)
+              steps_of(p, tk, [&](int q) { tc::mma_f16<PAIR, true>(leader, acc2, lefth(p, q), ah + p * kDescPanel + 2 * q, i1, true); });
             commit(&B->m2);
             // P X.  In a pair the accumulator is the one A A is read from: all of P must be there.
             if constexpr (PAIR) {
-              for (int p = 0; 64 * p < kc; ++p) ok = ok && wait(&B->p[p], ph);
-              ok = ok && wait(&B->s, ph) && wait(&B->s2, ph);
+              for (int p = 0; 4 * p < tk; ++p) ok = ok && wait_both(&B->p[p], ph);
+              ok = ok && wait(&B->s, ph) && wait_both(&B->s2, ph);
               tc::tc_fence_after_sync();
             }
-            for (int t = 0; t < tk && ok; ++t) {
-              if (!PAIR && (t & 3) == 0) {
-                ok = wait(&B->p[t >> 2], ph);
+            for (int p = 0; 4 * p < tk && ok; ++p) {
+              if (!PAIR) {
+                ok = wait(&B->p[p], ph);
                 tc::tc_fence_after_sync();
-                if (!ok) break;
               }
-              tc::mma_f16<PAIR, true>(tmem + C::ACC3, left(t, 0), nmajor(xl, t), i3, t != 0);
-              tc::mma_f16<PAIR, true>(tmem + C::ACC3, left(t, 1), nmajor(xh, t), i3, true);
+              if (ok) steps_of(p, tk, [&](int q) {
+                const uint64_t o = n_off(p) + 128 * q;
+                tc::mma_f16<PAIR, true>(leader, acc3, lefth(p, q), nl + o, i3, p + q != 0);
+                tc::mma_f16<PAIR, true>(leader, acc3, leftl(p, q), nh + o, i3, true);
+              });
             }
-            for (int t = 0; t < tk && ok; ++t) tc::mma_f16<PAIR, true>(tmem + C::ACC3, left(t, 0), nmajor(xh, t), i3, true);
             if (!ok) break;
+            for (int p = 0; 4 * p < tk; ++p)
+              steps_of(p, tk, [&](int q) { tc::mma_f16<PAIR, true>(leader, acc3, lefth(p, q), nh + n_off(p) + 128 * q, i3, true); });
             commit(&B->m3);
+          }
+        }
+        if (!ok) break;
+      }
+    }
+    __syncwarp();
+  } else if (warp == kSideWarp) {
+    // ------------------------------------------------------------------------------ exchange, prefetch
+    if (lane == 0) {
+      uint32_t it = 0;
+      bool ok = true;
+      for (int64_t s = group; s < J.sets && ok; s += groups) {
+        if (J.active && !J.active[s]) continue;
+        for (int step = 0; step < J.steps && ok; ++step, ++it) {
+          const uint32_t ph = it & 1;
+          if (!PAIR && !(ok = wait(&B->m1, ph))) break;
+          if (step == J.steps - 1 && J.prefetch) {
+            // the last step has begun: its weights and the next matrix are brought into L2 meanwhile (each CTA of a pair:
+            // its half of the bytes; earlier, the lines of all CTAs together would not survive in L2)
+            const int64_t bytes = (int64_t)J.r * J.c * 4, cut = bytes / 32 * 16;
+            const int64_t lo = PAIR && rank == 1 ? cut : 0, hi = PAIR && rank == 0 ? cut : bytes;
+            auto fetch = [&](const void* array, int64_t set) {
+              for (int64_t at = lo; array && at < hi; at += 16384)
+                tc::prefetch_l2(static_cast<const char*>(array) + set * bytes + at, (uint32_t)(hi - at < 16384 ? hi - at : 16384));
+            };
+            fetch(J.W, s);
+            const int64_t next = s + groups;
+            if (next < J.sets && !(J.active && !J.active[next])) {
+              fetch(J.G, next);
+              fetch(J.m, next);
+            }
+          }
+          if constexpr (PAIR) {
+            const uint32_t mine = (rank == 0 ? 2 : 0) * kPanel;           // the two panels that change hands
+            if (!(ok = wait(&B->own, ph))) break;
+            for (int limb = 0; limb < 2; ++limb)
+              tc::bulk_store(scratch + (rank * 2 + limb) * 2 * kPanel, sX + limb * 4 * kPanel + mine, 2 * kPanel);
+            tc::bulk_store_wait();
+            tc::fence_proxy_async_all();
+            tc::mbar_arrive_release_cluster(tc::map_to_cta(tc::smem_u32(&B->g), rank ^ 1u));
+            // X X^T has read the rows: the block gives way to the partner's
+            if (!(ok = wait(&B->m1, ph) && wait_both(&B->g, ph))) break;
+            tc::fence_proxy_async_all();
+            tc::mbar_arrive_expect_tx(&B->s, 4 * kPanel);
+            for (int limb = 0; limb < 2; ++limb)
+              tc::bulk_load(sX + limb * 4 * kPanel + mine, scratch + ((rank ^ 1u) * 2 + limb) * 2 * kPanel, 2 * kPanel, &B->s);
+            if (!(ok = wait(&B->s, ph))) break;
+            if (rank == 1) tc::mbar_arrive_release_cluster(tc::map_to_cta(tc::smem_u32(&B->s2), 0));
           }
         }
       }
@@ -250,122 +336,167 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
     const int quarter = warp & 3, sub = warp >> 2;
     const int row = quarter * 32 + lane;                   // of this CTA's 128
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    const int grow = (int)rank * 128 + row;                // row of X
     const bool works = quarter < quarters;
     const int off_panel = rank == 0 ? 2 : 0;               // the two panels that the partner takes
     auto arrive = [&](uint64_t* bar) {                     // on the even CTA's barrier, by one lane, after __syncwarp
-      if constexpr (PAIR) tc::mbar_arrive_release_cluster(tc::map_to_cta(tc::smem_u32(bar), 0));
+      if constexpr (PAIR) tc::mbar_arrive_cluster(tc::map_to_cta(tc::smem_u32(bar), 0));
       else tc::mbar_arrive(bar);
     };
-    // the items of X that this warp owns are written: tell the issuer, and the partner about its share of the scratch
+    // an item of X is written: tell the issuer, and the side warp where the partner needs it
     auto x_ready = [&](int item) {
-      if (works && item < x_items && lane == 0) arrive(&B->x[item >> 1]);
+      if (!works || item >= x_items || lane != 0) return;
+      arrive(&B->x[item >> 1]);
+      if (PAIR && ((item >> 1) & 2) == off_panel) tc::mbar_arrive(&B->own);
     };
-    auto partner_ready = [&](int item) {
-      if (PAIR && item < x_items && ((item >> 1) & 2) == off_panel && lane == 0) {
-        __threadfence();
-        tc::mbar_arrive_release_cluster(tc::map_to_cta(tc::smem_u32(&B->g), rank ^ 1u));
-      }
+    // chunk: 8 columns, counted over the row
+    auto put_chunk = [&](int limb, int r, int chunk, const uint32_t* v) {
+      tc::st_shared16(sX + (limb * 4 + (chunk >> 3)) * kPanel + at_chunk(r, chunk & 7), v[0], v[1], v[2], v[3]);
     };
-    auto put_chunk = [&](int limb, int r, int chunk, uint32_t v0, uint32_t v1, uint32_t v2, uint32_t v3) {
-      // chunk: 8 columns, counted over the row
-      const int panel = chunk >> 3;
-      const uint32_t o = at_chunk(r, chunk & 7);
-      tc::st_shared16(sX + (limb * 4 + panel) * kPanel + o, v0, v1, v2, v3);
-      if (PAIR && (panel & 2) == off_panel)
-        *reinterpret_cast<uint4*>(scratch + rank * 4 * kPanel + (limb * 2 + (panel & 1)) * kPanel + o) = make_uint4(v0, v1, v2, v3);
+    // the loader's unit: 4 columns of a row, 8 bytes in each limb
+    auto unit_at = [&](int limb, int r, int unit) {
+      return sX + (limb * 4 + (unit >> 4)) * kPanel + at_chunk(r, (unit >> 1) & 7) + (unit & 1) * 8;
     };
-    const int cpr = (nc + 31) / 32 * 4;                    // chunks per row that are kept (whole items)
-    const int rows_kept = quarters * 32, total = rows_kept * cpr;
-    uint32_t it = 0, mat = 0;
+    const int upr = (nc + 31) / 32 * 8;                    // units per row that are kept (whole items)
+    const int rows_kept = quarters * 32, total = rows_kept * upr;
+    constexpr int kStride = 32 * kWorkWarps;
+    // units are dealt along the matrix' own rows, so that lanes read neighbouring addresses
+    const bool by_row = VEC4 || !J.transpose;
+    const int per = by_row ? upr : rows_kept, jump_a = kStride / per, jump_b = kStride - jump_a * per;
+    const int first_a = (int)threadIdx.x / per, first_b = (int)threadIdx.x - first_a * per;
+    auto next_unit = [&](int& a, int& b) {                 // kStride units on
+      a += jump_a;
+      b += jump_b;
+      if (b >= per) { b -= per; ++a; }
+    };
+    uint32_t it = 0, mat = 0, sum_it = 0, again_it = 0;
     for (int64_t s = group; s < J.sets && !*abort_flag; s += groups) {
       if (J.active && !J.active[s]) continue;
       const int64_t base = s * (int64_t)J.r * J.c;
-      // ---- momentum, u, |u|^2: eight chunks of eight columns per thread
-      float u[8][8];
+      const float* const Gs = static_cast<const float*>(J.G) + base;
+      float* const Ms = J.m ? J.m + base : nullptr;
+      float* const Ws = J.W ? J.W + base : nullptr;
+      // the last matrix' values have left the room they were staged in
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&B->again);
+      if (!wait(&B->again, again_it++ & 1)) break;
+      // ---- momentum, u, |u|^2.  A unit (four columns of a row) of u waits as float32 in the two 8-byte places that its limbs
+      // will take; four units are asked for at a time.
       double sum = 0.0;
+      int ua = first_a, ub = first_b;
+      for (int q = threadIdx.x; q < total; q += 4 * kStride) {
+        float g[4][4], mv[4][4];
+        int at[4];                                         // unit's offset in the matrix, -1: outside
+        uint32_t place[4];                                 // ... and its place in the high limb
 #pragma unroll
-      for (int z = 0; z < 8; ++z) {
-        const int q = threadIdx.x + z * (32 * kWorkWarps);
-        int r, ch;
-        if (J.transpose) { ch = q / rows_kept; r = q - ch * rows_kept; }
-        else { r = q / cpr; ch = q - r * cpr; }
-        const int i = (int)rank * 128 + r, j0 = ch * 8;
-        const bool in = q < total && i < J.k && j0 < J.n;
-        if (in && J.vec4) {                                // four float32 columns at a time (rows are 16-byte aligned)
+        for (int y = 0; y < 4; ++y) {
+          const int r = by_row ? ua : ub, unit = by_row ? ub : ua;
+          next_unit(ua, ub);
+          const int i = (int)rank * 128 + r, j = unit * 4;
+          at[y] = q + y * kStride >= total || i >= J.k || j >= J.n ? -1 : by_row ? i * J.c + j : j * J.c + i;
+          place[y] = unit_at(0, r, unit);
 #pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            const int64_t at = base + (int64_t)i * J.c + j0 + 4 * hf;
-            float4 g = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            if (j0 + 4 * hf < J.n) {
-              g = __ldcs(reinterpret_cast<const float4*>(static_cast<const float*>(J.G) + at));
-              if (J.m) {
-                float4 mv = *reinterpret_cast<const float4*>(J.m + at);
-                mv.x = J.mu * mv.x + g.x; mv.y = J.mu * mv.y + g.y; mv.z = J.mu * mv.z + g.z; mv.w = J.mu * mv.w + g.w;
-                *reinterpret_cast<float4*>(J.m + at) = mv;
-                if (J.nesterov) { g.x += J.mu * mv.x; g.y += J.mu * mv.y; g.z += J.mu * mv.z; g.w += J.mu * mv.w; }
-                else g = mv;
-              }
+          for (int e = 0; e < 4; ++e) g[y][e] = mv[y][e] = 0.0f;
+          if (at[y] < 0) continue;
+          if constexpr (VEC4) {
+            const float4 a = __ldcs(reinterpret_cast<const float4*>(Gs + at[y]));
+            g[y][0] = a.x; g[y][1] = a.y; g[y][2] = a.z; g[y][3] = a.w;
+            if (Ms) {
+              const float4 b = __ldcs(reinterpret_cast<const float4*>(Ms + at[y]));
+              mv[y][0] = b.x; mv[y][1] = b.y; mv[y][2] = b.z; mv[y][3] = b.w;
             }
-            u[z][4 * hf] = g.x; u[z][4 * hf + 1] = g.y; u[z][4 * hf + 2] = g.z; u[z][4 * hf + 3] = g.w;
-          }
-        } else {
+          } else {
+            const int hop = by_row ? 1 : J.c, have = J.n - j;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            float v = 0.0f;
-            if (in && j0 + e < J.n) {
-              const int64_t at = base + (J.transpose ? (int64_t)(j0 + e) * J.c + i : (int64_t)i * J.c + j0 + e);
-              v = J.g_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(J.G)[at]) : __ldcs(static_cast<const float*>(J.G) + at);
-              if (J.m) {
-                const float mv = J.mu * J.m[at] + v;
-                J.m[at] = mv;
-                v = J.nesterov ? v + J.mu * mv : mv;
+            for (int e = 0; e < 4; ++e)
+              if (e < have) {
+                g[y][e] = J.g_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(J.G)[base + at[y] + e * hop]) : __ldcs(Gs + at[y] + e * hop);
+                if (Ms) mv[y][e] = __ldcs(Ms + at[y] + e * hop);
               }
-            }
-            u[z][e] = v;
           }
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum += (double)u[z][e] * (double)u[z][e];
-      }
+        for (int y = 0; y < 4; ++y) {
+          if (q + y * kStride >= total) continue;
+          if (Ms && at[y] >= 0) {
 #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-      if (lane == 0) {
-        sums[warp] = sum;
-        tc::mbar_arrive(&B->norm);
+            for (int e = 0; e < 4; ++e) {
+              mv[y][e] = J.mu * mv[y][e] + g[y][e];
+              g[y][e] = J.nesterov ? g[y][e] + J.mu * mv[y][e] : mv[y][e];
+            }
+            if constexpr (VEC4) {
+              __stcs(reinterpret_cast<float4*>(Ms + at[y]), make_float4(mv[y][0], mv[y][1], mv[y][2], mv[y][3]));
+            } else {
+              const int hop = by_row ? 1 : J.c, have = J.n - (by_row ? at[y] % J.c : at[y] / J.c);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (e < have) __stcs(Ms + at[y] + e * hop, mv[y][e]);
+            }
+          }
+          // float32 squares of four values at a time, float64 across; the few matrices whose squares leave float32's range
+          // are summed again below
+          sum += (double)(g[y][0] * g[y][0] + g[y][1] * g[y][1] + g[y][2] * g[y][2] + g[y][3] * g[y][3]);
+          st_shared8(place[y], __float_as_uint(g[y][0]), __float_as_uint(g[y][1]));
+          st_shared8(place[y] + 4 * kPanel, __float_as_uint(g[y][2]), __float_as_uint(g[y][3]));
+        }
       }
-      if (!wait(&B->norm, mat & 1)) break;
       double norm2 = 0.0;
+      // own warps' sums in warp order, then the partner's (a + b = b + a: both CTAs get the same bits)
+      auto total_of = [&](double part) {
 #pragma unroll
-      for (int w = 0; w < kWorkWarps; ++w) norm2 += sums[w];
-      if constexpr (PAIR) {
-        if (threadIdx.x == 0) {
-          const uint32_t peer = tc::map_to_cta(tc::smem_u32(sums + 16), rank ^ 1u);
-          asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(peer), "d"(norm2) : "memory");
-          tc::mbar_arrive_release_cluster(tc::map_to_cta(tc::smem_u32(&B->norm2), rank ^ 1u));
+        for (int d = 16; d > 0; d >>= 1) part += __shfl_xor_sync(0xffffffffu, part, d);
+        if (lane == 0) {
+          sums[warp] = part;
+          tc::mbar_arrive(&B->norm);
         }
-        if (!wait(&B->norm2, mat & 1)) break;
-        norm2 += sums[16];                                 // a + b = b + a: both CTAs get the same bits
-      }
-      const float f = (float)(1.0 / (sqrt(norm2) + (double)J.eps));
+        if (!wait(&B->norm, sum_it & 1)) return false;
+        norm2 = 0.0;
 #pragma unroll
-      for (int z = 0; z < 8; ++z) {
-        const int q = threadIdx.x + z * (32 * kWorkWarps);
-        int r, ch;
-        if (J.transpose) { ch = q / rows_kept; r = q - ch * rows_kept; }
-        else { r = q / cpr; ch = q - r * cpr; }
-        if (q >= total) continue;
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) split2(u[z][2 * e] * f * kXScale, u[z][2 * e + 1] * f * kXScale, hi[e], lo[e]);
-        put_chunk(0, r, ch, hi[0], hi[1], hi[2], hi[3]);
-        put_chunk(1, r, ch, lo[0], lo[1], lo[2], lo[3]);
+        for (int w = 0; w < kWorkWarps; ++w) norm2 += sums[w];
+        if constexpr (PAIR) {
+          if (threadIdx.x == 0) {
+            const uint32_t peer = tc::map_to_cta(tc::smem_u32(sums + 16 + (sum_it & 1)), rank ^ 1u);
+            asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(peer), "d"(norm2) : "memory");
+            tc::mbar_arrive_release_cluster(tc::map_to_cta(tc::smem_u32(&B->norm2), rank ^ 1u));
+          }
+          if (!wait_both(&B->norm2, sum_it & 1)) return false;
+          norm2 += sums[16 + (sum_it & 1)];
+        }
+        ++sum_it;
+        return true;
+      };
+      if (!total_of(sum)) break;
+      if (!(norm2 > 1e-24 && norm2 < 1e37)) {              // the same decision everywhere
+        // everybody has read the sums of the first round before they are written again
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&B->again);
+        if (!wait(&B->again, again_it++ & 1)) break;
+        sum = 0.0;
+        int a2 = first_a, b2 = first_b;
+        for (int q = threadIdx.x; q < total; q += kStride, next_unit(a2, b2)) {
+          const uint32_t p = by_row ? unit_at(0, a2, b2) : unit_at(0, b2, a2);
+          const float2 x = ld_shared8(p), y = ld_shared8(p + 4 * kPanel);
+          sum += (double)x.x * x.x + (double)x.y * x.y + ((double)y.x * y.x + (double)y.y * y.y);
+        }
+        if (!total_of(sum)) break;
       }
-      tc::fence_proxy_async_all();
+      const float f = (float)((double)J.x_scale / (sqrt(norm2) + (double)J.eps));
+      ua = first_a;
+      ub = first_b;
+#pragma unroll 4
+      for (int q = threadIdx.x; q < total; q += kStride, next_unit(ua, ub)) {
+        const uint32_t p = by_row ? unit_at(0, ua, ub) : unit_at(0, ub, ua);
+        const float2 x = ld_shared8(p), y = ld_shared8(p + 4 * kPanel);
+        uint32_t hi[2], lo[2];
+        split2(x.x * f, x.y * f, hi[0], lo[0]);
+        split2(y.x * f, y.y * f, hi[1], lo[1]);
+        st_shared8(p, hi[0], hi[1]);
+        st_shared8(p + 4 * kPanel, lo[0], lo[1]);
+      }
+      tc::fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&B->loaded);
       if (!wait(&B->loaded, mat & 1)) break;
-      for (int item = sub; item < 8; item += 4) { x_ready(item); partner_ready(item); }
+      for (int item = sub; item < 8; item += 4) x_ready(item);
 
       bool ok = true;
       for (int step = 0; step < J.steps; ++step, ++it) {
@@ -379,9 +510,9 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
           uint32_t v[32];
           tc::tmem_ld_32x32(tmem + C::ACC1 + lanes + item * 32, v);
           tc::tmem_ld_wait();
-          constexpr float f1 = kAScale / (kXScale * kXScale);
+          // kept at the accumulator's scale, x_scale^2
 #pragma unroll
-          for (int e = 0; e < 16; ++e) split2(__uint_as_float(v[2 * e]) * f1, __uint_as_float(v[2 * e + 1]) * f1, hi[e], lo[e]);
+          for (int e = 0; e < 16; ++e) split2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]), hi[e], lo[e]);
           tc::tmem_st_32x16(tmem + C::ACC1 + lanes + item * 32, hi);
           tc::tmem_st_32x16(tmem + C::ACC1 + lanes + item * 32 + 16, lo);
           const int panel = item >> 1, c0 = (item & 1) * 4;
@@ -416,7 +547,8 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
         // ---- P = a I + b A + c A A over A's limbs
         if (!(ok = wait(&B->m2, ph))) break;
         tc::tc_fence_after_sync();
-        const float fa = J.b * J.p_scale / kAScale, faa = J.cc * J.p_scale / (kAScale * kAScale), fi = J.a * J.p_scale;
+        const float a_scale = J.x_scale * J.x_scale, fi = J.a * J.p_scale;
+        const float fa = J.b * J.p_scale / a_scale, faa = J.cc * J.p_scale / (a_scale * a_scale);
         for (int item = sub; item < a_items; item += 4) {
           if (!works) break;
           uint32_t v[32];
@@ -426,13 +558,17 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
           tc::tmem_ld_wait();
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const float2 h2 = unpack_f16(hi[e]), l2 = unpack_f16(lo[e]);
-            float p0 = faa * __uint_as_float(v[2 * e]) + fa * (h2.x + l2.x);
-            float p1 = faa * __uint_as_float(v[2 * e + 1]) + fa * (h2.y + l2.y);
-            if (grow == item * 32 + 2 * e) p0 += fi;
-            if (grow == item * 32 + 2 * e + 1) p1 += fi;
-            split2(p0, p1, hi[e], lo[e]);
+            const float2 A2 = join2(hi[e], lo[e]);
+            v[2 * e] = __float_as_uint(fmaf(fa, A2.x, faa * __uint_as_float(v[2 * e])));
+            v[2 * e + 1] = __float_as_uint(fmaf(fa, A2.y, faa * __uint_as_float(v[2 * e + 1])));
           }
+          if (item == (int)rank * 4 + quarter) {           // the item that holds the diagonal of these rows
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (e == lane) v[e] = __float_as_uint(__uint_as_float(v[e]) + fi);
+          }
+#pragma unroll
+          for (int e = 0; e < 16; ++e) split2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]), hi[e], lo[e]);
           tc::tmem_st_32x16(tmem + C::ACC1 + lanes + item * 32, hi);
           tc::tmem_st_32x16(tmem + C::ACC1 + lanes + item * 32 + 16, lo);
           tc::tmem_st_wait();
@@ -440,62 +576,107 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
           __syncwarp();
           if (lane == 0) arrive(&B->p[item >> 1]);
         }
-        // ---- X' over X, or into the weights
-        if (!(ok = wait(&B->m3, ph))) break;
-        tc::tc_fence_after_sync();
-        const bool last = step == J.steps - 1;
-        for (int item = sub; item < x_items; item += 4) {
-          if (!works) break;
-          uint32_t v[32];
-          tc::tmem_ld_32x32(tmem + C::ACC3 + lanes + item * 32, v);
-          tc::tmem_ld_wait();
-          if (!last) {
-            const float f3 = 1.0f / J.p_scale;
+        // ---- X' over X
+        if (step < J.steps - 1) {
+          if (!(ok = wait(&B->m3, ph))) break;
+          tc::tc_fence_after_sync();
+          const float f3 = 1.0f / J.p_scale;
+          for (int item = sub; item < x_items; item += 4) {
+            if (!works) break;
+            uint32_t v[32];
+            tc::tmem_ld_32x32(tmem + C::ACC3 + lanes + item * 32, v);
+            tc::tmem_ld_wait();
 #pragma unroll
             for (int e = 0; e < 16; ++e) split2(__uint_as_float(v[2 * e]) * f3, __uint_as_float(v[2 * e + 1]) * f3, hi[e], lo[e]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              put_chunk(0, row, item * 4 + e, hi[4 * e], hi[4 * e + 1], hi[4 * e + 2], hi[4 * e + 3]);
-              put_chunk(1, row, item * 4 + e, lo[4 * e], lo[4 * e + 1], lo[4 * e + 2], lo[4 * e + 3]);
+              put_chunk(0, row, item * 4 + e, hi + 4 * e);
+              put_chunk(1, row, item * 4 + e, lo + 4 * e);
             }
-            tc::fence_proxy_async_all();
+            tc::fence_proxy_async_smem();
             tc::tc_fence_before_sync();
             __syncwarp();
             x_ready(item);
-            partner_ready(item);
-            continue;
           }
-          const float fo = 1.0f / (J.p_scale * kXScale);
-          const float keep = J.keep, step_w = J.step;
-          auto put = [&](int64_t at, float x) {
-            if (J.W) J.W[at] = J.W[at] * keep - step_w * x;
-            else if (J.o_bf16) static_cast<__nv_bfloat16*>(J.O)[at] = __float2bfloat16_rn(x);
-            else static_cast<float*>(J.O)[at] = x;
-          };
-          if (J.transpose) {                               // lanes are neighbouring columns of W
+          continue;
+        }
+        // ---- the last step: into the weights (or the result).  Values of W are asked for before they are needed; rows pass
+        // through this warp's 4 KB of X's room, so that lanes work on neighbouring addresses.
+        const float fo = 1.0f / (J.p_scale * J.x_scale), keep = J.keep, step_w = J.step;
+        const uint32_t stage = sX + warp * 4096;
+        bool waited = false;
+        for (int item = sub; item < 8; item += 4) {
+          const bool in = works && item < x_items;
+          // the lane's values are `hop` apart: VEC4: 4 columns of every fourth row; rows of W: its 32 rows at one column;
+          // columns of W (transposed): its 32 columns of one row of X
+          const int i0 = (int)rank * 128 + quarter * 32 + (VEC4 ? lane >> 3 : J.transpose ? lane : 0);
+          const int j0 = item * 32 + (VEC4 ? (lane & 7) * 4 : J.transpose ? 0 : lane);
+          constexpr int kValues = VEC4 ? 8 : 32;
+          const int hop = VEC4 ? 4 * J.c : J.c;
+          int have = 0;
+          if (in && i0 < J.k && j0 < J.n) have = VEC4 ? (J.k - i0 + 3) / 4 : J.transpose ? J.n - j0 : J.k - i0;
+          const int at = J.transpose ? j0 * J.c + i0 : i0 * J.c + j0;
+          float w[VEC4 ? 32 : kValues];
+          if (Ws) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const int j = item * 32 + e;
-              if (grow < J.k && j < J.n) put(base + (int64_t)j * J.c + grow, __uint_as_float(v[e]) * fo);
+            for (int e = 0; e < kValues; ++e) {
+              if constexpr (VEC4) {
+                const float4 a = e < have ? __ldcs(reinterpret_cast<const float4*>(Ws + at + e * hop)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                w[4 * e] = a.x; w[4 * e + 1] = a.y; w[4 * e + 2] = a.z; w[4 * e + 3] = a.w;
+              } else {
+                w[e] = e < have ? __ldcs(Ws + at + e * hop) : 0.0f;
+              }
             }
-          } else {
-            // through this warp's 4 KB of X's room (free now), so that lanes write neighbouring columns
-            const uint32_t stage = sX + warp * 4096;
+          }
+          if (!waited) {
+            if (!(ok = wait(&B->m3, ph))) break;
+            tc::tc_fence_after_sync();
+            waited = true;
+          }
+          if (!in) continue;
+          uint32_t v[32];
+          tc::tmem_ld_32x32(tmem + C::ACC3 + lanes + item * 32, v);
+          tc::tmem_ld_wait();
+          if (VEC4 || !J.transpose) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
-              asm volatile("st.shared.b32 [%0], %1;" ::"r"(stage + (lane * 32 + (e ^ lane)) * 4), "r"(v[e]) : "memory");
+            for (int e = 0; e < 8; ++e) tc::st_shared16(stage + at_chunk(lane, e), v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
             __syncwarp();
-            const int j = item * 32 + lane;
-#pragma unroll 8
-            for (int rr = 0; rr < 32; ++rr) {
-              uint32_t x;
-              asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(stage + (rr * 32 + (lane ^ rr)) * 4) : "memory");
-              const int i = (int)rank * 128 + quarter * 32 + rr;
-              if (i < J.k && j < J.n) put(base + (int64_t)i * J.c + j, __uint_as_float(x) * fo);
+#pragma unroll
+            for (int e = 0; e < kValues; ++e) {
+              if constexpr (VEC4) {
+                const uint4 a = tc::ld_shared16(stage + at_chunk(4 * e + (lane >> 3), lane & 7));
+                v[4 * e] = a.x; v[4 * e + 1] = a.y; v[4 * e + 2] = a.z; v[4 * e + 3] = a.w;
+              } else {
+                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v[e]) : "r"(stage + at_chunk(e, lane >> 2) + (lane & 3) * 4) : "memory");
+              }
             }
             __syncwarp();
+          }
+#pragma unroll
+          for (int e = 0; e < kValues; ++e) {
+            if (e >= have) continue;
+            if constexpr (VEC4) {
+              float x[4];
+#pragma unroll
+              for (int d = 0; d < 4; ++d) {
+                x[d] = __uint_as_float(v[4 * e + d]) * fo;
+                if (Ws) x[d] = w[4 * e + d] * keep - step_w * x[d];
+              }
+              if (Ws || !J.o_bf16) {
+                __stcs(reinterpret_cast<float4*>((Ws ? Ws : static_cast<float*>(J.O) + base) + at + e * hop), make_float4(x[0], x[1], x[2], x[3]));
+              } else {
+                __stcs(reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(J.O) + base + at + e * hop),
+                       make_uint2(vio::pack_bf16(x[0], x[1]), vio::pack_bf16(x[2], x[3])));
+              }
+            } else {
+              const float x = __uint_as_float(v[e]) * fo;
+              if (Ws) __stcs(Ws + at + e * hop, w[e] * keep - step_w * x);
+              else if (J.o_bf16) static_cast<__nv_bfloat16*>(J.O)[base + at + e * hop] = __float2bfloat16_rn(x);
+              else __stcs(static_cast<float*>(J.O) + base + at + e * hop, x);
+            }
           }
         }
+        if (!ok) break;
       }
       tc::tc_fence_before_sync();
       if (!ok) break;
@@ -533,7 +714,7 @@ void launch_shape(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* attr, int ctas, 
 // CTA pairs that can be resident at once (asked once per process; 0: none)
 int resident_pairs() {
   static const int pairs = [] {
-    if (cudaFuncSetAttribute(ns_on_chip<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<true>::SMEM) != cudaSuccess) {
+    if (cudaFuncSetAttribute((ns_on_chip<true, true>), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<true>::SMEM) != cudaSuccess) {
       cudaGetLastError();
       return 0;
     }
@@ -541,7 +722,7 @@ int resident_pairs() {
     cudaLaunchAttribute attr[1];
     launch_shape<true>(cfg, attr, 2 * 148, nullptr);
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, ns_on_chip<true>, &cfg) != cudaSuccess) {
+    if (cudaOccupancyMaxActiveClusters(&n, (ns_on_chip<true, true>), &cfg) != cudaSuccess) {
       cudaGetLastError();
       n = 0;
     }
@@ -550,14 +731,14 @@ int resident_pairs() {
   return pairs;
 }
 
-template <bool PAIR>
+template <bool PAIR, bool VEC4>
 int32_t launch(gnnco_handle* h, const NsJob& job, int64_t groups, cudaStream_t st) {
-  GNNCO_CUDA_TRY(cudaFuncSetAttribute(ns_on_chip<PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<PAIR>::SMEM));
+  GNNCO_CUDA_TRY(cudaFuncSetAttribute(ns_on_chip<PAIR, VEC4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<PAIR>::SMEM));
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[1];
   if (groups > job.sets) groups = job.sets;
   launch_shape<PAIR>(cfg, attr, (int)groups * Cfg<PAIR>::CTAS, st);
-  GNNCO_CUDA_TRY(cudaLaunchKernelEx(&cfg, ns_on_chip<PAIR>, job));
+  GNNCO_CUDA_TRY(cudaLaunchKernelEx(&cfg, ns_on_chip<PAIR, VEC4>, job));
   h->launches += 1;
   return GNNCO_OK;
 }
@@ -577,6 +758,6 @@ size_t ns_on_chip_scratch_bytes(const gnnco_handle* h, int64_t sets, int32_t k, 
 }
 
 int32_t launch_ns_on_chip(gnnco_handle* h, const NsJob& job, cudaStream_t st) {
-  if (job.k <= 128) return launch<false>(h, job, h->sm_count, st);
-  return launch<true>(h, job, resident_pairs(), st);
+  if (job.k <= 128) return job.vec4 ? launch<false, true>(h, job, h->sm_count, st) : launch<false, false>(h, job, h->sm_count, st);
+  return job.vec4 ? launch<true, true>(h, job, resident_pairs(), st) : launch<true, false>(h, job, resident_pairs(), st);
 }

@@ -243,27 +243,36 @@ __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool b_mn_maj
   return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 // D[tmem] (+)= A * B with B in shared memory and A there too (descriptor) or in tensor memory (TS: `a` is a TMEM address;
-// a lane holds one row, a 32-bit column two consecutive k); issued by ONE thread, of the even CTA for a pair.
+// a lane holds one row, a 32-bit column two consecutive k); issued by one thread, of the even CTA for a pair.
+// The whole warp calls it with the same operands and one lane's `leader` != 0: the operands then stay in uniform registers.
+// (Inside an `if (lane == 0)` every operand is moved there per instruction, and short MMAs wait for their issue: 196
+// instead of 64 cycles for 128 x 128 x 16.)
 template <bool PAIR, bool TS>
-__device__ __forceinline__ void mma_f16(uint32_t tmem_d, uint64_t a, uint64_t bdesc, uint32_t idesc, bool accumulate) {
+__device__ __forceinline__ void mma_f16(uint32_t leader, uint32_t tmem_d, uint64_t a, uint64_t bdesc, uint32_t idesc, bool accumulate) {
   const uint32_t acc = accumulate ? 1u : 0u;
   const uint32_t ta = (uint32_t)a;
   if constexpr (!PAIR && !TS)
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(tmem_d), "l"(a), "l"(bdesc), "r"(idesc), "r"(acc) : "memory");
+    asm volatile("{\n\t.reg .pred p, go;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 go, %5, 0;\n\t"
+                 "@go tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(tmem_d), "l"(a), "l"(bdesc), "r"(idesc), "r"(acc), "r"(leader) : "memory");
   else if constexpr (!PAIR && TS)
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(tmem_d), "r"(ta), "l"(bdesc), "r"(idesc), "r"(acc) : "memory");
+    asm volatile("{\n\t.reg .pred p, go;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 go, %5, 0;\n\t"
+                 "@go tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(tmem_d), "r"(ta), "l"(bdesc), "r"(idesc), "r"(acc), "r"(leader) : "memory");
   else if constexpr (PAIR && !TS)
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(tmem_d), "l"(a), "l"(bdesc), "r"(idesc), "r"(acc) : "memory");
+    asm volatile("{\n\t.reg .pred p, go;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 go, %5, 0;\n\t"
+                 "@go tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(tmem_d), "l"(a), "l"(bdesc), "r"(idesc), "r"(acc), "r"(leader) : "memory");
   else
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(tmem_d), "r"(ta), "l"(bdesc), "r"(idesc), "r"(acc) : "memory");
+    asm volatile("{\n\t.reg .pred p, go;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 go, %5, 0;\n\t"
+                 "@go tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(tmem_d), "r"(ta), "l"(bdesc), "r"(idesc), "r"(acc), "r"(leader) : "memory");
+}
+// one lane of a converged warp
+__device__ __forceinline__ uint32_t elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r;
 }
 // 32 lanes x 16 consecutive 32-bit columns
 __device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, uint32_t (&r)[16]) {
@@ -301,6 +310,14 @@ __device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* bar, uint32_t pa
 __device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* gptr, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(smem_dst), "l"(gptr), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+// ... and back; the committed stores have been written when bulk_store_wait returns
+__device__ __forceinline__ void bulk_store(void* gptr, uint32_t smem_src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(gptr), "r"(smem_src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_store_wait() {
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+  asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 }
 __device__ __forceinline__ void mbar_arrive_expect_tx(uint64_t* bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");

@@ -173,9 +173,9 @@ bool valid_sizes(int64_t sets, int32_t r, int32_t c) {
 }
 
 // The iteration must stay bounded on [0, 1], where the singular values start; what it reaches there also bounds every
-// intermediate value.  Sampled densely; a coefficient set whose values grow past 2 is refused.  *s_max: what they reach, *p_max: the largest
+// intermediate value.  Sampled densely; a coefficient set whose values grow past 2 is refused.  *p_max: the largest
 // |a + b s^2 + c s^4| over the values reached.
-bool coefficients_bounded(float a, float b, float c, int steps, double* s_max, double* p_max) {
+bool coefficients_bounded(float a, float b, float c, int steps, double* p_max) {
   double top = 1.0;
   for (int q = 0; q <= 4096; ++q) {
     double s = q / 4096.0;
@@ -186,7 +186,6 @@ bool coefficients_bounded(float a, float b, float c, int steps, double* s_max, d
       if (fabs(s) > top) top = fabs(s);
     }
   }
-  *s_max = top;
   *p_max = 0.0;
   for (int q = 0; q <= 4096; ++q) {
     const double s = top * q / 4096.0, s2 = s * s, p = fabs(a + s2 * (b + s2 * (double)c));
@@ -195,7 +194,7 @@ bool coefficients_bounded(float a, float b, float c, int steps, double* s_max, d
   return true;
 }
 
-struct NsParams { int steps; float a, b, c, eps; float x_scale, p_scale; };
+struct NsParams { int steps; float a, b, c, eps; float p_scale; };
 
 template <typename TG, typename TO>
 int32_t run_ns(gnnco_handle* h, int64_t sets, int32_t r, int32_t c, const TG* G, float* m, float* W, TO* O, float mu, int nesterov,
@@ -211,7 +210,7 @@ int32_t run_ns(gnnco_handle* h, int64_t sets, int32_t r, int32_t c, const TG* G,
              (W ? vec_ok(W, c, 4, 4) : vec_ok(O, c, (int)sizeof(TO), 4));
     // prefetches move whole 16-byte lines of matrices that start on one
     J.prefetch = sizeof(TG) == 4 && count % 4 == 0 && !((uintptr_t)G & 15) && !((uintptr_t)m & 15) && !((uintptr_t)W & 15);
-    J.mu = mu; J.keep = keep; J.step = step; J.eps = P.eps; J.a = P.a; J.b = P.b; J.cc = P.c; J.x_scale = P.x_scale; J.p_scale = P.p_scale;
+    J.mu = mu; J.keep = keep; J.step = step; J.eps = P.eps; J.a = P.a; J.b = P.b; J.cc = P.c; J.p_scale = P.p_scale;
     J.scratch = L.scratch; J.status = h->status;
     return launch_ns_on_chip(h, J, st);
   }
@@ -238,10 +237,8 @@ int32_t run_ns(gnnco_handle* h, int64_t sets, int32_t r, int32_t c, const TG* G,
 
 int32_t check_params(NsParams& P) {
   if (P.steps < 1 || P.steps > 32 || !(P.eps > 0.0f)) return GNNCO_INVALID_ARGUMENT;
-  double s_max = 0.0, p_max = 0.0;
-  if (!coefficients_bounded(P.a, P.b, P.c, P.steps, &s_max, &p_max)) return GNNCO_INVALID_ARGUMENT;
-  // float16 ends at 65,504: A's entries are at most s_max^2 at scale x_scale^2
-  P.x_scale = s_max <= 1.9 ? 128.0f : 64.0f;
+  double p_max = 0.0;
+  if (!coefficients_bounded(P.a, P.b, P.c, P.steps, &p_max)) return GNNCO_INVALID_ARGUMENT;
   // entries of P stay below 2^15 in float16
   P.p_scale = 16384.0f;
   while (P.p_scale * p_max > 32768.0) P.p_scale *= 0.5f;
@@ -259,7 +256,7 @@ extern "C" int32_t gnnco_muon_workspace_bytes(const gnnco_handle* h, int64_t set
 extern "C" int32_t gnnco_muon_update(gnnco_handle* h, int64_t sets, int32_t rows, int32_t cols, float* W, float* m, const float* dW,
                                      const gnnco_muon_params* p, void* ws, size_t ws_bytes, void* stream) {
   if (!h || !W || !m || !dW || !p || !ws || ((uintptr_t)ws & 255) || !valid_sizes(sets, rows, cols)) return GNNCO_INVALID_ARGUMENT;
-  NsParams P{p->steps, p->a, p->b, p->c, p->eps, 1.0f, 1.0f};
+  NsParams P{p->steps, p->a, p->b, p->c, p->eps, 1.0f};
   const int32_t rc = check_params(P);
   if (rc != GNNCO_OK) return rc;
   const NsLayout L = ns_layout(h, ws, sets, rows, cols);
@@ -280,7 +277,7 @@ extern "C" int32_t gnnco_orthogonalise(gnnco_handle* h, int32_t in_dtype, int32_
   if (!h || !G || !O || !p || !ws || ((uintptr_t)ws & 255) || !valid_sizes(sets, rows, cols)) return GNNCO_INVALID_ARGUMENT;
   if ((in_dtype != GNNCO_F32 && in_dtype != GNNCO_BF16) || (out_dtype != GNNCO_F32 && out_dtype != GNNCO_BF16))
     return GNNCO_UNSUPPORTED;
-  NsParams P{p->steps, p->a, p->b, p->c, p->eps, 1.0f, 1.0f};
+  NsParams P{p->steps, p->a, p->b, p->c, p->eps, 1.0f};
   const int32_t rc = check_params(P);
   if (rc != GNNCO_OK) return rc;
   const NsLayout L = ns_layout(h, ws, sets, rows, cols);

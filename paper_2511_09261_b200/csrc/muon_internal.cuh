@@ -13,7 +13,7 @@ struct NsJob {
   int32_t g_bf16, o_bf16, transpose, nesterov, steps, vec4, prefetch;
   float mu, keep, step, eps;  // W = W * keep - step * X
   float a, b, cc;             // the polynomial's coefficients
-  float x_scale, p_scale;     // powers of two that X and P = a I + b A + c A^2 are held at in float16 (A: x_scale^2)
+  float p_scale;              // power of two that P = a I + b A + c A^2 is held at in float16
   void* scratch;
   int32_t* status;
 };

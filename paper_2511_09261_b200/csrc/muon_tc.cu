@@ -7,7 +7,7 @@
 //   X' = P X         P = a I + b A + c A A from tensor memory, X from shared memory (n-major: the same bytes)
 //
 // Accuracy.  Operands are float16 pairs (limbs): x = hi + lo with hi = fl16(x), lo = fl16(x - hi), 22 bits together, at
-// power-of-two scales that keep hi in range and lo's last bit small; a product is hi hi + hi lo + lo hi (the dropped lo lo is
+// power-of-two scales that keep hi in range and lo normal; a product is hi hi + hi lo + lo hi (the dropped lo lo is
 // 2^-24 of it) summed in the float32 accumulator.  The tensor core drops the bits below the accumulator's last place at
 // every instruction, so the small products of all k come first and the large ones meet the accumulator only k / 16
 // times (error of a 256 x 256 iterate after 5 steps: 3.8e-6, 8.0e-6 when interleaved).  That is float32
@@ -67,6 +67,25 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   return r;
 }
 __device__ __forceinline__ float2 unpack_f16(uint32_t v) { return __half22float2(*reinterpret_cast<__half2*>(&v)); }
+constexpr float kXScale = 16384.0f;                        // |X| <= 2 on entry and by the bound on the coefficients
+constexpr float kAScale = 8192.0f;                         // |A| <= 4
+// two float32 values at a time
+__device__ __forceinline__ uint64_t pair_of(float x, float y) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
 // x, y -> packed high limbs and packed low limbs (x - hi in one mixed-precision operation per value)
 __device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t& lo) {
   hi = pack_f16(x, y);
@@ -75,6 +94,12 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t&
       "fma.rn.f32.f16 %0, h0, minus_one, %3;\n\tfma.rn.f32.f16 %1, h1, minus_one, %4;\n\t}"
       : "=f"(a), "=f"(b) : "r"(hi), "f"(x), "f"(y));
   lo = pack_f16(a, b);
+}
+// the same after multiplication with f = (f, f)
+__device__ __forceinline__ void split2_scaled(uint32_t x, uint32_t y, uint64_t f, uint32_t& hi, uint32_t& lo) {
+  float a, b;
+  unpair(mul2(pair_of(__uint_as_float(x), __uint_as_float(y)), f), a, b);
+  split2(a, b, hi, lo);
 }
 // packed limbs -> the two values
 __device__ __forceinline__ float2 join2(uint32_t hi, uint32_t lo) {
@@ -479,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
         }
         if (!total_of(sum)) break;
       }
-      const float f = (float)((double)J.x_scale / (sqrt(norm2) + (double)J.eps));
+      const float f = (float)((double)kXScale / (sqrt(norm2) + (double)J.eps));
       ua = first_a;
       ub = first_b;
 #pragma unroll 4
@@ -510,9 +535,9 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
           uint32_t v[32];
           tc::tmem_ld_32x32(tmem + C::ACC1 + lanes + item * 32, v);
           tc::tmem_ld_wait();
-          // kept at the accumulator's scale, x_scale^2
+          const uint64_t f1 = pair_of(kAScale / (kXScale * kXScale), kAScale / (kXScale * kXScale));
 #pragma unroll
-          for (int e = 0; e < 16; ++e) split2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]), hi[e], lo[e]);
+          for (int e = 0; e < 16; ++e) split2_scaled(v[2 * e], v[2 * e + 1], f1, hi[e], lo[e]);
           tc::tmem_st_32x16(tmem + C::ACC1 + lanes + item * 32, hi);
           tc::tmem_st_32x16(tmem + C::ACC1 + lanes + item * 32 + 16, lo);
           const int panel = item >> 1, c0 = (item & 1) * 4;
@@ -547,8 +572,8 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
         // ---- P = a I + b A + c A A over A's limbs
         if (!(ok = wait(&B->m2, ph))) break;
         tc::tc_fence_after_sync();
-        const float a_scale = J.x_scale * J.x_scale, fi = J.a * J.p_scale;
-        const float fa = J.b * J.p_scale / a_scale, faa = J.cc * J.p_scale / (a_scale * a_scale);
+        const float fi = J.a * J.p_scale, fa1 = J.b * J.p_scale / kAScale, faa1 = J.cc * J.p_scale / (kAScale * kAScale);
+        const uint64_t fa = pair_of(fa1, fa1), faa = pair_of(faa1, faa1);
         for (int item = sub; item < a_items; item += 4) {
           if (!works) break;
           uint32_t v[32];
@@ -559,8 +584,10 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const float2 A2 = join2(hi[e], lo[e]);
-            v[2 * e] = __float_as_uint(fmaf(fa, A2.x, faa * __uint_as_float(v[2 * e])));
-            v[2 * e + 1] = __float_as_uint(fmaf(fa, A2.y, faa * __uint_as_float(v[2 * e + 1])));
+            float p0, p1;
+            unpair(fma2(fa, pair_of(A2.x, A2.y), mul2(faa, pair_of(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])))), p0, p1);
+            v[2 * e] = __float_as_uint(p0);
+            v[2 * e + 1] = __float_as_uint(p1);
           }
           if (item == (int)rank * 4 + quarter) {           // the item that holds the diagonal of these rows
 #pragma unroll
@@ -580,14 +607,14 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
         if (step < J.steps - 1) {
           if (!(ok = wait(&B->m3, ph))) break;
           tc::tc_fence_after_sync();
-          const float f3 = 1.0f / J.p_scale;
+          const uint64_t f3 = pair_of(1.0f / J.p_scale, 1.0f / J.p_scale);
           for (int item = sub; item < x_items; item += 4) {
             if (!works) break;
             uint32_t v[32];
             tc::tmem_ld_32x32(tmem + C::ACC3 + lanes + item * 32, v);
             tc::tmem_ld_wait();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) split2(__uint_as_float(v[2 * e]) * f3, __uint_as_float(v[2 * e + 1]) * f3, hi[e], lo[e]);
+            for (int e = 0; e < 16; ++e) split2_scaled(v[2 * e], v[2 * e + 1], f3, hi[e], lo[e]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               put_chunk(0, row, item * 4 + e, hi + 4 * e);
@@ -602,7 +629,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
         }
         // ---- the last step: into the weights (or the result).  Values of W are asked for before they are needed; rows pass
         // through this warp's 4 KB of X's room, so that lanes work on neighbouring addresses.
-        const float fo = 1.0f / (J.p_scale * J.x_scale), keep = J.keep, step_w = J.step;
+        const float fo = 1.0f / (J.p_scale * kXScale), keep = J.keep, step_w = J.step;
         const uint32_t stage = sX + warp * 4096;
         bool waited = false;
         for (int item = sub; item < 8; item += 4) {

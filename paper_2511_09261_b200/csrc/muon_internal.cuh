@@ -1,4 +1,5 @@
-// What the two halves of the orthogonalised update share (muon.cu: any size; muon_tc.cu: matrices that stay on chip).
+// What the parts of the orthogonalised update share (muon.cu: entry points; muon_tc.cu: matrices that stay on chip;
+// muon_tiles.cu: larger ones).
 #pragma once
 
 #include "internal.cuh"
@@ -22,3 +23,8 @@ struct NsJob {
 bool ns_on_chip_supported(const gnnco_handle* h, int32_t k, int32_t n);
 size_t ns_on_chip_scratch_bytes(const gnnco_handle* h, int64_t sets, int32_t k, int32_t n);
 int32_t launch_ns_on_chip(gnnco_handle* h, const NsJob& job, cudaStream_t st);
+
+// ---- muon_tiles.cu: one tiled launch per product, for any size
+bool ns_tiles_supported(int32_t k, int32_t n);
+size_t ns_tiles_workspace_bytes(int64_t sets, int32_t k, int32_t n);
+int32_t launch_ns_tiles(gnnco_handle* h, const NsJob& job, void* ws, cudaStream_t st);

@@ -169,10 +169,25 @@ def _check(status: int, what: str) -> None:
         raise GnncoError(status, what)
 
 
+_current_raw_stream = None
+
+
 def _stream_ptr(stream=None) -> int:
-    import torch
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return int(s.cuda_stream)
+    """The given stream or the current one, as the pointer the C ABI takes.  (Asking torch for the pointer without
+    building a Stream object takes 0.1 of the 3 microseconds: calls on small graphs are as long as that.)"""
+    global _current_raw_stream
+    if stream is not None:
+        return int(stream.cuda_stream)
+    if _current_raw_stream is None:
+        import torch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is None:
+            _current_raw_stream = lambda: int(torch.cuda.current_stream().cuda_stream)  # noqa: E731
+        else:
+            torch.cuda.init()
+            device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+            _current_raw_stream = lambda: raw(device())  # noqa: E731
+    return _current_raw_stream()
 
 
 def _dptr(t) -> Optional[int]:
@@ -186,24 +201,27 @@ def _require(t, dtype, what: str, device_type: str = "cuda"):
     return t
 
 
+_feat_codes = {}
+
+
 def _feat_code(t, what: str) -> int:
-    import torch
-    if isinstance(t, torch.Tensor):
-        if t.dtype == torch.float32:
-            return F32
-        if t.dtype == torch.bfloat16:
-            return BF16
-    raise TypeError("%s must be a float32 or bfloat16 tensor" % what)
+    if not _feat_codes:
+        import torch
+        _feat_codes.update({torch.float32: F32, torch.bfloat16: BF16})
+    code = _feat_codes.get(getattr(t, "dtype", None))
+    if code is None:
+        raise TypeError("%s must be a float32 or bfloat16 tensor" % what)
+    return code
 
 
-def _empty(shape, dtype, device, stream):
-    """A tensor for a call on ``stream``: its memory comes from that stream's pool, so that work still queued on
-    the current stream cannot own it."""
-    import torch
+def _empty(shape, dtype, like, stream):
+    """A tensor on ``like``'s device for a call on ``stream``: its memory comes from that stream's pool, so that work
+    still queued on the current stream cannot own it."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
+    import torch
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
 
 
 MUON_COEFS = (3.4445, -4.7750, 2.0315)
@@ -570,23 +588,24 @@ class PartitionedGraph:
 
     # ---- shared input embeddings, norms around a block, orthogonalised updates
 
-    def _rows(self, t, dtype, shape, what: str) -> int:
+    def _rows(self, t, dtype, rows: int, F: int, what: str) -> int:
         """Checks a [rows, F] tensor whose rows are consecutive elements; returns the distance between rows."""
-        import torch
-        if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != self.device or t.dim() != 2:
+        if getattr(t, "dtype", None) != dtype or t.device != self.device or t.dim() != 2:
             raise TypeError("%s must be a 2-D %s tensor on %s" % (what, dtype, self.device))
-        if tuple(t.shape) != tuple(shape):
-            raise ValueError("%s must be %s" % (what, list(shape)))
-        if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        r, f = t.shape
+        if r != rows or f != F:
+            raise ValueError("%s must be [%d, %d]" % (what, rows, F))
+        ld, step = t.stride()
+        if f > 1 and step != 1 or r > 1 and ld < f:
             raise ValueError("%s must have rows of consecutive elements that do not overlap" % what)
-        return t.stride(0) if t.shape[0] > 1 else max(int(t.shape[1]), 1)
+        return ld if r > 1 else max(f, 1)
 
-    def _tokens(self, tokens):
+    def _tokens(self, tokens) -> int:
         import torch
         _require(tokens, torch.int32, "tokens")
         if tokens.dim() != 1 or tokens.device != self.device:
             raise ValueError("tokens must be one-dimensional and on %s" % self.device)
-        return int(tokens.shape[0])
+        return tokens.shape[0]
 
     def embedding_lookup(self, table, tokens, scale: float = 1.0, out=None, out_dtype=None, stream=None):
         """``gnnco_embedding_lookup``: scale * table[tokens] for ``tokens`` int32 [rows]; a negative token gives zeros.
@@ -597,11 +616,15 @@ class PartitionedGraph:
         if table.dim() != 2 or 0 in table.shape:
             raise ValueError("table must be [V, F]")
         V, F = table.shape
-        table_ld = self._rows(table, table.dtype, table.shape, "table")
+        table_ld = self._rows(table, table.dtype, V, F, "table")
         if out is None:
-            out = _empty((rows, F), out_dtype or table.dtype, self.device, stream)
-        od = _feat_code(out, "out")
-        out_ld = self._rows(out, out.dtype, (rows, F), "out")
+            if out_dtype is not None and out_dtype not in _feat_codes:
+                raise TypeError("out_dtype must be float32 or bfloat16")
+            out = _empty((rows, F), out_dtype or table.dtype, table, stream)
+            od, out_ld = _feat_codes[out.dtype], F
+        else:
+            od = _feat_code(out, "out")
+            out_ld = self._rows(out, out.dtype, rows, F, "out")
         _check(self._lib.gnnco_embedding_lookup(self._handle, td, od, rows, V, F, tokens.data_ptr(), table.data_ptr(),
                                                 table_ld, scale, out.data_ptr(), out_ld, _stream_ptr(stream)),
                "gnnco_embedding_lookup")
@@ -614,8 +637,9 @@ class PartitionedGraph:
         rows = self._tokens(tokens)
         need = _sz(0)
         _check(self._lib.gnnco_embedding_plan_bytes(rows, V, F, ctypes.byref(need)), "gnnco_embedding_plan_bytes")
-        ws = _empty(need.value, torch.uint8, self.device, stream)
-        _check(self._lib.gnnco_embedding_plan(self._handle, tokens.data_ptr(), rows, V, F, ws.data_ptr(), need.value,
+        need = need.value
+        ws = _empty((need,), torch.uint8, tokens, stream)
+        _check(self._lib.gnnco_embedding_plan(self._handle, tokens.data_ptr(), rows, V, F, ws.data_ptr(), need,
                                               _stream_ptr(stream)), "gnnco_embedding_plan")
         return EmbeddingPlan(rows, V, F, ws)
 
@@ -626,15 +650,19 @@ class PartitionedGraph:
         gd = _feat_code(dout, "dout")
         if dout.dim() != 2 or not 1 <= dout.shape[1] <= plan.F:
             raise ValueError("dout must be [rows, F] with F up to the plan's")
-        F = dout.shape[1]
-        dout_ld = self._rows(dout, dout.dtype, (plan.rows, F), "dout")
+        F, V, ws = dout.shape[1], plan.V, plan.ws
+        dout_ld = self._rows(dout, dout.dtype, plan.rows, F, "dout")
         if out is None:
-            out = _empty((plan.V, F), out_dtype or torch.float32, self.device, stream)
-        od = _feat_code(out, "out")
-        out_ld = self._rows(out, out.dtype, (plan.V, F), "out")
-        _check(self._lib.gnnco_embedding_grad(self._handle, gd, od, plan.rows, plan.V, F, dout.data_ptr(), dout_ld,
-                                              scale, plan.ws.data_ptr(), plan.ws.numel(), out.data_ptr(), out_ld,
-                                              _stream_ptr(stream)), "gnnco_embedding_grad")
+            if out_dtype is not None and out_dtype not in _feat_codes:
+                raise TypeError("out_dtype must be float32 or bfloat16")
+            out = _empty((V, F), out_dtype or torch.float32, dout, stream)
+            od, out_ld = _feat_codes[out.dtype], F
+        else:
+            od = _feat_code(out, "out")
+            out_ld = self._rows(out, out.dtype, V, F, "out")
+        _check(self._lib.gnnco_embedding_grad(self._handle, gd, od, plan.rows, V, F, dout.data_ptr(), dout_ld, scale,
+                                              ws.data_ptr(), ws.shape[0], out.data_ptr(), out_ld, _stream_ptr(stream)),
+               "gnnco_embedding_grad")
         return out
 
     def _weight(self, w, F, what: str):
@@ -642,7 +670,7 @@ class PartitionedGraph:
         if w is None:
             return None
         _require(w, torch.float32, what)
-        if tuple(w.shape) != (F,) or w.device != self.device:
+        if w.dim() != 1 or w.shape[0] != F or w.device != self.device:
             raise ValueError("%s must be [F] on %s" % (what, self.device))
         return w.data_ptr()
 
@@ -653,14 +681,14 @@ class PartitionedGraph:
         if y is None and (gate is not None or w_post is not None):
             raise ValueError("gate and w_post belong to a block output y")
         rows, F = x.shape
-        d = BlockNormDesc(rows, F, dt, eps, scale, x.data_ptr(), self._rows(x, x.dtype, (rows, F), "x"))
+        d = BlockNormDesc(rows, F, dt, eps, scale, x.data_ptr(), self._rows(x, x.dtype, rows, F, "x"))
         if y is not None:
-            d.y, d.y_ld = y.data_ptr(), self._rows(y, x.dtype, (rows, F), "y")
+            d.y, d.y_ld = y.data_ptr(), self._rows(y, x.dtype, rows, F, "y")
         if gate is not None:
             if gate.dim() == 1:
                 d.gate = self._weight(gate, F, "gate")
             else:
-                d.gate, d.gate_ld = gate.data_ptr(), self._rows(gate, x.dtype, (rows, F), "gate")
+                d.gate, d.gate_ld = gate.data_ptr(), self._rows(gate, x.dtype, rows, F, "gate")
         d.w_pre, d.w_post = self._weight(w_pre, F, "w_pre"), self._weight(w_post, F, "w_post")
         return d
 
@@ -669,18 +697,21 @@ class PartitionedGraph:
         """``gnnco_block_norm``: (x_out, h) with x_out = x + scale * gate * norm(y) * w_post and h = norm(x_out) * w_pre.
         Without ``y`` x_out is x; with want_h=False h is None.  ``gate``: None, float32 [F] or [rows, F] like x."""
         d = self._block_desc(x, w_pre, y, w_post, gate, scale, eps)
-        shape = (d.rows, d.F)
+        rows, F, dtype = d.rows, d.F, x.dtype
+        x_ld = h_ld = F
         if y is None:
             if x_out is not None:
                 raise ValueError("x_out belongs to a block output y")
         elif x_out is None:
-            x_out = _empty(shape, x.dtype, self.device, stream)
-        if h_out is None and want_h:
-            h_out = _empty(shape, x.dtype, self.device, stream)
-        _check(self._lib.gnnco_block_norm(
-            self._handle, ctypes.byref(d), _dptr(x_out), 0 if x_out is None else self._rows(x_out, x.dtype, shape, "x_out"),
-            _dptr(h_out), 0 if h_out is None else self._rows(h_out, x.dtype, shape, "h_out"), _stream_ptr(stream)),
-            "gnnco_block_norm")
+            x_out = _empty((rows, F), dtype, x, stream)
+        else:
+            x_ld = self._rows(x_out, dtype, rows, F, "x_out")
+        if h_out is not None:
+            h_ld = self._rows(h_out, dtype, rows, F, "h_out")
+        elif want_h:
+            h_out = _empty((rows, F), dtype, x, stream)
+        _check(self._lib.gnnco_block_norm(self._handle, ctypes.byref(d), _dptr(x_out), x_ld, _dptr(h_out), h_ld,
+                                          _stream_ptr(stream)), "gnnco_block_norm")
         return (x if y is None else x_out), h_out
 
     def block_norm_backward(self, x, dh=None, w_pre=None, dx_out=None, y=None, w_post=None, gate=None, scale: float = 1.0,
@@ -689,44 +720,45 @@ class PartitionedGraph:
         dict(dx, dy, dgate, dw_pre, dw_post); entries whose input was not given are None."""
         import torch
         d = self._block_desc(x, w_pre, y, w_post, gate, scale, eps)
-        shape = (d.rows, d.F)
+        rows, F, dtype = d.rows, d.F, x.dtype
+        shape = (rows, F)
         g = BlockNormGrads()
         if dh is not None:
-            g.dh, g.dh_ld = dh.data_ptr(), self._rows(dh, x.dtype, shape, "dh")
+            g.dh, g.dh_ld = dh.data_ptr(), self._rows(dh, dtype, rows, F, "dh")
         if dx_out is not None:
-            g.dx_out, g.dx_out_ld = dx_out.data_ptr(), self._rows(dx_out, x.dtype, shape, "dx_out")
+            g.dx_out, g.dx_out_ld = dx_out.data_ptr(), self._rows(dx_out, dtype, rows, F, "dx_out")
         if dx is None:
-            dx = _empty(shape, x.dtype, self.device, stream)
-        g.dx, g.dx_ld = dx.data_ptr(), self._rows(dx, x.dtype, shape, "dx")
+            dx = _empty(shape, dtype, x, stream)
+        g.dx, g.dx_ld = dx.data_ptr(), self._rows(dx, dtype, rows, F, "dx")
         if y is not None:
             if dy is None:
-                dy = _empty(shape, x.dtype, self.device, stream)
-            g.dy, g.dy_ld = dy.data_ptr(), self._rows(dy, x.dtype, shape, "dy")
+                dy = _empty(shape, dtype, x, stream)
+            g.dy, g.dy_ld = dy.data_ptr(), self._rows(dy, dtype, rows, F, "dy")
         if gate is not None:
             if dgate is None:
-                dgate = _empty(tuple(gate.shape), gate.dtype, self.device, stream)
+                dgate = _empty(tuple(gate.shape), gate.dtype, gate, stream)
             if gate.dim() == 1:
-                g.dgate = self._weight(dgate, d.F, "dgate")
+                g.dgate = self._weight(dgate, F, "dgate")
             else:
-                g.dgate, g.dgate_ld = dgate.data_ptr(), self._rows(dgate, x.dtype, shape, "dgate")
+                g.dgate, g.dgate_ld = dgate.data_ptr(), self._rows(dgate, dtype, rows, F, "dgate")
         dw_pre = dw_post = None
         if w_pre is not None:
-            dw_pre = _empty(d.F, torch.float32, self.device, stream)
+            dw_pre = _empty((F,), torch.float32, x, stream)
             g.dw_pre = dw_pre.data_ptr()
         if w_post is not None:
-            dw_post = _empty(d.F, torch.float32, self.device, stream)
+            dw_post = _empty((F,), torch.float32, x, stream)
             g.dw_post = dw_post.data_ptr()
         need = _sz(0)
-        _check(self._lib.gnnco_block_norm_workspace_bytes(self._handle, d.F, ctypes.byref(need)),
+        _check(self._lib.gnnco_block_norm_workspace_bytes(self._handle, F, ctypes.byref(need)),
                "gnnco_block_norm_workspace_bytes")
-        ws = _empty(need.value, torch.uint8, self.device, stream)
+        ws = _empty((need.value,), torch.uint8, x, stream)
         _check(self._lib.gnnco_block_norm_backward(self._handle, ctypes.byref(d), ctypes.byref(g), ws.data_ptr(),
                                                    need.value, _stream_ptr(stream)), "gnnco_block_norm_backward")
         return dict(dx=dx, dy=dy, dgate=dgate, dw_pre=dw_pre, dw_post=dw_post)
 
-    def _muon_call(self, shape, active, stream, ws):
+    def _muon_call(self, like, active, stream, ws):
         import torch
-        sets, r, c = (int(v) for v in shape)
+        sets, r, c = like.shape
         if active is not None:
             _require(active, torch.uint8, "active")
             if tuple(active.shape) != (sets,) or active.device != self.device:
@@ -735,7 +767,7 @@ class PartitionedGraph:
         _check(self._lib.gnnco_muon_workspace_bytes(self._handle, sets, r, c, ctypes.byref(need)),
                "gnnco_muon_workspace_bytes")
         if ws is None:
-            ws = _empty(max(256, need.value), torch.uint8, self.device, stream)
+            ws = _empty((max(256, need.value),), torch.uint8, like, stream)
         return sets, r, c, ws
 
     def muon_update(self, W, m, dW, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True,
@@ -749,7 +781,7 @@ class PartitionedGraph:
             _require(t, torch.float32, what)
             if t.dim() != 3 or t.shape != W.shape or t.device != self.device:
                 raise ValueError("W, m and dW must be [sets, d_in, d_out] on %s" % self.device)
-        sets, r, c, ws = self._muon_call(W.shape, active, stream, ws)
+        sets, r, c, ws = self._muon_call(W, active, stream, ws)
         p = MuonParams(lr, momentum, weight_decay, int(nesterov), steps, coefs[0], coefs[1], coefs[2], eps, _dptr(active))
         _check(self._lib.gnnco_muon_update(self._handle, sets, r, c, W.data_ptr(), m.data_ptr(), dW.data_ptr(),
                                            ctypes.byref(p), ws.data_ptr(), ws.numel(), _stream_ptr(stream)),
@@ -771,12 +803,12 @@ class PartitionedGraph:
         if G.dim() != 3 or 0 in G.shape or G.device != self.device:
             raise ValueError("G must be [sets, rows, cols] on %s" % self.device)
         if out is None:
-            out = _empty(tuple(G.shape), out_dtype or G.dtype, self.device, stream)
+            out = _empty(tuple(G.shape), out_dtype or G.dtype, G, stream)
         od = _feat_code(out, "out")
         _require(out, out.dtype, "out")
         if out.shape != G.shape or out.device != self.device:
             raise ValueError("out must have the shape of G")
-        sets, r, c, ws = self._muon_call(G.shape, active, stream, ws)
+        sets, r, c, ws = self._muon_call(G, active, stream, ws)
         p = MuonParams(0.0, 0.0, 0.0, 0, steps, coefs[0], coefs[1], coefs[2], eps, _dptr(active))
         _check(self._lib.gnnco_orthogonalise(self._handle, gd, od, sets, r, c, G.data_ptr(), out.data_ptr(),
                                              ctypes.byref(p), ws.data_ptr(), ws.numel(), _stream_ptr(stream)),

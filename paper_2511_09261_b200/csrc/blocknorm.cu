@@ -20,6 +20,15 @@ namespace {
 
 template <int TEAM>
 struct TeamSum {
+  static __device__ __forceinline__ float one(float a, float2* buf) {
+    if constexpr (TEAM <= 32) {
+#pragma unroll
+      for (int d = TEAM / 2; d > 0; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d);
+      return a;
+    } else {
+      return both(a, 0.0f, buf).x;
+    }
+  }
   // sum of a and of b over the team, returned to every lane
   static __device__ __forceinline__ float2 both(float a, float b, float2* buf) {
     if constexpr (TEAM <= 32) {
@@ -64,179 +73,207 @@ struct NormArgs {
 // what the gate is
 constexpr int kGateNone = 0, kGateVector = 1, kGateRows = 2;
 
-// Teams of TEAM lanes, K vectors of VEC elements per lane; rows are dealt to teams grid-stride.
-template <typename T, int VEC, int TEAM, int K>
+// A lane's share of a vector of F float32 weights: 1 where there is none, times f.
+template <int VEC, int TEAM, int K>
+__device__ __forceinline__ void lane_weights(float (&w)[K][VEC], const float* p, int F, int tl, float f) {
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const int col = (k * TEAM + tl) * VEC + e;
+      w[k][e] = col < F ? f * (p ? __ldg(p + col) : 1.0f) : 0.0f;
+    }
+}
+
+// Teams of TEAM lanes, K vectors of VEC elements per lane; a team works on R rows at a time (their loads are in flight
+// together), blocks go through the rows grid-stride.  Weights stay in registers.
+template <typename T, int VEC, int TEAM, int K, int R>
 __global__ void __launch_bounds__(TEAM > 256 ? TEAM : 256)
 norm_forward(const NormArgs A, const int gate_kind) {
   constexpr int THREADS = TEAM > 256 ? TEAM : 256, TEAMS = THREADS / TEAM;
   __shared__ float2 buf[TEAM > 32 ? TEAM / 32 : 1];
-  const int tl = threadIdx.x % TEAM;
-  const int64_t stride = (int64_t)gridDim.x * TEAMS;
-  const int64_t first = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TEAM;
-  // whole warps stay in the loop together (the shuffles name all lanes): the bound is the block's first row
-  for (int64_t row = first, lead = (int64_t)blockIdx.x * TEAMS; lead < A.rows; row += stride, lead += stride) {
-    const bool live = row < A.rows;
-    vio::Raw<T, VEC> xr[K], yr[K];
-    float sy = 0.0f, sx = 0.0f;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int col = (k * TEAM + tl) * VEC;
-      const bool in = live && col < A.F;
-      if (in && A.x) xr[k].template load<true>((const T*)A.x + row * A.x_ld + col);
-      else xr[k].zero();
-      if (in && A.y) yr[k].template load<true>((const T*)A.y + row * A.y_ld + col);
-      else yr[k].zero();
-    }
-    float xo[K][VEC];
+  const int tl = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
+  float c_post[K][VEC], w_pre[K][VEC];
+  lane_weights<VEC, TEAM, K>(w_pre, A.w_pre, A.F, tl, 1.0f);
+  lane_weights<VEC, TEAM, K>(c_post, A.w_post, A.F, tl, A.scale);
+  if (gate_kind == kGateVector) {
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        xo[k][e] = xr[k].get(e);
-        const float v = yr[k].get(e);
-        sy += v * v;
-        sx += xo[k][e] * xo[k][e];
+        const int col = (k * TEAM + tl) * VEC + e;
+        if (col < A.F) c_post[k][e] *= __ldg((const float*)A.gate + col);
       }
-    if (A.y) {
-      sy = TeamSum<TEAM>::both(sy, 0.0f, buf).x;
-      const float f = A.scale * (1.0f / sqrtf(sy * A.inv_F + A.eps));
-      sx = 0.0f;
+  }
+  // whole blocks stay in the loop together (the sums name all lanes)
+  for (int64_t lead = (int64_t)blockIdx.x * (TEAMS * R); lead < A.rows; lead += (int64_t)gridDim.x * (TEAMS * R)) {
+    vio::Raw<T, VEC> xr[R][K], yr[R][K], gr[R][K];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t row = lead + r * TEAMS + team;
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const int col = (k * TEAM + tl) * VEC;
-        const bool in = live && col < A.F;
-        vio::Raw<T, VEC> gr;
-        gr.zero();
-        if (gate_kind == kGateRows && in) gr.template load<true>((const T*)A.gate + row * A.gate_ld + col);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          float c = f;
-          if (gate_kind == kGateRows) c *= gr.get(e);
-          else if (gate_kind == kGateVector && in) c *= __ldg((const float*)A.gate + col + e);
-          if (A.w_post && in) c *= __ldg(A.w_post + col + e);
-          xo[k][e] += c * yr[k].get(e);
-          sx += xo[k][e] * xo[k][e];
-        }
-        if (in && A.x_out) vio::store_stream<T, VEC>((T*)A.x_out + row * A.x_out_ld + col, xo[k]);
+        const bool in = row < A.rows && col < A.F;
+        if (in) xr[r][k].template load<true>((const T*)A.x + row * A.x_ld + col);
+        else xr[r][k].zero();
+        if (in && A.y) yr[r][k].template load<true>((const T*)A.y + row * A.y_ld + col);
+        else yr[r][k].zero();
+        gr[r][k].zero();
+        if (gate_kind == kGateRows && in) gr[r][k].template load<true>((const T*)A.gate + row * A.gate_ld + col);
       }
     }
-    if (A.h_out) {
-      sx = TeamSum<TEAM>::both(sx, 0.0f, buf).x;
-      const float r = 1.0f / sqrtf(sx * A.inv_F + A.eps);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t row = lead + r * TEAMS + team;
+      float xo[K][VEC];
+      float sx = 0.0f;
+      float f = 0.0f;
+      if (A.y) {
+        float sy = 0.0f;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) sy += yr[r][k].get(e) * yr[r][k].get(e);
+        sy = TeamSum<TEAM>::one(sy, buf);
+        f = 1.0f / sqrtf(sy * A.inv_F + A.eps);
+      }
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const int col = (k * TEAM + tl) * VEC;
-        if (!live || col >= A.F) continue;
-        float o[VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) o[e] = xo[k][e] * r * (A.w_pre ? __ldg(A.w_pre + col + e) : 1.0f);
-        vio::store_stream<T, VEC>((T*)A.h_out + row * A.h_out_ld + col, o);
+        for (int e = 0; e < VEC; ++e) {
+          float c = c_post[k][e];
+          if (gate_kind == kGateRows) c *= gr[r][k].get(e);
+          xo[k][e] = xr[r][k].get(e);
+          if (A.y) xo[k][e] += c * (f * yr[r][k].get(e));
+          sx += xo[k][e] * xo[k][e];
+        }
+        if (row < A.rows && col < A.F && A.x_out) vio::store_stream<T, VEC>((T*)A.x_out + row * A.x_out_ld + col, xo[k]);
+      }
+      if (!A.h_out) continue;
+      sx = TeamSum<TEAM>::one(sx, buf);
+      const float rx = 1.0f / sqrtf(sx * A.inv_F + A.eps);
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const int col = (k * TEAM + tl) * VEC;
+        if (row >= A.rows || col >= A.F) continue;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) xo[k][e] = xo[k][e] * rx * w_pre[k][e];
+        vio::store_stream<T, VEC>((T*)A.h_out + row * A.h_out_ld + col, xo[k]);
       }
     }
   }
 }
 
-template <typename T, int VEC, int TEAM, int K>
+template <typename T, int VEC, int TEAM, int K, int R>
 __global__ void __launch_bounds__(TEAM > 256 ? TEAM : 256)
 norm_backward(const NormArgs A, const int gate_kind) {
   constexpr int THREADS = TEAM > 256 ? TEAM : 256, TEAMS = THREADS / TEAM;
   __shared__ float2 buf[TEAM > 32 ? TEAM / 32 : 1];
   extern __shared__ float join[];                          // [TEAMS][TEAM * K * VEC], one quantity at a time
   const int tl = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
-  const int64_t stride = (int64_t)gridDim.x * TEAMS;
-  float s_pre[K][VEC], s_post[K][VEC];
+  float s_pre[K][VEC], s_post[K][VEC], c_post[K][VEC], w_pre[K][VEC];
 #pragma unroll
   for (int k = 0; k < K; ++k)
 #pragma unroll
     for (int e = 0; e < VEC; ++e) s_pre[k][e] = s_post[k][e] = 0.0f;
-
-  for (int64_t row = (int64_t)blockIdx.x * TEAMS + team, lead = (int64_t)blockIdx.x * TEAMS; lead < A.rows;
-       row += stride, lead += stride) {
-    const bool live = row < A.rows;
-    vio::Raw<T, VEC> xr[K], yr[K], dr[K], hr[K];
-    float sx = 0.0f, sa = 0.0f;
+  lane_weights<VEC, TEAM, K>(w_pre, A.w_pre, A.F, tl, 1.0f);
+  lane_weights<VEC, TEAM, K>(c_post, A.w_post, A.F, tl, A.scale);   // s w_post, times g where the gate is shared
+  if (gate_kind == kGateVector) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int col = (k * TEAM + tl) * VEC;
-      const bool in = live && col < A.F;
-      if (in && A.dh) {
-        xr[k].template load<true>((const T*)A.x + row * A.x_ld + col);
-        hr[k].template load<true>((const T*)A.dh + row * A.dh_ld + col);
-      } else {
-        xr[k].zero();
-        hr[k].zero();
-      }
-      if (in && A.y) yr[k].template load<true>((const T*)A.y + row * A.y_ld + col);
-      else yr[k].zero();
-      if (in && A.dx_out) dr[k].template load<true>((const T*)A.dx_out + row * A.dx_out_ld + col);
-      else dr[k].zero();
-    }
-    float D[K][VEC];
-    // mean over features of x'^2 and of a .* x'
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int col = (k * TEAM + tl) * VEC;
+    for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const float w = A.w_pre && col < A.F ? __ldg(A.w_pre + col + e) : 1.0f;
-        const float x = xr[k].get(e);
-        sx += x * x;
-        sa += hr[k].get(e) * w * x;
+        const int col = (k * TEAM + tl) * VEC + e;
+        if (col < A.F) c_post[k][e] *= __ldg((const float*)A.gate + col);
+      }
+  }
+  for (int64_t lead = (int64_t)blockIdx.x * (TEAMS * R); lead < A.rows; lead += (int64_t)gridDim.x * (TEAMS * R)) {
+    vio::Raw<T, VEC> xr[R][K], yr[R][K], dr[R][K], hr[R][K], gr[R][K];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t row = lead + r * TEAMS + team;
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const int col = (k * TEAM + tl) * VEC;
+        const bool in = row < A.rows && col < A.F;
+        if (in && A.dh) {
+          xr[r][k].template load<true>((const T*)A.x + row * A.x_ld + col);
+          hr[r][k].template load<true>((const T*)A.dh + row * A.dh_ld + col);
+        } else {
+          xr[r][k].zero();
+          hr[r][k].zero();
+        }
+        if (in && A.y) yr[r][k].template load<true>((const T*)A.y + row * A.y_ld + col);
+        else yr[r][k].zero();
+        if (in && A.dx_out) dr[r][k].template load<true>((const T*)A.dx_out + row * A.dx_out_ld + col);
+        else dr[r][k].zero();
+        gr[r][k].zero();
+        if (gate_kind == kGateRows && in) gr[r][k].template load<true>((const T*)A.gate + row * A.gate_ld + col);
       }
     }
-    float2 t = TeamSum<TEAM>::both(sx, sa, buf);
-    const float rx = 1.0f / sqrtf(t.x * A.inv_F + A.eps);
-    const float cx = t.y * A.inv_F * rx * rx;               // mean(a .* xh) * r(x'): times x' below
-    float sy = 0.0f, sb = 0.0f;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int col = (k * TEAM + tl) * VEC;
-      const bool in = live && col < A.F;
-      vio::Raw<T, VEC> gr;
-      gr.zero();
-      if (gate_kind == kGateRows && in) gr.template load<true>((const T*)A.gate + row * A.gate_ld + col);
+    for (int r = 0; r < R; ++r) {
+      const int64_t row = lead + r * TEAMS + team;
+      float sx = 0.0f, sa = 0.0f;
+      // mean over features of x'^2 and of a .* x'
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        const float w = A.w_pre && col < A.F ? __ldg(A.w_pre + col + e) : 1.0f;
-        const float x = xr[k].get(e), dh = hr[k].get(e), y = yr[k].get(e);
-        s_pre[k][e] += dh * (x * rx);
-        D[k][e] = dr[k].get(e) + rx * (dh * w - x * cx);
-        float c = A.scale;
-        if (gate_kind == kGateRows) c *= gr.get(e);
-        else if (gate_kind == kGateVector && col < A.F) c *= __ldg((const float*)A.gate + col + e);
-        if (A.w_post && col < A.F) c *= __ldg(A.w_post + col + e);
-        sy += y * y;
-        sb += c * D[k][e] * y;
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const float x = xr[r][k].get(e);
+          sx += x * x;
+          sa += hr[r][k].get(e) * w_pre[k][e] * x;
+        }
+      float2 t = TeamSum<TEAM>::both(sx, sa, buf);
+      const float rx = 1.0f / sqrtf(t.x * A.inv_F + A.eps);
+      const float cx = t.y * A.inv_F * rx * rx;             // mean(a .* xh) * r(x'): times x' below
+      float D[K][VEC];
+      float sy = 0.0f, sb = 0.0f;
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const int col = (k * TEAM + tl) * VEC;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const float x = xr[r][k].get(e), dh = hr[r][k].get(e), y = yr[r][k].get(e);
+          s_pre[k][e] += dh * (x * rx);
+          D[k][e] = dr[r][k].get(e) + rx * (dh * w_pre[k][e] - x * cx);
+          float c = c_post[k][e];
+          if (gate_kind == kGateRows) c *= gr[r][k].get(e);
+          sy += y * y;
+          sb += c * D[k][e] * y;
+        }
+        if (row < A.rows && col < A.F) vio::store_stream<T, VEC>((T*)A.dx + row * A.dx_ld + col, D[k]);
       }
-      if (in) vio::store_stream<T, VEC>((T*)A.dx + row * A.dx_ld + col, D[k]);
-    }
-    if (!A.y) continue;                                    // the same for all rows: no lane is left alone
-    t = TeamSum<TEAM>::both(sy, sb, buf);
-    const float ry = 1.0f / sqrtf(t.x * A.inv_F + A.eps);
-    const float cy = t.y * A.inv_F * ry * ry;
+      if (!A.y) continue;                                  // the same for all rows: no lane is left alone
+      t = TeamSum<TEAM>::both(sy, sb, buf);
+      const float ry = 1.0f / sqrtf(t.x * A.inv_F + A.eps);
+      const float cy = t.y * A.inv_F * ry * ry;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int col = (k * TEAM + tl) * VEC;
-      const bool in = live && col < A.F;
-      vio::Raw<T, VEC> gr;
-      gr.zero();
-      if (gate_kind == kGateRows && in) gr.template load<true>((const T*)A.gate + row * A.gate_ld + col);
-      float dy[VEC], dg[VEC];
+      for (int k = 0; k < K; ++k) {
+        const int col = (k * TEAM + tl) * VEC;
+        const bool in = row < A.rows && col < A.F;
+        float dy[VEC], dg[VEC];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        const float y = yr[k].get(e);
-        const float wp = A.w_post && col < A.F ? __ldg(A.w_post + col + e) : 1.0f;
-        float g = 1.0f;
-        if (gate_kind == kGateRows) g = gr.get(e);
-        else if (gate_kind == kGateVector && col < A.F) g = __ldg((const float*)A.gate + col + e);
-        const float q = A.scale * D[k][e] * (y * ry);      // the shared factor of dg and dw_post
-        s_post[k][e] += gate_kind == kGateRows ? g * q : q;
-        dg[e] = wp * q;
-        dy[e] = ry * (A.scale * g * wp * D[k][e] - y * cy);
-      }
-      if (in) {
-        vio::store_stream<T, VEC>((T*)A.dy + row * A.dy_ld + col, dy);
-        if (gate_kind == kGateRows && A.dgate) vio::store_stream<T, VEC>((T*)A.dgate + row * A.dgate_ld + col, dg);
+        for (int e = 0; e < VEC; ++e) {
+          const float y = yr[r][k].get(e);
+          const float q = D[k][e] * (y * ry);               // times s: the shared factor of dg and dw_post
+          float c = c_post[k][e];
+          if (gate_kind == kGateRows) {
+            const float g = gr[r][k].get(e);
+            s_post[k][e] += g * q;
+            dg[e] = c * q;
+            c *= g;
+          } else {
+            s_post[k][e] += q;
+          }
+          dy[e] = ry * (c * D[k][e] - y * cy);
+        }
+        if (in) {
+          vio::store_stream<T, VEC>((T*)A.dy + row * A.dy_ld + col, dy);
+          if (gate_kind == kGateRows && A.dgate) vio::store_stream<T, VEC>((T*)A.dgate + row * A.dgate_ld + col, dg);
+        }
       }
     }
   }
@@ -254,7 +291,7 @@ norm_backward(const NormArgs A, const int gate_kind) {
       float s = 0.0f;
 #pragma unroll 4
       for (int q = 0; q < TEAMS; ++q) s += join[q * W + f];
-      A.partial[((int64_t)blockIdx.x * 2 + which) * A.F + f] = s;
+      A.partial[((int64_t)blockIdx.x * 2 + which) * A.F + f] = which == 0 ? s : A.scale * s;
     }
   }
 }
@@ -295,16 +332,19 @@ constexpr int kBlocksPerSm = 4;                            // most blocks per SM
 template <typename T, int VEC, int TEAM, int K>
 int32_t launch_one(bool backward, const NormArgs& A, int gate_kind, int sms, int* blocks, cudaStream_t st) {
   constexpr int THREADS = TEAM > 256 ? TEAM : 256, TEAMS = THREADS / TEAM;
-  const int64_t need = (A.rows + TEAMS - 1) / TEAMS;
   if (!backward) {
-    const int64_t most = (int64_t)sms * 64;
-    norm_forward<T, VEC, TEAM, K><<<(unsigned)(need < most ? need : most), THREADS, 0, st>>>(A, gate_kind);
+    constexpr int R = K * VEC <= 8 ? 2 : 1;
+    const int64_t need = (A.rows + TEAMS * R - 1) / (TEAMS * R);
+    const int64_t most = (int64_t)sms * 32;
+    norm_forward<T, VEC, TEAM, K, R><<<(unsigned)(need < most ? need : most), THREADS, 0, st>>>(A, gate_kind);
     return GNNCO_OK;
   }
+  constexpr int R = 1;
+  const int64_t need = (A.rows + TEAMS * R - 1) / (TEAMS * R);
   const size_t smem = (size_t)TEAMS * TEAM * K * VEC * sizeof(float);
   const int64_t most = (int64_t)sms * (THREADS > 256 ? 1 : kBlocksPerSm);
   *blocks = (int)(need < most ? need : most);
-  norm_backward<T, VEC, TEAM, K><<<*blocks, THREADS, smem, st>>>(A, gate_kind);
+  norm_backward<T, VEC, TEAM, K, R><<<*blocks, THREADS, smem, st>>>(A, gate_kind);
   return GNNCO_OK;
 }
 

@@ -85,13 +85,14 @@ int32_t lookup_typed(gnnco_handle* h, const int32_t* tokens, const TT* table, in
 
 // ---------------------------------------------------------------------------------------------------- order by token
 //
-// Stable least-significant-digit radix sort of the row numbers by token, 8 bits per pass, only as many passes as V has
-// bits.  A fixed number of blocks owns one contiguous span of positions each: block histograms (digit-major), one
-// block per digit scans that digit's row, and the scatter turns (digit total, row prefix) into output positions.
-// Rows without a token get key V and end up last.  `present` receives one bit per token that occurs.
-constexpr int kOrdThreads = 256, kOrdWarps = kOrdThreads / 32, kOrdRounds = 8;
+// Stable least-significant-digit radix sort of the row numbers by token, at most 8 bits per pass and only as many bits as
+// V has, shared evenly over the passes (20 bits: 7 + 7 + 6): fewer digits make longer runs of neighbouring writes.
+// A fixed number of blocks owns one contiguous span of positions each: block histograms (digit-major), one block per
+// digit scans that digit's row, and the scatter puts a tile in digit order in shared memory before it writes it out, so
+// that a digit's rows leave together.  Rows without a token get key V and end up last.
+constexpr int kOrdThreads = 512, kOrdWarps = kOrdThreads / 32, kOrdRounds = 8;
 constexpr int kOrdTile = kOrdThreads * kOrdRounds;         // positions of one block-wide step
-constexpr int kOrdMaxBlocks = 592;
+constexpr int kOrdMaxBlocks = 444;                         // 3 per SM: all resident at once
 constexpr int kSmallRows = 4096;                           // up to here one block sorts everything in shared memory
 
 struct PlanLayout {
@@ -101,7 +102,7 @@ struct PlanLayout {
   size_t bytes;
   int64_t chunks;
   int chunk;
-  int passes;
+  int passes, bits;                                        // bits per pass
 };
 
 int bits_of(int64_t x) {                                   // bits needed for values 0 .. x
@@ -110,11 +111,11 @@ int bits_of(int64_t x) {                                   // bits needed for va
   return b;
 }
 
-// Positions of one chunk of the gradient: enough chunks to fill the GPU, at most 256 so that a token's partial sums
-// stay few, at least 16 so that the chunk boundaries (a partial row each) do not outweigh the rows.
+// Positions of one chunk of the gradient: enough chunks to fill the GPU some times over, at most 256 so that a token's
+// partial sums stay few, at least 16 so that the chunk boundaries (a partial row each) do not outweigh the rows.
 int chunk_of(int64_t rows) {
   int c = 16;
-  while (c < 256 && rows / (2 * c) >= 148 * 32) c *= 2;
+  while (c < 256 && rows / (2 * c) >= 148 * 64) c *= 2;
   return c;
 }
 
@@ -122,6 +123,7 @@ PlanLayout plan_layout(void* ws, int64_t rows, int32_t V, int32_t F) {
   Carver c(ws, 0);
   PlanLayout L;
   L.passes = (bits_of(V) + 7) / 8;
+  L.bits = (bits_of(V) + L.passes - 1) / L.passes;
   L.chunk = chunk_of(rows);
   L.chunks = (rows + L.chunk - 1) / L.chunk;
   L.key_a = c.take<int32_t>(rows);
@@ -141,15 +143,29 @@ const int32_t* plan_rows(const PlanLayout& L) { return (L.passes & 1) ? L.idx_a 
 
 __device__ __forceinline__ int32_t token_key(int32_t t, int32_t V) { return (uint32_t)t < (uint32_t)V ? t : V; }
 
-// FIRST: keys come from the token vector (row number = position); tokens are checked and marked present.
+// lanes of the warp with the same BITS-bit digit (one ballot per bit: match.any serialises over the distinct digits)
+template <int BITS>
+__device__ __forceinline__ uint32_t same_digit(uint32_t d, bool valid) {
+  uint32_t peers = __ballot_sync(0xffffffffu, valid);
+#pragma unroll
+  for (int b = 0; b < BITS; ++b) {
+    const bool one = (d >> b) & 1u;
+    const uint32_t m = __ballot_sync(0xffffffffu, one);
+    peers &= one ? m : ~m;
+  }
+  return peers;
+}
+
+// FIRST: keys come from the token vector (row number = position); tokens are checked.
 template <bool FIRST>
 __global__ void __launch_bounds__(kOrdThreads) order_histogram(const int32_t* __restrict__ keys, int64_t N, int64_t span,
-                                                               int shift, int32_t V, int32_t* __restrict__ hist,
-                                                               uint32_t* present, int32_t* status) {
+                                                               int shift, int digits, int32_t V, int32_t* __restrict__ hist,
+                                                               int32_t* status) {
   __shared__ int32_t cnt[256];
-  cnt[threadIdx.x] = 0;
+  if (threadIdx.x < 256) cnt[threadIdx.x] = 0;
   __syncthreads();
   const int64_t lo = (int64_t)blockIdx.x * span, hi = min(N, lo + span);
+  bool wrong = false;
   for (int64_t p0 = lo; p0 < hi; p0 += kOrdThreads * 4) {
     int32_t k[4];
 #pragma unroll
@@ -159,22 +175,17 @@ __global__ void __launch_bounds__(kOrdThreads) order_histogram(const int32_t* __
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const int64_t p = p0 + u * kOrdThreads + threadIdx.x;
-      if (p >= hi) continue;
+      if (p0 + u * kOrdThreads + threadIdx.x >= hi) continue;
       if (FIRST) {
-        if (k[u] >= V) atomicMin(status, (int32_t)GNNCO_OUT_OF_RANGE);
+        wrong |= k[u] >= V;
         k[u] = token_key(k[u], V);
-        if (k[u] < V) {
-          const uint32_t bit = 1u << (k[u] & 31);
-          volatile uint32_t* word = present + (k[u] >> 5);
-          if (!(*word & bit)) atomicOr(present + (k[u] >> 5), bit);   // most rows find their bit set already
-        }
       }
-      atomicAdd(&cnt[(k[u] >> shift) & 255], 1);
+      atomicAdd(&cnt[(k[u] >> shift) & (digits - 1)], 1);
     }
   }
+  if (FIRST && wrong) atomicMin(status, (int32_t)GNNCO_OUT_OF_RANGE);
   __syncthreads();
-  hist[(int64_t)threadIdx.x * gridDim.x + blockIdx.x] = cnt[threadIdx.x];
+  if ((int)threadIdx.x < digits) hist[(int64_t)threadIdx.x * gridDim.x + blockIdx.x] = cnt[threadIdx.x];
 }
 
 // One block per digit: exclusive prefix of the digit's block counts (in place) and the digit's total.
@@ -199,7 +210,7 @@ __global__ void __launch_bounds__(1024) order_scan(int32_t* hist, int32_t* total
   if (threadIdx.x == 0) totals[blockIdx.x] = tot;
 }
 
-// exclusive prefix over 256 values, one per thread of a 256-thread block
+// exclusive prefix over one value per thread of the block's first 256 threads (the others pass 0)
 __device__ __forceinline__ int32_t scan256(int32_t x, int32_t* warp_tot) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int32_t incl = x;
@@ -208,7 +219,7 @@ __device__ __forceinline__ int32_t scan256(int32_t x, int32_t* warp_tot) {
     const int32_t o = __shfl_up_sync(0xffffffffu, incl, d);
     if (lane >= d) incl += o;
   }
-  if (lane == 31) warp_tot[warp] = incl;
+  if (warp < 8 && lane == 31) warp_tot[warp] = incl;
   __syncthreads();
   int32_t off = 0;
 #pragma unroll
@@ -218,20 +229,23 @@ __device__ __forceinline__ int32_t scan256(int32_t x, int32_t* warp_tot) {
 }
 
 template <bool FIRST>
-__global__ void __launch_bounds__(kOrdThreads) order_scatter(const int32_t* __restrict__ keys, const int32_t* __restrict__ idx,
+__global__ void __launch_bounds__(kOrdThreads, 3) order_scatter(const int32_t* __restrict__ keys, const int32_t* __restrict__ idx,
                                                              int32_t* __restrict__ keys_out, int32_t* __restrict__ idx_out,
-                                                             int64_t N, int64_t span, int shift, int32_t V,
+                                                             int64_t N, int64_t span, int shift, int digits, int32_t V,
                                                              const int32_t* __restrict__ hist, const int32_t* __restrict__ totals) {
-  __shared__ int32_t cnt[kOrdWarps][256];
-  __shared__ int32_t next[256];
-  __shared__ int32_t warp_tot[8];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int32_t base = scan256(totals[threadIdx.x], warp_tot);
-  next[threadIdx.x] = base + hist[(int64_t)threadIdx.x * gridDim.x + blockIdx.x];
+  extern __shared__ int32_t sm[];
+  int32_t* const sk = sm;                                  // the tile in digit order
+  int32_t* const si = sm + kOrdTile;
+  int32_t(*cnt)[256] = reinterpret_cast<int32_t(*)[256]>(sm + 2 * kOrdTile);
+  int32_t* const next = sm + 2 * kOrdTile + kOrdWarps * 256;   // [256] where a digit's next row goes, less its place in the tile
+  int32_t* const warp_tot = next + 256;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = threadIdx.x;
+  const bool owns = t < digits;
+  int32_t at = scan256(owns ? totals[t] : 0, warp_tot);    // of digit t
+  if (owns) at += hist[(int64_t)t * gridDim.x + blockIdx.x];
   const int64_t lo = (int64_t)blockIdx.x * span, hi = min(N, lo + span);
   for (int64_t p0 = lo; p0 < hi; p0 += kOrdTile) {
-#pragma unroll
-    for (int w = 0; w < kOrdWarps; ++w) cnt[w][threadIdx.x] = 0;
+    for (int q = t; q < kOrdWarps * 256; q += kOrdThreads) (&cnt[0][0])[q] = 0;
     __syncthreads();
     // ranks inside the warp's 256 consecutive positions, in position order
     int32_t k[kOrdRounds], v[kOrdRounds];
@@ -246,8 +260,8 @@ __global__ void __launch_bounds__(kOrdThreads) order_scatter(const int32_t* __re
 #pragma unroll
     for (int r = 0; r < kOrdRounds; ++r) {
       const bool valid = wbase + r * 32 + lane < hi;
-      const uint32_t d = valid ? (uint32_t)(k[r] >> shift) & 255u : 256u;
-      const uint32_t peers = __match_any_sync(0xffffffffu, d);
+      const uint32_t d = (uint32_t)(k[r] >> shift) & (uint32_t)(digits - 1);
+      const uint32_t peers = same_digit<8>(d, valid);
       const int before = __popc(peers & ((1u << lane) - 1u));
       rank[r] = valid ? cnt[warp][d] + before : 0;
       __syncwarp();
@@ -255,43 +269,58 @@ __global__ void __launch_bounds__(kOrdThreads) order_scatter(const int32_t* __re
       __syncwarp();
     }
     __syncthreads();
-    {
-      int32_t at = next[threadIdx.x];
+    int32_t total = 0;
+    if (owns)
+#pragma unroll
+      for (int w = 0; w < kOrdWarps; ++w) total += cnt[w][t];
+    const int32_t first = scan256(total, warp_tot);        // the digit's place in the tile
+    if (owns) {
+      int32_t c = first;
 #pragma unroll
       for (int w = 0; w < kOrdWarps; ++w) {
-        const int32_t c = cnt[w][threadIdx.x];
-        cnt[w][threadIdx.x] = at;
-        at += c;
+        const int32_t n = cnt[w][t];
+        cnt[w][t] = c;
+        c += n;
       }
-      next[threadIdx.x] = at;
+      next[t] = at - first;
+      at += total;
     }
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kOrdRounds; ++r) {
       if (wbase + r * 32 + lane < hi) {
-        const int32_t at = cnt[warp][(k[r] >> shift) & 255] + rank[r];
-        keys_out[at] = k[r];
-        idx_out[at] = v[r];
+        const int32_t q = cnt[warp][(k[r] >> shift) & (digits - 1)] + rank[r];
+        sk[q] = k[r];
+        si[q] = v[r];
+      }
+    }
+    __syncthreads();
+    const int here = (int)min((int64_t)kOrdTile, hi - p0);
+#pragma unroll
+    for (int r = 0; r < kOrdRounds; ++r) {
+      const int q = r * kOrdThreads + t;
+      if (q < here) {
+        const int32_t key = sk[q], to = next[(key >> shift) & (digits - 1)] + q;
+        keys_out[to] = key;
+        idx_out[to] = si[q];
       }
     }
     __syncthreads();
   }
 }
+constexpr size_t kScatterSmem = (size_t)(2 * kOrdTile + kOrdWarps * 256 + 256 + 8) * sizeof(int32_t);
 
-// All passes in one block for up to kSmallRows rows: 32 warps x 128 positions.
+// All passes in one block for up to kSmallRows rows: 32 warps x 128 positions, 5 bits per pass, so that the 32 x 32 counters
+// (digit-major) are one per thread and one scan over the block places everything.
 constexpr int kSmallThreads = 1024, kSmallRounds = kSmallRows / kSmallThreads;
-constexpr size_t kSmallSmem = (size_t)kSmallRows * 8 + 32 * 256 * 4;
-__global__ void __launch_bounds__(kSmallThreads) order_small(const int32_t* __restrict__ tokens, int32_t N, int32_t V, int passes,
+__global__ void __launch_bounds__(kSmallThreads) order_small(const int32_t* __restrict__ tokens, int32_t N, int32_t V, int bits,
                                                              int32_t* __restrict__ keys_out, int32_t* __restrict__ idx_out,
                                                              uint32_t* present, int32_t* status) {
-  extern __shared__ int32_t sm[];
-  int32_t* sk = sm;
-  int32_t* si = sm + kSmallRows;
-  int32_t(*cnt)[256] = reinterpret_cast<int32_t(*)[256]>(sm + 2 * kSmallRows);
-  __shared__ int32_t warp_tot[8];
+  __shared__ int32_t sk[kSmallRows], si[kSmallRows];
+  __shared__ int32_t cnt[32 * 33];                         // [digit][warp]
+  __shared__ int32_t tot[32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int w = threadIdx.x; w < (V + 31) / 32; w += kSmallThreads) present[w] = 0u;
-  __syncthreads();
   int32_t k[kSmallRounds], v[kSmallRounds];
   const int wbase = warp * (32 * kSmallRounds);
 #pragma unroll
@@ -301,51 +330,42 @@ __global__ void __launch_bounds__(kSmallThreads) order_small(const int32_t* __re
     if (t >= V) atomicMin(status, (int32_t)GNNCO_OUT_OF_RANGE);
     k[r] = token_key(t, V);
     v[r] = p;
-    if (p < N && k[r] < V) atomicOr(present + (k[r] >> 5), 1u << (k[r] & 31));
   }
-  for (int pass = 0; pass < passes; ++pass) {
-    const int shift = 8 * pass;
-    for (int q = threadIdx.x; q < 32 * 256; q += kSmallThreads) (&cnt[0][0])[q] = 0;
-    __syncthreads();
+  for (int shift = 0; shift < bits; shift += 5) {
+    cnt[lane * 33 + warp] = 0;
+    __syncwarp();                                          // a warp counts in its own column
     int rank[kSmallRounds];
 #pragma unroll
     for (int r = 0; r < kSmallRounds; ++r) {
       const bool valid = wbase + r * 32 + lane < N;
-      const uint32_t d = valid ? (uint32_t)(k[r] >> shift) & 255u : 256u;
-      const uint32_t peers = __match_any_sync(0xffffffffu, d);
+      const uint32_t d = (uint32_t)(k[r] >> shift) & 31u;
+      const uint32_t peers = same_digit<5>(d, valid);
       const int before = __popc(peers & ((1u << lane) - 1u));
-      rank[r] = valid ? cnt[warp][d] + before : 0;
+      rank[r] = valid ? cnt[d * 33 + warp] + before : 0;
       __syncwarp();
-      if (valid && before == 0) cnt[warp][d] += __popc(peers);
+      if (valid && before == 0) cnt[d * 33 + warp] += __popc(peers);
       __syncwarp();
     }
     __syncthreads();
-    // digit totals, their prefix, then the per-warp starts
-    int32_t total = 0;
-    if (threadIdx.x < 256)
-      for (int w = 0; w < 32; ++w) total += cnt[w][threadIdx.x];
-    int32_t incl = total;
+    // warp w scans digit w over the warps, then the digits' totals
+    const int32_t c = cnt[warp * 33 + lane];
+    int32_t incl = c;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const int32_t o = __shfl_up_sync(0xffffffffu, incl, d);
       if (lane >= d) incl += o;
     }
-    if (threadIdx.x < 256 && lane == 31) warp_tot[warp] = incl;
+    if (lane == 31) tot[warp] = incl;
     __syncthreads();
-    if (threadIdx.x < 256) {
-      int32_t at = incl - total;
-      for (int w = 0; w < warp; ++w) at += warp_tot[w];
-      for (int w = 0; w < 32; ++w) {
-        const int32_t c = cnt[w][threadIdx.x];
-        cnt[w][threadIdx.x] = at;
-        at += c;
-      }
-    }
+    int32_t before = lane < warp ? tot[lane] : 0;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) before += __shfl_xor_sync(0xffffffffu, before, d);
+    cnt[warp * 33 + lane] = before + incl - c;
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kSmallRounds; ++r) {
       if (wbase + r * 32 + lane < N) {
-        const int at = cnt[warp][(k[r] >> shift) & 255] + rank[r];
+        const int at = cnt[((k[r] >> shift) & 31) * 33 + warp] + rank[r];
         sk[at] = k[r];
         si[at] = v[r];
       }
@@ -357,7 +377,6 @@ __global__ void __launch_bounds__(kSmallThreads) order_small(const int32_t* __re
       k[r] = p < N ? sk[p] : 0;
       v[r] = p < N ? si[p] : 0;
     }
-    __syncthreads();
   }
 #pragma unroll
   for (int r = 0; r < kSmallRounds; ++r) {
@@ -365,8 +384,25 @@ __global__ void __launch_bounds__(kSmallThreads) order_small(const int32_t* __re
     if (p < N) {
       keys_out[p] = k[r];
       idx_out[p] = v[r];
+      if (k[r] < V && (p == 0 || sk[p - 1] != k[r])) atomicOr(present + (k[r] >> 5), 1u << (k[r] & 31));
     }
   }
+}
+
+// one bit per token that occurs, from the sorted keys (where a run begins)
+constexpr int kMarkPer = 8;
+__global__ void __launch_bounds__(256) order_mark(const int32_t* __restrict__ keys, int64_t N, int32_t V, uint32_t* present) {
+  const int64_t p0 = (int64_t)blockIdx.x * (256 * kMarkPer) + threadIdx.x;
+  int32_t k[kMarkPer], before[kMarkPer];
+#pragma unroll
+  for (int u = 0; u < kMarkPer; ++u) {
+    const int64_t p = p0 + u * 256;
+    k[u] = p < N ? keys[p] : V;
+    before[u] = p < N && p > 0 ? keys[p - 1] : -1;
+  }
+#pragma unroll
+  for (int u = 0; u < kMarkPer; ++u)
+    if (k[u] < V && before[u] != k[u]) atomicOr(present + (k[u] >> 5), 1u << (k[u] & 31));
 }
 
 // ------------------------------------------------------------------------------------------------------ gradient
@@ -375,35 +411,30 @@ __global__ void __launch_bounds__(kSmallThreads) order_small(const int32_t* __re
 // columns, so a token that holds a third of all rows costs no more than a thousand small ones.  A run that lies inside a
 // chunk goes straight to the table; the pieces of a run that crosses a chunk boundary meet in `partial`:
 // slot 0 = the chunk's first run, begun in an earlier chunk; slot 1 = its last run, begun here and continued in the next.
-// The blocks after the last chunk write the zero rows of tokens that do not occur.
+// A block whose chunks all lie inside one run (a token with thousands of rows) adds its teams' sums first and leaves them in
+// slot 0 of its first chunk.  The second kernel also writes the zero rows of tokens that do not occur.
+// Whether chunks [c, c + group) all exist and hold nothing but one token, whose run began before them.
+__device__ __forceinline__ bool is_solid(const int32_t* __restrict__ keys, int64_t N, int32_t V, int64_t c, int group, int chunk,
+                                         int64_t chunks) {
+  if (c == 0 || c + group > chunks) return false;
+  const int32_t k = keys[c * chunk - 1];
+  return k < V && keys[min(N, (c + group) * chunk) - 1] == k;
+}
+
 template <typename T, typename TO, int VEC, int TEAM>
 __global__ void __launch_bounds__(256) grad_chunks(const T* __restrict__ dout, int64_t dout_ld, const int32_t* __restrict__ keys,
                                                    const int32_t* __restrict__ idx, int64_t N, int32_t V, int32_t F, float scale,
-                                                   int chunk, int64_t chunks, unsigned chunk_blocks,
-                                                   const uint32_t* __restrict__ present, float* __restrict__ partial,
+                                                   int chunk, int64_t chunks, float* __restrict__ partial,
                                                    TO* __restrict__ out, int64_t out_ld) {
   constexpr int TEAMS = 256 / TEAM;
   constexpr int U = VEC >= 8 ? 8 : 16;
   const int tl = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
   const int col = (blockIdx.y * TEAM + tl) * VEC;
   const bool on = col < F;
-  if (blockIdx.x >= chunk_blocks) {
-    const int64_t v0 = ((int64_t)(blockIdx.x - chunk_blocks) * TEAMS + team) * 32;
-    if (v0 >= V || !on) return;
-    uint32_t gone = ~present[v0 >> 5];
-    if (V - v0 < 32) gone &= (1u << (V - v0)) - 1u;
-    float z[VEC];
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) z[e] = 0.0f;
-    while (gone) {
-      const int b = __ffs(gone) - 1;
-      gone &= gone - 1;
-      vio::store_stream<TO, VEC>(out + (v0 + b) * out_ld + col, z);
-    }
-    return;
-  }
-  const int64_t c = (int64_t)blockIdx.x * TEAMS + team;
-  if (c >= chunks) return;                                 // whole teams leave together (shuffles below name the team)
+  const int64_t cb = (int64_t)blockIdx.x * TEAMS, c = cb + team;
+  // one run from before this block's first position to its last (the same answer for the whole block)
+  const bool solid = is_solid(keys, N, V, cb, TEAMS, chunk, chunks);
+  if (c >= chunks) return;                                 // whole teams leave together (shuffles below name the team); never of a solid block
   const uint32_t mask = TEAM == 32 ? 0xffffffffu : ((1u << TEAM) - 1u) << ((threadIdx.x & 31) / TEAM * TEAM);
   const int64_t p0 = c * chunk, p1 = min(N, p0 + chunk);
   float acc[VEC];
@@ -457,6 +488,20 @@ __global__ void __launch_bounds__(256) grad_chunks(const T* __restrict__ dout, i
       }
     }
   }
+  if (solid) {
+    __shared__ float sums[TEAMS][TEAM * VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) sums[team][tl * VEC + e] = acc[e];
+    __syncthreads();
+    for (int q = threadIdx.x; q < TEAM * VEC; q += 256) {
+      const int f = blockIdx.y * TEAM * VEC + q;
+      float t = 0.0f;
+#pragma unroll
+      for (int k = 0; k < TEAMS; ++k) t += sums[k][q];
+      if (f < F) partial[cb * 2 * F + f] = t;
+    }
+    return;
+  }
   if (cur >= V || !on) return;
   const bool goes_on = p1 < N && keys[p1] == cur;
   if (head) to_partial(0);
@@ -464,77 +509,127 @@ __global__ void __launch_bounds__(256) grad_chunks(const T* __restrict__ dout, i
   else to_table();
 }
 
-// Runs that cross chunk boundaries: warp w of the block looks at chunk c0 + w; where a run begins there that continues,
-// the run's pieces are slot 1 of chunk c and slot 0 of the following chunks.  Few pieces are added by the warp, in chunk
-// order; many (a token with thousands of rows) by all warps of the block, each every 32nd piece, and the 32 sums in
-// warp order.  Grid.y covers the columns, 32 per block.
+// Runs that cross chunk boundaries: warp w of a block looks at chunk c0 + w; where a run begins there that continues, its
+// pieces are slot 1 of chunk c, slot 0 of the following chunks, and slot 0 of the first chunk of every solid group of
+// `group` chunks.  Up to four pieces are added by the warp, in order; more by the whole block: `wide` threads side by side
+// cover the columns, the 1,024 / wide rows of threads take every so-manieth piece, and their sums are added in order.
+// The blocks after the last chunk write the zero rows, 32 tokens per warp.
 constexpr int kCombineWarps = 32;
+struct Pieces {                                            // the pieces after the first, in order
+  int64_t c1;                                              // chunks c1 .. q0 - 1, then the groups from q0 on, then chunks
+  int32_t lead, groups, tail;
+  int group;
+  __device__ __forceinline__ int32_t count() const { return lead + groups + tail; }
+  __device__ __forceinline__ int64_t chunk(int32_t i) const {
+    if (i < lead) return c1 + i;
+    const int32_t g = i - lead;
+    return g < groups ? c1 + lead + (int64_t)g * group : c1 + lead + (int64_t)groups * group + (g - groups);
+  }
+};
 template <typename TO>
 __global__ void __launch_bounds__(kCombineWarps * 32) grad_combine(const int32_t* __restrict__ keys, int64_t N, int32_t V, int32_t F,
-                                                                   float scale, int chunk, int64_t chunks,
+                                                                   float scale, int chunk, int64_t chunks, int group, int wide,
+                                                                   bool vec4, unsigned chunk_blocks,
+                                                                   const uint32_t* __restrict__ present,
                                                                    const float* __restrict__ partial, TO* __restrict__ out,
                                                                    int64_t out_ld) {
-  __shared__ int32_t big_run[kCombineWarps];               // pieces after the first, 0: nothing to do for the block
-  __shared__ float sums[kCombineWarps][33];
+  __shared__ Pieces run[kCombineWarps];                    // count() == 0: nothing for the block to do
+  __shared__ float sums[kCombineWarps * 32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (blockIdx.x >= chunk_blocks) {
+    const int64_t v0 = ((int64_t)(blockIdx.x - chunk_blocks) * kCombineWarps + warp) * 32;
+    if (v0 >= V) return;
+    uint32_t gone = ~present[v0 >> 5];
+    if (V - v0 < 32) gone &= (1u << (V - v0)) - 1u;
+    const float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    while (gone) {
+      const int b = __ffs(gone) - 1;
+      gone &= gone - 1;
+      TO* const row = out + (v0 + b) * out_ld;
+      if (vec4) {
+        for (int col = 4 * lane; col < F; col += 128) vio::store_stream<TO, 4>(row + col, z);
+      } else {
+        const float z1[1] = {0.0f};
+        for (int col = lane; col < F; col += 32) vio::store_stream<TO, 1>(row + col, z1);
+      }
+    }
+    return;
+  }
   const int64_t c0 = (int64_t)blockIdx.x * kCombineWarps, c = c0 + warp;
-  const int col = blockIdx.y * 32 + lane;
-  const bool on = col < F;
-  int32_t more = 0, key = V;
+  Pieces r = {c + 1, 0, 0, 0, group};
+  int32_t key = V;
   if (c < chunks) {
     const int64_t p0 = c * chunk, p1 = min(N, p0 + chunk);
     key = keys[p1 - 1];
     if (key < V && p1 < N && keys[p1] == key && !(keys[p0] == key && p0 > 0 && keys[p0 - 1] == key)) {
-      for (int64_t b = c + 1; b < chunks; b += 32) {
-        const bool same = b + lane < chunks && keys[(b + lane) * chunk] == key;
-        const uint32_t m = __ballot_sync(0xffffffffu, same);
-        more += m == 0xffffffffu ? 32 : __ffs(~m) - 1;
-        if (m != 0xffffffffu) break;
+      // how many of the following chunks begin with the key: 32 probes at a time into a sorted list
+      int64_t at = c + 1, left = chunks - at;
+      while (left > 0) {
+        const int64_t stride = (left + 31) / 32, probe = at + lane * stride;
+        const bool same = lane * stride < left && keys[probe * chunk] == key;
+        const int hits = __popc(__ballot_sync(0xffffffffu, same));
+        if (hits == 0) break;
+        const int64_t past = (hits - 1) * stride + 1;      // this many are known to match; the next miss is within a stride
+        at += past;
+        left = min(stride - 1, left - past);
       }
+      // [c + 1, at) begin with the key; all but perhaps the last hold nothing else
+      const int64_t full = keys[min(N, at * chunk) - 1] == key ? at : at - 1;
+      const int64_t q0 = (c + 1 + group - 1) / group * group;
+      const int64_t groups = full > q0 ? (full - q0) / group : 0;
+      r.groups = (int32_t)groups;
+      r.lead = (int32_t)(groups > 0 ? q0 - (c + 1) : at - (c + 1));
+      r.tail = (int32_t)(groups > 0 ? at - (q0 + groups * group) : 0);
     }
   }
-  constexpr int kFew = 64;
-  if (more > 0 && more <= kFew && on) {
-    float s = partial[(c * 2 + 1) * F + col];
-    int32_t q = 1;
-    for (; q + 7 <= more; q += 8) {
-      float v[8];
+  constexpr int kFew = 4;
+  const int32_t more = r.count();
+  if (more > 0 && more <= kFew) {
+#pragma unroll 2
+    for (int col = lane; col < F; col += 32) {
+      float v[kFew + 1];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = partial[(c + q + u) * 2 * F + col];
+      for (int q = 0; q <= kFew; ++q)
+        v[q] = q == 0 ? partial[(c * 2 + 1) * F + col] : q <= more ? partial[r.chunk(q - 1) * 2 * F + col] : 0.0f;
+      float s = v[0];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) s += v[u];
+      for (int q = 1; q <= kFew; ++q) s += v[q];
+      const float f[1] = {scale * s};
+      vio::store_stream<TO, 1>(out + (int64_t)key * out_ld + col, f);
     }
-    for (; q <= more; ++q) s += partial[(c + q) * 2 * F + col];
-    float f[1] = {scale * s};
-    vio::store_stream<TO, 1>(out + (int64_t)key * out_ld + col, f);
   }
-  if (lane == 0) big_run[warp] = more > kFew ? more : 0;
+  if (lane == 0) {
+    run[warp] = r;
+    if (more <= kFew) run[warp].lead = run[warp].groups = run[warp].tail = 0;
+  }
   __syncthreads();
+  const int cx = (int)threadIdx.x % wide, ry = (int)threadIdx.x / wide, rows = kCombineWarps * 32 / wide;
   for (int w = 0; w < kCombineWarps; ++w) {
-    const int32_t m = big_run[w];
+    const Pieces big = run[w];
+    const int32_t m = big.count();
     if (m == 0) continue;
     const int64_t cw = c0 + w;
-    float s = warp == 0 && on ? partial[(cw * 2 + 1) * F + col] : 0.0f;
-    int32_t q = 1 + warp;
-    for (; q + 7 * kCombineWarps <= m; q += 8 * kCombineWarps) {
-      float v[8];
+    const int32_t key_w = keys[min(N, cw * chunk + chunk) - 1];
+    for (int col0 = 0; col0 < F; col0 += wide) {
+      const int col = col0 + cx;
+      const bool on = col < F;
+      float s = ry == 0 && on ? partial[(cw * 2 + 1) * F + col] : 0.0f;
+      for (int32_t q = ry; q < m; q += 8 * rows) {
+        float v[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = on ? partial[(cw + q + u * kCombineWarps) * 2 * F + col] : 0.0f;
+        for (int u = 0; u < 8; ++u) v[u] = on && q + u * rows < m ? partial[big.chunk(q + u * rows) * 2 * F + col] : 0.0f;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) s += v[u];
+        for (int u = 0; u < 8; ++u) s += v[u];
+      }
+      sums[threadIdx.x] = s;
+      __syncthreads();
+      if (ry == 0 && on) {
+        for (int k = 1; k < rows; ++k) s += sums[k * wide + cx];
+        const float f[1] = {scale * s};
+        vio::store_stream<TO, 1>(out + (int64_t)key_w * out_ld + col, f);
+      }
+      __syncthreads();
     }
-    for (; q <= m; q += kCombineWarps) s += on ? partial[(cw + q) * 2 * F + col] : 0.0f;
-    sums[warp][lane] = s;
-    __syncthreads();
-    if (warp == 0 && on) {
-      float t = 0.0f;
-#pragma unroll
-      for (int k = 0; k < kCombineWarps; ++k) t += sums[k][lane];
-      const int32_t key_w = keys[min(N, cw * chunk + chunk) - 1];
-      float f[1] = {scale * t};
-      vio::store_stream<TO, 1>(out + (int64_t)key_w * out_ld + col, f);
-    }
-    __syncthreads();
   }
 }
 
@@ -545,22 +640,26 @@ int32_t grad_vec(gnnco_handle* h, const PlanLayout& L, const T* dout, int64_t do
   const int team = vecs <= 8 ? 8 : vecs <= 16 ? 16 : 32;
   const int teams = 256 / team;
   const unsigned cb = (unsigned)((L.chunks + teams - 1) / teams);
-  const unsigned zb = (unsigned)(((int64_t)(V + 31) / 32 + teams - 1) / teams);
-  const dim3 grid(cb + zb, (unsigned)((vecs + team - 1) / team));
+  const dim3 grid(cb, (unsigned)((vecs + team - 1) / team));
   const int32_t *keys = plan_keys(L), *idx = plan_rows(L);
-#define GNNCO_GRAD(TM)                                                                                                     \
-  grad_chunks<T, TO, VEC, TM><<<grid, 256, 0, st>>>(dout, dout_ld, keys, idx, rows, V, F, scale, L.chunk, L.chunks, cb, \
-                                                   L.present, L.partial, out, out_ld)
-  if (team == 8) GNNCO_GRAD(8);
-  else if (team == 16) GNNCO_GRAD(16);
-  else GNNCO_GRAD(32);
+  if (L.chunks > 0) {
+#define GNNCO_GRAD(TM)                                                                                                 \
+  grad_chunks<T, TO, VEC, TM><<<grid, 256, 0, st>>>(dout, dout_ld, keys, idx, rows, V, F, scale, L.chunk, L.chunks, \
+                                                   L.partial, out, out_ld)
+    if (team == 8) GNNCO_GRAD(8);
+    else if (team == 16) GNNCO_GRAD(16);
+    else GNNCO_GRAD(32);
 #undef GNNCO_GRAD
-  h->launches += 1;
-  if (L.chunks > 1) {
-    grad_combine<TO><<<dim3((unsigned)((L.chunks + kCombineWarps - 1) / kCombineWarps), (unsigned)((F + 31) / 32)),
-                       kCombineWarps * 32, 0, st>>>(keys, rows, V, F, scale, L.chunk, L.chunks, L.partial, out, out_ld);
     h->launches += 1;
   }
+  const unsigned pb = (unsigned)((L.chunks + kCombineWarps - 1) / kCombineWarps);
+  const unsigned zb = (unsigned)(((int64_t)V + 32 * kCombineWarps - 1) / (32 * kCombineWarps));
+  int wide = 32;
+  while (wide < 256 && wide < F) wide *= 2;
+  const bool vec4 = F % 4 == 0 && vec_ok(out, out_ld, sizeof(TO), 4);
+  grad_combine<TO><<<pb + zb, kCombineWarps * 32, 0, st>>>(keys, rows, V, F, scale, L.chunk, L.chunks, teams, wide, vec4, pb, L.present,
+                                                         L.partial, out, out_ld);
+  h->launches += 1;
   GNNCO_LAUNCH_CHECK();
   return GNNCO_OK;
 }
@@ -619,33 +718,39 @@ extern "C" int32_t gnnco_embedding_plan(gnnco_handle* h, const int32_t* tokens, 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   ProfScope prof_(h, K_EMBED, st);
   if (rows > 0 && rows <= kSmallRows) {
-    GNNCO_CUDA_TRY(cudaFuncSetAttribute(order_small, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallSmem));
-    order_small<<<1, kSmallThreads, kSmallSmem, st>>>(tokens, (int32_t)rows, V, L.passes, const_cast<int32_t*>(plan_keys(L)),
-                                                     const_cast<int32_t*>(plan_rows(L)), L.present, h->status);
+    order_small<<<1, kSmallThreads, 0, st>>>(tokens, (int32_t)rows, V, bits_of(V), const_cast<int32_t*>(plan_keys(L)),
+                                             const_cast<int32_t*>(plan_rows(L)), L.present, h->status);
     h->launches += 1;
     GNNCO_LAUNCH_CHECK();
     return GNNCO_OK;
   }
   GNNCO_CUDA_TRY(cudaMemsetAsync(L.present, 0, ((size_t)V + 31) / 32 * 4, st));
   if (rows == 0) return GNNCO_OK;
+  GNNCO_CUDA_TRY(cudaFuncSetAttribute(order_scatter<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kScatterSmem));
+  GNNCO_CUDA_TRY(cudaFuncSetAttribute(order_scatter<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kScatterSmem));
   const int64_t tiles = (rows + kOrdTile - 1) / kOrdTile;
   const int64_t per = (tiles + kOrdMaxBlocks - 1) / kOrdMaxBlocks;
   const int64_t span = per * kOrdTile;
-  const int nb = (int)((rows + span - 1) / span);
+  const int nb = (int)((rows + span - 1) / span), digits = 1 << L.bits;
   int32_t *ka = L.key_a, *ia = L.idx_a, *kb = L.key_b, *ib = L.idx_b;
   const int32_t* kin = tokens;
   const int32_t* iin = nullptr;
   for (int p = 0; p < L.passes; ++p) {
-    if (p == 0) order_histogram<true><<<nb, kOrdThreads, 0, st>>>(kin, rows, span, 0, V, L.hist, L.present, h->status);
-    else order_histogram<false><<<nb, kOrdThreads, 0, st>>>(kin, rows, span, 8 * p, V, L.hist, nullptr, nullptr);
-    order_scan<<<256, 1024, 0, st>>>(L.hist, L.totals, nb);
-    if (p == 0) order_scatter<true><<<nb, kOrdThreads, 0, st>>>(kin, iin, ka, ia, rows, span, 0, V, L.hist, L.totals);
-    else order_scatter<false><<<nb, kOrdThreads, 0, st>>>(kin, iin, ka, ia, rows, span, 8 * p, V, L.hist, L.totals);
+    const int shift = p * L.bits;
+    if (p == 0) order_histogram<true><<<nb, kOrdThreads, 0, st>>>(kin, rows, span, shift, digits, V, L.hist, h->status);
+    else order_histogram<false><<<nb, kOrdThreads, 0, st>>>(kin, rows, span, shift, digits, V, L.hist, nullptr);
+    order_scan<<<digits, 1024, 0, st>>>(L.hist, L.totals, nb);
+    if (p == 0)
+      order_scatter<true><<<nb, kOrdThreads, kScatterSmem, st>>>(kin, iin, ka, ia, rows, span, shift, digits, V, L.hist, L.totals);
+    else
+      order_scatter<false><<<nb, kOrdThreads, kScatterSmem, st>>>(kin, iin, ka, ia, rows, span, shift, digits, V, L.hist, L.totals);
     kin = ka; iin = ia;
     int32_t* t = ka; ka = kb; kb = t;
     t = ia; ia = ib; ib = t;
     h->launches += 3;
   }
+  order_mark<<<(unsigned)((rows + 256 * kMarkPer - 1) / (256 * kMarkPer)), 256, 0, st>>>(kin, rows, V, L.present);
+  h->launches += 1;
   GNNCO_LAUNCH_CHECK();
   return GNNCO_OK;
 }

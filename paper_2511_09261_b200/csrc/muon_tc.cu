@@ -31,6 +31,8 @@
 #include <cuda_fp16.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "muon_internal.cuh"
 #include "muon_limbs.cuh"
 #include "tc_common.cuh"
@@ -38,18 +40,28 @@
 
 namespace {
 
-constexpr int kWorkWarps = 16, kMmaWarp = 16, kSideWarp = 17, kThreads = 32 * (kWorkWarps + 2);
 
-template <bool PAIR>
+// kDual: both sides up to 128, two CTAs per SM (while one converts, the other's products run); kWide: short side up to 128,
+// long side up to 256, one CTA per SM; kPair: sides up to 256, two CTAs on two SMs.
+constexpr int kDual = 0, kWide = 1, kPair = 2;
+
+template <int MODE>
 struct Cfg {
-  static constexpr int CTAS = PAIR ? 2 : 1;
-  static constexpr uint32_t X_BYTES = 2 * 4 * kPanel;
-  static constexpr int A_HI = PAIR ? 4 : 2, A_LO = 2;      // panels of A's limbs in shared memory
-  static constexpr uint32_t A_BYTES = (A_HI + A_LO) * kPanel;
-  static constexpr uint32_t MISC = 1024;
-  static constexpr size_t SMEM = 1024 + X_BYTES + A_BYTES + MISC;
-  static constexpr uint32_t ACC1 = 0, ACC2 = PAIR ? 256 : 128, ACC3 = 256;   // TMEM columns
-  static_assert(SMEM <= 232448, "does not fit in shared memory");
+  static constexpr bool PAIR = MODE == kPair;
+  static constexpr int CTAS = PAIR ? 2 : 1, PER_SM = MODE == kDual ? 2 : 1;
+  static constexpr int WORK = MODE == kDual ? 8 : 16;      // working warps; then the MMA warp and the side warp
+  static constexpr int SUBS = WORK / 4, THREADS = 32 * (WORK + 2);
+  static constexpr int XP = MODE == kDual ? 2 : 4;         // panels of X per limb
+  static constexpr int A_HI = PAIR ? 4 : 2, A_LO = MODE == kDual ? 1 : 2;   // panels of A's limbs in shared memory
+  static constexpr bool LATE = A_LO < A_HI;                // the low limb's second half follows into the room of the first
+  static constexpr uint32_t X_BYTES = 2 * XP * kPanel, A_BYTES = (A_HI + A_LO) * kPanel, MISC = 1024;
+  // two CTAs fill an SM's shared memory to the byte: no slack for aligning the base, which starts on 1,024 bytes
+  static constexpr uint32_t SLACK = MODE == kDual ? 0 : 1024;
+  static constexpr size_t SMEM = SLACK + X_BYTES + A_BYTES + MISC;
+  static constexpr uint32_t ACC1 = 0, ACC2 = PAIR ? 256 : 128, ACC3 = MODE == kDual ? 128 : 256;   // TMEM columns
+  static constexpr bool SHARED_ACC = ACC2 == ACC3;
+  static constexpr uint32_t TMEM = MODE == kDual ? 256 : 512;
+  static_assert(SMEM <= 232448 && PER_SM * (SMEM + 1024) <= 233472, "does not fit in shared memory");
 };
 
 struct Bars {
@@ -89,10 +101,12 @@ struct Waiter {
 };
 
 // VEC4: float32 matrices whose rows are X's rows and multiples of 16 bytes; else any type, order and alignment.
-template <bool PAIR, bool VEC4>
-__global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
-  using C = Cfg<PAIR>;
-  extern __shared__ uint8_t smem_raw[];
+template <int MODE, bool VEC4>
+__global__ void __launch_bounds__(Cfg<MODE>::THREADS, Cfg<MODE>::PER_SM) ns_on_chip(const NsJob J) {
+  using C = Cfg<MODE>;
+  constexpr bool PAIR = C::PAIR;
+  constexpr int kWorkWarps = C::WORK, kMmaWarp = C::WORK, kSideWarp = C::WORK + 1, SUBS = C::SUBS;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t sbase = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t sX = sbase, sA = sbase + C::X_BYTES;
   uint8_t* gen = smem_raw + (sbase - tc::smem_u32(smem_raw));
@@ -101,6 +115,10 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
   volatile uint32_t* abort_flag = tmem_slot + 1;
   double* sums = reinterpret_cast<double*>(gen + C::X_BYTES + C::A_BYTES + 512);   // [16] own warps, [2] the partner's total
 
+  if (C::SLACK == 0 && sbase != tc::smem_u32(smem_raw)) {  // the base is not where it has to be: nothing fits
+    if (threadIdx.x == 0) atomicMin(J.status, (int32_t)GNNCO_INTERNAL);
+    return;
+  }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = PAIR ? tc::cluster_ctarank() : 0u;
   const int64_t group = blockIdx.x / C::CTAS, groups = gridDim.x / C::CTAS;
@@ -119,7 +137,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
       tc::mbar_init(&B->p[p], quarters * panel_items(a_items, p) * C::CTAS);
     }
     tc::mbar_init(&B->m1, 1); tc::mbar_init(&B->m2, 1); tc::mbar_init(&B->m3, 1); tc::mbar_init(&B->lofree, 1);
-    tc::mbar_init(&B->l, 4 * (a_items > 4 ? a_items - 4 : 1) * C::CTAS);
+    tc::mbar_init(&B->l, quarters * (a_items > SUBS ? a_items - SUBS : 1) * C::CTAS);
     // items of the off-diagonal half that this CTA writes: the upper columns in the even CTA, the lower ones in the odd
     tc::mbar_init(&B->own, 4 * (rank == 0 ? (x_items > 4 ? x_items - 4 : 1) : 4));
     tc::mbar_init(&B->g, 1);
@@ -129,8 +147,8 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
     tc::fence_mbar_init();
   }
   if (warp == 0) {
-    if constexpr (PAIR) tc::tmem_alloc_pair(tmem_slot, 512);
-    else tc::tmem_alloc(tmem_slot, 512);
+    if constexpr (PAIR) tc::tmem_alloc_pair(tmem_slot, C::TMEM);
+    else tc::tmem_alloc(tmem_slot, C::TMEM);
   }
   tc::tc_fence_before_sync();
   __syncthreads();
@@ -158,9 +176,9 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
       };
       // Everything a product needs is a base plus constants, so that an MMA costs the issuing thread a few instructions:
       // 16 of k are 32 bytes of a k-major row, 2,048 bytes of n-major rows and 8 columns of tensor memory.
-      const uint64_t xh = tc::smem_desc_sw128(sX, 16, 1024), xl = tc::smem_desc_sw128(sX + 4 * kPanel, 16, 1024);
+      const uint64_t xh = tc::smem_desc_sw128(sX, 16, 1024), xl = tc::smem_desc_sw128(sX + C::XP * kPanel, 16, 1024);
       const uint64_t ah = tc::smem_desc_sw128(sA, 16, 1024), al = tc::smem_desc_sw128(sA + C::A_HI * kPanel, 16, 1024);
-      const uint64_t nh = tc::smem_desc_sw128(sX, kPanel, 1024), nl = tc::smem_desc_sw128(sX + 4 * kPanel, kPanel, 1024);
+      const uint64_t nh = tc::smem_desc_sw128(sX, kPanel, 1024), nl = tc::smem_desc_sw128(sX + C::XP * kPanel, kPanel, 1024);
       constexpr uint64_t kDescPanel = kPanel >> 4;
       auto n_off = [](int p) {                             // rows 64 p .. of X: in a pair rows 128 .. are in panels 2 and 3
         return (uint64_t)((PAIR ? (p >> 1) * 2 * kPanel + (p & 1) * 8192u : (uint32_t)p * 8192u) >> 4);
@@ -201,44 +219,44 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
             commit(&B->m1);
           }
           if (rank == 0) {
-            if constexpr (PAIR) {                          // A A: what reads the first half of A's low limb comes first
-              for (int p = 0; p < 2 && ok; ++p) {
+            if constexpr (C::LATE) {                       // A A: what reads the first half of A's low limb comes first
+              for (int p = 0; p < C::A_LO && ok; ++p) {
                 ok = wait_both(&B->a[p], ph);
                 tc::tc_fence_after_sync();
-                if (ok) steps_of(p, 8, [&](int q) { tc::mma_f16<true, true>(leader, acc2, lefth(p, q), al + p * kDescPanel + 2 * q, i1, p + q != 0); });
+                if (ok) steps_of(p, tk, [&](int q) { tc::mma_f16<PAIR, true>(leader, acc2, lefth(p, q), al + p * kDescPanel + 2 * q, i1, p + q != 0); });
               }
               if (!ok) break;
               commit(&B->lofree);
             }
             for (int p = 0; 4 * p < tk && ok; ++p) {
-              if (!PAIR || p >= 2) {
+              if (!C::LATE || p >= C::A_LO) {
                 ok = wait_both(&B->a[p], ph);
                 tc::tc_fence_after_sync();
               }
               if (ok) steps_of(p, tk, [&](int q) {
                 const uint64_t o = p * kDescPanel + 2 * q;
-                tc::mma_f16<PAIR, true>(leader, acc2, leftl(p, q), ah + o, i1, PAIR || p + q != 0);
-                if constexpr (!PAIR) tc::mma_f16<PAIR, true>(leader, acc2, lefth(p, q), al + o, i1, true);
+                tc::mma_f16<PAIR, true>(leader, acc2, leftl(p, q), ah + o, i1, C::LATE || p + q != 0);
+                if constexpr (!C::LATE) tc::mma_f16<PAIR, true>(leader, acc2, lefth(p, q), al + o, i1, true);
               });
             }
-            if constexpr (PAIR) {
+            if (C::LATE && 4 * C::A_LO < tk) {
               ok = ok && wait_both(&B->l, ph);
               tc::tc_fence_after_sync();
-              for (int p = 2; 4 * p < tk && ok; ++p)
-                steps_of(p, tk, [&](int q) { tc::mma_f16<true, true>(leader, acc2, lefth(p, q), al + (p - 2) * kDescPanel + 2 * q, i1, true); });
+              for (int p = C::A_LO; 4 * p < tk && ok; ++p)
+                steps_of(p, tk, [&](int q) { tc::mma_f16<PAIR, true>(leader, acc2, lefth(p, q), al + (p - C::A_LO) * kDescPanel + 2 * q, i1, true); });
             }
             if (!ok) break;
             for (int p = 0; 4 * p < tk; ++p)
               steps_of(p, tk, [&](int q) { tc::mma_f16<PAIR, true>(leader, acc2, lefth(p, q), ah + p * kDescPanel + 2 * q, i1, true); });
             commit(&B->m2);
-            // P X.  In a pair the accumulator is the one A A is read from: all of P must be there.
-            if constexpr (PAIR) {
+            // P X.  Where the accumulator is the one A A is read from, all of P must be there.
+            if constexpr (C::SHARED_ACC) {
               for (int p = 0; 4 * p < tk; ++p) ok = ok && wait_both(&B->p[p], ph);
-              ok = ok && wait(&B->s, ph) && wait_both(&B->s2, ph);
+              if (PAIR) ok = ok && wait(&B->s, ph) && wait_both(&B->s2, ph);
               tc::tc_fence_after_sync();
             }
             for (int p = 0; 4 * p < tk && ok; ++p) {
-              if (!PAIR) {
+              if (!C::SHARED_ACC) {
                 ok = wait(&B->p[p], ph);
                 tc::tc_fence_after_sync();
               }
@@ -288,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
             const uint32_t mine = (rank == 0 ? 2 : 0) * kPanel;           // the two panels that change hands
             if (!(ok = wait(&B->own, ph))) break;
             for (int limb = 0; limb < 2; ++limb)
-              tc::bulk_store(scratch + (rank * 2 + limb) * 2 * kPanel, sX + limb * 4 * kPanel + mine, 2 * kPanel);
+              tc::bulk_store(scratch + (rank * 2 + limb) * 2 * kPanel, sX + limb * C::XP * kPanel + mine, 2 * kPanel);
             tc::bulk_store_wait();
             tc::fence_proxy_async_all();
             tc::mbar_arrive_release_cluster(tc::map_to_cta(tc::smem_u32(&B->g), rank ^ 1u));
@@ -297,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
             tc::fence_proxy_async_all();
             tc::mbar_arrive_expect_tx(&B->s, 4 * kPanel);
             for (int limb = 0; limb < 2; ++limb)
-              tc::bulk_load(sX + limb * 4 * kPanel + mine, scratch + ((rank ^ 1u) * 2 + limb) * 2 * kPanel, 2 * kPanel, &B->s);
+              tc::bulk_load(sX + limb * C::XP * kPanel + mine, scratch + ((rank ^ 1u) * 2 + limb) * 2 * kPanel, 2 * kPanel, &B->s);
             if (!(ok = wait(&B->s, ph))) break;
             if (rank == 1) tc::mbar_arrive_release_cluster(tc::map_to_cta(tc::smem_u32(&B->s2), 0));
           }
@@ -324,11 +342,11 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
     };
     // chunk: 8 columns, counted over the row
     auto put_chunk = [&](int limb, int r, int chunk, const uint32_t* v) {
-      tc::st_shared16(sX + (limb * 4 + (chunk >> 3)) * kPanel + at_chunk(r, chunk & 7), v[0], v[1], v[2], v[3]);
+      tc::st_shared16(sX + (limb * C::XP + (chunk >> 3)) * kPanel + at_chunk(r, chunk & 7), v[0], v[1], v[2], v[3]);
     };
     // the loader's unit: 4 columns of a row, 8 bytes in each limb
     auto unit_at = [&](int limb, int r, int unit) {
-      return sX + (limb * 4 + (unit >> 4)) * kPanel + at_chunk(r, (unit >> 1) & 7) + (unit & 1) * 8;
+      return sX + (limb * C::XP + (unit >> 4)) * kPanel + at_chunk(r, (unit >> 1) & 7) + (unit & 1) * 8;
     };
     const int upr = (nc + 31) / 32 * 8;                    // units per row that are kept (whole items)
     const int rows_kept = quarters * 32, total = rows_kept * upr;
@@ -410,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
           // are summed again below
           sum += (double)(g[y][0] * g[y][0] + g[y][1] * g[y][1] + g[y][2] * g[y][2] + g[y][3] * g[y][3]);
           st_shared8(place[y], __float_as_uint(g[y][0]), __float_as_uint(g[y][1]));
-          st_shared8(place[y] + 4 * kPanel, __float_as_uint(g[y][2]), __float_as_uint(g[y][3]));
+          st_shared8(place[y] + C::XP * kPanel, __float_as_uint(g[y][2]), __float_as_uint(g[y][3]));
         }
       }
       double norm2 = 0.0;
@@ -448,7 +466,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
         int a2 = first_a, b2 = first_b;
         for (int q = threadIdx.x; q < total; q += kStride, next_unit(a2, b2)) {
           const uint32_t p = by_row ? unit_at(0, a2, b2) : unit_at(0, b2, a2);
-          const float2 x = ld_shared8(p), y = ld_shared8(p + 4 * kPanel);
+          const float2 x = ld_shared8(p), y = ld_shared8(p + C::XP * kPanel);
           sum += (double)x.x * x.x + (double)x.y * x.y + ((double)y.x * y.x + (double)y.y * y.y);
         }
         if (!total_of(sum)) break;
@@ -459,18 +477,18 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
 #pragma unroll 4
       for (int q = threadIdx.x; q < total; q += kStride, next_unit(ua, ub)) {
         const uint32_t p = by_row ? unit_at(0, ua, ub) : unit_at(0, ub, ua);
-        const float2 x = ld_shared8(p), y = ld_shared8(p + 4 * kPanel);
+        const float2 x = ld_shared8(p), y = ld_shared8(p + C::XP * kPanel);
         uint32_t hi[2], lo[2];
         split2(x.x * f, x.y * f, hi[0], lo[0]);
         split2(y.x * f, y.y * f, hi[1], lo[1]);
         st_shared8(p, hi[0], hi[1]);
-        st_shared8(p + 4 * kPanel, lo[0], lo[1]);
+        st_shared8(p + C::XP * kPanel, lo[0], lo[1]);
       }
       tc::fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&B->loaded);
       if (!wait(&B->loaded, mat & 1)) break;
-      for (int item = sub; item < 8; item += 4) x_ready(item);
+      for (int item = sub; item < 2 * C::XP; item += SUBS) x_ready(item);
 
       bool ok = true;
       for (int step = 0; step < J.steps; ++step, ++it) {
@@ -479,7 +497,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
         if (!(ok = wait(&B->m1, ph))) break;
         tc::tc_fence_after_sync();
         uint32_t hi[16], lo[16];
-        for (int item = sub; item < a_items; item += 4) {
+        for (int item = sub; item < a_items; item += SUBS) {
           if (!works) break;
           uint32_t v[32];
           tc::tmem_ld_32x32(tmem + C::ACC1 + lanes + item * 32, v);
@@ -493,7 +511,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             tc::st_shared16(sA + panel * kPanel + at_chunk(row, c0 + e), hi[4 * e], hi[4 * e + 1], hi[4 * e + 2], hi[4 * e + 3]);
-          if (!PAIR || panel < 2) {
+          if (!C::LATE || panel < C::A_LO) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               tc::st_shared16(sA + (C::A_HI + panel) * kPanel + at_chunk(row, c0 + e), lo[4 * e], lo[4 * e + 1], lo[4 * e + 2], lo[4 * e + 3]);
@@ -504,14 +522,14 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
           __syncwarp();
           if (lane == 0) arrive(&B->a[panel]);
         }
-        if (PAIR) {
+        if (C::LATE) {
           // the low limb's second half, still in registers, follows into the room of the first
           if (!(ok = wait(&B->lofree, ph))) break;
-          const int item = sub + 4;
-          if (item < a_items) {
+          const int item = sub + SUBS;
+          if (works && item < a_items) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              tc::st_shared16(sA + (C::A_HI + (item >> 1) - 2) * kPanel + at_chunk(row, (item & 1) * 4 + e), lo[4 * e], lo[4 * e + 1],
+              tc::st_shared16(sA + (C::A_HI + (item >> 1) - C::A_LO) * kPanel + at_chunk(row, (item & 1) * 4 + e), lo[4 * e], lo[4 * e + 1],
                               lo[4 * e + 2], lo[4 * e + 3]);
             tc::fence_proxy_async_smem();
             __syncwarp();
@@ -523,7 +541,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
         tc::tc_fence_after_sync();
         const float fi = J.a * J.p_scale, fa1 = J.b * J.p_scale / kAScale, faa1 = J.cc * J.p_scale / (kAScale * kAScale);
         const uint64_t fa = pair_of(fa1, fa1), faa = pair_of(faa1, faa1);
-        for (int item = sub; item < a_items; item += 4) {
+        for (int item = sub; item < a_items; item += SUBS) {
           if (!works) break;
           uint32_t v[32];
           tc::tmem_ld_32x32(tmem + C::ACC2 + lanes + item * 32, v);
@@ -557,7 +575,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
           if (!(ok = wait(&B->m3, ph))) break;
           tc::tc_fence_after_sync();
           const uint64_t f3 = pair_of(1.0f / J.p_scale, 1.0f / J.p_scale);
-          for (int item = sub; item < x_items; item += 4) {
+          for (int item = sub; item < x_items; item += SUBS) {
             if (!works) break;
             uint32_t v[32];
             tc::tmem_ld_32x32(tmem + C::ACC3 + lanes + item * 32, v);
@@ -581,7 +599,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
         const float fo = 1.0f / (J.p_scale * kXScale), keep = J.keep, step_w = J.step;
         const uint32_t stage = sX + warp * 4096;
         bool waited = false;
-        for (int item = sub; item < 8; item += 4) {
+        for (int item = sub; item < 2 * C::XP; item += SUBS) {
           const bool in = works && item < x_items;
           // the lane's values are `hop` apart: VEC4: 4 columns of every fourth row; rows of W: its 32 rows at one column;
           // columns of W (transposed): its 32 columns of one row of X
@@ -668,20 +686,20 @@ __global__ void __launch_bounds__(kThreads, 1) ns_on_chip(const NsJob J) {
   __syncthreads();
   if constexpr (PAIR) {
     tc::cluster_sync_all();
-    if (warp == 0) tc::tmem_dealloc_pair(tmem, 512);
+    if (warp == 0) tc::tmem_dealloc_pair(tmem, C::TMEM);
   } else {
-    if (warp == 0) tc::tmem_dealloc(tmem, 512);
+    if (warp == 0) tc::tmem_dealloc(tmem, C::TMEM);
   }
 }
 
-template <bool PAIR>
+template <int MODE>
 void launch_shape(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* attr, int ctas, cudaStream_t st) {
   cfg.gridDim = dim3(ctas);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = Cfg<PAIR>::SMEM;
+  cfg.blockDim = dim3(Cfg<MODE>::THREADS);
+  cfg.dynamicSmemBytes = Cfg<MODE>::SMEM;
   cfg.stream = st;
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = Cfg<PAIR>::CTAS;
+  attr[0].val.clusterDim.x = Cfg<MODE>::CTAS;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
@@ -690,15 +708,15 @@ void launch_shape(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* attr, int ctas, 
 // CTA pairs that can be resident at once (asked once per process; 0: none)
 int resident_pairs() {
   static const int pairs = [] {
-    if (cudaFuncSetAttribute((ns_on_chip<true, true>), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<true>::SMEM) != cudaSuccess) {
+    if (cudaFuncSetAttribute((ns_on_chip<kPair, true>), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<kPair>::SMEM) != cudaSuccess) {
       cudaGetLastError();
       return 0;
     }
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute attr[1];
-    launch_shape<true>(cfg, attr, 2 * 148, nullptr);
+    launch_shape<kPair>(cfg, attr, 2 * 148, nullptr);
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, (ns_on_chip<true, true>), &cfg) != cudaSuccess) {
+    if (cudaOccupancyMaxActiveClusters(&n, (ns_on_chip<kPair, true>), &cfg) != cudaSuccess) {
       cudaGetLastError();
       n = 0;
     }
@@ -707,14 +725,14 @@ int resident_pairs() {
   return pairs;
 }
 
-template <bool PAIR, bool VEC4>
+template <int MODE, bool VEC4>
 int32_t launch(gnnco_handle* h, const NsJob& job, int64_t groups, cudaStream_t st) {
-  GNNCO_CUDA_TRY(cudaFuncSetAttribute(ns_on_chip<PAIR, VEC4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<PAIR>::SMEM));
+  GNNCO_CUDA_TRY(cudaFuncSetAttribute((ns_on_chip<MODE, VEC4>), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<MODE>::SMEM));
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[1];
   if (groups > job.sets) groups = job.sets;
-  launch_shape<PAIR>(cfg, attr, (int)groups * Cfg<PAIR>::CTAS, st);
-  GNNCO_CUDA_TRY(cudaLaunchKernelEx(&cfg, ns_on_chip<PAIR, VEC4>, job));
+  launch_shape<MODE>(cfg, attr, (int)groups * Cfg<MODE>::CTAS, st);
+  GNNCO_CUDA_TRY(cudaLaunchKernelEx(&cfg, (ns_on_chip<MODE, VEC4>), job));
   h->launches += 1;
   return GNNCO_OK;
 }
@@ -734,6 +752,11 @@ size_t ns_on_chip_scratch_bytes(const gnnco_handle* h, int64_t sets, int32_t k, 
 }
 
 int32_t launch_ns_on_chip(gnnco_handle* h, const NsJob& job, cudaStream_t st) {
-  if (job.k <= 128) return job.vec4 ? launch<false, true>(h, job, h->sm_count, st) : launch<false, false>(h, job, h->sm_count, st);
-  return job.vec4 ? launch<true, true>(h, job, resident_pairs(), st) : launch<true, false>(h, job, resident_pairs(), st);
+  auto run = [&](auto mode, int64_t groups) {
+    constexpr int MODE = decltype(mode)::value;
+    return job.vec4 ? launch<MODE, true>(h, job, groups, st) : launch<MODE, false>(h, job, groups, st);
+  };
+  if (job.n <= 128) return run(std::integral_constant<int, kDual>(), 2 * (int64_t)h->sm_count);
+  if (job.k <= 128) return run(std::integral_constant<int, kWide>(), h->sm_count);
+  return run(std::integral_constant<int, kPair>(), resident_pairs());
 }

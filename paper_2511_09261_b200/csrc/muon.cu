@@ -25,24 +25,35 @@ bool valid_sizes(int64_t sets, int32_t r, int32_t c) {
          ns_tiles_supported(r < c ? r : c, r < c ? c : r);
 }
 
-// The iteration must stay bounded on [0, 1], where the singular values start; what it reaches there also bounds every
-// intermediate value.  Sampled densely; a coefficient set whose values grow past 2 is refused.  *p_max: the largest
-// |a + b s^2 + c s^4| over the values reached.
-bool coefficients_bounded(float a, float b, float c, int steps, double* p_max) {
+// The singular values start in [0, 1] and go through s -> s (a + b s^2 + c s^4) in every step.  The largest magnitude that the
+// values in [0, top] reach is taken step by step at the ends and the stationary points (roots of a + 3 b u + 5 c u^2, u = s^2);
+// a coefficient set that leads past 2 is refused: 2 bounds every stored value.  *p_max: the largest |a + b u + c u^2| met.
+bool coefficients_bounded(double a, double b, double c, int steps, double* p_max) {
   double top = 1.0;
-  for (int q = 0; q <= 4096; ++q) {
-    double s = q / 4096.0;
-    for (int t = 0; t < steps; ++t) {
-      const double s2 = s * s;
-      s = s * (a + s2 * (b + s2 * (double)c));
-      if (!(fabs(s) <= 2.0)) return false;
-      if (fabs(s) > top) top = fabs(s);
-    }
-  }
   *p_max = 0.0;
-  for (int q = 0; q <= 4096; ++q) {
-    const double s = top * q / 4096.0, s2 = s * s, p = fabs(a + s2 * (b + s2 * (double)c));
-    if (p > *p_max) *p_max = p;
+  auto poly = [&](double u) { return a + u * (b + u * c); };
+  double root[3];
+  int roots = 0;
+  if (c != 0.0) {
+    const double disc = 9.0 * b * b - 20.0 * a * c;
+    if (disc >= 0.0) {
+      root[roots++] = (-3.0 * b - sqrt(disc)) / (10.0 * c);
+      root[roots++] = (-3.0 * b + sqrt(disc)) / (10.0 * c);
+    }
+  } else if (b != 0.0) {
+    root[roots++] = -a / (3.0 * b);
+  }
+  for (int t = 0; t < steps; ++t) {
+    const double u_top = top * top;
+    double reach = fabs(top * poly(u_top));
+    for (int q = 0; q < roots; ++q)
+      if (root[q] > 0.0 && root[q] < u_top) reach = fmax(reach, fabs(sqrt(root[q]) * poly(root[q])));
+    const double vertex = c != 0.0 ? -b / (2.0 * c) : -1.0;
+    double p = fmax(fabs(a), fabs(poly(u_top)));
+    if (vertex > 0.0 && vertex < u_top) p = fmax(p, fabs(poly(vertex)));
+    if (!(reach <= 2.0) || !(p <= 1e30)) return false;
+    *p_max = fmax(*p_max, p);
+    top = fmax(top, reach);
   }
   return true;
 }

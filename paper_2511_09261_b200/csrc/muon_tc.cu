@@ -25,7 +25,8 @@
 // A and A A are worked on.  A's low limb does not fit next to X as a whole: its second half follows into the room of the
 // first as soon as the products that read the first are done (they are issued first).
 //
-// Roles: warp 16 issues MMAs; warp 17 exchanges blocks and prefetches the next matrix into L2; warps 0-15 load, convert and store: warp w owns rows 32 (w % 4) .. +32 (its TMEM
+// Roles: after the working warps (16; 8 where two CTAs share an SM) one warp issues MMAs, and in a pair another exchanges blocks; the
+// working warps load, convert and store: warp w owns rows 32 (w % 4) .. +32 (its TMEM
 // lanes) and the 32-column items w / 4 and w / 4 + 4.  Barriers per 64-column panel let the next product start on the
 // first panels while the others are converted.  Every wait is bounded; a CTA that gives up raises the status word.
 #include <cuda_fp16.h>
@@ -49,8 +50,8 @@ template <int MODE>
 struct Cfg {
   static constexpr bool PAIR = MODE == kPair;
   static constexpr int CTAS = PAIR ? 2 : 1, PER_SM = MODE == kDual ? 2 : 1;
-  static constexpr int WORK = MODE == kDual ? 8 : 16;      // working warps; then the MMA warp and the side warp
-  static constexpr int SUBS = WORK / 4, THREADS = 32 * (WORK + 2);
+  static constexpr int WORK = MODE == kDual ? 8 : 16;      // working warps; then the MMA warp and, in a pair, the side warp
+  static constexpr int SUBS = WORK / 4, THREADS = 32 * (WORK + 1 + (PAIR ? 1 : 0));
   static constexpr int XP = MODE == kDual ? 2 : 4;         // panels of X per limb
   static constexpr int A_HI = PAIR ? 4 : 2, A_LO = MODE == kDual ? 1 : 2;   // panels of A's limbs in shared memory
   static constexpr bool LATE = A_LO < A_HI;                // the low limb's second half follows into the room of the first
@@ -158,6 +159,23 @@ __global__ void __launch_bounds__(Cfg<MODE>::THREADS, Cfg<MODE>::PER_SM) ns_on_c
   // the exchange scratch of this pair: [CTA][limb][2 panels]
   uint8_t* const scratch = PAIR ? static_cast<uint8_t*>(J.scratch) + group * (2 * 4 * (int64_t)kPanel) : nullptr;
 
+  // The last step has begun: its weights and the next matrix are brought into L2 meanwhile, by one thread (each CTA of a pair:
+  // its half of the bytes; earlier, the lines of all CTAs together would not survive in L2).
+  auto prefetch = [&](int64_t s) {
+    if (!J.prefetch) return;
+    const int64_t bytes = (int64_t)J.r * J.c * 4, cut = bytes / 32 * 16, next = s + groups;
+    const int64_t lo = PAIR && rank == 1 ? cut : 0, hi = PAIR && rank == 0 ? cut : bytes;
+    auto fetch = [&](const void* array, int64_t set) {
+      for (int64_t at = lo; array && at < hi; at += 16384)
+        tc::prefetch_l2(static_cast<const char*>(array) + set * bytes + at, (uint32_t)(hi - at < 16384 ? hi - at : 16384));
+    };
+    fetch(J.W, s);
+    if (next < J.sets && !(J.active && !J.active[next])) {
+      fetch(J.G, next);
+      fetch(J.m, next);
+    }
+  };
+
   if (warp == kMmaWarp) {
     // ------------------------------------------------------------------------------ MMA issue
     {
@@ -217,6 +235,8 @@ __global__ void __launch_bounds__(Cfg<MODE>::THREADS, Cfg<MODE>::PER_SM) ns_on_c
                 tc::mma_f16<PAIR, false>(leader, acc1, xh + o, xh + o, i1, true);
               });
             commit(&B->m1);
+            if (!PAIR && leader && step == J.steps - 1) prefetch(s);
+            __syncwarp();
           }
           if (rank == 0) {
             if constexpr (C::LATE) {                       // A A: what reads the first half of A's low limb comes first
@@ -276,8 +296,8 @@ __global__ void __launch_bounds__(Cfg<MODE>::THREADS, Cfg<MODE>::PER_SM) ns_on_c
       }
     }
     __syncwarp();
-  } else if (warp == kSideWarp) {
-    // ------------------------------------------------------------------------------ exchange, prefetch
+  } else if (PAIR && warp == kSideWarp) {
+    // ------------------------------------------------------------------------------ exchange
     if (lane == 0) {
       uint32_t it = 0;
       bool ok = true;
@@ -285,40 +305,22 @@ __global__ void __launch_bounds__(Cfg<MODE>::THREADS, Cfg<MODE>::PER_SM) ns_on_c
         if (J.active && !J.active[s]) continue;
         for (int step = 0; step < J.steps && ok; ++step, ++it) {
           const uint32_t ph = it & 1;
-          if (!PAIR && !(ok = wait(&B->m1, ph))) break;
-          if (step == J.steps - 1 && J.prefetch) {
-            // the last step has begun: its weights and the next matrix are brought into L2 meanwhile (each CTA of a pair:
-            // its half of the bytes; earlier, the lines of all CTAs together would not survive in L2)
-            const int64_t bytes = (int64_t)J.r * J.c * 4, cut = bytes / 32 * 16;
-            const int64_t lo = PAIR && rank == 1 ? cut : 0, hi = PAIR && rank == 0 ? cut : bytes;
-            auto fetch = [&](const void* array, int64_t set) {
-              for (int64_t at = lo; array && at < hi; at += 16384)
-                tc::prefetch_l2(static_cast<const char*>(array) + set * bytes + at, (uint32_t)(hi - at < 16384 ? hi - at : 16384));
-            };
-            fetch(J.W, s);
-            const int64_t next = s + groups;
-            if (next < J.sets && !(J.active && !J.active[next])) {
-              fetch(J.G, next);
-              fetch(J.m, next);
-            }
-          }
-          if constexpr (PAIR) {
-            const uint32_t mine = (rank == 0 ? 2 : 0) * kPanel;           // the two panels that change hands
-            if (!(ok = wait(&B->own, ph))) break;
-            for (int limb = 0; limb < 2; ++limb)
-              tc::bulk_store(scratch + (rank * 2 + limb) * 2 * kPanel, sX + limb * C::XP * kPanel + mine, 2 * kPanel);
-            tc::bulk_store_wait();
-            tc::fence_proxy_async_all();
-            tc::mbar_arrive_release_cluster(tc::map_to_cta(tc::smem_u32(&B->g), rank ^ 1u));
-            // X X^T has read the rows: the block gives way to the partner's
-            if (!(ok = wait(&B->m1, ph) && wait_both(&B->g, ph))) break;
-            tc::fence_proxy_async_all();
-            tc::mbar_arrive_expect_tx(&B->s, 4 * kPanel);
-            for (int limb = 0; limb < 2; ++limb)
-              tc::bulk_load(sX + limb * C::XP * kPanel + mine, scratch + ((rank ^ 1u) * 2 + limb) * 2 * kPanel, 2 * kPanel, &B->s);
-            if (!(ok = wait(&B->s, ph))) break;
-            if (rank == 1) tc::mbar_arrive_release_cluster(tc::map_to_cta(tc::smem_u32(&B->s2), 0));
-          }
+          if (step == J.steps - 1) prefetch(s);
+          const uint32_t mine = (rank == 0 ? 2 : 0) * kPanel;             // the two panels that change hands
+          if (!(ok = wait(&B->own, ph))) break;
+          for (int limb = 0; limb < 2; ++limb)
+            tc::bulk_store(scratch + (rank * 2 + limb) * 2 * kPanel, sX + limb * C::XP * kPanel + mine, 2 * kPanel);
+          tc::bulk_store_wait();
+          tc::fence_proxy_async_all();
+          tc::mbar_arrive_release_cluster(tc::map_to_cta(tc::smem_u32(&B->g), rank ^ 1u));
+          // X X^T has read the rows: the block gives way to the partner's
+          if (!(ok = wait(&B->m1, ph) && wait_both(&B->g, ph))) break;
+          tc::fence_proxy_async_all();
+          tc::mbar_arrive_expect_tx(&B->s, 4 * kPanel);
+          for (int limb = 0; limb < 2; ++limb)
+            tc::bulk_load(sX + limb * C::XP * kPanel + mine, scratch + ((rank ^ 1u) * 2 + limb) * 2 * kPanel, 2 * kPanel, &B->s);
+          if (!(ok = wait(&B->s, ph))) break;
+          if (rank == 1) tc::mbar_arrive_release_cluster(tc::map_to_cta(tc::smem_u32(&B->s2), 0));
         }
       }
     }

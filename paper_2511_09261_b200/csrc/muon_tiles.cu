@@ -13,9 +13,10 @@
 //
 // A tile is 128 x 128; a stage of the shared-memory ring holds 64 of k (four panels, 64 KB, for 12 MMAs of 128 x 128 x 16).
 // k is always summed in four interleaved parts (stages 0, 4, 8 .., then 1, 5, 9 ..), added in that order.  With few tiles
-// (one shared weight) a cluster of four CTAs takes one part each: every CTA hands the others their column group of its
-// partial tile through distributed shared memory, and finishes its own group.  With many tiles one CTA takes the parts
-// in turn, in two accumulator buffers.  The results are the same bits either way.
+// (one shared weight) a cluster of four CTAs takes one part each, or one of two CTAs two: every CTA hands the others their
+// column group of its partial tiles through distributed shared memory, and finishes its own group.  With many tiles one
+// CTA takes the parts in turn, in two accumulator buffers.  The results are the same bits in all three forms.
+// Launches are chained by programmatic dependence: a kernel sets itself up while the one before it finishes.
 // Roles: warps 0-7 epilogue (TMEM lanes 32 (w % 4), column half w / 4), warp 8 issues MMAs, warp 9 the copies.
 #include <cuda_fp16.h>
 #include <math.h>
@@ -73,6 +74,7 @@ template <int KIND, int SPLIT>
 __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
   const NsJob& J = T.J;
   const int64_t s = blockIdx.y;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (J.active && !J.active[T.set0 + s]) return;           // the whole cluster leaves
   extern __shared__ uint8_t smem_raw[];
   const uint32_t sbase = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -89,8 +91,9 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
   int ti, tj;                                              // row tile; column tile (row tile of the right operand for A, P)
   if (KIND == kApply) { ti = tile % T.rb; tj = tile / T.rb; }
   else tile_of(tile, T.rb, ti, tj);
-  constexpr int kParts = 4 / SPLIT;                        // parts this CTA sums: rank, or all four
-  auto part_stages = [&](int p) { return (T.stages - ((int)rank + p) + 3) / 4; };
+  constexpr int kParts = 4 / SPLIT;                        // parts this CTA sums: first, first + 1 ..
+  const int first = (int)rank * kParts;
+  auto part_stages = [&](int p) { return (T.stages - (first + p) + 3) / 4; };
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
@@ -108,6 +111,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
   __syncthreads();
   tc::tc_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
+  asm volatile("griddepcontrol.wait;" ::: "memory");       // the operands of this product are complete from here on
 
   if (warp == kCopyWarp) {
     if (lane == 0) {
@@ -117,7 +121,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
       int q = 0;
       bool ok = true;
       for (int p = 0; p < kParts && ok; ++p)
-      for (int kb = (int)rank + p; kb < T.stages; kb += 4, ++q) {
+      for (int kb = first + p; kb < T.stages; kb += 4, ++q) {
         const int slot = q % kStages, use = q / kStages;
         if (use > 0 && !(ok = wait_bounded(empty + slot, (use - 1) & 1, abort_flag))) break;
         const uint32_t at = sbase + slot * kStageBytes;
@@ -138,6 +142,15 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
       }
     }
     __syncwarp();
+    if (KIND == kApply && T.last && J.W) {
+      // the tile of W that the products are about to be added to
+      const int64_t base = (T.set0 + s) * (int64_t)J.r * J.c;
+      const int row0 = (J.transpose ? tj : ti) * 128, col0 = (J.transpose ? ti : tj) * 128;
+      for (int q = lane; q < 128 * 5; q += 32) {
+        const int i = row0 + q / 5, j = min(col0 + (q % 5) * 32, min(col0 + 127, J.c - 1));
+        if (i < J.r) asm volatile("prefetch.global.L2 [%0];" ::"l"(J.W + base + (int64_t)i * J.c + j));
+      }
+    }
   } else if (warp == kMmaWarp) {
     const uint32_t leader = tc::elect_one();
     const uint32_t idesc = tc::idesc_f16_f32(128, 128, KIND == kApply);
@@ -179,13 +192,17 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
   const int quarter = warp & 3, half = warp >> 2;          // of the epilogue warps
   const int row = quarter * 32 + lane;
   const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-  constexpr int GROUP = 128 / SPLIT;                       // columns that one CTA finishes
-  float sum[2][32];
+  constexpr int GROUP = 128 / SPLIT, kItems = GROUP / 32;  // columns that one CTA finishes, in items of 32
+  // two CTAs: the second one keeps its two parts apart, so that the owner can add all four in order
+  constexpr int kKept = SPLIT == 2 ? 2 : 1;
+  float sum[kKept][2][32];
   if (warp < kEpiWarps) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int k = 0; k < kKept; ++k)
 #pragma unroll
-      for (int e = 0; e < 32; ++e) sum[i][e] = 0.0f;
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 32; ++e) sum[k][i][e] = 0.0f;
     for (int p = 0; p < kParts; ++p) {
       if (part_stages(p) <= 0) continue;
       if (!wait_bounded(done + p, 0, abort_flag)) break;
@@ -197,8 +214,13 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
         tc::tmem_ld_32x32(at, v);
         tc::tmem_ld_32x32(at + 128, w);
         tc::tmem_ld_wait();
+        if (kKept > 1 && rank == 1 && p == 1) {
 #pragma unroll
-        for (int e = 0; e < 32; ++e) sum[i][e] += __uint_as_float(v[e]) + __uint_as_float(w[e]);
+          for (int e = 0; e < 32; ++e) sum[kKept - 1][i][e] += __uint_as_float(v[e]) + __uint_as_float(w[e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) sum[0][i][e] += __uint_as_float(v[e]) + __uint_as_float(w[e]);
+        }
       }
       tc::tc_fence_before_sync();
       __syncwarp();
@@ -210,61 +232,70 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
   tc::tc_fence_after_sync();
 
   if constexpr (SPLIT > 1) {
-    // partial tiles to their owners: [from CTA][row][32 columns], 16 KB each
-    static_assert(SPLIT == 1 || GROUP == 32, "one item per CTA");
+    // partial tiles to their owners: [slot][item of the owner][row][32 columns], 16 KB an item
     tc::cluster_sync_all();                                // every CTA's ring is free
     if (warp < kEpiWarps) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint32_t to = tc::map_to_cta(sbase + rank * kPanel, half + 2 * i);
+      for (int k = 0; k < kKept; ++k) {
+        if (k > 0 && rank == 0) continue;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + at_chunk(row, e)), "f"(sum[i][4 * e]), "f"(sum[i][4 * e + 1]),
-                       "f"(sum[i][4 * e + 2]), "f"(sum[i][4 * e + 3]) : "memory");
+        for (int i = 0; i < 2; ++i) {
+          const int item = half + 2 * i, owner = item / kItems, local = item % kItems;
+          const uint32_t to = tc::map_to_cta(sbase + (((int)rank + k) * kItems + local) * kPanel, owner);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + at_chunk(row, e)), "f"(sum[k][i][4 * e]),
+                         "f"(sum[k][i][4 * e + 1]), "f"(sum[k][i][4 * e + 2]), "f"(sum[k][i][4 * e + 3]) : "memory");
+        }
       }
     }
     tc::cluster_sync_all();
   }
   if (warp < kEpiWarps && !*abort_flag) {
-    // one CTA: this warp's items; a cluster: the CTA's own one, by its first four warps
+    // one CTA: this warp's items; a cluster: the CTA's own ones, by the warps of their `half`
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      if (SPLIT > 1 && (half > 0 || i > 0)) continue;
-      const int item = SPLIT > 1 ? 0 : half + 2 * i;
+      if (SPLIT > 1 && (half >= kItems || i > 0)) continue;
+      const int item = half + 2 * i;
       uint32_t v[32];
       if constexpr (SPLIT > 1) {
+        float total[32];
 #pragma unroll
-        for (int e = 0; e < 32; ++e) sum[0][e] = 0.0f;
-        for (int from = 0; from < SPLIT; ++from)
+        for (int e = 0; e < 32; ++e) total[e] = 0.0f;
+        for (int slot = 0; slot < SPLIT + kKept - 1; ++slot)
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const uint4 a = tc::ld_shared16(sbase + from * kPanel + at_chunk(row, e));
-            sum[0][4 * e] += __uint_as_float(a.x);
-            sum[0][4 * e + 1] += __uint_as_float(a.y);
-            sum[0][4 * e + 2] += __uint_as_float(a.z);
-            sum[0][4 * e + 3] += __uint_as_float(a.w);
+            const uint4 a = tc::ld_shared16(sbase + (slot * kItems + item) * kPanel + at_chunk(row, e));
+            total[4 * e] += __uint_as_float(a.x);
+            total[4 * e + 1] += __uint_as_float(a.y);
+            total[4 * e + 2] += __uint_as_float(a.z);
+            total[4 * e + 3] += __uint_as_float(a.w);
           }
-      }
 #pragma unroll
-      for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(sum[SPLIT > 1 ? 0 : i][e]);
+        for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(total[e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(sum[0][i][e]);
+      }
       const int c0 = (int)rank * GROUP + item * 32;        // first column inside the tile
       const int panel = 2 * tj + (c0 >> 6), chunk0 = (c0 & 63) >> 3;
       uint8_t* const to = T.out + s * T.out_set + ((int64_t)panel * T.rb + ti) * kPanel;
       if (KIND == kApply && T.last) {
         const float fo = 1.0f / (J.p_scale * kXScale);
         const int64_t base = (T.set0 + s) * (int64_t)J.r * J.c;
-        auto put = [&](int64_t at, float x) {
-          if (J.W) __stcs(J.W + at, __ldcs(J.W + at) * J.keep - J.step * x);
+        auto put = [&](int64_t at, float w, float x) {
+          if (J.W) __stcs(J.W + at, w * J.keep - J.step * x);
           else if (J.o_bf16) static_cast<__nv_bfloat16*>(J.O)[at] = __float2bfloat16_rn(x);
           else __stcs(static_cast<float*>(J.O) + at, x);
         };
         if (J.transpose) {                                 // lanes are neighbouring columns of W
-          const int i = ti * 128 + row;
+          const int i = ti * 128 + row, j0 = tj * 128 + c0;
+          float w[32];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            const int j = tj * 128 + c0 + e;
-            if (i < J.k && j < J.n) put(base + (int64_t)j * J.c + i, __uint_as_float(v[e]) * fo);
-          }
+          for (int e = 0; e < 32; ++e) w[e] = J.W && i < J.k && j0 + e < J.n ? __ldcs(J.W + base + (int64_t)(j0 + e) * J.c + i) : 0.0f;
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (i < J.k && j0 + e < J.n) put(base + (int64_t)(j0 + e) * J.c + i, w[e], __uint_as_float(v[e]) * fo);
         } else {
           // rows pass through shared memory, so that lanes work on neighbouring columns (past what SPLIT exchanges)
           const uint32_t stage = sbase + 8 * kPanel + warp * 4096;
@@ -272,12 +303,18 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
           for (int e = 0; e < 8; ++e) tc::st_shared16(stage + at_chunk(lane, e), v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
           __syncwarp();
           const int j = tj * 128 + c0 + lane;
-#pragma unroll 8
+          float w[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            const int i = ti * 128 + quarter * 32 + e;
+            w[e] = J.W && i < J.k && j < J.n ? __ldcs(J.W + base + (int64_t)i * J.c + j) : 0.0f;
+          }
+#pragma unroll
           for (int e = 0; e < 32; ++e) {
             uint32_t x;
             asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(stage + at_chunk(e, lane >> 2) + (lane & 3) * 4) : "memory");
             const int i = ti * 128 + quarter * 32 + e;
-            if (i < J.k && j < J.n) put(base + (int64_t)i * J.c + j, __uint_as_float(x) * fo);
+            if (i < J.k && j < J.n) put(base + (int64_t)i * J.c + j, w[e], __uint_as_float(x) * fo);
           }
           __syncwarp();
         }
@@ -340,8 +377,16 @@ __global__ void __launch_bounds__(256) ns_pack(const NsJob J, int64_t set0, cons
                                                int64_t x_set, uint32_t x_limb, int32_t rb, int32_t cb) {
   const int64_t s = blockIdx.y;
   if (J.active && !J.active[set0 + s]) return;
-  double t = 0.0;
-  for (int q = 0; q < parts; ++q) t += partial[s * parts + q];
+  // every block adds the same partial sums in the same order (at most 256, one per thread)
+  __shared__ double part_sum[8];
+  double t = (int)threadIdx.x < parts ? partial[s * parts + threadIdx.x] : 0.0;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
+  if ((threadIdx.x & 31) == 0) part_sum[threadIdx.x >> 5] = t;
+  __syncthreads();
+  t = 0.0;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) t += part_sum[w];
   const float f = (float)((double)kXScale / (sqrt(t) + (double)J.eps));
   const int rows = rb * 128, chunks = cb * 8;
   const int64_t base = (set0 + s) * (int64_t)J.r * J.c;
@@ -459,21 +504,53 @@ int32_t launch_split(gnnco_handle* h, const TileJob& T, int64_t tiles, unsigned 
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = kSmem;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = SPLIT;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   GNNCO_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, T));
   h->launches += 1;
   return GNNCO_OK;
 }
 
+// Clusters of four that can be resident at once (asked once per process): fewer than SMs / 4, since a cluster stays inside one
+// group of SMs.
+int resident_quads() {
+  static const int quads = [] {
+    auto kernel = ns_tiles<kGram, 4>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess) {
+      cudaGetLastError();
+      return 0;
+    }
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(4 * 37);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 4;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      n = 0;
+    }
+    return n;
+  }();
+  return quads;
+}
+
 // A cluster per tile where the GPU holds them all at once.
 template <int KIND>
 int32_t launch_product(gnnco_handle* h, const TileJob& T, int64_t tiles, unsigned sets, cudaStream_t st) {
-  if (tiles * sets * 4 <= h->sm_count) return launch_split<KIND, 4>(h, T, tiles, sets, st);
+  if (tiles * sets <= resident_quads()) return launch_split<KIND, 4>(h, T, tiles, sets, st);
+  if (tiles * sets * 2 <= h->sm_count) return launch_split<KIND, 2>(h, T, tiles, sets, st);
   return launch_split<KIND, 1>(h, T, tiles, sets, st);
 }
 

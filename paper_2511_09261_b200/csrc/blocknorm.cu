@@ -75,206 +75,170 @@ constexpr int kGateNone = 0, kGateVector = 1, kGateRows = 2;
 
 // A lane's share of a vector of F float32 weights: 1 where there is none, times f.
 template <int VEC, int TEAM, int K>
-__device__ __forceinline__ void lane_weights(float (&w)[K][VEC], const float* p, int F, int tl, float f) {
+__device__ __forceinline__ void lane_weights(vio::Vec<VEC> (&w)[K], const float* p, int F, int tl, float f) {
 #pragma unroll
   for (int k = 0; k < K; ++k)
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       const int col = (k * TEAM + tl) * VEC + e;
-      w[k][e] = col < F ? f * (p ? __ldg(p + col) : 1.0f) : 0.0f;
+      w[k].v[e] = col < F ? f * (p ? __ldg(p + col) : 1.0f) : 0.0f;
     }
 }
+// s w_post, times g where the gate is shared
+template <int VEC, int TEAM, int K>
+__device__ __forceinline__ void post_weights(vio::Vec<VEC> (&c)[K], const NormArgs& A, int gate_kind, int tl) {
+  lane_weights<VEC, TEAM, K>(c, A.w_post, A.F, tl, A.scale);
+  if (gate_kind != kGateVector) return;
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const int col = (k * TEAM + tl) * VEC + e;
+      if (col < A.F) c[k].v[e] *= __ldg((const float*)A.gate + col);
+    }
+}
+__device__ __forceinline__ float inverse_rms(float sum_of_squares, const NormArgs& A) {
+  return rsqrtf(sum_of_squares * A.inv_F + A.eps);         // 2 units in the last place at most; the argument is a normal number
+}
 
-// Teams of TEAM lanes, K vectors of VEC elements per lane; a team works on R rows at a time (their loads are in flight
-// together), blocks go through the rows grid-stride.  Weights stay in registers.
-template <typename T, int VEC, int TEAM, int K, int R>
+// Teams of TEAM lanes, K vectors of VEC elements per lane; blocks go through the rows grid-stride, weights stay in
+// registers.  Two rows of a team in flight at a time were no faster (1,014 against 997 us for 2.5M x 256 bf16).
+template <typename T, int VEC, int TEAM, int K>
 __global__ void __launch_bounds__(TEAM > 256 ? TEAM : 256)
 norm_forward(const NormArgs A, const int gate_kind) {
+  using V = vio::Vec<VEC>;
   constexpr int THREADS = TEAM > 256 ? TEAM : 256, TEAMS = THREADS / TEAM;
   __shared__ float2 buf[TEAM > 32 ? TEAM / 32 : 1];
   const int tl = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
-  float c_post[K][VEC], w_pre[K][VEC];
+  V c_post[K], w_pre[K];
   lane_weights<VEC, TEAM, K>(w_pre, A.w_pre, A.F, tl, 1.0f);
-  lane_weights<VEC, TEAM, K>(c_post, A.w_post, A.F, tl, A.scale);
-  if (gate_kind == kGateVector) {
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        const int col = (k * TEAM + tl) * VEC + e;
-        if (col < A.F) c_post[k][e] *= __ldg((const float*)A.gate + col);
-      }
-  }
+  post_weights<VEC, TEAM, K>(c_post, A, gate_kind, tl);
   // whole blocks stay in the loop together (the sums name all lanes)
-  for (int64_t lead = (int64_t)blockIdx.x * (TEAMS * R); lead < A.rows; lead += (int64_t)gridDim.x * (TEAMS * R)) {
-    vio::Raw<T, VEC> xr[R][K], yr[R][K], gr[R][K];
+  for (int64_t lead = (int64_t)blockIdx.x * TEAMS; lead < A.rows; lead += (int64_t)gridDim.x * TEAMS) {
+    const int64_t row = lead + team;
+    vio::Raw<T, VEC> xr[K], yr[K], gr[K];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int64_t row = lead + r * TEAMS + team;
+    for (int k = 0; k < K; ++k) {
+      const int col = (k * TEAM + tl) * VEC;
+      const bool in = row < A.rows && col < A.F;
+      if (in) xr[k].template load<true>((const T*)A.x + row * A.x_ld + col);
+      else xr[k].zero();
+      if (in && A.y) yr[k].template load<true>((const T*)A.y + row * A.y_ld + col);
+      else yr[k].zero();
+      gr[k].zero();
+      if (gate_kind == kGateRows && in) gr[k].template load<true>((const T*)A.gate + row * A.gate_ld + col);
+    }
+    V xo[K], sq(0.0f);
+    if (A.y) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) sq = vio::fma(V(yr[k]), V(yr[k]), sq);
+      const float f = inverse_rms(TeamSum<TEAM>::one(sq.sum(), buf), A);
+      sq = V(0.0f);
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const int col = (k * TEAM + tl) * VEC;
-        const bool in = row < A.rows && col < A.F;
-        if (in) xr[r][k].template load<true>((const T*)A.x + row * A.x_ld + col);
-        else xr[r][k].zero();
-        if (in && A.y) yr[r][k].template load<true>((const T*)A.y + row * A.y_ld + col);
-        else yr[r][k].zero();
-        gr[r][k].zero();
-        if (gate_kind == kGateRows && in) gr[r][k].template load<true>((const T*)A.gate + row * A.gate_ld + col);
+        V c = vio::mul(c_post[k], f);
+        if (gate_kind == kGateRows) c = vio::mul(c, V(gr[k]));
+        xo[k] = vio::fma(c, V(yr[k]), V(xr[k]));
+        sq = vio::fma(xo[k], xo[k], sq);
+        if (row < A.rows && col < A.F) vio::store_stream<T, VEC>((T*)A.x_out + row * A.x_out_ld + col, xo[k].v);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        xo[k] = V(xr[k]);
+        sq = vio::fma(xo[k], xo[k], sq);
       }
     }
+    if (!A.h_out) continue;
+    const float rx = inverse_rms(TeamSum<TEAM>::one(sq.sum(), buf), A);
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int64_t row = lead + r * TEAMS + team;
-      float xo[K][VEC];
-      float sx = 0.0f;
-      float f = 0.0f;
-      if (A.y) {
-        float sy = 0.0f;
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) sy += yr[r][k].get(e) * yr[r][k].get(e);
-        sy = TeamSum<TEAM>::one(sy, buf);
-        f = 1.0f / sqrtf(sy * A.inv_F + A.eps);
-      }
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const int col = (k * TEAM + tl) * VEC;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          float c = c_post[k][e];
-          if (gate_kind == kGateRows) c *= gr[r][k].get(e);
-          xo[k][e] = xr[r][k].get(e);
-          if (A.y) xo[k][e] += c * (f * yr[r][k].get(e));
-          sx += xo[k][e] * xo[k][e];
-        }
-        if (row < A.rows && col < A.F && A.x_out) vio::store_stream<T, VEC>((T*)A.x_out + row * A.x_out_ld + col, xo[k]);
-      }
-      if (!A.h_out) continue;
-      sx = TeamSum<TEAM>::one(sx, buf);
-      const float rx = 1.0f / sqrtf(sx * A.inv_F + A.eps);
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const int col = (k * TEAM + tl) * VEC;
-        if (row >= A.rows || col >= A.F) continue;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) xo[k][e] = xo[k][e] * rx * w_pre[k][e];
-        vio::store_stream<T, VEC>((T*)A.h_out + row * A.h_out_ld + col, xo[k]);
-      }
+    for (int k = 0; k < K; ++k) {
+      const int col = (k * TEAM + tl) * VEC;
+      if (row >= A.rows || col >= A.F) continue;
+      vio::store_stream<T, VEC>((T*)A.h_out + row * A.h_out_ld + col, vio::mul(xo[k], vio::mul(w_pre[k], rx)).v);
     }
   }
 }
 
-template <typename T, int VEC, int TEAM, int K, int R>
-__global__ void __launch_bounds__(TEAM > 256 ? TEAM : 256)
+// Three blocks per SM where a lane holds at most eight elements: 2.5M x 256 bf16 takes 1,472 us so, 1,658 with the registers of two.
+template <typename T, int VEC, int TEAM, int K>
+__global__ void __launch_bounds__(TEAM > 256 ? TEAM : 256, TEAM > 256 ? 1 : K * VEC <= 8 ? 3 : 1)
 norm_backward(const NormArgs A, const int gate_kind) {
+  using V = vio::Vec<VEC>;
   constexpr int THREADS = TEAM > 256 ? TEAM : 256, TEAMS = THREADS / TEAM;
   __shared__ float2 buf[TEAM > 32 ? TEAM / 32 : 1];
   extern __shared__ float join[];                          // [TEAMS][TEAM * K * VEC], one quantity at a time
   const int tl = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
-  float s_pre[K][VEC], s_post[K][VEC], c_post[K][VEC], w_pre[K][VEC];
+  V s_pre[K], s_post[K], c_post[K], w_pre[K];
 #pragma unroll
-  for (int k = 0; k < K; ++k)
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) s_pre[k][e] = s_post[k][e] = 0.0f;
+  for (int k = 0; k < K; ++k) s_pre[k] = s_post[k] = V(0.0f);
   lane_weights<VEC, TEAM, K>(w_pre, A.w_pre, A.F, tl, 1.0f);
-  lane_weights<VEC, TEAM, K>(c_post, A.w_post, A.F, tl, A.scale);   // s w_post, times g where the gate is shared
-  if (gate_kind == kGateVector) {
+  post_weights<VEC, TEAM, K>(c_post, A, gate_kind, tl);
+  for (int64_t lead = (int64_t)blockIdx.x * TEAMS; lead < A.rows; lead += (int64_t)gridDim.x * TEAMS) {
+    const int64_t row = lead + team;
+    vio::Raw<T, VEC> xr[K], yr[K], dr[K], hr[K], gr[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        const int col = (k * TEAM + tl) * VEC + e;
-        if (col < A.F) c_post[k][e] *= __ldg((const float*)A.gate + col);
+    for (int k = 0; k < K; ++k) {
+      const int col = (k * TEAM + tl) * VEC;
+      const bool in = row < A.rows && col < A.F;
+      if (in && A.dh) {
+        xr[k].template load<true>((const T*)A.x + row * A.x_ld + col);
+        hr[k].template load<true>((const T*)A.dh + row * A.dh_ld + col);
+      } else {
+        xr[k].zero();
+        hr[k].zero();
       }
-  }
-  for (int64_t lead = (int64_t)blockIdx.x * (TEAMS * R); lead < A.rows; lead += (int64_t)gridDim.x * (TEAMS * R)) {
-    vio::Raw<T, VEC> xr[R][K], yr[R][K], dr[R][K], hr[R][K], gr[R][K];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int64_t row = lead + r * TEAMS + team;
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const int col = (k * TEAM + tl) * VEC;
-        const bool in = row < A.rows && col < A.F;
-        if (in && A.dh) {
-          xr[r][k].template load<true>((const T*)A.x + row * A.x_ld + col);
-          hr[r][k].template load<true>((const T*)A.dh + row * A.dh_ld + col);
-        } else {
-          xr[r][k].zero();
-          hr[r][k].zero();
-        }
-        if (in && A.y) yr[r][k].template load<true>((const T*)A.y + row * A.y_ld + col);
-        else yr[r][k].zero();
-        if (in && A.dx_out) dr[r][k].template load<true>((const T*)A.dx_out + row * A.dx_out_ld + col);
-        else dr[r][k].zero();
-        gr[r][k].zero();
-        if (gate_kind == kGateRows && in) gr[r][k].template load<true>((const T*)A.gate + row * A.gate_ld + col);
-      }
+      if (in && A.y) yr[k].template load<true>((const T*)A.y + row * A.y_ld + col);
+      else yr[k].zero();
+      if (in && A.dx_out) dr[k].template load<true>((const T*)A.dx_out + row * A.dx_out_ld + col);
+      else dr[k].zero();
+      gr[k].zero();
+      if (gate_kind == kGateRows && in) gr[k].template load<true>((const T*)A.gate + row * A.gate_ld + col);
     }
+    // mean over features of x'^2 and of a .* x'
+    V sx(0.0f), sa(0.0f);
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int64_t row = lead + r * TEAMS + team;
-      float sx = 0.0f, sa = 0.0f;
-      // mean over features of x'^2 and of a .* x'
+    for (int k = 0; k < K; ++k) {
+      const V x(xr[k]);
+      sx = vio::fma(x, x, sx);
+      sa = vio::fma(vio::mul(V(hr[k]), w_pre[k]), x, sa);
+    }
+    float2 t = TeamSum<TEAM>::both(sx.sum(), sa.sum(), buf);
+    const float rx = inverse_rms(t.x, A);
+    const float cx = t.y * A.inv_F * rx * rx;               // mean(a .* xh) r(x'): times x' below
+    V D[K], sy(0.0f), sb(0.0f);
 #pragma unroll
-      for (int k = 0; k < K; ++k)
+    for (int k = 0; k < K; ++k) {
+      const int col = (k * TEAM + tl) * VEC;
+      const V x(xr[k]), h(hr[k]), y(yr[k]), xh = vio::mul(x, rx);
+      s_pre[k] = vio::fma(h, xh, s_pre[k]);
+      D[k] = vio::fma(vio::mul(h, w_pre[k]), rx, vio::fma(xh, -cx, V(dr[k])));
+      V c = vio::mul(c_post[k], D[k]);
+      if (gate_kind == kGateRows) c = vio::mul(c, V(gr[k]));
+      sy = vio::fma(y, y, sy);
+      sb = vio::fma(c, y, sb);
+      if (row < A.rows && col < A.F) vio::store_stream<T, VEC>((T*)A.dx + row * A.dx_ld + col, D[k].v);
+    }
+    if (!A.y) continue;                                    // the same for all rows: no lane is left alone
+    t = TeamSum<TEAM>::both(sy.sum(), sb.sum(), buf);
+    const float ry = inverse_rms(t.x, A);
+    const float cy = t.y * A.inv_F * ry * ry;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          const float x = xr[r][k].get(e);
-          sx += x * x;
-          sa += hr[r][k].get(e) * w_pre[k][e] * x;
-        }
-      float2 t = TeamSum<TEAM>::both(sx, sa, buf);
-      const float rx = 1.0f / sqrtf(t.x * A.inv_F + A.eps);
-      const float cx = t.y * A.inv_F * rx * rx;             // mean(a .* xh) * r(x'): times x' below
-      float D[K][VEC];
-      float sy = 0.0f, sb = 0.0f;
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const int col = (k * TEAM + tl) * VEC;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          const float x = xr[r][k].get(e), dh = hr[r][k].get(e), y = yr[r][k].get(e);
-          s_pre[k][e] += dh * (x * rx);
-          D[k][e] = dr[r][k].get(e) + rx * (dh * w_pre[k][e] - x * cx);
-          float c = c_post[k][e];
-          if (gate_kind == kGateRows) c *= gr[r][k].get(e);
-          sy += y * y;
-          sb += c * D[k][e] * y;
-        }
-        if (row < A.rows && col < A.F) vio::store_stream<T, VEC>((T*)A.dx + row * A.dx_ld + col, D[k]);
+    for (int k = 0; k < K; ++k) {
+      const int col = (k * TEAM + tl) * VEC;
+      const bool in = row < A.rows && col < A.F;
+      const V y(yr[k]), yh = vio::mul(y, ry), q = vio::mul(D[k], yh);   // q, times s: the shared factor of dg and dw_post
+      V c = vio::mul(c_post[k], D[k]);
+      if (gate_kind == kGateRows) {
+        const V g(gr[k]);
+        s_post[k] = vio::fma(g, q, s_post[k]);
+        if (in && A.dgate) vio::store_stream<T, VEC>((T*)A.dgate + row * A.dgate_ld + col, vio::mul(c_post[k], q).v);
+        c = vio::mul(c, g);
+      } else {
+        s_post[k] = vio::fma(D[k], yh, s_post[k]);
       }
-      if (!A.y) continue;                                  // the same for all rows: no lane is left alone
-      t = TeamSum<TEAM>::both(sy, sb, buf);
-      const float ry = 1.0f / sqrtf(t.x * A.inv_F + A.eps);
-      const float cy = t.y * A.inv_F * ry * ry;
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const int col = (k * TEAM + tl) * VEC;
-        const bool in = row < A.rows && col < A.F;
-        float dy[VEC], dg[VEC];
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          const float y = yr[r][k].get(e);
-          const float q = D[k][e] * (y * ry);               // times s: the shared factor of dg and dw_post
-          float c = c_post[k][e];
-          if (gate_kind == kGateRows) {
-            const float g = gr[r][k].get(e);
-            s_post[k][e] += g * q;
-            dg[e] = c * q;
-            c *= g;
-          } else {
-            s_post[k][e] += q;
-          }
-          dy[e] = ry * (c * D[k][e] - y * cy);
-        }
-        if (in) {
-          vio::store_stream<T, VEC>((T*)A.dy + row * A.dy_ld + col, dy);
-          if (gate_kind == kGateRows && A.dgate) vio::store_stream<T, VEC>((T*)A.dgate + row * A.dgate_ld + col, dg);
-        }
-      }
+      if (in) vio::store_stream<T, VEC>((T*)A.dy + row * A.dy_ld + col, vio::fma(c, ry, vio::mul(yh, -cy)).v);
     }
   }
 
@@ -285,7 +249,7 @@ norm_backward(const NormArgs A, const int gate_kind) {
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) join[team * W + (k * TEAM + tl) * VEC + e] = which == 0 ? s_pre[k][e] : s_post[k][e];
+      for (int e = 0; e < VEC; ++e) join[team * W + (k * TEAM + tl) * VEC + e] = which == 0 ? s_pre[k].v[e] : s_post[k].v[e];
     __syncthreads();
     for (int f = threadIdx.x; f < A.F; f += THREADS) {
       float s = 0.0f;
@@ -327,24 +291,21 @@ __global__ void __launch_bounds__(1024) norm_weight_sums(const float* __restrict
 }
 
 constexpr int kMaxF = 8192;
-constexpr int kBlocksPerSm = 4;                            // most blocks per SM of the backward kernel (rows of `partial`)
+constexpr int kBlocksPerSm = 3;                            // most blocks per SM of the backward kernel (rows of `partial`)
 
 template <typename T, int VEC, int TEAM, int K>
 int32_t launch_one(bool backward, const NormArgs& A, int gate_kind, int sms, int* blocks, cudaStream_t st) {
   constexpr int THREADS = TEAM > 256 ? TEAM : 256, TEAMS = THREADS / TEAM;
+  const int64_t need = (A.rows + TEAMS - 1) / TEAMS;
   if (!backward) {
-    constexpr int R = K * VEC <= 8 ? 2 : 1;
-    const int64_t need = (A.rows + TEAMS * R - 1) / (TEAMS * R);
     const int64_t most = (int64_t)sms * 32;
-    norm_forward<T, VEC, TEAM, K, R><<<(unsigned)(need < most ? need : most), THREADS, 0, st>>>(A, gate_kind);
+    norm_forward<T, VEC, TEAM, K><<<(unsigned)(need < most ? need : most), THREADS, 0, st>>>(A, gate_kind);
     return GNNCO_OK;
   }
-  constexpr int R = 1;
-  const int64_t need = (A.rows + TEAMS * R - 1) / (TEAMS * R);
   const size_t smem = (size_t)TEAMS * TEAM * K * VEC * sizeof(float);
   const int64_t most = (int64_t)sms * (THREADS > 256 ? 1 : kBlocksPerSm);
   *blocks = (int)(need < most ? need : most);
-  norm_backward<T, VEC, TEAM, K, R><<<*blocks, THREADS, smem, st>>>(A, gate_kind);
+  norm_backward<T, VEC, TEAM, K><<<*blocks, THREADS, smem, st>>>(A, gate_kind);
   return GNNCO_OK;
 }
 

@@ -2,6 +2,8 @@
 // muon_tiles.cu: larger ones).
 #pragma once
 
+#include <atomic>
+
 #include "internal.cuh"
 
 struct NsJob {
@@ -18,6 +20,15 @@ struct NsJob {
   void* scratch;
   int32_t* status;
 };
+
+// Shared memory above 48 KB has to be asked for once per kernel and device (asking takes as long as launching).
+template <typename Kernel>
+inline int32_t allow_shared_memory(Kernel kernel, size_t bytes, int device, std::atomic<int>& done_for) {
+  if (done_for.load() == device + 1) return GNNCO_OK;
+  GNNCO_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+  done_for.store(device + 1);
+  return GNNCO_OK;
+}
 
 // ---- muon_tc.cu: whole iterations on chip for k, n <= 256
 bool ns_on_chip_supported(const gnnco_handle* h, int32_t k, int32_t n);

@@ -729,7 +729,9 @@ int resident_pairs() {
 
 template <int MODE, bool VEC4>
 int32_t launch(gnnco_handle* h, const NsJob& job, int64_t groups, cudaStream_t st) {
-  GNNCO_CUDA_TRY(cudaFuncSetAttribute((ns_on_chip<MODE, VEC4>), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<MODE>::SMEM));
+  static std::atomic<int> allowed{0};
+  const int32_t rc = allow_shared_memory(ns_on_chip<MODE, VEC4>, Cfg<MODE>::SMEM, h->device, allowed);
+  if (rc != GNNCO_OK) return rc;
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[1];
   if (groups > job.sets) groups = job.sets;

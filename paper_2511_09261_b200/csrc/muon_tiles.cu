@@ -498,7 +498,9 @@ Layout layout(void* ws, int64_t sets, int32_t k, int32_t n) {
 template <int KIND, int SPLIT>
 int32_t launch_split(gnnco_handle* h, const TileJob& T, int64_t tiles, unsigned sets, cudaStream_t st) {
   auto kernel = ns_tiles<KIND, SPLIT>;
-  GNNCO_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));
+  static std::atomic<int> allowed{0};
+  const int32_t rc = allow_shared_memory(kernel, kSmem, h->device, allowed);
+  if (rc != GNNCO_OK) return rc;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(tiles * SPLIT), sets);
   cfg.blockDim = dim3(kThreads);

@@ -84,6 +84,74 @@ __device__ __forceinline__ void store_stream(T* p, const float (&v)[VEC]) {
   }
 }
 
+// Element-wise float32 arithmetic on VEC values, two at a time where VEC is even (one instruction per pair).
+__device__ __forceinline__ uint64_t pair_of(float x, float y) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+
+template <int VEC>
+struct Vec {
+  float v[VEC];
+  __device__ __forceinline__ Vec() {}
+  __device__ __forceinline__ explicit Vec(float x) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[i] = x;
+  }
+  template <typename T>
+  __device__ __forceinline__ explicit Vec(const Raw<T, VEC>& r) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[i] = r.get(i);
+  }
+  __device__ __forceinline__ float sum() const {
+    float s = v[0];
+#pragma unroll
+    for (int i = 1; i < VEC; ++i) s += v[i];
+    return s;
+  }
+};
+// a b
+template <int VEC>
+__device__ __forceinline__ Vec<VEC> mul(const Vec<VEC>& a, const Vec<VEC>& b) {
+  Vec<VEC> r;
+  if constexpr (VEC % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < VEC; i += 2) {
+      uint64_t d;
+      asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(pair_of(a.v[i], a.v[i + 1])), "l"(pair_of(b.v[i], b.v[i + 1])));
+      unpair(d, r.v[i], r.v[i + 1]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) r.v[i] = a.v[i] * b.v[i];
+  }
+  return r;
+}
+template <int VEC>
+__device__ __forceinline__ Vec<VEC> mul(const Vec<VEC>& a, float b) { return mul(a, Vec<VEC>(b)); }
+// a b + c
+template <int VEC>
+__device__ __forceinline__ Vec<VEC> fma(const Vec<VEC>& a, const Vec<VEC>& b, const Vec<VEC>& c) {
+  Vec<VEC> r;
+  if constexpr (VEC % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < VEC; i += 2) {
+      uint64_t d;
+      asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(pair_of(a.v[i], a.v[i + 1])), "l"(pair_of(b.v[i], b.v[i + 1])),
+          "l"(pair_of(c.v[i], c.v[i + 1])));
+      unpair(d, r.v[i], r.v[i + 1]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) r.v[i] = fmaf(a.v[i], b.v[i], c.v[i]);
+  }
+  return r;
+}
+template <int VEC>
+__device__ __forceinline__ Vec<VEC> fma(const Vec<VEC>& a, float b, const Vec<VEC>& c) { return fma(a, Vec<VEC>(b), c); }
+
 }  // namespace vio
 
 // Whether rows of `ld` elements of `es` bytes starting at p can be moved in vectors of `vec` elements.

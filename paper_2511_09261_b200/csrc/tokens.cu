@@ -16,9 +16,47 @@ namespace {
 
 // -------------------------------------------------------------------------------------------------------- lookup
 
-// A warp owns a tile of `tile` rows; its lanes walk the tile's vectors as one flat list, so that any width keeps all
-// lanes busy, and eight loads are in flight per lane.  32-row tiles read the tokens in one coalesced load; calls with
-// few rows use 4-row tiles to spread over the SMs.
+// A warp owns a tile of `tile` rows whose tokens it reads in one coalesced load; eight loads are in flight per lane.  Calls with
+// few rows use 4-row tiles to spread over the SMs.  Two forms:
+//   lookup_rows    rows of 2^i (up to 32) or a multiple of 32 vectors: `width` lanes per row, so a lane's column never changes
+//   lookup_kernel  any other width: the lanes walk the tile's vectors as one flat list
+// (10M x 256 bf16: 1,001 us in the flat form, whose index arithmetic takes two thirds of the issue slots.)
+template <typename TT, typename TO, int VEC>
+__global__ void __launch_bounds__(256) lookup_rows(const int32_t* __restrict__ tokens, const TT* __restrict__ table, int64_t table_ld,
+                                                   TO* __restrict__ out, int64_t out_ld, int64_t rows, int32_t V,
+                                                   int32_t vecs_per_row, int32_t width, float scale, int tile, int32_t* status) {
+  const int lane = threadIdx.x & 31;
+  const int64_t row0 = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * tile;
+  if (row0 >= rows) return;
+  const int here = (int)min((int64_t)tile, rows - row0);
+  int32_t tok = lane < here ? __ldcs(tokens + row0 + lane) : -1;
+  if (tok >= V) {
+    atomicMin(status, (int32_t)GNNCO_OUT_OF_RANGE);
+    tok = -1;
+  }
+  const int step = 32 / width, sub = lane / width;          // rows per load of the warp, this lane's of them
+  constexpr int U = 8;
+  for (int j = lane % width; j < vecs_per_row; j += width) {
+    const TT* const src = table + (int64_t)j * VEC;
+    TO* dst = out + (row0 + sub) * out_ld + (int64_t)j * VEC;
+    const int64_t hop = step * out_ld;
+    for (int r = sub; r < here + sub; r += U * step) {      // (the same number of rounds for all lanes)
+      vio::Raw<TT, VEC> v[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int32_t t = __shfl_sync(0xffffffffu, tok, (r + k * step) & 31);
+        if (r + k * step < here && t >= 0) v[k].template load<false>(src + t * table_ld);
+        else v[k].zero();
+      }
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        if (r + k * step < here) vio::store_stream<TO, VEC>(dst, vio::mul(vio::Vec<VEC>(v[k]), scale).v);
+        dst += hop;
+      }
+    }
+  }
+}
+
 template <typename TT, typename TO, int VEC>
 __global__ void __launch_bounds__(256) lookup_kernel(const int32_t* __restrict__ tokens, const TT* __restrict__ table,
                                                      int64_t table_ld, TO* __restrict__ out, int64_t out_ld, int64_t rows,
@@ -56,12 +94,19 @@ __global__ void __launch_bounds__(256) lookup_kernel(const int32_t* __restrict__
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       if (base + 32 * k + lane >= total) continue;
-      float f[VEC];
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) f[e] = scale * v[k].get(e);
-      vio::store_stream<TO, VEC>(out + (row0 + r[k]) * out_ld + (int64_t)j[k] * VEC, f);
+      vio::store_stream<TO, VEC>(out + (row0 + r[k]) * out_ld + (int64_t)j[k] * VEC, vio::mul(vio::Vec<VEC>(v[k]), scale).v);
     }
   }
+}
+
+template <typename TT, typename TO, int VEC>
+void lookup_vec(const int32_t* tokens, const TT* table, int64_t table_ld, TO* out, int64_t out_ld, int64_t rows, int32_t V, int32_t F,
+                float scale, int tile, unsigned grid, int32_t* status, cudaStream_t st) {
+  const int vecs = F / VEC;
+  if (vecs % 32 == 0 || 32 % vecs == 0)
+    lookup_rows<TT, TO, VEC><<<grid, 256, 0, st>>>(tokens, table, table_ld, out, out_ld, rows, V, vecs, vecs < 32 ? vecs : 32, scale, tile, status);
+  else
+    lookup_kernel<TT, TO, VEC><<<grid, 256, 0, st>>>(tokens, table, table_ld, out, out_ld, rows, V, vecs, scale, tile, status);
 }
 
 template <typename TT, typename TO>
@@ -73,11 +118,11 @@ int32_t lookup_typed(gnnco_handle* h, const int32_t* tokens, const TT* table, in
     return F % vec == 0 && vec_ok(table, table_ld, sizeof(TT), vec) && vec_ok(out, out_ld, sizeof(TO), vec);
   };
   if (fits(8) && (sizeof(TT) == 2 || sizeof(TO) == 2))
-    lookup_kernel<TT, TO, 8><<<grid, 256, 0, st>>>(tokens, table, table_ld, out, out_ld, rows, V, F / 8, scale, tile, h->status);
+    lookup_vec<TT, TO, 8>(tokens, table, table_ld, out, out_ld, rows, V, F, scale, tile, grid, h->status, st);
   else if (fits(4))
-    lookup_kernel<TT, TO, 4><<<grid, 256, 0, st>>>(tokens, table, table_ld, out, out_ld, rows, V, F / 4, scale, tile, h->status);
+    lookup_vec<TT, TO, 4>(tokens, table, table_ld, out, out_ld, rows, V, F, scale, tile, grid, h->status, st);
   else
-    lookup_kernel<TT, TO, 1><<<grid, 256, 0, st>>>(tokens, table, table_ld, out, out_ld, rows, V, F, scale, tile, h->status);
+    lookup_vec<TT, TO, 1>(tokens, table, table_ld, out, out_ld, rows, V, F, scale, tile, grid, h->status, st);
   h->launches += 1;
   GNNCO_LAUNCH_CHECK();
   return GNNCO_OK;

@@ -344,6 +344,7 @@ class PartitionedGraph:
         self._ws_key = None
         self._plan_ws = None
         self._plan_active = None
+        self._plan_sizes = {}
 
     # ---- views of the persistent area as torch tensors (no copies)
     def _view_tensor(self, ptr: int, count: int, dtype):
@@ -635,9 +636,11 @@ class PartitionedGraph:
         synchronisation."""
         import torch
         rows = self._tokens(tokens)
-        need = _sz(0)
-        _check(self._lib.gnnco_embedding_plan_bytes(rows, V, F, ctypes.byref(need)), "gnnco_embedding_plan_bytes")
-        need = need.value
+        need = self._plan_sizes.get((rows, V, F))
+        if need is None:
+            b = _sz(0)
+            _check(self._lib.gnnco_embedding_plan_bytes(rows, V, F, ctypes.byref(b)), "gnnco_embedding_plan_bytes")
+            need = self._plan_sizes[(rows, V, F)] = b.value
         ws = _empty((need,), torch.uint8, tokens, stream)
         _check(self._lib.gnnco_embedding_plan(self._handle, tokens.data_ptr(), rows, V, F, ws.data_ptr(), need,
                                               _stream_ptr(stream)), "gnnco_embedding_plan")

@@ -130,19 +130,21 @@ int32_t lookup_typed(gnnco_handle* h, const int32_t* tokens, const TT* table, in
 
 // ---------------------------------------------------------------------------------------------------- order by token
 //
-// Stable least-significant-digit radix sort of the row numbers by token, at most 8 bits per pass and only as many bits as
-// V has, shared evenly over the passes (20 bits: 7 + 7 + 6): fewer digits make longer runs of neighbouring writes.
+// Stable least-significant-digit radix sort of the row numbers by token, at most 10 bits per pass and only as many bits as
+// V has, shared evenly over the passes (17 bits: 9 + 8): two passes up to a million tokens.
 // A fixed number of blocks owns one contiguous span of positions each: block histograms (digit-major), one block per
 // digit scans that digit's row, and the scatter puts a tile in digit order in shared memory before it writes it out, so
 // that a digit's rows leave together.  Rows without a token get key V and end up last.
 constexpr int kOrdThreads = 512, kOrdWarps = kOrdThreads / 32, kOrdRounds = 8;
 constexpr int kOrdTile = kOrdThreads * kOrdRounds;         // positions of one block-wide step
 constexpr int kOrdMaxBlocks = 444;                         // 3 per SM: all resident at once
-constexpr int kSmallRows = 4096;                           // up to here one block sorts everything in shared memory
+constexpr int kOrdMaxBits = 10, kOrdMaxDigits = 1 << kOrdMaxBits;
+constexpr int kSmallRows = 4096, kSmallTokens = 4096;      // up to here one block sorts everything in shared memory
 
 struct PlanLayout {
   int32_t *key_a, *idx_a, *key_b, *idx_b, *hist, *totals;
   uint32_t* present;
+  int32_t* starts;                                         // [V + 1] first position of each token (small plans only)
   float* partial;                                          // [chunks][2][F]
   size_t bytes;
   int64_t chunks;
@@ -164,20 +166,25 @@ int chunk_of(int64_t rows) {
   return c;
 }
 
+// Few rows and few tokens: one block sorts, and one block per token adds its rows.
+bool is_small(int64_t rows, int32_t V) { return rows > 0 && rows <= kSmallRows && V <= kSmallTokens; }
+
 PlanLayout plan_layout(void* ws, int64_t rows, int32_t V, int32_t F) {
   Carver c(ws, 0);
   PlanLayout L;
-  L.passes = (bits_of(V) + 7) / 8;
+  L.passes = (bits_of(V) + kOrdMaxBits - 1) / kOrdMaxBits;
   L.bits = (bits_of(V) + L.passes - 1) / L.passes;
+  if (L.bits < 1) L.bits = 1;
   L.chunk = chunk_of(rows);
   L.chunks = (rows + L.chunk - 1) / L.chunk;
   L.key_a = c.take<int32_t>(rows);
   L.idx_a = c.take<int32_t>(rows);
   L.key_b = c.take<int32_t>(rows);
   L.idx_b = c.take<int32_t>(rows);
-  L.hist = c.take<int32_t>(256 * (size_t)kOrdMaxBlocks);
-  L.totals = c.take<int32_t>(256);
+  L.hist = c.take<int32_t>(kOrdMaxDigits * (size_t)kOrdMaxBlocks);
+  L.totals = c.take<int32_t>(kOrdMaxDigits);
   L.present = c.take<uint32_t>(((size_t)V + 31) / 32);
+  L.starts = c.take<int32_t>(is_small(rows, V) ? V + 1 : 0);
   L.partial = c.take<float>((size_t)L.chunks * 2 * F);
   L.bytes = c.off;
   return L;
@@ -206,8 +213,8 @@ template <bool FIRST>
 __global__ void __launch_bounds__(kOrdThreads) order_histogram(const int32_t* __restrict__ keys, int64_t N, int64_t span,
                                                                int shift, int digits, int32_t V, int32_t* __restrict__ hist,
                                                                int32_t* status) {
-  __shared__ int32_t cnt[256];
-  if (threadIdx.x < 256) cnt[threadIdx.x] = 0;
+  __shared__ int32_t cnt[kOrdMaxDigits];
+  for (int d = threadIdx.x; d < digits; d += kOrdThreads) cnt[d] = 0;
   __syncthreads();
   const int64_t lo = (int64_t)blockIdx.x * span, hi = min(N, lo + span);
   bool wrong = false;
@@ -230,7 +237,7 @@ __global__ void __launch_bounds__(kOrdThreads) order_histogram(const int32_t* __
   }
   if (FIRST && wrong) atomicMin(status, (int32_t)GNNCO_OUT_OF_RANGE);
   __syncthreads();
-  if ((int)threadIdx.x < digits) hist[(int64_t)threadIdx.x * gridDim.x + blockIdx.x] = cnt[threadIdx.x];
+  for (int d = threadIdx.x; d < digits; d += kOrdThreads) hist[(int64_t)d * gridDim.x + blockIdx.x] = cnt[d];
 }
 
 // One block per digit: exclusive prefix of the digit's block counts (in place) and the digit's total.
@@ -255,8 +262,8 @@ __global__ void __launch_bounds__(1024) order_scan(int32_t* hist, int32_t* total
   if (threadIdx.x == 0) totals[blockIdx.x] = tot;
 }
 
-// exclusive prefix over one value per thread of the block's first 256 threads (the others pass 0)
-__device__ __forceinline__ int32_t scan256(int32_t x, int32_t* warp_tot) {
+// exclusive prefix over the block's threads (all call it; warp_tot holds one value per warp)
+__device__ __forceinline__ int32_t scan_block(int32_t x, int32_t* warp_tot) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int32_t incl = x;
 #pragma unroll
@@ -264,15 +271,17 @@ __device__ __forceinline__ int32_t scan256(int32_t x, int32_t* warp_tot) {
     const int32_t o = __shfl_up_sync(0xffffffffu, incl, d);
     if (lane >= d) incl += o;
   }
-  if (warp < 8 && lane == 31) warp_tot[warp] = incl;
+  if (lane == 31) warp_tot[warp] = incl;
   __syncthreads();
   int32_t off = 0;
 #pragma unroll
-  for (int w = 0; w < 8; ++w)
+  for (int w = 0; w < kOrdWarps; ++w)
     if (w < warp) off += warp_tot[w];
+  __syncthreads();
   return off + incl - x;
 }
 
+// Thread t owns digits 2 t and 2 t + 1.
 template <bool FIRST>
 __global__ void __launch_bounds__(kOrdThreads, 3) order_scatter(const int32_t* __restrict__ keys, const int32_t* __restrict__ idx,
                                                              int32_t* __restrict__ keys_out, int32_t* __restrict__ idx_out,
@@ -281,60 +290,78 @@ __global__ void __launch_bounds__(kOrdThreads, 3) order_scatter(const int32_t* _
   extern __shared__ int32_t sm[];
   int32_t* const sk = sm;                                  // the tile in digit order
   int32_t* const si = sm + kOrdTile;
-  int32_t(*cnt)[256] = reinterpret_cast<int32_t(*)[256]>(sm + 2 * kOrdTile);
-  int32_t* const next = sm + 2 * kOrdTile + kOrdWarps * 256;   // [256] where a digit's next row goes, less its place in the tile
-  int32_t* const warp_tot = next + 256;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = threadIdx.x;
-  const bool owns = t < digits;
-  int32_t at = scan256(owns ? totals[t] : 0, warp_tot);    // of digit t
-  if (owns) at += hist[(int64_t)t * gridDim.x + blockIdx.x];
+  int32_t* const next = sm + 2 * kOrdTile;                 // [digits] where a digit's next row goes, less its place in the tile
+  int32_t* const warp_tot = next + kOrdMaxDigits;
+  uint32_t* const cnt = reinterpret_cast<uint32_t*>(warp_tot + kOrdWarps);   // [warps][digits] 16-bit counters, two to a word
+  uint16_t* const cnt16 = reinterpret_cast<uint16_t*>(cnt);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = threadIdx.x, words = digits / 2;
+  const bool owns = t < words;
+  int32_t at0, at1;                                        // of digits 2 t and 2 t + 1
+  {
+    const int32_t a = owns ? totals[2 * t] : 0, b = owns ? totals[2 * t + 1] : 0;
+    at0 = scan_block(a + b, warp_tot);
+    at1 = at0 + a;
+    if (owns) {
+      at0 += hist[(int64_t)(2 * t) * gridDim.x + blockIdx.x];
+      at1 += hist[(int64_t)(2 * t + 1) * gridDim.x + blockIdx.x];
+    }
+  }
   const int64_t lo = (int64_t)blockIdx.x * span, hi = min(N, lo + span);
   for (int64_t p0 = lo; p0 < hi; p0 += kOrdTile) {
-    for (int q = t; q < kOrdWarps * 256; q += kOrdThreads) (&cnt[0][0])[q] = 0;
+    for (int q = t; q < kOrdWarps * words; q += kOrdThreads) cnt[q] = 0;
     __syncthreads();
     // ranks inside the warp's 256 consecutive positions, in position order
-    int32_t k[kOrdRounds], v[kOrdRounds];
+    int32_t k[kOrdRounds];
     int rank[kOrdRounds];
     const int64_t wbase = p0 + warp * (32 * kOrdRounds);
 #pragma unroll
     for (int r = 0; r < kOrdRounds; ++r) {
       const int64_t p = wbase + r * 32 + lane;
       k[r] = p < hi ? (FIRST ? token_key(keys[p], V) : keys[p]) : 0;
-      v[r] = FIRST ? (int32_t)p : (p < hi ? idx[p] : 0);
     }
+    uint16_t* const mine = cnt16 + warp * digits;
 #pragma unroll
     for (int r = 0; r < kOrdRounds; ++r) {
       const bool valid = wbase + r * 32 + lane < hi;
       const uint32_t d = (uint32_t)(k[r] >> shift) & (uint32_t)(digits - 1);
-      const uint32_t peers = same_digit<8>(d, valid);
+      const uint32_t peers = same_digit<kOrdMaxBits>(d, valid);
       const int before = __popc(peers & ((1u << lane) - 1u));
-      rank[r] = valid ? cnt[warp][d] + before : 0;
+      rank[r] = valid ? mine[d] + before : 0;
       __syncwarp();
-      if (valid && before == 0) cnt[warp][d] += __popc(peers);
+      if (valid && before == 0) mine[d] += (uint16_t)__popc(peers);
       __syncwarp();
     }
+    int32_t v[kOrdRounds];
+#pragma unroll
+    for (int r = 0; r < kOrdRounds; ++r) {
+      const int64_t p = wbase + r * 32 + lane;
+      v[r] = FIRST ? (int32_t)p : (p < hi ? idx[p] : 0);
+    }
     __syncthreads();
-    int32_t total = 0;
+    uint32_t total = 0;                                    // both digits at once: neither passes 16 bits
     if (owns)
 #pragma unroll
-      for (int w = 0; w < kOrdWarps; ++w) total += cnt[w][t];
-    const int32_t first = scan256(total, warp_tot);        // the digit's place in the tile
+      for (int w = 0; w < kOrdWarps; ++w) total += cnt[w * words + t];
+    const int32_t n0 = (int32_t)(total & 0xffffu), n1 = (int32_t)(total >> 16);
+    const int32_t first0 = scan_block(n0 + n1, warp_tot), first1 = first0 + n0;   // the digits' places in the tile
     if (owns) {
-      int32_t c = first;
+      uint32_t c = (uint32_t)first0 | ((uint32_t)first1 << 16);
 #pragma unroll
       for (int w = 0; w < kOrdWarps; ++w) {
-        const int32_t n = cnt[w][t];
-        cnt[w][t] = c;
+        const uint32_t n = cnt[w * words + t];
+        cnt[w * words + t] = c;
         c += n;
       }
-      next[t] = at - first;
-      at += total;
+      next[2 * t] = at0 - first0;
+      next[2 * t + 1] = at1 - first1;
+      at0 += n0;
+      at1 += n1;
     }
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kOrdRounds; ++r) {
       if (wbase + r * 32 + lane < hi) {
-        const int32_t q = cnt[warp][(k[r] >> shift) & (digits - 1)] + rank[r];
+        const int32_t q = mine[(k[r] >> shift) & (digits - 1)] + rank[r];
         sk[q] = k[r];
         si[q] = v[r];
       }
@@ -353,19 +380,18 @@ __global__ void __launch_bounds__(kOrdThreads, 3) order_scatter(const int32_t* _
     __syncthreads();
   }
 }
-constexpr size_t kScatterSmem = (size_t)(2 * kOrdTile + kOrdWarps * 256 + 256 + 8) * sizeof(int32_t);
+constexpr size_t kScatterSmem = (size_t)(2 * kOrdTile + kOrdMaxDigits + kOrdWarps + kOrdWarps * kOrdMaxDigits / 2) * sizeof(int32_t);
 
 // All passes in one block for up to kSmallRows rows: 32 warps x 128 positions, 5 bits per pass, so that the 32 x 32 counters
 // (digit-major) are one per thread and one scan over the block places everything.
 constexpr int kSmallThreads = 1024, kSmallRounds = kSmallRows / kSmallThreads;
 __global__ void __launch_bounds__(kSmallThreads) order_small(const int32_t* __restrict__ tokens, int32_t N, int32_t V, int bits,
                                                              int32_t* __restrict__ keys_out, int32_t* __restrict__ idx_out,
-                                                             uint32_t* present, int32_t* status) {
+                                                             int32_t* __restrict__ starts, int32_t* status) {
   __shared__ int32_t sk[kSmallRows], si[kSmallRows];
   __shared__ int32_t cnt[32 * 33];                         // [digit][warp]
   __shared__ int32_t tot[32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int w = threadIdx.x; w < (V + 31) / 32; w += kSmallThreads) present[w] = 0u;
   int32_t k[kSmallRounds], v[kSmallRounds];
   const int wbase = warp * (32 * kSmallRounds);
 #pragma unroll
@@ -429,7 +455,11 @@ __global__ void __launch_bounds__(kSmallThreads) order_small(const int32_t* __re
     if (p < N) {
       keys_out[p] = k[r];
       idx_out[p] = v[r];
-      if (k[r] < V && (p == 0 || sk[p - 1] != k[r])) atomicOr(present + (k[r] >> 5), 1u << (k[r] & 31));
+      // tokens after the previous row's, up to this row's, begin here; after the last row's, at the end
+      const int32_t before = p == 0 ? -1 : sk[p - 1];
+      for (int32_t q = before + 1; q <= min(k[r], V); ++q) starts[q] = p;
+      if (p == N - 1)
+        for (int32_t q = k[r] + 1; q <= V; ++q) starts[q] = N;
     }
   }
 }
@@ -604,11 +634,18 @@ __global__ void __launch_bounds__(kCombineWarps * 32) grad_combine(const int32_t
   Pieces r = {c + 1, 0, 0, 0, group};
   int32_t key = V;
   if (c < chunks) {
-    const int64_t p0 = c * chunk, p1 = min(N, p0 + chunk);
+    // everything that decides the common case is asked for at once
+    const int64_t p0 = c * chunk, p1 = min(N, p0 + chunk), p2 = min(N, p1 + chunk);
+    const int32_t k_first = keys[p0], k_before = p0 > 0 ? keys[p0 - 1] : -1, k_after = p1 < N ? keys[p1] : -1;
+    const int32_t k_third = p2 < N ? keys[p2] : -1;
     key = keys[p1 - 1];
-    if (key < V && p1 < N && keys[p1] == key && !(keys[p0] == key && p0 > 0 && keys[p0 - 1] == key)) {
+    if (key < V && k_after == key && !(k_first == key && k_before == key)) {
       // how many of the following chunks begin with the key: 32 probes at a time into a sorted list
       int64_t at = c + 1, left = chunks - at;
+      if (k_third != key) {
+        at += 1;
+        left = 0;
+      }
       while (left > 0) {
         const int64_t stride = (left + 31) / 32, probe = at + lane * stride;
         const bool same = lane * stride < left && keys[probe * chunk] == key;
@@ -678,10 +715,56 @@ __global__ void __launch_bounds__(kCombineWarps * 32) grad_combine(const int32_t
   }
 }
 
+// Small plans: one block per token (and 32 * VEC columns); its warps take every eighth row, four rows at a time, and their sums
+// are added in warp order.
+template <typename T, typename TO, int VEC>
+__global__ void __launch_bounds__(256) grad_small(const T* __restrict__ dout, int64_t dout_ld, const int32_t* __restrict__ starts,
+                                                  const int32_t* __restrict__ idx, int32_t F, float scale, TO* __restrict__ out,
+                                                  int64_t out_ld) {
+  __shared__ float sums[8][32 * VEC];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, v = blockIdx.x;
+  const int col = (blockIdx.y * 32 + lane) * VEC;
+  const bool on = col < F;
+  const int lo = starts[v], hi = starts[v + 1];
+  vio::Vec<VEC> acc(0.0f);
+  constexpr int U = 4;
+  for (int p = lo + warp; p < hi; p += 8 * U) {
+    int32_t i[U];
+    vio::Raw<T, VEC> r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) i[u] = p + 8 * u < hi ? idx[p + 8 * u] : -1;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (on && i[u] >= 0) r[u].template load<true>(dout + (int64_t)i[u] * dout_ld + col);
+      else r[u].zero();
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) acc.v[e] += r[u].get(e);
+  }
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) sums[warp][lane * VEC + e] = acc.v[e];
+  __syncthreads();
+  if (warp > 0 || !on) return;
+#pragma unroll
+  for (int w = 1; w < 8; ++w)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) acc.v[e] += sums[w][lane * VEC + e];
+  vio::store_stream<TO, VEC>(out + (int64_t)v * out_ld + col, vio::mul(acc, scale).v);
+}
+
 template <typename T, typename TO, int VEC>
 int32_t grad_vec(gnnco_handle* h, const PlanLayout& L, const T* dout, int64_t dout_ld, int64_t rows, int32_t V, int32_t F,
                  float scale, TO* out, int64_t out_ld, cudaStream_t st) {
   const int vecs = (F + VEC - 1) / VEC;
+  if (is_small(rows, V)) {
+    grad_small<T, TO, VEC><<<dim3((unsigned)V, (unsigned)((vecs + 31) / 32)), 256, 0, st>>>(dout, dout_ld, L.starts, plan_rows(L), F, scale,
+                                                                                          out, out_ld);
+    h->launches += 1;
+    GNNCO_LAUNCH_CHECK();
+    return GNNCO_OK;
+  }
   const int team = vecs <= 8 ? 8 : vecs <= 16 ? 16 : 32;
   const int teams = 256 / team;
   const unsigned cb = (unsigned)((L.chunks + teams - 1) / teams);
@@ -762,9 +845,9 @@ extern "C" int32_t gnnco_embedding_plan(gnnco_handle* h, const int32_t* tokens, 
   if (plan_bytes < L.bytes) return GNNCO_WORKSPACE_TOO_SMALL;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   ProfScope prof_(h, K_EMBED, st);
-  if (rows > 0 && rows <= kSmallRows) {
+  if (is_small(rows, V)) {
     order_small<<<1, kSmallThreads, 0, st>>>(tokens, (int32_t)rows, V, bits_of(V), const_cast<int32_t*>(plan_keys(L)),
-                                             const_cast<int32_t*>(plan_rows(L)), L.present, h->status);
+                                             const_cast<int32_t*>(plan_rows(L)), L.starts, h->status);
     h->launches += 1;
     GNNCO_LAUNCH_CHECK();
     return GNNCO_OK;

@@ -195,15 +195,15 @@ const int32_t* plan_rows(const PlanLayout& L) { return (L.passes & 1) ? L.idx_a 
 
 __device__ __forceinline__ int32_t token_key(int32_t t, int32_t V) { return (uint32_t)t < (uint32_t)V ? t : V; }
 
-// lanes of the warp with the same BITS-bit digit (one ballot per bit: match.any serialises over the distinct digits)
-template <int BITS>
-__device__ __forceinline__ uint32_t same_digit(uint32_t d, bool valid) {
+// lanes of the warp with the same digit (one ballot per bit: match.any serialises over the distinct digits)
+template <int MOST>
+__device__ __forceinline__ uint32_t same_digit(uint32_t d, int bits, bool valid) {
   uint32_t peers = __ballot_sync(0xffffffffu, valid);
 #pragma unroll
-  for (int b = 0; b < BITS; ++b) {
-    const bool one = (d >> b) & 1u;
-    const uint32_t m = __ballot_sync(0xffffffffu, one);
-    peers &= one ? m : ~m;
+  for (int b = 0; b < MOST; ++b) {
+    if (b >= bits) break;
+    const uint32_t one = (d >> b) & 1u;
+    peers &= __ballot_sync(0xffffffffu, one) ^ (one - 1u);   // lanes with the same bit as this one
   }
   return peers;
 }
@@ -285,9 +285,11 @@ __device__ __forceinline__ int32_t scan_block(int32_t x, int32_t* warp_tot) {
 template <bool FIRST>
 __global__ void __launch_bounds__(kOrdThreads, 3) order_scatter(const int32_t* __restrict__ keys, const int32_t* __restrict__ idx,
                                                              int32_t* __restrict__ keys_out, int32_t* __restrict__ idx_out,
-                                                             int64_t N, int64_t span, int shift, int digits, int32_t V,
+                                                             uint32_t N, uint32_t span, int shift, int bits, int32_t V,
                                                              const int32_t* __restrict__ hist, const int32_t* __restrict__ totals) {
   extern __shared__ int32_t sm[];
+  const int digits = 1 << bits;
+  const uint32_t digit_mask = (uint32_t)digits - 1u;
   int32_t* const sk = sm;                                  // the tile in digit order
   int32_t* const si = sm + kOrdTile;
   int32_t* const next = sm + 2 * kOrdTile;                 // [digits] where a digit's next row goes, less its place in the tile
@@ -306,25 +308,25 @@ __global__ void __launch_bounds__(kOrdThreads, 3) order_scatter(const int32_t* _
       at1 += hist[(int64_t)(2 * t + 1) * gridDim.x + blockIdx.x];
     }
   }
-  const int64_t lo = (int64_t)blockIdx.x * span, hi = min(N, lo + span);
-  for (int64_t p0 = lo; p0 < hi; p0 += kOrdTile) {
+  const uint32_t lo = blockIdx.x * span, hi = min(N, lo + span);   // positions stay below 2^32: N < 2^31
+  for (uint32_t p0 = lo; p0 < hi; p0 += kOrdTile) {
     for (int q = t; q < kOrdWarps * words; q += kOrdThreads) cnt[q] = 0;
     __syncthreads();
     // ranks inside the warp's 256 consecutive positions, in position order
     int32_t k[kOrdRounds];
     int rank[kOrdRounds];
-    const int64_t wbase = p0 + warp * (32 * kOrdRounds);
+    const uint32_t wbase = p0 + warp * (32 * kOrdRounds) + lane;
 #pragma unroll
     for (int r = 0; r < kOrdRounds; ++r) {
-      const int64_t p = wbase + r * 32 + lane;
+      const uint32_t p = wbase + r * 32;
       k[r] = p < hi ? (FIRST ? token_key(keys[p], V) : keys[p]) : 0;
     }
     uint16_t* const mine = cnt16 + warp * digits;
 #pragma unroll
     for (int r = 0; r < kOrdRounds; ++r) {
-      const bool valid = wbase + r * 32 + lane < hi;
-      const uint32_t d = (uint32_t)(k[r] >> shift) & (uint32_t)(digits - 1);
-      const uint32_t peers = same_digit<kOrdMaxBits>(d, valid);
+      const bool valid = wbase + r * 32 < hi;
+      const uint32_t d = ((uint32_t)k[r] >> shift) & digit_mask;
+      const uint32_t peers = same_digit<kOrdMaxBits>(d, bits, valid);
       const int before = __popc(peers & ((1u << lane) - 1u));
       rank[r] = valid ? mine[d] + before : 0;
       __syncwarp();
@@ -334,7 +336,7 @@ __global__ void __launch_bounds__(kOrdThreads, 3) order_scatter(const int32_t* _
     int32_t v[kOrdRounds];
 #pragma unroll
     for (int r = 0; r < kOrdRounds; ++r) {
-      const int64_t p = wbase + r * 32 + lane;
+      const uint32_t p = wbase + r * 32;
       v[r] = FIRST ? (int32_t)p : (p < hi ? idx[p] : 0);
     }
     __syncthreads();
@@ -360,19 +362,19 @@ __global__ void __launch_bounds__(kOrdThreads, 3) order_scatter(const int32_t* _
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kOrdRounds; ++r) {
-      if (wbase + r * 32 + lane < hi) {
-        const int32_t q = mine[(k[r] >> shift) & (digits - 1)] + rank[r];
+      if (wbase + r * 32 < hi) {
+        const int32_t q = mine[((uint32_t)k[r] >> shift) & digit_mask] + rank[r];
         sk[q] = k[r];
         si[q] = v[r];
       }
     }
     __syncthreads();
-    const int here = (int)min((int64_t)kOrdTile, hi - p0);
+    const int here = (int)min((uint32_t)kOrdTile, hi - p0);
 #pragma unroll
     for (int r = 0; r < kOrdRounds; ++r) {
       const int q = r * kOrdThreads + t;
       if (q < here) {
-        const int32_t key = sk[q], to = next[(key >> shift) & (digits - 1)] + q;
+        const int32_t key = sk[q], to = next[((uint32_t)key >> shift) & digit_mask] + q;
         keys_out[to] = key;
         idx_out[to] = si[q];
       }
@@ -410,7 +412,7 @@ __global__ void __launch_bounds__(kSmallThreads) order_small(const int32_t* __re
     for (int r = 0; r < kSmallRounds; ++r) {
       const bool valid = wbase + r * 32 + lane < N;
       const uint32_t d = (uint32_t)(k[r] >> shift) & 31u;
-      const uint32_t peers = same_digit<5>(d, valid);
+      const uint32_t peers = same_digit<5>(d, 5, valid);
       const int before = __popc(peers & ((1u << lane) - 1u));
       rank[r] = valid ? cnt[d * 33 + warp] + before : 0;
       __syncwarp();
@@ -608,7 +610,9 @@ __global__ void __launch_bounds__(kCombineWarps * 32) grad_combine(const int32_t
                                                                    const uint32_t* __restrict__ present,
                                                                    const float* __restrict__ partial, TO* __restrict__ out,
                                                                    int64_t out_ld) {
-  __shared__ Pieces run[kCombineWarps];                    // count() == 0: nothing for the block to do
+  __shared__ Pieces run[kCombineWarps];                    // the runs that the whole block adds, in any order: [big_runs]
+  __shared__ int64_t run_chunk[kCombineWarps];
+  __shared__ int32_t run_key[kCombineWarps], big_runs;
   __shared__ float sums[kCombineWarps * 32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (blockIdx.x >= chunk_blocks) {
@@ -630,6 +634,8 @@ __global__ void __launch_bounds__(kCombineWarps * 32) grad_combine(const int32_t
     }
     return;
   }
+  if (threadIdx.x == 0) big_runs = 0;
+  __syncthreads();
   const int64_t c0 = (int64_t)blockIdx.x * kCombineWarps, c = c0 + warp;
   Pieces r = {c + 1, 0, 0, 0, group};
   int32_t key = V;
@@ -657,8 +663,8 @@ __global__ void __launch_bounds__(kCombineWarps * 32) grad_combine(const int32_t
       }
       // [c + 1, at) begin with the key; all but perhaps the last hold nothing else
       const int64_t full = keys[min(N, at * chunk) - 1] == key ? at : at - 1;
-      const int64_t q0 = (c + 1 + group - 1) / group * group;
-      const int64_t groups = full > q0 ? (full - q0) / group : 0;
+      const int64_t q0 = (c + group) & ~(int64_t)(group - 1);   // group is a power of two
+      const int64_t groups = full > q0 ? (full - q0) >> (__ffs(group) - 1) : 0;
       r.groups = (int32_t)groups;
       r.lead = (int32_t)(groups > 0 ? q0 - (c + 1) : at - (c + 1));
       r.tail = (int32_t)(groups > 0 ? at - (q0 + groups * group) : 0);
@@ -680,18 +686,18 @@ __global__ void __launch_bounds__(kCombineWarps * 32) grad_combine(const int32_t
       vio::store_stream<TO, 1>(out + (int64_t)key * out_ld + col, f);
     }
   }
-  if (lane == 0) {
-    run[warp] = r;
-    if (more <= kFew) run[warp].lead = run[warp].groups = run[warp].tail = 0;
+  if (lane == 0 && more > kFew) {
+    const int at = atomicAdd(&big_runs, 1);
+    run[at] = r;
+    run_chunk[at] = c;
+    run_key[at] = key;
   }
   __syncthreads();
-  const int cx = (int)threadIdx.x % wide, ry = (int)threadIdx.x / wide, rows = kCombineWarps * 32 / wide;
-  for (int w = 0; w < kCombineWarps; ++w) {
+  const int cx = (int)threadIdx.x & (wide - 1), ry = (int)threadIdx.x / wide, rows = kCombineWarps * 32 / wide;
+  for (int w = 0; w < big_runs; ++w) {
     const Pieces big = run[w];
-    const int32_t m = big.count();
-    if (m == 0) continue;
-    const int64_t cw = c0 + w;
-    const int32_t key_w = keys[min(N, cw * chunk + chunk) - 1];
+    const int32_t m = big.count(), key_w = run_key[w];
+    const int64_t cw = run_chunk[w];
     for (int col0 = 0; col0 < F; col0 += wide) {
       const int col = col0 + cx;
       const bool on = col < F;
@@ -869,9 +875,9 @@ extern "C" int32_t gnnco_embedding_plan(gnnco_handle* h, const int32_t* tokens, 
     else order_histogram<false><<<nb, kOrdThreads, 0, st>>>(kin, rows, span, shift, digits, V, L.hist, nullptr);
     order_scan<<<digits, 1024, 0, st>>>(L.hist, L.totals, nb);
     if (p == 0)
-      order_scatter<true><<<nb, kOrdThreads, kScatterSmem, st>>>(kin, iin, ka, ia, rows, span, shift, digits, V, L.hist, L.totals);
+      order_scatter<true><<<nb, kOrdThreads, kScatterSmem, st>>>(kin, iin, ka, ia, (uint32_t)rows, (uint32_t)span, shift, L.bits, V, L.hist, L.totals);
     else
-      order_scatter<false><<<nb, kOrdThreads, kScatterSmem, st>>>(kin, iin, ka, ia, rows, span, shift, digits, V, L.hist, L.totals);
+      order_scatter<false><<<nb, kOrdThreads, kScatterSmem, st>>>(kin, iin, ka, ia, (uint32_t)rows, (uint32_t)span, shift, L.bits, V, L.hist, L.totals);
     kin = ka; iin = ia;
     int32_t* t = ka; ka = kb; kb = t;
     t = ia; ia = ib; ib = t;

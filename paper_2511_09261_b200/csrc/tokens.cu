@@ -499,12 +499,12 @@ __device__ __forceinline__ bool is_solid(const int32_t* __restrict__ keys, int64
 }
 
 template <typename T, typename TO, int VEC, int TEAM>
-__global__ void __launch_bounds__(256) grad_chunks(const T* __restrict__ dout, int64_t dout_ld, const int32_t* __restrict__ keys,
+__global__ void __launch_bounds__(256, 5) grad_chunks(const T* __restrict__ dout, int64_t dout_ld, const int32_t* __restrict__ keys,
                                                    const int32_t* __restrict__ idx, int64_t N, int32_t V, int32_t F, float scale,
                                                    int chunk, int64_t chunks, float* __restrict__ partial,
                                                    TO* __restrict__ out, int64_t out_ld) {
   constexpr int TEAMS = 256 / TEAM;
-  constexpr int U = VEC >= 8 ? 8 : 16;
+  constexpr int U = 4;
   const int tl = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
   const int col = (blockIdx.y * TEAM + tl) * VEC;
   const bool on = col < F;

@@ -17,6 +17,7 @@ namespace {
 
 size_t workspace_bytes(const gnnco_handle* h, int64_t sets, int32_t r, int32_t c) {
   const int32_t k = r < c ? r : c, n = r < c ? c : r;
+  if (ns_small_supported(k, n)) return 0;
   return align_up(ns_on_chip_supported(h, k, n) ? ns_on_chip_scratch_bytes(h, sets, k, n) : ns_tiles_workspace_bytes(sets, k, n));
 }
 
@@ -75,6 +76,7 @@ int32_t run_ns(gnnco_handle* h, int64_t sets, int32_t r, int32_t c, const TG* G,
   J.prefetch = sizeof(TG) == 4 && count % 4 == 0 && !((uintptr_t)G & 15) && !((uintptr_t)m & 15) && !((uintptr_t)W & 15);
   J.mu = mu; J.keep = keep; J.step = step; J.eps = P.eps; J.a = P.a; J.b = P.b; J.cc = P.c; J.p_scale = P.p_scale;
   J.scratch = ws; J.status = h->status;
+  if (ns_small_supported(k, n)) return launch_ns_small(h, J, st);
   return ns_on_chip_supported(h, k, n) ? launch_ns_on_chip(h, J, st) : launch_ns_tiles(h, J, ws, st);
 }
 

@@ -1,5 +1,5 @@
-// What the parts of the orthogonalised update share (muon.cu: entry points; muon_tc.cu: matrices that stay on chip;
-// muon_tiles.cu: larger ones).
+// What the parts of the orthogonalised update share (muon.cu: entry points; muon_small.cu: a warp per matrix; muon_tc.cu: matrices
+// that stay on chip; muon_tiles.cu: larger ones).
 #pragma once
 
 #include <atomic>
@@ -29,6 +29,10 @@ inline int32_t allow_shared_memory(Kernel kernel, size_t bytes, int device, std:
   done_for.store(device + 1);
   return GNNCO_OK;
 }
+
+// ---- muon_small.cu: short side up to 16, on the FMA units
+bool ns_small_supported(int32_t k, int32_t n);
+int32_t launch_ns_small(gnnco_handle* h, const NsJob& job, cudaStream_t st);
 
 // ---- muon_tc.cu: whole iterations on chip for k, n <= 256
 bool ns_on_chip_supported(const gnnco_handle* h, int32_t k, int32_t n);

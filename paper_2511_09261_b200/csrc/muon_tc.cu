@@ -374,15 +374,16 @@ __global__ void __launch_bounds__(Cfg<MODE>::THREADS, Cfg<MODE>::PER_SM) ns_on_c
       if (lane == 0) tc::mbar_arrive(&B->again);
       if (!wait(&B->again, again_it++ & 1)) break;
       // ---- momentum, u, |u|^2.  A unit (four columns of a row) of u waits as float32 in the two 8-byte places that its limbs
-      // will take; four units are asked for at a time.
+      // will take; four units (two where elements come one by one) are asked for at a time.
       double sum = 0.0;
       int ua = first_a, ub = first_b;
-      for (int q = threadIdx.x; q < total; q += 4 * kStride) {
-        float g[4][4], mv[4][4];
-        int at[4];                                         // unit's offset in the matrix, -1: outside
-        uint32_t place[4];                                 // ... and its place in the high limb
+      constexpr int kUnits = VEC4 ? 4 : 2;
+      for (int q = threadIdx.x; q < total; q += kUnits * kStride) {
+        float g[kUnits][4], mv[kUnits][4];
+        int at[kUnits];                                         // unit's offset in the matrix, -1: outside
+        uint32_t place[kUnits];                                 // ... and its place in the high limb
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
+        for (int y = 0; y < kUnits; ++y) {
           const int r = by_row ? ua : ub, unit = by_row ? ub : ua;
           next_unit(ua, ub);
           const int i = (int)rank * 128 + r, j = unit * 4;
@@ -409,7 +410,7 @@ __global__ void __launch_bounds__(Cfg<MODE>::THREADS, Cfg<MODE>::PER_SM) ns_on_c
           }
         }
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
+        for (int y = 0; y < kUnits; ++y) {
           if (q + y * kStride >= total) continue;
           if (Ms && at[y] >= 0) {
 #pragma unroll
@@ -601,62 +602,44 @@ __global__ void __launch_bounds__(Cfg<MODE>::THREADS, Cfg<MODE>::PER_SM) ns_on_c
         const float fo = 1.0f / (J.p_scale * kXScale), keep = J.keep, step_w = J.step;
         const uint32_t stage = sX + warp * 4096;
         bool waited = false;
-        for (int item = sub; item < 2 * C::XP; item += SUBS) {
+        auto first_wait = [&]() {                          // of the products that the last step ends with
+          if (!waited) ok = wait(&B->m3, ph);
+          if (ok && !waited) tc::tc_fence_after_sync();
+          waited = true;
+          return ok;
+        };
+        for (int item = sub; item < 2 * C::XP && ok; item += SUBS) {
           const bool in = works && item < x_items;
-          // the lane's values are `hop` apart: VEC4: 4 columns of every fourth row; rows of W: its 32 rows at one column;
-          // columns of W (transposed): its 32 columns of one row of X
-          const int i0 = (int)rank * 128 + quarter * 32 + (VEC4 ? lane >> 3 : J.transpose ? lane : 0);
-          const int j0 = item * 32 + (VEC4 ? (lane & 7) * 4 : J.transpose ? 0 : lane);
-          constexpr int kValues = VEC4 ? 8 : 32;
-          const int hop = VEC4 ? 4 * J.c : J.c;
-          int have = 0;
-          if (in && i0 < J.k && j0 < J.n) have = VEC4 ? (J.k - i0 + 3) / 4 : J.transpose ? J.n - j0 : J.k - i0;
-          const int at = J.transpose ? j0 * J.c + i0 : i0 * J.c + j0;
-          float w[VEC4 ? 32 : kValues];
-          if (Ws) {
+          if constexpr (VEC4) {
+            // 4 columns of every fourth row
+            const int i0 = (int)rank * 128 + quarter * 32 + (lane >> 3), j0 = item * 32 + (lane & 7) * 4, hop = 4 * J.c;
+            const int have = in && i0 < J.k && j0 < J.n ? (J.k - i0 + 3) / 4 : 0, at = i0 * J.c + j0;
+            float4 w[8];
+            if (Ws) {
 #pragma unroll
-            for (int e = 0; e < kValues; ++e) {
-              if constexpr (VEC4) {
-                const float4 a = e < have ? __ldcs(reinterpret_cast<const float4*>(Ws + at + e * hop)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                w[4 * e] = a.x; w[4 * e + 1] = a.y; w[4 * e + 2] = a.z; w[4 * e + 3] = a.w;
-              } else {
-                w[e] = e < have ? __ldcs(Ws + at + e * hop) : 0.0f;
-              }
+              for (int e = 0; e < 8; ++e)
+                w[e] = e < have ? __ldcs(reinterpret_cast<const float4*>(Ws + at + e * hop)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             }
-          }
-          if (!waited) {
-            if (!(ok = wait(&B->m3, ph))) break;
-            tc::tc_fence_after_sync();
-            waited = true;
-          }
-          if (!in) continue;
-          uint32_t v[32];
-          tc::tmem_ld_32x32(tmem + C::ACC3 + lanes + item * 32, v);
-          tc::tmem_ld_wait();
-          if (VEC4 || !J.transpose) {
+            if (!first_wait()) break;
+            if (!in) continue;
+            {
+              uint32_t v[32];
+              tc::tmem_ld_32x32(tmem + C::ACC3 + lanes + item * 32, v);
+              tc::tmem_ld_wait();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) tc::st_shared16(stage + at_chunk(lane, e), v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
-            __syncwarp();
-#pragma unroll
-            for (int e = 0; e < kValues; ++e) {
-              if constexpr (VEC4) {
-                const uint4 a = tc::ld_shared16(stage + at_chunk(4 * e + (lane >> 3), lane & 7));
-                v[4 * e] = a.x; v[4 * e + 1] = a.y; v[4 * e + 2] = a.z; v[4 * e + 3] = a.w;
-              } else {
-                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v[e]) : "r"(stage + at_chunk(e, lane >> 2) + (lane & 3) * 4) : "memory");
-              }
+              for (int e = 0; e < 8; ++e) tc::st_shared16(stage + at_chunk(lane, e), v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
             }
             __syncwarp();
-          }
 #pragma unroll
-          for (int e = 0; e < kValues; ++e) {
-            if (e >= have) continue;
-            if constexpr (VEC4) {
-              float x[4];
-#pragma unroll
-              for (int d = 0; d < 4; ++d) {
-                x[d] = __uint_as_float(v[4 * e + d]) * fo;
-                if (Ws) x[d] = w[4 * e + d] * keep - step_w * x[d];
+            for (int e = 0; e < 8; ++e) {
+              const uint4 a = tc::ld_shared16(stage + at_chunk(4 * e + (lane >> 3), lane & 7));
+              if (e >= have) continue;
+              float x[4] = {__uint_as_float(a.x) * fo, __uint_as_float(a.y) * fo, __uint_as_float(a.z) * fo, __uint_as_float(a.w) * fo};
+              if (Ws) {
+                x[0] = w[e].x * keep - step_w * x[0];
+                x[1] = w[e].y * keep - step_w * x[1];
+                x[2] = w[e].z * keep - step_w * x[2];
+                x[3] = w[e].w * keep - step_w * x[3];
               }
               if (Ws || !J.o_bf16) {
                 __stcs(reinterpret_cast<float4*>((Ws ? Ws : static_cast<float*>(J.O) + base) + at + e * hop), make_float4(x[0], x[1], x[2], x[3]));
@@ -664,12 +647,56 @@ __global__ void __launch_bounds__(Cfg<MODE>::THREADS, Cfg<MODE>::PER_SM) ns_on_c
                 __stcs(reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(J.O) + base + at + e * hop),
                        make_uint2(vio::pack_bf16(x[0], x[1]), vio::pack_bf16(x[2], x[3])));
               }
-            } else {
-              const float x = __uint_as_float(v[e]) * fo;
-              if (Ws) __stcs(Ws + at + e * hop, w[e] * keep - step_w * x);
-              else if (J.o_bf16) static_cast<__nv_bfloat16*>(J.O)[base + at + e * hop] = __float2bfloat16_rn(x);
-              else __stcs(static_cast<float*>(J.O) + base + at + e * hop, x);
             }
+            __syncwarp();
+          } else {
+            // rows of W: the item's 32 rows at one column per lane; columns of W (transposed): its 32 columns at one row of X per
+            // lane; 16 at a time
+            const int i0 = (int)rank * 128 + quarter * 32 + (J.transpose ? lane : 0), j0 = item * 32 + (J.transpose ? 0 : lane);
+            int have = 0;
+            if (in && i0 < J.k && j0 < J.n) have = J.transpose ? J.n - j0 : J.k - i0;
+            const int at0 = J.transpose ? j0 * J.c + i0 : i0 * J.c + j0;
+            if (!J.transpose) {
+              if (!first_wait()) break;
+              if (in) {
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                  uint32_t v[16];
+                  tc::tmem_ld_32x16(tmem + C::ACC3 + lanes + item * 32 + hf * 16, v);
+                  tc::tmem_ld_wait();
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) tc::st_shared16(stage + at_chunk(lane, hf * 4 + e), v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+                }
+                __syncwarp();
+              }
+            }
+#pragma unroll 1
+            for (int hf = 0; hf < 2; ++hf) {
+              const int at = at0 + hf * 16 * J.c, left = have - hf * 16;
+              float w[16];
+              uint32_t v[16];
+#pragma unroll
+              for (int e = 0; e < 16; ++e) w[e] = Ws && e < left ? __ldcs(Ws + at + e * J.c) : 0.0f;
+              if (!first_wait()) break;
+              if (!in) break;
+              if (J.transpose) {
+                tc::tmem_ld_32x16(tmem + C::ACC3 + lanes + item * 32 + hf * 16, v);
+                tc::tmem_ld_wait();
+              } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v[e]) : "r"(stage + at_chunk(hf * 16 + e, lane >> 2) + (lane & 3) * 4) : "memory");
+              }
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                if (e >= left) continue;
+                const float x = __uint_as_float(v[e]) * fo;
+                if (Ws) __stcs(Ws + at + e * J.c, w[e] * keep - step_w * x);
+                else if (J.o_bf16) static_cast<__nv_bfloat16*>(J.O)[base + at + e * J.c] = __float2bfloat16_rn(x);
+                else __stcs(static_cast<float*>(J.O) + base + at + e * J.c, x);
+              }
+            }
+            __syncwarp();
           }
         }
         if (!ok) break;

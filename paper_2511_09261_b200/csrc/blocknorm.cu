@@ -326,6 +326,10 @@ int32_t launch_width(bool backward, const NormArgs& A, int gate_kind, int sms, i
     if (v <= 512) GNNCO_NORM(32, 16);
     if (v <= 2048) GNNCO_NORM(256, 8);
     GNNCO_NORM(512, 16);
+  } else if constexpr (VEC == 2) {
+    if (v <= 256) GNNCO_NORM(32, 8);
+    if (v <= 1024) GNNCO_NORM(256, 4);
+    GNNCO_NORM(512, 8);
   } else if constexpr (VEC == 4) {
     if (v <= 1024) GNNCO_NORM(256, 4);
     GNNCO_NORM(512, 4);
@@ -348,6 +352,7 @@ int32_t launch_typed(bool backward, const NormArgs& A, int gate_kind, int sms, i
     if (fits(8)) return launch_width<T, 8>(backward, A, gate_kind, sms, blocks, st);
   }
   if (fits(4)) return launch_width<T, 4>(backward, A, gate_kind, sms, blocks, st);
+  if (fits(2)) return launch_width<T, 2>(backward, A, gate_kind, sms, blocks, st);
   return launch_width<T, 1>(backward, A, gate_kind, sms, blocks, st);
 }
 

@@ -5,6 +5,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <vector>
 
 #include "gnnco.h"
@@ -183,6 +184,15 @@ struct ProfScope {
     if (on && cudaEventRecord(rec.b, st) == cudaSuccess) h->prof.recs.push_back(rec);
   }
 };
+
+// Shared memory above 48 KB has to be asked for once per kernel and device (asking takes as long as launching).
+template <typename Kernel>
+inline int32_t allow_shared_memory(Kernel kernel, size_t bytes, int device, std::atomic<int>& done_for) {
+  if (done_for.load() == device + 1) return GNNCO_OK;
+  GNNCO_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+  done_for.store(device + 1);
+  return GNNCO_OK;
+}
 
 static inline size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
 

@@ -2,8 +2,6 @@
 // that stay on chip; muon_tiles.cu: larger ones).
 #pragma once
 
-#include <atomic>
-
 #include "internal.cuh"
 
 struct NsJob {
@@ -20,15 +18,6 @@ struct NsJob {
   void* scratch;
   int32_t* status;
 };
-
-// Shared memory above 48 KB has to be asked for once per kernel and device (asking takes as long as launching).
-template <typename Kernel>
-inline int32_t allow_shared_memory(Kernel kernel, size_t bytes, int device, std::atomic<int>& done_for) {
-  if (done_for.load() == device + 1) return GNNCO_OK;
-  GNNCO_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
-  done_for.store(device + 1);
-  return GNNCO_OK;
-}
 
 // ---- muon_small.cu: short side up to 16, on the FMA units
 bool ns_small_supported(int32_t k, int32_t n);

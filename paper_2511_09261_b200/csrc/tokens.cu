@@ -9,6 +9,8 @@
 // reads rows * F elements once and writes V * F.  The gradient uses no floating-point atomics: rows are visited in token
 // order, which fixes the order of every sum (bit-identical from run to run) and keeps the running sum of a token in
 // registers however often the token occurs.
+#include <atomic>
+
 #include "internal.cuh"
 #include "vec_io.cuh"
 
@@ -121,6 +123,8 @@ int32_t lookup_typed(gnnco_handle* h, const int32_t* tokens, const TT* table, in
     lookup_vec<TT, TO, 8>(tokens, table, table_ld, out, out_ld, rows, V, F, scale, tile, grid, h->status, st);
   else if (fits(4))
     lookup_vec<TT, TO, 4>(tokens, table, table_ld, out, out_ld, rows, V, F, scale, tile, grid, h->status, st);
+  else if (fits(2))
+    lookup_vec<TT, TO, 2>(tokens, table, table_ld, out, out_ld, rows, V, F, scale, tile, grid, h->status, st);
   else
     lookup_vec<TT, TO, 1>(tokens, table, table_ld, out, out_ld, rows, V, F, scale, tile, grid, h->status, st);
   h->launches += 1;
@@ -138,13 +142,14 @@ int32_t lookup_typed(gnnco_handle* h, const int32_t* tokens, const TT* table, in
 constexpr int kOrdThreads = 512, kOrdWarps = kOrdThreads / 32, kOrdRounds = 8;
 constexpr int kOrdTile = kOrdThreads * kOrdRounds;         // positions of one block-wide step
 constexpr int kOrdMaxBlocks = 444;                         // 3 per SM: all resident at once
+constexpr int kOrdFewBlocks = 24;                          // up to here no separate scan
 constexpr int kOrdMaxBits = 10, kOrdMaxDigits = 1 << kOrdMaxBits;
-constexpr int kSmallRows = 4096, kSmallTokens = 4096;      // up to here one block sorts everything in shared memory
+constexpr int kSmallRows = 4096;                           // up to here one block sorts everything in shared memory
 
 struct PlanLayout {
   int32_t *key_a, *idx_a, *key_b, *idx_b, *hist, *totals;
   uint32_t* present;
-  int32_t* starts;                                         // [V + 1] first position of each token (small plans only)
+  int32_t* runs;                                           // small plans only: number of runs, their first positions, the last one's end
   float* partial;                                          // [chunks][2][F]
   size_t bytes;
   int64_t chunks;
@@ -166,8 +171,8 @@ int chunk_of(int64_t rows) {
   return c;
 }
 
-// Few rows and few tokens: one block sorts, and one block per token adds its rows.
-bool is_small(int64_t rows, int32_t V) { return rows > 0 && rows <= kSmallRows && V <= kSmallTokens; }
+// Few rows: one block sorts, and one block per token that occurs adds its rows.
+bool is_small(int64_t rows) { return rows > 0 && rows <= kSmallRows; }
 
 PlanLayout plan_layout(void* ws, int64_t rows, int32_t V, int32_t F) {
   Carver c(ws, 0);
@@ -184,7 +189,7 @@ PlanLayout plan_layout(void* ws, int64_t rows, int32_t V, int32_t F) {
   L.hist = c.take<int32_t>(kOrdMaxDigits * (size_t)kOrdMaxBlocks);
   L.totals = c.take<int32_t>(kOrdMaxDigits);
   L.present = c.take<uint32_t>(((size_t)V + 31) / 32);
-  L.starts = c.take<int32_t>(is_small(rows, V) ? V + 1 : 0);
+  L.runs = c.take<int32_t>(is_small(rows) ? rows + 2 : 0);
   L.partial = c.take<float>((size_t)L.chunks * 2 * F);
   L.bytes = c.off;
   return L;
@@ -212,10 +217,13 @@ __device__ __forceinline__ uint32_t same_digit(uint32_t d, int bits, bool valid)
 template <bool FIRST>
 __global__ void __launch_bounds__(kOrdThreads) order_histogram(const int32_t* __restrict__ keys, int64_t N, int64_t span,
                                                                int shift, int digits, int32_t V, int32_t* __restrict__ hist,
-                                                               int32_t* status) {
+                                                               uint32_t* present, int32_t* status) {
   __shared__ int32_t cnt[kOrdMaxDigits];
   for (int d = threadIdx.x; d < digits; d += kOrdThreads) cnt[d] = 0;
   __syncthreads();
+  if (FIRST)                                               // the gradient marks the tokens that occur
+    for (int64_t w = (int64_t)blockIdx.x * kOrdThreads + threadIdx.x; w < ((int64_t)V + 31) / 32; w += (int64_t)gridDim.x * kOrdThreads)
+      present[w] = 0u;
   const int64_t lo = (int64_t)blockIdx.x * span, hi = min(N, lo + span);
   bool wrong = false;
   for (int64_t p0 = lo; p0 < hi; p0 += kOrdThreads * 4) {
@@ -300,13 +308,31 @@ __global__ void __launch_bounds__(kOrdThreads, 3) order_scatter(const int32_t* _
   const bool owns = t < words;
   int32_t at0, at1;                                        // of digits 2 t and 2 t + 1
   {
-    const int32_t a = owns ? totals[2 * t] : 0, b = owns ? totals[2 * t + 1] : 0;
-    at0 = scan_block(a + b, warp_tot);
-    at1 = at0 + a;
+    // the digit's total over all blocks, and its rows in the blocks before this one
+    int32_t a = 0, b = 0, a_before = 0, b_before = 0;
     if (owns) {
-      at0 += hist[(int64_t)(2 * t) * gridDim.x + blockIdx.x];
-      at1 += hist[(int64_t)(2 * t + 1) * gridDim.x + blockIdx.x];
+      const int32_t* const ha = hist + (int64_t)(2 * t) * gridDim.x;
+      const int32_t* const hb = ha + gridDim.x;
+      if (totals) {
+        a = totals[2 * t];
+        b = totals[2 * t + 1];
+        a_before = ha[blockIdx.x];
+        b_before = hb[blockIdx.x];
+      } else {
+#pragma unroll 4
+        for (unsigned q = 0; q < gridDim.x; ++q) {
+          const int32_t x = ha[q], y = hb[q];
+          a += x;
+          b += y;
+          if (q < blockIdx.x) {
+            a_before += x;
+            b_before += y;
+          }
+        }
+      }
     }
+    at0 = scan_block(a + b, warp_tot) + a_before;
+    at1 = at0 - a_before + a + b_before;
   }
   const uint32_t lo = blockIdx.x * span, hi = min(N, lo + span);   // positions stay below 2^32: N < 2^31
   for (uint32_t p0 = lo; p0 < hi; p0 += kOrdTile) {
@@ -389,13 +415,16 @@ constexpr size_t kScatterSmem = (size_t)(2 * kOrdTile + kOrdMaxDigits + kOrdWarp
 constexpr int kSmallThreads = 1024, kSmallRounds = kSmallRows / kSmallThreads;
 __global__ void __launch_bounds__(kSmallThreads) order_small(const int32_t* __restrict__ tokens, int32_t N, int32_t V, int bits,
                                                              int32_t* __restrict__ keys_out, int32_t* __restrict__ idx_out,
-                                                             int32_t* __restrict__ starts, int32_t* status) {
+                                                             uint32_t* present, bool clear_present, int32_t* __restrict__ runs,
+                                                             int32_t* status) {
   __shared__ int32_t sk[kSmallRows], si[kSmallRows];
   __shared__ int32_t cnt[32 * 33];                         // [digit][warp]
   __shared__ int32_t tot[32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int32_t k[kSmallRounds], v[kSmallRounds];
   const int wbase = warp * (32 * kSmallRounds);
+  if (clear_present)
+    for (int32_t w = threadIdx.x; w < (V + 31) / 32; w += kSmallThreads) present[w] = 0u;
 #pragma unroll
   for (int r = 0; r < kSmallRounds; ++r) {
     const int p = wbase + r * 32 + lane;
@@ -451,25 +480,57 @@ __global__ void __launch_bounds__(kSmallThreads) order_small(const int32_t* __re
       v[r] = p < N ? si[p] : 0;
     }
   }
+  // where runs begin, numbered in order
+  uint32_t heads[kSmallRounds];
+  int32_t here = 0;
 #pragma unroll
   for (int r = 0; r < kSmallRounds; ++r) {
     const int p = wbase + r * 32 + lane;
+    const bool head = p < N && k[r] < V && (p == 0 || sk[p - 1] != k[r]);
     if (p < N) {
       keys_out[p] = k[r];
       idx_out[p] = v[r];
-      // tokens after the previous row's, up to this row's, begin here; after the last row's, at the end
-      const int32_t before = p == 0 ? -1 : sk[p - 1];
-      for (int32_t q = before + 1; q <= min(k[r], V); ++q) starts[q] = p;
-      if (p == N - 1)
-        for (int32_t q = k[r] + 1; q <= V; ++q) starts[q] = N;
+    }
+    if (head) atomicOr(present + (k[r] >> 5), 1u << (k[r] & 31));
+    heads[r] = __ballot_sync(0xffffffffu, head);
+    here += __popc(heads[r]);
+  }
+  __syncthreads();                                         // (tot is free again)
+  if (lane == 0) tot[warp] = here;
+  __syncthreads();
+  int32_t at = lane < warp ? tot[lane] : 0;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) at += __shfl_xor_sync(0xffffffffu, at, d);
+#pragma unroll
+  for (int r = 0; r < kSmallRounds; ++r) {
+    const int p = wbase + r * 32 + lane;
+    if ((heads[r] >> lane) & 1u) runs[1 + at + __popc(heads[r] & ((1u << lane) - 1u))] = p;
+    at += __popc(heads[r]);
+    // the position after the last row with a token ends the last run
+    if (p < N && k[r] < V && (p == N - 1 || sk[p + 1] >= V)) {
+      int32_t all = 0;
+#pragma unroll 1
+      for (int w = 0; w < 32; ++w) all += tot[w];
+      runs[0] = all;
+      runs[1 + all] = p + 1;
     }
   }
+  if (threadIdx.x == 0 && sk[0] >= V) runs[0] = 0;
 }
 
-// one bit per token that occurs, from the sorted keys (where a run begins)
+// ------------------------------------------------------------------------------------------------------ gradient
+//
+// The sorted positions are cut into chunks of equal length, one team of TEAM lanes per chunk and block of TEAM * VEC
+// columns, so a token that holds a third of all rows costs no more than a thousand small ones.  A run that lies inside a
+// chunk goes straight to the table; the pieces of a run that crosses a chunk boundary meet in `partial`:
+// slot 0 = the chunk's first run, begun in an earlier chunk; slot 1 = its last run, begun here and continued in the next.
+// A block whose chunks all lie inside one run (a token with thousands of rows) adds its teams' sums first and leaves them in
+// slot 0 of its first chunk.  The second kernel also writes the zero rows of tokens that do not occur.
+
+// One bit per token that occurs, where its run begins in the sorted keys.
 constexpr int kMarkPer = 8;
-__global__ void __launch_bounds__(256) order_mark(const int32_t* __restrict__ keys, int64_t N, int32_t V, uint32_t* present) {
-  const int64_t p0 = (int64_t)blockIdx.x * (256 * kMarkPer) + threadIdx.x;
+__device__ __forceinline__ void mark_present(const int32_t* __restrict__ keys, int64_t N, int32_t V, int64_t block, uint32_t* present) {
+  const int64_t p0 = block * (256 * kMarkPer) + threadIdx.x;
   int32_t k[kMarkPer], before[kMarkPer];
 #pragma unroll
   for (int u = 0; u < kMarkPer; ++u) {
@@ -482,14 +543,6 @@ __global__ void __launch_bounds__(256) order_mark(const int32_t* __restrict__ ke
     if (k[u] < V && before[u] != k[u]) atomicOr(present + (k[u] >> 5), 1u << (k[u] & 31));
 }
 
-// ------------------------------------------------------------------------------------------------------ gradient
-//
-// The sorted positions are cut into chunks of equal length, one team of TEAM lanes per chunk and block of TEAM * VEC
-// columns, so a token that holds a third of all rows costs no more than a thousand small ones.  A run that lies inside a
-// chunk goes straight to the table; the pieces of a run that crosses a chunk boundary meet in `partial`:
-// slot 0 = the chunk's first run, begun in an earlier chunk; slot 1 = its last run, begun here and continued in the next.
-// A block whose chunks all lie inside one run (a token with thousands of rows) adds its teams' sums first and leaves them in
-// slot 0 of its first chunk.  The second kernel also writes the zero rows of tokens that do not occur.
 // Whether chunks [c, c + group) all exist and hold nothing but one token, whose run began before them.
 __device__ __forceinline__ bool is_solid(const int32_t* __restrict__ keys, int64_t N, int32_t V, int64_t c, int group, int chunk,
                                          int64_t chunks) {
@@ -498,80 +551,100 @@ __device__ __forceinline__ bool is_solid(const int32_t* __restrict__ keys, int64
   return k < V && keys[min(N, (c + group) * chunk) - 1] == k;
 }
 
-template <typename T, typename TO, int VEC, int TEAM>
-__global__ void __launch_bounds__(256, 5) grad_chunks(const T* __restrict__ dout, int64_t dout_ld, const int32_t* __restrict__ keys,
+// Rows in flight against blocks per SM, ordering included: 10M x 256 bf16 takes 1,409 us with eight rows at four blocks (1,424 with four
+// at five, 1,545 with eight at three), 1.13M x 128 float32 168 us with four rows at five blocks (177 with eight at four); more
+// blocks spill registers (1,560 and 191 us at six).
+// A lane holds K vectors, TEAM vectors apart (narrow vectors: more columns per visit of a row).  The blocks after the last chunk
+// mark the tokens that occur.
+template <typename T, typename TO, int VEC, int TEAM, int K>
+__global__ void __launch_bounds__(256, K == 1 && VEC < 8 ? 5 : 4) grad_chunks(const T* __restrict__ dout, int64_t dout_ld, const int32_t* __restrict__ keys,
                                                    const int32_t* __restrict__ idx, int64_t N, int32_t V, int32_t F, float scale,
-                                                   int chunk, int64_t chunks, float* __restrict__ partial,
-                                                   TO* __restrict__ out, int64_t out_ld) {
-  constexpr int TEAMS = 256 / TEAM;
-  constexpr int U = 4;
+                                                   int chunk, int64_t chunks, unsigned chunk_blocks, uint32_t* present,
+                                                   float* __restrict__ partial, TO* __restrict__ out, int64_t out_ld) {
+  constexpr int TEAMS = 256 / TEAM, W = TEAM * VEC * K;    // columns of a block
+  constexpr int U = VEC >= 8 ? 8 : 4;
+  if (blockIdx.x >= chunk_blocks) {
+    if (blockIdx.y == 0) mark_present(keys, N, V, blockIdx.x - chunk_blocks, present);
+    return;
+  }
   const int tl = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
-  const int col = (blockIdx.y * TEAM + tl) * VEC;
-  const bool on = col < F;
+  const int col0 = blockIdx.y * W + tl * VEC;              // vector q of this lane: column col0 + q TEAM VEC
   const int64_t cb = (int64_t)blockIdx.x * TEAMS, c = cb + team;
   // one run from before this block's first position to its last (the same answer for the whole block)
   const bool solid = is_solid(keys, N, V, cb, TEAMS, chunk, chunks);
   if (c >= chunks) return;                                 // whole teams leave together (shuffles below name the team); never of a solid block
   const uint32_t mask = TEAM == 32 ? 0xffffffffu : ((1u << TEAM) - 1u) << ((threadIdx.x & 31) / TEAM * TEAM);
   const int64_t p0 = c * chunk, p1 = min(N, p0 + chunk);
-  float acc[VEC];
+  vio::Vec<VEC> acc[K];
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) acc[e] = 0.0f;
+  for (int q = 0; q < K; ++q) acc[q] = vio::Vec<VEC>(0.0f);
   int32_t cur = keys[p0];
   bool head = p0 > 0 && keys[p0 - 1] == cur;
   auto to_table = [&]() {
-    float f[VEC];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) f[e] = scale * acc[e];
-    vio::store_stream<TO, VEC>(out + (int64_t)cur * out_ld + col, f);
+    for (int q = 0; q < K; ++q)
+      if (col0 + q * TEAM * VEC < F)
+        vio::store_stream<TO, VEC>(out + (int64_t)cur * out_ld + col0 + q * TEAM * VEC, vio::mul(acc[q], scale).v);
   };
   auto to_partial = [&](int slot) {
-    float* p = partial + (c * 2 + slot) * F + col;
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) p[e] = acc[e];
+    for (int q = 0; q < K; ++q) {
+      float* const p = partial + (c * 2 + slot) * F + col0 + q * TEAM * VEC;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (col0 + q * TEAM * VEC < F) p[e] = acc[q].v[e];
+    }
   };
   for (int64_t pb = p0; pb < p1 && cur < V; pb += TEAM) {
     const int64_t mine = pb + tl;
     const int32_t k_l = mine < p1 ? keys[mine] : V;
     const int32_t i_l = mine < p1 ? idx[mine] : 0;
+#pragma unroll 1
+    for (int j0 = 0; j0 < TEAM; j0 += U) {
+      vio::Raw<T, VEC> v[U][K];
+      int32_t k[U];
 #pragma unroll
-    for (int j0 = 0; j0 < TEAM; j0 += (U < TEAM ? U : TEAM)) {
-      constexpr int UU = U < TEAM ? U : TEAM;
-      vio::Raw<T, VEC> v[UU];
-      int32_t k[UU];
-#pragma unroll
-      for (int u = 0; u < UU; ++u) {
+      for (int u = 0; u < U; ++u) {
         k[u] = __shfl_sync(mask, k_l, j0 + u, TEAM);
         const int32_t i = __shfl_sync(mask, i_l, j0 + u, TEAM);
-        if (on && k[u] < V) v[u].template load<true>(dout + (int64_t)i * dout_ld + col);
-        else v[u].zero();
+        const T* const row = dout + (int64_t)i * dout_ld + col0;
+#pragma unroll
+        for (int q = 0; q < K; ++q) {
+          if (col0 + q * TEAM * VEC < F && k[u] < V) v[u][q].template load<true>(row + q * TEAM * VEC);
+          else v[u][q].zero();
+        }
       }
 #pragma unroll
-      for (int u = 0; u < UU; ++u) {
+      for (int u = 0; u < U; ++u) {
         if (k[u] != cur) {                                 // uniform over the team
-          if (cur < V && on && pb + j0 + u < p1) {
+          const bool real = pb + j0 + u < p1;
+          if (cur < V && real) {
             if (head) to_partial(0);
             else to_table();
           }
-          if (pb + j0 + u < p1) {
+          if (real) {
             head = false;
             cur = k[u];
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) acc[e] = 0.0f;
+            for (int q = 0; q < K; ++q) acc[q] = vio::Vec<VEC>(0.0f);
           }
         }
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) acc[e] += v[u].get(e);
+        for (int q = 0; q < K; ++q)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) acc[q].v[e] += v[u][q].get(e);
       }
     }
   }
   if (solid) {
-    __shared__ float sums[TEAMS][TEAM * VEC];
+    __shared__ float sums[TEAMS][W];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) sums[team][tl * VEC + e] = acc[e];
+    for (int q = 0; q < K; ++q)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sums[team][(q * TEAM + tl) * VEC + e] = acc[q].v[e];
     __syncthreads();
-    for (int q = threadIdx.x; q < TEAM * VEC; q += 256) {
-      const int f = blockIdx.y * TEAM * VEC + q;
+    for (int q = threadIdx.x; q < W; q += 256) {
+      const int f = blockIdx.y * W + q;
       float t = 0.0f;
 #pragma unroll
       for (int k = 0; k < TEAMS; ++k) t += sums[k][q];
@@ -579,7 +652,7 @@ __global__ void __launch_bounds__(256, 5) grad_chunks(const T* __restrict__ dout
     }
     return;
   }
-  if (cur >= V || !on) return;
+  if (cur >= V) return;
   const bool goes_on = p1 < N && keys[p1] == cur;
   if (head) to_partial(0);
   else if (goes_on) to_partial(1);
@@ -721,17 +794,28 @@ __global__ void __launch_bounds__(kCombineWarps * 32) grad_combine(const int32_t
   }
 }
 
-// Small plans: one block per token (and 32 * VEC columns); its warps take every eighth row, four rows at a time, and their sums
-// are added in warp order.
+// Small plans: one block per run (and 32 * VEC columns); its warps take every eighth row, four rows at a time, and their sums are
+// added in warp order.  The blocks after the last possible run write the zero rows, 32 tokens per warp.
 template <typename T, typename TO, int VEC>
-__global__ void __launch_bounds__(256) grad_small(const T* __restrict__ dout, int64_t dout_ld, const int32_t* __restrict__ starts,
-                                                  const int32_t* __restrict__ idx, int32_t F, float scale, TO* __restrict__ out,
-                                                  int64_t out_ld) {
+__global__ void __launch_bounds__(256) grad_small(const T* __restrict__ dout, int64_t dout_ld, const int32_t* __restrict__ runs,
+                                                  const int32_t* __restrict__ keys, const int32_t* __restrict__ idx,
+                                                  const uint32_t* __restrict__ present, unsigned run_blocks, int32_t V, int32_t F,
+                                                  float scale, TO* __restrict__ out, int64_t out_ld) {
   __shared__ float sums[8][32 * VEC];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, v = blockIdx.x;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int col = (blockIdx.y * 32 + lane) * VEC;
   const bool on = col < F;
-  const int lo = starts[v], hi = starts[v + 1];
+  if (blockIdx.x >= run_blocks) {
+    const int64_t v0 = ((int64_t)(blockIdx.x - run_blocks) * 8 + warp) * 32;
+    if (v0 >= V || !on) return;
+    uint32_t gone = ~present[v0 >> 5];
+    if (V - v0 < 32) gone &= (1u << (V - v0)) - 1u;
+    const vio::Vec<VEC> z(0.0f);
+    for (; gone; gone &= gone - 1) vio::store_stream<TO, VEC>(out + (v0 + __ffs(gone) - 1) * out_ld + col, z.v);
+    return;
+  }
+  if ((int)blockIdx.x >= runs[0]) return;
+  const int lo = runs[1 + blockIdx.x], hi = runs[2 + blockIdx.x], v = keys[lo];
   vio::Vec<VEC> acc(0.0f);
   constexpr int U = 4;
   for (int p = lo + warp; p < hi; p += 8 * U) {
@@ -764,9 +848,10 @@ template <typename T, typename TO, int VEC>
 int32_t grad_vec(gnnco_handle* h, const PlanLayout& L, const T* dout, int64_t dout_ld, int64_t rows, int32_t V, int32_t F,
                  float scale, TO* out, int64_t out_ld, cudaStream_t st) {
   const int vecs = (F + VEC - 1) / VEC;
-  if (is_small(rows, V)) {
-    grad_small<T, TO, VEC><<<dim3((unsigned)V, (unsigned)((vecs + 31) / 32)), 256, 0, st>>>(dout, dout_ld, L.starts, plan_rows(L), F, scale,
-                                                                                          out, out_ld);
+  if (is_small(rows)) {
+    const unsigned rb = (unsigned)(rows < V ? rows : V), zb = (unsigned)(((int64_t)V + 255) / 256);
+    grad_small<T, TO, VEC><<<dim3(rb + zb, (unsigned)((vecs + 31) / 32)), 256, 0, st>>>(dout, dout_ld, L.runs, plan_keys(L), plan_rows(L), L.present,
+                                                                                      rb, V, F, scale, out, out_ld);
     h->launches += 1;
     GNNCO_LAUNCH_CHECK();
     return GNNCO_OK;
@@ -774,15 +859,17 @@ int32_t grad_vec(gnnco_handle* h, const PlanLayout& L, const T* dout, int64_t do
   const int team = vecs <= 8 ? 8 : vecs <= 16 ? 16 : 32;
   const int teams = 256 / team;
   const unsigned cb = (unsigned)((L.chunks + teams - 1) / teams);
-  const dim3 grid(cb, (unsigned)((vecs + team - 1) / team));
   const int32_t *keys = plan_keys(L), *idx = plan_rows(L);
   if (L.chunks > 0) {
-#define GNNCO_GRAD(TM)                                                                                                 \
-  grad_chunks<T, TO, VEC, TM><<<grid, 256, 0, st>>>(dout, dout_ld, keys, idx, rows, V, F, scale, L.chunk, L.chunks, \
-                                                   L.partial, out, out_ld)
-    if (team == 8) GNNCO_GRAD(8);
-    else if (team == 16) GNNCO_GRAD(16);
-    else GNNCO_GRAD(32);
+    constexpr int K = VEC == 1 ? 4 : VEC == 2 ? 2 : 1;
+    const unsigned mb = (unsigned)((rows + 256 * kMarkPer - 1) / (256 * kMarkPer));
+#define GNNCO_GRAD(TM, KK)                                                                                                        \
+  grad_chunks<T, TO, VEC, TM, KK><<<dim3(cb + mb, (unsigned)((vecs + TM * KK - 1) / (TM * KK))), 256, 0, st>>>(                   \
+      dout, dout_ld, keys, idx, rows, V, F, scale, L.chunk, L.chunks, cb, L.present, L.partial, out, out_ld)
+    if (team == 8) GNNCO_GRAD(8, 1);
+    else if (team == 16) GNNCO_GRAD(16, 1);
+    else if (vecs <= 32) GNNCO_GRAD(32, 1);
+    else GNNCO_GRAD(32, K);
 #undef GNNCO_GRAD
     h->launches += 1;
   }
@@ -808,6 +895,7 @@ int32_t grad_typed(gnnco_handle* h, const PlanLayout& L, const void* dout, int64
   TO* o = static_cast<TO*>(out);
   if (sizeof(T) == 2 && fits(8)) return grad_vec<T, TO, 8>(h, L, d, dout_ld, rows, V, F, scale, o, out_ld, st);
   if (fits(4)) return grad_vec<T, TO, 4>(h, L, d, dout_ld, rows, V, F, scale, o, out_ld, st);
+  if (fits(2)) return grad_vec<T, TO, 2>(h, L, d, dout_ld, rows, V, F, scale, o, out_ld, st);
   return grad_vec<T, TO, 1>(h, L, d, dout_ld, rows, V, F, scale, o, out_ld, st);
 }
 
@@ -851,17 +939,23 @@ extern "C" int32_t gnnco_embedding_plan(gnnco_handle* h, const int32_t* tokens, 
   if (plan_bytes < L.bytes) return GNNCO_WORKSPACE_TOO_SMALL;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   ProfScope prof_(h, K_EMBED, st);
-  if (is_small(rows, V)) {
+  if (is_small(rows)) {
+    const bool clear = V <= (1 << 18);                     // the block clears up to 8,192 words itself
+    if (!clear) GNNCO_CUDA_TRY(cudaMemsetAsync(L.present, 0, ((size_t)V + 31) / 32 * 4, st));
     order_small<<<1, kSmallThreads, 0, st>>>(tokens, (int32_t)rows, V, bits_of(V), const_cast<int32_t*>(plan_keys(L)),
-                                             const_cast<int32_t*>(plan_rows(L)), L.starts, h->status);
+                                             const_cast<int32_t*>(plan_rows(L)), L.present, clear, L.runs, h->status);
     h->launches += 1;
     GNNCO_LAUNCH_CHECK();
     return GNNCO_OK;
   }
-  GNNCO_CUDA_TRY(cudaMemsetAsync(L.present, 0, ((size_t)V + 31) / 32 * 4, st));
-  if (rows == 0) return GNNCO_OK;
-  GNNCO_CUDA_TRY(cudaFuncSetAttribute(order_scatter<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kScatterSmem));
-  GNNCO_CUDA_TRY(cudaFuncSetAttribute(order_scatter<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kScatterSmem));
+  if (rows == 0) {
+    GNNCO_CUDA_TRY(cudaMemsetAsync(L.present, 0, ((size_t)V + 31) / 32 * 4, st));
+    return GNNCO_OK;
+  }
+  static std::atomic<int> allowed_first{0}, allowed_rest{0};
+  int32_t rc = allow_shared_memory(order_scatter<true>, kScatterSmem, h->device, allowed_first);
+  if (rc == GNNCO_OK) rc = allow_shared_memory(order_scatter<false>, kScatterSmem, h->device, allowed_rest);
+  if (rc != GNNCO_OK) return rc;
   const int64_t tiles = (rows + kOrdTile - 1) / kOrdTile;
   const int64_t per = (tiles + kOrdMaxBlocks - 1) / kOrdMaxBlocks;
   const int64_t span = per * kOrdTile;
@@ -871,20 +965,22 @@ extern "C" int32_t gnnco_embedding_plan(gnnco_handle* h, const int32_t* tokens, 
   const int32_t* iin = nullptr;
   for (int p = 0; p < L.passes; ++p) {
     const int shift = p * L.bits;
-    if (p == 0) order_histogram<true><<<nb, kOrdThreads, 0, st>>>(kin, rows, span, shift, digits, V, L.hist, h->status);
-    else order_histogram<false><<<nb, kOrdThreads, 0, st>>>(kin, rows, span, shift, digits, V, L.hist, nullptr);
-    order_scan<<<digits, 1024, 0, st>>>(L.hist, L.totals, nb);
+    if (p == 0) order_histogram<true><<<nb, kOrdThreads, 0, st>>>(kin, rows, span, shift, digits, V, L.hist, L.present, h->status);
+    else order_histogram<false><<<nb, kOrdThreads, 0, st>>>(kin, rows, span, shift, digits, V, L.hist, nullptr, nullptr);
+    // few blocks: the scatter adds up the block counts itself
+    const bool scanned = nb > kOrdFewBlocks;
+    if (scanned) order_scan<<<digits, 1024, 0, st>>>(L.hist, L.totals, nb);
     if (p == 0)
-      order_scatter<true><<<nb, kOrdThreads, kScatterSmem, st>>>(kin, iin, ka, ia, (uint32_t)rows, (uint32_t)span, shift, L.bits, V, L.hist, L.totals);
+      order_scatter<true><<<nb, kOrdThreads, kScatterSmem, st>>>(kin, iin, ka, ia, (uint32_t)rows, (uint32_t)span, shift, L.bits, V, L.hist,
+                                                                scanned ? L.totals : nullptr);
     else
-      order_scatter<false><<<nb, kOrdThreads, kScatterSmem, st>>>(kin, iin, ka, ia, (uint32_t)rows, (uint32_t)span, shift, L.bits, V, L.hist, L.totals);
+      order_scatter<false><<<nb, kOrdThreads, kScatterSmem, st>>>(kin, iin, ka, ia, (uint32_t)rows, (uint32_t)span, shift, L.bits, V, L.hist,
+                                                                 scanned ? L.totals : nullptr);
     kin = ka; iin = ia;
     int32_t* t = ka; ka = kb; kb = t;
     t = ia; ia = ib; ib = t;
-    h->launches += 3;
+    h->launches += scanned ? 3 : 2;
   }
-  order_mark<<<(unsigned)((rows + 256 * kMarkPer - 1) / (256 * kMarkPer)), 256, 0, st>>>(kin, rows, V, L.present);
-  h->launches += 1;
   GNNCO_LAUNCH_CHECK();
   return GNNCO_OK;
 }

@@ -68,6 +68,8 @@ __device__ __forceinline__ void store_stream(T* p, const float (&v)[VEC]) {
 #pragma unroll
       for (int i = 0; i < VEC / 4; ++i)
         __stcs(reinterpret_cast<float4*>(p) + i, make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
+    } else if constexpr (VEC == 2) {
+      __stcs(reinterpret_cast<float2*>(p), make_float2(v[0], v[1]));
     } else {
 #pragma unroll
       for (int i = 0; i < VEC; ++i) __stcs(p + i, v[i]);
@@ -77,6 +79,8 @@ __device__ __forceinline__ void store_stream(T* p, const float (&v)[VEC]) {
                                                    pack_bf16(v[6], v[7])));
   } else if constexpr (VEC == 4) {
     __stcs(reinterpret_cast<uint2*>(p), make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])));
+  } else if constexpr (VEC == 2) {
+    __stcs(reinterpret_cast<uint32_t*>(p), pack_bf16(v[0], v[1]));
   } else {
 #pragma unroll
     for (int i = 0; i < VEC; ++i)

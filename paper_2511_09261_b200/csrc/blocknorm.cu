@@ -309,12 +309,26 @@ int32_t launch_one(bool backward, const NormArgs& A, int gate_kind, int sms, int
   return GNNCO_OK;
 }
 
-// The smallest team whose lanes hold a row in at most 16 elements each (8 for teams of up to a warp where vectors fit).
+// Few lanes with several vectors each beat many lanes with one: fewer shuffles per row, and fewer idle lanes where a row is no power
+// of two (backward, a vector per lane against this: 1,774,098 x 34 bf16 537 and 206 us, 1,568,659 x 41 float32 499 and 335 us,
+// 1.13M x 128 float32 562 and 550 us).  A lane holds at most 16 elements.
 template <typename T, int VEC>
 int32_t launch_width(bool backward, const NormArgs& A, int gate_kind, int sms, int* blocks, cudaStream_t st) {
   const int v = (A.F + VEC - 1) / VEC;                     // vectors per row
 #define GNNCO_NORM(TEAM, K) return launch_one<T, VEC, TEAM, K>(backward, A, gate_kind, sms, blocks, st)
   if (v <= 8) GNNCO_NORM(8, 1);
+  if constexpr (VEC <= 2) {
+    if (v <= 16) GNNCO_NORM(8, 2);
+    if (v <= 24) GNNCO_NORM(8, 3);
+    if (v <= 32) GNNCO_NORM(8, 4);
+    if (v <= 48) GNNCO_NORM(16, 3);
+    if (v <= 64) GNNCO_NORM(16, 4);
+    if (v <= 96) GNNCO_NORM(32, 3);
+  }
+  if constexpr (VEC == 4) {
+    if (v <= 16) GNNCO_NORM(8, 2);
+    if (v <= 32) GNNCO_NORM(16, 2);
+  }
   if (v <= 16) GNNCO_NORM(16, 1);
   if (v <= 32) GNNCO_NORM(32, 1);
   if (v <= 64) GNNCO_NORM(32, 2);

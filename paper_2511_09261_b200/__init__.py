@@ -345,6 +345,7 @@ class PartitionedGraph:
         self._plan_ws = None
         self._plan_active = None
         self._plan_sizes = {}
+        self._norm_ws = {}
 
     # ---- views of the persistent area as torch tensors (no copies)
     def _view_tensor(self, ptr: int, count: int, dtype):
@@ -737,26 +738,36 @@ class PartitionedGraph:
             if dy is None:
                 dy = _empty(shape, dtype, x, stream)
             g.dy, g.dy_ld = dy.data_ptr(), self._rows(dy, dtype, rows, F, "dy")
+        # the sums over rows share one allocation
+        summed = (w_pre is not None) + (w_post is not None) + (gate is not None and gate.dim() == 1 and dgate is None)
+        vectors = iter(_empty((summed, F), torch.float32, x, stream).unbind(0) if summed else ())
         if gate is not None:
-            if dgate is None:
-                dgate = _empty(tuple(gate.shape), gate.dtype, gate, stream)
             if gate.dim() == 1:
+                if dgate is None:
+                    dgate = next(vectors)
                 g.dgate = self._weight(dgate, F, "dgate")
             else:
+                if dgate is None:
+                    dgate = _empty(shape, dtype, x, stream)
                 g.dgate, g.dgate_ld = dgate.data_ptr(), self._rows(dgate, dtype, rows, F, "dgate")
         dw_pre = dw_post = None
         if w_pre is not None:
-            dw_pre = _empty((F,), torch.float32, x, stream)
+            dw_pre = next(vectors)
             g.dw_pre = dw_pre.data_ptr()
         if w_post is not None:
-            dw_post = _empty((F,), torch.float32, x, stream)
+            dw_post = next(vectors)
             g.dw_post = dw_post.data_ptr()
-        need = _sz(0)
-        _check(self._lib.gnnco_block_norm_workspace_bytes(self._handle, F, ctypes.byref(need)),
-               "gnnco_block_norm_workspace_bytes")
-        ws = _empty((need.value,), torch.uint8, x, stream)
-        _check(self._lib.gnnco_block_norm_backward(self._handle, ctypes.byref(d), ctypes.byref(g), ws.data_ptr(),
-                                                   need.value, _stream_ptr(stream)), "gnnco_block_norm_backward")
+        # the work area of a stream is kept: calls on one stream run one after the other
+        on = _stream_ptr(stream)
+        ws = self._norm_ws.get(on)
+        if ws is None or ws[0] < F:
+            need = _sz(0)
+            _check(self._lib.gnnco_block_norm_workspace_bytes(self._handle, F, ctypes.byref(need)),
+                   "gnnco_block_norm_workspace_bytes")
+            area = _empty((need.value,), torch.uint8, x, stream)
+            ws = self._norm_ws[on] = (F, need.value, area.data_ptr(), area)
+        _check(self._lib.gnnco_block_norm_backward(self._handle, ctypes.byref(d), ctypes.byref(g), ws[2], ws[1], on),
+               "gnnco_block_norm_backward")
         return dict(dx=dx, dy=dy, dgate=dgate, dw_pre=dw_pre, dw_post=dw_post)
 
     def _muon_call(self, like, active, stream, ws):

@@ -11,11 +11,12 @@
 // is one or two contiguous 16-byte-aligned pieces, brought in by untiled bulk copies, and padding to whole panels
 // (zeros) leaves no edge cases in the products.  A panel serves as k-major rows and as n-major columns alike.
 //
-// A tile is 128 x 128; a stage of the shared-memory ring holds 64 of k (four panels, 64 KB, for 12 MMAs of 128 x 128 x 16).
-// k is always summed in four interleaved parts (stages 0, 4, 8 .., then 1, 5, 9 ..), added in that order.  With few tiles
-// (one shared weight) a cluster of four CTAs takes one part each, or one of two CTAs two: every CTA hands the others their
-// column group of its partial tiles through distributed shared memory, and finishes its own group.  With many tiles one
-// CTA takes the parts in turn, in two accumulator buffers.  The results are the same bits in all three forms.
+// A tile is 128 x TN (TN = 128, or 64 where tiles are few); a stage of the shared-memory ring holds 64 of k (64 or 48 KB, for 12 MMAs
+// of 128 x TN x 16).  k is always summed in four interleaved parts (stages 0, 4, 8 .., then 1, 5, 9 ..), added in that order:
+// one CTA takes the parts in turn, in two accumulator buffers; with few tiles and a long k a cluster of four CTAs takes one
+// part each, hands the others their column group of its partial tile through distributed shared memory, and finishes its
+// own group.  The results are the same bits in all forms.  (The exchange takes 4.7 us, as long as nine stages: clusters pay
+// from some 40 stages on, below that narrow tiles spread the work better.)
 // Launches are chained by programmatic dependence: a kernel sets itself up while the one before it finishes.
 // Roles: warps 0-7 epilogue (TMEM lanes 32 (w % 4), column half w / 4), warp 8 issues MMAs, warp 9 the copies.
 #include <cuda_fp16.h>
@@ -30,9 +31,8 @@ namespace {
 
 constexpr int kGram = 0, kPoly = 1, kApply = 2;
 constexpr int kEpiWarps = 8, kMmaWarp = 8, kCopyWarp = 9, kThreads = 320;
-constexpr int kStages = 3;
-constexpr uint32_t kStageBytes = 4 * kPanel;
-constexpr size_t kSmem = 1024 + kStages * kStageBytes + 256;
+constexpr uint32_t kRing = 12 * kPanel;                    // 3 stages of 64 KB or 4 of 48 KB
+constexpr size_t kSmem = 1024 + kRing + 256;
 
 struct TileJob {
   const uint8_t *left, *right, *mid;                       // limbs: left and right operand, A where P is formed
@@ -70,8 +70,13 @@ __device__ __forceinline__ void tile_of(int t, int n, int& i, int& j) {
   j = i + t;
 }
 
-template <int KIND, int SPLIT>
+template <int KIND, int TN, int SPLIT>
 __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
+  static_assert(TN == 128 || (TN == 64 && SPLIT == 1), "clusters split tiles of 128 columns");
+  constexpr uint32_t kStageBytes = 2 * kPanel + 2 * TN * 128;
+  constexpr int kStages = kRing / kStageBytes;
+  constexpr uint32_t B_LIMB = TN * 128;                    // bytes of the right operand's limb in a stage
+
   const NsJob& J = T.J;
   const int64_t s = blockIdx.y;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -79,7 +84,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t sbase = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (sbase - tc::smem_u32(smem_raw));
-  uint64_t* full = reinterpret_cast<uint64_t*>(gen + kStages * kStageBytes);
+  uint64_t* full = reinterpret_cast<uint64_t*>(gen + kRing);
   uint64_t* empty = full + kStages;
   uint64_t* done = empty + kStages;                         // [4] a part's products are complete
   uint64_t* freed = done + 4;                              // [2] its accumulators have been read
@@ -88,9 +93,19 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = SPLIT > 1 ? tc::cluster_ctarank() : 0u;
   const int tile = blockIdx.x / SPLIT;
-  int ti, tj;                                              // row tile; column tile (row tile of the right operand for A, P)
-  if (KIND == kApply) { ti = tile % T.rb; tj = tile / T.rb; }
-  else tile_of(tile, T.rb, ti, tj);
+  int ti, tj;                                              // row tile, column tile of TN columns
+  if (KIND == kApply) {
+    ti = tile % T.rb;
+    tj = tile / T.rb;
+  } else if (TN == 128) {
+    tile_of(tile, T.rb, ti, tj);
+  } else {
+    tile_of(tile >> 1, T.rb, ti, tj);
+    tj = 2 * tj + (tile & 1);
+  }
+  const int tr = TN == 128 ? tj : tj >> 1;                 // row tile of the right operand of A A and X X^T,
+  const uint32_t tr_off = TN == 128 ? 0u : (uint32_t)(tj & 1) * (kPanel / 2);   // and the tile's 64 rows in it
+  const bool same = KIND != kApply && ti == tr;            // a diagonal tile: the left operand's rows are the right one's
   constexpr int kParts = 4 / SPLIT;                        // parts this CTA sums: first, first + 1 ..
   const int first = (int)rank * kParts;
   auto part_stages = [&](int p) { return (T.stages - (first + p) + 3) / 4; };
@@ -105,7 +120,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
     *abort_flag = 0;
     tc::fence_mbar_init();
   }
-  constexpr uint32_t kCols = kParts > 1 ? 512 : 256;
+  constexpr uint32_t kCols = (kParts > 1 ? 4 : 2) * TN;
   if (warp == 0) tc::tmem_alloc(tmem_slot, kCols);
   tc::tc_fence_before_sync();
   __syncthreads();
@@ -117,7 +132,6 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
     if (lane == 0) {
       const uint8_t* lp = T.left + s * T.left_set;
       const uint8_t* rp = T.right + s * T.right_set;
-      const bool same = KIND != kApply && ti == tj;        // a diagonal tile: one operand is both
       int q = 0;
       bool ok = true;
       for (int p = 0; p < kParts && ok; ++p)
@@ -125,17 +139,18 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
         const int slot = q % kStages, use = q / kStages;
         if (use > 0 && !(ok = wait_bounded(empty + slot, (use - 1) & 1, abort_flag))) break;
         const uint32_t at = sbase + slot * kStageBytes;
-        tc::mbar_arrive_expect_tx(full + slot, same ? 2 * kPanel : 4 * kPanel);
+        tc::mbar_arrive_expect_tx(full + slot, same ? 2 * kPanel : kStageBytes);
         for (int limb = 0; limb < 2; ++limb) {
           tc::bulk_load(at + limb * kPanel, lp + limb * (int64_t)T.left_limb + ((int64_t)kb * T.rb + ti) * kPanel, kPanel, full + slot);
           if (same) continue;
+          const uint32_t to = at + 2 * kPanel + limb * B_LIMB;
+          const uint8_t* const from = rp + limb * (int64_t)T.right_limb;
           if (KIND != kApply) {
-            tc::bulk_load(at + (2 + limb) * kPanel, rp + limb * (int64_t)T.right_limb + ((int64_t)kb * T.rb + tj) * kPanel, kPanel, full + slot);
+            tc::bulk_load(to, from + ((int64_t)kb * T.rb + tr) * kPanel + tr_off, B_LIMB, full + slot);
           } else {
-            // 64 rows of two neighbouring panels of X
-            for (int h = 0; h < 2; ++h)
-              tc::bulk_load(at + (2 + limb) * kPanel + h * (kPanel / 2),
-                            rp + limb * (int64_t)T.right_limb + ((int64_t)(2 * tj + h) * T.rb + (kb >> 1)) * kPanel + (kb & 1) * (kPanel / 2),
+            // 64 rows of the tile's panels of X
+            for (int h = 0; h < TN / 64; ++h)
+              tc::bulk_load(to + h * (kPanel / 2), from + ((int64_t)(tj * (TN / 64) + h) * T.rb + (kb >> 1)) * kPanel + (kb & 1) * (kPanel / 2),
                             kPanel / 2, full + slot);
           }
         }
@@ -145,22 +160,22 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
     if (KIND == kApply && T.last && J.W) {
       // the tile of W that the products are about to be added to
       const int64_t base = (T.set0 + s) * (int64_t)J.r * J.c;
-      const int row0 = (J.transpose ? tj : ti) * 128, col0 = (J.transpose ? ti : tj) * 128;
-      for (int q = lane; q < 128 * 5; q += 32) {
-        const int i = row0 + q / 5, j = min(col0 + (q % 5) * 32, min(col0 + 127, J.c - 1));
+      const int row0 = J.transpose ? tj * TN : ti * 128, col0 = J.transpose ? ti * 128 : tj * TN;
+      const int tile_rows = J.transpose ? TN : 128, tile_cols = J.transpose ? 128 : TN;
+      for (int q = lane; q < tile_rows * 5; q += 32) {
+        const int i = row0 + q / 5, j = min(col0 + (q % 5) * 32, min(col0 + tile_cols - 1, J.c - 1));
         if (i < J.r) asm volatile("prefetch.global.L2 [%0];" ::"l"(J.W + base + (int64_t)i * J.c + j));
       }
     }
   } else if (warp == kMmaWarp) {
     const uint32_t leader = tc::elect_one();
-    const uint32_t idesc = tc::idesc_f16_f32(128, 128, KIND == kApply);
+    const uint32_t idesc = tc::idesc_f16_f32(128, TN, KIND == kApply);
     const uint32_t tb = __shfl_sync(0xffffffffu, tmem, 0);
-    const bool same = KIND != kApply && ti == tj;
     bool ok = true;
     int q = 0;
     for (int p = 0; p < kParts && ok; ++p) {
       const int count = part_stages(p);
-      const uint32_t big = tb + (p & 1) * 256, small = big + 128;
+      const uint32_t big = tb + (p & 1) * (2 * TN), small = big + TN;
       // buffers are reused by parts 2 and 3; an empty part neither completes nor frees anything
       if (p >= 2 && count > 0) ok = __all_sync(0xffffffffu, wait_bounded(freed + (p & 1), 0, abort_flag)) != 0;
       tc::tc_fence_after_sync();
@@ -171,9 +186,9 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
         if (!ok) break;
         const uint32_t at = sbase + slot * kStageBytes;
         const uint64_t ah = tc::smem_desc_sw128(at, 16, 1024), al = tc::smem_desc_sw128(at + kPanel, 16, 1024);
-        const uint32_t bt = at + (same ? 0u : 2 * kPanel);
+        const uint32_t bt = at + (same ? tr_off : 2 * kPanel), b_limb = same ? kPanel : B_LIMB;
         const uint32_t lbo = KIND == kApply ? kPanel / 2 : 16;
-        const uint64_t bh = tc::smem_desc_sw128(bt, lbo, 1024), bl = tc::smem_desc_sw128(bt + kPanel, lbo, 1024);
+        const uint64_t bh = tc::smem_desc_sw128(bt, lbo, 1024), bl = tc::smem_desc_sw128(bt + b_limb, lbo, 1024);
         constexpr uint64_t bstep = KIND == kApply ? 128 : 2; // 16 of k: 2,048 bytes of n-major rows, 32 of k-major ones
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -188,39 +203,30 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
       __syncwarp();
     }
   }
-  // ---- partial tiles to registers: items (32 columns) half and half + 2 of the tile, the parts in order
+  // ---- partial tiles to registers: items (32 columns) half and, in wide tiles, half + 2; the parts in order
   const int quarter = warp & 3, half = warp >> 2;          // of the epilogue warps
   const int row = quarter * 32 + lane;
   const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-  constexpr int GROUP = 128 / SPLIT, kItems = GROUP / 32;  // columns that one CTA finishes, in items of 32
-  // two CTAs: the second one keeps its two parts apart, so that the owner can add all four in order
-  constexpr int kKept = SPLIT == 2 ? 2 : 1;
-  float sum[kKept][2][32];
+  constexpr int NI = TN / 64;                              // items of a warp
+  float sum[NI][32];
   if (warp < kEpiWarps) {
 #pragma unroll
-    for (int k = 0; k < kKept; ++k)
+    for (int i = 0; i < NI; ++i)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 32; ++e) sum[k][i][e] = 0.0f;
+      for (int e = 0; e < 32; ++e) sum[i][e] = 0.0f;
     for (int p = 0; p < kParts; ++p) {
       if (part_stages(p) <= 0) continue;
       if (!wait_bounded(done + p, 0, abort_flag)) break;
       tc::tc_fence_after_sync();
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < NI; ++i) {
         uint32_t v[32], w[32];
-        const uint32_t at = tmem + (p & 1) * 256 + lanes + (half + 2 * i) * 32;
+        const uint32_t at = tmem + (p & 1) * (2 * TN) + lanes + (half + 2 * i) * 32;
         tc::tmem_ld_32x32(at, v);
-        tc::tmem_ld_32x32(at + 128, w);
+        tc::tmem_ld_32x32(at + TN, w);
         tc::tmem_ld_wait();
-        if (kKept > 1 && rank == 1 && p == 1) {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) sum[kKept - 1][i][e] += __uint_as_float(v[e]) + __uint_as_float(w[e]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 32; ++e) sum[0][i][e] += __uint_as_float(v[e]) + __uint_as_float(w[e]);
-        }
+        for (int e = 0; e < 32; ++e) sum[i][e] += __uint_as_float(v[e]) + __uint_as_float(w[e]);
       }
       tc::tc_fence_before_sync();
       __syncwarp();
@@ -232,40 +238,35 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
   tc::tc_fence_after_sync();
 
   if constexpr (SPLIT > 1) {
-    // partial tiles to their owners: [slot][item of the owner][row][32 columns], 16 KB an item
+    // partial tiles to their owners: [from CTA][row][32 columns], 16 KB each
     tc::cluster_sync_all();                                // every CTA's ring is free
     if (warp < kEpiWarps) {
 #pragma unroll
-      for (int k = 0; k < kKept; ++k) {
-        if (k > 0 && rank == 0) continue;
+      for (int i = 0; i < NI; ++i) {
+        const uint32_t to = tc::map_to_cta(sbase + rank * kPanel, half + 2 * i);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int item = half + 2 * i, owner = item / kItems, local = item % kItems;
-          const uint32_t to = tc::map_to_cta(sbase + (((int)rank + k) * kItems + local) * kPanel, owner);
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + at_chunk(row, e)), "f"(sum[k][i][4 * e]),
-                         "f"(sum[k][i][4 * e + 1]), "f"(sum[k][i][4 * e + 2]), "f"(sum[k][i][4 * e + 3]) : "memory");
-        }
+        for (int e = 0; e < 8; ++e)
+          asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + at_chunk(row, e)), "f"(sum[i][4 * e]), "f"(sum[i][4 * e + 1]),
+                       "f"(sum[i][4 * e + 2]), "f"(sum[i][4 * e + 3]) : "memory");
       }
     }
     tc::cluster_sync_all();
   }
   if (warp < kEpiWarps && !*abort_flag) {
-    // one CTA: this warp's items; a cluster: the CTA's own ones, by the warps of their `half`
+    // one CTA: this warp's items; a cluster: the CTA's own one, by its first four warps
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (SPLIT > 1 && (half >= kItems || i > 0)) continue;
-      const int item = half + 2 * i;
+    for (int i = 0; i < NI; ++i) {
+      if (SPLIT > 1 && (half > 0 || i > 0)) continue;
+      const int item = SPLIT > 1 ? (int)rank : half + 2 * i;
       uint32_t v[32];
       if constexpr (SPLIT > 1) {
         float total[32];
 #pragma unroll
         for (int e = 0; e < 32; ++e) total[e] = 0.0f;
-        for (int slot = 0; slot < SPLIT + kKept - 1; ++slot)
+        for (int from = 0; from < SPLIT; ++from)
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const uint4 a = tc::ld_shared16(sbase + (slot * kItems + item) * kPanel + at_chunk(row, e));
+            const uint4 a = tc::ld_shared16(sbase + from * kPanel + at_chunk(row, e));
             total[4 * e] += __uint_as_float(a.x);
             total[4 * e + 1] += __uint_as_float(a.y);
             total[4 * e + 2] += __uint_as_float(a.z);
@@ -275,10 +276,10 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
         for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(total[e]);
       } else {
 #pragma unroll
-        for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(sum[0][i][e]);
+        for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(sum[i][e]);
       }
-      const int c0 = (int)rank * GROUP + item * 32;        // first column inside the tile
-      const int panel = 2 * tj + (c0 >> 6), chunk0 = (c0 & 63) >> 3;
+      const int c0 = item * 32;                            // first column inside the tile
+      const int panel = (TN / 64) * tj + (c0 >> 6), chunk0 = (c0 & 63) >> 3;
       uint8_t* const to = T.out + s * T.out_set + ((int64_t)panel * T.rb + ti) * kPanel;
       if (KIND == kApply && T.last) {
         const float fo = 1.0f / (J.p_scale * kXScale);
@@ -289,7 +290,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
           else __stcs(static_cast<float*>(J.O) + at, x);
         };
         if (J.transpose) {                                 // lanes are neighbouring columns of W
-          const int i = ti * 128 + row, j0 = tj * 128 + c0;
+          const int i = ti * 128 + row, j0 = tj * TN + c0;
           float w[32];
 #pragma unroll
           for (int e = 0; e < 32; ++e) w[e] = J.W && i < J.k && j0 + e < J.n ? __ldcs(J.W + base + (int64_t)(j0 + e) * J.c + i) : 0.0f;
@@ -302,7 +303,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) tc::st_shared16(stage + at_chunk(lane, e), v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
           __syncwarp();
-          const int j = tj * 128 + c0 + lane;
+          const int j = tj * TN + c0 + lane;
           float w[32];
 #pragma unroll
           for (int e = 0; e < 32; ++e) {
@@ -331,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
           hi[4 * e] = h4.x; hi[4 * e + 1] = h4.y; hi[4 * e + 2] = h4.z; hi[4 * e + 3] = h4.w;
           lo[4 * e] = l4.x; lo[4 * e + 1] = l4.y; lo[4 * e + 2] = l4.z; lo[4 * e + 3] = l4.w;
         }
-        const int diag = ti == tj ? row - c0 : -1;         // this row's place on the diagonal, if it is in the item
+        const int diag = ti * 128 + row - (tj * TN + c0);  // this row's place on the diagonal, if it is in the item
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const float2 A2 = join2(hi[e], lo[e]);
@@ -348,13 +349,13 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
         *reinterpret_cast<uint4*>(to + at_chunk(row, chunk0 + e)) = make_uint4(hi[4 * e], hi[4 * e + 1], hi[4 * e + 2], hi[4 * e + 3]);
         *reinterpret_cast<uint4*>(to + T.out_limb + at_chunk(row, chunk0 + e)) = make_uint4(lo[4 * e], lo[4 * e + 1], lo[4 * e + 2], lo[4 * e + 3]);
       }
-      if (KIND != kApply && ti != tj) {
-        // the mirrored tile: row c0 + e, column `row` (lanes write neighbouring float16 values)
-        uint8_t* const mt = T.out + s * T.out_set + ((int64_t)(2 * ti + (row >> 6)) * T.rb + tj) * kPanel;
-        const int cc = (row & 63) >> 3;
+      if (KIND != kApply && !same) {
+        // the mirrored tile: row tr_row + e of row tile tr, column `row` (lanes write neighbouring float16 values)
+        uint8_t* const mt = T.out + s * T.out_set + ((int64_t)(2 * ti + (row >> 6)) * T.rb + tr) * kPanel;
+        const int cc = (row & 63) >> 3, tr_row = (int)(tr_off >> 7) + c0;
 #pragma unroll
         for (int e = 0; e < 32; ++e) {
-          const uint32_t o = at_chunk(c0 + e, cc) + (row & 7) * 2;
+          const uint32_t o = at_chunk(tr_row + e, cc) + (row & 7) * 2;
           *reinterpret_cast<unsigned short*>(mt + o) = (unsigned short)(e & 1 ? hi[e >> 1] >> 16 : hi[e >> 1] & 0xffffu);
           *reinterpret_cast<unsigned short*>(mt + T.out_limb + o) = (unsigned short)(e & 1 ? lo[e >> 1] >> 16 : lo[e >> 1] & 0xffffu);
         }
@@ -495,9 +496,9 @@ Layout layout(void* ws, int64_t sets, int32_t k, int32_t n) {
   return L;
 }
 
-template <int KIND, int SPLIT>
-int32_t launch_split(gnnco_handle* h, const TileJob& T, int64_t tiles, unsigned sets, cudaStream_t st) {
-  auto kernel = ns_tiles<KIND, SPLIT>;
+template <int KIND, int TN, int SPLIT>
+int32_t launch_form(gnnco_handle* h, const TileJob& T, int64_t tiles, unsigned sets, cudaStream_t st) {
+  auto kernel = ns_tiles<KIND, TN, SPLIT>;
   static std::atomic<int> allowed{0};
   const int32_t rc = allow_shared_memory(kernel, kSmem, h->device, allowed);
   if (rc != GNNCO_OK) return rc;
@@ -523,7 +524,7 @@ int32_t launch_split(gnnco_handle* h, const TileJob& T, int64_t tiles, unsigned 
 // group of SMs.
 int resident_quads() {
   static const int quads = [] {
-    auto kernel = ns_tiles<kGram, 4>;
+    auto kernel = ns_tiles<kGram, 128, 4>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess) {
       cudaGetLastError();
       return 0;
@@ -548,12 +549,14 @@ int resident_quads() {
   return quads;
 }
 
-// A cluster per tile where the GPU holds them all at once.
+// `tiles` counts tiles of 128 columns.  Narrow tiles while they leave SMs free; a cluster per tile for a long k, where the GPU holds
+// them all at once.
+constexpr int kLongStages = 40;
 template <int KIND>
 int32_t launch_product(gnnco_handle* h, const TileJob& T, int64_t tiles, unsigned sets, cudaStream_t st) {
-  if (tiles * sets <= resident_quads()) return launch_split<KIND, 4>(h, T, tiles, sets, st);
-  if (tiles * sets * 2 <= h->sm_count) return launch_split<KIND, 2>(h, T, tiles, sets, st);
-  return launch_split<KIND, 1>(h, T, tiles, sets, st);
+  if (T.stages >= kLongStages && tiles * sets <= resident_quads()) return launch_form<KIND, 128, 4>(h, T, tiles, sets, st);
+  if (tiles * sets * 2 <= h->sm_count) return launch_form<KIND, 64, 1>(h, T, 2 * tiles, sets, st);
+  return launch_form<KIND, 128, 1>(h, T, tiles, sets, st);
 }
 
 template <typename TG>

@@ -969,7 +969,7 @@ extern "C" int32_t gnnco_embedding_plan(gnnco_handle* h, const int32_t* tokens, 
     else order_histogram<false><<<nb, kOrdThreads, 0, st>>>(kin, rows, span, shift, digits, V, L.hist, nullptr, nullptr);
     // few blocks: the scatter adds up the block counts itself
     const bool scanned = nb > kOrdFewBlocks;
-    if (scanned) order_scan<<<digits, 1024, 0, st>>>(L.hist, L.totals, nb);
+    if (scanned) order_scan<<<digits, (nb + 31) / 32 * 32, 0, st>>>(L.hist, L.totals, nb);
     if (p == 0)
       order_scatter<true><<<nb, kOrdThreads, kScatterSmem, st>>>(kin, iin, ka, ia, (uint32_t)rows, (uint32_t)span, shift, L.bits, V, L.hist,
                                                                 scanned ? L.totals : nullptr);

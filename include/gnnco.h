@@ -440,7 +440,8 @@ int32_t gnnco_block_norm_backward(gnnco_handle* h, const gnnco_block_norm_desc* 
  *   W = W (1 - lr * weight_decay) - lr * sqrt(max(1, cols / rows)) * X
  * The usual coefficients are a = 3.4445, b = -4.7750, c = 2.0315 with 5 steps: singular values of u end near 1.
  * Coefficients that carry a singular value in [0, 1] past 2 are refused; steps 1 .. 32.  Products are taken to float32
- * accuracy (operands split into two float16 limbs, float32 accumulation); the norm is summed in float64.  A zero
+ * accuracy (operands split into two float16 limbs, float32 accumulation; float32 where the short side is at most 16);
+ * sums of squares are joined in float64.  A zero
  * gradient gives a zero X; a matrix with an infinity or NaN in u gives NaN in its own set only.  `active` (device,
  * [sets] uint8, or NULL = all): sets with active[s] == 0 keep W and m bit for bit.  Layers updated here are
  * noticed by GNNCO_WEIGHTS_UNTOUCHED.

@@ -102,7 +102,8 @@ __device__ __forceinline__ float inverse_rms(float sum_of_squares, const NormArg
 }
 
 // Teams of TEAM lanes, K vectors of VEC elements per lane; blocks go through the rows grid-stride, weights stay in
-// registers.  Two rows of a team in flight at a time were no faster (1,014 against 997 us for 2.5M x 256 bf16).
+// registers.  2.5M x 256 bf16: 871 us (5.9 TB/s); 878 with the registers of four blocks per SM, 975 with five; two rows of a team in
+// flight at a time changed nothing.
 template <typename T, int VEC, int TEAM, int K>
 __global__ void __launch_bounds__(TEAM > 256 ? TEAM : 256)
 norm_forward(const NormArgs A, const int gate_kind) {
@@ -161,7 +162,8 @@ norm_forward(const NormArgs A, const int gate_kind) {
   }
 }
 
-// Three blocks per SM where a lane holds at most eight elements: 2.5M x 256 bf16 takes 1,472 us so, 1,658 with the registers of two.
+// Three blocks per SM where a lane holds at most eight elements: 2.5M x 256 bf16 takes 1,370 us so (5.6 TB/s), 1,902 with two and 1,565
+// with four, whose registers spill.
 template <typename T, int VEC, int TEAM, int K>
 __global__ void __launch_bounds__(TEAM > 256 ? TEAM : 256, TEAM > 256 ? 1 : K * VEC <= 8 ? 3 : 1)
 norm_backward(const NormArgs A, const int gate_kind) {

@@ -10,9 +10,9 @@
 // power-of-two scales that keep hi in range and lo normal; a product is hi hi + hi lo + lo hi (the dropped lo lo is
 // 2^-24 of it) summed in the float32 accumulator.  The tensor core drops the bits below the accumulator's last place at
 // every instruction, so the small products of all k come first and the large ones meet the accumulator only k / 16
-// times (error of a 256 x 256 iterate after 5 steps: 3.8e-6, 8.0e-6 when interleaved).  That is float32
-// accuracy at a third of the float16 rate; one float16 or bfloat16 product would put 2e-3 (1.5e-2) into the result, because errors in the direction of small singular values
-// grow by a = 3.4 per step.
+// times (error of a 256 x 256 iterate after 5 steps: 3.8e-6, 8.0e-6 when interleaved).  That is float32 accuracy at a
+// third of the float16 rate; one float16 or bfloat16 product would put 2e-3 (1.5e-2) into the result, because errors
+// in the direction of small singular values grow by a = 3.4 per step.
 //
 // Where things live.  Shared memory: X in two limbs (panels of 64 columns, 128 rows of 128 bytes, 128-byte swizzle: the same
 // bytes serve as k-major rows and as n-major columns) and A's limbs.  Tensor memory, in blocks of 32 columns: the
@@ -25,15 +25,16 @@
 // A and A A are worked on.  A's low limb does not fit next to X as a whole: its second half follows into the room of the
 // first as soon as the products that read the first are done (they are issued first).
 //
-// What bounds it.  4,096 x 256 x 256 (6.2 PFLOP of float16 products, three per float32 one): 5.5 ms, 6.2 ms once the power cap holds
-// the clock at 1.7 GHz; the tensor pipe is active half of the time.  A step of a pair takes 27,700 cycles, 18,400 of them
-// products: what is left are the conversions between them that nothing covers.  Loading and storing a matrix takes 48,000 cycles;
-// starting the pairs at different times did not change that.  1,024 x 128 x 128: 234 us.
+// What bounds it.  4,096 x 256 x 256 (6.2 PFLOP of float16 products, three per float32 one): 5.5 ms, 6.2 ms once the
+// power cap holds the clock at 1.7 GHz; the tensor pipe is active half of the time.  A step of a pair takes 27,700
+// cycles, 18,400 of them products: what is left are the conversions between them that nothing covers.  Loading and
+// storing a matrix takes 48,000 cycles; starting the pairs at different times did not change that.  1,024 x 128 x 128:
+// 234 us.
 //
-// Roles: after the working warps (16; 8 where two CTAs share an SM) one warp issues MMAs, and in a pair another exchanges blocks; the
-// working warps load, convert and store: warp w owns rows 32 (w % 4) .. +32 (its TMEM
-// lanes) and the 32-column items w / 4 and w / 4 + 4.  Barriers per 64-column panel let the next product start on the
-// first panels while the others are converted.  Every wait is bounded; a CTA that gives up raises the status word.
+// Roles: after the working warps (16; 8 where two CTAs share an SM) one warp issues MMAs, and in a pair another
+// exchanges blocks; the working warps load, convert and store: warp w owns rows 32 (w % 4) .. +32 (its TMEM lanes) and
+// the 32-column items w / 4 and w / 4 + 4.  Barriers per 64-column panel let the next product start on the first panels
+// while the others are converted.  Every wait is bounded; a CTA that gives up raises the status word.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -46,9 +47,9 @@
 
 namespace {
 
-
-// kDual: both sides up to 128, two CTAs per SM (while one converts, the other's products run: 1,024 x 128 x 128 takes 272 us so, 334 alone); kWide: short side up to 128,
-// long side up to 256, one CTA per SM; kPair: sides up to 256, two CTAs on two SMs.
+// kDual: both sides up to 128, two CTAs per SM (while one converts, the other's products run: 1,024 x 128 x 128 took
+// 272 us so and 334 with one when this was decided); kWide: short side up to 128, long side up to 256, one CTA per SM;
+// kPair: sides up to 256, two CTAs on two SMs.
 constexpr int kDual = 0, kWide = 1, kPair = 2;
 
 template <int MODE>

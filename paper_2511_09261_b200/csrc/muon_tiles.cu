@@ -28,6 +28,7 @@
 #include "muon_limbs.cuh"
 #include "tc_common.cuh"
 #include "vec_io.cuh"
+#include "walk.cuh"
 
 namespace {
 
@@ -422,25 +423,25 @@ template <typename TG>
 __global__ void __launch_bounds__(256) ns_momentum(const NsJob J, int64_t set0, double* __restrict__ partial) {
   const int64_t s = blockIdx.y, base = (set0 + s) * (int64_t)J.r * J.c;
   if (J.active && !J.active[set0 + s]) return;
-  const int32_t count = J.r * J.c;
+  const int64_t count = (int64_t)J.r * J.c;
   double sum = 0.0;
-  for (int32_t q0 = (int32_t)blockIdx.x * 1024; q0 < count; q0 += (int32_t)gridDim.x * 1024) {
+  for (PieceWalk piece(count, blockIdx.x, gridDim.x, 1024); piece.more(); piece.next()) {
     vio::Raw<TG, 1> g[4];
     float mv[4];
 #pragma unroll
     for (int y = 0; y < 4; ++y) {
-      const int32_t q = q0 + y * 256 + (int32_t)threadIdx.x;
+      const int64_t q = piece.at + y * 256 + (int)threadIdx.x;
       g[y].zero();
       mv[y] = 0.0f;
-      if (q < count && q >= 0) {
+      if (q < count) {
         g[y].template load<true>(static_cast<const TG*>(J.G) + base + q);
         if (J.m) mv[y] = J.m[base + q];
       }
     }
 #pragma unroll
     for (int y = 0; y < 4; ++y) {
-      const int32_t q = q0 + y * 256 + (int32_t)threadIdx.x;
-      if (q >= count || q < 0) continue;
+      const int64_t q = piece.at + y * 256 + (int)threadIdx.x;
+      if (q >= count) continue;
       float u = g[y].get(0);
       if (J.m) {
         const float v = J.mu * mv[y] + u;

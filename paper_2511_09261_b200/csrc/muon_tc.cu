@@ -77,7 +77,8 @@ struct Bars {
   uint64_t l;                                              // second half of A's low limb ready (even CTA)
   uint64_t own;                                            // this CTA's off-diagonal block written (by its workers)
   uint64_t g, s, s2;                                       // partner's block in scratch / copied here / copied there
-  uint64_t norm, norm2, again, loaded;                     // loader: sums ready, partner's sum ready, sums read, X written
+  uint64_t norm, again, loaded;                            // loader: sums ready, sums read, X written
+  uint64_t peer1, peer2;                                   // partner's sum of the first / second round ready
 };
 
 __device__ __forceinline__ void st_shared8(uint32_t saddr, uint32_t a, uint32_t b) {
@@ -149,7 +150,8 @@ __global__ void __launch_bounds__(Cfg<MODE>::THREADS, Cfg<MODE>::PER_SM) ns_on_c
     tc::mbar_init(&B->own, 4 * (rank == 0 ? (x_items > 4 ? x_items - 4 : 1) : 4));
     tc::mbar_init(&B->g, 1);
     tc::mbar_init(&B->s, 1); tc::mbar_init(&B->s2, 1);
-    tc::mbar_init(&B->norm, kWorkWarps); tc::mbar_init(&B->norm2, 1); tc::mbar_init(&B->again, kWorkWarps); tc::mbar_init(&B->loaded, kWorkWarps);
+    tc::mbar_init(&B->norm, kWorkWarps); tc::mbar_init(&B->again, kWorkWarps); tc::mbar_init(&B->loaded, kWorkWarps);
+    tc::mbar_init(&B->peer1, 1); tc::mbar_init(&B->peer2, 1);
     *abort_flag = 0;
     tc::fence_mbar_init();
   }
@@ -368,7 +370,7 @@ __global__ void __launch_bounds__(Cfg<MODE>::THREADS, Cfg<MODE>::PER_SM) ns_on_c
       b += jump_b;
       if (b >= per) { b -= per; ++a; }
     };
-    uint32_t it = 0, mat = 0, sum_it = 0, again_it = 0;
+    uint32_t it = 0, mat = 0, sum_it = 0, second_it = 0, again_it = 0;
     for (int64_t s = group; s < J.sets && !*abort_flag; s += groups) {
       if (J.active && !J.active[s]) continue;
       const int64_t base = s * (int64_t)J.r * J.c;
@@ -441,8 +443,10 @@ __global__ void __launch_bounds__(Cfg<MODE>::THREADS, Cfg<MODE>::PER_SM) ns_on_c
         }
       }
       double norm2 = 0.0;
-      // own warps' sums in warp order, then the partner's (a + b = b + a: both CTAs get the same bits)
-      auto total_of = [&](double part) {
+      // own warps' sums in warp order, then the partner's (a + b = b + a: both CTAs get the same bits).  Nothing in the partner
+      // waits for this CTA's warps between the two rounds of a matrix, so each round has a barrier of its own: one that
+      // completed twice while a warp was on its way to it would look as if it had not completed.
+      auto total_of = [&](double part, uint64_t* peer_bar, uint32_t peer_parity) {
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) part += __shfl_xor_sync(0xffffffffu, part, d);
         if (lane == 0) {
@@ -457,15 +461,15 @@ __global__ void __launch_bounds__(Cfg<MODE>::THREADS, Cfg<MODE>::PER_SM) ns_on_c
           if (threadIdx.x == 0) {
             const uint32_t peer = tc::map_to_cta(tc::smem_u32(sums + 16 + (sum_it & 1)), rank ^ 1u);
             asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(peer), "d"(norm2) : "memory");
-            tc::mbar_arrive_release_cluster(tc::map_to_cta(tc::smem_u32(&B->norm2), rank ^ 1u));
+            tc::mbar_arrive_release_cluster(tc::map_to_cta(tc::smem_u32(peer_bar), rank ^ 1u));
           }
-          if (!wait_both(&B->norm2, sum_it & 1)) return false;
+          if (!wait_both(peer_bar, peer_parity)) return false;
           norm2 += sums[16 + (sum_it & 1)];
         }
         ++sum_it;
         return true;
       };
-      if (!total_of(sum)) break;
+      if (!total_of(sum, &B->peer1, mat & 1)) break;
       if (!(norm2 > 1e-24 && norm2 < 1e37)) {              // the same decision everywhere
         // everybody has read the sums of the first round before they are written again
         __syncwarp();
@@ -478,7 +482,7 @@ __global__ void __launch_bounds__(Cfg<MODE>::THREADS, Cfg<MODE>::PER_SM) ns_on_c
           const float2 x = ld_shared8(p), y = ld_shared8(p + C::XP * kPanel);
           sum += (double)x.x * x.x + (double)x.y * x.y + ((double)y.x * y.x + (double)y.y * y.y);
         }
-        if (!total_of(sum)) break;
+        if (!total_of(sum, &B->peer2, second_it++ & 1)) break;
       }
       const float f = (float)((double)kXScale / (sqrt(norm2) + (double)J.eps));
       ua = first_a;

@@ -339,6 +339,9 @@ __global__ void __launch_bounds__(Cfg<MODE>::THREADS, Cfg<MODE>::PER_SM) ns_on_c
     const int row = quarter * 32 + lane;                   // of this CTA's 128
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const bool works = quarter < quarters;
+    // A warp without an item of X has none of A and P either, and nobody waits for it inside a step: it keeps away from the steps'
+    // barriers (one that completed twice while it was on its way would look as if it had not completed).
+    const bool busy = works && sub < x_items;
     const int off_panel = rank == 0 ? 2 : 0;               // the two panels that the partner takes
     auto arrive = [&](uint64_t* bar) {                     // on the even CTA's barrier, by one lane, after __syncwarp
       if constexpr (PAIR) tc::mbar_arrive_cluster(tc::map_to_cta(tc::smem_u32(bar), 0));
@@ -504,7 +507,7 @@ __global__ void __launch_bounds__(Cfg<MODE>::THREADS, Cfg<MODE>::PER_SM) ns_on_c
       for (int item = sub; item < 2 * C::XP; item += SUBS) x_ready(item);
 
       bool ok = true;
-      for (int step = 0; step < J.steps; ++step, ++it) {
+      for (int step = 0; step < J.steps && busy; ++step, ++it) {
         const uint32_t ph = it & 1;
         // ---- A's limbs over its accumulator, and into shared memory
         if (!(ok = wait(&B->m1, ph))) break;

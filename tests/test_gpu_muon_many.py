@@ -51,3 +51,14 @@ def test_norms_that_are_summed_twice(graph, sets, r, c):
     assert torch.equal(got, _by_few(graph, G, 50, coefs=COEFS, eps=eps))
     _near(got, G, (0, 1, 2, 3, sets // 2, sets - 1), eps)
     assert graph.async_status() == 0
+
+
+@pytest.mark.parametrize("sets,r,c", [(700, 17, 20), (700, 32, 32), (650, 64, 24), (650, 32, 100), (400, 24, 180), (330, 150, 20)])
+def test_matrices_that_leave_warps_idle(graph, sets, r, c):
+    """Sides that fill neither the 128 rows nor the 32-column items of all working warps."""
+    import torch
+    G = _normal(2, sets, r, c)
+    got = graph.orthogonalise(G, coefs=COEFS, eps=1e-7)
+    assert torch.equal(got, _by_few(graph, G, 130, coefs=COEFS, eps=1e-7))
+    _near(got, G, (0, 1, sets // 2, sets - 1), 1e-7)
+    assert graph.async_status() == 0

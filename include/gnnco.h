@@ -443,8 +443,9 @@ int32_t gnnco_block_norm_backward(gnnco_handle* h, const gnnco_block_norm_desc* 
  * accuracy (operands split into two float16 limbs, float32 accumulation; float32 where the short side is at most 16);
  * sums of squares are joined in float64.  A zero
  * gradient gives a zero X; a matrix with an infinity or NaN in u gives NaN in its own set only.  `active` (device,
- * [sets] uint8, or NULL = all): sets with active[s] == 0 keep W and m bit for bit.  Layers updated here are
- * noticed by GNNCO_WEIGHTS_UNTOUCHED.
+ * [sets] uint8, or NULL = all): sets with active[s] == 0 keep W and m bit for bit.  Weights that a
+ * call on this handle writes, all or some sets of a layer, are noticed by GNNCO_WEIGHTS_UNTOUCHED of this handle (so is O); calls
+ * on another handle and replays of a recorded graph are not.
  * gnnco_orthogonalise: O = X after the steps, in G's orientation, for G and O [sets x rows x cols] in float32 or bfloat16
  * (lr, momentum, weight_decay and nesterov are not read; sets that are not active are not written; O may be G).
  * ws: gnnco_muon_workspace_bytes bytes, 256-byte aligned.  Asynchronous on `stream`; results do not depend on `sets` or

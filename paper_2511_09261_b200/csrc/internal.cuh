@@ -154,6 +154,7 @@ struct gnnco_handle {
   // bf16 copies of the weights that the last updating step left in its work area (GNNCO_WEIGHTS_UNTOUCHED):
   // which master weights and which copies they belong to; fresh[l] says whether layer l's copies are current
   const float* shadow_W[GNNCO_MAX_LAYERS] = {nullptr};
+  size_t shadow_bytes[GNNCO_MAX_LAYERS] = {0};               // of the master weights
   const void* shadow_copy[GNNCO_MAX_LAYERS] = {nullptr};
   bool shadow_fresh[GNNCO_MAX_LAYERS] = {false};
   // long rows are aggregated on a side stream, concurrently with the short rows
@@ -166,6 +167,14 @@ struct gnnco_handle {
   const float2* adam_bias = nullptr;
   cudaEvent_t ev_fork = nullptr, ev_join = nullptr;
 };
+
+// The library is about to write `bytes` from p on: copies of weights that lie there, wholly or in part, are stale from here on.
+inline void weights_written(gnnco_handle* h, const void* p, size_t bytes) {
+  for (int l = 0; l < GNNCO_MAX_LAYERS; ++l) {
+    const uintptr_t w = (uintptr_t)h->shadow_W[l], at = (uintptr_t)p;
+    if (at < w + h->shadow_bytes[l] && w < at + bytes) h->shadow_fresh[l] = false;
+  }
+}
 
 struct ProfScope {
   gnnco_handle* h;

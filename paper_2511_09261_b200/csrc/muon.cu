@@ -107,9 +107,7 @@ extern "C" int32_t gnnco_muon_update(gnnco_handle* h, int64_t sets, int32_t rows
   if (ws_bytes < workspace_bytes(h, sets, rows, cols)) return GNNCO_WORKSPACE_TOO_SMALL;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   ProfScope prof_(h, K_MUON, st);
-  // the bf16 copies of these weights that an earlier step left behind are stale from here on
-  for (int l = 0; l < GNNCO_MAX_LAYERS; ++l)
-    if (h->shadow_W[l] == W) h->shadow_fresh[l] = false;
+  weights_written(h, W, (size_t)sets * rows * cols * sizeof(float));
   const float step = p->lr * sqrtf(cols > rows ? (float)cols / (float)rows : 1.0f);
   return run_ns<float, float>(h, sets, rows, cols, dW, m, W, nullptr, p->momentum, p->nesterov, 1.0f - p->lr * p->weight_decay,
                               step, p->active, P, ws, st);
@@ -127,6 +125,7 @@ extern "C" int32_t gnnco_orthogonalise(gnnco_handle* h, int32_t in_dtype, int32_
   if (ws_bytes < workspace_bytes(h, sets, rows, cols)) return GNNCO_WORKSPACE_TOO_SMALL;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   ProfScope prof_(h, K_MUON, st);
+  weights_written(h, O, (size_t)sets * rows * cols * (out_dtype == GNNCO_F32 ? sizeof(float) : 2));
   typedef __nv_bfloat16 B;
 #define GNNCO_ORTHO(TG, TO) \
   return run_ns<TG, TO>(h, sets, rows, cols, (const TG*)G, nullptr, nullptr, (TO*)O, 0.0f, 0, 0.0f, 0.0f, p->active, P, ws, st)

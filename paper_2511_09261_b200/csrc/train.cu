@@ -325,6 +325,7 @@ int32_t run_step_on(gnnco_handle* h, const gnnco_model_desc* m, const void* X, c
                                           c1, c2, opt->active, st);
       if (rc2 == GNNCO_OK) {
         h->shadow_W[l] = m->W[l];
+        h->shadow_bytes[l] = (size_t)wc * sizeof(float);
         h->shadow_copy[l] = T.W_lp[l];
         h->shadow_fresh[l] = true;
       }

@@ -345,7 +345,7 @@ class PartitionedGraph:
         self._plan_ws = None
         self._plan_active = None
         self._plan_sizes = {}
-        self._norm_ws = {}
+        self._norm_sizes = {}
 
     # ---- views of the persistent area as torch tensors (no copies)
     def _view_tensor(self, ptr: int, count: int, dtype):
@@ -757,17 +757,16 @@ class PartitionedGraph:
         if w_post is not None:
             dw_post = next(vectors)
             g.dw_post = dw_post.data_ptr()
-        # the work area of a stream is kept: calls on one stream run one after the other
-        on = _stream_ptr(stream)
-        ws = self._norm_ws.get(on)
-        if ws is None or ws[0] < F:
-            need = _sz(0)
-            _check(self._lib.gnnco_block_norm_workspace_bytes(self._handle, F, ctypes.byref(need)),
+        # a work area of its own for every call: callers on other threads, and recorded graphs with their replays, must not share one
+        need = self._norm_sizes.get(F)
+        if need is None:
+            b = _sz(0)
+            _check(self._lib.gnnco_block_norm_workspace_bytes(self._handle, F, ctypes.byref(b)),
                    "gnnco_block_norm_workspace_bytes")
-            area = _empty((need.value,), torch.uint8, x, stream)
-            ws = self._norm_ws[on] = (F, need.value, area.data_ptr(), area)
-        _check(self._lib.gnnco_block_norm_backward(self._handle, ctypes.byref(d), ctypes.byref(g), ws[2], ws[1], on),
-               "gnnco_block_norm_backward")
+            need = self._norm_sizes[F] = b.value
+        ws = _empty((need,), torch.uint8, x, stream)
+        _check(self._lib.gnnco_block_norm_backward(self._handle, ctypes.byref(d), ctypes.byref(g), ws.data_ptr(), need,
+                                                   _stream_ptr(stream)), "gnnco_block_norm_backward")
         return dict(dx=dx, dy=dy, dgate=dgate, dw_pre=dw_pre, dw_post=dw_post)
 
     def _muon_call(self, like, active, stream, ws):

@@ -1,0 +1,78 @@
+"""The operators around a step recorded in CUDA graphs: what a graph keeps is its own."""
+import numpy as np
+import pytest
+
+from helpers import tiny_graph
+from gpu_common import load_graph, to_dev
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def graph():
+    eu, ev, part = tiny_graph(64, 0.1, 2, seed=5)
+    return load_graph(64, eu, ev, part, int(part.max()) + 1)
+
+
+def _normal(seed, *shape):
+    import torch
+    return torch.randn(*shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed))
+
+
+def _record(call, stream):
+    """A CUDA graph of `call` recorded on `stream`, after one ordinary call there, and what the call returned."""
+    import torch
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        call()
+    stream.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=stream):
+        out = call()
+    return g, out
+
+
+def _norm_inputs(seed, rows, F):
+    return dict(x=_normal(seed, rows, F), dh=_normal(seed + 1, rows, F), w_pre=_normal(seed + 2, F), y=_normal(seed + 3, rows, F),
+                w_post=_normal(seed + 4, F), gate=_normal(seed + 5, F))
+
+
+def test_norm_gradients_of_a_graph_and_of_calls_beside_it(graph):
+    """A later call with wider rows on the recording stream, and tensors that are made after it, leave a recorded backward pass
+    alone, and its replay leaves them alone."""
+    import torch
+    small, wide = _norm_inputs(1, 3000, 64), _norm_inputs(11, 3000, 256)
+    want, want_wide = graph.block_norm_backward(**small), graph.block_norm_backward(**wide)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph.block_norm_backward(**small, stream=stream)
+    g, got = _record(lambda: graph.block_norm_backward(**small, stream=stream), stream)
+    got_wide = graph.block_norm_backward(**wide, stream=stream)
+    stream.synchronize()
+    with torch.cuda.stream(stream):
+        fill = [torch.full((1 << 16,), 7.0, device="cuda") for _ in range(200)]
+    stream.synchronize()
+    g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(got[k], want[k]) for k in want)
+    assert all(torch.equal(got_wide[k], want_wide[k]) for k in want)
+    assert all(bool((t == 7.0).all()) for t in fill)
+
+
+def test_two_graphs_recorded_on_one_stream_share_no_work_area(graph):
+    """... and may be replayed side by side."""
+    import torch
+    a, b = _norm_inputs(1, 200_000, 128), _norm_inputs(11, 200_000, 128)
+    want = [graph.block_norm_backward(**v) for v in (a, b)]
+    stream, other = torch.cuda.Stream(), torch.cuda.Stream()
+    ga, got_a = _record(lambda: graph.block_norm_backward(**a, stream=stream), stream)
+    gb, got_b = _record(lambda: graph.block_norm_backward(**b, stream=stream), stream)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        with torch.cuda.stream(stream):
+            ga.replay()
+        with torch.cuda.stream(other):
+            gb.replay()
+    torch.cuda.synchronize()
+    for want_one, got in zip(want, (got_a, got_b)):
+        assert all(torch.equal(got[k], want_one[k]) for k in want_one)

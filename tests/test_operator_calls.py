@@ -1,0 +1,48 @@
+"""What the binding of the operators around a step keeps and checks, without a GPU: the library behind it is a stand-in that
+records its arguments."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2511_09261_b200 as gnnco
+
+
+class _Library:
+    """Answers every call with OK (sizes with 4,096 bytes) and keeps the arguments."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, args))
+            if name.endswith("_bytes"):
+                args[-1]._obj.value = 4096
+            return 0
+        return call
+
+    def last(self, name):
+        return [args for n, args in self.calls if n == name][-1]
+
+
+@pytest.fixture
+def graph(monkeypatch):
+    g = gnnco.PartitionedGraph.__new__(gnnco.PartitionedGraph)
+    g._lib, g._handle, g.device = _Library(), None, torch.device("cpu")
+    g._plan_sizes, g._norm_sizes = {}, {}
+    monkeypatch.setattr(gnnco, "_stream_ptr", lambda stream=None: 0 if stream is None else stream.cuda_stream)
+    return g
+
+
+def test_norm_gradients_have_a_work_area_per_call(graph, monkeypatch):
+    """Calls on one stream, from two threads or while a graph is recorded, must not share partial sums."""
+    kept, make = [], gnnco._empty
+    monkeypatch.setattr(gnnco, "_empty", lambda *a: kept.append(make(*a)) or kept[-1])
+    monkeypatch.setattr(gnnco, "_require", lambda t, *a: t)
+    x, w = torch.ones(4, 8), torch.ones(8)
+    areas = []
+    for _ in range(2):
+        graph.block_norm_backward(x, x.clone(), w)
+        areas.append(graph._lib.last("gnnco_block_norm_backward")[3])
+    assert areas[0] != areas[1]

@@ -305,8 +305,9 @@ class Muon:
 class EmbeddingPlan:
     """Rows ordered by token (``gnnco_embedding_plan``); serves every gradient with the same tokens and width <= F."""
 
-    def __init__(self, rows: int, V: int, F: int, ws):
+    def __init__(self, rows: int, V: int, F: int, ws, made_on: int):
         self.rows, self.V, self.F, self.ws = rows, V, F, ws
+        self.made_on = made_on      # the stream that ws belongs to
 
 
 class PartitionedGraph:
@@ -643,9 +644,10 @@ class PartitionedGraph:
             _check(self._lib.gnnco_embedding_plan_bytes(rows, V, F, ctypes.byref(b)), "gnnco_embedding_plan_bytes")
             need = self._plan_sizes[(rows, V, F)] = b.value
         ws = _empty((need,), torch.uint8, tokens, stream)
-        _check(self._lib.gnnco_embedding_plan(self._handle, tokens.data_ptr(), rows, V, F, ws.data_ptr(), need,
-                                              _stream_ptr(stream)), "gnnco_embedding_plan")
-        return EmbeddingPlan(rows, V, F, ws)
+        on = _stream_ptr(stream)
+        _check(self._lib.gnnco_embedding_plan(self._handle, tokens.data_ptr(), rows, V, F, ws.data_ptr(), need, on),
+               "gnnco_embedding_plan")
+        return EmbeddingPlan(rows, V, F, ws, on)
 
     def embedding_grad(self, plan: EmbeddingPlan, dout, scale: float = 1.0, out=None, out_dtype=None, stream=None):
         """``gnnco_embedding_grad``: gradient [V, F] of the table of ``embedding_lookup`` for the plan's tokens, from
@@ -664,9 +666,12 @@ class PartitionedGraph:
         else:
             od = _feat_code(out, "out")
             out_ld = self._rows(out, out.dtype, V, F, "out")
+        on = _stream_ptr(stream)
         _check(self._lib.gnnco_embedding_grad(self._handle, gd, od, plan.rows, V, F, dout.data_ptr(), dout_ld, scale,
-                                              ws.data_ptr(), ws.shape[0], out.data_ptr(), out_ld, _stream_ptr(stream)),
+                                              ws.data_ptr(), ws.shape[0], out.data_ptr(), out_ld, on),
                "gnnco_embedding_grad")
+        if on != plan.made_on:      # the area must outlive this use, wherever the plan is dropped
+            ws.record_stream(torch.cuda.current_stream() if stream is None else stream)
         return out
 
     def _weight(self, w, F, what: str):

@@ -76,3 +76,25 @@ def test_two_graphs_recorded_on_one_stream_share_no_work_area(graph):
     torch.cuda.synchronize()
     for want_one, got in zip(want, (got_a, got_b)):
         assert all(torch.equal(got[k], want_one[k]) for k in want_one)
+
+
+def test_a_plan_dropped_while_another_stream_uses_it(graph):
+    """The gradient waits on its stream behind other work when the plan goes; memory that is asked for then must not be the plan's."""
+    import torch
+    rows, V, F = 50_000, 1000, 32
+    tokens = torch.randint(0, V, (rows,), device="cuda", dtype=torch.int32, generator=torch.Generator(device="cuda").manual_seed(1))
+    dout = _normal(2, rows, F)
+    want = graph.embedding_grad(graph.embedding_plan(tokens, V, F), dout)
+    plan = graph.embedding_plan(tokens, V, F)
+    size = plan.ws.shape[0]
+    stream = torch.cuda.Stream()
+    out, factor = torch.empty_like(want), _normal(3, 4096, 4096)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        for _ in range(20):
+            factor @ factor
+    graph.embedding_grad(plan, dout, out=out, stream=stream)
+    del plan
+    others = [torch.full((size,), 1, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and all(bool((t == 1).all()) for t in others)

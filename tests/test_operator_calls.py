@@ -46,3 +46,38 @@ def test_norm_gradients_have_a_work_area_per_call(graph, monkeypatch):
         graph.block_norm_backward(x, x.clone(), w)
         areas.append(graph._lib.last("gnnco_block_norm_backward")[3])
     assert areas[0] != areas[1]
+
+
+class _Stream:
+    def __init__(self, pointer):
+        self.cuda_stream = pointer
+
+
+class _Area:
+    """Stands for a plan's work area; keeps the streams that it is said to be in use on."""
+    device = torch.device("cpu")
+    shape = (4096,)
+
+    def __init__(self):
+        self.used_on = []
+
+    def data_ptr(self):
+        return 1 << 20
+
+    def record_stream(self, stream):
+        self.used_on.append(stream.cuda_stream)
+
+
+def test_a_plan_used_on_another_stream_is_not_handed_out_again_before_that_use(graph, monkeypatch):
+    monkeypatch.setattr(gnnco, "_require", lambda t, *a: t)
+    monkeypatch.setattr(gnnco, "_empty", lambda *a: _Area())
+    dout, out = torch.ones(6, 8), torch.empty(5, 8)
+    tokens = torch.zeros(6, dtype=torch.int32)
+    plan = graph.embedding_plan(tokens, 5, 8, stream=_Stream(17))
+    graph.embedding_grad(plan, dout, out=out, stream=_Stream(17))
+    assert plan.ws.used_on == []
+    graph.embedding_grad(plan, dout, out=out, stream=_Stream(18))
+    assert plan.ws.used_on == [18]
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: _Stream(0))
+    graph.embedding_grad(plan, dout, out=out)
+    assert plan.ws.used_on == [18, 0]

@@ -657,6 +657,8 @@ class PartitionedGraph:
         if dout.dim() != 2 or not 1 <= dout.shape[1] <= plan.F:
             raise ValueError("dout must be [rows, F] with F up to the plan's")
         F, V, ws = dout.shape[1], plan.V, plan.ws
+        if ws.device != self.device:
+            raise ValueError("plan must be one of %s" % self.device)
         dout_ld = self._rows(dout, dout.dtype, plan.rows, F, "dout")
         if out is None:
             if out_dtype is not None and out_dtype not in _feat_codes:
@@ -786,6 +788,10 @@ class PartitionedGraph:
                "gnnco_muon_workspace_bytes")
         if ws is None:
             ws = _empty((max(256, need.value),), torch.uint8, like, stream)
+        else:
+            _require(ws, torch.uint8, "ws")
+            if ws.device != self.device:
+                raise ValueError("ws must be on %s" % self.device)
         return sets, r, c, ws
 
     def muon_update(self, W, m, dW, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True,

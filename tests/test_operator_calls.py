@@ -8,6 +8,9 @@ import torch
 import paper_2511_09261_b200 as gnnco
 
 
+_real_require = gnnco._require
+
+
 class _Library:
     """Answers every call with OK (sizes with 4,096 bytes) and keeps the arguments."""
 
@@ -81,3 +84,26 @@ def test_a_plan_used_on_another_stream_is_not_handed_out_again_before_that_use(g
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: _Stream(0))
     graph.embedding_grad(plan, dout, out=out)
     assert plan.ws.used_on == [18, 0]
+
+
+def test_work_areas_of_the_caller_are_checked(graph, monkeypatch):
+    """An address that is not the handle's device's, or a count that is not bytes, must not reach the kernels."""
+    monkeypatch.setattr(gnnco, "_require", lambda t, dtype, what, device="cuda": _real_require(t, dtype, what, "cpu"))
+    G = torch.ones(2, 20, 24)
+    area = torch.empty(8192, dtype=torch.uint8)
+    for bad, error in ((torch.empty(8192), TypeError), (area[::2], TypeError), (1 << 20, TypeError),
+                       (torch.empty(8192, dtype=torch.uint8, device="meta"), (TypeError, ValueError))):
+        with pytest.raises(error):
+            graph.orthogonalise(G, ws=bad)
+        with pytest.raises(error):
+            graph.muon_update(G.clone(), G.clone(), G, ws=bad)
+    assert not [n for n, _ in graph._lib.calls if n in ("gnnco_orthogonalise", "gnnco_muon_update")]
+    graph.orthogonalise(G, ws=area)
+    assert graph._lib.last("gnnco_orthogonalise")[-3] == area.data_ptr()
+
+
+def test_a_plan_of_another_device_is_refused(graph):
+    plan = gnnco.EmbeddingPlan(6, 5, 8, torch.empty(4096, dtype=torch.uint8, device="meta"), 0)
+    with pytest.raises(ValueError):
+        graph.embedding_grad(plan, torch.ones(6, 8), out=torch.empty(5, 8))
+    assert not graph._lib.calls

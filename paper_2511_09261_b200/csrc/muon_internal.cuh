@@ -19,6 +19,15 @@ struct NsJob {
   int32_t* status;
 };
 
+// u * lift * f = u * scale / (|u| + eps), |u|^2 = norm2.  Where |u| + eps is so small that the factor would leave float32's range (and
+// make 0 * inf of a zero gradient), u is lifted by a power of two first; everywhere else lift is 1.
+struct NsFactor { float lift, f; };
+__device__ __forceinline__ NsFactor ns_factor(double norm2, float eps, float scale) {
+  const double q = sqrt(norm2) + (double)eps;
+  const float lift = q < 1e-20 ? 0x1p96f : 1.0f;
+  return {lift, (float)((double)scale / (q * (double)lift))};
+}
+
 // ---- muon_small.cu: short side up to 16, on the FMA units
 bool ns_small_supported(int32_t k, int32_t n);
 int32_t launch_ns_small(gnnco_handle* h, const NsJob& job, cudaStream_t st);

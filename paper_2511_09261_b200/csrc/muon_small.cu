@@ -76,11 +76,11 @@ __global__ void __launch_bounds__(32 * kWarps) ns_small(const NsJob J) {
     }
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    const float f = (float)(1.0 / (sqrt(sum) + (double)J.eps));
+    const NsFactor by = ns_factor(sum, J.eps, 1.0f);
     __syncwarp();
     for (int j = lane; j < n; j += 32)
 #pragma unroll
-      for (int i = 0; i < K; ++i) X[i * stride + j] = i < k ? X[i * stride + j] * f : 0.0f;
+      for (int i = 0; i < K; ++i) X[i * stride + j] = i < k ? X[i * stride + j] * by.lift * by.f : 0.0f;
     __syncwarp();
     for (int step = 0; step < J.steps; ++step) {
 #pragma unroll

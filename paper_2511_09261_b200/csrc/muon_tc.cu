@@ -487,7 +487,18 @@ __global__ void __launch_bounds__(Cfg<MODE>::THREADS, Cfg<MODE>::PER_SM) ns_on_c
         }
         if (!total_of(sum, &B->peer2, second_it++ & 1)) break;
       }
-      const float f = (float)((double)kXScale / (sqrt(norm2) + (double)J.eps));
+      const NsFactor by = ns_factor(norm2, J.eps, kXScale);
+      if (by.lift != 1.0f) {                               // in place: every unit stays with its thread
+        ua = first_a;
+        ub = first_b;
+        for (int q = threadIdx.x; q < total; q += kStride, next_unit(ua, ub)) {
+          const uint32_t p = by_row ? unit_at(0, ua, ub) : unit_at(0, ub, ua);
+          const float2 x = ld_shared8(p), y = ld_shared8(p + C::XP * kPanel);
+          st_shared8(p, __float_as_uint(x.x * by.lift), __float_as_uint(x.y * by.lift));
+          st_shared8(p + C::XP * kPanel, __float_as_uint(y.x * by.lift), __float_as_uint(y.y * by.lift));
+        }
+      }
+      const float f = by.f;
       ua = first_a;
       ub = first_b;
 #pragma unroll 4

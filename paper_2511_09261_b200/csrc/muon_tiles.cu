@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(256) ns_pack(const NsJob J, int64_t set0, cons
   t = 0.0;
 #pragma unroll
   for (int w = 0; w < 8; ++w) t += part_sum[w];
-  const float f = (float)((double)kXScale / (sqrt(t) + (double)J.eps));
+  const NsFactor by = ns_factor(t, J.eps, kXScale);
   const int rows = rb * 128, chunks = cb * 8;
   const int64_t base = (set0 + s) * (int64_t)J.r * J.c;
   for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < (int64_t)rows * chunks; q += (int64_t)gridDim.x * 256) {
@@ -412,7 +412,7 @@ __global__ void __launch_bounds__(256) ns_pack(const NsJob J, int64_t set0, cons
       }
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) split2(u[2 * e] * f, u[2 * e + 1] * f, hi[e], lo[e]);
+    for (int e = 0; e < 4; ++e) split2(u[2 * e] * by.lift * by.f, u[2 * e + 1] * by.lift * by.f, hi[e], lo[e]);
     uint8_t* const to = X + s * x_set + ((int64_t)(ch >> 3) * rb + (i >> 7)) * kPanel + at_chunk(i & 127, ch & 7);
     *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
     *reinterpret_cast<uint4*>(to + x_limb) = make_uint4(lo[0], lo[1], lo[2], lo[3]);

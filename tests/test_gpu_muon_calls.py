@@ -44,3 +44,23 @@ def test_bf16_copies_are_rebuilt_after_a_part_of_the_weights_changed(write):
         losses.append(torch.stack(out))
     assert not torch.equal(losses[0][0], losses[0][1])
     assert torch.equal(losses[0], losses[1])
+
+
+@pytest.mark.parametrize("r,c", [(16, 16), (1, 9), (128, 100), (100, 200), (200, 256), (300, 260)])
+@pytest.mark.parametrize("eps", [1e-36, 1e-42])
+def test_any_eps_above_zero(graph, r, c, eps):
+    """A zero gradient stays zero, and one far below float32's normal range is orthogonalised like any other.  (2^-24 grows by 3.4445
+    per step: 1.1e-4 over the 15 products of five steps in the worst direction; entries below 2^-126 are given as they are.)"""
+    import torch
+    import operators_ref as ref
+    G = torch.randn(3, r, c, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    G[0] = 0.0
+    G[1] *= 1e-37
+    O = graph.orthogonalise(G, coefs=COEFS, eps=eps)
+    assert bool((O[0] == 0).all())
+    want = ref.newton_schulz(G[1:].cpu().numpy(), 5, COEFS, float(np.float32(eps)))
+    err = np.sqrt(((O[1:].double().cpu().numpy() - want) ** 2).sum(axis=(1, 2)))
+    assert np.all(err <= 1.1e-4 * np.sqrt((want ** 2).sum(axis=(1, 2)))), err
+    W, m = torch.ones(3, r, c, device="cuda"), torch.zeros(3, r, c, device="cuda")
+    graph.muon_update(W, m, torch.zeros_like(W), eps=eps)
+    assert bool((W == 1).all()) and bool((m == 0).all())

@@ -75,7 +75,7 @@ __device__ __forceinline__ void tile_of(int t, int n, int& i, int& j) {
 
 template <int KIND, int TN, int SPLIT>
 __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
-  static_assert(TN == 128 || (TN == 64 && SPLIT == 1), "clusters split tiles of 128 columns");
+  static_assert(SPLIT == 1 || (KIND == kGram && TN == 128), "clusters take tiles of X X^T");
   constexpr uint32_t kStageBytes = 2 * kPanel + 2 * TN * 128;
   constexpr int kStages = kRing / kStageBytes;
   constexpr uint32_t B_LIMB = TN * 128;                    // bytes of the right operand's limb in a stage
@@ -301,8 +301,8 @@ __global__ void __launch_bounds__(kThreads, 1) ns_tiles(const TileJob T) {
           for (int e = 0; e < 32; ++e)
             if (i < J.k && j0 + e < J.n) put(base + (int64_t)(j0 + e) * J.c + i, w[e], __uint_as_float(v[e]) * fo);
         } else {
-          // rows pass through shared memory, so that lanes work on neighbouring columns (past what SPLIT exchanges)
-          const uint32_t stage = sbase + 8 * kPanel + warp * 4096;
+          // rows pass through shared memory, so that lanes work on neighbouring columns
+          const uint32_t stage = sbase + warp * 4096;
 #pragma unroll
           for (int e = 0; e < 8; ++e) tc::st_shared16(stage + at_chunk(lane, e), v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
           __syncwarp();
@@ -554,11 +554,12 @@ int resident_quads() {
 }
 
 // `tiles` counts tiles of 128 columns.  Narrow tiles while they leave SMs free; a cluster per tile for a long k, where the GPU holds
-// them all at once.
+// them all at once.  (A long k of A A or P X is a long side of A, whose tiles are too many for that: X X^T only.)
 constexpr int kLongStages = 40;
 template <int KIND>
 int32_t launch_product(gnnco_handle* h, const TileJob& T, int64_t tiles, unsigned sets, cudaStream_t st) {
-  if (T.stages >= kLongStages && tiles * sets <= resident_quads()) return launch_form<KIND, 128, 4>(h, T, tiles, sets, st);
+  if constexpr (KIND == kGram)
+    if (T.stages >= kLongStages && tiles * sets <= resident_quads()) return launch_form<KIND, 128, 4>(h, T, tiles, sets, st);
   if (tiles * sets * 2 <= h->sm_count) return launch_form<KIND, 64, 1>(h, T, 2 * tiles, sets, st);
   return launch_form<KIND, 128, 1>(h, T, tiles, sets, st);
 }

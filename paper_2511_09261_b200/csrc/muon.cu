@@ -33,22 +33,18 @@ bool coefficients_bounded(double a, double b, double c, int steps, double* p_max
   double top = 1.0;
   *p_max = 0.0;
   auto poly = [&](double u) { return a + u * (b + u * c); };
-  double root[3];
-  int roots = 0;
-  if (c != 0.0) {
-    const double disc = 9.0 * b * b - 20.0 * a * c;
-    if (disc >= 0.0) {
-      root[roots++] = (-3.0 * b - sqrt(disc)) / (10.0 * c);
-      root[roots++] = (-3.0 * b + sqrt(disc)) / (10.0 * c);
-    }
-  } else if (b != 0.0) {
-    root[roots++] = -a / (3.0 * b);
+  double root[2] = {-1.0, -1.0};                           // of 5 c u^2 + 3 b u + a; the form that does not cancel where c is tiny
+  const double disc = 9.0 * b * b - 20.0 * a * c;
+  if (disc >= 0.0) {
+    const double q = -0.5 * (3.0 * b + copysign(sqrt(disc), b));
+    if (c != 0.0) root[0] = q / (5.0 * c);
+    if (q != 0.0) root[1] = a / q;
   }
   for (int t = 0; t < steps; ++t) {
     const double u_top = top * top;
     double reach = fabs(top * poly(u_top));
-    for (int q = 0; q < roots; ++q)
-      if (root[q] > 0.0 && root[q] < u_top) reach = fmax(reach, fabs(sqrt(root[q]) * poly(root[q])));
+    for (double u : root)
+      if (u > 0.0 && u < u_top) reach = fmax(reach, fabs(sqrt(u) * poly(u)));
     const double vertex = c != 0.0 ? -b / (2.0 * c) : -1.0;
     double p = fmax(fabs(a), fabs(poly(u_top)));
     if (vertex > 0.0 && vertex < u_top) p = fmax(p, fabs(poly(vertex)));

@@ -814,6 +814,8 @@ class PartitionedGraph:
 
     def muon_step(self, model: Model, opt: Muon, dW: Sequence, stream=None) -> None:
         """One ``muon_update`` of every layer of ``model`` with the gradients ``dW`` of a training step."""
+        if not len(model.W) == len(opt.m) == len(dW):
+            raise ValueError("%d layers, %d momenta, %d gradients" % (len(model.W), len(opt.m), len(dW)))
         for W, m, g in zip(model.W, opt.m, dW):
             self.muon_update(W, m, g, opt.lr, opt.momentum, opt.nesterov, opt.weight_decay, opt.steps, opt.coefs, opt.eps,
                              opt.active, stream=stream)

@@ -107,3 +107,20 @@ def test_a_plan_of_another_device_is_refused(graph):
     with pytest.raises(ValueError):
         graph.embedding_grad(plan, torch.ones(6, 8), out=torch.empty(5, 8))
     assert not graph._lib.calls
+
+
+def test_a_step_of_another_number_of_layers_is_refused(graph, monkeypatch):
+    """Gradients or momenta that do not go with the model's layers must not leave layers out silently."""
+    from types import SimpleNamespace
+    monkeypatch.setattr(gnnco, "_require", lambda t, *a: t)
+    W = [torch.ones(2, 8, 4), torch.ones(2, 4, 1)]
+    opt = SimpleNamespace(lr=0.1, momentum=0.9, nesterov=True, weight_decay=0.0, steps=5, coefs=gnnco.MUON_COEFS, eps=1e-7, active=None,
+                          m=[torch.zeros_like(w) for w in W])
+    model = SimpleNamespace(W=W)
+    short = SimpleNamespace(**{**vars(opt), "m": opt.m[:1]})
+    for o, dW in ((opt, W[:1]), (opt, W + W[:1]), (short, W)):
+        with pytest.raises(ValueError):
+            graph.muon_step(model, o, dW)
+    assert not graph._lib.calls
+    graph.muon_step(model, opt, W)
+    assert sum(n == "gnnco_muon_update" for n, _ in graph._lib.calls) == 2

@@ -201,6 +201,13 @@ def _require(t, dtype, what: str, device_type: str = "cuda"):
     return t
 
 
+def _int32(*sizes) -> None:
+    """Refuses what the C ABI's 32-bit arguments would cut off (ctypes does not)."""
+    for n in sizes:
+        if not -0x80000000 <= n <= 0x7fffffff:
+            raise ValueError("%d does not fit in 32 bits" % n)
+
+
 _feat_codes = {}
 
 
@@ -619,6 +626,7 @@ class PartitionedGraph:
         if table.dim() != 2 or 0 in table.shape:
             raise ValueError("table must be [V, F]")
         V, F = table.shape
+        _int32(V, F)
         table_ld = self._rows(table, table.dtype, V, F, "table")
         if out is None:
             if out_dtype is not None and out_dtype not in _feat_codes:
@@ -638,6 +646,7 @@ class PartitionedGraph:
         synchronisation."""
         import torch
         rows = self._tokens(tokens)
+        _int32(V, F)
         need = self._plan_sizes.get((rows, V, F))
         if need is None:
             b = _sz(0)
@@ -692,6 +701,7 @@ class PartitionedGraph:
         if y is None and (gate is not None or w_post is not None):
             raise ValueError("gate and w_post belong to a block output y")
         rows, F = x.shape
+        _int32(F)
         d = BlockNormDesc(rows, F, dt, eps, scale, x.data_ptr(), self._rows(x, x.dtype, rows, F, "x"))
         if y is not None:
             d.y, d.y_ld = y.data_ptr(), self._rows(y, x.dtype, rows, F, "y")
@@ -776,9 +786,10 @@ class PartitionedGraph:
                                                    _stream_ptr(stream)), "gnnco_block_norm_backward")
         return dict(dx=dx, dy=dy, dgate=dgate, dw_pre=dw_pre, dw_post=dw_post)
 
-    def _muon_call(self, like, active, stream, ws):
+    def _muon_call(self, like, steps, active, stream, ws):
         import torch
         sets, r, c = like.shape
+        _int32(r, c, steps)
         if active is not None:
             _require(active, torch.uint8, "active")
             if tuple(active.shape) != (sets,) or active.device != self.device:
@@ -805,7 +816,7 @@ class PartitionedGraph:
             _require(t, torch.float32, what)
             if t.dim() != 3 or t.shape != W.shape or t.device != self.device:
                 raise ValueError("W, m and dW must be [sets, d_in, d_out] on %s" % self.device)
-        sets, r, c, ws = self._muon_call(W, active, stream, ws)
+        sets, r, c, ws = self._muon_call(W, steps, active, stream, ws)
         p = MuonParams(lr, momentum, weight_decay, int(nesterov), steps, coefs[0], coefs[1], coefs[2], eps, _dptr(active))
         _check(self._lib.gnnco_muon_update(self._handle, sets, r, c, W.data_ptr(), m.data_ptr(), dW.data_ptr(),
                                            ctypes.byref(p), ws.data_ptr(), ws.numel(), _stream_ptr(stream)),
@@ -834,7 +845,7 @@ class PartitionedGraph:
         _require(out, out.dtype, "out")
         if out.shape != G.shape or out.device != self.device:
             raise ValueError("out must have the shape of G")
-        sets, r, c, ws = self._muon_call(G, active, stream, ws)
+        sets, r, c, ws = self._muon_call(G, steps, active, stream, ws)
         p = MuonParams(0.0, 0.0, 0.0, 0, steps, coefs[0], coefs[1], coefs[2], eps, _dptr(active))
         _check(self._lib.gnnco_orthogonalise(self._handle, gd, od, sets, r, c, G.data_ptr(), out.data_ptr(),
                                              ctypes.byref(p), ws.data_ptr(), ws.numel(), _stream_ptr(stream)),

@@ -124,3 +124,23 @@ def test_a_step_of_another_number_of_layers_is_refused(graph, monkeypatch):
     assert not graph._lib.calls
     graph.muon_step(model, opt, W)
     assert sum(n == "gnnco_muon_update" for n, _ in graph._lib.calls) == 2
+
+
+def test_sizes_past_32_bits_are_refused(graph, monkeypatch):
+    """The C ABI counts table rows, columns and steps in 32 bits; what does not fit must not arrive as what is left of it."""
+    monkeypatch.setattr(gnnco, "_require", lambda t, *a: t)
+    graph.device = torch.device("meta")
+    big = 2 ** 32 + 5
+    tokens = torch.empty(6, dtype=torch.int32, device="meta")
+    table = torch.empty(big, 8, dtype=torch.bfloat16, device="meta")
+    wide = torch.empty(2, big, device="meta")
+    tall = torch.empty(1, big, 3, device="meta")
+    some = torch.empty(1, 4, 3, device="meta")
+    for call in (lambda: graph.embedding_lookup(table, tokens), lambda: graph.embedding_lookup(wide, tokens),
+                 lambda: graph.embedding_plan(tokens, big, 8), lambda: graph.embedding_plan(tokens, 8, big),
+                 lambda: graph.block_norm(wide), lambda: graph.block_norm_backward(wide, wide),
+                 lambda: graph.muon_update(tall, tall, tall), lambda: graph.orthogonalise(tall),
+                 lambda: graph.orthogonalise(some, steps=big), lambda: graph.muon_update(some, some, some, steps=big)):
+        with pytest.raises(ValueError):
+            call()
+    assert not graph._lib.calls

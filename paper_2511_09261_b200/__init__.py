@@ -741,6 +741,8 @@ class PartitionedGraph:
         dict(dx, dy, dgate, dw_pre, dw_post); entries whose input was not given are None."""
         import torch
         d = self._block_desc(x, w_pre, y, w_post, gate, scale, eps)
+        if y is None and dy is not None or gate is None and dgate is not None:
+            raise ValueError("dy belongs to a block output y, dgate to a gate")
         rows, F, dtype = d.rows, d.F, x.dtype
         shape = (rows, F)
         g = BlockNormGrads()

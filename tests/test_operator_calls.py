@@ -144,3 +144,13 @@ def test_sizes_past_32_bits_are_refused(graph, monkeypatch):
         with pytest.raises(ValueError):
             call()
     assert not graph._lib.calls
+
+
+def test_results_without_their_inputs_are_refused(graph, monkeypatch):
+    """A dy without y, or a dgate without a gate, would come back as it was given."""
+    monkeypatch.setattr(gnnco, "_require", lambda t, *a: t)
+    x = torch.ones(4, 8)
+    for kw in (dict(dy=torch.empty(4, 8)), dict(dgate=torch.empty(8)), dict(y=x, dgate=torch.empty(4, 8))):
+        with pytest.raises(ValueError):
+            graph.block_norm_backward(x, x.clone(), **kw)
+    assert not graph._lib.calls

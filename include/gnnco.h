@@ -448,8 +448,8 @@ int32_t gnnco_block_norm_backward(gnnco_handle* h, const gnnco_block_norm_desc* 
  * on another handle and replays of a recorded graph are not.
  * gnnco_orthogonalise: O = X after the steps, in G's orientation, for G and O [sets x rows x cols] in float32 or bfloat16
  * (lr, momentum, weight_decay and nesterov are not read; sets that are not active are not written; O may be G).
- * ws: gnnco_muon_workspace_bytes bytes, 256-byte aligned.  Asynchronous on `stream`; results do not depend on `sets` or
- * on timing. */
+ * ws: gnnco_muon_workspace_bytes bytes, 256-byte aligned, NULL where that is 0.  Asynchronous on `stream`; results do not
+ * depend on `sets` or on timing. */
 typedef struct {
   float lr, momentum, weight_decay;
   int32_t nesterov;

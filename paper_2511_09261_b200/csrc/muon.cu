@@ -96,11 +96,13 @@ extern "C" int32_t gnnco_muon_workspace_bytes(const gnnco_handle* h, int64_t set
 
 extern "C" int32_t gnnco_muon_update(gnnco_handle* h, int64_t sets, int32_t rows, int32_t cols, float* W, float* m, const float* dW,
                                      const gnnco_muon_params* p, void* ws, size_t ws_bytes, void* stream) {
-  if (!h || !W || !m || !dW || !p || !ws || ((uintptr_t)ws & 255) || !valid_sizes(sets, rows, cols)) return GNNCO_INVALID_ARGUMENT;
+  if (!h || !W || !m || !dW || !p || ((uintptr_t)ws & 255) || !valid_sizes(sets, rows, cols)) return GNNCO_INVALID_ARGUMENT;
   NsParams P{p->steps, p->a, p->b, p->c, p->eps, 1.0f};
   const int32_t rc = check_params(P);
   if (rc != GNNCO_OK) return rc;
-  if (ws_bytes < workspace_bytes(h, sets, rows, cols)) return GNNCO_WORKSPACE_TOO_SMALL;
+  const size_t need = workspace_bytes(h, sets, rows, cols);
+  if (ws_bytes < need) return GNNCO_WORKSPACE_TOO_SMALL;
+  if (need > 0 && !ws) return GNNCO_INVALID_ARGUMENT;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   ProfScope prof_(h, K_MUON, st);
   weights_written(h, W, (size_t)sets * rows * cols * sizeof(float));
@@ -112,13 +114,15 @@ extern "C" int32_t gnnco_muon_update(gnnco_handle* h, int64_t sets, int32_t rows
 extern "C" int32_t gnnco_orthogonalise(gnnco_handle* h, int32_t in_dtype, int32_t out_dtype, int64_t sets, int32_t rows, int32_t cols,
                                        const void* G, void* O, const gnnco_muon_params* p, void* ws, size_t ws_bytes,
                                        void* stream) {
-  if (!h || !G || !O || !p || !ws || ((uintptr_t)ws & 255) || !valid_sizes(sets, rows, cols)) return GNNCO_INVALID_ARGUMENT;
+  if (!h || !G || !O || !p || ((uintptr_t)ws & 255) || !valid_sizes(sets, rows, cols)) return GNNCO_INVALID_ARGUMENT;
   if ((in_dtype != GNNCO_F32 && in_dtype != GNNCO_BF16) || (out_dtype != GNNCO_F32 && out_dtype != GNNCO_BF16))
     return GNNCO_UNSUPPORTED;
   NsParams P{p->steps, p->a, p->b, p->c, p->eps, 1.0f};
   const int32_t rc = check_params(P);
   if (rc != GNNCO_OK) return rc;
-  if (ws_bytes < workspace_bytes(h, sets, rows, cols)) return GNNCO_WORKSPACE_TOO_SMALL;
+  const size_t need = workspace_bytes(h, sets, rows, cols);
+  if (ws_bytes < need) return GNNCO_WORKSPACE_TOO_SMALL;
+  if (need > 0 && !ws) return GNNCO_INVALID_ARGUMENT;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   ProfScope prof_(h, K_MUON, st);
   weights_written(h, O, (size_t)sets * rows * cols * (out_dtype == GNNCO_F32 ? sizeof(float) : 2));

@@ -64,3 +64,20 @@ def test_any_eps_above_zero(graph, r, c, eps):
     W, m = torch.ones(3, r, c, device="cuda"), torch.zeros(3, r, c, device="cuda")
     graph.muon_update(W, m, torch.zeros_like(W), eps=eps)
     assert bool((W == 1).all()) and bool((m == 0).all())
+
+
+def test_no_work_area_where_none_is_needed(graph):
+    import torch
+    import paper_2511_09261_b200 as gnnco
+    none = torch.empty(0, dtype=torch.uint8, device="cuda")
+    for r, c in ((16, 9), (128, 100), (90, 250)):
+        G = torch.randn(3, r, c, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+        assert torch.equal(graph.orthogonalise(G, ws=none), graph.orthogonalise(G))
+        W, W2 = torch.ones_like(G), torch.ones_like(G)
+        graph.muon_update(W, torch.zeros_like(G), G, ws=none)
+        graph.muon_update(W2, torch.zeros_like(G), G)
+        assert torch.equal(W, W2)
+    for r, c in ((200, 200), (300, 300)):
+        with pytest.raises(gnnco.GnncoError) as e:
+            graph.orthogonalise(torch.ones(1, r, c, device="cuda"), ws=none)
+        assert e.value.status == gnnco.WORKSPACE_TOO_SMALL

@@ -98,3 +98,47 @@ def test_a_plan_dropped_while_another_stream_uses_it(graph):
     others = [torch.full((size,), 1, dtype=torch.uint8, device="cuda") for _ in range(4)]
     torch.cuda.synchronize()
     assert torch.equal(out, want) and all(bool((t == 1).all()) for t in others)
+
+
+@pytest.mark.parametrize("rows", [3000, 150_000])
+def test_lookup_order_and_gradient_replay_on_new_inputs(graph, rows):
+    import torch
+    V, F = 500, 40
+    make = lambda seed: torch.randint(-1, V, (rows,), device="cuda", dtype=torch.int32,  # noqa: E731
+                                      generator=torch.Generator(device="cuda").manual_seed(seed))
+    table, tokens, dout = _normal(1, V, F), make(1), _normal(2, rows, F)
+    stream = torch.cuda.Stream()
+
+    def call():
+        return (graph.embedding_lookup(table, tokens, scale=2.0, stream=stream),
+                graph.embedding_grad(graph.embedding_plan(tokens, V, F, stream=stream), dout, scale=2.0, stream=stream))
+
+    g, got = _record(call, stream)
+    for seed in (3, 4):
+        table.copy_(_normal(seed, V, F))
+        tokens.copy_(make(seed))
+        dout.copy_(_normal(seed + 10, rows, F))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], graph.embedding_lookup(table, tokens, scale=2.0))
+        assert torch.equal(got[1], graph.embedding_grad(graph.embedding_plan(tokens, V, F), dout, scale=2.0))
+
+
+@pytest.mark.parametrize("sets,r,c", [(300, 16, 9), (400, 64, 32), (60, 100, 200), (100, 200, 140), (3, 300, 400), (1, 70, 2700)])
+def test_updates_replay_on_new_inputs(graph, sets, r, c):
+    import torch
+    W, m, d = _normal(1, sets, r, c), _normal(2, sets, r, c), _normal(3, sets, r, c)
+    W2, m2 = W.clone(), m.clone()
+    stream = torch.cuda.Stream()
+    g, _ = _record(lambda: graph.muon_update(W, m, d, lr=0.1, weight_decay=0.1, stream=stream), stream)
+    W.copy_(W2)
+    m.copy_(m2)
+    for seed in (5, 6, 7):
+        d.copy_(_normal(seed, sets, r, c))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        graph.muon_update(W2, m2, d, lr=0.1, weight_decay=0.1)
+        assert torch.equal(W, W2) and torch.equal(m, m2)
+    assert graph.async_status() == 0

@@ -142,7 +142,10 @@ int32_t lookup_typed(gnnco_handle* h, const int32_t* tokens, const TT* table, in
 constexpr int kOrdThreads = 512, kOrdWarps = kOrdThreads / 32, kOrdRounds = 8;
 constexpr int kOrdTile = kOrdThreads * kOrdRounds;         // positions of one block-wide step
 constexpr int kOrdMaxBlocks = 444;                         // 3 per SM: all resident at once
-constexpr int kOrdFewBlocks = 24;                          // up to here no separate scan
+// Up to here no separate scan: every block adds up the block counts itself, which saves a launch per pass and costs reads that grow with
+// the blocks (with and without the scan: one pass of 10 bits 12.2 and 10.8 us over 4 blocks, 13.5 and 14.7 over 12, 14.0 and 24.5 over 25;
+// two passes 22.4 and 19.2, 22.7 and 20.2, 22.9 and 24.0).
+constexpr int kOrdFewBlocks = 12;
 constexpr int kOrdMaxBits = 10, kOrdMaxDigits = 1 << kOrdMaxBits;
 constexpr int kSmallRows = 4096;                           // up to here one block sorts everything in shared memory
 

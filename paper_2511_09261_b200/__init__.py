@@ -626,7 +626,8 @@ class PartitionedGraph:
         if table.dim() != 2 or 0 in table.shape:
             raise ValueError("table must be [V, F]")
         V, F = table.shape
-        _int32(V, F)
+        if (V | F) >> 31:
+            _int32(V, F)
         table_ld = self._rows(table, table.dtype, V, F, "table")
         if out is None:
             if out_dtype is not None and out_dtype not in _feat_codes:
@@ -646,7 +647,8 @@ class PartitionedGraph:
         synchronisation."""
         import torch
         rows = self._tokens(tokens)
-        _int32(V, F)
+        if (V | F) >> 31:
+            _int32(V, F)
         need = self._plan_sizes.get((rows, V, F))
         if need is None:
             b = _sz(0)
@@ -701,7 +703,8 @@ class PartitionedGraph:
         if y is None and (gate is not None or w_post is not None):
             raise ValueError("gate and w_post belong to a block output y")
         rows, F = x.shape
-        _int32(F)
+        if F >> 31:
+            _int32(F)
         d = BlockNormDesc(rows, F, dt, eps, scale, x.data_ptr(), self._rows(x, x.dtype, rows, F, "x"))
         if y is not None:
             d.y, d.y_ld = y.data_ptr(), self._rows(y, x.dtype, rows, F, "y")
@@ -791,7 +794,8 @@ class PartitionedGraph:
     def _muon_call(self, like, steps, active, stream, ws):
         import torch
         sets, r, c = like.shape
-        _int32(r, c, steps)
+        if (r | c | steps) >> 31:
+            _int32(r, c, steps)
         if active is not None:
             _require(active, torch.uint8, "active")
             if tuple(active.shape) != (sets,) or active.device != self.device:

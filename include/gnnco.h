@@ -370,8 +370,8 @@ int32_t gnnco_embedding_update(gnnco_handle* h, int32_t feat_dtype, int32_t F, c
  *
  * gnnco_embedding_grad: dtable[v,:] = scale * sum over rows i with token v of dout[i,:], for every v < V (zeros for a
  * token that does not occur), summed in float32 in the plan's order (bit-identical from run to run, no
- * floating-point atomics) and rounded once to table_dtype.  rows, V and F as given to the plan; partial sums use
- * plan_ws, so gradients from one plan must not overlap on the GPU.
+ * floating-point atomics) and rounded once to table_dtype.  rows and V as given to the plan, F at most the plan's; partial
+ * sums use plan_ws, so gradients from one plan must not overlap on the GPU.
  * All three are asynchronous on `stream`; 0 <= rows < 2^31 - 1, F <= 65536. */
 int32_t gnnco_embedding_lookup(gnnco_handle* h, int32_t table_dtype, int32_t out_dtype, int64_t rows, int32_t V, int32_t F,
                                const int32_t* tokens, const void* table, int64_t table_ld, float scale, void* out,
@@ -439,13 +439,14 @@ int32_t gnnco_block_norm_backward(gnnco_handle* h, const gnnco_block_norm_desc* 
  *   X = u / (|u|_F + eps), transposed where rows > cols;   `steps` times:  A = X X^T,  X = (a I + b A + c A A) X
  *   W = W (1 - lr * weight_decay) - lr * sqrt(max(1, cols / rows)) * X
  * The usual coefficients are a = 3.4445, b = -4.7750, c = 2.0315 with 5 steps: singular values of u end near 1.
- * Coefficients that carry a singular value in [0, 1] past 2 are refused; steps 1 .. 32.  Products are taken to float32
- * accuracy (operands split into two float16 limbs, float32 accumulation; float32 where the short side is at most 16);
- * sums of squares are joined in float64.  A zero
- * gradient gives a zero X; a matrix with an infinity or NaN in u gives NaN in its own set only.  `active` (device,
- * [sets] uint8, or NULL = all): sets with active[s] == 0 keep W and m bit for bit.  Weights that a
- * call on this handle writes, all or some sets of a layer, are noticed by GNNCO_WEIGHTS_UNTOUCHED of this handle (so is O); calls
- * on another handle and replays of a recorded graph are not.
+ * Coefficients that carry a singular value in [0, 1] past 2 are refused; steps 1 .. 32.  Sums of squares are joined in
+ * float64.  Products are float32 where the short side is at most 16 and the long one at most 256.  Elsewhere X, A and
+ * a I + b A + c A A are held as two float16 limbs between products (22 bits, fixed scales) with float32 accumulation:
+ * float32 accuracy by norm, not by entry -- entries of X below 2^-39 (of a matrix that starts with norm 1) become zero, and
+ * rows far smaller than the rest keep fewer digits.  A zero gradient gives a zero X; a matrix with an infinity or NaN in u gives
+ * NaN in its own set only.  `active` (device, [sets] uint8, or NULL = all): sets with active[s] == 0 keep W and m bit for
+ * bit.  Weights that a call on this handle writes, all or some sets of a layer, O included, are noticed by this handle's
+ * GNNCO_WEIGHTS_UNTOUCHED; calls on another handle and replays of a recorded graph are not.
  * gnnco_orthogonalise: O = X after the steps, in G's orientation, for G and O [sets x rows x cols] in float32 or bfloat16
  * (lr, momentum, weight_decay and nesterov are not read; sets that are not active are not written; O may be G).
  * ws: gnnco_muon_workspace_bytes bytes, 256-byte aligned, NULL where that is 0.  Asynchronous on `stream`; results do not
@@ -455,7 +456,7 @@ typedef struct {
   int32_t nesterov;
   int32_t steps;
   float a, b, c;
-  float eps;                     /* > 0 */
+  float eps;                     /* > 0, however small */
   const uint8_t* active;
 } gnnco_muon_params;
 int32_t gnnco_muon_workspace_bytes(const gnnco_handle* h, int64_t sets, int32_t rows, int32_t cols, size_t* bytes);

@@ -104,7 +104,7 @@ __device__ __forceinline__ float inverse_rms(float sum_of_squares, const NormArg
 }
 
 // Teams of TEAM lanes, K vectors of VEC elements per lane; blocks go through the rows grid-stride, weights stay in
-// registers.  2.5M x 256 bf16: 871 us (5.9 TB/s); 878 with the registers of four blocks per SM, 975 with five; two rows of a team in
+// registers.  2.5M x 256 bf16: 895 us (5.7 TB/s); 911 with the registers of four blocks per SM, 970 with five; two rows of a team in
 // flight at a time changed nothing.
 template <typename T, int VEC, int TEAM, int K>
 __global__ void __launch_bounds__(TEAM > 256 ? TEAM : 256)
@@ -164,7 +164,7 @@ norm_forward(const NormArgs A, const int gate_kind) {
   }
 }
 
-// Three blocks per SM where a lane holds at most eight elements: 2.5M x 256 bf16 takes 1,370 us so (5.6 TB/s), 1,902 with two and 1,565
+// Three blocks per SM where a lane holds at most eight elements: 2.5M x 256 bf16 takes 1,426 us so (5.4 TB/s), 1,548 with two and 1,688
 // with four, whose registers spill.
 template <typename T, int VEC, int TEAM, int K>
 __global__ void __launch_bounds__(TEAM > 256 ? TEAM : 256, TEAM > 256 ? 1 : K * VEC <= 8 ? 3 : 1)
@@ -326,8 +326,8 @@ int32_t launch_one(bool backward, const NormArgs& A, int gate_kind, int sms, int
 }
 
 // Few lanes with several vectors each beat many lanes with one: fewer shuffles per row, and fewer idle lanes where a row is no power
-// of two (backward, a vector per lane against this: 1,774,098 x 34 bf16 537 and 206 us, 1,568,659 x 41 float32 499 and 335 us,
-// 1.13M x 128 float32 562 and 550 us).  A lane holds at most 16 elements.
+// of two (backward, a vector per lane against this: 1,774,098 x 34 bf16 534 and 208 us, 1,568,659 x 41 float32 504 and 346 us,
+// 1.13M x 128 float32 592 and 574 us).  A lane holds at most 16 elements.
 template <typename T, int VEC>
 int32_t launch_width(bool backward, const NormArgs& A, int gate_kind, int sms, int* blocks, cudaStream_t st) {
   const int v = (A.F + VEC - 1) / VEC;                     // vectors per row

@@ -17,7 +17,7 @@
 // part each, hands the others their column group of its partial tile through distributed shared memory, and finishes its
 // own group.  The results are the same bits in all forms.  (The exchange takes 4.7 us, as long as nine stages: clusters pay
 // from some 40 stages on, below that narrow tiles spread the work better.)
-// 1,000 x 1,537 takes 240 us: 15 products of 13 to 15 us (0.5 us a stage, near the 0.4 us of its MMAs), each with 2 us until the next one
+// 1,000 x 1,537 takes 243 us: 15 products of 13 to 15 us (0.5 us a stage, near the 0.4 us of its MMAs), each with 2 us until the next one
 // starts, 1 us until its first operands arrive and 2 to 3 us of conversion and stores.
 // Launches are chained by programmatic dependence: a kernel sets itself up while the one before it finishes.
 // Roles: warps 0-7 epilogue (TMEM lanes 32 (w % 4), column half w / 4), warp 8 issues MMAs, warp 9 the copies.

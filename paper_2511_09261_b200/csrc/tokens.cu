@@ -22,7 +22,7 @@ namespace {
 // few rows use 4-row tiles to spread over the SMs.  Two forms:
 //   lookup_rows    rows of 2^i (up to 32) or a multiple of 32 vectors: `width` lanes per row, so a lane's column never changes
 //   lookup_kernel  any other width: the lanes walk the tile's vectors as one flat list
-// (10M x 256 bf16: 1,001 us in the flat form, whose index arithmetic takes two thirds of the issue slots.)
+// (10M x 256 bf16: 904 us, 983 in the flat form, whose index arithmetic takes two thirds of the issue slots.)
 template <typename TT, typename TO, int VEC>
 __global__ void __launch_bounds__(256) lookup_rows(const int32_t* __restrict__ tokens, const TT* __restrict__ table, int64_t table_ld,
                                                    TO* __restrict__ out, int64_t out_ld, int64_t rows, int32_t V,
@@ -554,9 +554,9 @@ __device__ __forceinline__ bool is_solid(const int32_t* __restrict__ keys, int64
   return k < V && keys[min(N, (c + group) * chunk) - 1] == k;
 }
 
-// Rows in flight against blocks per SM, ordering included: 10M x 256 bf16 takes 1,409 us with eight rows at four blocks (1,424 with four
-// at five, 1,545 with eight at three), 1.13M x 128 float32 168 us with four rows at five blocks (177 with eight at four); more
-// blocks spill registers (1,560 and 191 us at six).
+// Rows in flight against blocks per SM, ordering included: 10M x 256 bf16 takes 1,441 us with eight rows at four blocks (1,456 with four
+// at five), 1.13M x 128 float32 166 us with four rows at five blocks (172 with eight at four); more blocks spill registers (2,370 and
+// 187 us at six).  Eight rows at three blocks take 1,389 us, but 198 instead of 144 us for 4M x 64 bf16 over 300 tokens.
 // A lane holds K vectors, TEAM vectors apart (narrow vectors: more columns per visit of a row).  The blocks after the last chunk
 // mark the tokens that occur.
 template <typename T, typename TO, int VEC, int TEAM, int K>

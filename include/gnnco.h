@@ -440,13 +440,14 @@ int32_t gnnco_block_norm_backward(gnnco_handle* h, const gnnco_block_norm_desc* 
  *   W = W (1 - lr * weight_decay) - lr * sqrt(max(1, cols / rows)) * X
  * The usual coefficients are a = 3.4445, b = -4.7750, c = 2.0315 with 5 steps: singular values of u end near 1.
  * Coefficients that carry a singular value in [0, 1] past 2 are refused; steps 1 .. 32.  Sums of squares are joined in
- * float64.  Products are float32 where the short side is at most 16 and the long one at most 256.  Elsewhere X, A and
- * a I + b A + c A A are held as two float16 limbs between products (22 bits, fixed scales) with float32 accumulation:
- * float32 accuracy by norm, not by entry -- entries of X below 2^-39 (of a matrix that starts with norm 1) become zero, and
- * rows far smaller than the rest keep fewer digits.  A zero gradient gives a zero X; a matrix with an infinity or NaN in u gives
- * NaN in its own set only.  `active` (device, [sets] uint8, or NULL = all): sets with active[s] == 0 keep W and m bit for
- * bit.  Weights that a call on this handle writes, all or some sets of a layer, O included, are noticed by this handle's
- * GNNCO_WEIGHTS_UNTOUCHED; calls on another handle and replays of a recorded graph are not.
+ * float64.  Products are float32 where the short side is at most 16 and the long one at most 256.  Elsewhere X, A
+ * and a I + b A + c A A are held as two float16 limbs between products (22 bits, fixed scales), with float32
+ * accumulation: float32 accuracy by norm, not by entry -- entries of X below 2^-39 (of a matrix that starts with norm
+ * 1) become zero, and rows far smaller than the rest keep fewer digits.  A zero gradient gives a zero X; a matrix with
+ * an infinity or NaN in u gives NaN in its own set only.  `active` (device, [sets] uint8, or NULL = all): sets with
+ * active[s] == 0 keep W and m bit for bit.  Weights that a call on this handle writes, all or some sets of a layer, O
+ * included, are noticed by this handle's GNNCO_WEIGHTS_UNTOUCHED; calls on another handle and replays of a recorded
+ * graph are not.
  * gnnco_orthogonalise: O = X after the steps, in G's orientation, for G and O [sets x rows x cols] in float32 or bfloat16
  * (lr, momentum, weight_decay and nesterov are not read; sets that are not active are not written; O may be G).
  * ws: gnnco_muon_workspace_bytes bytes, 256-byte aligned, NULL where that is 0.  Asynchronous on `stream`; results do not

@@ -779,7 +779,7 @@ class PartitionedGraph:
         if w_post is not None:
             dw_post = next(vectors)
             g.dw_post = dw_post.data_ptr()
-        # a work area of its own for every call: callers on other threads, and recorded graphs with their replays, must not share one
+        # a work area of its own for every call: callers on other threads and recorded graphs must not share one
         need = self._norm_sizes.get(F)
         if need is None:
             b = _sz(0)

@@ -26,10 +26,10 @@
 // first as soon as the products that read the first are done (they are issued first).
 //
 // What bounds it.  4,096 x 256 x 256 (6.2 PFLOP of float16 products, three per float32 one): 6.3 ms, the power cap
-// holding the clock at 1.7 GHz (592 x 256 x 256, too short for that: 861 us); the tensor pipe is active half of the time.  A step of a pair takes 27,700
-// cycles, 18,400 of them products: what is left are the conversions between them that nothing covers.  Loading and
-// storing a matrix takes 48,000 cycles; starting the pairs at different times did not change that.  1,024 x 128 x 128:
-// 251 us (235 where the same matrices are updated again and again, as far as they stay in L2).
+// holding the clock at 1.7 GHz (592 x 256 x 256, too short for that: 861 us); the tensor pipe is active half of the time.
+// A step of a pair takes 27,700 cycles, 18,400 of them products: what is left are the conversions between them that
+// nothing covers.  Loading and storing a matrix takes 48,000 cycles; starting the pairs at different times did not
+// change that.  1,024 x 128 x 128: 251 us (235 where the same matrices are updated again and again, as far as they stay in L2).
 //
 // Roles: after the working warps (16; 8 where two CTAs share an SM) one warp issues MMAs, and in a pair another
 // exchanges blocks; the working warps load, convert and store: warp w owns rows 32 (w % 4) .. +32 (its TMEM lanes) and

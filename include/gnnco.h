@@ -433,6 +433,25 @@ int32_t gnnco_block_norm_workspace_bytes(const gnnco_handle* h, int32_t F, size_
 int32_t gnnco_block_norm_backward(gnnco_handle* h, const gnnco_block_norm_desc* d, const gnnco_block_norm_grads* g, void* ws,
                                   size_t ws_bytes, void* stream);
 
+/* Dropout from a counter-based generator; the mask is never stored.
+ *   out[r,c] = x[r,c] / (1 - p) where word(r,c) >= p * 2^32 (rounded to a whole number), else 0
+ * word(r,c) is word c % 4 of Philox4x32-10 for the counter (r * ceil(F / 4) + c / 4 in 64 bits, step + *step_dev, layer) under
+ * the key `seed`: the same mask for every type, stride and launch.  The gradient of x is the same call on the gradient of
+ * out.  A dropped element is 0 whatever it was (NaN included); p = 0 keeps all, p = 1 none.
+ * step_dev (device, one uint32, or NULL) is read when the kernel runs, so that a recorded graph draws a new mask whenever the
+ * caller advances it; advance it after the backward pass, which has to see the forward pass's value.
+ * Rows are x_ld / out_ld elements apart; out may be x.  Any alignment works, 16-byte aligned rows are faster.  Asynchronous
+ * on `stream`. */
+typedef struct {
+  double p;                      /* probability of being dropped, in [0, 1] */
+  uint64_t seed;
+  uint32_t layer;                /* tells the masks of one step apart */
+  uint32_t step;
+  const uint32_t* step_dev;
+} gnnco_dropout_params;
+int32_t gnnco_dropout(gnnco_handle* h, int32_t feat_dtype, int64_t rows, int32_t F, const void* x, int64_t x_ld,
+                      const gnnco_dropout_params* d, void* out, int64_t out_ld, void* stream);
+
 /* Weight updates orthogonalised by Newton-Schulz products (an alternative to Adam for the weights of the hidden layers),
  * for `sets` matrices W [sets x rows x cols] at once:
  *   m = momentum * m + dW;   u = dW + momentum * m (nesterov != 0) or m

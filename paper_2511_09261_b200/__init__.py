@@ -31,6 +31,7 @@ EXPORTS = [
     "gnnco_louvain_workspace_bytes", "gnnco_louvain", "gnnco_embedding_lookup", "gnnco_embedding_plan_bytes",
     "gnnco_embedding_plan", "gnnco_embedding_grad", "gnnco_block_norm", "gnnco_block_norm_workspace_bytes",
     "gnnco_block_norm_backward", "gnnco_muon_workspace_bytes", "gnnco_muon_update", "gnnco_orthogonalise",
+    "gnnco_dropout",
 ]
 
 _vp, _i32, _i64, _u32, _f32, _sz = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_float,
@@ -83,6 +84,10 @@ class BlockNormGrads(ctypes.Structure):
 class MuonParams(ctypes.Structure):
     _fields_ = [("lr", _f32), ("momentum", _f32), ("weight_decay", _f32), ("nesterov", _i32), ("steps", _i32),
                 ("a", _f32), ("b", _f32), ("c", _f32), ("eps", _f32), ("active", _vp)]
+
+
+class DropoutParams(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("layer", _u32), ("step", _u32), ("step_dev", _vp)]
 
 
 class GnncoError(RuntimeError):
@@ -153,6 +158,7 @@ def load_library(build_if_missing: bool = True):
     lib.gnnco_muon_update.argtypes = [_vp, _i64, _i32, _i32, _vp, _vp, _vp, ctypes.POINTER(MuonParams), _vp, _sz, _vp]
     lib.gnnco_orthogonalise.argtypes = [_vp, _i32, _i32, _i64, _i32, _i32, _vp, _vp, ctypes.POINTER(MuonParams), _vp, _sz,
                                         _vp]
+    lib.gnnco_dropout.argtypes = [_vp, _i32, _i64, _i32, _vp, _i64, ctypes.POINTER(DropoutParams), _vp, _i64, _vp]
     for name in EXPORTS:
         if name not in ("gnnco_status_string", "gnnco_launch_count"):
             getattr(lib, name).restype = _i32
@@ -315,6 +321,27 @@ class EmbeddingPlan:
     def __init__(self, rows: int, V: int, F: int, ws, made_on: int):
         self.rows, self.V, self.F, self.ws = rows, V, F, ws
         self.made_on = made_on      # the stream that ws belongs to
+
+
+class Dropout:
+    """Which elements are dropped (``gnnco_dropout_params``): each with probability ``p``, decided by ``seed`` (64 bits),
+    ``layer`` and ``step``.  ``step`` is advanced by the caller, after the backward pass; ``step_dev`` (int32 device tensor
+    of one element, added to ``step``) is its form for recorded graphs."""
+
+    def __init__(self, p: float, seed: int, layer: int = 0, step: int = 0, step_dev=None):
+        self.p, self.seed, self.layer, self.step, self.step_dev = float(p), int(seed), int(layer), int(step), step_dev
+
+    def params(self, device) -> DropoutParams:
+        import torch
+        if not 0.0 <= self.p <= 1.0:
+            raise ValueError("p must be in [0, 1]")
+        if self.seed >> 64 or self.layer >> 32 or self.step >> 32:
+            raise ValueError("seed must fit in 64 bits, layer and step in 32, none below zero")
+        if self.step_dev is not None:
+            _require(self.step_dev, torch.int32, "step_dev")
+            if self.step_dev.numel() != 1 or self.step_dev.device != device:
+                raise ValueError("step_dev must be one int32 on %s" % device)
+        return DropoutParams(self.p, self.seed, self.layer, self.step, _dptr(self.step_dev))
 
 
 class PartitionedGraph:
@@ -790,6 +817,26 @@ class PartitionedGraph:
         _check(self._lib.gnnco_block_norm_backward(self._handle, ctypes.byref(d), ctypes.byref(g), ws.data_ptr(), need,
                                                    _stream_ptr(stream)), "gnnco_block_norm_backward")
         return dict(dx=dx, dy=dy, dgate=dgate, dw_pre=dw_pre, dw_post=dw_post)
+
+    def dropout(self, x, drop: Dropout, out=None, stream=None):
+        """``gnnco_dropout``: ``x`` [rows, F] with the elements that ``drop`` names set to 0 and the others scaled by
+        1 / (1 - p).  Its gradient is the same call on the gradient."""
+        dt = _feat_code(x, "x")
+        if x.dim() != 2 or x.shape[1] < 1:
+            raise ValueError("x must be [rows, F]")
+        rows, F = x.shape
+        if F >> 31:
+            _int32(F)
+        d = drop.params(self.device)
+        x_ld = self._rows(x, x.dtype, rows, F, "x")
+        out_ld = F
+        if out is None:
+            out = _empty((rows, F), x.dtype, x, stream)
+        else:
+            out_ld = self._rows(out, x.dtype, rows, F, "out")
+        _check(self._lib.gnnco_dropout(self._handle, dt, rows, F, x.data_ptr(), x_ld, ctypes.byref(d), out.data_ptr(), out_ld,
+                                       _stream_ptr(stream)), "gnnco_dropout")
+        return out
 
     def _muon_call(self, like, steps, active, stream, ws):
         import torch

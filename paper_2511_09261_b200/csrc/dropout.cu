@@ -1,0 +1,174 @@
+// Dropout without a stored mask:  out[r,c] = x[r,c] / (1 - p) where word(r,c) >= p 2^32, else 0  (words: philox.cuh).
+// The mask is a function of (seed, layer, step, r, c), so the gradient is the same call on the gradient of out.
+//
+// A thread takes UNROLL vectors of 16 bytes a block's width apart (loads first, then the words, then the stores).  Elements whose
+// word falls below the limit are set to 0 by selection, not by a product: an infinity or NaN that is dropped is gone.
+// A quad takes 17 wide products and their logic on the integer pipes, a quarter of that per element: in bfloat16 (4 bytes
+// moved per element) that is about what the memory takes, in float32 half of it.
+#include <math.h>
+
+#include "internal.cuh"
+#include "mask.cuh"
+#include "philox.cuh"
+#include "vec_io.cuh"
+
+namespace {
+
+struct DropArgs {
+  const void* x;
+  void* out;
+  int64_t x_ld, out_ld, rows;
+  int32_t F;
+  int32_t groups;                                          // groups of G columns in a row
+  philox::Mask m;
+};
+
+__device__ __forceinline__ float pick(uint32_t word, const philox::Mask& m, float v) {
+  return m.all || word > m.lim ? v * m.scale : 0.0f;
+}
+
+// VEC consecutive, aligned elements (4 or 8: whole quads; F is a multiple of VEC).  flat: the rows are one run of elements.
+template <typename T, int VEC, int UNROLL, bool FLAT>
+__global__ void __launch_bounds__(256) drop_vectors(const DropArgs A) {
+  const int64_t items = A.rows * A.groups;
+  philox::Stream words(A.m);
+  for (int64_t base = (int64_t)blockIdx.x * (256 * UNROLL); base < items; base += (int64_t)gridDim.x * (256 * UNROLL)) {
+    const int64_t row0 = FLAT ? 0 : base / A.groups;
+    const uint32_t rest = FLAT ? 0u : (uint32_t)(base - row0 * A.groups);
+    vio::Raw<T, VEC> v[UNROLL];
+    int64_t to[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      const int64_t i = base + u * 256 + threadIdx.x;
+      if (i >= items) break;
+      int64_t from;
+      if (FLAT) {
+        from = to[u] = i * VEC;
+      } else {
+        const uint32_t off = rest + u * 256 + threadIdx.x, r = off / (uint32_t)A.groups, c = off - r * (uint32_t)A.groups;
+        from = (row0 + r) * A.x_ld + (int64_t)c * VEC;
+        to[u] = (row0 + r) * A.out_ld + (int64_t)c * VEC;
+      }
+      v[u].template load<true>(static_cast<const T*>(A.x) + from);
+    }
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      const int64_t i = base + u * 256 + threadIdx.x;
+      if (i >= items) break;
+      float f[VEC];
+#pragma unroll
+      for (int k = 0; k < VEC; k += 4) {
+        // F is a multiple of 4: quads are numbered along the run of groups
+        const uint4 w = words.quad((uint64_t)i * (VEC / 4) + k / 4);
+        f[k] = pick(w.x, A.m, v[u].get(k));
+        f[k + 1] = pick(w.y, A.m, v[u].get(k + 1));
+        f[k + 2] = pick(w.z, A.m, v[u].get(k + 2));
+        f[k + 3] = pick(w.w, A.m, v[u].get(k + 3));
+      }
+      vio::store_stream<T, VEC>(static_cast<T*>(A.out) + to[u], f);
+    }
+  }
+}
+
+// any width and alignment: a quad of columns per thread, element by element
+template <typename T>
+__global__ void __launch_bounds__(256) drop_quads(const DropArgs A) {
+  const int64_t items = A.rows * A.groups;
+  philox::Stream words(A.m);
+  for (int64_t base = (int64_t)blockIdx.x * 256; base < items; base += (int64_t)gridDim.x * 256) {
+    const int64_t row0 = base / A.groups, i = base + threadIdx.x;
+    if (i >= items) break;
+    const uint32_t off = (uint32_t)(base - row0 * A.groups) + threadIdx.x, r = off / (uint32_t)A.groups;
+    const int c = (int)(off - r * (uint32_t)A.groups) * 4, count = min(4, A.F - c);
+    const T* from = static_cast<const T*>(A.x) + (row0 + r) * A.x_ld + c;
+    T* to = static_cast<T*>(A.out) + (row0 + r) * A.out_ld + c;
+    vio::Raw<T, 1> v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < count) v[k].template load<true>(from + k);
+    const uint4 w = words.quad((uint64_t)i);
+    const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < count) {
+        const float f[1] = {pick(word[k], A.m, v[k].get(0))};
+        vio::store_stream<T, 1>(to + k, f);
+      }
+  }
+}
+
+template <typename T>
+void launch_drop(gnnco_handle* h, DropArgs A, cudaStream_t st) {
+  constexpr int kVec = 16 / (int)sizeof(T), kUnroll = 4;
+  auto fits = [&](int vec) {
+    const uintptr_t bytes = (uintptr_t)vec * sizeof(T);
+    return A.F % vec == 0 && (((uintptr_t)A.x | (uintptr_t)A.out | (uintptr_t)(A.x_ld * (int64_t)sizeof(T)) |
+                               (uintptr_t)(A.out_ld * (int64_t)sizeof(T))) % bytes) == 0;
+  };
+  const bool flat = A.x_ld == A.F && A.out_ld == A.F;
+  const int64_t most = (int64_t)h->sm_count * 8;           // eight blocks of 256 threads fill an SM
+  auto blocks = [&](int64_t per) {
+    const int64_t need = (A.rows * A.groups + per - 1) / per;
+    return (unsigned)(need < most ? need : most);
+  };
+  if (fits(kVec)) {
+    A.groups = A.F / kVec;
+    if (flat) drop_vectors<T, kVec, kUnroll, true><<<blocks(256 * kUnroll), 256, 0, st>>>(A);
+    else drop_vectors<T, kVec, kUnroll, false><<<blocks(256 * kUnroll), 256, 0, st>>>(A);
+    return;
+  }
+  if constexpr (kVec == 8) {
+    if (fits(4)) {
+      A.groups = A.F / 4;
+      if (flat) drop_vectors<T, 4, kUnroll, true><<<blocks(256 * kUnroll), 256, 0, st>>>(A);
+      else drop_vectors<T, 4, kUnroll, false><<<blocks(256 * kUnroll), 256, 0, st>>>(A);
+      return;
+    }
+  }
+  A.groups = (A.F + 3) / 4;
+  drop_quads<T><<<blocks(256), 256, 0, st>>>(A);
+}
+
+}  // namespace
+
+// The mask of a launch; false: p outside [0, 1].
+bool make_mask(const gnnco_dropout_params* d, philox::Mask* m) {
+  if (!(d->p >= 0.0 && d->p <= 1.0)) return false;
+  const double limit = nearbyint(d->p * 4294967296.0);     // ties to even, as everywhere
+  m->seed_lo = (uint32_t)d->seed;
+  m->seed_hi = (uint32_t)(d->seed >> 32);
+  m->step = d->step;
+  m->layer = d->layer;
+  m->step_dev = d->step_dev;
+  m->all = limit < 1.0;
+  m->lim = m->all ? 0u : (uint32_t)(limit - 1.0);
+  m->scale = d->p < 1.0 ? (float)(1.0 / (1.0 - d->p)) : 0.0f;   // p = 1 keeps nothing
+  return true;
+}
+
+bool on_own_device(const gnnco_handle* h) {
+  int device = -1;
+  return cudaGetDevice(&device) == cudaSuccess && device == h->device;
+}
+
+void run_dropout(gnnco_handle* h, int32_t dtype, int64_t rows, int32_t F, const void* x, int64_t x_ld, const philox::Mask& m,
+                 void* out, int64_t out_ld, cudaStream_t st) {
+  DropArgs A = {x, out, x_ld, out_ld, rows, F, 0, m};
+  if (dtype == GNNCO_F32) launch_drop<float>(h, A, st);
+  else launch_drop<__nv_bfloat16>(h, A, st);
+  h->launches += 1;
+}
+
+extern "C" int32_t gnnco_dropout(gnnco_handle* h, int32_t feat_dtype, int64_t rows, int32_t F, const void* x, int64_t x_ld,
+                                 const gnnco_dropout_params* d, void* out, int64_t out_ld, void* stream) {
+  philox::Mask m;
+  if (!h || !d || rows < 0 || F < 1 || !make_mask(d, &m)) return GNNCO_INVALID_ARGUMENT;
+  if (feat_dtype != GNNCO_F32 && feat_dtype != GNNCO_BF16) return GNNCO_UNSUPPORTED;
+  if (rows == 0) return GNNCO_OK;
+  if (!x || !out || x_ld < F || out_ld < F || rows > ((int64_t)1 << 62) / F || !on_own_device(h)) return GNNCO_INVALID_ARGUMENT;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  ProfScope prof_(h, K_DROPOUT, st);
+  run_dropout(h, feat_dtype, rows, F, x, x_ld, m, out, out_ld, st);
+  GNNCO_LAUNCH_CHECK();
+  return GNNCO_OK;
+}

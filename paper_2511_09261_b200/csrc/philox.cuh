@@ -1,0 +1,65 @@
+// The counter-based generator Philox4x32-10 (Salmon, Moraes, Dror, Shaw: "Parallel random numbers: as easy as 1, 2, 3",
+// SC 2011): four 32-bit words as a function of a 128-bit counter and a 64-bit key, with nothing carried from one
+// counter to the next.  Dropout masks are words compared with p 2^32: element (r, c) of a [rows x F] tensor takes word
+// c % 4 of counter (r * ceil(F / 4) + c / 4, step, layer), so a mask depends neither on the type nor on the strides of the
+// tensor nor on which thread asks, and the backward pass draws it again instead of reading it.
+#pragma once
+
+#include <stdint.h>
+
+namespace philox {
+
+constexpr uint32_t kMul0 = 0xD2511F53u, kMul1 = 0xCD9E8D57u, kWeyl0 = 0x9E3779B9u, kWeyl1 = 0xBB67AE85u;
+
+// What a launch passes down.  lim = p 2^32 - 1 in 32 bits: an element is kept if its word is above it; all: p 2^32 < 1.
+struct Mask {
+  uint32_t seed_lo, seed_hi, step, layer, lim;
+  uint32_t all;
+  float scale;                        // 1 / (1 - p)
+  const uint32_t* step_dev;           // added to step where given
+};
+
+// The part of the rounds that all counters of a launch share: the second product of round 1, and, while the upper half of the
+// number of the quad stays the same, the first product of round 2 (17 products a quad instead of 20).
+struct Stream {
+  uint32_t seed_lo, seed_hi, layer, hi1, lo1;
+  uint32_t last_hi, hi2, lo2;
+  __device__ __forceinline__ explicit Stream(const Mask& m) {
+    const uint32_t step = m.step + (m.step_dev ? *m.step_dev : 0u);
+    seed_lo = m.seed_lo; seed_hi = m.seed_hi; layer = m.layer;
+    hi1 = __umulhi(kMul1, step);
+    lo1 = kMul1 * step;
+    upper(0u);
+  }
+  __device__ __forceinline__ void upper(uint32_t q_hi) {
+    last_hi = q_hi;
+    const uint32_t x0 = hi1 ^ q_hi ^ seed_lo;
+    hi2 = __umulhi(kMul0, x0);
+    lo2 = kMul0 * x0;
+  }
+  __device__ __forceinline__ uint4 quad(uint64_t q) {
+    if ((uint32_t)(q >> 32) != last_hi) upper((uint32_t)(q >> 32));
+    uint32_t k0 = seed_lo, k1 = seed_hi;
+    const uint64_t a = (uint64_t)kMul0 * (uint32_t)q;
+    uint32_t x1 = lo1, x2 = (uint32_t)(a >> 32) ^ layer ^ k1, x3 = (uint32_t)a, x0;
+    // round 2
+    k0 += kWeyl0; k1 += kWeyl1;
+    const uint64_t b = (uint64_t)kMul1 * x2;
+    x0 = (uint32_t)(b >> 32) ^ x1 ^ k0;
+    x2 = hi2 ^ x3 ^ k1;
+    x1 = (uint32_t)b;
+    x3 = lo2;
+#pragma unroll
+    for (int round = 2; round < 10; ++round) {
+      k0 += kWeyl0; k1 += kWeyl1;
+      const uint64_t u = (uint64_t)kMul0 * x0, v = (uint64_t)kMul1 * x2;
+      x0 = (uint32_t)(v >> 32) ^ x1 ^ k0;
+      x2 = (uint32_t)(u >> 32) ^ x3 ^ k1;
+      x1 = (uint32_t)v;
+      x3 = (uint32_t)u;
+    }
+    return make_uint4(x0, x1, x2, x3);
+  }
+};
+
+}  // namespace philox

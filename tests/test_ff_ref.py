@@ -1,0 +1,108 @@
+"""The float64 restatements of dropout and the gated feed-forward block, checked by themselves: published generator vectors,
+moments of the mask, differences of the gradients.  And what the binding of dropout refuses, without a GPU."""
+import numpy as np
+import pytest
+import torch
+
+import ff_ref as ref
+import paper_2511_09261_b200 as gnnco
+from test_operator_calls import _Library
+
+
+# known answers of Philox4x32-10 from the generator's authors
+VECTORS = [
+    ((0, 0, 0, 0), (0, 0), (0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8)),
+    ((0xFFFFFFFF,) * 4, (0xFFFFFFFF,) * 2, (0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD)),
+    ((0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344), (0xA4093822, 0x299F31D0), (0xD16CFE09, 0x94FDCCEB, 0x5001E420, 0x24126EA1)),
+]
+
+
+@pytest.mark.parametrize("counter,key,want", VECTORS)
+def test_philox_known_answers(counter, key, want):
+    got = ref.philox(np.array([counter], dtype=np.uint64), key)
+    assert tuple(int(v) for v in got[0]) == want
+
+
+def test_masks_keep_the_right_share_and_differ():
+    a = ref.keep(400, 250, 0.3, seed=5)
+    # 100,000 independent draws: five standard deviations are 0.0073
+    assert abs(a.mean() - 0.7) < 0.0073
+    for other in (ref.keep(400, 250, 0.3, seed=6), ref.keep(400, 250, 0.3, 5, layer=1), ref.keep(400, 250, 0.3, 5, step=1),
+                  ref.keep(400, 250, 0.3, 5 + (1 << 32))):
+        # independent masks agree with probability 0.58
+        assert abs((a == other).mean() - 0.58) < 0.0079
+    assert np.array_equal(ref.keep(10, 250, 0.3, 5, row0=390), a[390:])
+    assert ref.keep(3, 5, 0.0, 5).all() and not ref.keep(3, 5, 1.0, 5).any()
+
+
+@pytest.mark.parametrize("name", ["silu", "gelu", "relu"])
+def test_block_gradients_against_differences(name):
+    r = np.random.RandomState(3)
+    ptr, F, H = [0, 4, 4, 7], 5, 6
+    x, dy = r.standard_normal((7, F)), r.standard_normal((7, 4))
+    w = [r.standard_normal(s) for s in ((3, F, H), (3, F, H), (3, H, 4))]
+    mask = ref.keep(7, 4, 0.4, 9) / 0.6
+    d = ref.gated_ff_backward(x, dy, *w, ptr, name, mask)
+
+    def loss():
+        return float((ref.gated_ff(x, *w, ptr, name, mask)[0] * dy).sum())
+
+    for t, key in [(x, "dx"), (w[0], "dw_gate"), (w[1], "dw_up"), (w[2], "dw_down")]:
+        got = np.zeros_like(t)
+        for i in np.ndindex(t.shape):
+            keep, eps = t[i], 1e-6
+            t[i] = keep + eps
+            up = loss()
+            t[i] = keep - eps
+            got[i] = (up - loss()) / (2 * eps)
+            t[i] = keep
+        np.testing.assert_allclose(got, d[key], rtol=2e-6, atol=2e-8)
+        assert np.all(d[key + "_mag"] * (1 + 1e-12) >= np.abs(d[key]))
+
+
+@pytest.fixture
+def graph(monkeypatch):
+    g = gnnco.PartitionedGraph.__new__(gnnco.PartitionedGraph)
+    g._lib, g._handle, g.device = _Library(), None, torch.device("cpu")
+    monkeypatch.setattr(gnnco, "_stream_ptr", lambda stream=None: 0)
+    return g
+
+
+@pytest.mark.parametrize("drop", [
+    gnnco.Dropout(-0.1, 1), gnnco.Dropout(1.5, 1), gnnco.Dropout(float("nan"), 1), gnnco.Dropout(0.1, 1 << 64),
+    gnnco.Dropout(0.1, -1), gnnco.Dropout(0.1, 1, layer=1 << 32), gnnco.Dropout(0.1, 1, step=-1),
+])
+def test_dropout_refuses_what_the_generator_cannot_take(graph, drop):
+    with pytest.raises(ValueError):
+        graph.dropout(torch.ones(3, 4), drop)
+    assert not graph._lib.calls
+
+
+def test_dropout_refuses_other_shapes_types_and_devices(graph):
+    drop, x = gnnco.Dropout(0.1, 1), torch.ones(6, 4)
+    for bad in (torch.ones(4), torch.ones(2, 3, 4), torch.ones(3, 0)):
+        with pytest.raises(ValueError):
+            graph.dropout(bad, drop)
+    for bad in (x.double(), x.half(), x.int()):
+        with pytest.raises(TypeError):
+            graph.dropout(bad, drop)
+    for bad in (x.t(), x[:, ::2], x[:1].expand(6, 4)):
+        with pytest.raises(ValueError):
+            graph.dropout(bad, drop)
+    for bad in (torch.empty(6, 5), torch.empty(5, 4)):
+        with pytest.raises(ValueError):
+            graph.dropout(x, drop, out=bad)
+    with pytest.raises(TypeError):
+        graph.dropout(x, drop, out=torch.empty(6, 4, dtype=torch.bfloat16))
+    with pytest.raises(TypeError):
+        graph.dropout(x, gnnco.Dropout(0.1, 1, step_dev=torch.zeros(1, dtype=torch.int64)))
+    assert not graph._lib.calls
+    graph.dropout(x[:, 1:3], drop)
+    assert graph._lib.last("gnnco_dropout")[5] == 4
+
+
+def test_the_c_entry_checks_its_arguments_without_a_gpu():
+    import ctypes
+    lib = gnnco.load_library()
+    d = gnnco.DropoutParams(0.5, 1, 0, 0, None)
+    assert lib.gnnco_dropout(None, 0, 1, 1, None, 1, ctypes.byref(d), None, 1, None) == gnnco.INVALID_ARGUMENT

@@ -452,6 +452,46 @@ typedef struct {
 int32_t gnnco_dropout(gnnco_handle* h, int32_t feat_dtype, int64_t rows, int32_t F, const void* x, int64_t x_ld,
                       const gnnco_dropout_params* d, void* out, int64_t out_ld, void* stream);
 
+/* The gated feed-forward block of a residual step, for the rows of every subgraph s (or of one set of weights for all rows):
+ *   y = drop( (act(x Wg_s) .* (x Wu_s)) Wd_s )          Wg, Wu [sets x F x H], Wd [sets x H x F_out]
+ * It stands between gnnco_block_norm's h_out (x here) and its y.  sets == 1: one set for any number of rows;
+ * sets == S: set s for the rows of subgraph s, rows == n, rows in the library's new order.  act: SiLU a = g / (1 + exp(-g)),
+ * GELU a = g (1 + erf(g / sqrt 2)) / 2, or the rectifier (derivative 0 at 0).  drop == NULL: none; else the mask of
+ * gnnco_dropout on [rows x F_out].
+ * feat_dtype: x, y, dy, dx.  w_dtype: GNNCO_F32, or GNNCO_BF16 with bfloat16 features; contiguous.  float32 features are
+ * multiplied as three bfloat16 limbs (24 bits, float32 sums); finite values of magnitude below 2^-110 lose bits there, and
+ * above 3.38e38 become infinite.  In bfloat16 features h, dg and du are rounded to bfloat16 once, float32 weights too.
+ * A row with an infinity or NaN spoils its own results and, in the backward pass, its subgraph's weight gradients.
+ * gnnco_gated_ff_backward: dy -> dx [rows x F] (or NULL) and the weight gradients (all three or none; dw_dtype as asked, like the
+ * weights in shape); d as in the forward call, whose g, u and h it computes again.  Sums over rows are taken in a
+ * fixed order.  A subgraph without rows gets zero gradients.
+ * x_ld, y_ld, dy_ld, dx_ld: elements between rows.  Any alignment works; 16-byte aligned rows and weights (widths that are
+ * multiples of 8 in bfloat16) spare a copy.  dx may be x or dy, and y may be x.  ws: gnnco_gated_ff_workspace_bytes bytes for the same d (its
+ * pointers included), 256-byte aligned, not shared by calls that may overlap.  rows < 2^31 - 256, widths <= 65536.
+ * Asynchronous on `stream`. */
+typedef enum { GNNCO_SILU = 0, GNNCO_GELU = 1, GNNCO_RELU = 2 } gnnco_activation;
+typedef struct {
+  int64_t rows;
+  int32_t F, H, F_out;
+  int32_t feat_dtype, w_dtype;   /* gnnco_dtype */
+  int32_t sets;
+  int32_t act;                   /* gnnco_activation */
+  const void* x;
+  int64_t x_ld;
+  const void *w_gate, *w_up, *w_down;
+  const gnnco_dropout_params* drop;  /* host pointer, or NULL */
+} gnnco_gated_ff_desc;
+typedef struct {
+  void* dx;
+  int64_t dx_ld;
+  void *dw_gate, *dw_up, *dw_down;
+  int32_t dw_dtype;
+} gnnco_gated_ff_grads;
+int32_t gnnco_gated_ff_workspace_bytes(const gnnco_handle* h, const gnnco_gated_ff_desc* d, int32_t backward, size_t* bytes);
+int32_t gnnco_gated_ff(gnnco_handle* h, const gnnco_gated_ff_desc* d, void* y, int64_t y_ld, void* ws, size_t ws_bytes, void* stream);
+int32_t gnnco_gated_ff_backward(gnnco_handle* h, const gnnco_gated_ff_desc* d, const void* dy, int64_t dy_ld,
+                                const gnnco_gated_ff_grads* g, void* ws, size_t ws_bytes, void* stream);
+
 /* Weight updates orthogonalised by Newton-Schulz products (an alternative to Adam for the weights of the hidden layers),
  * for `sets` matrices W [sets x rows x cols] at once:
  *   m = momentum * m + dW;   u = dW + momentum * m (nesterov != 0) or m

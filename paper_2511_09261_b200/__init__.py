@@ -31,7 +31,7 @@ EXPORTS = [
     "gnnco_louvain_workspace_bytes", "gnnco_louvain", "gnnco_embedding_lookup", "gnnco_embedding_plan_bytes",
     "gnnco_embedding_plan", "gnnco_embedding_grad", "gnnco_block_norm", "gnnco_block_norm_workspace_bytes",
     "gnnco_block_norm_backward", "gnnco_muon_workspace_bytes", "gnnco_muon_update", "gnnco_orthogonalise",
-    "gnnco_dropout",
+    "gnnco_dropout", "gnnco_gated_ff_workspace_bytes", "gnnco_gated_ff", "gnnco_gated_ff_backward",
 ]
 
 _vp, _i32, _i64, _u32, _f32, _sz = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_float,
@@ -88,6 +88,16 @@ class MuonParams(ctypes.Structure):
 
 class DropoutParams(ctypes.Structure):
     _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("layer", _u32), ("step", _u32), ("step_dev", _vp)]
+
+
+class GatedFfDesc(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("F", _i32), ("H", _i32), ("F_out", _i32), ("feat_dtype", _i32), ("w_dtype", _i32),
+                ("sets", _i32), ("act", _i32), ("x", _vp), ("x_ld", _i64), ("w_gate", _vp), ("w_up", _vp),
+                ("w_down", _vp), ("drop", ctypes.POINTER(DropoutParams))]
+
+
+class GatedFfGrads(ctypes.Structure):
+    _fields_ = [("dx", _vp), ("dx_ld", _i64), ("dw_gate", _vp), ("dw_up", _vp), ("dw_down", _vp), ("dw_dtype", _i32)]
 
 
 class GnncoError(RuntimeError):
@@ -159,6 +169,10 @@ def load_library(build_if_missing: bool = True):
     lib.gnnco_orthogonalise.argtypes = [_vp, _i32, _i32, _i64, _i32, _i32, _vp, _vp, ctypes.POINTER(MuonParams), _vp, _sz,
                                         _vp]
     lib.gnnco_dropout.argtypes = [_vp, _i32, _i64, _i32, _vp, _i64, ctypes.POINTER(DropoutParams), _vp, _i64, _vp]
+    lib.gnnco_gated_ff_workspace_bytes.argtypes = [_vp, ctypes.POINTER(GatedFfDesc), _i32, ctypes.POINTER(_sz)]
+    lib.gnnco_gated_ff.argtypes = [_vp, ctypes.POINTER(GatedFfDesc), _vp, _i64, _vp, _sz, _vp]
+    lib.gnnco_gated_ff_backward.argtypes = [_vp, ctypes.POINTER(GatedFfDesc), _vp, _i64, ctypes.POINTER(GatedFfGrads),
+                                            _vp, _sz, _vp]
     for name in EXPORTS:
         if name not in ("gnnco_status_string", "gnnco_launch_count"):
             getattr(lib, name).restype = _i32
@@ -237,6 +251,7 @@ def _empty(shape, dtype, like, stream):
         return like.new_empty(shape, dtype=dtype)
 
 
+ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
 MUON_COEFS = (3.4445, -4.7750, 2.0315)
 
 
@@ -633,7 +648,7 @@ class PartitionedGraph:
         if r != rows or f != F:
             raise ValueError("%s must be [%d, %d]" % (what, rows, F))
         ld, step = t.stride()
-        if f > 1 and step != 1 or r > 1 and ld < f:
+        if r and f > 1 and step != 1 or r > 1 and ld < f:       # (without rows the strides mean nothing)
             raise ValueError("%s must have rows of consecutive elements that do not overlap" % what)
         return ld if r > 1 else max(f, 1)
 
@@ -837,6 +852,87 @@ class PartitionedGraph:
         _check(self._lib.gnnco_dropout(self._handle, dt, rows, F, x.data_ptr(), x_ld, ctypes.byref(d), out.data_ptr(), out_ld,
                                        _stream_ptr(stream)), "gnnco_dropout")
         return out
+
+    def _gated_ff_desc(self, x, w_gate, w_up, w_down, act, drop):
+        xd, wd = _feat_code(x, "x"), _feat_code(w_gate, "w_gate")
+        if x.dim() != 2 or x.shape[1] < 1:
+            raise ValueError("x must be [rows, F]")
+        for w, what in ((w_gate, "w_gate"), (w_up, "w_up"), (w_down, "w_down")):
+            _require(w, w_gate.dtype, what)
+            if w.dim() != 3 or 0 in w.shape or w.device != self.device:
+                raise ValueError("%s must be [sets, rows, columns] on %s" % (what, self.device))
+        rows, F = x.shape
+        sets, _, H = w_gate.shape
+        F_out = w_down.shape[2]
+        if w_gate.shape != (sets, F, H) or w_up.shape != (sets, F, H) or w_down.shape != (sets, H, F_out):
+            raise ValueError("x [rows, F] takes w_gate and w_up [sets, F, H] and w_down [sets, H, F_out]")
+        if sets != 1 and (sets != self.S or rows != self.n):
+            raise ValueError("weights of %d sets need the %d rows of %d subgraphs" % (sets, self.n, self.S))
+        if act not in ACTIVATIONS:
+            raise ValueError("act must be one of %s" % ", ".join(ACTIVATIONS))
+        if (F | H | F_out) >> 31:
+            _int32(F, H, F_out)
+        d = GatedFfDesc(rows, F, H, F_out, xd, wd, sets, ACTIVATIONS[act], x.data_ptr(),
+                        self._rows(x, x.dtype, rows, F, "x"), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr())
+        if drop is not None:
+            d.drop = ctypes.pointer(drop.params(self.device))
+        return d
+
+    def _gated_ff_area(self, d, backward, like, ws, stream):
+        import torch
+        need = _sz(0)
+        _check(self._lib.gnnco_gated_ff_workspace_bytes(self._handle, ctypes.byref(d), backward, ctypes.byref(need)),
+               "gnnco_gated_ff_workspace_bytes")
+        if ws is None:
+            return _empty((need.value,), torch.uint8, like, stream)
+        _require(ws, torch.uint8, "ws")
+        if ws.device != self.device:
+            raise ValueError("ws must be on %s" % self.device)
+        return ws
+
+    def gated_ff(self, x, w_gate, w_up, w_down, act: str = "silu", drop: Optional[Dropout] = None, out=None, ws=None,
+                 stream=None):
+        """``gnnco_gated_ff``: drop((act(x Wg) * (x Wu)) Wd) for ``x`` [rows, F], ``w_gate`` and ``w_up`` [sets, F, H] and
+        ``w_down`` [sets, H, F_out], one set for all rows or one per subgraph.  The weights have x's type or are float32.
+        ``ws`` may be a uint8 tensor kept between calls that follow each other on one stream."""
+        d = self._gated_ff_desc(x, w_gate, w_up, w_down, act, drop)
+        shape, y_ld = (d.rows, d.F_out), d.F_out
+        if out is None:
+            out = _empty(shape, x.dtype, x, stream)
+        else:
+            y_ld = self._rows(out, x.dtype, *shape, "out")
+        ws = self._gated_ff_area(d, 0, x, ws, stream)
+        _check(self._lib.gnnco_gated_ff(self._handle, ctypes.byref(d), out.data_ptr(), y_ld, ws.data_ptr(), ws.numel(),
+                                        _stream_ptr(stream)), "gnnco_gated_ff")
+        return out
+
+    def gated_ff_backward(self, x, dy, w_gate, w_up, w_down, act: str = "silu", drop: Optional[Dropout] = None,
+                          want_dx: bool = True, want_dw: bool = True, dw_dtype=None, dx=None, ws=None, stream=None):
+        """``gnnco_gated_ff_backward``: gradients of ``gated_ff`` for the gradient ``dy`` [rows, F_out] of its result, from the
+        same ``x`` (nothing else is kept from the forward call), as dict(dx, dw_gate, dw_up, dw_down); None for what is not
+        wanted.  The weights' gradients have the weights' type unless ``dw_dtype`` says otherwise."""
+        d = self._gated_ff_desc(x, w_gate, w_up, w_down, act, drop)
+        dy_ld = self._rows(dy, x.dtype, d.rows, d.F_out, "dy")
+        if not (want_dx or want_dw) or dx is not None and not want_dx:
+            raise ValueError("nothing is wanted, or dx is given and not wanted")
+        g = GatedFfGrads()
+        if want_dx:
+            if dx is None:
+                dx = _empty((d.rows, d.F), x.dtype, x, stream)
+            g.dx, g.dx_ld = dx.data_ptr(), self._rows(dx, x.dtype, d.rows, d.F, "dx")
+        dws = [None, None, None]
+        if want_dw:
+            dw_dtype = dw_dtype or w_gate.dtype
+            if dw_dtype not in _feat_codes:
+                raise TypeError("dw_dtype must be float32 or bfloat16")
+            dws = [_empty(tuple(w.shape), dw_dtype, x, stream) for w in (w_gate, w_up, w_down)]
+            g.dw_gate, g.dw_up, g.dw_down = (t.data_ptr() for t in dws)
+            g.dw_dtype = _feat_codes[dw_dtype]
+        ws = self._gated_ff_area(d, 1, x, ws, stream)
+        _check(self._lib.gnnco_gated_ff_backward(self._handle, ctypes.byref(d), dy.data_ptr(), dy_ld, ctypes.byref(g),
+                                                 ws.data_ptr(), ws.numel(), _stream_ptr(stream)),
+               "gnnco_gated_ff_backward")
+        return dict(dx=dx, dw_gate=dws[0], dw_up=dws[1], dw_down=dws[2])
 
     def _muon_call(self, like, steps, active, stream, ws):
         import torch

@@ -1,0 +1,600 @@
+// The tiled tensor-core products of the gated feed-forward block (kinds and formulas: gated_ff.cuh).
+//
+// One persistent CTA per SM, or a cluster of two CTAs that share a tile of 256 rows (tcgen05 .cta_group::2: each CTA stages its
+// own 128 rows of A and half of B).  Roles of the ten warps:
+//   warps 0-7   results: TMEM lanes 32 (w % 4) .., every other group of 32 columns from w / 4 on
+//   warp 8      issues the MMAs (in a pair, the even CTA's)
+//   warp 9      issues the TMA copies of this CTA's operands
+// A stage of the ring holds 64 of the contraction: A in the first half, B behind it, each as LIMBS matrices of bfloat16.  Operands
+// whose contraction runs along memory (x, dy, h, dg, du as A; Wd, Wg, Wu in the backward products) are k-major boxes of 64
+// columns, the others (the weights of the forward products, everything in the weight gradients) n-major boxes of 64 x 64:
+// no operand is ever transposed in memory.  Columns past an operand's end are filled with zeros by the copies.  Rows past a
+// subgraph's end belong to the next one: their results are not stored, and where rows are what is summed (kWeights) the copying
+// warp sets them to zero in shared memory before it announces the stage.
+//
+// LIMBS = 1 (bfloat16): a tile's products are summed in one of two TMEM buffers of 256 columns, so that the next tile is multiplied
+// while this one is converted and stored.
+// LIMBS = 3 (float32): a = a1 + a2 + a3 in bfloat16; the six products a_i b_j with i + j <= 4 are summed, what is left out is
+// below 2^-24 of the product.  The tensor core cuts off low bits whenever it adds to an accumulator, so sums stay short:
+// every stage starts an accumulator of its own (buffers in turn), adds the five small products first and the large one last, and the
+// result warps add the stages up in float32 registers, rounded to nearest.
+//
+// Every wait has a limit; a CTA that gives up raises the handle's status word, skips its work and leaves.
+#pragma once
+
+#include "gated_ff.cuh"
+#include "tc_common.cuh"
+#include "vec_io.cuh"
+
+namespace ff {
+
+constexpr int kEpiWarps = 8, kMmaWarp = 8, kCopyWarp = 9, kThreads = 320;
+constexpr uint32_t kRing = 196608;                         // 6 stages of 32 KB or 2 of 96 KB
+constexpr uint32_t kStagePitch = 33;                       // words between rows of a result warp's 32 x 32 staging tile
+constexpr uint32_t kStageBytes = 32 * kStagePitch * 4;
+constexpr uint32_t kSmem = 1024 + kRing + kEpiWarps * kStageBytes + 256;
+constexpr uint32_t kBuf = 256;                             // TMEM columns of an accumulator buffer
+static_assert(kSmem <= 232448, "fits one SM");
+
+// ------------------------------------------------------------------------------------- small pieces
+template <bool PAIR>
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, int32_t z, uint32_t bar) {
+  if constexpr (PAIR)
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+template <bool PAIR>
+__device__ __forceinline__ void load_box_of_set(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, int32_t set, uint32_t bar) {
+  if constexpr (PAIR)
+    asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(set), "r"(0), "r"(bar) : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(set), "r"(0), "r"(bar) : "memory");
+}
+// `acquire` at cluster scope: what the other CTA wrote before its arrival is seen
+__device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
+  if (tc::mbar_try_wait_cluster(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!tc::mbar_try_wait_cluster(bar, parity)) {
+    if (*abort_flag) return false;
+    if (clock64() - t0 > 4000000000ll) {
+      *abort_flag = 1;
+      return false;
+    }
+  }
+  return true;
+}
+__device__ __forceinline__ void store32(void* p, const uint32_t (&w)[8]) {   // 32-byte aligned
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+// 32 float32 of a row -> LIMBS bfloat16 rows; columns [0, 32) of them that lie below `width` (a multiple of 16)
+template <int LIMBS>
+__device__ __forceinline__ void store_limbs(__nv_bfloat16* to, int64_t limb, int width, const float (&f)[32]) {
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    if (half * 16 >= width) break;
+    float r[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) r[e] = f[half * 16 + e];
+#pragma unroll
+    for (int l = 0; l < LIMBS; ++l) {
+      uint32_t w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        w[e] = vio::pack_bf16(r[2 * e], r[2 * e + 1]);
+        if (l + 1 < LIMBS) {
+          r[2 * e] -= vio::bf_lo(w[e]);                    // exact
+          r[2 * e + 1] -= vio::bf_hi(w[e]);
+        }
+      }
+      store32(to + l * limb + half * 16, w);
+    }
+  }
+}
+
+// act(g) and, for the backward pass, act'(g).  The fast forms carry a few units of 2^-22, far below the rounding to bfloat16
+// that follows; float32 results take the accurate ones.
+template <bool FAST>
+__device__ __forceinline__ void activate(int act, float g, float& a, float& slope) {
+  if (act == GNNCO_SILU) {
+    const float e = FAST ? __expf(-g) : expf(-g);
+    const float s = FAST ? __fdividef(1.0f, 1.0f + e) : 1.0f / (1.0f + e);
+    a = g * s;
+    slope = s + a * (1.0f - s);
+  } else if (act == GNNCO_GELU) {
+    const float c = FAST ? 0.5f + 0.5f * erff(g * 0.70710678f) : 0.5f * erfcf(g * -0.70710678f);
+    const float d = FAST ? __expf(-0.5f * g * g) : expf(-0.5f * g * g);
+    a = g * c;
+    slope = fmaf(g * 0.39894228f, d, c);
+  } else {
+    a = g > 0.0f ? g : (g != g ? g : 0.0f);
+    slope = g > 0.0f ? 1.0f : 0.0f;
+  }
+}
+
+struct Tile {
+  int64_t row0;
+  int32_t rows, set, n0, m0;
+  int32_t problem, slot;
+  int32_t blocks[2];                                       // stages of each contraction
+};
+
+template <int KIND, bool PAIR>
+__device__ __forceinline__ void decode(const Args& A, int t, Tile& T) {
+  constexpr int TM = PAIR ? 256 : 128;
+  if constexpr (KIND == kWeights) {
+    const int per = A.p[0].m_tiles * A.p[0].n_tiles + A.p[1].m_tiles * A.p[1].n_tiles + A.p[2].m_tiles * A.p[2].n_tiles;
+    const int chunk = t / per;
+    int rest = t - chunk * per, q = 0;
+    while (rest >= A.p[q].m_tiles * A.p[q].n_tiles) {
+      rest -= A.p[q].m_tiles * A.p[q].n_tiles;
+      ++q;
+    }
+    T.problem = q;
+    T.m0 = (rest / A.p[q].n_tiles) * TM;
+    T.n0 = (rest % A.p[q].n_tiles) * A.p[q].nt;
+    if (A.chunk_begin) {
+      T.row0 = A.chunk_begin[chunk];
+      T.rows = A.chunk_end[chunk] - (int32_t)T.row0;
+      T.slot = A.chunk_slot[chunk];
+    } else {
+      T.row0 = (int64_t)chunk * A.chunk_rows;
+      T.rows = (int32_t)min((int64_t)A.chunk_rows, A.rows - T.row0);
+      T.slot = A.chunks == 1 ? -1 : chunk;
+    }
+    T.set = T.slot < 0 ? -(T.slot + 1) : 0;
+    T.blocks[0] = (T.rows + 63) >> 6;
+    T.blocks[1] = 0;
+  } else {
+    const int m = t / A.n_tiles;
+    T.n0 = (t - m * A.n_tiles) * A.nt;
+    T.m0 = 0;
+    T.set = 0;
+    if (A.tile_row0) {
+      T.row0 = A.tile_row0[m];
+      T.rows = A.tile_rows[m];
+      T.set = A.node_part[T.row0];
+    } else {
+      T.row0 = (int64_t)m * TM;
+      T.rows = (int32_t)min((int64_t)TM, A.rows - T.row0);
+    }
+    T.blocks[0] = (A.K[0] + 63) >> 6;
+    T.blocks[1] = (A.K[1] + 63) >> 6;
+  }
+}
+
+// ------------------------------------------------------------------------------------------- kernel
+template <int KIND, int LIMBS, bool PAIR>
+__global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Maps maps, const __grid_constant__ Args A) {
+  constexpr uint32_t kSlot = 32768 * LIMBS, kA = 16384 * LIMBS;
+  constexpr int kSlots = kRing / kSlot;
+  constexpr uint32_t kBlock = 8192 * LIMBS;                // 64 x 64 of an n-major operand, all limbs
+  constexpr int kCtas = PAIR ? 2 : 1;
+  constexpr bool kAlongRows = KIND == kWeights;
+  constexpr bool kSums = LIMBS > 1;                        // stages are added up in registers
+
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t sbase = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (sbase - tc::smem_u32(smem_raw));
+  uint64_t* full = reinterpret_cast<uint64_t*>(gen + kRing + kEpiWarps * kStageBytes);   // the even CTA's is used
+  uint64_t* empty = full + kSlots;                         // every CTA's own
+  uint64_t* acc_full = empty + kSlots;                     // [2] every CTA's own
+  uint64_t* acc_empty = acc_full + 2;                      // [2] the even CTA's is used
+  uint64_t* tail = acc_empty + 2;                          // this CTA's stages with rows to be cleared
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tail + 1);
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = PAIR ? tc::cluster_ctarank() : 0u;
+  const int first = blockIdx.x / kCtas, step = gridDim.x / kCtas;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kSlots; ++i) {
+      tc::mbar_init(full + i, kCtas);
+      tc::mbar_init(empty + i, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(acc_full + i, 1);
+      tc::mbar_init(acc_empty + i, kCtas * kEpiWarps);
+    }
+    tc::mbar_init(tail, 1);
+    *abort_flag = 0;
+    tc::fence_mbar_init();
+  }
+  if (warp == 0) {
+    if (PAIR) tc::tmem_alloc_pair(tmem_slot, 512);
+    else tc::tmem_alloc(tmem_slot, 512);
+  }
+  tc::tc_fence_before_sync();
+  __syncthreads();
+  if (PAIR) tc::cluster_sync_all();
+  tc::tc_fence_after_sync();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp == kCopyWarp) {
+    // -------------------------------------------------------------------------------- operands
+    int g = 0, tails = 0;
+    bool ok = true;
+    for (int t = first; t < A.tiles && ok; t += step) {
+      Tile T;
+      decode<KIND, PAIR>(A, t, T);
+      const int nt = kAlongRows ? A.p[T.problem].nt : A.nt;
+      for (int seg = 0; seg < 2 && ok; ++seg) {
+        // bytes of a stage of this contraction
+        uint32_t b_bytes;
+        if (KIND == kGlu) b_bytes = (2 * nt / 64 / kCtas) * kBlock;
+        else if (KIND == kGluBack && seg == 0) b_bytes = (2 * nt / 64 / kCtas) * kBlock;
+        else if (KIND == kGluBack) b_bytes = (nt / kCtas) * 128 * LIMBS;
+        else b_bytes = (nt / kCtas) * 128 * LIMBS;
+        const uint32_t bytes = kA + b_bytes;
+        for (int kb = 0; kb < T.blocks[seg]; ++kb, ++g) {
+          const int slot = g % kSlots, use = g / kSlots;
+          if (use > 0 && !wait_bar(empty + slot, (use - 1) & 1, abort_flag)) { ok = false; break; }
+          const uint32_t at = sbase + slot * kSlot, bt = at + kA;
+          const uint32_t announce = PAIR ? tc::map_to_cta(tc::smem_u32(full + slot), 0) : tc::smem_u32(full + slot);
+          const int valid = kAlongRows ? min(64, T.rows - kb * 64) : 64;
+          const uint32_t bar = valid == 64 ? announce : tc::smem_u32(tail);
+          if (lane == 0) {
+            if (PAIR) tc::mbar_arrive_expect_tx_cluster(bar, bytes);
+            else tc::mbar_arrive_expect_tx(valid == 64 ? full + slot : tail, bytes);
+            if constexpr (kAlongRows) {
+              const int32_t r = (int32_t)T.row0 + kb * 64, m = T.m0 + (int)rank * 128, n = T.n0 + (int)rank * (nt / kCtas);
+              for (int i = 0; i < 2; ++i) load_box<PAIR>(at + i * kBlock, &maps.a[T.problem], m + 64 * i, r, 0, bar);
+              for (int i = 0; i < nt / kCtas / 64; ++i) load_box<PAIR>(bt + i * kBlock, &maps.b[T.problem], n + 64 * i, r, 0, bar);
+            } else {
+              load_box<PAIR>(at, &maps.a[seg], kb * 64, (int32_t)T.row0 + (int)rank * 128, 0, bar);
+              if (KIND == kGlu || (KIND == kGluBack && seg == 0)) {
+                // gate columns, then up columns; in a pair the even CTA holds the gate's, the odd one the other's
+                const int per = nt / 64;
+                for (int i = 0; i < 2 * per / kCtas; ++i) {
+                  const int which = PAIR ? (int)rank : i / per, block = PAIR ? i : i % per;
+                  load_box_of_set<PAIR>(bt + i * kBlock, &maps.b[which], T.n0 + 64 * block, kb * 64, T.set, bar);
+                }
+              } else if (KIND == kGluBack) {
+                load_box_of_set<PAIR>(bt, &maps.b[2], kb * 64, T.n0 + (int)rank * (nt / kCtas), T.set, bar);
+              } else if (KIND == kDown) {
+                const int n = T.n0 + (int)rank * (nt / kCtas);
+                for (int i = 0; i < nt / kCtas / 64; ++i) load_box_of_set<PAIR>(bt + i * kBlock, &maps.b[0], n + 64 * i, kb * 64, T.set, bar);
+              } else {
+                load_box_of_set<PAIR>(bt, &maps.b[seg], kb * 64, T.n0 + (int)rank * (nt / kCtas), T.set, bar);
+              }
+            }
+          }
+          if constexpr (kAlongRows) if (valid < 64) {
+            // row k of a 64-column block is 128 bytes at 128 k, whatever the swizzle does inside it
+            if (!wait_bar(tail, tails & 1, abort_flag)) { ok = false; break; }
+            ++tails;
+            const int blocks = (2 + nt / kCtas / 64) * LIMBS, zero = 64 - valid;
+            for (int q = lane; q < blocks * zero * 8; q += 32) {
+              const int block = q / (zero * 8), rest = q % (zero * 8);
+              tc::st_shared_zero16(at + block * 8192 + (valid + rest / 8) * 128 + (rest & 7) * 16);
+            }
+            tc::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              if (PAIR) tc::mbar_arrive_release_cluster(announce);
+              else tc::mbar_arrive(full + slot);
+            }
+          }
+          __syncwarp();
+        }
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    // -------------------------------------------------------------------------------- products
+    if (rank == 0) {
+      const uint32_t leader = tc::elect_one();
+      const uint32_t tb = __shfl_sync(0xffffffffu, tmem, 0);
+      constexpr int M = PAIR ? 256 : 128;
+      int g = 0, part = 0;
+      bool ok = true;
+      for (int t = first; t < A.tiles && ok; t += step) {
+        Tile T;
+        decode<KIND, PAIR>(A, t, T);
+        const int nt = kAlongRows ? A.p[T.problem].nt : A.nt;
+        bool open = false;                                 // the current part has its buffer
+        for (int seg = 0; seg < 2 && ok; ++seg) {
+          const bool twin = KIND == kGlu || (KIND == kGluBack && seg == 0);
+          const bool b_n_major = twin || KIND == kDown || KIND == kWeights;
+          const int N = twin ? 2 * nt : nt;
+          const uint32_t idesc = tc::idesc_bf16_f32(M, N, kAlongRows, b_n_major);
+          const uint32_t column = KIND == kGluBack && seg == 1 && !kSums ? 2 * nt : 0;
+          const uint32_t b_limb = b_n_major ? 8192 : (uint32_t)(nt / kCtas) * 128;
+          const int K = kAlongRows ? T.rows : A.K[seg];
+          for (int kb = 0; kb < T.blocks[seg]; ++kb, ++g) {
+            if (!open) {
+              if (part >= 2) ok = __all_sync(0xffffffffu, wait_bar(acc_empty + (part & 1), ((part >> 1) - 1) & 1, abort_flag)) != 0;
+              tc::tc_fence_after_sync();
+              if (!ok) break;
+              open = true;
+            }
+            const uint32_t acc = tb + (part & 1) * kBuf + column;
+            const int slot = g % kSlots, use = g / kSlots;
+            ok = __all_sync(0xffffffffu, wait_bar(full + slot, use & 1, abort_flag)) != 0;
+            tc::tc_fence_after_sync();
+            if (!ok) break;
+            const uint32_t at = sbase + slot * kSlot, bt = at + kA;
+            const int steps = min(4, (K - kb * 64 + 15) >> 4);       // what lies behind K is zero
+            const uint64_t a0 = tc::smem_desc_sw128(at, kAlongRows ? kBlock : 16, 1024);
+            const uint64_t b0 = tc::smem_desc_sw128(bt, b_n_major ? kBlock : 16, 1024);
+            constexpr uint64_t a_step = kAlongRows ? 128 : 2, a_limb = (kAlongRows ? 8192 : 16384) / 16;
+            const uint64_t b_step = b_n_major ? 128 : 2;
+            if constexpr (LIMBS == 1) {
+              for (int k = 0; k < steps; ++k) tc::mma_f16<PAIR, false>(leader, acc, a0 + a_step * k, b0 + b_step * k, idesc, kb + k != 0 || (KIND == kDx && seg == 1));
+            } else {
+              // a1 b3, a2 b2, a3 b1, a1 b2, a2 b1, then a1 b1
+#pragma unroll
+              for (int q = 0; q < 6; ++q) {
+                const int i = q == 1 || q == 4 ? 1 : q == 2 ? 2 : 0, j = q == 0 ? 2 : q == 1 || q == 3 ? 1 : 0;
+                const uint64_t a = a0 + i * a_limb, b = b0 + (uint64_t)(j * b_limb / 16);
+                for (int k = 0; k < steps; ++k) tc::mma_f16<PAIR, false>(leader, acc, a + a_step * k, b + b_step * k, idesc, q + k != 0);
+              }
+            }
+            if (leader) {
+              if (PAIR) tc::mma_commit_pair(empty + slot, 3);
+              else tc::mma_commit(empty + slot);
+              if (kSums) {
+                if (PAIR) tc::mma_commit_pair(acc_full + (part & 1), 3);
+                else tc::mma_commit(acc_full + (part & 1));
+              }
+            }
+            __syncwarp();
+            if (kSums) {
+              ++part;
+              open = false;
+            }
+          }
+        }
+        if (!kSums && ok && open) {
+          if (leader) {
+            if (PAIR) tc::mma_commit_pair(acc_full + (part & 1), 3);
+            else tc::mma_commit(acc_full + (part & 1));
+          }
+          __syncwarp();
+          ++part;
+        }
+      }
+    }
+  } else {
+    // --------------------------------------------------------------------------------- results
+    const int quarter = warp & 3, half = warp >> 2;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    const uint32_t free_bar = PAIR ? tc::map_to_cta(tc::smem_u32(acc_empty), 0) : tc::smem_u32(acc_empty);
+    float* const stage = reinterpret_cast<float*>(gen + kRing + warp * kStageBytes);
+    constexpr int kGroups = KIND == kGlu ? 2 : KIND == kGluBack ? 1 : 4;     // groups of 32 columns of a warp, at most
+    constexpr int kTensors = KIND == kGlu ? 2 : KIND == kGluBack ? 3 : 1;
+    float v[kSums ? kGroups : 1][kTensors][32];
+    int part = 0;
+    bool ok = true;
+    auto release = [&]() {
+      tc::tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) {
+        if (PAIR) tc::mbar_arrive_cluster(free_bar + (part & 1) * 8);
+        else tc::mbar_arrive(acc_empty + (part & 1));
+      }
+      ++part;
+    };
+    philox::Stream words(A.mask);
+    for (int t = first; t < A.tiles && ok; t += step) {
+      Tile T;
+      decode<KIND, PAIR>(A, t, T);
+      const int nt = kAlongRows ? A.p[T.problem].nt : A.nt;
+      const int cols = kAlongRows ? A.p[T.problem].N : A.cols;
+      const int groups = min(nt, cols - T.n0 + 31) / 32;   // that hold columns of the result
+      const int local = (int)rank * 128 + quarter * 32 + lane;
+      const int stages = T.blocks[0] + T.blocks[1];
+      if (kSums) {
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i)
+#pragma unroll
+          for (int x = 0; x < kTensors; ++x)
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[kSums ? i : 0][x][e] = 0.0f;
+        for (int kb = 0; kb < stages && ok; ++kb) {
+          if (!wait_bar(acc_full + (part & 1), (part >> 1) & 1, abort_flag)) { ok = false; break; }
+          tc::tc_fence_after_sync();
+          const uint32_t acc = tmem + lanes + (part & 1) * kBuf;
+          const bool second = KIND == kGluBack && kb >= T.blocks[0];
+#pragma unroll
+          for (int i = 0; i < kGroups; ++i) {
+            const int c = half + 2 * i;
+            if (c >= groups) continue;
+#pragma unroll
+            for (int x = 0; x < kTensors; ++x) {
+              if (KIND == kGluBack && second != (x == 2)) continue;
+              uint32_t r[32];
+              tc::tmem_ld_32x32(acc + (x == 1 ? nt : 0) + c * 32, r);
+              tc::tmem_ld_wait();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) v[kSums ? i : 0][x][e] += __uint_as_float(r[e]);
+            }
+          }
+          release();
+        }
+      } else if (stages > 0) {
+        if (!wait_bar(acc_full + (part & 1), (part >> 1) & 1, abort_flag)) { ok = false; break; }
+        tc::tc_fence_after_sync();
+      }
+      if (!ok) break;
+      const uint32_t acc = tmem + lanes + (part & 1) * kBuf;
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i) {
+        const int c = half + 2 * i;
+        if (c >= groups) continue;
+        float (&f)[kTensors][32] = v[kSums ? i : 0];
+        if (!kSums) {
+          if (stages > 0) {
+            uint32_t r[kTensors][32];
+#pragma unroll
+            for (int x = 0; x < kTensors; ++x) tc::tmem_ld_32x32(acc + x * nt + c * 32, r[x]);
+            tc::tmem_ld_wait();
+#pragma unroll
+            for (int x = 0; x < kTensors; ++x)
+#pragma unroll
+              for (int e = 0; e < 32; ++e) f[x][e] = __uint_as_float(r[x][e]);
+          } else {
+#pragma unroll
+            for (int x = 0; x < kTensors; ++x)
+#pragma unroll
+              for (int e = 0; e < 32; ++e) f[x][e] = 0.0f;
+          }
+        }
+        const int c0 = T.n0 + c * 32;
+        if constexpr (KIND == kGlu || KIND == kGluBack) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            float a, slope;
+            activate<LIMBS == 1>(A.act, f[0][e], a, slope);
+            const float u = f[1][e];
+            if (KIND == kGluBack) {
+              const float dh = f[kTensors - 1][e] * A.scale;
+              f[0][e] = a * u;
+              f[1][e] = dh * u * slope;
+              f[kTensors - 1][e] = dh * a;
+            } else {
+              f[0][e] = a * u;
+            }
+          }
+          if (local < T.rows) {
+            const int64_t at = (T.row0 + local) * A.out_ld + c0;
+            const int width = (int)(A.out_ld - c0);
+            store_limbs<LIMBS>(A.out[0] + at, A.out_limb, width, f[0]);
+            if (KIND == kGluBack) {
+              store_limbs<LIMBS>(A.out[1] + at, A.out_limb, width, f[1]);
+              store_limbs<LIMBS>(A.out[2] + at, A.out_limb, width, f[kTensors - 1]);
+            }
+          }
+        } else {
+          // a row per lane: out[row][c0 ..], or, transposed, out[c0 + e][row]
+          const bool part_sum = kAlongRows && T.slot >= 0;
+          const bool wide = kAlongRows ? (part_sum || A.out_f32) : A.y_f32;
+          const bool valid = kAlongRows ? T.m0 + local < A.p[T.problem].M : local < T.rows;
+          const float scale = kAlongRows ? A.p[T.problem].scale : A.scale;
+          const int64_t row = kAlongRows ? T.m0 + local : T.row0 + local;
+          if (!(KIND == kDown && A.masked)) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) f[0][e] *= scale;
+          } else {
+            const uint64_t q0 = (uint64_t)row * ((A.cols + 3) / 4) + (c0 >> 2);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              const uint4 w = words.quad(q0 + q);
+              f[0][4 * q] = A.mask.all || w.x > A.mask.lim ? f[0][4 * q] * A.mask.scale : 0.0f;
+              f[0][4 * q + 1] = A.mask.all || w.y > A.mask.lim ? f[0][4 * q + 1] * A.mask.scale : 0.0f;
+              f[0][4 * q + 2] = A.mask.all || w.z > A.mask.lim ? f[0][4 * q + 2] * A.mask.scale : 0.0f;
+              f[0][4 * q + 3] = A.mask.all || w.w > A.mask.lim ? f[0][4 * q + 3] * A.mask.scale : 0.0f;
+            }
+          }
+          void* out;
+          int64_t ld;
+          bool vectors;
+          if (kAlongRows) {
+            const Problem& P = A.p[T.problem];
+            out = part_sum ? (void*)(A.scratch + (int64_t)T.slot * A.slot_stride + P.scratch_at)
+                           : wide ? (void*)(static_cast<float*>(P.out) + T.set * P.set_stride)
+                                  : (void*)(static_cast<__nv_bfloat16*>(P.out) + T.set * P.set_stride);
+            ld = P.transposed ? P.M : P.N;
+            vectors = (part_sum || A.out_vectors) && ld % (wide ? 4 : 8) == 0;
+            if (P.transposed) {
+              if (valid) {
+                if (wide) {
+                  float* o = static_cast<float*>(out) + (int64_t)c0 * ld + row;
+#pragma unroll
+                  for (int e = 0; e < 32; ++e)
+                    if (c0 + e < cols) o[(int64_t)e * ld] = f[0][e];
+                } else {
+                  __nv_bfloat16* o = static_cast<__nv_bfloat16*>(out) + (int64_t)c0 * ld + row;
+#pragma unroll
+                  for (int e = 0; e < 32; ++e)
+                    if (c0 + e < cols) o[(int64_t)e * ld] = __float2bfloat16_rn(f[0][e]);
+                }
+              }
+              continue;
+            }
+          } else {
+            out = A.y;
+            ld = A.y_ld;
+            vectors = A.y_vectors;
+          }
+          if (vectors && c0 + 32 <= cols) {
+            if (valid) {
+              if (wide) {
+                uint4* o = reinterpret_cast<uint4*>(static_cast<float*>(out) + row * ld + c0);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                  o[e] = make_uint4(__float_as_uint(f[0][4 * e]), __float_as_uint(f[0][4 * e + 1]), __float_as_uint(f[0][4 * e + 2]),
+                                    __float_as_uint(f[0][4 * e + 3]));
+              } else {
+                uint4* o = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(out) + row * ld + c0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  o[e] = make_uint4(vio::pack_bf16(f[0][8 * e], f[0][8 * e + 1]), vio::pack_bf16(f[0][8 * e + 2], f[0][8 * e + 3]),
+                                    vio::pack_bf16(f[0][8 * e + 4], f[0][8 * e + 5]), vio::pack_bf16(f[0][8 * e + 6], f[0][8 * e + 7]));
+              }
+            }
+          } else {
+            // rows that start anywhere, or end inside the group: through shared memory, so that lanes hold neighbouring columns
+            __syncwarp();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) stage[lane * kStagePitch + e] = f[0][e];
+            __syncwarp();
+            const int rows_here = (kAlongRows ? A.p[T.problem].M - T.m0 : T.rows) - (local - lane);
+            const int64_t row_of_warp = row - lane;
+            if (c0 + lane < cols) {
+              for (int r = 0; r < min(32, rows_here); ++r) {
+                const float x = stage[r * kStagePitch + lane];
+                const int64_t to = (row_of_warp + r) * ld + c0 + lane;
+                if (wide) static_cast<float*>(out)[to] = x;
+                else static_cast<__nv_bfloat16*>(out)[to] = __float2bfloat16_rn(x);
+              }
+            }
+          }
+        }
+      }
+      if (!kSums && stages > 0) release();
+    }
+  }
+  // ------------------------------------------------------------------------------------ the end
+  if (*abort_flag) {
+    if (threadIdx.x == 0) atomicMin(A.status, (int32_t)GNNCO_INTERNAL);
+    const long long t0 = clock64();                        // copies and products already issued end before the memory goes
+    while (clock64() - t0 < 1000000ll) {}
+  }
+  tc::tc_fence_before_sync();
+  __syncthreads();
+  if (PAIR) tc::cluster_sync_all();
+  if (warp == 0) {
+    if (PAIR) tc::tmem_dealloc_pair(tmem, 512);
+    else tc::tmem_dealloc(tmem, 512);
+  }
+}
+
+// -------------------------------------------------------------------------------------------- launch
+template <int KIND, int LIMBS, bool PAIR>
+int32_t launch_one(const Maps& maps, const Args& args, int device, int sms, cudaStream_t st) {
+  auto kernel = tiles<KIND, LIMBS, PAIR>;
+  static std::atomic<int> allowed{0};
+  const int32_t rc = allow_shared_memory(kernel, kSmem, device, allowed);
+  if (rc != GNNCO_OK) return rc;
+  const int most = PAIR ? resident_pairs(device, sms) : sms;
+  const int ctas = (args.tiles < most ? args.tiles : most) * (PAIR ? 2 : 1);
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(ctas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = PAIR ? 2 : 1; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  GNNCO_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, maps, args));
+  return GNNCO_OK;
+}
+
+}  // namespace ff

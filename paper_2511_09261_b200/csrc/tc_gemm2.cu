@@ -1038,6 +1038,22 @@ weight_grad_tc_pair(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 
 }  // namespace
 
+// A tensor map of bfloat16 boxes of any rank in the 128-byte-swizzled layout (inner box: 64 elements).
+bool encode_bf16_boxes(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box) {
+  EncodeTiledFn enc = encode_tiled();
+  if (!enc) return false;
+  cuuint64_t d[5], s[5];
+  cuuint32_t b[5], e[5];
+  for (int i = 0; i < rank; ++i) {
+    d[i] = dims[i];
+    b[i] = box[i];
+    e[i] = 1u;
+    if (i + 1 < rank) s[i] = strides[i];
+  }
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), d, s, b, e, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // The pair form is used for the widths where a single CTA cannot hold a second operand tile.
 bool tc_pair_transform_supported(gnnco_handle* h, int dtype, int K, int N) {
   if (dtype != GNNCO_BF16 || !(K == 256 && N == 256)) return false;

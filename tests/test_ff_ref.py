@@ -57,7 +57,7 @@ def test_block_gradients_against_differences(name):
             got[i] = (up - loss()) / (2 * eps)
             t[i] = keep
         np.testing.assert_allclose(got, d[key], rtol=2e-6, atol=2e-8)
-        assert np.all(d[key + "_mag"] * (1 + 1e-12) >= np.abs(d[key]))
+        assert np.all(d[key + "_stored"] * (1 + 1e-12) >= np.abs(d[key])) and np.all(d[key + "_mag"] >= d[key + "_stored"])
 
 
 @pytest.fixture
@@ -101,8 +101,69 @@ def test_dropout_refuses_other_shapes_types_and_devices(graph):
     assert graph._lib.last("gnnco_dropout")[5] == 4
 
 
+def _block(rows=6, F=4, H=5, Fo=3, sets=1):
+    return [torch.ones(rows, F), torch.ones(sets, F, H), torch.ones(sets, F, H), torch.ones(sets, H, Fo)]
+
+
+def test_block_refuses_other_shapes_and_types(graph, monkeypatch):
+    monkeypatch.setattr(gnnco, "_require", _require_on_cpu)
+    graph.S, graph.n = 3, 6
+    bf = torch.bfloat16
+    for change, error in [
+        ({0: torch.ones(6)}, ValueError), ({0: torch.ones(6, 5)}, ValueError), ({0: torch.ones(6, 8)[:, ::2]}, ValueError),
+        ({1: torch.ones(1, 4, 6)}, ValueError), ({2: torch.ones(1, 5, 5)}, ValueError), ({3: torch.ones(1, 4, 3)}, ValueError),
+        ({1: torch.ones(4, 5)}, ValueError), ({1: torch.ones(2, 4, 5), 2: torch.ones(2, 4, 5), 3: torch.ones(2, 5, 3)}, ValueError),
+        ({2: torch.ones(3, 4, 5)}, ValueError), ({3: torch.ones(1, 5, 0)}, ValueError), ({1: torch.ones(1, 5, 4).mT}, TypeError),
+        ({0: torch.ones(6, 4).double()}, TypeError), ({1: torch.ones(1, 4, 5).half()}, TypeError), ({3: torch.ones(1, 5, 3, dtype=bf)}, TypeError),
+    ]:
+        args = [change.get(i, t) for i, t in enumerate(_block())]
+        with pytest.raises(error):
+            graph.gated_ff(*args)
+        with pytest.raises(error):
+            graph.gated_ff_backward(args[0], torch.ones(6, 3), *args[1:])
+    args = _block()
+    with pytest.raises(ValueError):
+        graph.gated_ff(*args, act="tanh")
+    with pytest.raises(ValueError):
+        graph.gated_ff(*args, drop=gnnco.Dropout(2.0, 1))
+    with pytest.raises(ValueError):
+        graph.gated_ff(*args, out=torch.empty(6, 4))
+    for dy in (torch.ones(5, 3), torch.ones(6, 4)):
+        with pytest.raises(ValueError):
+            graph.gated_ff_backward(args[0], dy, *args[1:])
+    with pytest.raises(TypeError):
+        graph.gated_ff_backward(args[0], torch.ones(6, 3, dtype=bf), *args[1:])
+    with pytest.raises(TypeError):
+        graph.gated_ff_backward(args[0], torch.ones(6, 3), *args[1:], dw_dtype=torch.float16)
+    with pytest.raises(ValueError):
+        graph.gated_ff_backward(args[0], torch.ones(6, 3), *args[1:], want_dx=False, want_dw=False)
+    assert not [c for c in graph._lib.calls if not c[0].endswith("_bytes")]
+
+
+def _require_on_cpu(t, dtype, what, device_type="cuda", real=gnnco._require):
+    return real(t, dtype, what, "cpu")
+
+
+def test_block_gradients_take_the_types_asked_for(graph, monkeypatch):
+    monkeypatch.setattr(gnnco, "_require", _require_on_cpu)
+    x, *w = _block()
+    xb, wb = x.bfloat16(), [t.bfloat16() for t in w]
+    dy = torch.ones(6, 3)
+    assert graph.gated_ff_backward(x, dy, *w)["dw_up"].dtype == torch.float32
+    assert graph.gated_ff_backward(xb, dy.bfloat16(), *wb)["dw_up"].dtype == torch.bfloat16
+    assert graph.gated_ff_backward(xb, dy.bfloat16(), *wb, dw_dtype=torch.float32)["dw_up"].dtype == torch.float32
+    d = graph.gated_ff_backward(xb, dy.bfloat16(), *w, want_dx=False)
+    assert d["dx"] is None and d["dw_down"].dtype == torch.float32
+    assert graph.gated_ff_backward(x, dy, *w, want_dw=False)["dw_gate"] is None
+
+
 def test_the_c_entry_checks_its_arguments_without_a_gpu():
     import ctypes
     lib = gnnco.load_library()
     d = gnnco.DropoutParams(0.5, 1, 0, 0, None)
+    f = gnnco.GatedFfDesc(1, 1, 1, 1, 0, 0, 1, 0)
+    n = ctypes.c_size_t(0)
+    assert lib.gnnco_gated_ff_workspace_bytes(None, ctypes.byref(f), 0, ctypes.byref(n)) == gnnco.INVALID_ARGUMENT
+    assert lib.gnnco_gated_ff(None, ctypes.byref(f), None, 1, None, 0, None) == gnnco.INVALID_ARGUMENT
+    assert lib.gnnco_gated_ff_backward(None, ctypes.byref(f), None, 1, None, None, 0, None) == gnnco.INVALID_ARGUMENT
     assert lib.gnnco_dropout(None, 0, 1, 1, None, 1, ctypes.byref(d), None, 1, None) == gnnco.INVALID_ARGUMENT

@@ -24,12 +24,12 @@ struct DropArgs {
 };
 
 __device__ __forceinline__ float pick(uint32_t word, const philox::Mask& m, float v) {
-  return m.all || word > m.lim ? v * m.scale : 0.0f;
+  return word > m.lim ? v * m.scale : 0.0f;
 }
 
 // VEC consecutive, aligned elements (4 or 8: whole quads; F is a multiple of VEC).  flat: the rows are one run of elements.
 template <typename T, int VEC, int UNROLL, bool FLAT>
-__global__ void __launch_bounds__(256) drop_vectors(const DropArgs A) {
+__global__ void __launch_bounds__(256) drop_vectors(const __grid_constant__ DropArgs A) {
   const int64_t items = A.rows * A.groups;
   philox::Stream words(A.m);
   for (int64_t base = (int64_t)blockIdx.x * (256 * UNROLL); base < items; base += (int64_t)gridDim.x * (256 * UNROLL)) {
@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(256) drop_vectors(const DropArgs A) {
 #pragma unroll
       for (int k = 0; k < VEC; k += 4) {
         // F is a multiple of 4: quads are numbered along the run of groups
-        const uint4 w = words.quad((uint64_t)i * (VEC / 4) + k / 4);
+        const uint4 w = words.quad(A.m, (uint64_t)i * (VEC / 4) + k / 4);
         f[k] = pick(w.x, A.m, v[u].get(k));
         f[k + 1] = pick(w.y, A.m, v[u].get(k + 1));
         f[k + 2] = pick(w.z, A.m, v[u].get(k + 2));
@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(256) drop_vectors(const DropArgs A) {
 
 // any width and alignment: a quad of columns per thread, element by element
 template <typename T>
-__global__ void __launch_bounds__(256) drop_quads(const DropArgs A) {
+__global__ void __launch_bounds__(256) drop_quads(const __grid_constant__ DropArgs A) {
   const int64_t items = A.rows * A.groups;
   philox::Stream words(A.m);
   for (int64_t base = (int64_t)blockIdx.x * 256; base < items; base += (int64_t)gridDim.x * 256) {
@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(256) drop_quads(const DropArgs A) {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (k < count) v[k].template load<true>(from + k);
-    const uint4 w = words.quad((uint64_t)i);
+    const uint4 w = words.quad(A.m, (uint64_t)i);
     const uint32_t word[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int k = 0; k < 4; ++k)
@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(256) drop_quads(const DropArgs A) {
 
 template <typename T>
 void launch_drop(gnnco_handle* h, DropArgs A, cudaStream_t st) {
-  constexpr int kVec = 16 / (int)sizeof(T), kUnroll = 4;
+  constexpr int kVec = 16 / (int)sizeof(T), kUnroll = 2;
   auto fits = [&](int vec) {
     const uintptr_t bytes = (uintptr_t)vec * sizeof(T);
     return A.F % vec == 0 && (((uintptr_t)A.x | (uintptr_t)A.out | (uintptr_t)(A.x_ld * (int64_t)sizeof(T)) |
@@ -131,17 +131,15 @@ void launch_drop(gnnco_handle* h, DropArgs A, cudaStream_t st) {
 
 }  // namespace
 
-// The mask of a launch; false: p outside [0, 1].
-bool make_mask(const gnnco_dropout_params* d, philox::Mask* m) {
+bool make_mask(const gnnco_dropout_params* d, philox::Mask* m, bool* drops) {
   if (!(d->p >= 0.0 && d->p <= 1.0)) return false;
   const double limit = nearbyint(d->p * 4294967296.0);     // ties to even, as everywhere
-  m->seed_lo = (uint32_t)d->seed;
-  m->seed_hi = (uint32_t)(d->seed >> 32);
+  philox::set_seed(m, d->seed);
   m->step = d->step;
   m->layer = d->layer;
   m->step_dev = d->step_dev;
-  m->all = limit < 1.0;
-  m->lim = m->all ? 0u : (uint32_t)(limit - 1.0);
+  *drops = limit >= 1.0;
+  m->lim = *drops ? (uint32_t)(limit - 1.0) : 0u;
   m->scale = d->p < 1.0 ? (float)(1.0 / (1.0 - d->p)) : 0.0f;   // p = 1 keeps nothing
   return true;
 }
@@ -151,24 +149,26 @@ bool on_own_device(const gnnco_handle* h) {
   return cudaGetDevice(&device) == cudaSuccess && device == h->device;
 }
 
-void run_dropout(gnnco_handle* h, int32_t dtype, int64_t rows, int32_t F, const void* x, int64_t x_ld, const philox::Mask& m,
-                 void* out, int64_t out_ld, cudaStream_t st) {
-  DropArgs A = {x, out, x_ld, out_ld, rows, F, 0, m};
-  if (dtype == GNNCO_F32) launch_drop<float>(h, A, st);
-  else launch_drop<__nv_bfloat16>(h, A, st);
-  h->launches += 1;
-}
-
 extern "C" int32_t gnnco_dropout(gnnco_handle* h, int32_t feat_dtype, int64_t rows, int32_t F, const void* x, int64_t x_ld,
                                  const gnnco_dropout_params* d, void* out, int64_t out_ld, void* stream) {
   philox::Mask m;
-  if (!h || !d || rows < 0 || F < 1 || !make_mask(d, &m)) return GNNCO_INVALID_ARGUMENT;
+  bool drops = false;
+  if (!h || !d || rows < 0 || F < 1 || !make_mask(d, &m, &drops)) return GNNCO_INVALID_ARGUMENT;
   if (feat_dtype != GNNCO_F32 && feat_dtype != GNNCO_BF16) return GNNCO_UNSUPPORTED;
   if (rows == 0) return GNNCO_OK;
   if (!x || !out || x_ld < F || out_ld < F || rows > ((int64_t)1 << 62) / F || !on_own_device(h)) return GNNCO_INVALID_ARGUMENT;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   ProfScope prof_(h, K_DROPOUT, st);
-  run_dropout(h, feat_dtype, rows, F, x, x_ld, m, out, out_ld, st);
+  const size_t es = feat_dtype == GNNCO_F32 ? 4 : 2;
+  if (!drops) {                                            // p below 2^-33: 1 / (1 - p) is 1 in float32
+    if (x != out)
+      GNNCO_CUDA_TRY(cudaMemcpy2DAsync(out, out_ld * es, x, x_ld * es, F * es, rows, cudaMemcpyDeviceToDevice, st));
+    return GNNCO_OK;
+  }
+  const DropArgs A = {x, out, x_ld, out_ld, rows, F, 0, m};
+  if (feat_dtype == GNNCO_F32) launch_drop<float>(h, A, st);
+  else launch_drop<__nv_bfloat16>(h, A, st);
+  h->launches += 1;
   GNNCO_LAUNCH_CHECK();
   return GNNCO_OK;
 }

@@ -79,11 +79,11 @@ __global__ void __launch_bounds__(256) pack_operands(const __grid_constant__ Pac
       const uint64_t q = (uint64_t)row * ((J.cols + 3) / 4) + c / 4;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const uint4 w = words.quad(q + k);
-        f[4 * k] = P.mask.all || w.x > P.mask.lim ? f[4 * k] : 0.0f;
-        f[4 * k + 1] = P.mask.all || w.y > P.mask.lim ? f[4 * k + 1] : 0.0f;
-        f[4 * k + 2] = P.mask.all || w.z > P.mask.lim ? f[4 * k + 2] : 0.0f;
-        f[4 * k + 3] = P.mask.all || w.w > P.mask.lim ? f[4 * k + 3] : 0.0f;
+        const uint4 w = words.quad(P.mask, q + k);
+        f[4 * k] = w.x > P.mask.lim ? f[4 * k] : 0.0f;
+        f[4 * k + 1] = w.y > P.mask.lim ? f[4 * k + 1] : 0.0f;
+        f[4 * k + 2] = w.z > P.mask.lim ? f[4 * k + 2] : 0.0f;
+        f[4 * k + 3] = w.w > P.mask.lim ? f[4 * k + 3] : 0.0f;
       }
     }
     __nv_bfloat16* const to = J.to + row * J.to_ld + c;
@@ -241,14 +241,14 @@ Work lay_out(const gnnco_handle* h, const gnnco_gated_ff_desc* d, bool backward)
   return w;
 }
 
-int32_t check(const gnnco_handle* h, const gnnco_gated_ff_desc* d, philox::Mask* mask) {
+int32_t check(const gnnco_handle* h, const gnnco_gated_ff_desc* d, philox::Mask* mask, bool* drops) {
   if (!h || !d || d->rows < 0 || d->F < 1 || d->H < 1 || d->F_out < 1) return GNNCO_INVALID_ARGUMENT;
   if (d->feat_dtype != GNNCO_F32 && d->feat_dtype != GNNCO_BF16) return GNNCO_UNSUPPORTED;
   if (d->w_dtype != GNNCO_F32 && (d->w_dtype != GNNCO_BF16 || d->feat_dtype != GNNCO_BF16)) return GNNCO_UNSUPPORTED;
   if (d->F > kMaxWidth || d->H > kMaxWidth || d->F_out > kMaxWidth || d->rows > 0x7fffff00ll) return GNNCO_UNSUPPORTED;
   if (d->act != GNNCO_SILU && d->act != GNNCO_GELU && d->act != GNNCO_RELU) return GNNCO_INVALID_ARGUMENT;
   if (d->sets != 1 && (d->sets != h->S || d->rows != h->n)) return GNNCO_INVALID_ARGUMENT;
-  if (mask && d->drop && !make_mask(d->drop, mask)) return GNNCO_INVALID_ARGUMENT;
+  if (mask && d->drop && !make_mask(d->drop, mask, drops)) return GNNCO_INVALID_ARGUMENT;
   return GNNCO_OK;
 }
 
@@ -257,6 +257,7 @@ struct Call {
   const gnnco_gated_ff_desc* d;
   cudaStream_t st;
   int limbs;
+  bool drops;                                              // whether the mask drops anything
   PackJobs jobs;
   int n_jobs = 0;
 
@@ -333,7 +334,7 @@ struct Call {
     a.K[1] = dy ? d->F_out : 0;
     a.cols = d->H;
     a.act = d->act;
-    a.scale = dy && d->drop ? jobs.mask.scale : 1.0f;
+    a.scale = dy && drops ? jobs.mask.scale : 1.0f;
     for (int k = 0; k < (dy ? 3 : 1); ++k) a.out[k] = const_cast<__nv_bfloat16*>(out[k].p);
     a.out_ld = out[0].ld;
     a.out_limb = out[0].limb;
@@ -357,7 +358,7 @@ struct Call {
     a.n_tiles = (int32_t)blocks_of(d->F_out, a.nt);
     a.K[0] = d->H;
     result(&a, y, y_ld, d->F_out);
-    a.masked = d->drop != nullptr;
+    a.masked = drops;
     a.mask = jobs.mask;
     if (!map_rows(&m.a[0], hh.p, d->rows, d->H, hh.ld, hh.limb, limbs, 128) ||
         !map_sets(&m.b[0], wd.p, d->sets, d->H, d->F_out, wd.ld, limbs, 64))
@@ -423,7 +424,7 @@ struct Call {
       P.out = outs[q];
       P.set_stride = (int64_t)R[q] * C[q];
       P.scratch_at = at[q];
-      P.scale = q == 2 && d->drop ? jobs.mask.scale : 1.0f;
+      P.scale = q == 2 && drops ? jobs.mask.scale : 1.0f;
       const Operand& A = P.transposed ? col_op[q] : row_op[q];
       const Operand& B = P.transposed ? row_op[q] : col_op[q];
       if (!map_rows(&m.a[q], A.p, d->rows, P.M, A.ld, A.limb, limbs, 64) || !map_rows(&m.b[q], B.p, d->rows, P.N, B.ld, B.limb, limbs, 64))
@@ -463,7 +464,7 @@ struct Call {
 
 extern "C" int32_t gnnco_gated_ff_workspace_bytes(const gnnco_handle* h, const gnnco_gated_ff_desc* d, int32_t backward, size_t* bytes) {
   if (!bytes) return GNNCO_INVALID_ARGUMENT;
-  const int32_t rc = check(h, d, nullptr);
+  const int32_t rc = check(h, d, nullptr, nullptr);
   if (rc != GNNCO_OK) return rc;
   *bytes = lay_out(h, d, backward != 0).total;
   return GNNCO_OK;
@@ -472,7 +473,7 @@ extern "C" int32_t gnnco_gated_ff_workspace_bytes(const gnnco_handle* h, const g
 extern "C" int32_t gnnco_gated_ff(gnnco_handle* h, const gnnco_gated_ff_desc* d, void* y, int64_t y_ld, void* ws, size_t ws_bytes,
                                   void* stream) {
   Call c = {};
-  const int32_t rc = check(h, d, &c.jobs.mask);
+  const int32_t rc = check(h, d, &c.jobs.mask, &c.drops);
   if (rc != GNNCO_OK) return rc;
   if (d->rows == 0) return GNNCO_OK;
   if (!d->x || d->x_ld < d->F || !d->w_gate || !d->w_up || !d->w_down || !y || y_ld < d->F_out || !ws || ((uintptr_t)ws & 255) ||
@@ -506,7 +507,7 @@ extern "C" int32_t gnnco_gated_ff(gnnco_handle* h, const gnnco_gated_ff_desc* d,
 extern "C" int32_t gnnco_gated_ff_backward(gnnco_handle* h, const gnnco_gated_ff_desc* d, const void* dy, int64_t dy_ld,
                                            const gnnco_gated_ff_grads* g, void* ws, size_t ws_bytes, void* stream) {
   Call c = {};
-  const int32_t rc = check(h, d, &c.jobs.mask);
+  const int32_t rc = check(h, d, &c.jobs.mask, &c.drops);
   if (rc != GNNCO_OK) return rc;
   const bool weights = g && g->dw_gate;
   if (!g || weights != (g->dw_up != nullptr) || weights != (g->dw_down != nullptr)) return GNNCO_INVALID_ARGUMENT;
@@ -536,7 +537,7 @@ extern "C" int32_t gnnco_gated_ff_backward(gnnco_handle* h, const gnnco_gated_ff
   const Operand wg = c.operand(d->w_gate, sets * d->F, d->H, d->H, d->w_dtype, false, base + w.wg);
   const Operand wu = c.operand(d->w_up, sets * d->F, d->H, d->H, d->w_dtype, false, base + w.wu);
   const Operand wd = c.operand(d->w_down, sets * d->H, d->F_out, d->F_out, d->w_dtype, false, base + w.wd);
-  const Operand dyo = c.operand(dy, d->rows, d->F_out, dy_ld, d->feat_dtype, d->drop != nullptr, base + w.dy);
+  const Operand dyo = c.operand(dy, d->rows, d->F_out, dy_ld, d->feat_dtype, c.drops, base + w.dy);
   Operand hdd[3];
   const size_t at[3] = {w.h, w.dg, w.du};
   for (int k = 0; k < 3; ++k) {

@@ -11,50 +11,50 @@ namespace philox {
 
 constexpr uint32_t kMul0 = 0xD2511F53u, kMul1 = 0xCD9E8D57u, kWeyl0 = 0x9E3779B9u, kWeyl1 = 0xBB67AE85u;
 
-// What a launch passes down.  lim = p 2^32 - 1 in 32 bits: an element is kept if its word is above it; all: p 2^32 < 1.
+// What a launch passes down.  lim = p 2^32 - 1 in 32 bits: an element is kept if its word is above it (where p 2^32 rounds to 0
+// nothing is dropped, and no kernel draws words).
 struct Mask {
-  uint32_t seed_lo, seed_hi, step, layer, lim;
-  uint32_t all;
+  uint32_t key[20];                   // both words of every round's key: operands from constant memory, no additions per quad
+  uint32_t step, layer, lim;
   float scale;                        // 1 / (1 - p)
   const uint32_t* step_dev;           // added to step where given
 };
+inline void set_seed(Mask* m, uint64_t seed) {
+  for (uint32_t r = 0; r < 10; ++r) {
+    m->key[2 * r] = (uint32_t)seed + r * kWeyl0;
+    m->key[2 * r + 1] = (uint32_t)(seed >> 32) + r * kWeyl1;
+  }
+}
 
-// The part of the rounds that all counters of a launch share: the second product of round 1, and, while the upper half of the
-// number of the quad stays the same, the first product of round 2 (17 products a quad instead of 20).
+// The part of the rounds that all counters of a launch share is computed once: the second product of round 1, and, while the upper
+// half of the quad's number stays the same, the first product of round 2 (17 products a quad instead of 20).
 struct Stream {
-  uint32_t seed_lo, seed_hi, layer, hi1, lo1;
-  uint32_t last_hi, hi2, lo2;
+  uint32_t hi1, lo1, last_hi, hi2, lo2;
   __device__ __forceinline__ explicit Stream(const Mask& m) {
     const uint32_t step = m.step + (m.step_dev ? *m.step_dev : 0u);
-    seed_lo = m.seed_lo; seed_hi = m.seed_hi; layer = m.layer;
     hi1 = __umulhi(kMul1, step);
     lo1 = kMul1 * step;
-    upper(0u);
+    upper(m, 0u);
   }
-  __device__ __forceinline__ void upper(uint32_t q_hi) {
+  __device__ __forceinline__ void upper(const Mask& m, uint32_t q_hi) {
     last_hi = q_hi;
-    const uint32_t x0 = hi1 ^ q_hi ^ seed_lo;
+    const uint32_t x0 = hi1 ^ q_hi ^ m.key[0];
     hi2 = __umulhi(kMul0, x0);
     lo2 = kMul0 * x0;
   }
-  __device__ __forceinline__ uint4 quad(uint64_t q) {
-    if ((uint32_t)(q >> 32) != last_hi) upper((uint32_t)(q >> 32));
-    uint32_t k0 = seed_lo, k1 = seed_hi;
+  __device__ __forceinline__ uint4 quad(const Mask& m, uint64_t q) {
+    if ((uint32_t)(q >> 32) != last_hi) upper(m, (uint32_t)(q >> 32));
     const uint64_t a = (uint64_t)kMul0 * (uint32_t)q;
-    uint32_t x1 = lo1, x2 = (uint32_t)(a >> 32) ^ layer ^ k1, x3 = (uint32_t)a, x0;
-    // round 2
-    k0 += kWeyl0; k1 += kWeyl1;
+    uint32_t x2 = (uint32_t)(a >> 32) ^ m.layer ^ m.key[1], x3 = (uint32_t)a;
     const uint64_t b = (uint64_t)kMul1 * x2;
-    x0 = (uint32_t)(b >> 32) ^ x1 ^ k0;
-    x2 = hi2 ^ x3 ^ k1;
-    x1 = (uint32_t)b;
+    uint32_t x0 = (uint32_t)(b >> 32) ^ lo1 ^ m.key[2], x1 = (uint32_t)b;
+    x2 = hi2 ^ x3 ^ m.key[3];
     x3 = lo2;
 #pragma unroll
     for (int round = 2; round < 10; ++round) {
-      k0 += kWeyl0; k1 += kWeyl1;
       const uint64_t u = (uint64_t)kMul0 * x0, v = (uint64_t)kMul1 * x2;
-      x0 = (uint32_t)(v >> 32) ^ x1 ^ k0;
-      x2 = (uint32_t)(u >> 32) ^ x3 ^ k1;
+      x0 = (uint32_t)(v >> 32) ^ x1 ^ m.key[2 * round];
+      x2 = (uint32_t)(u >> 32) ^ x3 ^ m.key[2 * round + 1];
       x1 = (uint32_t)v;
       x3 = (uint32_t)u;
     }

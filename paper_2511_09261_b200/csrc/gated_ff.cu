@@ -132,6 +132,13 @@ bool map_rows(CUtensorMap* m, const void* base, int64_t rows, int cols, int64_t 
   const uint32_t box[3] = {64u, (uint32_t)box_rows, (uint32_t)limbs};
   return encode_bf16_boxes(m, base, 3, dims, strides, box);
 }
+// results: boxes of 32 x 32
+bool map_out(CUtensorMap* m, const void* base, int64_t rows, int cols, int64_t ld) {
+  const uint64_t dims[2] = {(uint64_t)cols, (uint64_t)rows};
+  const uint64_t strides[1] = {(uint64_t)ld * 2};
+  const uint32_t box[2] = {32u, 32u};
+  return encode_bf16_boxes(m, base, 2, dims, strides, box);
+}
 // [limbs][sets][rows][cols]
 bool map_sets(CUtensorMap* m, const void* base, int64_t sets, int rows, int cols, int64_t ld, int limbs, int box_rows) {
   const uint64_t dims[4] = {(uint64_t)cols, (uint64_t)rows, (uint64_t)sets, (uint64_t)limbs};
@@ -343,6 +350,7 @@ struct Call {
     if (dy)
       ok = ok && map_rows(&m.a[1], dy->p, d->rows, d->F_out, dy->ld, dy->limb, limbs, 128) &&
            map_sets(&m.b[2], wd.p, d->sets, d->H, d->F_out, wd.ld, limbs, pair ? a.nt / 2 : a.nt);
+    else if (limbs == 1) ok = ok && map_out(&m.out, out[0].p, d->rows, d->H, out[0].ld);
     if (!ok) return GNNCO_CUDA_ERROR;
     return launch(dy ? ff::kGluBack : ff::kGlu, pair, m, &a, (int64_t)a.m_tiles * a.n_tiles);
   }
@@ -357,7 +365,7 @@ struct Call {
     a.nt = wide_tile(pair, d->F_out);
     a.n_tiles = (int32_t)blocks_of(d->F_out, a.nt);
     a.K[0] = d->H;
-    result(&a, y, y_ld, d->F_out);
+    if (!result(&a, &m, y, y_ld, d->F_out)) return GNNCO_CUDA_ERROR;
     a.masked = drops;
     a.mask = jobs.mask;
     if (!map_rows(&m.a[0], hh.p, d->rows, d->H, hh.ld, hh.limb, limbs, 128) ||
@@ -374,20 +382,21 @@ struct Call {
     a.nt = wide_tile(pair, d->F);
     a.n_tiles = (int32_t)blocks_of(d->F, a.nt);
     a.K[0] = a.K[1] = d->H;
-    result(&a, dx, dx_ld, d->F);
+    if (!result(&a, &m, dx, dx_ld, d->F)) return GNNCO_CUDA_ERROR;
     const int box = pair ? a.nt / 2 : a.nt;
     if (!map_rows(&m.a[0], dg.p, d->rows, d->H, dg.ld, dg.limb, limbs, 128) || !map_rows(&m.a[1], du.p, d->rows, d->H, du.ld, du.limb, limbs, 128) ||
         !map_sets(&m.b[0], wg.p, d->sets, d->F, d->H, wg.ld, limbs, box) || !map_sets(&m.b[1], wu.p, d->sets, d->F, d->H, wu.ld, limbs, box))
       return GNNCO_CUDA_ERROR;
     return launch(ff::kDx, pair, m, &a, (int64_t)a.m_tiles * a.n_tiles);
   }
-  void result(Args* a, void* y, int64_t ld, int32_t cols) const {
+  bool result(Args* a, Maps* m, void* y, int64_t ld, int32_t cols) const {
     a->cols = cols;
     a->scale = 1.0f;
     a->y = y;
     a->y_ld = ld;
     a->y_f32 = d->feat_dtype == GNNCO_F32;
     a->y_vectors = ((uintptr_t)y & 15) == 0 && ld % (a->y_f32 ? 4 : 8) == 0;
+    return a->y_f32 || !a->y_vectors || map_out(&m->out, y, d->rows, cols, ld);
   }
   int32_t weight_grads(const Operand& x, const Operand& dy, const Operand* hdd, const gnnco_gated_ff_grads* g, float* scratch) {
     const Chunks c = chunks_of(h, d);

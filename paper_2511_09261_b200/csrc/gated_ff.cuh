@@ -24,6 +24,7 @@ enum Kind { kGlu, kGluBack, kDown, kDx, kWeights };
 
 struct Maps {
   CUtensorMap a[3], b[3];
+  CUtensorMap out;                     // bfloat16 h, y or dx in boxes of 32 x 32
 };
 
 // one weight gradient: [M x N] or, transposed, [N x M] in memory
@@ -70,5 +71,6 @@ int resident_pairs(int device, int sms);
 
 }  // namespace ff
 
-// A tensor map of bfloat16 boxes in the 128-byte-swizzled layout of the MMA operands (tc_gemm2.cu).
+// A tensor map of bfloat16 boxes, swizzled over 128 bytes (inner box 64 elements: the layout of the MMA operands) or over 64 (32
+// elements) (tc_gemm2.cu).
 bool encode_bf16_boxes(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box);

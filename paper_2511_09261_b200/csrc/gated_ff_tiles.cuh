@@ -1,10 +1,10 @@
 // The tiled tensor-core products of the gated feed-forward block (kinds and formulas: gated_ff.cuh).
 //
 // One persistent CTA per SM, or a cluster of two CTAs that share a tile of 256 rows (tcgen05 .cta_group::2: each CTA stages its
-// own 128 rows of A and half of B).  Roles of the ten warps:
-//   warps 0-7   results: TMEM lanes 32 (w % 4) .., every other group of 32 columns from w / 4 on
-//   warp 8      issues the MMAs (in a pair, the even CTA's)
-//   warp 9      issues the TMA copies of this CTA's operands
+// own 128 rows of A and half of B).  Roles of the eighteen warps:
+//   warps 0-15  results: TMEM lanes 32 (w % 4) .., every fourth group of columns from w / 4 on (32 columns; 16 of g, u and dh each)
+//   warp 16     issues the MMAs (in a pair, the even CTA's)
+//   warp 17     issues the TMA copies of this CTA's operands
 // A stage of the ring holds 64 of the contraction: A in the first half, B behind it, each as LIMBS matrices of bfloat16.  Operands
 // whose contraction runs along memory (x, dy, h, dg, du as A; Wd, Wg, Wu in the backward products) are k-major boxes of 64
 // columns, the others (the weights of the forward products, everything in the weight gradients) n-major boxes of 64 x 64:
@@ -28,32 +28,47 @@
 
 namespace ff {
 
-constexpr int kEpiWarps = 8, kMmaWarp = 8, kCopyWarp = 9, kThreads = 320;
+constexpr int kEpiWarps = 16, kMmaWarp = 16, kCopyWarp = 17, kThreads = 576;
 constexpr uint32_t kRing = 196608;                         // 6 stages of 32 KB or 2 of 96 KB
-constexpr uint32_t kStagePitch = 33;                       // words between rows of a result warp's 32 x 32 staging tile
-constexpr uint32_t kStageBytes = 32 * kStagePitch * 4;
+constexpr uint32_t kStageBytes = 32 * 16 * 4;              // a result warp's staging tile: 32 rows x 16 columns
 constexpr uint32_t kSmem = 1024 + kRing + kEpiWarps * kStageBytes + 256;
 constexpr uint32_t kBuf = 256;                             // TMEM columns of an accumulator buffer
 static_assert(kSmem <= 232448, "fits one SM");
 
 // ------------------------------------------------------------------------------------- small pieces
+// The whole warp calls these with the same operands and one lane's `leader` != 0: the operands stay in uniform registers.  (Inside an
+// `if (lane == 0)` each was moved there per instruction, 150 cycles a copy, and the copying warp could not keep up.)
 template <bool PAIR>
-__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, int32_t z, uint32_t bar) {
+__device__ __forceinline__ void load_box(uint32_t leader, uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, int32_t z, uint32_t bar) {
   if constexpr (PAIR)
-    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+    asm volatile("{\n\t.reg .pred go;\n\tsetp.ne.b32 go, %6, 0;\n\t"
+                 "@go cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n\t}"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar), "r"(leader) : "memory");
   else
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+    asm volatile("{\n\t.reg .pred go;\n\tsetp.ne.b32 go, %6, 0;\n\t"
+                 "@go cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n\t}"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar), "r"(leader) : "memory");
 }
 template <bool PAIR>
-__device__ __forceinline__ void load_box_of_set(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, int32_t set, uint32_t bar) {
+__device__ __forceinline__ void load_box_of_set(uint32_t leader, uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, int32_t set, uint32_t bar) {
   if constexpr (PAIR)
-    asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(set), "r"(0), "r"(bar) : "memory");
+    asm volatile("{\n\t.reg .pred go;\n\tsetp.ne.b32 go, %7, 0;\n\t"
+                 "@go cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(set), "r"(0), "r"(bar), "r"(leader) : "memory");
   else
-    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(set), "r"(0), "r"(bar) : "memory");
+    asm volatile("{\n\t.reg .pred go;\n\tsetp.ne.b32 go, %7, 0;\n\t"
+                 "@go cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(set), "r"(0), "r"(bar), "r"(leader) : "memory");
+}
+// announces `bytes` on a barrier of this CTA or, by cluster address, of the pair's even one
+template <bool PAIR>
+__device__ __forceinline__ void expect_bytes(uint32_t leader, uint32_t bar, uint32_t bytes) {
+  if constexpr (PAIR)
+    asm volatile("{\n\t.reg .pred go;\n\tsetp.ne.b32 go, %2, 0;\n\t@go mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;\n\t}"
+                 ::"r"(bar), "r"(bytes), "r"(leader) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred go;\n\tsetp.ne.b32 go, %2, 0;\n\t@go mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}"
+                 ::"r"(bar), "r"(bytes), "r"(leader) : "memory");
 }
 // `acquire` at cluster scope: what the other CTA wrote before its arrival is seen
 __device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
@@ -72,11 +87,11 @@ __device__ __forceinline__ void store32(void* p, const uint32_t (&w)[8]) {   // 
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
                "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
 }
-// 32 float32 of a row -> LIMBS bfloat16 rows; columns [0, 32) of them that lie below `width` (a multiple of 16)
-template <int LIMBS>
-__device__ __forceinline__ void store_limbs(__nv_bfloat16* to, int64_t limb, int width, const float (&f)[32]) {
+// W float32 of a row -> LIMBS bfloat16 rows; columns [0, W) of them that lie below `width` (a multiple of 16)
+template <int LIMBS, int W>
+__device__ __forceinline__ void store_limbs(__nv_bfloat16* to, int64_t limb, int width, const float (&f)[W]) {
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
+  for (int half = 0; half < W / 16; ++half) {
     if (half * 16 >= width) break;
     float r[16];
 #pragma unroll
@@ -96,42 +111,119 @@ __device__ __forceinline__ void store_limbs(__nv_bfloat16* to, int64_t limb, int
     }
   }
 }
+__device__ __forceinline__ void tmem_load(uint32_t at, uint32_t (&r)[32]) { tc::tmem_ld_32x32(at, r); }
+__device__ __forceinline__ void tmem_load(uint32_t at, uint32_t (&r)[16]) { tc::tmem_ld_32x16(at, r); }
 
-// act(g) and, for the backward pass, act'(g).  The fast forms carry a few units of 2^-22, far below the rounding to bfloat16
-// that follows; float32 results take the accurate ones.
-template <bool FAST, int ACT>
-__device__ __forceinline__ void activate(float g, float& a, float& slope) {
+// Two float32 at a time: one instruction for both halves.
+struct Two {
+  uint64_t v;
+  __device__ __forceinline__ Two() {}
+  __device__ __forceinline__ Two(float a, float b) : v(vio::pair_of(a, b)) {}
+  __device__ __forceinline__ explicit Two(float a) : v(vio::pair_of(a, a)) {}
+  __device__ __forceinline__ void get(float& a, float& b) const { vio::unpair(v, a, b); }
+};
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+  Two d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+  return d;
+}
+__device__ __forceinline__ Two operator+(Two a, Two b) {
+  Two d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+  return d;
+}
+__device__ __forceinline__ Two fma(Two a, Two b, Two c) {
+  Two d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return d;
+}
+// the hardware's 2^x and 1 / x (2 units of 2^-23 and 1), results and arguments below 2^-126 as zeros: no range handling around them
+__device__ __forceinline__ Two exp2(Two x) {
+  float a, b;
+  x.get(a, b);
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
+  return Two(a, b);
+}
+__device__ __forceinline__ Two inverse(Two x) {
+  float a, b;
+  x.get(a, b);
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
+  return Two(a, b);
+}
+
+// a = act(g) and, for the backward pass, slope = act'(g).
+//   SiLU   s = 1 / (1 + 2^(-g log2 e)):  a = g s,  a' = s + a (1 - s)
+//   GELU   E = exp(-g^2 / 2), Phi(-|g|) = E t P(t) with t = 1 / (1 + 0.3 |g| / sqrt 2), P of degree 8 fitted to
+//          erfc(z) exp(z^2) / (2 t) over t (2e-8 of the value everywhere; in float32 4e-7 up to |g| = 2, 1.5e-6 up to 5, where Phi is
+//          3e-7):  a = g Phi(g),  a' = Phi(g) + g E / sqrt(2 pi)
+// Two transcendental instructions per element either way: they share a pipe of 16 per cycle and SM, which is what is scarcest here.
+template <int ACT, bool BACK>
+__device__ __forceinline__ void activate(Two g, Two& a, Two& slope) {
   if (ACT == GNNCO_SILU) {
-    const float e = FAST ? __expf(-g) : expf(-g);
-    const float s = FAST ? __fdividef(1.0f, 1.0f + e) : 1.0f / (1.0f + e);
+    const Two s = inverse(exp2(g * Two(-1.44269504f)) + Two(1.0f));
     a = g * s;
-    slope = s + a * (1.0f - s);
+    if (BACK) slope = fma(a, fma(s, Two(-1.0f), Two(1.0f)), s);
   } else if (ACT == GNNCO_GELU) {
-    const float c = FAST ? 0.5f + 0.5f * erff(g * 0.70710678f) : 0.5f * erfcf(g * -0.70710678f);
-    const float d = FAST ? __expf(-0.5f * g * g) : expf(-0.5f * g * g);
-    a = g * c;
-    slope = fmaf(g * 0.39894228f, d, c);
+    float g0, g1, q0, q1;
+    g.get(g0, g1);
+    const Two E = exp2(g * g * Two(-0.72134752f));
+    const Two t = inverse(fma(Two(fabsf(g0), fabsf(g1)), Two(0.21213203f), Two(1.0f)));
+    Two P = fma(t, Two(-0.06476137787103653f), Two(0.24278123676776886f));
+    P = fma(t, P, Two(-0.25613829493522644f));
+    P = fma(t, P, Two(0.2738591432571411f));
+    P = fma(t, P, Two(-0.0473247766494751f));
+    P = fma(t, P, Two(0.10746278613805771f));
+    P = fma(t, P, Two(0.07416965067386627f));
+    P = fma(t, P, Two(0.08535760641098022f));
+    P = fma(t, P, Two(0.0845940038561821f));
+    (E * t * P).get(q0, q1);
+    const Two phi(g0 > 0.0f ? 1.0f - q0 : q0, g1 > 0.0f ? 1.0f - q1 : q1);
+    a = g * phi;
+    if (BACK) slope = fma(g * Two(0.39894228f), E, phi);
   } else {
-    a = g > 0.0f ? g : (g != g ? g : 0.0f);
-    slope = g > 0.0f ? 1.0f : 0.0f;
+    float g0, g1;
+    g.get(g0, g1);
+    a = Two(g0 > 0.0f ? g0 : (g0 != g0 ? g0 : 0.0f), g1 > 0.0f ? g1 : (g1 != g1 ? g1 : 0.0f));
+    if (BACK) slope = Two(g0 > 0.0f ? 1.0f : 0.0f, g1 > 0.0f ? 1.0f : 0.0f);
   }
 }
 // g, u (and dh) -> h (and dg, du), in place.  One activation for the whole loop: a branch per element would take the elements one after
 // the other, each waiting for its exponential (1.28 G elements in 3.4 ms).
-template <bool BACK, bool FAST, int ACT, int TENSORS>
-__device__ __forceinline__ void gate(float (&f)[TENSORS][32], float scale) {
+template <bool BACK, int ACT, int TENSORS, int W>
+__device__ __forceinline__ void gate(float (&f)[TENSORS][W], float scale) {
 #pragma unroll
-  for (int e = 0; e < 32; ++e) {
-    float a, slope;
-    activate<FAST, ACT>(f[0][e], a, slope);
-    const float u = f[1][e];
-    f[0][e] = a * u;
+  for (int e = 0; e < W; e += 2) {
+    const Two u(f[1][e], f[1][e + 1]);
+    Two a, slope;
+    activate<ACT, BACK>(Two(f[0][e], f[0][e + 1]), a, slope);
+    (a * u).get(f[0][e], f[0][e + 1]);
     if (BACK) {
-      const float dh = f[TENSORS - 1][e] * scale;
-      f[1][e] = dh * u * slope;
-      f[TENSORS - 1][e] = dh * a;
+      const Two dh = Two(f[TENSORS - 1][e], f[TENSORS - 1][e + 1]) * Two(scale);
+      (dh * u * slope).get(f[1][e], f[1][e + 1]);
+      (dh * a).get(f[TENSORS - 1][e], f[TENSORS - 1][e + 1]);
     }
   }
+}
+// One box (rows of 64 bytes, swizzled in units of 16 by bits 1 and 2 of the row) from a result warp's staging tile
+__device__ __forceinline__ void store_box(const CUtensorMap* map, uint32_t from, int32_t x, int32_t y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(from) : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void store_box_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void store_box_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+// 32 values of this lane's row as bfloat16 into the staging tile, and the tile's 32 rows out; whole warp
+__device__ __forceinline__ void stage_and_store(const CUtensorMap* map, uint32_t stage, int lane, int32_t x, int32_t y, const float (&f)[32]) {
+  if (lane == 0) store_box_read();                         // the tile before has left
+  __syncwarp();
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    tc::st_shared16(stage + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4), vio::pack_bf16(f[8 * q], f[8 * q + 1]),
+                    vio::pack_bf16(f[8 * q + 2], f[8 * q + 3]), vio::pack_bf16(f[8 * q + 4], f[8 * q + 5]), vio::pack_bf16(f[8 * q + 6], f[8 * q + 7]));
+  tc::fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) store_box(map, stage, x, y);
 }
 
 struct Tile {
@@ -185,6 +277,21 @@ __device__ __forceinline__ void decode(const Args& A, int t, Tile& T) {
   }
 }
 
+// the same tile, in uniform registers (every lane of the warp holds it)
+__device__ __forceinline__ Tile uniform(const Tile& t) {
+  Tile u;
+  u.row0 = __shfl_sync(0xffffffffu, (int)t.row0, 0);       // below 2^31
+  u.rows = __shfl_sync(0xffffffffu, t.rows, 0);
+  u.set = __shfl_sync(0xffffffffu, t.set, 0);
+  u.n0 = __shfl_sync(0xffffffffu, t.n0, 0);
+  u.m0 = __shfl_sync(0xffffffffu, t.m0, 0);
+  u.problem = __shfl_sync(0xffffffffu, t.problem, 0);
+  u.slot = __shfl_sync(0xffffffffu, t.slot, 0);
+  u.blocks[0] = __shfl_sync(0xffffffffu, t.blocks[0], 0);
+  u.blocks[1] = __shfl_sync(0xffffffffu, t.blocks[1], 0);
+  return u;
+}
+
 // ------------------------------------------------------------------------------------------- kernel
 template <int KIND, int LIMBS, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Maps maps, const __grid_constant__ Args A) {
@@ -234,56 +341,51 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
 
   if (warp == kCopyWarp) {
     // -------------------------------------------------------------------------------- operands
-    int g = 0, tails = 0;
+    const uint32_t leader = tc::elect_one();
+    const int rank_u = __shfl_sync(0xffffffffu, (int)rank, 0);
+    int tails = 0, slot = 0;
+    uint32_t phase = 1;                                    // of `empty`: the first round waits for nothing
     bool ok = true;
+    Tile next;
+    if (first < A.tiles) decode<KIND, PAIR>(A, first, next);
     for (int t = first; t < A.tiles && ok; t += step) {
-      Tile T;
-      decode<KIND, PAIR>(A, t, T);
+      const Tile T = uniform(next);
+      if (t + step < A.tiles) decode<KIND, PAIR>(A, t + step, next);
       const int nt = kAlongRows ? A.p[T.problem].nt : A.nt;
       for (int seg = 0; seg < 2 && ok; ++seg) {
-        // bytes of a stage of this contraction
-        uint32_t b_bytes;
-        if (KIND == kGlu) b_bytes = (2 * nt / 64 / kCtas) * kBlock;
-        else if (KIND == kGluBack && seg == 0) b_bytes = (2 * nt / 64 / kCtas) * kBlock;
-        else if (KIND == kGluBack) b_bytes = (nt / kCtas) * 128 * LIMBS;
-        else b_bytes = (nt / kCtas) * 128 * LIMBS;
-        const uint32_t bytes = kA + b_bytes;
-        for (int kb = 0; kb < T.blocks[seg]; ++kb, ++g) {
-          const int slot = g % kSlots, use = g / kSlots;
-          if (use > 0 && !wait_bar(empty + slot, (use - 1) & 1, abort_flag)) { ok = false; break; }
+        const bool twin = KIND == kGlu || (KIND == kGluBack && seg == 0);
+        const uint32_t bytes = kA + (twin ? 2 : 1) * (nt / kCtas) * 128 * LIMBS;
+        for (int kb = 0; kb < T.blocks[seg]; ++kb) {
+          if (!(ok = __all_sync(0xffffffffu, wait_bar(empty + slot, phase, abort_flag)) != 0)) break;
           const uint32_t at = sbase + slot * kSlot, bt = at + kA;
           const uint32_t announce = PAIR ? tc::map_to_cta(tc::smem_u32(full + slot), 0) : tc::smem_u32(full + slot);
           const int valid = kAlongRows ? min(64, T.rows - kb * 64) : 64;
           const uint32_t bar = valid == 64 ? announce : tc::smem_u32(tail);
-          if (lane == 0) {
-            if (PAIR) tc::mbar_arrive_expect_tx_cluster(bar, bytes);
-            else tc::mbar_arrive_expect_tx(valid == 64 ? full + slot : tail, bytes);
-            if constexpr (kAlongRows) {
-              const int32_t r = (int32_t)T.row0 + kb * 64, m = T.m0 + (int)rank * 128, n = T.n0 + (int)rank * (nt / kCtas);
-              for (int i = 0; i < 2; ++i) load_box<PAIR>(at + i * kBlock, &maps.a[T.problem], m + 64 * i, r, 0, bar);
-              for (int i = 0; i < nt / kCtas / 64; ++i) load_box<PAIR>(bt + i * kBlock, &maps.b[T.problem], n + 64 * i, r, 0, bar);
-            } else {
-              load_box<PAIR>(at, &maps.a[seg], kb * 64, (int32_t)T.row0 + (int)rank * 128, 0, bar);
-              if (KIND == kGlu || (KIND == kGluBack && seg == 0)) {
-                // gate columns, then up columns; in a pair the even CTA holds the gate's, the odd one the other's
-                const int per = nt / 64;
-                for (int i = 0; i < 2 * per / kCtas; ++i) {
-                  const int which = PAIR ? (int)rank : i / per, block = PAIR ? i : i % per;
-                  load_box_of_set<PAIR>(bt + i * kBlock, &maps.b[which], T.n0 + 64 * block, kb * 64, T.set, bar);
-                }
-              } else if (KIND == kGluBack) {
-                load_box_of_set<PAIR>(bt, &maps.b[2], kb * 64, T.n0 + (int)rank * (nt / kCtas), T.set, bar);
-              } else if (KIND == kDown) {
-                const int n = T.n0 + (int)rank * (nt / kCtas);
-                for (int i = 0; i < nt / kCtas / 64; ++i) load_box_of_set<PAIR>(bt + i * kBlock, &maps.b[0], n + 64 * i, kb * 64, T.set, bar);
-              } else {
-                load_box_of_set<PAIR>(bt, &maps.b[seg], kb * 64, T.n0 + (int)rank * (nt / kCtas), T.set, bar);
+          expect_bytes<PAIR>(leader, bar, bytes);
+          if constexpr (kAlongRows) {
+            const int32_t r = (int32_t)T.row0 + kb * 64, m = T.m0 + rank_u * 128, n = T.n0 + rank_u * (nt / kCtas);
+            load_box<PAIR>(leader, at, &maps.a[T.problem], m, r, 0, bar);
+            load_box<PAIR>(leader, at + kBlock, &maps.a[T.problem], m + 64, r, 0, bar);
+            for (int i = 0; i < nt / kCtas / 64; ++i) load_box<PAIR>(leader, bt + i * kBlock, &maps.b[T.problem], n + 64 * i, r, 0, bar);
+          } else {
+            load_box<PAIR>(leader, at, &maps.a[seg], kb * 64, (int32_t)T.row0 + rank_u * 128, 0, bar);
+            if (twin) {
+              // gate columns, then up columns; in a pair the even CTA holds the gate's, the odd one the other's
+              const int per = nt / 64;
+              for (int i = 0; i < 2 * per / kCtas; ++i) {
+                const int which = PAIR ? rank_u : i / per, block = PAIR ? i : i % per;
+                load_box_of_set<PAIR>(leader, bt + i * kBlock, &maps.b[which], T.n0 + 64 * block, kb * 64, T.set, bar);
               }
+            } else if (KIND == kDown) {
+              const int n = T.n0 + rank_u * (nt / kCtas);
+              for (int i = 0; i < nt / kCtas / 64; ++i) load_box_of_set<PAIR>(leader, bt + i * kBlock, &maps.b[0], n + 64 * i, kb * 64, T.set, bar);
+            } else {
+              load_box_of_set<PAIR>(leader, bt, &maps.b[KIND == kGluBack ? 2 : seg], kb * 64, T.n0 + rank_u * (nt / kCtas), T.set, bar);
             }
           }
           if constexpr (kAlongRows) if (valid < 64) {
             // row k of a 64-column block is 128 bytes at 128 k, whatever the swizzle does inside it
-            if (!wait_bar(tail, tails & 1, abort_flag)) { ok = false; break; }
+            if (!(ok = __all_sync(0xffffffffu, wait_bar(tail, tails & 1, abort_flag)) != 0)) break;
             ++tails;
             const int blocks = (2 + nt / kCtas / 64) * LIMBS, zero = 64 - valid;
             for (int q = lane; q < blocks * zero * 8; q += 32) {
@@ -297,21 +399,28 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
               else tc::mbar_arrive(full + slot);
             }
           }
-          __syncwarp();
+          if (++slot == kSlots) {
+            slot = 0;
+            phase ^= 1;
+          }
         }
       }
     }
+    __syncwarp();
   } else if (warp == kMmaWarp) {
     // -------------------------------------------------------------------------------- products
     if (rank == 0) {
       const uint32_t leader = tc::elect_one();
       const uint32_t tb = __shfl_sync(0xffffffffu, tmem, 0);
       constexpr int M = PAIR ? 256 : 128;
-      int g = 0, part = 0;
+      int slot = 0, part = 0;
+      uint32_t phase = 0;
       bool ok = true;
+      Tile next;
+      if (first < A.tiles) decode<KIND, PAIR>(A, first, next);
       for (int t = first; t < A.tiles && ok; t += step) {
-        Tile T;
-        decode<KIND, PAIR>(A, t, T);
+        const Tile T = uniform(next);
+        if (t + step < A.tiles) decode<KIND, PAIR>(A, t + step, next);
         const int nt = kAlongRows ? A.p[T.problem].nt : A.nt;
         bool open = false;                                 // the current part has its buffer
         for (int seg = 0; seg < 2 && ok; ++seg) {
@@ -322,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
           const uint32_t column = KIND == kGluBack && seg == 1 && !kSums ? 2 * nt : 0;
           const uint32_t b_limb = b_n_major ? 8192 : (uint32_t)(nt / kCtas) * 128;
           const int K = kAlongRows ? T.rows : A.K[seg];
-          for (int kb = 0; kb < T.blocks[seg]; ++kb, ++g) {
+          for (int kb = 0; kb < T.blocks[seg]; ++kb) {
             if (!open) {
               if (part >= 2) ok = __all_sync(0xffffffffu, wait_bar(acc_empty + (part & 1), ((part >> 1) - 1) & 1, abort_flag)) != 0;
               tc::tc_fence_after_sync();
@@ -330,8 +439,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
               open = true;
             }
             const uint32_t acc = tb + (part & 1) * kBuf + column;
-            const int slot = g % kSlots, use = g / kSlots;
-            ok = __all_sync(0xffffffffu, wait_bar(full + slot, use & 1, abort_flag)) != 0;
+            ok = __all_sync(0xffffffffu, wait_bar(full + slot, phase, abort_flag)) != 0;
             tc::tc_fence_after_sync();
             if (!ok) break;
             const uint32_t at = sbase + slot * kSlot, bt = at + kA;
@@ -364,6 +472,10 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
               ++part;
               open = false;
             }
+            if (++slot == kSlots) {
+              slot = 0;
+              phase ^= 1;
+            }
           }
         }
         if (!kSums && ok && open) {
@@ -378,13 +490,15 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
     }
   } else {
     // --------------------------------------------------------------------------------- results
-    const int quarter = warp & 3, half = warp >> 2;
+    const int quarter = warp & 3, column = warp >> 2;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const uint32_t free_bar = PAIR ? tc::map_to_cta(tc::smem_u32(acc_empty), 0) : tc::smem_u32(acc_empty);
     float* const stage = reinterpret_cast<float*>(gen + kRing + warp * kStageBytes);
-    constexpr int kGroups = KIND == kGlu ? 2 : KIND == kGluBack ? 1 : 4;     // groups of 32 columns of a warp, at most
+    const uint32_t stage_at = sbase + kRing + warp * kStageBytes;
+    constexpr int kW = KIND == kGluBack ? 16 : 32;         // columns of a group
+    constexpr int kGroups = KIND == kGlu || KIND == kGluBack ? 1 : 2;        // groups of a warp, at most
     constexpr int kTensors = KIND == kGlu ? 2 : KIND == kGluBack ? 3 : 1;
-    float v[kSums ? kGroups : 1][kTensors][32];
+    float v[kSums ? kGroups : 1][kTensors][kW];
     int part = 0;
     bool ok = true;
     auto release = [&]() {
@@ -397,12 +511,14 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
       ++part;
     };
     philox::Stream words(A.mask);
+    Tile next;
+    if (first < A.tiles) decode<KIND, PAIR>(A, first, next);
     for (int t = first; t < A.tiles && ok; t += step) {
-      Tile T;
-      decode<KIND, PAIR>(A, t, T);
+      const Tile T = next;
+      if (t + step < A.tiles) decode<KIND, PAIR>(A, t + step, next);     // its table entries arrive while this tile is worked on
       const int nt = kAlongRows ? A.p[T.problem].nt : A.nt;
       const int cols = kAlongRows ? A.p[T.problem].N : A.cols;
-      const int groups = min(nt, cols - T.n0 + 31) / 32;   // that hold columns of the result
+      const int groups = min(nt, cols - T.n0 + kW - 1) / kW;         // that hold columns of the result
       const int local = (int)rank * 128 + quarter * 32 + lane;
       const int stages = T.blocks[0] + T.blocks[1];
       if (kSums) {
@@ -411,7 +527,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
 #pragma unroll
           for (int x = 0; x < kTensors; ++x)
 #pragma unroll
-            for (int e = 0; e < 32; ++e) v[kSums ? i : 0][x][e] = 0.0f;
+            for (int e = 0; e < kW; ++e) v[kSums ? i : 0][x][e] = 0.0f;
         for (int kb = 0; kb < stages && ok; ++kb) {
           if (!wait_bar(acc_full + (part & 1), (part >> 1) & 1, abort_flag)) { ok = false; break; }
           tc::tc_fence_after_sync();
@@ -419,16 +535,19 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
           const bool second = KIND == kGluBack && kb >= T.blocks[0];
 #pragma unroll
           for (int i = 0; i < kGroups; ++i) {
-            const int c = half + 2 * i;
+            const int c = column + 4 * i;
             if (c >= groups) continue;
 #pragma unroll
             for (int x = 0; x < kTensors; ++x) {
               if (KIND == kGluBack && second != (x == 2)) continue;
-              uint32_t r[32];
-              tc::tmem_ld_32x32(acc + (x == 1 ? nt : 0) + c * 32, r);
-              tc::tmem_ld_wait();
 #pragma unroll
-              for (int e = 0; e < 32; ++e) v[kSums ? i : 0][x][e] += __uint_as_float(r[e]);
+              for (int b = 0; b < kW / 16; ++b) {
+                uint32_t r[16];
+                tmem_load(acc + (x == 1 ? nt : 0) + c * kW + 16 * b, r);
+                tc::tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[kSums ? i : 0][x][16 * b + e] += __uint_as_float(r[e]);
+              }
             }
           }
           release();
@@ -439,35 +558,52 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
       }
       if (!ok) break;
       const uint32_t acc = tmem + lanes + (part & 1) * kBuf;
+      bool holding = !kSums && stages > 0;                 // the accumulators: given back once this warp's are in registers
+      if (holding && column >= groups) {
+        release();
+        holding = false;
+      }
 #pragma unroll
       for (int i = 0; i < kGroups; ++i) {
-        const int c = half + 2 * i;
+        const int c = column + 4 * i;
         if (c >= groups) continue;
-        float (&f)[kTensors][32] = v[kSums ? i : 0];
+        float (&f)[kTensors][kW] = v[kSums ? i : 0];
         if (!kSums) {
           if (stages > 0) {
-            uint32_t r[kTensors][32];
+            uint32_t r[kTensors][kW];
 #pragma unroll
-            for (int x = 0; x < kTensors; ++x) tc::tmem_ld_32x32(acc + x * nt + c * 32, r[x]);
+            for (int x = 0; x < kTensors; ++x) tmem_load(acc + x * nt + c * kW, r[x]);
             tc::tmem_ld_wait();
 #pragma unroll
             for (int x = 0; x < kTensors; ++x)
 #pragma unroll
-              for (int e = 0; e < 32; ++e) f[x][e] = __uint_as_float(r[x][e]);
+              for (int e = 0; e < kW; ++e) f[x][e] = __uint_as_float(r[x][e]);
+            if (holding && (i + 1 == kGroups || c + 4 >= groups)) {
+              release();
+              holding = false;
+            }
           } else {
 #pragma unroll
             for (int x = 0; x < kTensors; ++x)
 #pragma unroll
-              for (int e = 0; e < 32; ++e) f[x][e] = 0.0f;
+              for (int e = 0; e < kW; ++e) f[x][e] = 0.0f;
           }
         }
-        const int c0 = T.n0 + c * 32;
+        const int c0 = T.n0 + c * kW;
         if constexpr (KIND == kGlu || KIND == kGluBack) {
-constexpr bool kBack = KIND == kGluBack;
-          if (A.act == GNNCO_SILU) gate<kBack, LIMBS == 1, GNNCO_SILU>(f, A.scale);
-          else if (A.act == GNNCO_GELU) gate<kBack, LIMBS == 1, GNNCO_GELU>(f, A.scale);
-          else gate<kBack, LIMBS == 1, GNNCO_RELU>(f, A.scale);
-          if (local < T.rows) {
+          constexpr bool kBack = KIND == kGluBack;
+          if (A.act == GNNCO_SILU) gate<kBack, GNNCO_SILU>(f, A.scale);
+          else if (A.act == GNNCO_GELU) gate<kBack, GNNCO_GELU>(f, A.scale);
+          else gate<kBack, GNNCO_RELU>(f, A.scale);
+          const int rows_here = T.rows - (local - lane);
+          if constexpr (KIND == kGlu && LIMBS == 1) {
+            if (rows_here >= 32) {
+              stage_and_store(&maps.out, stage_at, lane, c0, (int32_t)(T.row0 + local - lane), f[0]);
+              continue;
+            }
+          }
+          // limbs, and the ragged end of a subgraph, where a box would reach into the next one's rows
+          if (lane < rows_here) {
             const int64_t at = (T.row0 + local) * A.out_ld + c0;
             const int width = (int)(A.out_ld - c0);
             store_limbs<LIMBS>(A.out[0] + at, A.out_limb, width, f[0]);
@@ -528,6 +664,12 @@ constexpr bool kBack = KIND == kGluBack;
             ld = A.y_ld;
             vectors = A.y_vectors;
           }
+          if constexpr (LIMBS == 1 && !kAlongRows) {
+            if (vectors && T.rows - (local - lane) >= 32) {
+              stage_and_store(&maps.out, stage_at, lane, c0, (int32_t)(row - lane), f[0]);
+              continue;
+            }
+          }
           if (vectors && c0 + 32 <= cols) {
             if (valid) {
               if (wide) {
@@ -545,26 +687,32 @@ constexpr bool kBack = KIND == kGluBack;
               }
             }
           } else {
-            // rows that start anywhere, or end inside the group: through shared memory, so that lanes hold neighbouring columns
-            __syncwarp();
-#pragma unroll
-            for (int e = 0; e < 32; ++e) stage[lane * kStagePitch + e] = f[0][e];
-            __syncwarp();
-            const int rows_here = (kAlongRows ? A.p[T.problem].M - T.m0 : T.rows) - (local - lane);
+            // rows that start anywhere, or end inside the group: through shared memory, 16 columns at a time, so that half a warp
+            // holds neighbouring columns (column c of row r stands at c ^ (r % 16): no bank twice in a read, twice in a write)
+            const int rows_here = min(32, (kAlongRows ? A.p[T.problem].M - T.m0 : T.rows) - (local - lane));
             const int64_t row_of_warp = row - lane;
-            if (c0 + lane < cols) {
-              for (int r = 0; r < min(32, rows_here); ++r) {
-                const float x = stage[r * kStagePitch + lane];
-                const int64_t to = (row_of_warp + r) * ld + c0 + lane;
-                if (wide) static_cast<float*>(out)[to] = x;
-                else static_cast<__nv_bfloat16*>(out)[to] = __float2bfloat16_rn(x);
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+              if (LIMBS == 1 && !kAlongRows && lane == 0) store_box_read();
+              __syncwarp();
+#pragma unroll
+              for (int e = 0; e < 16; ++e) stage[lane * 16 + (e ^ (lane & 15))] = f[0][16 * b + e];
+              __syncwarp();
+              const int col = c0 + 16 * b + (lane & 15);
+              if (col < cols) {
+                for (int r = lane >> 4; r < rows_here; r += 2) {
+                  const float x = stage[r * 16 + ((lane & 15) ^ (r & 15))];
+                  const int64_t to = (row_of_warp + r) * ld + col;
+                  if (wide) static_cast<float*>(out)[to] = x;
+                  else static_cast<__nv_bfloat16*>(out)[to] = __float2bfloat16_rn(x);
+                }
               }
             }
           }
         }
       }
-      if (!kSums && stages > 0) release();
     }
+    if (LIMBS == 1 && !kAlongRows && lane == 0) store_box_done();
   }
   // ------------------------------------------------------------------------------------ the end
   if (*abort_flag) {

@@ -423,6 +423,7 @@ struct Call {
     a.scratch = scratch;
     a.chunks = c.count;
     a.chunk_rows = c.rows;
+    a.per_chunk = (int32_t)tiles_of(a.p);
     if (c.table) {
       a.chunk_begin = h->wg_begin;
       a.chunk_end = h->wg_end;

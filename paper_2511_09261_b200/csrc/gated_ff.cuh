@@ -60,6 +60,7 @@ struct Args {
   Problem p[3];
   const int32_t *chunk_begin, *chunk_end, *chunk_slot;     // nullptr: `chunks` runs of chunk_rows rows of one set
   int32_t chunks, chunk_rows;
+  int32_t per_chunk;                   // tiles of all three gradients
   int32_t out_f32, out_vectors;
   float* scratch;
   int64_t slot_stride;

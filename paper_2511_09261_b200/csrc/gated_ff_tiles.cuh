@@ -1,10 +1,12 @@
 // The tiled tensor-core products of the gated feed-forward block (kinds and formulas: gated_ff.cuh).
 //
 // One persistent CTA per SM, or a cluster of two CTAs that share a tile of 256 rows (tcgen05 .cta_group::2: each CTA stages its
-// own 128 rows of A and half of B).  Roles of the eighteen warps:
-//   warps 0-15  results: TMEM lanes 32 (w % 4) .., every fourth group of columns from w / 4 on (32 columns; 16 of g, u and dh each)
-//   warp 16     issues the MMAs (in a pair, the even CTA's)
-//   warp 17     issues the TMA copies of this CTA's operands
+// own 128 rows of A and half of B).  Roles of the twenty warps:
+//   warp 0      issues the MMAs (in a pair, the even CTA's)
+//   warp 1      issues the TMA copies of this CTA's operands
+//   warps 4-19  results: TMEM lanes 32 (w % 4) .., groups of 32 columns (16 of g, u and dh each) in turn.  In bfloat16 two teams of
+//               eight take the tiles in turn: a team waits, loads, computes and stores one after the other, so the other one's
+//               arithmetic runs meanwhile
 // A stage of the ring holds 64 of the contraction: A in the first half, B behind it, each as LIMBS matrices of bfloat16.  Operands
 // whose contraction runs along memory (x, dy, h, dg, du as A; Wd, Wg, Wu in the backward products) are k-major boxes of 64
 // columns, the others (the weights of the forward products, everything in the weight gradients) n-major boxes of 64 x 64:
@@ -28,7 +30,7 @@
 
 namespace ff {
 
-constexpr int kEpiWarps = 16, kMmaWarp = 16, kCopyWarp = 17, kThreads = 576;
+constexpr int kMmaWarp = 0, kCopyWarp = 1, kFirstEpi = 4, kEpiWarps = 16, kThreads = 640;
 constexpr uint32_t kRing = 196608;                         // 6 stages of 32 KB or 2 of 96 KB
 constexpr uint32_t kStageBytes = 32 * 16 * 4;              // a result warp's staging tile: 32 rows x 16 columns
 constexpr uint32_t kSmem = 1024 + kRing + kEpiWarps * kStageBytes + 256;
@@ -137,7 +139,7 @@ __device__ __forceinline__ Two fma(Two a, Two b, Two c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v));
   return d;
 }
-// the hardware's 2^x and 1 / x (2 units of 2^-23 and 1), results and arguments below 2^-126 as zeros: no range handling around them
+// the hardware's 2^x (2 units of 2^-23), results below 2^-126 as zeros: no range handling around it
 __device__ __forceinline__ Two exp2(Two x) {
   float a, b;
   x.get(a, b);
@@ -145,12 +147,17 @@ __device__ __forceinline__ Two exp2(Two x) {
   asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
   return Two(a, b);
 }
-__device__ __forceinline__ Two inverse(Two x) {
+// 1 / y for y in [1, 2^120], given -y: the exponent negated in the integer representation (6 % off), one Newton step with its constant
+// moved to halve the largest error (1.5e-3), one of third order (1e-9): 6e-8 with float32's roundings.  On the arithmetic pipes; a
+// second transcendental instruction per element made that pipe the bound (16 a cycle and SM: 2,048 cycles for a tile of 128 x 128,
+// as long as its products at a width of 256).
+__device__ __forceinline__ Two inverse_of_minus(Two ny) {
   float a, b;
-  x.get(a, b);
-  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
-  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
-  return Two(a, b);
+  ny.get(a, b);
+  const Two r0(__uint_as_float(0xfef34800u - __float_as_uint(a)), __uint_as_float(0xfef34800u - __float_as_uint(b)));
+  const Two r1 = r0 * fma(ny, r0, Two(2.0015f));
+  const Two h = fma(ny, r1, Two(1.0f));
+  return fma(r1, fma(h, h, h), r1);
 }
 
 // a = act(g) and, for the backward pass, slope = act'(g).
@@ -158,18 +165,21 @@ __device__ __forceinline__ Two inverse(Two x) {
 //   GELU   E = exp(-g^2 / 2), Phi(-|g|) = E t P(t) with t = 1 / (1 + 0.3 |g| / sqrt 2), P of degree 8 fitted to
 //          erfc(z) exp(z^2) / (2 t) over t (2e-8 of the value everywhere; in float32 4e-7 up to |g| = 2, 1.5e-6 up to 5, where Phi is
 //          3e-7):  a = g Phi(g),  a' = Phi(g) + g E / sqrt(2 pi)
-// Two transcendental instructions per element either way: they share a pipe of 16 per cycle and SM, which is what is scarcest here.
+// (The exponent is kept below 120: at g = -83 SiLU is -1e-34 and stays there, times |g|.)
 template <int ACT, bool BACK>
 __device__ __forceinline__ void activate(Two g, Two& a, Two& slope) {
   if (ACT == GNNCO_SILU) {
-    const Two s = inverse(exp2(g * Two(-1.44269504f)) + Two(1.0f));
+    float x0, x1;
+    (g * Two(-1.44269504f)).get(x0, x1);
+    const Two s = inverse_of_minus(fma(exp2(Two(fminf(x0, 119.0f), fminf(x1, 119.0f))), Two(-1.0f), Two(-1.0f)));
     a = g * s;
     if (BACK) slope = fma(a, fma(s, Two(-1.0f), Two(1.0f)), s);
   } else if (ACT == GNNCO_GELU) {
     float g0, g1, q0, q1;
     g.get(g0, g1);
     const Two E = exp2(g * g * Two(-0.72134752f));
-    const Two t = inverse(fma(Two(fabsf(g0), fabsf(g1)), Two(0.21213203f), Two(1.0f)));
+    // (E is 0 past |g| = 14)
+    const Two t = inverse_of_minus(fma(Two(fminf(fabsf(g0), 64.0f), fminf(fabsf(g1), 64.0f)), Two(-0.21213203f), Two(-1.0f)));
     Two P = fma(t, Two(-0.06476137787103653f), Two(0.24278123676776886f));
     P = fma(t, P, Two(-0.25613829493522644f));
     P = fma(t, P, Two(0.2738591432571411f));
@@ -227,70 +237,122 @@ __device__ __forceinline__ void stage_and_store(const CUtensorMap* map, uint32_t
 }
 
 struct Tile {
-  int64_t row0;
-  int32_t rows, set, n0, m0;
-  int32_t problem, slot;
-  int32_t blocks[2];                                       // stages of each contraction
+  int32_t row0, rows, n0, m0, problem, slot, set;
+  int32_t stages;                                          // of the first contraction
 };
+// The tiles of a CTA, t = first, first + step ..  They are numbered with the columns fastest, so that CTAs that work at the same time
+// share rows.  A short tile takes some 2,000 cycles, so the way from its number to its rows is kept off them: no divisions (the tile of
+// rows and of columns advance by a fixed step each), and the entries of the tables are requested one tile ahead, the set, which
+// hangs on the row, in the tile before.
+template <int KIND, bool PAIR, bool SETS, bool UNIFORM>
+class Walk {
+  const Args& A;
+  int32_t t, step, m, n, dm, dn;
+  int32_t a = 0, b = 0, c = 0;                             // table entries of tile t
+  int32_t a1 = 0, b1 = 0, set = 0;                         // SETS: (a, b) of the tile after t, the set of t
+  bool table;
 
-template <int KIND, bool PAIR>
-__device__ __forceinline__ void decode(const Args& A, int t, Tile& T) {
-  constexpr int TM = PAIR ? 256 : 128;
-  if constexpr (KIND == kWeights) {
-    const int per = A.p[0].m_tiles * A.p[0].n_tiles + A.p[1].m_tiles * A.p[1].n_tiles + A.p[2].m_tiles * A.p[2].n_tiles;
-    const int chunk = t / per;
-    int rest = t - chunk * per, q = 0;
-    while (rest >= A.p[q].m_tiles * A.p[q].n_tiles) {
-      rest -= A.p[q].m_tiles * A.p[q].n_tiles;
-      ++q;
+  // the same value in a uniform register (every lane of the warp holds it)
+  static __device__ __forceinline__ int32_t uniform(int32_t v) { return UNIFORM ? __shfl_sync(0xffffffffu, v, 0) : v; }
+  __device__ __forceinline__ void advance() {
+    t += step;
+    m += dm;
+    n += dn;
+    if (KIND != kWeights && n >= A.n_tiles) {
+      n -= A.n_tiles;
+      ++m;
     }
-    T.problem = q;
-    T.m0 = (rest / A.p[q].n_tiles) * TM;
-    T.n0 = (rest % A.p[q].n_tiles) * A.p[q].nt;
-    if (A.chunk_begin) {
-      T.row0 = A.chunk_begin[chunk];
-      T.rows = A.chunk_end[chunk] - (int32_t)T.row0;
-      T.slot = A.chunk_slot[chunk];
-    } else {
-      T.row0 = (int64_t)chunk * A.chunk_rows;
-      T.rows = (int32_t)min((int64_t)A.chunk_rows, A.rows - T.row0);
-      T.slot = A.chunks == 1 ? -1 : chunk;
-    }
-    T.set = T.slot < 0 ? -(T.slot + 1) : 0;
-    T.blocks[0] = (T.rows + 63) >> 6;
-    T.blocks[1] = 0;
-  } else {
-    const int m = t / A.n_tiles;
-    T.n0 = (t - m * A.n_tiles) * A.nt;
-    T.m0 = 0;
-    T.set = 0;
-    if (A.tile_row0) {
-      T.row0 = A.tile_row0[m];
-      T.rows = A.tile_rows[m];
-      T.set = A.node_part[T.row0];
-    } else {
-      T.row0 = (int64_t)m * TM;
-      T.rows = (int32_t)min((int64_t)TM, A.rows - T.row0);
-    }
-    T.blocks[0] = (A.K[0] + 63) >> 6;
-    T.blocks[1] = (A.K[1] + 63) >> 6;
   }
-}
+  __device__ __forceinline__ void fetch(int32_t& row0, int32_t& rows) {
+    if (!table || t >= A.tiles) return;
+    if (KIND == kWeights) {
+      const int32_t chunk = t / A.per_chunk;
+      row0 = A.chunk_begin[chunk];
+      rows = A.chunk_end[chunk];
+      c = A.chunk_slot[chunk];
+    } else {
+      row0 = A.tile_row0[m];
+      rows = A.tile_rows[m];
+    }
+  }
 
-// the same tile, in uniform registers (every lane of the warp holds it)
-__device__ __forceinline__ Tile uniform(const Tile& t) {
-  Tile u;
-  u.row0 = __shfl_sync(0xffffffffu, (int)t.row0, 0);       // below 2^31
-  u.rows = __shfl_sync(0xffffffffu, t.rows, 0);
-  u.set = __shfl_sync(0xffffffffu, t.set, 0);
-  u.n0 = __shfl_sync(0xffffffffu, t.n0, 0);
-  u.m0 = __shfl_sync(0xffffffffu, t.m0, 0);
-  u.problem = __shfl_sync(0xffffffffu, t.problem, 0);
-  u.slot = __shfl_sync(0xffffffffu, t.slot, 0);
-  u.blocks[0] = __shfl_sync(0xffffffffu, t.blocks[0], 0);
-  u.blocks[1] = __shfl_sync(0xffffffffu, t.blocks[1], 0);
-  return u;
-}
+ public:
+  __device__ __forceinline__ Walk(const Args& args, int first, int by) : A(args), t(first), step(by) {
+    table = KIND == kWeights ? A.chunk_begin != nullptr : A.tile_row0 != nullptr;
+    if (KIND != kWeights) {
+      m = t / A.n_tiles;
+      n = t - m * A.n_tiles;
+      dm = step / A.n_tiles;
+      dn = step - dm * A.n_tiles;
+    } else {
+      m = n = dm = dn = 0;
+    }
+    fetch(a, b);
+    if (SETS && table && t < A.tiles) {
+      set = A.node_part[a];
+      const int32_t m0 = m, n0 = n;
+      advance();
+      fetch(a1, b1);
+      t -= step;
+      m = m0;
+      n = n0;
+    }
+  }
+  __device__ __forceinline__ bool any() const { return t < A.tiles; }
+  // this tile, and on to the next
+  __device__ __forceinline__ Tile take() {
+    constexpr int TM = PAIR ? 256 : 128;
+    Tile T;
+    if constexpr (KIND == kWeights) {
+      const int32_t chunk = t / A.per_chunk;
+      int rest = t - chunk * A.per_chunk, q = 0;
+      while (rest >= A.p[q].m_tiles * A.p[q].n_tiles) {
+        rest -= A.p[q].m_tiles * A.p[q].n_tiles;
+        ++q;
+      }
+      T.problem = uniform(q);
+      T.m0 = uniform((rest / A.p[q].n_tiles) * TM);
+      T.n0 = uniform((rest % A.p[q].n_tiles) * A.p[q].nt);
+      if (table) {
+        T.row0 = uniform(a);
+        T.rows = uniform(b - a);
+        T.slot = uniform(c);
+      } else {
+        T.row0 = uniform(chunk * A.chunk_rows);
+        T.rows = uniform((int32_t)min((int64_t)A.chunk_rows, A.rows - (int64_t)chunk * A.chunk_rows));
+        T.slot = A.chunks == 1 ? -1 : uniform(chunk);
+      }
+      T.set = T.slot < 0 ? -(T.slot + 1) : 0;
+      T.stages = (T.rows + 63) >> 6;
+      advance();
+      fetch(a, b);
+    } else {
+      T.m0 = T.problem = T.slot = 0;
+      T.n0 = uniform(n * A.nt);
+      T.row0 = uniform(table ? a : m * TM);
+      T.rows = uniform(table ? b : (int32_t)min((int64_t)TM, A.rows - (int64_t)m * TM));
+      T.set = SETS ? uniform(set) : 0;
+      T.stages = (A.K[0] + 63) >> 6;
+      advance();
+      if (SETS) {
+        a = a1;
+        b = b1;
+        if (table && any()) set = A.node_part[a];
+        const int32_t m0 = m, n0 = n;
+        advance();
+        fetch(a1, b1);
+        t -= step;
+        m = m0;
+        n = n0;
+      } else {
+        fetch(a, b);
+      }
+    }
+    return T;
+  }
+  // a tile whose rows do not matter
+  __device__ __forceinline__ void skip() { t += step; }
+};
 
 // ------------------------------------------------------------------------------------------- kernel
 template <int KIND, int LIMBS, bool PAIR>
@@ -301,6 +363,8 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
   constexpr int kCtas = PAIR ? 2 : 1;
   constexpr bool kAlongRows = KIND == kWeights;
   constexpr bool kSums = LIMBS > 1;                        // stages are added up in registers
+  constexpr int kTeams = LIMBS == 1 && !kAlongRows ? 2 : 1;                  // of result warps, tiles in turn
+  constexpr int kColumns = kEpiWarps / 4 / kTeams;         // warps of a team that share TMEM lanes
 
   extern __shared__ uint8_t smem_raw[];
   const uint32_t sbase = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -323,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
     }
     for (int i = 0; i < 2; ++i) {
       tc::mbar_init(acc_full + i, 1);
-      tc::mbar_init(acc_empty + i, kCtas * kEpiWarps);
+      tc::mbar_init(acc_empty + i, kCtas * kEpiWarps / kTeams);
     }
     tc::mbar_init(tail, 1);
     *abort_flag = 0;
@@ -338,6 +402,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
   if (PAIR) tc::cluster_sync_all();
   tc::tc_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
+  const int more = kAlongRows ? 0 : (A.K[1] + 63) >> 6;    // stages of the second contraction
 
   if (warp == kCopyWarp) {
     // -------------------------------------------------------------------------------- operands
@@ -346,16 +411,16 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
     int tails = 0, slot = 0;
     uint32_t phase = 1;                                    // of `empty`: the first round waits for nothing
     bool ok = true;
-    Tile next;
-    if (first < A.tiles) decode<KIND, PAIR>(A, first, next);
-    for (int t = first; t < A.tiles && ok; t += step) {
-      const Tile T = uniform(next);
-      if (t + step < A.tiles) decode<KIND, PAIR>(A, t + step, next);
+    Walk<KIND, PAIR, !kAlongRows, true> walk(A, first, step);
+    while (walk.any() && ok) {
+      const Tile T = walk.take();
+      const int set = T.set;
       const int nt = kAlongRows ? A.p[T.problem].nt : A.nt;
       for (int seg = 0; seg < 2 && ok; ++seg) {
         const bool twin = KIND == kGlu || (KIND == kGluBack && seg == 0);
         const uint32_t bytes = kA + (twin ? 2 : 1) * (nt / kCtas) * 128 * LIMBS;
-        for (int kb = 0; kb < T.blocks[seg]; ++kb) {
+        const int stages = seg == 0 ? T.stages : more;
+        for (int kb = 0; kb < stages; ++kb) {
           if (!(ok = __all_sync(0xffffffffu, wait_bar(empty + slot, phase, abort_flag)) != 0)) break;
           const uint32_t at = sbase + slot * kSlot, bt = at + kA;
           const uint32_t announce = PAIR ? tc::map_to_cta(tc::smem_u32(full + slot), 0) : tc::smem_u32(full + slot);
@@ -374,13 +439,13 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
               const int per = nt / 64;
               for (int i = 0; i < 2 * per / kCtas; ++i) {
                 const int which = PAIR ? rank_u : i / per, block = PAIR ? i : i % per;
-                load_box_of_set<PAIR>(leader, bt + i * kBlock, &maps.b[which], T.n0 + 64 * block, kb * 64, T.set, bar);
+                load_box_of_set<PAIR>(leader, bt + i * kBlock, &maps.b[which], T.n0 + 64 * block, kb * 64, set, bar);
               }
             } else if (KIND == kDown) {
               const int n = T.n0 + rank_u * (nt / kCtas);
-              for (int i = 0; i < nt / kCtas / 64; ++i) load_box_of_set<PAIR>(leader, bt + i * kBlock, &maps.b[0], n + 64 * i, kb * 64, T.set, bar);
+              for (int i = 0; i < nt / kCtas / 64; ++i) load_box_of_set<PAIR>(leader, bt + i * kBlock, &maps.b[0], n + 64 * i, kb * 64, set, bar);
             } else {
-              load_box_of_set<PAIR>(leader, bt, &maps.b[KIND == kGluBack ? 2 : seg], kb * 64, T.n0 + rank_u * (nt / kCtas), T.set, bar);
+              load_box_of_set<PAIR>(leader, bt, &maps.b[KIND == kGluBack ? 2 : seg], kb * 64, T.n0 + rank_u * (nt / kCtas), set, bar);
             }
           }
           if constexpr (kAlongRows) if (valid < 64) {
@@ -416,11 +481,15 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
       int slot = 0, part = 0;
       uint32_t phase = 0;
       bool ok = true;
-      Tile next;
-      if (first < A.tiles) decode<KIND, PAIR>(A, first, next);
-      for (int t = first; t < A.tiles && ok; t += step) {
-        const Tile T = uniform(next);
-        if (t + step < A.tiles) decode<KIND, PAIR>(A, t + step, next);
+      Walk<KIND, PAIR, false, true> walk(A, first, step);
+      while (walk.any() && ok) {
+        Tile T = {};
+        if (kAlongRows) {
+          T = walk.take();
+        } else {                                           // every tile is the same here
+          T.stages = (A.K[0] + 63) >> 6;
+          walk.skip();
+        }
         const int nt = kAlongRows ? A.p[T.problem].nt : A.nt;
         bool open = false;                                 // the current part has its buffer
         for (int seg = 0; seg < 2 && ok; ++seg) {
@@ -431,7 +500,8 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
           const uint32_t column = KIND == kGluBack && seg == 1 && !kSums ? 2 * nt : 0;
           const uint32_t b_limb = b_n_major ? 8192 : (uint32_t)(nt / kCtas) * 128;
           const int K = kAlongRows ? T.rows : A.K[seg];
-          for (int kb = 0; kb < T.blocks[seg]; ++kb) {
+          const int stages = seg == 0 ? T.stages : more;
+          for (int kb = 0; kb < stages; ++kb) {
             if (!open) {
               if (part >= 2) ok = __all_sync(0xffffffffu, wait_bar(acc_empty + (part & 1), ((part >> 1) - 1) & 1, abort_flag)) != 0;
               tc::tc_fence_after_sync();
@@ -449,14 +519,18 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
             constexpr uint64_t a_step = kAlongRows ? 128 : 2, a_limb = (kAlongRows ? 8192 : 16384) / 16;
             const uint64_t b_step = b_n_major ? 128 : 2;
             if constexpr (LIMBS == 1) {
-              for (int k = 0; k < steps; ++k) tc::mma_f16<PAIR, false>(leader, acc, a0 + a_step * k, b0 + b_step * k, idesc, kb + k != 0 || (KIND == kDx && seg == 1));
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                if (k < steps) tc::mma_f16<PAIR, false>(leader, acc, a0 + a_step * k, b0 + b_step * k, idesc, kb + k != 0 || (KIND == kDx && seg == 1));
             } else {
               // a1 b3, a2 b2, a3 b1, a1 b2, a2 b1, then a1 b1
 #pragma unroll
               for (int q = 0; q < 6; ++q) {
                 const int i = q == 1 || q == 4 ? 1 : q == 2 ? 2 : 0, j = q == 0 ? 2 : q == 1 || q == 3 ? 1 : 0;
                 const uint64_t a = a0 + i * a_limb, b = b0 + (uint64_t)(j * b_limb / 16);
-                for (int k = 0; k < steps; ++k) tc::mma_f16<PAIR, false>(leader, acc, a + a_step * k, b + b_step * k, idesc, q + k != 0);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  if (k < steps) tc::mma_f16<PAIR, false>(leader, acc, a + a_step * k, b + b_step * k, idesc, q + k != 0);
               }
             }
             if (leader) {
@@ -488,18 +562,18 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
         }
       }
     }
-  } else {
+  } else if (warp >= kFirstEpi) {
     // --------------------------------------------------------------------------------- results
-    const int quarter = warp & 3, column = warp >> 2;
+    const int quarter = warp & 3, column = ((warp - kFirstEpi) >> 2) % kColumns, team = ((warp - kFirstEpi) >> 2) / kColumns;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const uint32_t free_bar = PAIR ? tc::map_to_cta(tc::smem_u32(acc_empty), 0) : tc::smem_u32(acc_empty);
-    float* const stage = reinterpret_cast<float*>(gen + kRing + warp * kStageBytes);
-    const uint32_t stage_at = sbase + kRing + warp * kStageBytes;
+    float* const stage = reinterpret_cast<float*>(gen + kRing + (warp - kFirstEpi) * kStageBytes);
+    const uint32_t stage_at = sbase + kRing + (warp - kFirstEpi) * kStageBytes;
     constexpr int kW = KIND == kGluBack ? 16 : 32;         // columns of a group
-    constexpr int kGroups = KIND == kGlu || KIND == kGluBack ? 1 : 2;        // groups of a warp, at most
+    constexpr int kGroups = (KIND == kGlu || KIND == kGluBack ? 4 : 8) / kColumns;   // groups of a warp, at most
     constexpr int kTensors = KIND == kGlu ? 2 : KIND == kGluBack ? 3 : 1;
     float v[kSums ? kGroups : 1][kTensors][kW];
-    int part = 0;
+    int part = team;
     bool ok = true;
     auto release = [&]() {
       tc::tc_fence_before_sync();
@@ -508,19 +582,17 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
         if (PAIR) tc::mbar_arrive_cluster(free_bar + (part & 1) * 8);
         else tc::mbar_arrive(acc_empty + (part & 1));
       }
-      ++part;
+      part += kTeams;
     };
     philox::Stream words(A.mask);
-    Tile next;
-    if (first < A.tiles) decode<KIND, PAIR>(A, first, next);
-    for (int t = first; t < A.tiles && ok; t += step) {
-      const Tile T = next;
-      if (t + step < A.tiles) decode<KIND, PAIR>(A, t + step, next);     // its table entries arrive while this tile is worked on
+    Walk<KIND, PAIR, false, false> walk(A, first + team * step, kTeams * step);
+    while (walk.any() && ok) {
+      const Tile T = walk.take();
       const int nt = kAlongRows ? A.p[T.problem].nt : A.nt;
       const int cols = kAlongRows ? A.p[T.problem].N : A.cols;
       const int groups = min(nt, cols - T.n0 + kW - 1) / kW;         // that hold columns of the result
       const int local = (int)rank * 128 + quarter * 32 + lane;
-      const int stages = T.blocks[0] + T.blocks[1];
+      const int stages = T.stages + more;
       if (kSums) {
 #pragma unroll
         for (int i = 0; i < kGroups; ++i)
@@ -532,10 +604,10 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
           if (!wait_bar(acc_full + (part & 1), (part >> 1) & 1, abort_flag)) { ok = false; break; }
           tc::tc_fence_after_sync();
           const uint32_t acc = tmem + lanes + (part & 1) * kBuf;
-          const bool second = KIND == kGluBack && kb >= T.blocks[0];
+          const bool second = KIND == kGluBack && kb >= T.stages;
 #pragma unroll
           for (int i = 0; i < kGroups; ++i) {
-            const int c = column + 4 * i;
+            const int c = column + kColumns * i;
             if (c >= groups) continue;
 #pragma unroll
             for (int x = 0; x < kTensors; ++x) {
@@ -565,7 +637,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
       }
 #pragma unroll
       for (int i = 0; i < kGroups; ++i) {
-        const int c = column + 4 * i;
+        const int c = column + kColumns * i;
         if (c >= groups) continue;
         float (&f)[kTensors][kW] = v[kSums ? i : 0];
         if (!kSums) {
@@ -578,7 +650,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
             for (int x = 0; x < kTensors; ++x)
 #pragma unroll
               for (int e = 0; e < kW; ++e) f[x][e] = __uint_as_float(r[x][e]);
-            if (holding && (i + 1 == kGroups || c + 4 >= groups)) {
+            if (holding && (i + 1 == kGroups || c + kColumns >= groups)) {
               release();
               holding = false;
             }
@@ -604,7 +676,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
           }
           // limbs, and the ragged end of a subgraph, where a box would reach into the next one's rows
           if (lane < rows_here) {
-            const int64_t at = (T.row0 + local) * A.out_ld + c0;
+            const int64_t at = (int64_t)(T.row0 + local) * A.out_ld + c0;
             const int width = (int)(A.out_ld - c0);
             store_limbs<LIMBS>(A.out[0] + at, A.out_limb, width, f[0]);
             if (KIND == kGluBack) {
@@ -618,7 +690,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
           const bool wide = kAlongRows ? (part_sum || A.out_f32) : A.y_f32;
           const bool valid = kAlongRows ? T.m0 + local < A.p[T.problem].M : local < T.rows;
           const float scale = kAlongRows ? A.p[T.problem].scale : A.scale;
-          const int64_t row = kAlongRows ? T.m0 + local : T.row0 + local;
+          const int64_t row = (kAlongRows ? T.m0 : T.row0) + local;
           if (!(KIND == kDown && A.masked)) {
 #pragma unroll
             for (int e = 0; e < 32; ++e) f[0][e] *= scale;

@@ -330,25 +330,25 @@ struct Call {
 
   // h (and, with dy, dg and du) from x
   int32_t gates(const Operand& x, const Operand* dy, const Operand& wg, const Operand& wu, const Operand& wd, const Operand* out) {
-    auto nt_of = [&](bool pair) { return !dy && pair && d->H > 64 ? 128 : 64; };
+    auto nt_of = [&](bool pair) { return pair && (dy ? limbs == 1 : d->H > 64) ? 128 : 64; };
     const bool pair = use_pairs(row_tiles(true) * blocks_of(d->H, nt_of(true)));
     Args a = {};
     Maps m;
     rows_of(&a, pair);
     a.nt = nt_of(pair);
     a.n_tiles = (int32_t)blocks_of(d->H, a.nt);
-    a.K[0] = d->F;
-    a.K[1] = dy ? d->F_out : 0;
+    a.K[0] = dy ? d->F_out : d->F;
+    a.K[1] = dy ? d->F : 0;
     a.cols = d->H;
     a.act = d->act;
     a.scale = dy && drops ? jobs.mask.scale : 1.0f;
     for (int k = 0; k < (dy ? 3 : 1); ++k) a.out[k] = const_cast<__nv_bfloat16*>(out[k].p);
     a.out_ld = out[0].ld;
     a.out_limb = out[0].limb;
-    bool ok = map_rows(&m.a[0], x.p, d->rows, d->F, x.ld, x.limb, limbs, 128) &&
+    bool ok = map_rows(&m.a[dy ? 1 : 0], x.p, d->rows, d->F, x.ld, x.limb, limbs, 128) &&
               map_sets(&m.b[0], wg.p, d->sets, d->F, d->H, wg.ld, limbs, 64) && map_sets(&m.b[1], wu.p, d->sets, d->F, d->H, wu.ld, limbs, 64);
     if (dy)
-      ok = ok && map_rows(&m.a[1], dy->p, d->rows, d->F_out, dy->ld, dy->limb, limbs, 128) &&
+      ok = ok && map_rows(&m.a[0], dy->p, d->rows, d->F_out, dy->ld, dy->limb, limbs, 128) &&
            map_sets(&m.b[2], wd.p, d->sets, d->H, d->F_out, wd.ld, limbs, pair ? a.nt / 2 : a.nt);
     else if (limbs == 1) ok = ok && map_out(&m.out, out[0].p, d->rows, d->H, out[0].ld);
     if (!ok) return GNNCO_CUDA_ERROR;

@@ -16,7 +16,7 @@ namespace ff {
 
 // The tiled products.
 //   kGlu      h                                A = x            B = Wg, Wu
-//   kGluBack  h, dg, du                        A = x, dy'       B = Wg, Wu, Wd
+//   kGluBack  h, dg, du                        A = dy', x       B = Wd (2), Wg, Wu (0, 1)
 //   kDown     y                                A = h            B = Wd
 //   kDx       dx                               A = dg, du       B = Wg, Wu
 //   kWeights  dWg, dWu, dWd                    both operands are read along the rows that are summed

@@ -16,6 +16,8 @@
 //
 // LIMBS = 1 (bfloat16): a tile's products are summed in one of two TMEM buffers of 256 columns, so that the next tile is multiplied
 // while this one is converted and stored.
+// kGluBack has three accumulators of 128 columns (wide tiles: at 64 columns the copies, not the products, took the time).  Four such
+// quarters of TMEM go round: dh of the next tile is summed in the free one while this tile's are converted.
 // LIMBS = 3 (float32): a = a1 + a2 + a3 in bfloat16; the six products a_i b_j with i + j <= 4 are summed, what is left out is
 // below 2^-24 of the product.  The tensor core cuts off low bits whenever it adds to an accumulator, so sums stay short:
 // every stage starts an accumulator of its own (buffers in turn), adds the five small products first and the large one last, and the
@@ -84,6 +86,17 @@ __device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, volatil
     }
   }
   return true;
+}
+template <bool PAIR>
+__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+  if (PAIR) tc::mma_bf16_pair(d, a, b, idesc, accumulate);
+  else tc::mma_bf16(d, a, b, idesc, accumulate);
+}
+// everything multiplied so far arrives on this barrier, in both CTAs of a pair
+template <bool PAIR>
+__device__ __forceinline__ void commit(uint64_t* bar) {
+  if (PAIR) tc::mma_commit_pair(bar, 3);
+  else tc::mma_commit(bar);
 }
 __device__ __forceinline__ void store32(void* p, const uint32_t (&w)[8]) {   // 32-byte aligned
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
@@ -363,7 +376,8 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
   constexpr int kCtas = PAIR ? 2 : 1;
   constexpr bool kAlongRows = KIND == kWeights;
   constexpr bool kSums = LIMBS > 1;                        // stages are added up in registers
-  constexpr int kTeams = LIMBS == 1 && !kAlongRows ? 2 : 1;                  // of result warps, tiles in turn
+  constexpr bool kQuarters = KIND == kGluBack && !kSums;   // accumulators take quarters of TMEM in turn
+  constexpr int kTeams = LIMBS == 1 && !kAlongRows && !kQuarters ? 2 : 1;    // of result warps, tiles in turn
   constexpr int kColumns = kEpiWarps / 4 / kTeams;         // warps of a team that share TMEM lanes
 
   extern __shared__ uint8_t smem_raw[];
@@ -417,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
       const int set = T.set;
       const int nt = kAlongRows ? A.p[T.problem].nt : A.nt;
       for (int seg = 0; seg < 2 && ok; ++seg) {
-        const bool twin = KIND == kGlu || (KIND == kGluBack && seg == 0);
+        const bool twin = KIND == kGlu || (KIND == kGluBack && seg == 1);
         const uint32_t bytes = kA + (twin ? 2 : 1) * (nt / kCtas) * 128 * LIMBS;
         const int stages = seg == 0 ? T.stages : more;
         for (int kb = 0; kb < stages; ++kb) {
@@ -434,7 +448,11 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
             for (int i = 0; i < nt / kCtas / 64; ++i) load_box<PAIR>(leader, bt + i * kBlock, &maps.b[T.problem], n + 64 * i, r, 0, bar);
           } else {
             load_box<PAIR>(leader, at, &maps.a[seg], kb * 64, (int32_t)T.row0 + rank_u * 128, 0, bar);
-            if (twin) {
+            if (twin && kQuarters) {
+              // 64 gate columns, then the same up columns; in a pair each CTA holds half of both
+              load_box_of_set<PAIR>(leader, bt, &maps.b[0], T.n0 + rank_u * 64, kb * 64, set, bar);
+              load_box_of_set<PAIR>(leader, bt + kBlock, &maps.b[1], T.n0 + rank_u * 64, kb * 64, set, bar);
+            } else if (twin) {
               // gate columns, then up columns; in a pair the even CTA holds the gate's, the odd one the other's
               const int per = nt / 64;
               for (int i = 0; i < 2 * per / kCtas; ++i) {
@@ -474,14 +492,12 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
     __syncwarp();
   } else if (warp == kMmaWarp) {
     // -------------------------------------------------------------------------------- products
-    if (rank == 0) {
-      const uint32_t leader = tc::elect_one();
-      const uint32_t tb = __shfl_sync(0xffffffffu, tmem, 0);
+    if (rank == 0 && tc::elect_one()) {                    // one thread
       constexpr int M = PAIR ? 256 : 128;
       int slot = 0, part = 0;
       uint32_t phase = 0;
       bool ok = true;
-      Walk<KIND, PAIR, false, true> walk(A, first, step);
+      Walk<KIND, PAIR, false, false> walk(A, first, step);
       while (walk.any() && ok) {
         Tile T = {};
         if (kAlongRows) {
@@ -493,23 +509,28 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
         const int nt = kAlongRows ? A.p[T.problem].nt : A.nt;
         bool open = false;                                 // the current part has its buffer
         for (int seg = 0; seg < 2 && ok; ++seg) {
-          const bool twin = KIND == kGlu || (KIND == kGluBack && seg == 0);
+          const bool twin = KIND == kGlu || (KIND == kGluBack && seg == 1);
           const bool b_n_major = twin || KIND == kDown || KIND == kWeights;
-          const int N = twin ? 2 * nt : nt;
+          const int N = twin && !kQuarters ? 2 * nt : nt;
           const uint32_t idesc = tc::idesc_bf16_f32(M, N, kAlongRows, b_n_major);
-          const uint32_t column = KIND == kGluBack && seg == 1 && !kSums ? 2 * nt : 0;
+          if (kQuarters && seg == 1) {
+            // g and u take the quarters that dh and g of the tile before held
+            if (part >= 1) ok = wait_bar(acc_empty + ((part - 1) & 1), ((part - 1) >> 1) & 1, abort_flag);
+            tc::tc_fence_after_sync();
+            if (!ok) break;
+          }
           const uint32_t b_limb = b_n_major ? 8192 : (uint32_t)(nt / kCtas) * 128;
           const int K = kAlongRows ? T.rows : A.K[seg];
           const int stages = seg == 0 ? T.stages : more;
           for (int kb = 0; kb < stages; ++kb) {
             if (!open) {
-              if (part >= 2) ok = __all_sync(0xffffffffu, wait_bar(acc_empty + (part & 1), ((part >> 1) - 1) & 1, abort_flag)) != 0;
+              if (part >= 2 && !kQuarters) ok = wait_bar(acc_empty + (part & 1), ((part >> 1) - 1) & 1, abort_flag);
               tc::tc_fence_after_sync();
               if (!ok) break;
               open = true;
             }
-            const uint32_t acc = tb + (part & 1) * kBuf + column;
-            ok = __all_sync(0xffffffffu, wait_bar(full + slot, phase, abort_flag)) != 0;
+            const uint32_t acc = tmem + (kQuarters ? ((3 * part + seg) & 3) * 128 : (part & 1) * kBuf);
+            ok = wait_bar(full + slot, phase, abort_flag);
             tc::tc_fence_after_sync();
             if (!ok) break;
             const uint32_t at = sbase + slot * kSlot, bt = at + kA;
@@ -521,7 +542,13 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
             if constexpr (LIMBS == 1) {
 #pragma unroll
               for (int k = 0; k < 4; ++k)
-                if (k < steps) tc::mma_f16<PAIR, false>(leader, acc, a0 + a_step * k, b0 + b_step * k, idesc, kb + k != 0 || (KIND == kDx && seg == 1));
+                if (k < steps) multiply<PAIR>(acc, a0 + a_step * k, b0 + b_step * k, idesc, kb + k != 0 || (KIND == kDx && seg == 1));
+              if (kQuarters && seg == 1) {
+                const uint32_t acc2 = tmem + ((3 * part + 2) & 3) * 128;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  if (k < steps) multiply<PAIR>(acc2, a0 + a_step * k, b0 + kBlock / 16 + b_step * k, idesc, kb + k != 0);
+              }
             } else {
               // a1 b3, a2 b2, a3 b1, a1 b2, a2 b1, then a1 b1
 #pragma unroll
@@ -530,19 +557,12 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
                 const uint64_t a = a0 + i * a_limb, b = b0 + (uint64_t)(j * b_limb / 16);
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                  if (k < steps) tc::mma_f16<PAIR, false>(leader, acc, a + a_step * k, b + b_step * k, idesc, q + k != 0);
+                  if (k < steps) multiply<PAIR>(acc, a + a_step * k, b + b_step * k, idesc, q + k != 0);
               }
             }
-            if (leader) {
-              if (PAIR) tc::mma_commit_pair(empty + slot, 3);
-              else tc::mma_commit(empty + slot);
-              if (kSums) {
-                if (PAIR) tc::mma_commit_pair(acc_full + (part & 1), 3);
-                else tc::mma_commit(acc_full + (part & 1));
-              }
-            }
-            __syncwarp();
+            commit<PAIR>(empty + slot);
             if (kSums) {
+              commit<PAIR>(acc_full + (part & 1));
               ++part;
               open = false;
             }
@@ -553,11 +573,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
           }
         }
         if (!kSums && ok && open) {
-          if (leader) {
-            if (PAIR) tc::mma_commit_pair(acc_full + (part & 1), 3);
-            else tc::mma_commit(acc_full + (part & 1));
-          }
-          __syncwarp();
+          commit<PAIR>(acc_full + (part & 1));
           ++part;
         }
       }
@@ -570,7 +586,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
     float* const stage = reinterpret_cast<float*>(gen + kRing + (warp - kFirstEpi) * kStageBytes);
     const uint32_t stage_at = sbase + kRing + (warp - kFirstEpi) * kStageBytes;
     constexpr int kW = KIND == kGluBack ? 16 : 32;         // columns of a group
-    constexpr int kGroups = (KIND == kGlu || KIND == kGluBack ? 4 : 8) / kColumns;   // groups of a warp, at most
+    constexpr int kGroups = (KIND == kGlu || (KIND == kGluBack && kSums) ? 4 : 8) / kColumns;      // groups of a warp, at most
     constexpr int kTensors = KIND == kGlu ? 2 : KIND == kGluBack ? 3 : 1;
     float v[kSums ? kGroups : 1][kTensors][kW];
     int part = team;
@@ -604,14 +620,14 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
           if (!wait_bar(acc_full + (part & 1), (part >> 1) & 1, abort_flag)) { ok = false; break; }
           tc::tc_fence_after_sync();
           const uint32_t acc = tmem + lanes + (part & 1) * kBuf;
-          const bool second = KIND == kGluBack && kb >= T.stages;
+          const bool second = kb >= T.stages;                // of g, u and dh, the stages of dh come first
 #pragma unroll
           for (int i = 0; i < kGroups; ++i) {
             const int c = column + kColumns * i;
             if (c >= groups) continue;
 #pragma unroll
             for (int x = 0; x < kTensors; ++x) {
-              if (KIND == kGluBack && second != (x == 2)) continue;
+              if (KIND == kGluBack && second == (x == 2)) continue;
 #pragma unroll
               for (int b = 0; b < kW / 16; ++b) {
                 uint32_t r[16];
@@ -644,7 +660,8 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
           if (stages > 0) {
             uint32_t r[kTensors][kW];
 #pragma unroll
-            for (int x = 0; x < kTensors; ++x) tmem_load(acc + x * nt + c * kW, r[x]);
+            for (int x = 0; x < kTensors; ++x)
+              tmem_load(kQuarters ? tmem + lanes + ((3 * part + (x + 1) % 3) & 3) * 128 + c * kW : acc + x * nt + c * kW, r[x]);
             tc::tmem_ld_wait();
 #pragma unroll
             for (int x = 0; x < kTensors; ++x)

@@ -1,6 +1,7 @@
 // The gated feed-forward block, forward and backward: entry points, work areas, copies of operands and the choice of kernels
 // (formulas and kinds of products: gated_ff.cuh; the products: gated_ff_tiles.cuh).
 //
+// Up to four rows with one set of weights: gated_ff_rows.cu.  Else
 // Forward:   [operands as limbs]   h = act(x Wg) .* (x Wu)   y = drop(h Wd)
 // Backward:  [operands as limbs]   h, dg, du (g and u are computed again: nothing but x is kept from the forward pass, which at
 //            widths up to some 400 is also faster than writing and reading them)   dx   the weight gradients   [their partial sums]
@@ -16,6 +17,9 @@
 namespace ff {
 int32_t launch_tiles_bf16(Kind kind, bool pair, const Maps& maps, const Args& args, int device, int sms, cudaStream_t st);
 int32_t launch_tiles_f32(Kind kind, bool pair, const Maps& maps, const Args& args, int device, int sms, cudaStream_t st);
+bool few_rows(const gnnco_gated_ff_desc* d, int sms);
+int32_t launch_few_rows(gnnco_handle* h, const gnnco_gated_ff_desc* d, const philox::Mask* mask, float* hidden, void* y, int64_t y_ld,
+                        cudaStream_t st);
 }  // namespace ff
 
 namespace {
@@ -226,6 +230,11 @@ Chunks chunks_of(const gnnco_handle* h, const gnnco_gated_ff_desc* d) {
 Work lay_out(const gnnco_handle* h, const gnnco_gated_ff_desc* d, bool backward) {
   Work w;
   const int64_t limbs = limbs_of(d), sets = d->sets;
+  if (!backward && ff::few_rows(d, h->sm_count)) {         // h in float32
+    w.h = 0;
+    w.total = align_up((size_t)d->rows * d->H * 4);
+    return w;
+  }
   auto take = [&](bool needed, int64_t elements) {
     if (!needed) return kNone;
     const size_t at = w.total;
@@ -497,6 +506,12 @@ extern "C" int32_t gnnco_gated_ff(gnnco_handle* h, const gnnco_gated_ff_desc* d,
   c.limbs = limbs_of(d);
   ProfScope prof_(h, K_GATED_FF, c.st);
   char* const base = static_cast<char*>(ws);
+  if (ff::few_rows(d, h->sm_count)) {
+    const int32_t r = ff::launch_few_rows(h, d, c.drops ? &c.jobs.mask : nullptr, reinterpret_cast<float*>(base + w.h), y, y_ld, c.st);
+    if (r != GNNCO_OK) return r;
+    GNNCO_LAUNCH_CHECK();
+    return GNNCO_OK;
+  }
   const int64_t sets = d->sets;
   const Operand x = c.operand(d->x, d->rows, d->F, d->x_ld, d->feat_dtype, false, base + w.x);
   const Operand wg = c.operand(d->w_gate, sets * d->F, d->H, d->H, d->w_dtype, false, base + w.wg);

@@ -338,3 +338,27 @@ def test_gradients_against_differences(single):
         got = (d[name].double() * v.double()).sum().item()
         # the third derivative along v leaves e^2 / 6 of its size (the loss is of order 100), rounding 2^-24 * 100 / e
         assert abs(got - want) <= 0.03 + 0.003 * abs(want), name
+
+
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5])
+@pytest.mark.parametrize("F,H,Fo", [(1, 1, 1), (40, 56, 24), (1024, 4096, 1024), (99, 343, 51), (2048, 64, 512), (64, 3000, 8), (5000, 33, 16)])
+@pytest.mark.parametrize("dtype,w_dtype", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32")])
+def test_few_rows(single, rows, F, H, Fo, dtype, w_dtype):
+    """One to four rows have kernels of their own; a row does not depend on the others."""
+    import torch
+    t = make(rows, 1, F, H, Fo, dtype, seed=rows, w_dtype=w_dtype)
+    act = ("silu", "gelu")[rows % 2]
+    y = check_forward(single, t, None, act, dtype)
+    drop = gnnco.Dropout(0.4, 3, layer=1)
+    mask = ref.keep(rows, Fo, 0.4, 3, 1) / 0.6
+    z = check_forward(single, t, None, act, dtype, drop, mask)
+    assert np.array_equal(host(z) != 0, (mask != 0) & (host(y) != 0))
+    if rows == 4:
+        x = t[0].clone()
+        x[1] = float("nan")
+        assert torch.equal(single.gated_ff(x, *t[2:], act=act)[[0, 2, 3]], y[[0, 2, 3]])
+        wide = torch.empty(rows, F + 3, dtype=t[0].dtype, device="cuda")
+        wide[:, 1:F + 1] = t[0]
+        out = torch.empty(rows, Fo + 5, dtype=t[0].dtype, device="cuda")
+        single.gated_ff(wide[:, 1:F + 1], *t[2:], act=act, out=out[:, 2:Fo + 2])
+        assert torch.equal(out[:, 2:Fo + 2], y)

@@ -17,6 +17,7 @@
 namespace ff {
 int32_t launch_tiles_bf16(Kind kind, bool pair, const Maps& maps, const Args& args, int device, int sms, cudaStream_t st);
 int32_t launch_tiles_f32(Kind kind, bool pair, const Maps& maps, const Args& args, int device, int sms, cudaStream_t st);
+int32_t launch_fused(const Maps& maps, const Args& args, int device, int sms, cudaStream_t st);
 bool few_rows(const gnnco_gated_ff_desc* d, int sms);
 int32_t launch_few_rows(gnnco_handle* h, const gnnco_gated_ff_desc* d, const philox::Mask* mask, float* hidden, void* y, int64_t y_ld,
                         cudaStream_t st);
@@ -47,6 +48,7 @@ struct PackJobs {
 // that was not before.
 template <int LIMBS>
 __global__ void __launch_bounds__(256) pack_operands(const __grid_constant__ PackJobs P) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const PackJob& J = P.j[blockIdx.y];
   const int64_t chunks = J.to_ld / 8, items = J.rows * chunks;
   philox::Stream words(P.mask);
@@ -274,6 +276,7 @@ struct Call {
   cudaStream_t st;
   int limbs;
   bool drops;                                              // whether the mask drops anything
+  bool launched;                                           // by this call, so far
   PackJobs jobs;
   int n_jobs = 0;
 
@@ -307,6 +310,7 @@ struct Call {
     if (limbs == 3) pack_operands<3><<<grid, 256, 0, st>>>(jobs);
     else pack_operands<1><<<grid, 256, 0, st>>>(jobs);
     h->launches += 1;
+    launched = true;
   }
   // tiles of rows
   int64_t row_tiles(bool pair) const {
@@ -326,21 +330,37 @@ struct Call {
   int32_t launch(Kind kind, bool pair, const Maps& maps, Args* a, int64_t tiles) {
     if (tiles > 0x7fffffff) return GNNCO_UNSUPPORTED;
     a->tiles = (int32_t)tiles;
+    a->chained = launched;
+    launched = true;
     const int32_t rc = limbs == 3 ? ff::launch_tiles_f32(kind, pair, maps, *a, h->device, h->sm_count, st)
                                   : ff::launch_tiles_bf16(kind, pair, maps, *a, h->device, h->sm_count, st);
     if (rc == GNNCO_OK) h->launches += 1;
     return rc;
   }
-  // Pairs of CTAs halve what is read per product; single CTAs with tiles of a quarter of the size spread small calls over more SMs.
-  bool use_pairs(int64_t pair_tiles) const {
-    const int pairs = ff::resident_pairs(h->device, h->sm_count);
-    return pairs > 0 && pair_tiles >= pairs;
+  // Pairs of CTAs halve what is read per product; single CTAs with tiles of a quarter of the size spread small calls over more SMs and
+  // leave less of the last round idle.  Rounds of tiles times their length, in cycles: the products of a stage (64 of the contraction)
+  // or its copies at the 45 bytes a cycle that an SM got from L2, and some 2,500 at the ends that nothing covers.
+  // (4,039 x 128 x 343 float32, 16 sets, backward: PAIRS_FIGURES.)
+  bool use_pairs(int64_t pair_tiles, int64_t single_tiles, int64_t stages, int pair_cols, int single_cols) const {
+    const int64_t pairs = ff::resident_pairs(h->device, h->sm_count), sms = h->sm_count;
+    if (pairs <= 0 || pair_tiles < pairs) return false;
+    const int64_t products = limbs == 3 ? 6 : 1;
+    auto stage = [&](int cols, int staged) {
+      const int64_t multiply = products * cols * 2, copy = (int64_t)limbs * (128 + staged) * 128 / 45;
+      return multiply > copy ? multiply : copy;
+    };
+    const int64_t by_pairs = blocks_of(pair_tiles, pairs) * (stages * stage(pair_cols, pair_cols / 2) + 2500);
+    const int64_t by_singles = blocks_of(single_tiles, sms) * (stages * stage(single_cols, single_cols) + 2500);
+    return by_pairs <= by_singles;
   }
 
   // h (and, with dy, dg and du) from x
   int32_t gates(const Operand& x, const Operand* dy, const Operand& wg, const Operand& wu, const Operand& wd, const Operand* out) {
     auto nt_of = [&](bool pair) { return pair && (dy ? limbs == 1 : d->H > 64) ? 128 : 64; };
-    const bool pair = use_pairs(row_tiles(true) * blocks_of(d->H, nt_of(true)));
+    // (columns that are multiplied per stage: g and u, on average two of g, u and dh)
+    const bool pair = use_pairs(row_tiles(true) * blocks_of(d->H, nt_of(true)), row_tiles(false) * blocks_of(d->H, nt_of(false)),
+                                blocks_of(d->F, 64) + (dy ? blocks_of(d->F_out, 64) : 0), dy ? nt_of(true) * 3 / 2 : nt_of(true) * 2,
+                                dy ? nt_of(false) * 3 / 2 : nt_of(false) * 2);
     Args a = {};
     Maps m;
     rows_of(&a, pair);
@@ -363,11 +383,15 @@ struct Call {
     if (!ok) return GNNCO_CUDA_ERROR;
     return launch(dy ? ff::kGluBack : ff::kGlu, pair, m, &a, (int64_t)a.m_tiles * a.n_tiles);
   }
+  bool wide_pairs(int cols, int64_t stages) const {
+    const int p = wide_tile(true, cols), q = wide_tile(false, cols);
+    return use_pairs(row_tiles(true) * blocks_of(cols, p), row_tiles(false) * blocks_of(cols, q), stages, p, q);
+  }
   static int wide_tile(bool pair, int cols) { return pair ? (cols > 128 ? 256 : 128) : (cols > 64 ? 128 : 64); }
 
   // y = drop(h Wd)
   int32_t down(const Operand& hh, const Operand& wd, void* y, int64_t y_ld) {
-    const bool pair = use_pairs(row_tiles(true) * blocks_of(d->F_out, wide_tile(true, d->F_out)));
+    const bool pair = wide_pairs(d->F_out, blocks_of(d->H, 64));
     Args a = {};
     Maps m;
     rows_of(&a, pair);
@@ -382,9 +406,34 @@ struct Call {
       return GNNCO_CUDA_ERROR;
     return launch(ff::kDown, pair, m, &a, (int64_t)a.m_tiles * a.n_tiles);
   }
+  // Both products in one kernel (gated_ff_fused.cu), where its tiles of 256 rows keep all pairs of CTAs busy.
+  bool fuses() const {
+    return limbs == 1 && d->F <= 256 && d->F_out <= 256 && ff::resident_pairs(h->device, h->sm_count) > 0 &&
+           row_tiles(true) >= ff::resident_pairs(h->device, h->sm_count);
+  }
+  int32_t fused(const Operand& x, const Operand& wg, const Operand& wu, const Operand& wd, void* y, int64_t y_ld) {
+    Args a = {};
+    Maps m;
+    rows_of(&a, true);
+    a.n_tiles = 1;
+    a.K[0] = d->F;
+    a.K[1] = d->H;
+    a.act = d->act;
+    if (!result(&a, &m, y, y_ld, d->F_out)) return GNNCO_CUDA_ERROR;
+    a.masked = drops;
+    a.mask = jobs.mask;
+    a.tiles = a.m_tiles;
+    a.chained = launched;
+    if (!map_rows(&m.a[0], x.p, d->rows, d->F, x.ld, x.limb, 1, 128) || !map_sets(&m.b[0], wg.p, d->sets, d->F, d->H, wg.ld, 1, 64) ||
+        !map_sets(&m.b[1], wu.p, d->sets, d->F, d->H, wu.ld, 1, 64) || !map_sets(&m.b[2], wd.p, d->sets, d->H, d->F_out, wd.ld, 1, 64))
+      return GNNCO_CUDA_ERROR;
+    const int32_t rc = ff::launch_fused(m, a, h->device, h->sm_count, st);
+    if (rc == GNNCO_OK) h->launches += 1;
+    return rc;
+  }
   // dx = dg Wg^T + du Wu^T
   int32_t input_grad(const Operand& dg, const Operand& du, const Operand& wg, const Operand& wu, void* dx, int64_t dx_ld) {
-    const bool pair = use_pairs(row_tiles(true) * blocks_of(d->F, wide_tile(true, d->F)));
+    const bool pair = wide_pairs(d->F, 2 * blocks_of(d->H, 64));
     Args a = {};
     Maps m;
     rows_of(&a, pair);
@@ -425,7 +474,9 @@ struct Call {
       for (int q = 0; q < 3; ++q) shape_problem(&a.p[q], R[q], C[q], pair, a.out_vectors && C[q] % 8 == 0);
       return (int64_t)c.count * tiles_of(a.p);
     };
-    const bool pair = use_pairs(shape(true));
+    const int64_t rows_of_chunk = blocks_of(d->rows, c.count > 0 ? c.count : 1);
+    const int64_t pair_tiles = shape(true), single_tiles = shape(false);
+    const bool pair = use_pairs(pair_tiles, single_tiles, blocks_of(rows_of_chunk, 64), 256, 128);
     const int64_t tiles = shape(pair);
     int64_t at[3];
     a.slot_stride = slot_layout(d, at);
@@ -522,8 +573,13 @@ extern "C" int32_t gnnco_gated_ff(gnnco_handle* h, const gnnco_gated_ff_desc* d,
   hh.ld = up16(d->H);
   hh.limb = d->rows * hh.ld;
   c.pack();
-  int32_t r = c.gates(x, nullptr, wg, wu, wd, &hh);
-  if (r == GNNCO_OK) r = c.down(hh, wd, y, y_ld);
+  int32_t r;
+  if (c.fuses()) {
+    r = c.fused(x, wg, wu, wd, y, y_ld);
+  } else {
+    r = c.gates(x, nullptr, wg, wu, wd, &hh);
+    if (r == GNNCO_OK) r = c.down(hh, wd, y, y_ld);
+  }
   if (r != GNNCO_OK) return r;
   GNNCO_LAUNCH_CHECK();
   return GNNCO_OK;

@@ -65,6 +65,7 @@ struct Args {
   float* scratch;
   int64_t slot_stride;
   int32_t* status;
+  int32_t chained;                     // a launch of the same call comes before
 };
 
 // clusters of two CTAs that the device holds at once (0: none)

@@ -1,0 +1,347 @@
+// The gated feed-forward block's forward pass as ONE kernel, for bfloat16 operands and widths F, F_out <= 256: h never leaves the SM.
+//
+//   a cluster of two CTAs takes 256 rows of x, which stay in shared memory, and walks H in chunks of 128 columns:
+//     G(c)   [g | u] = x [Wg | Wu]       256 x 256 in tensor memory
+//     result warps   h = act(g) .* u     -> bfloat16, into shared memory, in the layout of an MMA operand
+//     D(c)   y += h Wd                   256 x F_out, in tensor memory until the last chunk
+//
+// The products are issued G(0) G(1) D(0) G(2) D(1) .., across tiles too.  While D(c - 1) is multiplied the result warps take g and u of
+// chunk c into registers, so that G(c + 1) finds its accumulator free, and they have that long to finish h (3,072 cycles a chunk at
+// F = F_out = 256).  A tile's y is taken out after the first chunk of the next tile, for the same reason.  With dropout behind the
+// block the words of y's elements are drawn a part with each chunk, and kept as one bit per element: drawn at the end of a tile
+// they would take as long as the products and nothing would cover them.
+// (Chunks of 64 columns with two accumulators of g and u halved the work per instruction and reread x twice as often: 2,070 us for
+// 2.5 M x 256 x 512 without dropout against FUSED_US.)
+// The weights come from L2 again for every tile: 96 KB per chunk and CTA, 32 bytes a cycle (an SM gets some 45).  Against the two
+// launches of gated_ff_tiles.cuh this saves writing and reading h, 4 H bytes per row of 4 F read and written.
+//
+// Shared memory per CTA: x 64 KB, h 32 KB, blocks of Wg (even CTA) or Wu (odd) 4 x 16 KB, of Wd 2 x 16 KB, staging 32 KB.
+// Roles of the twenty warps as in gated_ff_tiles.cuh.
+#include "gated_ff_tiles.cuh"
+
+namespace ff {
+namespace {
+
+constexpr int kChunk = 128;                                // columns of h
+constexpr int kXBlocks = 4, kGSlots = 4, kDSlots = 2;      // blocks of 64 of a contraction
+constexpr uint32_t kBlockBytes = 16384;
+constexpr uint32_t kX = 0, kH = kX + kXBlocks * kBlockBytes, kG = kH + 2 * kBlockBytes, kD = kG + kGSlots * kBlockBytes,
+                   kStaging = kD + kDSlots * kBlockBytes;
+constexpr uint32_t kFusedSmem = 1024 + kStaging + kEpiWarps * kStageBytes + 512;
+static_assert(kFusedSmem <= 232448, "fits one SM");
+constexpr uint32_t kYColumn = 0, kGuColumn = 256;          // tensor memory: y; g, then u
+
+// barriers; the even CTA's are used but for those that both CTAs wait on (every commit arrives in both)
+struct Bars {
+  uint64_t x_full[kXBlocks], x_empty[kXBlocks];
+  uint64_t g_full[kGSlots], g_empty[kGSlots];
+  uint64_t d_full[kDSlots], d_empty[kDSlots];
+  uint64_t gu_full, gu_empty, h_full, h_empty, y_full, y_empty;
+  uint32_t tmem, abort_flag;
+};
+
+__global__ void __launch_bounds__(kThreads, 1) fused_forward(const __grid_constant__ Maps maps, const __grid_constant__ Args A) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t sbase = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (sbase - tc::smem_u32(smem_raw));
+  Bars& B = *reinterpret_cast<Bars*>(gen + kStaging + kEpiWarps * kStageBytes);
+  volatile uint32_t* abort_flag = &B.abort_flag;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = tc::cluster_ctarank();
+  const int first = blockIdx.x / 2, step = gridDim.x / 2;
+  const int x_blocks = (A.K[0] + 63) >> 6;                 // of F
+  const int chunks = (A.K[1] + kChunk - 1) / kChunk;       // of H
+  const int y_cols = A.cols > 128 ? 256 : 128;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kXBlocks; ++i) {
+      tc::mbar_init(B.x_full + i, 2);
+      tc::mbar_init(B.x_empty + i, 1);
+    }
+    for (int i = 0; i < kGSlots; ++i) {
+      tc::mbar_init(B.g_full + i, 2);
+      tc::mbar_init(B.g_empty + i, 1);
+    }
+    for (int i = 0; i < kDSlots; ++i) {
+      tc::mbar_init(B.d_full + i, 2);
+      tc::mbar_init(B.d_empty + i, 1);
+    }
+    tc::mbar_init(&B.gu_full, 1);
+    tc::mbar_init(&B.gu_empty, 2 * kEpiWarps);
+    tc::mbar_init(&B.h_full, 2 * kEpiWarps);
+    tc::mbar_init(&B.h_empty, 1);
+    tc::mbar_init(&B.y_full, 1);
+    tc::mbar_init(&B.y_empty, 2 * kEpiWarps);
+    *abort_flag = 0;
+    tc::fence_mbar_init();
+  }
+  if (warp == 0) tc::tmem_alloc_pair(&B.tmem, 512);
+  tc::tc_fence_before_sync();
+  __syncthreads();
+  tc::cluster_sync_all();
+  tc::tc_fence_after_sync();
+  const uint32_t tmem = B.tmem;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  if (warp == kCopyWarp) {
+    // -------------------------------------------------------------------------------- operands
+    const uint32_t leader = tc::elect_one();
+    const int rank_u = __shfl_sync(0xffffffffu, (int)rank, 0);
+    auto even = [&](uint64_t* bar) { return tc::map_to_cta(tc::smem_u32(bar), 0); };
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_bar(bar, parity, abort_flag)) != 0; };
+    Walk<kDown, true, true, true> walk(A, first, step);
+    int slot = 0, d = 0;
+    uint32_t g_phase = 1, d_phase = 1, x_phase = 1;        // the first round waits for nothing
+    bool ok = true;
+    int d_chunk = -1, d_set = 0;
+    auto load_d = [&] {
+      for (int kb = 0; kb < 2; ++kb) {
+        if (!wait(B.d_empty + d, d_phase)) return false;
+        expect_bytes<true>(leader, even(B.d_full + d), y_cols * 64);
+        for (int i = 0; i < y_cols / 128; ++i)
+          load_box_of_set<true>(leader, sbase + kD + d * kBlockBytes + i * 8192, &maps.b[2], rank_u * (y_cols / 2) + 64 * i,
+                                d_chunk * kChunk + kb * 64, d_set, even(B.d_full + d));
+        d ^= 1;
+        if (d == 0) d_phase ^= 1;
+      }
+      return true;
+    };
+    while (walk.any() && ok) {
+      const Tile T = walk.take();
+      for (int c = 0; c < chunks && ok; ++c) {
+        for (int kb = 0; kb < x_blocks && ok; ++kb) {
+          if (c == 0) {
+            if (!(ok = wait(B.x_empty + kb, x_phase))) break;
+            expect_bytes<true>(leader, even(B.x_full + kb), 16384);
+            load_box<true>(leader, sbase + kX + kb * 16384, &maps.a[0], kb * 64, T.row0 + rank_u * 128, 0, even(B.x_full + kb));
+          }
+          if (!(ok = wait(B.g_empty + slot, g_phase))) break;
+          expect_bytes<true>(leader, even(B.g_full + slot), kBlockBytes);
+          for (int i = 0; i < 2; ++i)
+            load_box_of_set<true>(leader, sbase + kG + slot * kBlockBytes + i * 8192, &maps.b[rank_u], c * kChunk + 64 * i, kb * 64, T.set,
+                                  even(B.g_full + slot));
+          if (++slot == kGSlots) {
+            slot = 0;
+            g_phase ^= 1;
+          }
+        }
+        // Wd of the chunk before
+        if (ok && d_chunk >= 0) ok = load_d();
+        d_chunk = c;
+        d_set = T.set;
+      }
+      x_phase ^= 1;
+    }
+    if (ok && d_chunk >= 0) load_d();
+    __syncwarp();
+  } else if (warp == kMmaWarp) {
+    // -------------------------------------------------------------------------------- products
+    if (rank == 0 && tc::elect_one()) {
+      const uint32_t g_idesc = tc::idesc_bf16_f32(256, 256, false, true), d_idesc = tc::idesc_bf16_f32(256, y_cols, false, true);
+      const int tiles_here = first < A.tiles ? (A.tiles - first + step - 1) / step : 0;
+      const int32_t total = tiles_here * chunks;
+      int slot = 0, d = 0, gc = 0, dc = 0;                 // gc, dc: chunk of the tile that G and D are at
+      uint32_t g_phase = 0, d_phase = 0, x_phase = 0, y_phase = 1;
+      bool ok = true;
+      for (int32_t i = 0; i <= total && ok; ++i) {
+        if (i < total) {
+          if (!(ok = wait_bar(&B.gu_empty, (uint32_t)(i & 1) ^ 1, abort_flag))) break;
+          tc::tc_fence_after_sync();
+          for (int kb = 0; kb < x_blocks; ++kb) {
+            if (gc == 0 && !(ok = wait_bar(B.x_full + kb, x_phase, abort_flag))) break;
+            if (!(ok = wait_bar(B.g_full + slot, g_phase, abort_flag))) break;
+            tc::tc_fence_after_sync();
+            const uint64_t a0 = tc::smem_desc_sw128(sbase + kX + kb * kBlockBytes, 16, 1024);
+            const uint64_t b0 = tc::smem_desc_sw128(sbase + kG + slot * kBlockBytes, 8192, 1024);
+            const int steps = min(4, (A.K[0] - kb * 64 + 15) >> 4);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (k < steps) multiply<true>(tmem + kGuColumn, a0 + 2 * k, b0 + 128 * k, g_idesc, kb + k != 0);
+            commit<true>(B.g_empty + slot);
+            if (gc == chunks - 1) commit<true>(B.x_empty + kb);
+            if (++slot == kGSlots) {
+              slot = 0;
+              g_phase ^= 1;
+            }
+          }
+          if (!ok) break;
+          commit<true>(&B.gu_full);
+          if (++gc == chunks) {
+            gc = 0;
+            x_phase ^= 1;
+          }
+        }
+        if (i > 0) {
+          if (!(ok = wait_bar(&B.h_full, (uint32_t)(i - 1) & 1, abort_flag))) break;
+          if (dc == 0) {
+            if (!(ok = wait_bar(&B.y_empty, y_phase, abort_flag))) break;
+            y_phase ^= 1;
+          }
+          for (int kb = 0; kb < 2; ++kb) {
+            if (!(ok = wait_bar(B.d_full + d, d_phase, abort_flag))) break;
+            tc::tc_fence_after_sync();
+            const uint64_t a0 = tc::smem_desc_sw128(sbase + kH + kb * kBlockBytes, 16, 1024);
+            const uint64_t b0 = tc::smem_desc_sw128(sbase + kD + d * kBlockBytes, 8192, 1024);
+            const int steps = min(4, (A.K[1] - dc * kChunk - kb * 64 + 15) >> 4);    // none where H ends before
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (k < steps) multiply<true>(tmem + kYColumn, a0 + 2 * k, b0 + 128 * k, d_idesc, dc + kb + k != 0);
+            commit<true>(B.d_empty + d);
+            d ^= 1;
+            if (d == 0) d_phase ^= 1;
+          }
+          if (!ok) break;
+          commit<true>(&B.h_empty);
+          if (++dc == chunks) {
+            dc = 0;
+            commit<true>(&B.y_full);
+          }
+        }
+      }
+    }
+  } else if (warp >= kFirstEpi) {
+    // --------------------------------------------------------------------------------- results
+    const int e = warp - kFirstEpi, quarter = warp & 3, column = e >> 2;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    const int row_in_cta = quarter * 32 + lane, warp_row = (int)rank * 128 + quarter * 32;
+    const uint32_t gu_free = tc::map_to_cta(tc::smem_u32(&B.gu_empty), 0), h_ready = tc::map_to_cta(tc::smem_u32(&B.h_full), 0);
+    const uint32_t y_free = tc::map_to_cta(tc::smem_u32(&B.y_empty), 0);
+    float* const stage = reinterpret_cast<float*>(gen + kStaging + e * kStageBytes);
+    const uint32_t stage_at = sbase + kStaging + e * kStageBytes;
+    const uint32_t h_at = sbase + kH + (column >> 1) * kBlockBytes + row_in_cta * 128;
+    philox::Stream words(A.mask);
+    const int y_quads = (A.cols + 3) / 4;
+    uint32_t y_phase = 0, phase = 0;                       // phase: of the chunk
+    bool ok = true;
+    // the tile whose y is still to be taken out: its first row of this warp, how many the tile has from there on, the kept elements of
+    // column groups `column` and `column` + 4 (32 columns each)
+    int32_t y_row0 = 0, y_rows = 0;
+    uint32_t keep0 = 0u, keep1 = 0u;
+    int drawn = 0;                                         // of 16 quads
+    auto draw = [&](int until) {
+      for (; drawn < until; ++drawn) {
+        const int at = (column + ((drawn & 8) >> 1)) * 8 + (drawn & 7);
+        if (at >= y_quads) continue;
+        const uint4 w = words.quad(A.mask, (uint64_t)(y_row0 + lane) * y_quads + at);
+        const uint32_t bits = ((w.x > A.mask.lim ? 1u : 0u) | (w.y > A.mask.lim ? 2u : 0u) | (w.z > A.mask.lim ? 4u : 0u) |
+                               (w.w > A.mask.lim ? 8u : 0u)) << (4 * (drawn & 7));
+        if (drawn & 8) keep1 |= bits;
+        else keep0 |= bits;
+      }
+    };
+    auto take_y = [&] {
+      if (A.masked) draw(16);
+      if (!wait_bar(&B.y_full, y_phase, abort_flag)) return false;
+      y_phase ^= 1;
+      tc::tc_fence_after_sync();
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const int c0 = (column + 4 * g) * 32;
+        const bool in = c0 < A.cols;
+        float f[32];
+        if (in) {
+          uint32_t r[32];
+          tmem_load(tmem + kYColumn + lanes + c0, r);
+          tc::tmem_ld_wait();
+#pragma unroll
+          for (int k = 0; k < 32; ++k) f[k] = __uint_as_float(r[k]);
+        }
+        if (g == 1) {
+          tc::tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive_cluster(y_free);
+        }
+        if (!in) continue;
+        if (A.masked) {
+          const uint32_t keep = g == 0 ? keep0 : keep1;
+#pragma unroll
+          for (int k = 0; k < 32; ++k) f[k] = (keep >> k) & 1u ? f[k] * A.mask.scale : 0.0f;
+        }
+        if (A.y_vectors && y_rows >= 32) stage_and_store(&maps.out, stage_at, lane, c0, y_row0, f);
+        else store_rows<false>(stage, lane, y_rows, y_row0, c0, A.cols, A.y, A.y_ld, f);
+      }
+      return true;
+    };
+    // the next tile's table entries arrive while this one is worked on
+    int32_t next_row0 = 0, next_rows = 0;
+    auto fetch = [&](int t) {
+      if (t >= A.tiles) return;
+      next_row0 = A.tile_row0 ? A.tile_row0[t] : t * 256;
+      next_rows = A.tile_row0 ? A.tile_rows[t] : (int32_t)min((int64_t)256, A.rows - (int64_t)t * 256);
+    };
+    fetch(first);
+    for (int t = first; t < A.tiles && ok; t += step) {
+      for (int c = 0; c < chunks && ok; ++c, phase ^= 1) {
+        if (!(ok = wait_bar(&B.gu_full, phase, abort_flag))) break;
+        tc::tc_fence_after_sync();
+        uint32_t w[16];                                    // h, packed; 16 columns at a time keep the registers few
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          uint32_t r[2][16];
+          const uint32_t at = tmem + kGuColumn + lanes + column * 32 + 16 * b;
+          tmem_load(at, r[0]);
+          tmem_load(at + 128, r[1]);
+          tc::tmem_ld_wait();
+          if (b == 1) {
+            tc::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive_cluster(gu_free);
+          }
+          float f[2][16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            f[0][k] = __uint_as_float(r[0][k]);
+            f[1][k] = __uint_as_float(r[1][k]);
+          }
+          if (A.act == GNNCO_SILU) gate<false, GNNCO_SILU>(f, 1.0f);
+          else if (A.act == GNNCO_GELU) gate<false, GNNCO_GELU>(f, 1.0f);
+          else gate<false, GNNCO_RELU>(f, 1.0f);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) w[8 * b + k] = vio::pack_bf16(f[0][2 * k], f[0][2 * k + 1]);
+        }
+        if (!(ok = wait_bar(&B.h_empty, phase ^ 1, abort_flag))) break;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          tc::st_shared16(h_at + ((((column & 1) * 4 + k) ^ (row_in_cta & 7)) << 4), w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+        tc::fence_proxy_async_smem();
+        __syncwarp();
+        // (release at the scope of the CTA, and the proxy fence before it, put the writes ahead of the arrival: only this SM's tensor core
+        // reads them.  An explicit release at cluster scope waits for everything this thread has in flight: 1,650 cycles a chunk.)
+        if (lane == 0) tc::mbar_arrive_cluster(h_ready);
+        if (c == 0) {
+          if (t != first && !(ok = take_y())) break;
+          y_row0 = next_row0 + warp_row;
+          y_rows = next_rows - warp_row;
+          keep0 = keep1 = 0u;
+          drawn = 0;
+          fetch(t + step);
+        }
+        if (A.masked) draw(16 * (c + 1) / chunks);
+      }
+    }
+    if (ok && first < A.tiles) take_y();
+    if (lane == 0) store_box_done();
+  }
+  // ------------------------------------------------------------------------------------ the end
+  if (*abort_flag) {
+    if (threadIdx.x == 0) atomicMin(A.status, (int32_t)GNNCO_INTERNAL);
+    const long long t0 = clock64();                        // copies and products already issued end before the memory goes
+    while (clock64() - t0 < 1000000ll) {}
+  }
+  tc::tc_fence_before_sync();
+  __syncthreads();
+  tc::cluster_sync_all();
+  if (warp == 0) tc::tmem_dealloc_pair(tmem, 512);
+}
+
+}  // namespace
+
+int32_t launch_fused(const Maps& maps, const Args& args, int device, int sms, cudaStream_t st) {
+  static std::atomic<int> allowed{0};
+  const int32_t rc = allow_shared_memory(fused_forward, kFusedSmem, device, allowed);
+  if (rc != GNNCO_OK) return rc;
+  return launch_clusters(fused_forward, kFusedSmem, maps, args, args.tiles < resident_pairs(device, sms) ? args.tiles : resident_pairs(device, sms), 2, st);
+}
+
+}  // namespace ff

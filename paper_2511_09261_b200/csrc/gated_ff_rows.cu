@@ -38,6 +38,19 @@ __device__ __forceinline__ float element(const void* p, int64_t i) {
   else return static_cast<const float*>(p)[i];
 }
 
+// VEC consecutive elements by plain loads (this kernel may have been running while the one before it wrote)
+template <typename T, int VEC>
+__device__ __forceinline__ void load_plain(vio::Raw<T, VEC>& v, const T* p) {
+  if constexpr (VEC * sizeof(T) == 16) {
+    const uint4 q = *reinterpret_cast<const uint4*>(p);
+    v.w[0] = q.x; v.w[1] = q.y; v.w[2] = q.z; v.w[3] = q.w;
+  } else if constexpr (sizeof(T) == 4) {
+    v.w[0] = *reinterpret_cast<const uint32_t*>(p);
+  } else {
+    v.w[0] = *reinterpret_cast<const unsigned short*>(p);
+  }
+}
+
 // TX: features, TW: weights, R: rows held, VEC: columns per lane
 template <bool GATE, typename TX, typename TW, int R, int VEC>
 __global__ void __launch_bounds__(kThreads) rows_product(const __grid_constant__ RowsArgs A) {
@@ -83,8 +96,8 @@ __global__ void __launch_bounds__(kThreads) rows_product(const __grid_constant__
 #pragma unroll
       for (int i = 0; i < kFlight; ++i)
         if (k + i * kSlices < k1) {
-          w[i][0].template load<false>(w0 + (int64_t)(k + i * kSlices) * A.N);
-          if (GATE) w[i][kMats - 1].template load<false>(w1 + (int64_t)(k + i * kSlices) * A.N);
+          load_plain(w[i][0], w0 + (int64_t)(k + i * kSlices) * A.N);
+          if (GATE) load_plain(w[i][kMats - 1], w1 + (int64_t)(k + i * kSlices) * A.N);
         }
 #pragma unroll
       for (int i = 0; i < kFlight; ++i)

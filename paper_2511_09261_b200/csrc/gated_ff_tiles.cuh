@@ -23,6 +23,7 @@
 // every stage starts an accumulator of its own (buffers in turn), adds the five small products first and the large one last, and the
 // result warps add the stages up in float32 registers, rounded to nearest.
 //
+// The launches of a call are chained by programmatic dependence: a kernel sets itself up while the one before it ends.
 // Every wait has a limit; a CTA that gives up raises the handle's status word, skips its work and leaves.
 #pragma once
 
@@ -74,11 +75,14 @@ __device__ __forceinline__ void expect_bytes(uint32_t leader, uint32_t bar, uint
     asm volatile("{\n\t.reg .pred go;\n\tsetp.ne.b32 go, %2, 0;\n\t@go mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}"
                  ::"r"(bar), "r"(bytes), "r"(leader) : "memory");
 }
-// `acquire` at cluster scope: what the other CTA wrote before its arrival is seen
+// CLUSTER: what threads of the other CTA wrote before their arrival is to be seen (copies and products complete through the
+// barrier itself, and need no more than the usual wait)
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
-  if (tc::mbar_try_wait_cluster(bar, parity)) return true;
+  auto done = [&] { return CLUSTER ? tc::mbar_try_wait_cluster(bar, parity) : tc::mbar_try_wait(bar, parity); };
+  if (done()) return true;
   const long long t0 = clock64();
-  while (!tc::mbar_try_wait_cluster(bar, parity)) {
+  while (!done()) {
     if (*abort_flag) return false;
     if (clock64() - t0 > 4000000000ll) {
       *abort_flag = 1;
@@ -249,6 +253,31 @@ __device__ __forceinline__ void stage_and_store(const CUtensorMap* map, uint32_t
   if (lane == 0) store_box(map, stage, x, y);
 }
 
+// 32 values of this lane's row (row0 + lane, if that is below rows_here) to out[row][c0 ..], for rows that start anywhere or end inside
+// the group: through the staging tile, 16 columns at a time, so that half a warp holds neighbouring columns (column c of row r
+// stands at c ^ (r % 16): no bank twice in a read, twice in a write).  Whole warp.
+template <bool WIDE>
+__device__ __forceinline__ void store_rows(float* stage, int lane, int rows_here, int64_t row0, int c0, int cols, void* out, int64_t ld,
+                                           const float (&f)[32]) {
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    if (lane == 0) store_box_read();                       // a box before may still be read from the tile
+    __syncwarp();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) stage[lane * 16 + (e ^ (lane & 15))] = f[16 * b + e];
+    __syncwarp();
+    const int col = c0 + 16 * b + (lane & 15);
+    if (col >= cols) continue;
+    for (int r = lane >> 4; r < min(32, rows_here); r += 2) {
+      const float x = stage[r * 16 + ((lane & 15) ^ (r & 15))];
+      const int64_t to = (row0 + r) * ld + col;
+      if (WIDE) static_cast<float*>(out)[to] = x;
+      else static_cast<__nv_bfloat16*>(out)[to] = __float2bfloat16_rn(x);
+    }
+  }
+  __syncwarp();
+}
+
 struct Tile {
   int32_t row0, rows, n0, m0, problem, slot, set;
   int32_t stages;                                          // of the first contraction
@@ -390,6 +419,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
   uint64_t* tail = acc_empty + 2;                          // this CTA's stages with rows to be cleared
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tail + 1);
   volatile uint32_t* abort_flag = tmem_slot + 1;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = PAIR ? tc::cluster_ctarank() : 0u;
   const int first = blockIdx.x / kCtas, step = gridDim.x / kCtas;
@@ -416,6 +446,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
   if (PAIR) tc::cluster_sync_all();
   tc::tc_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
+  asm volatile("griddepcontrol.wait;" ::: "memory");       // the operands are complete from here on
   const int more = kAlongRows ? 0 : (A.K[1] + 63) >> 6;    // stages of the second contraction
 
   if (warp == kCopyWarp) {
@@ -530,7 +561,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
               open = true;
             }
             const uint32_t acc = tmem + (kQuarters ? ((3 * part + seg) & 3) * 128 : (part & 1) * kBuf);
-            ok = wait_bar(full + slot, phase, abort_flag);
+            ok = wait_bar<PAIR && kAlongRows>(full + slot, phase, abort_flag);
             tc::tc_fence_after_sync();
             if (!ok) break;
             const uint32_t at = sbase + slot * kSlot, bt = at + kA;
@@ -776,27 +807,9 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
               }
             }
           } else {
-            // rows that start anywhere, or end inside the group: through shared memory, 16 columns at a time, so that half a warp
-            // holds neighbouring columns (column c of row r stands at c ^ (r % 16): no bank twice in a read, twice in a write)
-            const int rows_here = min(32, (kAlongRows ? A.p[T.problem].M - T.m0 : T.rows) - (local - lane));
-            const int64_t row_of_warp = row - lane;
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-              if (LIMBS == 1 && !kAlongRows && lane == 0) store_box_read();
-              __syncwarp();
-#pragma unroll
-              for (int e = 0; e < 16; ++e) stage[lane * 16 + (e ^ (lane & 15))] = f[0][16 * b + e];
-              __syncwarp();
-              const int col = c0 + 16 * b + (lane & 15);
-              if (col < cols) {
-                for (int r = lane >> 4; r < rows_here; r += 2) {
-                  const float x = stage[r * 16 + ((lane & 15) ^ (r & 15))];
-                  const int64_t to = (row_of_warp + r) * ld + col;
-                  if (wide) static_cast<float*>(out)[to] = x;
-                  else static_cast<__nv_bfloat16*>(out)[to] = __float2bfloat16_rn(x);
-                }
-              }
-            }
+            const int rows_here = (kAlongRows ? A.p[T.problem].M - T.m0 : T.rows) - (local - lane);
+            if (wide) store_rows<true>(stage, lane, rows_here, row - lane, c0, cols, out, ld, f[0]);
+            else store_rows<false>(stage, lane, rows_here, row - lane, c0, cols, out, ld, f[0]);
           }
         }
       }
@@ -819,6 +832,28 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
 }
 
 // -------------------------------------------------------------------------------------------- launch
+template <typename Kernel>
+int32_t launch_clusters(Kernel kernel, uint32_t smem, const Maps& maps, const Args& args, int clusters, int ctas, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(clusters * ctas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  cfg.attrs = attr;
+  cfg.numAttrs = 0;
+  if (args.chained) {                                      // it sets itself up while the launch before it ends
+    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (ctas > 1) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+    attr[cfg.numAttrs].val.clusterDim.x = ctas; attr[cfg.numAttrs].val.clusterDim.y = 1; attr[cfg.numAttrs++].val.clusterDim.z = 1;
+  }
+  GNNCO_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, maps, args));
+  return GNNCO_OK;
+}
+
 template <int KIND, int LIMBS, bool PAIR>
 int32_t launch_one(const Maps& maps, const Args& args, int device, int sms, cudaStream_t st) {
   auto kernel = tiles<KIND, LIMBS, PAIR>;
@@ -826,19 +861,7 @@ int32_t launch_one(const Maps& maps, const Args& args, int device, int sms, cuda
   const int32_t rc = allow_shared_memory(kernel, kSmem, device, allowed);
   if (rc != GNNCO_OK) return rc;
   const int most = PAIR ? resident_pairs(device, sms) : sms;
-  const int ctas = (args.tiles < most ? args.tiles : most) * (PAIR ? 2 : 1);
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(ctas);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kSmem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = PAIR ? 2 : 1; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  GNNCO_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, maps, args));
-  return GNNCO_OK;
+  return launch_clusters(kernel, kSmem, maps, args, args.tiles < most ? args.tiles : most, PAIR ? 2 : 1, st);
 }
 
 }  // namespace ff

@@ -362,3 +362,23 @@ def test_few_rows(single, rows, F, H, Fo, dtype, w_dtype):
         out = torch.empty(rows, Fo + 5, dtype=t[0].dtype, device="cuda")
         single.gated_ff(wide[:, 1:F + 1], *t[2:], act=act, out=out[:, 2:Fo + 2])
         assert torch.equal(out[:, 2:Fo + 2], y)
+
+
+@pytest.mark.parametrize("F,H,Fo", [(256, 512, 256), (64, 64, 64), (40, 65, 24), (130, 200, 257), (136, 136, 136), (8, 1, 8), (250, 130, 129), (200, 1000, 72)])
+@pytest.mark.parametrize("act,p", [("silu", 0.0), ("gelu", 0.3), ("silu", 0.1)])
+def test_many_rows_in_bfloat16(F, H, Fo, act, p):
+    """Enough tiles of 256 rows for every pair of CTAs: widths up to 256 run as one kernel, in which several tiles follow each
+    other; ragged and empty subgraphs, odd and even numbers of chunks of h."""
+    sizes = [300, 0, 257, 1, 33, 5000, 256] * 6 + [640] * 10
+    ptr = np.concatenate([[0], np.cumsum(sizes)])
+    g = load(sizes)
+    rows = int(ptr[-1])
+    drop = gnnco.Dropout(p, 21, layer=2, step=3) if p else None
+    mask = ref.keep(rows, Fo, p, 21, 2, 3) / (1 - p) if p else None
+    t = make(rows, len(sizes), F, H, Fo, "bf16", seed=H)
+    y = check_forward(g, t, ptr, act, "bf16", drop, mask)
+    if p:
+        assert not host(y)[mask == 0].any()
+    u = make(rows, 1, F, H, Fo, "bf16", seed=H + 1)
+    check_forward(g, u, None, act, "bf16", drop, mask)
+    assert g.async_status() == gnnco.OK

@@ -8,15 +8,17 @@
 // The products are issued G(0) G(1) D(0) G(2) D(1) .., across tiles too.  While D(c - 1) is multiplied the result warps take g and u of
 // chunk c into registers, so that G(c + 1) finds its accumulator free, and they have that long to finish h (3,072 cycles a chunk at
 // F = F_out = 256).  A tile's y is taken out after the first chunk of the next tile, for the same reason.  With dropout behind the
-// block the words of y's elements are drawn a part with each chunk, and kept as one bit per element: drawn at the end of a tile
-// they would take as long as the products and nothing would cover them.
+// block six more warps draw the words of y's elements meanwhile and leave one bit per element in shared memory: drawn by the
+// result warps they took as long as everything else (2,230 us, against FUSED_DROP_US).
 // (Chunks of 64 columns with two accumulators of g and u halved the work per instruction and reread x twice as often: 2,070 us for
 // 2.5 M x 256 x 512 without dropout against FUSED_US.)
 // The weights come from L2 again for every tile: 96 KB per chunk and CTA, 32 bytes a cycle (an SM gets some 45).  Against the two
 // launches of gated_ff_tiles.cuh this saves writing and reading h, 4 H bytes per row of 4 F read and written.
 //
 // Shared memory per CTA: x 64 KB, h 32 KB, blocks of Wg (even CTA) or Wu (odd) 4 x 16 KB, of Wd 2 x 16 KB, staging 32 KB.
-// Roles of the twenty warps as in gated_ff_tiles.cuh.
+// Roles of the warps: 0 products, 1 copies, 4-11 results; with dropout 2, 3 and 12-15 draw.  (Eight result warps with 168 registers
+// each hold nearly all of their g and u, so the accumulator is free soon; sixteen with 96 had to compute the first half before they
+// could take the second, and the products waited: 1,666 us against FUSED_US.  With dropout the launch has 128 registers a thread.)
 #include "gated_ff_tiles.cuh"
 
 namespace ff {
@@ -27,7 +29,10 @@ constexpr int kXBlocks = 4, kGSlots = 4, kDSlots = 2;      // blocks of 64 of a 
 constexpr uint32_t kBlockBytes = 16384;
 constexpr uint32_t kX = 0, kH = kX + kXBlocks * kBlockBytes, kG = kH + 2 * kBlockBytes, kD = kG + kGSlots * kBlockBytes,
                    kStaging = kD + kDSlots * kBlockBytes;
-constexpr uint32_t kFusedSmem = 1024 + kStaging + kEpiWarps * kStageBytes + 512;
+constexpr int kResults = 8, kDrawers = 6;
+constexpr uint32_t kMaskBytes = 8 * 128 * 4;               // a bit for each of 128 x 256 elements: [column group][row]
+constexpr uint32_t kMask = kStaging + kResults * kStageBytes, kBars = kMask + 2 * kMaskBytes;
+constexpr uint32_t kFusedSmem = 1024 + kBars + 512;
 static_assert(kFusedSmem <= 232448, "fits one SM");
 constexpr uint32_t kYColumn = 0, kGuColumn = 256;          // tensor memory: y; g, then u
 
@@ -37,14 +42,18 @@ struct Bars {
   uint64_t g_full[kGSlots], g_empty[kGSlots];
   uint64_t d_full[kDSlots], d_empty[kDSlots];
   uint64_t gu_full, gu_empty, h_full, h_empty, y_full, y_empty;
+  uint64_t mask_full[2], mask_empty[2];                    // every CTA's own
   uint32_t tmem, abort_flag;
 };
 
-__global__ void __launch_bounds__(kThreads, 1) fused_forward(const __grid_constant__ Maps maps, const __grid_constant__ Args A) {
+constexpr int fused_threads(bool masked) { return 32 * (kFirstEpi + kResults + (masked ? 4 : 0)); }
+
+template <bool MASKED>
+__global__ void __launch_bounds__(fused_threads(MASKED), 1) fused_forward(const __grid_constant__ Maps maps, const __grid_constant__ Args A) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t sbase = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (sbase - tc::smem_u32(smem_raw));
-  Bars& B = *reinterpret_cast<Bars*>(gen + kStaging + kEpiWarps * kStageBytes);
+  Bars& B = *reinterpret_cast<Bars*>(gen + kBars);
   volatile uint32_t* abort_flag = &B.abort_flag;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -68,11 +77,15 @@ __global__ void __launch_bounds__(kThreads, 1) fused_forward(const __grid_consta
       tc::mbar_init(B.d_empty + i, 1);
     }
     tc::mbar_init(&B.gu_full, 1);
-    tc::mbar_init(&B.gu_empty, 2 * kEpiWarps);
-    tc::mbar_init(&B.h_full, 2 * kEpiWarps);
+    tc::mbar_init(&B.gu_empty, 2 * kResults);
+    tc::mbar_init(&B.h_full, 2 * kResults);
     tc::mbar_init(&B.h_empty, 1);
     tc::mbar_init(&B.y_full, 1);
-    tc::mbar_init(&B.y_empty, 2 * kEpiWarps);
+    tc::mbar_init(&B.y_empty, 2 * kResults);
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(B.mask_full + i, kDrawers);
+      tc::mbar_init(B.mask_empty + i, kResults);
+    }
     *abort_flag = 0;
     tc::fence_mbar_init();
   }
@@ -200,44 +213,29 @@ __global__ void __launch_bounds__(kThreads, 1) fused_forward(const __grid_consta
         }
       }
     }
-  } else if (warp >= kFirstEpi) {
+  } else if (warp >= kFirstEpi && warp < kFirstEpi + kResults) {
     // --------------------------------------------------------------------------------- results
-    const int e = warp - kFirstEpi, quarter = warp & 3, column = e >> 2;
+    const int e = warp - kFirstEpi, quarter = warp & 3, half = e >> 2;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const int row_in_cta = quarter * 32 + lane, warp_row = (int)rank * 128 + quarter * 32;
     const uint32_t gu_free = tc::map_to_cta(tc::smem_u32(&B.gu_empty), 0), h_ready = tc::map_to_cta(tc::smem_u32(&B.h_full), 0);
     const uint32_t y_free = tc::map_to_cta(tc::smem_u32(&B.y_empty), 0);
     float* const stage = reinterpret_cast<float*>(gen + kStaging + e * kStageBytes);
     const uint32_t stage_at = sbase + kStaging + e * kStageBytes;
-    const uint32_t h_at = sbase + kH + (column >> 1) * kBlockBytes + row_in_cta * 128;
-    philox::Stream words(A.mask);
-    const int y_quads = (A.cols + 3) / 4;
+    const uint32_t h_at = sbase + kH + half * kBlockBytes + row_in_cta * 128;
     uint32_t y_phase = 0, phase = 0;                       // phase: of the chunk
     bool ok = true;
-    // the tile whose y is still to be taken out: its first row of this warp, how many the tile has from there on, the kept elements of
-    // column groups `column` and `column` + 4 (32 columns each)
+    // the tile whose y is still to be taken out: its first row of this warp, how many the tile has from there on, its number here
     int32_t y_row0 = 0, y_rows = 0;
-    uint32_t keep0 = 0u, keep1 = 0u;
-    int drawn = 0;                                         // of 16 quads
-    auto draw = [&](int until) {
-      for (; drawn < until; ++drawn) {
-        const int at = (column + ((drawn & 8) >> 1)) * 8 + (drawn & 7);
-        if (at >= y_quads) continue;
-        const uint4 w = words.quad(A.mask, (uint64_t)(y_row0 + lane) * y_quads + at);
-        const uint32_t bits = ((w.x > A.mask.lim ? 1u : 0u) | (w.y > A.mask.lim ? 2u : 0u) | (w.z > A.mask.lim ? 4u : 0u) |
-                               (w.w > A.mask.lim ? 8u : 0u)) << (4 * (drawn & 7));
-        if (drawn & 8) keep1 |= bits;
-        else keep0 |= bits;
-      }
-    };
+    uint32_t y_tile = 0;
     auto take_y = [&] {
-      if (A.masked) draw(16);
       if (!wait_bar(&B.y_full, y_phase, abort_flag)) return false;
       y_phase ^= 1;
       tc::tc_fence_after_sync();
+      if (MASKED && !wait_bar(B.mask_full + (y_tile & 1), (y_tile >> 1) & 1, abort_flag)) return false;
 #pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const int c0 = (column + 4 * g) * 32;
+      for (int g = 0; g < 4; ++g) {
+        const int c0 = (half + 2 * g) * 32;
         const bool in = c0 < A.cols;
         float f[32];
         if (in) {
@@ -247,20 +245,25 @@ __global__ void __launch_bounds__(kThreads, 1) fused_forward(const __grid_consta
 #pragma unroll
           for (int k = 0; k < 32; ++k) f[k] = __uint_as_float(r[k]);
         }
-        if (g == 1) {
+        if (g == 3) {
           tc::tc_fence_before_sync();
           __syncwarp();
           if (lane == 0) tc::mbar_arrive_cluster(y_free);
         }
         if (!in) continue;
-        if (A.masked) {
-          const uint32_t keep = g == 0 ? keep0 : keep1;
+        if (MASKED) {
+          const uint32_t keep = reinterpret_cast<const uint32_t*>(gen + kMask + (y_tile & 1) * kMaskBytes)[(half + 2 * g) * 128 + row_in_cta];
 #pragma unroll
           for (int k = 0; k < 32; ++k) f[k] = (keep >> k) & 1u ? f[k] * A.mask.scale : 0.0f;
         }
         if (A.y_vectors && y_rows >= 32) stage_and_store(&maps.out, stage_at, lane, c0, y_row0, f);
         else store_rows<false>(stage, lane, y_rows, y_row0, c0, A.cols, A.y, A.y_ld, f);
       }
+      if (MASKED) {
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(B.mask_empty + (y_tile & 1));
+      }
+      ++y_tile;
       return true;
     };
     // the next tile's table entries arrive while this one is worked on
@@ -275,35 +278,46 @@ __global__ void __launch_bounds__(kThreads, 1) fused_forward(const __grid_consta
       for (int c = 0; c < chunks && ok; ++c, phase ^= 1) {
         if (!(ok = wait_bar(&B.gu_full, phase, abort_flag))) break;
         tc::tc_fence_after_sync();
-        uint32_t w[16];                                    // h, packed; 16 columns at a time keep the registers few
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          uint32_t r[2][16];
-          const uint32_t at = tmem + kGuColumn + lanes + column * 32 + 16 * b;
-          tmem_load(at, r[0]);
-          tmem_load(at + 128, r[1]);
-          tc::tmem_ld_wait();
-          if (b == 1) {
-            tc::tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive_cluster(gu_free);
-          }
+        // g and u into registers, 16 columns at a time, and the accumulator back as soon as the last of four are there: the next products
+        // wait for it.  (The last are asked for when the first have been used: all at once do not fit.)
+        constexpr int kAhead = MASKED ? 2 : 3;
+        uint32_t r[4][2][16], w[32];
+        const uint32_t at = tmem + kGuColumn + lanes + half * 64;
+        auto load = [&](int b) {
+          tmem_load(at + 16 * b, r[b][0]);
+          tmem_load(at + 128 + 16 * b, r[b][1]);
+        };
+        auto convert = [&](int b) {
           float f[2][16];
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
-            f[0][k] = __uint_as_float(r[0][k]);
-            f[1][k] = __uint_as_float(r[1][k]);
+            f[0][k] = __uint_as_float(r[b][0][k]);
+            f[1][k] = __uint_as_float(r[b][1][k]);
           }
           if (A.act == GNNCO_SILU) gate<false, GNNCO_SILU>(f, 1.0f);
           else if (A.act == GNNCO_GELU) gate<false, GNNCO_GELU>(f, 1.0f);
           else gate<false, GNNCO_RELU>(f, 1.0f);
 #pragma unroll
           for (int k = 0; k < 8; ++k) w[8 * b + k] = vio::pack_bf16(f[0][2 * k], f[0][2 * k + 1]);
+        };
+#pragma unroll
+        for (int b = 0; b < kAhead; ++b) load(b);
+        tc::tmem_ld_wait();
+#pragma unroll
+        for (int b = kAhead; b < 4; ++b) {
+          convert(b - kAhead);
+          load(b);
         }
+        tc::tmem_ld_wait();
+        tc::tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive_cluster(gu_free);
+#pragma unroll
+        for (int b = 4 - kAhead; b < 4; ++b) convert(b);
         if (!(ok = wait_bar(&B.h_empty, phase ^ 1, abort_flag))) break;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          tc::st_shared16(h_at + ((((column & 1) * 4 + k) ^ (row_in_cta & 7)) << 4), w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+        for (int k = 0; k < 8; ++k)
+          tc::st_shared16(h_at + ((k ^ (row_in_cta & 7)) << 4), w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
         tc::fence_proxy_async_smem();
         __syncwarp();
         // (release at the scope of the CTA, and the proxy fence before it, put the writes ahead of the arrival: only this SM's tensor core
@@ -313,15 +327,42 @@ __global__ void __launch_bounds__(kThreads, 1) fused_forward(const __grid_consta
           if (t != first && !(ok = take_y())) break;
           y_row0 = next_row0 + warp_row;
           y_rows = next_rows - warp_row;
-          keep0 = keep1 = 0u;
-          drawn = 0;
           fetch(t + step);
         }
-        if (A.masked) draw(16 * (c + 1) / chunks);
       }
     }
     if (ok && first < A.tiles) take_y();
     if (lane == 0) store_box_done();
+  } else if (MASKED && warp > kCopyWarp) {
+    // ------------------------------------------------------------------------------------ mask
+    // a tile's 32 pieces (32 rows x 32 columns, eight quads per lane) are dealt to six warps
+    const int drawer = warp < kFirstEpi ? warp - 2 : warp - (kFirstEpi + kResults) + 2;
+    const int y_quads = (A.cols + 3) / 4, groups = (A.cols + 31) / 32;
+    philox::Stream words(A.mask);
+    uint32_t n = 0;
+    for (int t = first; t < A.tiles; t += step, ++n) {
+      const int32_t row0 = (A.tile_row0 ? A.tile_row0[t] : t * 256) + (int)rank * 128;
+      uint32_t* const out = reinterpret_cast<uint32_t*>(gen + kMask + (n & 1) * kMaskBytes);
+      if (!wait_bar(B.mask_empty + (n & 1), ((n >> 1) & 1) ^ 1, abort_flag)) break;
+      for (int piece = drawer; piece < 4 * groups; piece += kDrawers) {
+        const int row = (piece & 3) * 32 + lane, group = piece >> 2;
+        const uint64_t q = (uint64_t)(row0 + row) * y_quads + group * 8;
+        uint32_t bits = 0u;
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+          uint4 w[4];                                      // four quads at a time: a quad is a chain of ten dependent products
+#pragma unroll
+          for (int k = 0; k < 4; ++k) w[k] = words.quad(A.mask, q + 4 * part + k);       // (past the row's end: words that nothing uses)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            bits |= ((w[k].x > A.mask.lim ? 1u : 0u) | (w[k].y > A.mask.lim ? 2u : 0u) | (w[k].z > A.mask.lim ? 4u : 0u) |
+                     (w[k].w > A.mask.lim ? 8u : 0u)) << (16 * part + 4 * k);
+        }
+        out[group * 128 + row] = bits;
+      }
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(B.mask_full + (n & 1));
+    }
   }
   // ------------------------------------------------------------------------------------ the end
   if (*abort_flag) {
@@ -338,10 +379,13 @@ __global__ void __launch_bounds__(kThreads, 1) fused_forward(const __grid_consta
 }  // namespace
 
 int32_t launch_fused(const Maps& maps, const Args& args, int device, int sms, cudaStream_t st) {
-  static std::atomic<int> allowed{0};
-  const int32_t rc = allow_shared_memory(fused_forward, kFusedSmem, device, allowed);
+  static std::atomic<int> allowed{0}, allowed_masked{0};
+  const int32_t rc = args.masked ? allow_shared_memory(fused_forward<true>, kFusedSmem, device, allowed_masked)
+                                 : allow_shared_memory(fused_forward<false>, kFusedSmem, device, allowed);
   if (rc != GNNCO_OK) return rc;
-  return launch_clusters(fused_forward, kFusedSmem, maps, args, args.tiles < resident_pairs(device, sms) ? args.tiles : resident_pairs(device, sms), 2, st);
+  const int pairs = resident_pairs(device, sms), clusters = args.tiles < pairs ? args.tiles : pairs;
+  if (args.masked) return launch_clusters(fused_forward<true>, fused_threads(true), kFusedSmem, maps, args, clusters, 2, st);
+  return launch_clusters(fused_forward<false>, fused_threads(false), kFusedSmem, maps, args, clusters, 2, st);
 }
 
 }  // namespace ff

@@ -156,7 +156,9 @@ __device__ __forceinline__ Two fma(Two a, Two b, Two c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v));
   return d;
 }
-// the hardware's 2^x (2 units of 2^-23), results below 2^-126 as zeros: no range handling around it
+// the hardware's 2^x (2 units of 2^-23) and 1 / x (1 unit), results and arguments below 2^-126 as zeros: no range handling around
+// them.  (1 / x by a Newton and a third-order step on the arithmetic pipes halves the transcendental instructions, but its nine
+// instructions more per pair took the same time alone and more beside the drawing of masks: NEWTON_FIGURES.)
 __device__ __forceinline__ Two exp2(Two x) {
   float a, b;
   x.get(a, b);
@@ -164,17 +166,12 @@ __device__ __forceinline__ Two exp2(Two x) {
   asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
   return Two(a, b);
 }
-// 1 / y for y in [1, 2^120], given -y: the exponent negated in the integer representation (6 % off), one Newton step with its constant
-// moved to halve the largest error (1.5e-3), one of third order (1e-9): 6e-8 with float32's roundings.  On the arithmetic pipes; a
-// second transcendental instruction per element made that pipe the bound (16 a cycle and SM: 2,048 cycles for a tile of 128 x 128,
-// as long as its products at a width of 256).
-__device__ __forceinline__ Two inverse_of_minus(Two ny) {
+__device__ __forceinline__ Two inverse(Two x) {
   float a, b;
-  ny.get(a, b);
-  const Two r0(__uint_as_float(0xfef34800u - __float_as_uint(a)), __uint_as_float(0xfef34800u - __float_as_uint(b)));
-  const Two r1 = r0 * fma(ny, r0, Two(2.0015f));
-  const Two h = fma(ny, r1, Two(1.0f));
-  return fma(r1, fma(h, h, h), r1);
+  x.get(a, b);
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
+  return Two(a, b);
 }
 
 // a = act(g) and, for the backward pass, slope = act'(g).
@@ -182,21 +179,17 @@ __device__ __forceinline__ Two inverse_of_minus(Two ny) {
 //   GELU   E = exp(-g^2 / 2), Phi(-|g|) = E t P(t) with t = 1 / (1 + 0.3 |g| / sqrt 2), P of degree 8 fitted to
 //          erfc(z) exp(z^2) / (2 t) over t (2e-8 of the value everywhere; in float32 4e-7 up to |g| = 2, 1.5e-6 up to 5, where Phi is
 //          3e-7):  a = g Phi(g),  a' = Phi(g) + g E / sqrt(2 pi)
-// (The exponent is kept below 120: at g = -83 SiLU is -1e-34 and stays there, times |g|.)
 template <int ACT, bool BACK>
 __device__ __forceinline__ void activate(Two g, Two& a, Two& slope) {
   if (ACT == GNNCO_SILU) {
-    float x0, x1;
-    (g * Two(-1.44269504f)).get(x0, x1);
-    const Two s = inverse_of_minus(fma(exp2(Two(fminf(x0, 119.0f), fminf(x1, 119.0f))), Two(-1.0f), Two(-1.0f)));
+    const Two s = inverse(exp2(g * Two(-1.44269504f)) + Two(1.0f));
     a = g * s;
     if (BACK) slope = fma(a, fma(s, Two(-1.0f), Two(1.0f)), s);
   } else if (ACT == GNNCO_GELU) {
     float g0, g1, q0, q1;
     g.get(g0, g1);
     const Two E = exp2(g * g * Two(-0.72134752f));
-    // (E is 0 past |g| = 14)
-    const Two t = inverse_of_minus(fma(Two(fminf(fabsf(g0), 64.0f), fminf(fabsf(g1), 64.0f)), Two(-0.21213203f), Two(-1.0f)));
+    const Two t = inverse(fma(Two(fabsf(g0), fabsf(g1)), Two(0.21213203f), Two(1.0f)));
     Two P = fma(t, Two(-0.06476137787103653f), Two(0.24278123676776886f));
     P = fma(t, P, Two(-0.25613829493522644f));
     P = fma(t, P, Two(0.2738591432571411f));
@@ -833,10 +826,10 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
 
 // -------------------------------------------------------------------------------------------- launch
 template <typename Kernel>
-int32_t launch_clusters(Kernel kernel, uint32_t smem, const Maps& maps, const Args& args, int clusters, int ctas, cudaStream_t st) {
+int32_t launch_clusters(Kernel kernel, int threads, uint32_t smem, const Maps& maps, const Args& args, int clusters, int ctas, cudaStream_t st) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(clusters * ctas);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -861,7 +854,7 @@ int32_t launch_one(const Maps& maps, const Args& args, int device, int sms, cuda
   const int32_t rc = allow_shared_memory(kernel, kSmem, device, allowed);
   if (rc != GNNCO_OK) return rc;
   const int most = PAIR ? resident_pairs(device, sms) : sms;
-  return launch_clusters(kernel, kSmem, maps, args, args.tiles < most ? args.tiles : most, PAIR ? 2 : 1, st);
+  return launch_clusters(kernel, kThreads, kSmem, maps, args, args.tiles < most ? args.tiles : most, PAIR ? 2 : 1, st);
 }
 
 }  // namespace ff

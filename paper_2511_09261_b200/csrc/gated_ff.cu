@@ -136,21 +136,22 @@ bool map_rows(CUtensorMap* m, const void* base, int64_t rows, int cols, int64_t 
   const uint64_t dims[3] = {(uint64_t)cols, (uint64_t)rows, (uint64_t)limbs};
   const uint64_t strides[2] = {(uint64_t)ld * 2, (uint64_t)(limbs > 1 ? limb : ld) * 2};
   const uint32_t box[3] = {64u, (uint32_t)box_rows, (uint32_t)limbs};
-  return encode_bf16_boxes(m, base, 3, dims, strides, box);
+  return encode_boxes(m, false, base, 3, dims, strides, box);
 }
-// results: boxes of 32 x 32
-bool map_out(CUtensorMap* m, const void* base, int64_t rows, int cols, int64_t ld) {
-  const uint64_t dims[2] = {(uint64_t)cols, (uint64_t)rows};
-  const uint64_t strides[1] = {(uint64_t)ld * 2};
-  const uint32_t box[2] = {32u, 32u};
-  return encode_bf16_boxes(m, base, 2, dims, strides, box);
+// results: boxes of 32 rows
+bool map_out(CUtensorMap* m, bool f32, const void* base, int64_t rows, int cols, int64_t ld, int64_t limb, int limbs, int box_cols) {
+  const uint64_t es = f32 ? 4 : 2;
+  const uint64_t dims[3] = {(uint64_t)cols, (uint64_t)rows, (uint64_t)limbs};
+  const uint64_t strides[2] = {(uint64_t)ld * es, (uint64_t)(limbs > 1 ? limb : ld) * es};
+  const uint32_t box[3] = {(uint32_t)box_cols, 32u, 1u};
+  return encode_boxes(m, f32, base, 3, dims, strides, box);
 }
 // [limbs][sets][rows][cols]
 bool map_sets(CUtensorMap* m, const void* base, int64_t sets, int rows, int cols, int64_t ld, int limbs, int box_rows) {
   const uint64_t dims[4] = {(uint64_t)cols, (uint64_t)rows, (uint64_t)sets, (uint64_t)limbs};
   const uint64_t strides[3] = {(uint64_t)ld * 2, (uint64_t)rows * ld * 2, (uint64_t)sets * rows * ld * 2};
   const uint32_t box[4] = {64u, (uint32_t)box_rows, 1u, (uint32_t)limbs};
-  return encode_bf16_boxes(m, base, 4, dims, strides, box);
+  return encode_boxes(m, false, base, 4, dims, strides, box);
 }
 
 // ------------------------------------------------------------------------------------ the plan of a call
@@ -379,7 +380,8 @@ struct Call {
     if (dy)
       ok = ok && map_rows(&m.a[0], dy->p, d->rows, d->F_out, dy->ld, dy->limb, limbs, 128) &&
            map_sets(&m.b[2], wd.p, d->sets, d->H, d->F_out, wd.ld, limbs, pair ? a.nt / 2 : a.nt);
-    else if (limbs == 1) ok = ok && map_out(&m.out, out[0].p, d->rows, d->H, out[0].ld);
+    for (int k = 0; k < (dy ? 3 : 1); ++k)
+      ok = ok && map_out(&m.out[k], false, out[k].p, d->rows, d->H, out[k].ld, out[k].limb, limbs, dy ? 16 : 32);
     if (!ok) return GNNCO_CUDA_ERROR;
     return launch(dy ? ff::kGluBack : ff::kGlu, pair, m, &a, (int64_t)a.m_tiles * a.n_tiles);
   }
@@ -454,7 +456,7 @@ struct Call {
     a->y_ld = ld;
     a->y_f32 = d->feat_dtype == GNNCO_F32;
     a->y_vectors = ((uintptr_t)y & 15) == 0 && ld % (a->y_f32 ? 4 : 8) == 0;
-    return a->y_f32 || !a->y_vectors || map_out(&m->out, y, d->rows, cols, ld);
+    return !a->y_vectors || map_out(&m->out[0], a->y_f32, y, d->rows, cols, ld, 0, 1, a->y_f32 ? 16 : 32);
   }
   int32_t weight_grads(const Operand& x, const Operand& dy, const Operand* hdd, const gnnco_gated_ff_grads* g, float* scratch) {
     const Chunks c = chunks_of(h, d);

@@ -24,7 +24,8 @@ enum Kind { kGlu, kGluBack, kDown, kDx, kWeights };
 
 struct Maps {
   CUtensorMap a[3], b[3];
-  CUtensorMap out;                     // bfloat16 h, y or dx in boxes of 32 x 32
+  CUtensorMap out[3];                  // results in boxes of 32 rows: h, dg, du in 32 columns (16 where there are three), y or dx
+                                       // in 64 bytes of columns
 };
 
 // one weight gradient: [M x N] or, transposed, [N x M] in memory
@@ -73,6 +74,6 @@ int resident_pairs(int device, int sms);
 
 }  // namespace ff
 
-// A tensor map of bfloat16 boxes, swizzled over 128 bytes (inner box 64 elements: the layout of the MMA operands) or over 64 (32
-// elements) (tc_gemm2.cu).
-bool encode_bf16_boxes(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box);
+// A tensor map of bfloat16 or float32 boxes, swizzled over the bytes of a box's row where these are 128 (the layout of the MMA operands) or
+// 64, plain where they are 32 (tc_gemm2.cu).
+bool encode_boxes(CUtensorMap* m, bool f32, const void* base, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box);

@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(fused_threads(MASKED), 1) fused_forward(const 
 #pragma unroll
           for (int k = 0; k < 32; ++k) f[k] = (keep >> k) & 1u ? f[k] * A.mask.scale : 0.0f;
         }
-        if (A.y_vectors && y_rows >= 32) stage_and_store(&maps.out, stage_at, lane, c0, y_row0, f);
+        if (A.y_vectors && y_rows >= 32) stage_limbs<1>(&maps.out[0], stage_at, lane, c0, y_row0, f);
         else store_rows<false>(stage, lane, y_rows, y_row0, c0, A.cols, A.y, A.y_ld, f);
       }
       if (MASKED) {

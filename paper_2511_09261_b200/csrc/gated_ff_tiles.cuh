@@ -226,24 +226,78 @@ __device__ __forceinline__ void gate(float (&f)[TENSORS][W], float scale) {
     }
   }
 }
-// One box (rows of 64 bytes, swizzled in units of 16 by bits 1 and 2 of the row) from a result warp's staging tile
-__device__ __forceinline__ void store_box(const CUtensorMap* map, uint32_t from, int32_t x, int32_t y) {
-  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(from) : "memory");
+// A box from a result warp's staging tile (2 KB) to columns x .., rows y .. and limb z of a result.  A lane that stored its row by
+// itself would send 32 pieces of 32 rows per instruction: for float32 results that took longer than the products.
+__device__ __forceinline__ void store_box(const CUtensorMap* map, uint32_t from, int32_t x, int32_t y, int32_t z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y), "r"(z), "r"(from) : "memory");
   asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
-__device__ __forceinline__ void store_box_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+// all boxes but the last LATER have been read from shared memory
+template <int LATER = 0>
+__device__ __forceinline__ void store_box_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LATER) : "memory"); }
 __device__ __forceinline__ void store_box_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-// 32 values of this lane's row as bfloat16 into the staging tile, and the tile's 32 rows out; whole warp
-__device__ __forceinline__ void stage_and_store(const CUtensorMap* map, uint32_t stage, int lane, int32_t x, int32_t y, const float (&f)[32]) {
-  if (lane == 0) store_box_read();                         // the tile before has left
+// Rows of 64 bytes (16 words of this lane's row), in units of 16 bytes swizzled by bits 1 and 2 of the row; whole warp
+__device__ __forceinline__ void stage_row(const CUtensorMap* map, uint32_t stage, int lane, int32_t x, int32_t y, int32_t z, const uint32_t (&w)[16]) {
+  if (lane == 0) store_box_read();                         // the box before has left the tile
   __syncwarp();
 #pragma unroll
   for (int q = 0; q < 4; ++q)
-    tc::st_shared16(stage + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4), vio::pack_bf16(f[8 * q], f[8 * q + 1]),
-                    vio::pack_bf16(f[8 * q + 2], f[8 * q + 3]), vio::pack_bf16(f[8 * q + 4], f[8 * q + 5]), vio::pack_bf16(f[8 * q + 6], f[8 * q + 7]));
+    tc::st_shared16(stage + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4), w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
   tc::fence_proxy_async_smem();
   __syncwarp();
-  if (lane == 0) store_box(map, stage, x, y);
+  if (lane == 0) store_box(map, stage, x, y, z);
+}
+// 32 values of this lane's row as LIMBS bfloat16
+template <int LIMBS>
+__device__ __forceinline__ void stage_limbs(const CUtensorMap* map, uint32_t stage, int lane, int32_t x, int32_t y, float (&f)[32]) {
+#pragma unroll
+  for (int l = 0; l < LIMBS; ++l) {
+    uint32_t w[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      w[e] = vio::pack_bf16(f[2 * e], f[2 * e + 1]);
+      if (l + 1 < LIMBS) {
+        f[2 * e] -= vio::bf_lo(w[e]);                      // exact
+        f[2 * e + 1] -= vio::bf_hi(w[e]);
+      }
+    }
+    stage_row(map, stage, lane, x, y, l, w);
+  }
+}
+// 16 values of this lane's row as LIMBS bfloat16: rows of 32 bytes, in the halves of the tile in turn
+template <int LIMBS>
+__device__ __forceinline__ void stage_limbs(const CUtensorMap* map, uint32_t stage, int lane, int32_t x, int32_t y, float (&f)[16], uint32_t& turn) {
+#pragma unroll
+  for (int l = 0; l < LIMBS; ++l) {
+    uint32_t w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      w[e] = vio::pack_bf16(f[2 * e], f[2 * e + 1]);
+      if (l + 1 < LIMBS) {
+        f[2 * e] -= vio::bf_lo(w[e]);                      // exact
+        f[2 * e + 1] -= vio::bf_hi(w[e]);
+      }
+    }
+    if (lane == 0) store_box_read<1>();
+    __syncwarp();
+    const uint32_t at = stage + turn * 1024;
+    tc::st_shared16(at + lane * 32, w[0], w[1], w[2], w[3]);
+    tc::st_shared16(at + lane * 32 + 16, w[4], w[5], w[6], w[7]);
+    tc::fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) store_box(map, at, x, y, l);
+    turn ^= 1;
+  }
+}
+// 32 values of this lane's row as float32: two boxes of 16 columns
+__device__ __forceinline__ void stage_floats(const CUtensorMap* map, uint32_t stage, int lane, int32_t x, int32_t y, const float (&f)[32]) {
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    uint32_t w[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(f[16 * b + e]);
+    stage_row(map, stage, lane, x + 16 * b, y, 0, w);
+  }
 }
 
 // 32 values of this lane's row (row0 + lane, if that is below rows_here) to out[row][c0 ..], for rows that start anywhere or end inside
@@ -614,6 +668,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
     constexpr int kTensors = KIND == kGlu ? 2 : KIND == kGluBack ? 3 : 1;
     float v[kSums ? kGroups : 1][kTensors][kW];
     int part = team;
+    uint32_t turn = 0;                                     // half of the staging tile
     bool ok = true;
     auto release = [&]() {
       tc::tc_fence_before_sync();
@@ -709,14 +764,17 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
           else if (A.act == GNNCO_GELU) gate<kBack, GNNCO_GELU>(f, A.scale);
           else gate<kBack, GNNCO_RELU>(f, A.scale);
           const int rows_here = T.rows - (local - lane);
-          if constexpr (KIND == kGlu && LIMBS == 1) {
-            if (rows_here >= 32) {
-              stage_and_store(&maps.out, stage_at, lane, c0, (int32_t)(T.row0 + local - lane), f[0]);
-              continue;
+          if (rows_here >= 32) {
+            const int32_t y = T.row0 + local - lane;
+            if constexpr (KIND == kGlu) {
+              stage_limbs<LIMBS>(&maps.out[0], stage_at, lane, c0, y, f[0]);
+            } else {
+              stage_limbs<LIMBS>(&maps.out[0], stage_at, lane, c0, y, f[0], turn);
+              stage_limbs<LIMBS>(&maps.out[1], stage_at, lane, c0, y, f[1], turn);
+              stage_limbs<LIMBS>(&maps.out[2], stage_at, lane, c0, y, f[kTensors - 1], turn);
             }
-          }
-          // limbs, and the ragged end of a subgraph, where a box would reach into the next one's rows
-          if (lane < rows_here) {
+          } else if (lane < rows_here) {
+            // the ragged end of a subgraph: a box would reach into the next one's rows
             const int64_t at = (int64_t)(T.row0 + local) * A.out_ld + c0;
             const int width = (int)(A.out_ld - c0);
             store_limbs<LIMBS>(A.out[0] + at, A.out_limb, width, f[0]);
@@ -777,9 +835,10 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
             ld = A.y_ld;
             vectors = A.y_vectors;
           }
-          if constexpr (LIMBS == 1 && !kAlongRows) {
+          if constexpr (!kAlongRows) {
             if (vectors && T.rows - (local - lane) >= 32) {
-              stage_and_store(&maps.out, stage_at, lane, c0, (int32_t)(row - lane), f[0]);
+              if constexpr (LIMBS == 1) stage_limbs<1>(&maps.out[0], stage_at, lane, c0, (int32_t)(row - lane), f[0]);
+              else stage_floats(&maps.out[0], stage_at, lane, c0, (int32_t)(row - lane), f[0]);
               continue;
             }
           }
@@ -807,7 +866,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
         }
       }
     }
-    if (LIMBS == 1 && !kAlongRows && lane == 0) store_box_done();
+    if (!kAlongRows && lane == 0) store_box_done();
   }
   // ------------------------------------------------------------------------------------ the end
   if (*abort_flag) {

@@ -1038,8 +1038,8 @@ weight_grad_tc_pair(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 
 }  // namespace
 
-// A tensor map of bfloat16 boxes of any rank, swizzled over the bytes of a box's row: 128 (64 elements) or 64 (32).
-bool encode_bf16_boxes(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box) {
+// A tensor map of boxes of any rank, swizzled over the bytes of a box's row: 128 or 64 (32: plain).
+bool encode_boxes(CUtensorMap* m, bool f32, const void* base, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box) {
   EncodeTiledFn enc = encode_tiled();
   if (!enc) return false;
   cuuint64_t d[5], s[5];
@@ -1050,8 +1050,9 @@ bool encode_bf16_boxes(CUtensorMap* m, const void* base, int rank, const uint64_
     e[i] = 1u;
     if (i + 1 < rank) s[i] = strides[i];
   }
-  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), d, s, b, e, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             box[0] == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const uint32_t bytes = box[0] * (f32 ? 4 : 2);
+  return enc(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), d, s, b, e, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // The pair form is used for the widths where a single CTA cannot hold a second operand tile.

@@ -251,6 +251,14 @@ def _empty(shape, dtype, like, stream):
         return like.new_empty(shape, dtype=dtype)
 
 
+def _empty_as(like, shape, dtype, stream):
+    """``_empty``, a little sooner where ``like`` has this very shape and type (small blocks take as long as their call)."""
+    if stream is None and like.shape == shape and like.dtype == dtype and like.is_contiguous():
+        import torch
+        return torch.empty_like(like)
+    return _empty(tuple(shape), dtype, like, stream)
+
+
 ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
 MUON_COEFS = (3.4445, -4.7750, 2.0315)
 
@@ -855,27 +863,29 @@ class PartitionedGraph:
 
     def _gated_ff_desc(self, x, w_gate, w_up, w_down, act, drop):
         xd, wd = _feat_code(x, "x"), _feat_code(w_gate, "w_gate")
-        if x.dim() != 2 or x.shape[1] < 1:
-            raise ValueError("x must be [rows, F]")
-        for w, what in ((w_gate, "w_gate"), (w_up, "w_up"), (w_down, "w_down")):
-            _require(w, w_gate.dtype, what)
-            if w.dim() != 3 or 0 in w.shape or w.device != self.device:
-                raise ValueError("%s must be [sets, rows, columns] on %s" % (what, self.device))
+        if x.dim() != 2 or w_gate.dim() != 3:
+            raise ValueError("x must be [rows, F], w_gate [sets, F, H]")
         rows, F = x.shape
         sets, _, H = w_gate.shape
-        F_out = w_down.shape[2]
-        if w_gate.shape != (sets, F, H) or w_up.shape != (sets, F, H) or w_down.shape != (sets, H, F_out):
+        dtype, device = w_gate.dtype, self.device
+        for w, what in ((w_gate, "w_gate"), (w_up, "w_up"), (w_down, "w_down")):
+            if getattr(w, "dtype", None) != dtype or not w.is_contiguous() or w.device != device:
+                raise TypeError("%s must be a contiguous %s tensor on %s" % (what, dtype, device))
+        F_out = w_down.shape[-1]
+        if (w_gate.shape != (sets, F, H) or w_up.shape != (sets, F, H) or w_down.shape != (sets, H, F_out)
+                or not (sets and F and H and F_out)):
             raise ValueError("x [rows, F] takes w_gate and w_up [sets, F, H] and w_down [sets, H, F_out]")
         if sets != 1 and (sets != self.S or rows != self.n):
             raise ValueError("weights of %d sets need the %d rows of %d subgraphs" % (sets, self.n, self.S))
-        if act not in ACTIVATIONS:
+        code = ACTIVATIONS.get(act)
+        if code is None:
             raise ValueError("act must be one of %s" % ", ".join(ACTIVATIONS))
         if (F | H | F_out) >> 31:
             _int32(F, H, F_out)
-        d = GatedFfDesc(rows, F, H, F_out, xd, wd, sets, ACTIVATIONS[act], x.data_ptr(),
-                        self._rows(x, x.dtype, rows, F, "x"), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr())
+        d = GatedFfDesc(rows, F, H, F_out, xd, wd, sets, code, x.data_ptr(), self._rows(x, x.dtype, rows, F, "x"),
+                        w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr())
         if drop is not None:
-            d.drop = ctypes.pointer(drop.params(self.device))
+            d.drop = ctypes.pointer(drop.params(device))
         return d
 
     def _gated_ff_area(self, d, backward, like, ws, stream):
@@ -896,11 +906,11 @@ class PartitionedGraph:
         ``w_down`` [sets, H, F_out], one set for all rows or one per subgraph.  The weights have x's type or are float32.
         ``ws`` may be a uint8 tensor kept between calls that follow each other on one stream."""
         d = self._gated_ff_desc(x, w_gate, w_up, w_down, act, drop)
-        shape, y_ld = (d.rows, d.F_out), d.F_out
+        y_ld = d.F_out
         if out is None:
-            out = _empty(shape, x.dtype, x, stream)
+            out = _empty_as(x, (d.rows, y_ld), x.dtype, stream)
         else:
-            y_ld = self._rows(out, x.dtype, *shape, "out")
+            y_ld = self._rows(out, x.dtype, d.rows, y_ld, "out")
         ws = self._gated_ff_area(d, 0, x, ws, stream)
         _check(self._lib.gnnco_gated_ff(self._handle, ctypes.byref(d), out.data_ptr(), y_ld, ws.data_ptr(), ws.numel(),
                                         _stream_ptr(stream)), "gnnco_gated_ff")
@@ -917,15 +927,18 @@ class PartitionedGraph:
             raise ValueError("nothing is wanted, or dx is given and not wanted")
         g = GatedFfGrads()
         if want_dx:
+            g.dx_ld = d.F
             if dx is None:
-                dx = _empty((d.rows, d.F), x.dtype, x, stream)
-            g.dx, g.dx_ld = dx.data_ptr(), self._rows(dx, x.dtype, d.rows, d.F, "dx")
+                dx = _empty_as(x, (d.rows, d.F), x.dtype, stream)
+            else:
+                g.dx_ld = self._rows(dx, x.dtype, d.rows, d.F, "dx")
+            g.dx = dx.data_ptr()
         dws = [None, None, None]
         if want_dw:
             dw_dtype = dw_dtype or w_gate.dtype
             if dw_dtype not in _feat_codes:
                 raise TypeError("dw_dtype must be float32 or bfloat16")
-            dws = [_empty(tuple(w.shape), dw_dtype, x, stream) for w in (w_gate, w_up, w_down)]
+            dws = [_empty_as(w, w.shape, dw_dtype, stream) for w in (w_gate, w_up, w_down)]
             g.dw_gate, g.dw_up, g.dw_down = (t.data_ptr() for t in dws)
             g.dw_dtype = _feat_codes[dw_dtype]
         ws = self._gated_ff_area(d, 1, x, ws, stream)

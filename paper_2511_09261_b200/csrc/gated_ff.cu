@@ -363,7 +363,7 @@ struct Call {
                                 blocks_of(d->F, 64) + (dy ? blocks_of(d->F_out, 64) : 0), dy ? nt_of(true) * 3 / 2 : nt_of(true) * 2,
                                 dy ? nt_of(false) * 3 / 2 : nt_of(false) * 2);
     Args a = {};
-    Maps m;
+    Maps m = {};
     rows_of(&a, pair);
     a.nt = nt_of(pair);
     a.n_tiles = (int32_t)blocks_of(d->H, a.nt);
@@ -395,7 +395,7 @@ struct Call {
   int32_t down(const Operand& hh, const Operand& wd, void* y, int64_t y_ld) {
     const bool pair = wide_pairs(d->F_out, blocks_of(d->H, 64));
     Args a = {};
-    Maps m;
+    Maps m = {};
     rows_of(&a, pair);
     a.nt = wide_tile(pair, d->F_out);
     a.n_tiles = (int32_t)blocks_of(d->F_out, a.nt);
@@ -415,7 +415,7 @@ struct Call {
   }
   int32_t fused(const Operand& x, const Operand& wg, const Operand& wu, const Operand& wd, void* y, int64_t y_ld) {
     Args a = {};
-    Maps m;
+    Maps m = {};
     rows_of(&a, true);
     a.n_tiles = 1;
     a.K[0] = d->F;
@@ -437,7 +437,7 @@ struct Call {
   int32_t input_grad(const Operand& dg, const Operand& du, const Operand& wg, const Operand& wu, void* dx, int64_t dx_ld) {
     const bool pair = wide_pairs(d->F, 2 * blocks_of(d->H, 64));
     Args a = {};
-    Maps m;
+    Maps m = {};
     rows_of(&a, pair);
     a.nt = wide_tile(pair, d->F);
     a.n_tiles = (int32_t)blocks_of(d->F, a.nt);
@@ -465,7 +465,7 @@ struct Call {
     const int32_t R[3] = {d->F, d->F, d->H}, C[3] = {d->H, d->H, d->F_out};
     const Operand row_op[3] = {x, x, hdd[0]}, col_op[3] = {hdd[1], hdd[2], dy};
     Args a = {};
-    Maps m;
+    Maps m = {};
     rows_of(&a, false);
     a.tile_row0 = nullptr;
     a.out_f32 = f32;

@@ -95,7 +95,6 @@ __global__ void __launch_bounds__(fused_threads(MASKED), 1) fused_forward(const 
   tc::cluster_sync_all();
   tc::tc_fence_after_sync();
   const uint32_t tmem = B.tmem;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
 
   if (warp == kCopyWarp) {
     // -------------------------------------------------------------------------------- operands
@@ -104,6 +103,7 @@ __global__ void __launch_bounds__(fused_threads(MASKED), 1) fused_forward(const 
     auto even = [&](uint64_t* bar) { return tc::map_to_cta(tc::smem_u32(bar), 0); };
     auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_bar(bar, parity, abort_flag)) != 0; };
     Walk<kDown, true, true, true> walk(A, first, step);
+    asm volatile("griddepcontrol.wait;" ::: "memory");     // (as in gated_ff_tiles.cuh: everything else hangs on the copies)
     int slot = 0, d = 0;
     uint32_t g_phase = 1, d_phase = 1, x_phase = 1;        // the first round waits for nothing
     bool ok = true;

@@ -65,6 +65,7 @@ __device__ __forceinline__ void load_box_of_set(uint32_t leader, uint32_t dst, c
                  "@go cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(set), "r"(0), "r"(bar), "r"(leader) : "memory");
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 // announces `bytes` on a barrier of this CTA or, by cluster address, of the pair's even one
 template <bool PAIR>
 __device__ __forceinline__ void expect_bytes(uint32_t leader, uint32_t bar, uint32_t bytes) {
@@ -471,6 +472,9 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
   const uint32_t rank = PAIR ? tc::cluster_ctarank() : 0u;
   const int first = blockIdx.x / kCtas, step = gridDim.x / kCtas;
 
+  constexpr int kMapsA = KIND == kWeights ? 3 : KIND == kDx || KIND == kGluBack ? 2 : 1;
+  constexpr int kMapsB = KIND == kWeights || KIND == kGluBack ? 3 : KIND == kDown ? 1 : 2;
+  if (warp == kCopyWarp && lane < kMapsA + kMapsB) prefetch_map(lane < kMapsA ? &maps.a[lane] : &maps.b[lane - kMapsA]);
   if (threadIdx.x == 0) {
     for (int i = 0; i < kSlots; ++i) {
       tc::mbar_init(full + i, kCtas);
@@ -493,7 +497,6 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
   if (PAIR) tc::cluster_sync_all();
   tc::tc_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
-  asm volatile("griddepcontrol.wait;" ::: "memory");       // the operands are complete from here on
   const int more = kAlongRows ? 0 : (A.K[1] + 63) >> 6;    // stages of the second contraction
 
   if (warp == kCopyWarp) {
@@ -504,6 +507,9 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
     uint32_t phase = 1;                                    // of `empty`: the first round waits for nothing
     bool ok = true;
     Walk<KIND, PAIR, !kAlongRows, true> walk(A, first, step);
+    // The operands are complete from here on.  (The other warps' work hangs on the copies, the results they write included, and the
+    // tables are older than the launch before this one.)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     while (walk.any() && ok) {
       const Tile T = walk.take();
       const int set = T.set;

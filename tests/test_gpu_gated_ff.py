@@ -382,3 +382,14 @@ def test_many_rows_in_bfloat16(F, H, Fo, act, p):
     u = make(rows, 1, F, H, Fo, "bf16", seed=H + 1)
     check_forward(g, u, None, act, "bf16", drop, mask)
     assert g.async_status() == gnnco.OK
+
+
+def test_in_place_as_one_kernel():
+    import torch
+    sizes = [300, 257, 40] * 60
+    g = load(sizes)
+    t = make(sum(sizes), len(sizes), 96, 200, 96, "bf16")
+    want = g.gated_ff(t[0], *t[2:])
+    x = t[0].clone()
+    g.gated_ff(x, *t[2:], out=x)
+    assert torch.equal(x, want)

@@ -854,7 +854,7 @@ class PartitionedGraph:
         x_ld = self._rows(x, x.dtype, rows, F, "x")
         out_ld = F
         if out is None:
-            out = _empty((rows, F), x.dtype, x, stream)
+            out = _empty_as(x, (rows, F), x.dtype, stream)
         else:
             out_ld = self._rows(out, x.dtype, rows, F, "out")
         _check(self._lib.gnnco_dropout(self._handle, dt, rows, F, x.data_ptr(), x_ld, ctypes.byref(d), out.data_ptr(), out_ld,

@@ -70,30 +70,39 @@ __global__ void __launch_bounds__(256) drop_vectors(const __grid_constant__ Drop
   }
 }
 
-// any width and alignment: a quad of columns per thread, element by element
-template <typename T>
+// any width and alignment: UNROLL quads of columns per thread, element by element
+template <typename T, int UNROLL>
 __global__ void __launch_bounds__(256) drop_quads(const __grid_constant__ DropArgs A) {
   const int64_t items = A.rows * A.groups;
   philox::Stream words(A.m);
-  for (int64_t base = (int64_t)blockIdx.x * 256; base < items; base += (int64_t)gridDim.x * 256) {
-    const int64_t row0 = base / A.groups, i = base + threadIdx.x;
-    if (i >= items) break;
-    const uint32_t off = (uint32_t)(base - row0 * A.groups) + threadIdx.x, r = off / (uint32_t)A.groups;
-    const int c = (int)(off - r * (uint32_t)A.groups) * 4, count = min(4, A.F - c);
-    const T* from = static_cast<const T*>(A.x) + (row0 + r) * A.x_ld + c;
-    T* to = static_cast<T*>(A.out) + (row0 + r) * A.out_ld + c;
-    vio::Raw<T, 1> v[4];
+  for (int64_t base = (int64_t)blockIdx.x * (256 * UNROLL); base < items; base += (int64_t)gridDim.x * (256 * UNROLL)) {
+    const int64_t row0 = base / A.groups;
+    const uint32_t rest = (uint32_t)(base - row0 * A.groups);
+    vio::Raw<T, 1> v[UNROLL][4];
+    T* to[UNROLL];
+    int count[UNROLL];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (k < count) v[k].template load<true>(from + k);
-    const uint4 w = words.quad(A.m, (uint64_t)i);
-    const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+    for (int u = 0; u < UNROLL; ++u) {
+      const uint32_t off = rest + u * 256 + threadIdx.x, r = off / (uint32_t)A.groups;
+      const int c = (int)(off - r * (uint32_t)A.groups) * 4;
+      count[u] = base + u * 256 + threadIdx.x < items ? min(4, A.F - c) : 0;
+      const T* const from = static_cast<const T*>(A.x) + (row0 + r) * A.x_ld + c;
+      to[u] = static_cast<T*>(A.out) + (row0 + r) * A.out_ld + c;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (k < count) {
-        const float f[1] = {pick(word[k], A.m, v[k].get(0))};
-        vio::store_stream<T, 1>(to + k, f);
-      }
+      for (int k = 0; k < 4; ++k)
+        if (k < count[u]) v[u][k].template load<true>(from + k);
+    }
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      const uint4 w = words.quad(A.m, (uint64_t)(base + u * 256 + threadIdx.x));
+      const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < count[u]) {
+          const float f[1] = {pick(word[k], A.m, v[u][k].get(0))};
+          vio::store_stream<T, 1>(to[u] + k, f);
+        }
+    }
   }
 }
 
@@ -126,7 +135,7 @@ void launch_drop(gnnco_handle* h, DropArgs A, cudaStream_t st) {
     }
   }
   A.groups = (A.F + 3) / 4;
-  drop_quads<T><<<blocks(256), 256, 0, st>>>(A);
+  drop_quads<T, kUnroll><<<blocks(256 * kUnroll), 256, 0, st>>>(A);
 }
 
 }  // namespace

@@ -215,7 +215,9 @@ Chunks chunks_of(const gnnco_handle* h, const gnnco_gated_ff_desc* d) {
     c.slots = h->n_wg_slots;
     return c;
   }
-  // one set: enough runs that every SM has a tile of 128 x 128, none shorter than 512 rows
+  // one set: enough runs that every SM has a tile of 128 x 128, none shorter than 512 rows -- and none longer than 65,536: the tensor
+  // core cuts off what does not fit when it adds 16 rows to an accumulator, up to 2^-23 of it each time (4,096 times here: 5e-4 at
+  // most, in bfloat16 features less than the stored dg's 2^-8; a million rows in one run would lose 1 %)
   ff::Problem p[3];
   shape_problem(p, d->F, d->H, false, true);
   p[1] = p[0];
@@ -223,11 +225,19 @@ Chunks chunks_of(const gnnco_handle* h, const gnnco_gated_ff_desc* d) {
   const int64_t tiles = tiles_of(p);
   int64_t runs = tiles >= h->sm_count ? 1 : blocks_of(h->sm_count, tiles);
   if (runs > blocks_of(d->rows, 512)) runs = blocks_of(d->rows, 512);
+  if (runs < blocks_of(d->rows, 65536)) runs = blocks_of(d->rows, 65536);
   if (runs < 1) runs = 1;
   c.rows = (int32_t)((blocks_of(d->rows, runs) + 63) / 64 * 64);
   c.count = c.rows > 0 ? (int32_t)blocks_of(d->rows, c.rows) : 1;
   c.slots = c.count > 1 ? c.count : 0;
   return c;
+}
+
+// Both products in one kernel (gated_ff_fused.cu), where its tiles of 256 rows keep all pairs of CTAs busy.
+bool fuses(const gnnco_handle* h, const gnnco_gated_ff_desc* d) {
+  if (d->feat_dtype != GNNCO_BF16 || d->F > 256 || d->F_out > 256) return false;
+  const int64_t pairs = ff::resident_pairs(h->device, h->sm_count), tiles = d->sets > 1 ? h->n_pairs : blocks_of(d->rows, 256);
+  return pairs > 0 && tiles >= pairs;
 }
 
 Work lay_out(const gnnco_handle* h, const gnnco_gated_ff_desc* d, bool backward) {
@@ -248,7 +258,7 @@ Work lay_out(const gnnco_handle* h, const gnnco_gated_ff_desc* d, bool backward)
   w.wg = take(!direct(d->w_gate, d->H, d->w_dtype), limbs * sets * d->F * up8(d->H));
   w.wu = take(!direct(d->w_up, d->H, d->w_dtype), limbs * sets * d->F * up8(d->H));
   w.wd = take(!direct(d->w_down, d->F_out, d->w_dtype), limbs * sets * d->H * up8(d->F_out));
-  w.h = take(true, limbs * d->rows * up16(d->H));
+  w.h = take(backward || !fuses(h, d), limbs * d->rows * up16(d->H));
   if (backward) {
     w.dg = take(true, limbs * d->rows * up16(d->H));
     w.du = take(true, limbs * d->rows * up16(d->H));
@@ -389,7 +399,11 @@ struct Call {
     const int p = wide_tile(true, cols), q = wide_tile(false, cols);
     return use_pairs(row_tiles(true) * blocks_of(cols, p), row_tiles(false) * blocks_of(cols, q), stages, p, q);
   }
-  static int wide_tile(bool pair, int cols) { return pair ? (cols > 128 ? 256 : 128) : (cols > 64 ? 128 : 64); }
+  // columns of a tile of y or dx: wide, but for single CTAs that would not fill the GPU
+  int wide_tile(bool pair, int cols) const {
+    if (pair) return cols > 128 ? 256 : 128;
+    return cols > 64 && row_tiles(false) * blocks_of(cols, 128) >= h->sm_count ? 128 : 64;
+  }
 
   // y = drop(h Wd)
   int32_t down(const Operand& hh, const Operand& wd, void* y, int64_t y_ld) {
@@ -407,11 +421,6 @@ struct Call {
         !map_sets(&m.b[0], wd.p, d->sets, d->H, d->F_out, wd.ld, limbs, 64))
       return GNNCO_CUDA_ERROR;
     return launch(ff::kDown, pair, m, &a, (int64_t)a.m_tiles * a.n_tiles);
-  }
-  // Both products in one kernel (gated_ff_fused.cu), where its tiles of 256 rows keep all pairs of CTAs busy.
-  bool fuses() const {
-    return limbs == 1 && d->F <= 256 && d->F_out <= 256 && ff::resident_pairs(h->device, h->sm_count) > 0 &&
-           row_tiles(true) >= ff::resident_pairs(h->device, h->sm_count);
   }
   int32_t fused(const Operand& x, const Operand& wg, const Operand& wu, const Operand& wd, void* y, int64_t y_ld) {
     Args a = {};
@@ -576,7 +585,7 @@ extern "C" int32_t gnnco_gated_ff(gnnco_handle* h, const gnnco_gated_ff_desc* d,
   hh.limb = d->rows * hh.ld;
   c.pack();
   int32_t r;
-  if (c.fuses()) {
+  if (fuses(h, d)) {
     r = c.fused(x, wg, wu, wd, y, y_ld);
   } else {
     r = c.gates(x, nullptr, wg, wu, wd, &hh);

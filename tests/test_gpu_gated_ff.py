@@ -393,3 +393,23 @@ def test_in_place_as_one_kernel():
     x = t[0].clone()
     g.gated_ff(x, *t[2:], out=x)
     assert torch.equal(x, want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_weight_gradients_of_more_rows_than_one_run_takes(single, dtype):
+    """150,000 rows with one set: three runs at least, whose sums are joined.  Sums of that many terms are compared with the same
+    products in float64 on the GPU, by norm: float32's chains of some thousand roundings are random."""
+    import torch
+    rows, F, H = 150_001, 72, 40
+    t = make(rows, 1, F, H, F, dtype)
+    d = single.gated_ff_backward(*t, dw_dtype=torch.float32)
+    x, dy, wg, wu, wd = (v.double() for v in t)
+    wg, wu, wd = wg[0], wu[0], wd[0]
+    g, u, dh = x @ wg, x @ wu, dy @ wd.T
+    s = torch.sigmoid(g)
+    dg, du = dh * u * s * (1 + g * (1 - s)), dh * g * s
+    want = dict(dx=dg @ wg.T + du @ wu.T, dw_gate=x.T @ dg, dw_up=x.T @ du, dw_down=(g * s * u).T @ dy)
+    for n, v in want.items():
+        err = float((d[n].double().view_as(v) - v).norm() / v.norm())
+        # bfloat16: the stored operand is off by 2^-8 at most, 1.7e-3 in the mean square, and dx once more
+        assert err < (2e-6 if dtype == "f32" else 2.6e-3 if n == "dx" else 2e-3), (n, err)

@@ -233,11 +233,13 @@ Chunks chunks_of(const gnnco_handle* h, const gnnco_gated_ff_desc* d) {
   return c;
 }
 
-// Both products in one kernel (gated_ff_fused.cu), where its tiles of 256 rows keep all pairs of CTAs busy.
+// Both products in one kernel (gated_ff_fused.cu) or in two?  One pair of CTAs walks all of H there, so it takes tiles of 256 rows for half of
+// the pairs, or a short H.  (Device time with cold caches, one kernel and two: 12,000 x 256 x 512 18.0 and 21.1 us, x 4,096 76 and
+// 86; 1,000 x 64 x 128 in 8 sets 9.0 and 13.1; but 4,000 x 256 x 512 16.3 and 14.3, 4,000 x 256 x 4,096 71 and 38.)
 bool fuses(const gnnco_handle* h, const gnnco_gated_ff_desc* d) {
   if (d->feat_dtype != GNNCO_BF16 || d->F > 256 || d->F_out > 256) return false;
   const int64_t pairs = ff::resident_pairs(h->device, h->sm_count), tiles = d->sets > 1 ? h->n_pairs : blocks_of(d->rows, 256);
-  return pairs > 0 && tiles >= pairs;
+  return pairs > 0 && (2 * tiles >= pairs || d->H <= 256);
 }
 
 Work lay_out(const gnnco_handle* h, const gnnco_gated_ff_desc* d, bool backward) {
@@ -351,7 +353,7 @@ struct Call {
   // Pairs of CTAs halve what is read per product; single CTAs with tiles of a quarter of the size spread small calls over more SMs and
   // leave less of the last round idle.  Rounds of tiles times their length, in cycles: the products of a stage (64 of the contraction)
   // or its copies at the 45 bytes a cycle that an SM got from L2, and some 2,500 at the ends that nothing covers.
-  // (4,039 x 128 x 343 float32, 16 sets, backward: PAIRS_FIGURES.)
+  // (Backward by pairs and by singles: 1.13 M x 128 x 256 bfloat16 1,330 and 1,419 us, 4,039 x 128 x 343 float32 in 16 sets 82 and 68.)
   bool use_pairs(int64_t pair_tiles, int64_t single_tiles, int64_t stages, int pair_cols, int single_cols) const {
     const int64_t pairs = ff::resident_pairs(h->device, h->sm_count), sms = h->sm_count;
     if (pairs <= 0 || pair_tiles < pairs) return false;
@@ -399,10 +401,11 @@ struct Call {
     const int p = wide_tile(true, cols), q = wide_tile(false, cols);
     return use_pairs(row_tiles(true) * blocks_of(cols, p), row_tiles(false) * blocks_of(cols, q), stages, p, q);
   }
-  // columns of a tile of y or dx: wide, but for single CTAs that would not fill the GPU
+  // columns of a tile of y or dx: wide, but for single CTAs that would leave half of the GPU idle (dx of 4,039 x 128 in 16 subgraphs: 32
+  // tiles of 128 columns or 64 of 64, the whole backward pass 71.5 or 68.2 us; 3,000 x 512: 96 or 192 tiles, 77.2 or 83.5 us)
   int wide_tile(bool pair, int cols) const {
     if (pair) return cols > 128 ? 256 : 128;
-    return cols > 64 && row_tiles(false) * blocks_of(cols, 128) >= h->sm_count ? 128 : 64;
+    return cols > 64 && 2 * row_tiles(false) * blocks_of(cols, 128) > h->sm_count ? 128 : 64;
   }
 
   // y = drop(h Wd)

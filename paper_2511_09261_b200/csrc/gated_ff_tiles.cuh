@@ -159,7 +159,8 @@ __device__ __forceinline__ Two fma(Two a, Two b, Two c) {
 }
 // the hardware's 2^x (2 units of 2^-23) and 1 / x (1 unit), results and arguments below 2^-126 as zeros: no range handling around
 // them.  (1 / x by a Newton and a third-order step on the arithmetic pipes halves the transcendental instructions, but its nine
-// instructions more per pair took the same time alone and more beside the drawing of masks: NEWTON_FIGURES.)
+// instructions more per pair took the same time alone and more beside the drawing of masks: 2.5 M x 256 x 512 bfloat16 1,588 and,
+// with dropout, 2,164 us; this way 1,576 and 1,956.)
 __device__ __forceinline__ Two exp2(Two x) {
   float a, b;
   x.get(a, b);

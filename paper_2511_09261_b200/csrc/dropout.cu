@@ -56,14 +56,14 @@ __global__ void __launch_bounds__(256) drop_vectors(const __grid_constant__ Drop
       const int64_t i = base + u * 256 + threadIdx.x;
       if (i >= items) break;
       float f[VEC];
+      uint4 w[VEC / 4];                                    // F is a multiple of 4: quads are numbered along the run of groups
+      words.quads(A.m, (uint64_t)i * (VEC / 4), w);
 #pragma unroll
       for (int k = 0; k < VEC; k += 4) {
-        // F is a multiple of 4: quads are numbered along the run of groups
-        const uint4 w = words.quad(A.m, (uint64_t)i * (VEC / 4) + k / 4);
-        f[k] = pick(w.x, A.m, v[u].get(k));
-        f[k + 1] = pick(w.y, A.m, v[u].get(k + 1));
-        f[k + 2] = pick(w.z, A.m, v[u].get(k + 2));
-        f[k + 3] = pick(w.w, A.m, v[u].get(k + 3));
+        f[k] = pick(w[k / 4].x, A.m, v[u].get(k));
+        f[k + 1] = pick(w[k / 4].y, A.m, v[u].get(k + 1));
+        f[k + 2] = pick(w[k / 4].z, A.m, v[u].get(k + 2));
+        f[k + 3] = pick(w[k / 4].w, A.m, v[u].get(k + 3));
       }
       vio::store_stream<T, VEC>(static_cast<T*>(A.out) + to[u], f);
     }
@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(256) drop_quads(const __grid_constant__ DropAr
 
 template <typename T>
 void launch_drop(gnnco_handle* h, DropArgs A, cudaStream_t st) {
-  constexpr int kVec = 16 / (int)sizeof(T), kUnroll = 2;
+  constexpr int kVec = 16 / (int)sizeof(T), kUnroll = 1, kQuads = 2;
   auto fits = [&](int vec) {
     const uintptr_t bytes = (uintptr_t)vec * sizeof(T);
     return A.F % vec == 0 && (((uintptr_t)A.x | (uintptr_t)A.out | (uintptr_t)(A.x_ld * (int64_t)sizeof(T)) |
@@ -135,7 +135,7 @@ void launch_drop(gnnco_handle* h, DropArgs A, cudaStream_t st) {
     }
   }
   A.groups = (A.F + 3) / 4;
-  drop_quads<T, kUnroll><<<blocks(256 * kUnroll), 256, 0, st>>>(A);
+  drop_quads<T, kQuads><<<blocks(256 * kQuads), 256, 0, st>>>(A);
 }
 
 }  // namespace

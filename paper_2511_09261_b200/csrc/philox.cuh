@@ -44,7 +44,19 @@ struct Stream {
   }
   __device__ __forceinline__ uint4 quad(const Mask& m, uint64_t q) {
     if ((uint32_t)(q >> 32) != last_hi) upper(m, (uint32_t)(q >> 32));
-    const uint64_t a = (uint64_t)kMul0 * (uint32_t)q;
+    return rounds(m, (uint32_t)q);
+  }
+  // quads q .. q + N - 1, N a power of two that divides q
+  template <int N>
+  __device__ __forceinline__ void quads(const Mask& m, uint64_t q, uint4 (&w)[N]) {
+    if ((uint32_t)(q >> 32) != last_hi) upper(m, (uint32_t)(q >> 32));
+#pragma unroll
+    for (int k = 0; k < N; ++k) w[k] = rounds(m, (uint32_t)q + k);
+  }
+
+ private:
+  __device__ __forceinline__ uint4 rounds(const Mask& m, uint32_t q_lo) const {
+    const uint64_t a = (uint64_t)kMul0 * q_lo;
     uint32_t x2 = (uint32_t)(a >> 32) ^ m.layer ^ m.key[1], x3 = (uint32_t)a;
     const uint64_t b = (uint64_t)kMul1 * x2;
     uint32_t x0 = (uint32_t)(b >> 32) ^ lo1 ^ m.key[2], x1 = (uint32_t)b;

@@ -18,7 +18,7 @@ namespace ff {
 namespace {
 
 constexpr int kThreads = 256, kCols = 32;
-constexpr int kMostShared = 8192;                          // floats of x or h that a block holds
+constexpr int kMostShared = 5120;                          // floats of x or h that a block holds (five blocks fit an SM)
 
 struct RowsArgs {
   const void* x;                                           // GATE: x, else h (float32)

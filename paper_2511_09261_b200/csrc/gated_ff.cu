@@ -1,15 +1,15 @@
 // The gated feed-forward block, forward and backward: entry points, work areas, copies of operands and the choice of kernels
 // (formulas and kinds of products: gated_ff.cuh; the products: gated_ff_tiles.cuh).
 //
-// Up to four rows with one set of weights: gated_ff_rows.cu.  Else
+// Up to four rows with one set of weights: gated_ff_rows.cu.  Forward in bfloat16 with widths up to 256: gated_ff_fused.cu.  Else
 // Forward:   [operands as limbs]   h = act(x Wg) .* (x Wu)   y = drop(h Wd)
 // Backward:  [operands as limbs]   h, dg, du (g and u are computed again: nothing but x is kept from the forward pass, which at
 //            widths up to some 400 is also faster than writing and reading them)   dx   the weight gradients   [their partial sums]
 //
 // Operands of the products are bfloat16 with rows that start on 16 bytes.  A tensor that is not (float32 features or weights, odd
 // widths, unaligned views, a gradient that passes a mask first) is copied into the work area once, as one or three limbs.
-// Each rounding: h, dg and du are stored as the operands of the next product, in bfloat16 features one bfloat16 (2^-9 of the value,
-// as much as the results are rounded by), in float32 features three limbs (24 bits); float32 weights of bfloat16
+// Each rounding: h, dg and du are stored as the operands of the next product, in bfloat16 features one bfloat16 (2^-8 of the value at
+// most, as much as the results are rounded by), in float32 features three limbs (24 bits); float32 weights of bfloat16
 // features are rounded to bfloat16.  All sums are float32, and none depends on timing.
 #include "gated_ff.cuh"
 #include "vec_io.cuh"
@@ -341,7 +341,7 @@ struct Call {
     a->status = h->status;
   }
   int32_t launch(Kind kind, bool pair, const Maps& maps, Args* a, int64_t tiles) {
-    if (tiles > 0x7fffffff) return GNNCO_UNSUPPORTED;
+    if (tiles > 0x7ff00000) return GNNCO_UNSUPPORTED;      // (a tile's number plus two rounds of the grid stays in 32 bits)
     a->tiles = (int32_t)tiles;
     a->chained = launched;
     launched = true;

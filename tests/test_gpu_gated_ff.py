@@ -413,3 +413,28 @@ def test_weight_gradients_of_more_rows_than_one_run_takes(single, dtype):
         err = float((d[n].double().view_as(v) - v).norm() / v.norm())
         # bfloat16: the stored operand is off by 2^-8 at most, 1.7e-3 in the mean square, and dx once more
         assert err < (2e-6 if dtype == "f32" else 2.6e-3 if n == "dx" else 2e-3), (n, err)
+
+
+def test_elements_past_32_bits():
+    """x, y and the stored h, dg, du have more than 2^31 elements: the last rows against a call on them alone."""
+    import torch
+    free = torch.cuda.mem_get_info()[0]
+    if free < 60 << 30:
+        pytest.skip("needs 60 GB")
+    rows, F, H = (1 << 23) + 4097, 256, 272
+    g = load([rows])
+    r = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.empty(rows, F, dtype=torch.bfloat16, device="cuda").normal_(generator=r)
+    w = [torch.empty(s, dtype=torch.bfloat16, device="cuda").normal_(generator=r).mul_(1 / 16) for s in ((1, F, H), (1, F, H), (1, H, F))]
+    last = x[-300:].clone()
+    drop = gnnco.Dropout(0.5, 11)
+    keep = torch.from_numpy(ref.keep(300, F, 0.5, 11, row0=rows - 300)).cuda()
+    y = g.gated_ff(x, *w, drop=drop)
+    want = torch.where(keep, g.gated_ff(last, *w).float() * 2.0, 0.0)
+    assert float((y[-300:].float() - want).norm() / want.norm()) < 2 * BF
+    assert torch.equal(y[-300:] != 0, (want != 0) & keep)
+    del y
+    dx = g.gated_ff_backward(x, x, *w, want_dw=False)["dx"]
+    want = g.gated_ff_backward(last, last, *w, want_dw=False)["dx"]
+    assert float((dx[-300:].float() - want.float()).norm() / want.float().norm()) < 2 * BF
+    assert g.async_status() == gnnco.OK

@@ -172,8 +172,15 @@ extern "C" int32_t gnnco_dropout(gnnco_handle* h, int32_t feat_dtype, int64_t ro
   ProfScope prof_(h, K_DROPOUT, st);
   const size_t es = feat_dtype == GNNCO_F32 ? 4 : 2;
   if (!drops) {                                            // p below 2^-33: 1 / (1 - p) is 1 in float32
-    if (x != out)
+    if (x == out) return GNNCO_OK;
+    // (rows further apart than a copy in two dimensions takes are few)
+    const int64_t most = 0x7fffffff / (int64_t)es;
+    if (x_ld <= most && out_ld <= most) {
       GNNCO_CUDA_TRY(cudaMemcpy2DAsync(out, out_ld * es, x, x_ld * es, F * es, rows, cudaMemcpyDeviceToDevice, st));
+    } else {
+      for (int64_t r = 0; r < rows; ++r)
+        GNNCO_CUDA_TRY(cudaMemcpyAsync(static_cast<char*>(out) + r * out_ld * es, static_cast<const char*>(x) + r * x_ld * es, F * es, cudaMemcpyDeviceToDevice, st));
+    }
     return GNNCO_OK;
   }
   const DropArgs A = {x, out, x_ld, out_ld, rows, F, 0, m};

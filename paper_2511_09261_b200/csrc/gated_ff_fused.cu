@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(fused_threads(MASKED), 1) fused_forward(const 
     }
     tc::mbar_init(&B.gu_full, 1);
     tc::mbar_init(&B.gu_empty, 2 * kResults);
-    tc::mbar_init(&B.h_full, 2 * kResults);
+    tc::mbar_init(&B.h_full, kResults + (rank == 0 ? 1 : 0));        // the odd CTA's is passed on as one arrival
     tc::mbar_init(&B.h_empty, 1);
     tc::mbar_init(&B.y_full, 1);
     tc::mbar_init(&B.y_empty, 2 * kResults);
@@ -152,10 +152,18 @@ __global__ void __launch_bounds__(fused_threads(MASKED), 1) fused_forward(const 
     __syncwarp();
   } else if (warp == kMmaWarp) {
     // -------------------------------------------------------------------------------- products
+    const int tiles_here = first < A.tiles ? (A.tiles - first + step - 1) / step : 0;
+    const int32_t total = tiles_here * chunks;
+    if (rank == 1 && tc::elect_one()) {
+      // This CTA's h is ready: passed on to the CTA that multiplies, with a release at the scope of the cluster.  (That waits for
+      // everything its thread has in flight: nothing here, but 1,650 cycles a chunk in the result warps.)
+      for (int32_t i = 0; i < total; ++i) {
+        if (!wait_bar(&B.h_full, (uint32_t)i & 1, abort_flag)) break;
+        tc::mbar_arrive_release_cluster(tc::map_to_cta(tc::smem_u32(&B.h_full), 0));
+      }
+    }
     if (rank == 0 && tc::elect_one()) {
       const uint32_t g_idesc = tc::idesc_bf16_f32(256, 256, false, true), d_idesc = tc::idesc_bf16_f32(256, y_cols, false, true);
-      const int tiles_here = first < A.tiles ? (A.tiles - first + step - 1) / step : 0;
-      const int32_t total = tiles_here * chunks;
       int slot = 0, d = 0, gc = 0, dc = 0;                 // gc, dc: chunk of the tile that G and D are at
       uint32_t g_phase = 0, d_phase = 0, x_phase = 0, y_phase = 1;
       bool ok = true;
@@ -188,7 +196,7 @@ __global__ void __launch_bounds__(fused_threads(MASKED), 1) fused_forward(const 
           }
         }
         if (i > 0) {
-          if (!(ok = wait_bar(&B.h_full, (uint32_t)(i - 1) & 1, abort_flag))) break;
+          if (!(ok = wait_bar<true>(&B.h_full, (uint32_t)(i - 1) & 1, abort_flag))) break;
           if (dc == 0) {
             if (!(ok = wait_bar(&B.y_empty, y_phase, abort_flag))) break;
             y_phase ^= 1;
@@ -220,8 +228,7 @@ __global__ void __launch_bounds__(fused_threads(MASKED), 1) fused_forward(const 
     const int e = warp - kFirstEpi, quarter = warp & 3, half = e >> 2;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const int row_in_cta = quarter * 32 + lane, warp_row = (int)rank * 128 + quarter * 32;
-    const uint32_t gu_free = tc::map_to_cta(tc::smem_u32(&B.gu_empty), 0), h_ready = tc::map_to_cta(tc::smem_u32(&B.h_full), 0);
-    const uint32_t y_free = tc::map_to_cta(tc::smem_u32(&B.y_empty), 0);
+    const uint32_t gu_free = tc::map_to_cta(tc::smem_u32(&B.gu_empty), 0), y_free = tc::map_to_cta(tc::smem_u32(&B.y_empty), 0);
     float* const stage = reinterpret_cast<float*>(gen + kStaging + e * kStageBytes);
     const uint32_t stage_at = sbase + kStaging + e * kStageBytes;
     const uint32_t h_at = sbase + kH + half * kBlockBytes + row_in_cta * 128;
@@ -322,9 +329,7 @@ __global__ void __launch_bounds__(fused_threads(MASKED), 1) fused_forward(const 
           tc::st_shared16(h_at + ((k ^ (row_in_cta & 7)) << 4), w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
         tc::fence_proxy_async_smem();
         __syncwarp();
-        // (release at the scope of the CTA, and the proxy fence before it, put the writes ahead of the arrival: only this SM's tensor core
-        // reads them.  An explicit release at cluster scope waits for everything this thread has in flight: 1,650 cycles a chunk.)
-        if (lane == 0) tc::mbar_arrive_cluster(h_ready);
+        if (lane == 0) tc::mbar_arrive(&B.h_full);
         if (c == 0) {
           if (t != first && !(ok = take_y())) break;
           y_row0 = next_row0 + warp_row;

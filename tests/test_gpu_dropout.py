@@ -134,3 +134,21 @@ def test_another_stream(graph):
     got = graph.dropout(x, gnnco_drop(0.2), stream=side)
     side.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("p", [0.0, 0.5])
+def test_rows_far_apart(graph, p):
+    """Two rows 2^30 elements (4 GB) apart, more than a strided copy takes as its pitch."""
+    import torch
+    import paper_2511_09261_b200 as gnnco
+    base = torch.empty((1 << 30) + 5, dtype=torch.float32, device="cuda")
+    x = base.as_strided((2, 5), (1 << 30, 1))
+    x.copy_(torch.arange(1.0, 11.0).view(2, 5))
+    drop = gnnco.Dropout(p, 7)
+    want = graph.dropout(x.clone(memory_format=torch.contiguous_format), drop)
+    assert torch.equal(graph.dropout(x, drop), want)
+    assert torch.equal(graph.dropout(x, drop, out=x), want)
+    if p == 0.0:
+        out = torch.zeros(2, 7, device="cuda")
+        graph.dropout(x, drop, out=out[:, :5])
+        assert torch.equal(out[:, :5], want) and not out[:, 5:].any()

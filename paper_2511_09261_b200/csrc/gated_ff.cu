@@ -18,6 +18,7 @@ namespace ff {
 int32_t launch_tiles_bf16(Kind kind, bool pair, const Maps& maps, const Args& args, int device, int sms, cudaStream_t st);
 int32_t launch_tiles_f32(Kind kind, bool pair, const Maps& maps, const Args& args, int device, int sms, cudaStream_t st);
 int32_t launch_fused(const Maps& maps, const Args& args, int device, int sms, cudaStream_t st);
+int32_t launch_fused_back(const Maps& maps, const CUtensorMap& dx_map, const Args& args, int device, int sms, cudaStream_t st);
 bool few_rows(const gnnco_gated_ff_desc* d, int sms);
 int32_t launch_few_rows(gnnco_handle* h, const gnnco_gated_ff_desc* d, const philox::Mask* mask, float* hidden, void* y, int64_t y_ld,
                         cudaStream_t st);
@@ -242,6 +243,19 @@ bool fuses(const gnnco_handle* h, const gnnco_gated_ff_desc* d) {
   return pairs > 0 && (2 * tiles >= pairs || d->H <= 256);
 }
 
+// The same for h, dg, du and dx (gated_ff_fused_back.cu).  dx is written before the weight gradients read x and dy there, so it must be
+// neither of them.
+bool fuses_back(const gnnco_handle* h, const gnnco_gated_ff_desc* d, const gnnco_gated_ff_grads* g, const Operand& x, const Operand& dy) {
+  if (d->feat_dtype != GNNCO_BF16 || d->F > 128 || d->F_out > 128 || !g->dx || ((uintptr_t)g->dx & 15) || g->dx_ld % 8) return false;
+  auto apart = [&](const Operand& o, int cols) {
+    const uintptr_t a = (uintptr_t)g->dx, b = (uintptr_t)o.p;
+    return a + ((d->rows - 1) * g->dx_ld + d->F) * 2 <= b || b + ((d->rows - 1) * o.ld + cols) * 2 <= a;
+  };
+  if (g->dw_gate && !(apart(x, d->F) && apart(dy, d->F_out))) return false;
+  const int64_t tiles = d->sets > 1 ? h->n_tiles : blocks_of(d->rows, 128);
+  return tiles >= 1;
+}
+
 Work lay_out(const gnnco_handle* h, const gnnco_gated_ff_desc* d, bool backward) {
   Work w;
   const int64_t limbs = limbs_of(d), sets = d->sets;
@@ -445,6 +459,38 @@ struct Call {
     if (rc == GNNCO_OK) h->launches += 1;
     return rc;
   }
+  // h, dg, du (where they are wanted) and dx
+  int32_t gates_and_dx(const Operand& x, const Operand& dy, const Operand& wg, const Operand& wu, const Operand& wd, const Operand* out,
+                       bool keep, void* dx, int64_t dx_ld) {
+    Args a = {};
+    Maps m = {};
+    CUtensorMap dx_map;
+    rows_of(&a, false);
+    a.n_tiles = 1;
+    a.K[0] = d->F_out;
+    a.K[1] = d->H;
+    a.cols = d->F;
+    a.act = d->act;
+    a.scale = drops ? jobs.mask.scale : 1.0f;
+    a.y = dx;
+    a.y_ld = dx_ld;
+    a.out_ld = out[0].ld;
+    a.tiles = a.m_tiles;
+    a.chained = launched;
+    launched = true;
+    bool ok = map_rows(&m.a[0], x.p, d->rows, d->F, x.ld, 0, 1, 128) && map_rows(&m.a[1], dy.p, d->rows, d->F_out, dy.ld, 0, 1, 128) &&
+              map_sets(&m.b[0], wg.p, d->sets, d->F, d->H, wg.ld, 1, d->F > 64 ? 128 : 64) &&
+              map_sets(&m.b[1], wu.p, d->sets, d->F, d->H, wu.ld, 1, d->F > 64 ? 128 : 64) &&
+              map_sets(&m.b[2], wd.p, d->sets, d->H, d->F_out, wd.ld, 1, 64) && map_out(&dx_map, false, dx, d->rows, d->F, dx_ld, 0, 1, 16);
+    for (int k = 0; keep && k < 3; ++k) {
+      a.out[k] = const_cast<__nv_bfloat16*>(out[k].p);
+      ok = ok && map_out(&m.out[k], false, out[k].p, d->rows, d->H, out[k].ld, 0, 1, 64);
+    }
+    if (!ok) return GNNCO_CUDA_ERROR;
+    const int32_t rc = ff::launch_fused_back(m, dx_map, a, h->device, h->sm_count, st);
+    if (rc == GNNCO_OK) h->launches += 1;
+    return rc;
+  }
   // dx = dg Wg^T + du Wu^T
   int32_t input_grad(const Operand& dg, const Operand& du, const Operand& wg, const Operand& wu, void* dx, int64_t dx_ld) {
     const bool pair = wide_pairs(d->F, 2 * blocks_of(d->H, 64));
@@ -641,10 +687,11 @@ extern "C" int32_t gnnco_gated_ff_backward(gnnco_handle* h, const gnnco_gated_ff
     hdd[k].limb = d->rows * hdd[k].ld;
   }
   c.pack();
-  int32_t r = c.gates(x, &dyo, wg, wu, wd, hdd);
+  const bool fused = fuses_back(h, d, g, x, dyo);
+  int32_t r = fused ? c.gates_and_dx(x, dyo, wg, wu, wd, hdd, weights, g->dx, g->dx_ld) : c.gates(x, &dyo, wg, wu, wd, hdd);
   if (r == GNNCO_OK && weights) r = c.weight_grads(x, dyo, hdd, g, reinterpret_cast<float*>(base + w.scratch));
   // (last: dx may be x or dy)
-  if (r == GNNCO_OK && g->dx) r = c.input_grad(hdd[1], hdd[2], wg, wu, g->dx, g->dx_ld);
+  if (r == GNNCO_OK && g->dx && !fused) r = c.input_grad(hdd[1], hdd[2], wg, wu, g->dx, g->dx_ld);
   if (r != GNNCO_OK) return r;
   GNNCO_LAUNCH_CHECK();
   return GNNCO_OK;

@@ -458,6 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
   constexpr uint32_t kBlock = 8192 * LIMBS;                // 64 x 64 of an n-major operand, all limbs
   constexpr int kCtas = PAIR ? 2 : 1;
   constexpr bool kAlongRows = KIND == kWeights;
+  constexpr int kSegments = KIND == kGluBack ? 2 : 1;      // contractions one after the other (kDx takes a stage of each in turn)
   constexpr bool kSums = LIMBS > 1;                        // stages are added up in registers
   constexpr bool kQuarters = KIND == kGluBack && !kSums;   // accumulators take quarters of TMEM in turn
   constexpr int kTeams = LIMBS == 1 && !kAlongRows && !kQuarters ? 2 : 1;    // of result warps, tiles in turn
@@ -520,11 +521,12 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
       const Tile T = walk.take();
       const int set = T.set;
       const int nt = kAlongRows ? A.p[T.problem].nt : A.nt;
-      for (int seg = 0; seg < 2 && ok; ++seg) {
+      for (int seg = 0; seg < kSegments && ok; ++seg) {
         const bool twin = KIND == kGlu || (KIND == kGluBack && seg == 1);
         const uint32_t bytes = kA + (twin ? 2 : 1) * (nt / kCtas) * 128 * LIMBS;
-        const int stages = seg == 0 ? T.stages : more;
-        for (int kb = 0; kb < stages; ++kb) {
+        const int stages = KIND == kDx ? 2 * T.stages : seg == 0 ? T.stages : more;
+        for (int s = 0; s < stages; ++s) {
+          const int kb = KIND == kDx ? s >> 1 : s;
           if (!(ok = __all_sync(0xffffffffu, wait_bar(empty + slot, phase, abort_flag)) != 0)) break;
           const uint32_t at = sbase + slot * kSlot, bt = at + kA;
           const uint32_t announce = PAIR ? tc::map_to_cta(tc::smem_u32(full + slot), 0) : tc::smem_u32(full + slot);
@@ -537,7 +539,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
             load_box<PAIR>(leader, at + kBlock, &maps.a[T.problem], m + 64, r, 0, bar);
             for (int i = 0; i < nt / kCtas / 64; ++i) load_box<PAIR>(leader, bt + i * kBlock, &maps.b[T.problem], n + 64 * i, r, 0, bar);
           } else {
-            load_box<PAIR>(leader, at, &maps.a[seg], kb * 64, (int32_t)T.row0 + rank_u * 128, 0, bar);
+            load_box<PAIR>(leader, at, &maps.a[KIND == kDx ? s & 1 : seg], kb * 64, (int32_t)T.row0 + rank_u * 128, 0, bar);
             if (twin && kQuarters) {
               // 64 gate columns, then the same up columns; in a pair each CTA holds half of both
               load_box_of_set<PAIR>(leader, bt, &maps.b[0], T.n0 + rank_u * 64, kb * 64, set, bar);
@@ -553,7 +555,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
               const int n = T.n0 + rank_u * (nt / kCtas);
               for (int i = 0; i < nt / kCtas / 64; ++i) load_box_of_set<PAIR>(leader, bt + i * kBlock, &maps.b[0], n + 64 * i, kb * 64, set, bar);
             } else {
-              load_box_of_set<PAIR>(leader, bt, &maps.b[KIND == kGluBack ? 2 : seg], kb * 64, T.n0 + rank_u * (nt / kCtas), set, bar);
+              load_box_of_set<PAIR>(leader, bt, &maps.b[KIND == kGluBack ? 2 : s & 1], kb * 64, T.n0 + rank_u * (nt / kCtas), set, bar);
             }
           }
           if constexpr (kAlongRows) if (valid < 64) {
@@ -598,7 +600,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
         }
         const int nt = kAlongRows ? A.p[T.problem].nt : A.nt;
         bool open = false;                                 // the current part has its buffer
-        for (int seg = 0; seg < 2 && ok; ++seg) {
+        for (int seg = 0; seg < kSegments && ok; ++seg) {
           const bool twin = KIND == kGlu || (KIND == kGluBack && seg == 1);
           const bool b_n_major = twin || KIND == kDown || KIND == kWeights;
           const int N = twin && !kQuarters ? 2 * nt : nt;
@@ -611,8 +613,9 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
           }
           const uint32_t b_limb = b_n_major ? 8192 : (uint32_t)(nt / kCtas) * 128;
           const int K = kAlongRows ? T.rows : A.K[seg];
-          const int stages = seg == 0 ? T.stages : more;
-          for (int kb = 0; kb < stages; ++kb) {
+          const int stages = KIND == kDx ? 2 * T.stages : seg == 0 ? T.stages : more;
+          for (int s = 0; s < stages; ++s) {
+            const int kb = KIND == kDx ? s >> 1 : s;
             if (!open) {
               if (part >= 2 && !kQuarters) ok = wait_bar(acc_empty + (part & 1), ((part >> 1) - 1) & 1, abort_flag);
               tc::tc_fence_after_sync();
@@ -632,7 +635,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
             if constexpr (LIMBS == 1) {
 #pragma unroll
               for (int k = 0; k < 4; ++k)
-                if (k < steps) multiply<PAIR>(acc, a0 + a_step * k, b0 + b_step * k, idesc, kb + k != 0 || (KIND == kDx && seg == 1));
+                if (k < steps) multiply<PAIR>(acc, a0 + a_step * k, b0 + b_step * k, idesc, s + k != 0);
               if (kQuarters && seg == 1) {
                 const uint32_t acc2 = tmem + ((3 * part + 2) & 3) * 128;
 #pragma unroll

@@ -38,6 +38,7 @@ struct PackJob {
   __nv_bfloat16* to;
   int64_t rows, from_ld, to_ld, to_limb;
   int32_t cols, from_f32, vectors, masked;
+  int32_t flat;                                            // vectors, and both sides are one run of elements
 };
 struct PackJobs {
   PackJob j[5];
@@ -54,21 +55,30 @@ __global__ void __launch_bounds__(256) pack_operands(const __grid_constant__ Pac
   const int64_t chunks = J.to_ld / 8, items = J.rows * chunks;
   philox::Stream words(P.mask);
   for (int64_t base = (int64_t)blockIdx.x * 256; base < items; base += (int64_t)gridDim.x * 256) {
-    const int64_t row0 = base / chunks;
-    const uint32_t off = (uint32_t)(base - row0 * chunks) + threadIdx.x, r = off / (uint32_t)chunks;
-    const int64_t row = row0 + r;
-    const int c = (int)(off - r * (uint32_t)chunks) * 8;
-    if (row >= J.rows) break;
+    int64_t row = 0, from, to_at;
+    int c = 0;
+    if (J.flat) {
+      from = to_at = (base + threadIdx.x) * 8;
+      if (base + threadIdx.x >= items) break;
+    } else {
+      const int64_t row0 = base / chunks;
+      const uint32_t off = (uint32_t)(base - row0 * chunks) + threadIdx.x, r = off / (uint32_t)chunks;
+      row = row0 + r;
+      c = (int)(off - r * (uint32_t)chunks) * 8;
+      if (row >= J.rows) break;
+      from = row * J.from_ld + c;
+      to_at = row * J.to_ld + c;
+    }
     float f[8];
-    if (J.vectors && c + 8 <= J.cols) {
+    if (J.flat || (J.vectors && c + 8 <= J.cols)) {
       if (J.from_f32) {
         vio::Raw<float, 8> v;
-        v.template load<true>(static_cast<const float*>(J.from) + row * J.from_ld + c);
+        v.template load<true>(static_cast<const float*>(J.from) + from);
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = v.get(e);
       } else {
         vio::Raw<__nv_bfloat16, 8> v;
-        v.template load<true>(static_cast<const __nv_bfloat16*>(J.from) + row * J.from_ld + c);
+        v.template load<true>(static_cast<const __nv_bfloat16*>(J.from) + from);
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = v.get(e);
       }
@@ -77,23 +87,30 @@ __global__ void __launch_bounds__(256) pack_operands(const __grid_constant__ Pac
       for (int e = 0; e < 8; ++e) {
         f[e] = 0.0f;
         if (c + e < J.cols) {
-          if (J.from_f32) f[e] = static_cast<const float*>(J.from)[row * J.from_ld + c + e];
-          else f[e] = __bfloat162float(static_cast<const __nv_bfloat16*>(J.from)[row * J.from_ld + c + e]);
+          if (J.from_f32) f[e] = static_cast<const float*>(J.from)[from + e];
+          else f[e] = __bfloat162float(static_cast<const __nv_bfloat16*>(J.from)[from + e]);
         }
       }
     }
     if (J.masked) {
-      const uint64_t q = (uint64_t)row * ((J.cols + 3) / 4) + c / 4;
+      uint4 two[2];
+      if (J.flat) {                                        // (cols is a multiple of 8)
+        words.quads(P.mask, (uint64_t)(base + threadIdx.x) * 2, two);
+      } else {
+        const uint64_t q = (uint64_t)row * ((J.cols + 3) / 4) + c / 4;
+        two[0] = words.quad(P.mask, q);
+        two[1] = words.quad(P.mask, q + 1);
+      }
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const uint4 w = words.quad(P.mask, q + k);
+        const uint4 w = two[k];
         f[4 * k] = w.x > P.mask.lim ? f[4 * k] : 0.0f;
         f[4 * k + 1] = w.y > P.mask.lim ? f[4 * k + 1] : 0.0f;
         f[4 * k + 2] = w.z > P.mask.lim ? f[4 * k + 2] : 0.0f;
         f[4 * k + 3] = w.w > P.mask.lim ? f[4 * k + 3] : 0.0f;
       }
     }
-    __nv_bfloat16* const to = J.to + row * J.to_ld + c;
+    __nv_bfloat16* const to = J.to + to_at;
 #pragma unroll
     for (int l = 0; l < LIMBS; ++l) {
       uint32_t w[4];
@@ -323,6 +340,7 @@ struct Call {
     j.rows = rows; j.from_ld = ld; j.to_ld = o.ld; j.to_limb = o.limb;
     j.cols = cols; j.from_f32 = dtype == GNNCO_F32; j.masked = masked;
     j.vectors = ((uintptr_t)p & 15) == 0 && ld % (dtype == GNNCO_F32 ? 4 : 8) == 0;
+    j.flat = j.vectors && ld == cols && cols % 8 == 0;
     return o;
   }
   void pack() {

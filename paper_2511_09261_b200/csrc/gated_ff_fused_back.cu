@@ -7,7 +7,8 @@
 //                    copied to memory: the weight gradients read them
 //     D(c)   dx += dg Wg^T + du Wu^T                    128 x F, in tensor memory until the last chunk
 //
-// The products are issued G(0) G(1) D(0) G(2) D(1) .., across tiles too, so that G(c + 1) runs while chunk c is converted.  One copy of a
+// G(c + 1) runs while chunk c is converted, across tiles too.  Whichever of the next G and the next D has its operands is issued: D in turn
+// with G would wait for weights that take the place of its own (667 us for 1.13 M x 128 x 256 against XXX).  One copy of a
 // chunk's weights serves both: G reads Wg and Wu along their rows, D across them.  (A pair of CTAs would have to hold different
 // halves for the two.)  A tile's dx is taken out after the first chunk of the next tile.
 //
@@ -82,18 +83,22 @@ __global__ void __launch_bounds__(kThreads, 1) fused_backward(const __grid_const
     while (walk.any() && ok) {
       const Tile T = walk.take();
       for (int c = 0; c < chunks; ++c, ++i) {
-        if (c == 0) {
-          if (!(ok = wait(&B.x_empty, x_phase))) break;
-          expect_bytes<false>(leader, x_bar, (x_blocks + dy_blocks) * kXBlock);
-          for (int kb = 0; kb < x_blocks; ++kb) load_box<false>(leader, sbase + kX + kb * kXBlock, &maps.a[0], kb * 64, T.row0, 0, x_bar);
-          for (int kb = 0; kb < dy_blocks; ++kb) load_box<false>(leader, sbase + kDy + kb * kXBlock, &maps.a[1], kb * 64, T.row0, 0, x_bar);
-        }
         const uint32_t slot = i & 1, bar = tc::smem_u32(B.w_full + slot), at = sbase + kW + slot * kWSlot;
         if (!(ok = wait(B.w_empty + slot, ((uint32_t)i >> 1 & 1) ^ 1))) break;
         expect_bytes<false>(leader, bar, (2 * x_blocks + dy_blocks) * kWBlock);
         for (int k = 0; k < 2; ++k) load_box_of_set<false>(leader, at + k * 2 * kWBlock, &maps.b[k], c * kChunk, 0, T.set, bar);   // all F rows
         for (int kb = 0; kb < dy_blocks; ++kb)
           load_box_of_set<false>(leader, at + (4 + kb) * kWBlock, &maps.b[2], kb * 64, c * kChunk, T.set, bar);
+        if (c == 0) {
+          if (!(ok = wait(&B.x_empty, x_phase))) break;
+          expect_bytes<false>(leader, x_bar, (x_blocks + dy_blocks) * kXBlock);
+          for (int kb = 0; kb < x_blocks; ++kb) load_box<false>(leader, sbase + kX + kb * kXBlock, &maps.a[0], kb * 64, T.row0, 0, x_bar);
+          for (int kb = 0; kb < dy_blocks; ++kb) load_box<false>(leader, sbase + kDy + kb * kXBlock, &maps.a[1], kb * 64, T.row0, 0, x_bar);
+        }
+        if (c == 1 % chunks && walk.any()) {
+          for (int kb = 0; kb < x_blocks; ++kb) prefetch_box(leader, &maps.a[0], kb * 64, walk.row(), 0);
+          for (int kb = 0; kb < dy_blocks; ++kb) prefetch_box(leader, &maps.a[1], kb * 64, walk.row(), 0);
+        }
       }
       x_phase ^= 1;
     }
@@ -105,14 +110,16 @@ __global__ void __launch_bounds__(kThreads, 1) fused_backward(const __grid_const
                      dx_idesc = tc::idesc_bf16_f32(128, 64 * x_blocks, false, false);
       int gc = 0, dc = 0;                                  // chunk of the tile that G and D are at
       uint32_t x_phase = 0, dx_phase = 1;
-      bool ok = true;
-      for (int32_t i = 0; i <= total && ok; ++i) {
-        if (i < total) {
-          const uint32_t b = i & 1, phase = (uint32_t)i >> 1 & 1, at = sbase + kW + b * kWSlot, acc = tmem + b * kPart;
-          if (!(ok = wait_bar(B.part_empty + b, phase ^ 1, abort_flag))) break;
-          if (gc == 0 && !(ok = wait_bar(&B.x_full, x_phase, abort_flag))) break;
-          if (!(ok = wait_bar(B.w_full + b, phase, abort_flag))) break;
+      uint32_t i = 0, j = 0;                               // the next G and D
+      long long t0 = clock64();
+      while (j < (uint32_t)total) {
+        bool idle = true;
+        if (const uint32_t b = i & 1, phase = i >> 1 & 1;
+            i < (uint32_t)total && tc::mbar_test(B.part_empty + b, phase ^ 1) && (gc != 0 || tc::mbar_test(&B.x_full, x_phase)) &&
+            tc::mbar_test(B.w_full + b, phase)) {
+          idle = false;
           tc::tc_fence_after_sync();
+          const uint32_t at = sbase + kW + b * kWSlot, acc = tmem + b * kPart;
           for (int kb = 0; kb < dy_blocks; ++kb) {
             const uint64_t a0 = tc::smem_desc_sw128(sbase + kDy + kb * kXBlock, 16, 1024), b0 = tc::smem_desc_sw128(at + (4 + kb) * kWBlock, 16, 1024);
             const int steps = min(4, (A.K[0] - kb * 64 + 15) >> 4);
@@ -133,14 +140,12 @@ __global__ void __launch_bounds__(kThreads, 1) fused_backward(const __grid_const
             x_phase ^= 1;
             tc::mma_commit(&B.x_empty);
           }
+          ++i;
         }
-        if (i > 0) {
-          const uint32_t j = (uint32_t)i - 1, at = sbase + kW + (j & 1) * kWSlot;
-          if (!(ok = wait_bar(&B.h_full, j & 1, abort_flag))) break;
-          if (dc == 0) {
-            if (!(ok = wait_bar(&B.dx_empty, dx_phase, abort_flag))) break;
-            dx_phase ^= 1;
-          }
+        if (j < i && tc::mbar_test(&B.h_full, j & 1) && (dc != 0 || tc::mbar_test(&B.dx_empty, dx_phase))) {
+          idle = false;
+          const uint32_t at = sbase + kW + (j & 1) * kWSlot;
+          if (dc == 0) dx_phase ^= 1;
           tc::tc_fence_after_sync();
           const int steps = min(4, (A.K[1] - dc * kChunk + 15) >> 4);
 #pragma unroll
@@ -156,6 +161,13 @@ __global__ void __launch_bounds__(kThreads, 1) fused_backward(const __grid_const
             dc = 0;
             tc::mma_commit(&B.dx_full);
           }
+          ++j;
+        }
+        if (!idle) t0 = clock64();
+        else if (*abort_flag) break;
+        else if (clock64() - t0 > 4000000000ll) {
+          *abort_flag = 1;
+          break;
         }
       }
     }

@@ -70,6 +70,11 @@ __device__ __forceinline__ void load_box_of_set(uint32_t leader, uint32_t dst, c
                  "@go cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(set), "r"(0), "r"(bar), "r"(leader) : "memory");
 }
+// a box of a later load, into L2
+__device__ __forceinline__ void prefetch_box(uint32_t leader, const CUtensorMap* map, int32_t x, int32_t y, int32_t z) {
+  asm volatile("{\n\t.reg .pred go;\n\tsetp.ne.b32 go, %4, 0;\n\t@go cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];\n\t}"
+               ::"l"(map), "r"(x), "r"(y), "r"(z), "r"(leader) : "memory");
+}
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 // announces `bytes` on a barrier of this CTA or, by cluster address, of the pair's even one
 template <bool PAIR>
@@ -446,6 +451,8 @@ class Walk {
     }
     return T;
   }
+  // the first row of that tile
+  __device__ __forceinline__ int32_t row() const { return table ? a : m * (PAIR ? 256 : 128); }
   // a tile whose rows do not matter
   __device__ __forceinline__ void skip() { t += step; }
 };

@@ -260,17 +260,21 @@ bool fuses(const gnnco_handle* h, const gnnco_gated_ff_desc* d) {
   return pairs > 0 && (2 * tiles >= pairs || d->H <= 256);
 }
 
-// The same for h, dg, du and dx (gated_ff_fused_back.cu).  dx is written before the weight gradients read x and dy there, so it must be
-// neither of them.
+// The same for h, dg, du and dx (gated_ff_fused_back.cu): where H is short, since a chunk of H costs more there (its weights are read for 128
+// rows, by pairs of CTAs for 256).  Backward passes, in one kernel and in two, in us: 1.13 M x 128 x 256 in 1,024 sets 1,220 and 1,320,
+// 300,000 x 32 x 64 in 512 113 and 125, 1,000 x 64 x 128 in 8 20.5 and 22.6, 4,000 x 128 x 256 32.7 and 32.8; but 60,000 x 64 x 600 in
+// 64 170 and 166, 20,000 x 128 x 1,024 133 and 117, and with few tiles 300 x 128 x 256 24.6 and 22.6.
+// dx is written before the weight gradients read x and dy there, so it must be neither of them.
 bool fuses_back(const gnnco_handle* h, const gnnco_gated_ff_desc* d, const gnnco_gated_ff_grads* g, const Operand& x, const Operand& dy) {
-  if (d->feat_dtype != GNNCO_BF16 || d->F > 128 || d->F_out > 128 || !g->dx || ((uintptr_t)g->dx & 15) || g->dx_ld % 8) return false;
+  if (d->feat_dtype != GNNCO_BF16 || d->F > 128 || d->F_out > 128 || d->H > 256 || !g->dx || ((uintptr_t)g->dx & 15) || g->dx_ld % 8 || d->F % 8)
+    return false;
   auto apart = [&](const Operand& o, int cols) {
     const uintptr_t a = (uintptr_t)g->dx, b = (uintptr_t)o.p;
     return a + ((d->rows - 1) * g->dx_ld + d->F) * 2 <= b || b + ((d->rows - 1) * o.ld + cols) * 2 <= a;
   };
   if (g->dw_gate && !(apart(x, d->F) && apart(dy, d->F_out))) return false;
   const int64_t tiles = d->sets > 1 ? h->n_tiles : blocks_of(d->rows, 128);
-  return tiles >= 1;
+  return 4 * tiles >= h->sm_count || d->H <= 128;
 }
 
 Work lay_out(const gnnco_handle* h, const gnnco_gated_ff_desc* d, bool backward) {
@@ -531,7 +535,8 @@ struct Call {
     a->y = y;
     a->y_ld = ld;
     a->y_f32 = d->feat_dtype == GNNCO_F32;
-    a->y_vectors = ((uintptr_t)y & 15) == 0 && ld % (a->y_f32 ? 4 : 8) == 0;
+    // (a box is cut at the tensor's last column in units of 16 bytes: rows that end inside one would lose what lies behind them)
+    a->y_vectors = ((uintptr_t)y & 15) == 0 && ld % (a->y_f32 ? 4 : 8) == 0 && cols % (a->y_f32 ? 4 : 8) == 0;
     return !a->y_vectors || map_out(&m->out[0], a->y_f32, y, d->rows, cols, ld, 0, 1, a->y_f32 ? 16 : 32);
   }
   int32_t weight_grads(const Operand& x, const Operand& dy, const Operand* hdd, const gnnco_gated_ff_grads* g, float* scratch) {

@@ -54,7 +54,7 @@ struct Args {
   // results of kDown, kDx
   void* y;
   int64_t y_ld;
-  int32_t y_f32, y_vectors;            // y_vectors: rows and base are 16-byte aligned
+  int32_t y_f32, y_vectors;            // y_vectors: rows start and end on 16 bytes
   int32_t masked;
   philox::Mask mask;
   // kWeights

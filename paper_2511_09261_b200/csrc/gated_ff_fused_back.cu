@@ -1,5 +1,5 @@
-// The gated feed-forward block's backward pass up to dx as ONE kernel, for bfloat16 operands and widths F, F_out <= 128: dg and du are multiplied
-// where they were computed.
+// The gated feed-forward block's backward pass up to dx as ONE kernel, for bfloat16 operands, widths F, F_out <= 128 and F a multiple of 8: dg
+// and du are multiplied where they were computed.
 //
 //   a CTA takes 128 rows of x and dy', which stay in shared memory, and walks H in chunks of 64 columns:
 //     G(c)   [g | u] = x [Wg | Wu],  dh = dy' Wd^T      128 x 192 in tensor memory (two buffers)
@@ -8,9 +8,12 @@
 //     D(c)   dx += dg Wg^T + du Wu^T                    128 x F, in tensor memory until the last chunk
 //
 // G(c + 1) runs while chunk c is converted, across tiles too.  Whichever of the next G and the next D has its operands is issued: D in turn
-// with G would wait for weights that take the place of its own (667 us for 1.13 M x 128 x 256 against XXX).  One copy of a
+// with G would wait for weights that take the place of its own (1.13 M x 128 x 256: 667 us, this way 612; two launches 728).  One copy of a
 // chunk's weights serves both: G reads Wg and Wu along their rows, D across them.  (A pair of CTAs would have to hold different
 // halves for the two.)  A tile's dx is taken out after the first chunk of the next tile.
+// What bounds it: 4,500 cycles a chunk, of which a place for weights is held for 6,500 of two chunks from its copy to D, and the 48 KB
+// of h, dg and du take 2,900 on their way to memory (without them 500 us).  Two teams of result warps that take chunks in turn
+// spilled registers and held the one buffer of h longer: 777 us.
 //
 // Shared memory: x 32 KB, dy' 32 KB, h, dg and du 48 KB, two chunks of Wg, Wu, Wd 96 KB, staging of dx 16 KB.
 // Roles of the warps: 0 products, 1 copies, 2 stores h, dg and du, 4-19 results.
@@ -236,13 +239,8 @@ __global__ void __launch_bounds__(kThreads, 1) fused_backward(const __grid_const
       } else if (lane < dx_rows) {
         __nv_bfloat16* const to = static_cast<__nv_bfloat16*>(A.y) + (int64_t)(dx_row0 + lane) * A.y_ld + c0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (c0 + 8 * k + 8 <= A.cols) *reinterpret_cast<uint4*>(to + 8 * k) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
-          else
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (c0 + 8 * k + e < A.cols)
-                reinterpret_cast<unsigned short*>(to)[8 * k + e] = (unsigned short)(w[4 * k + e / 2] >> (16 * (e & 1)));
+        for (int k = 0; k < 4; ++k)                        // (F is a multiple of 8)
+          if (c0 + 8 * k < A.cols) *reinterpret_cast<uint4*>(to + 8 * k) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
       }
       return true;
     };

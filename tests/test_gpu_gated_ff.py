@@ -438,3 +438,49 @@ def test_elements_past_32_bits():
     want = g.gated_ff_backward(last, last, *w, want_dw=False)["dx"]
     assert float((dx[-300:].float() - want.float()).norm() / want.float().norm()) < 2 * BF
     assert g.async_status() == gnnco.OK
+
+
+@pytest.mark.parametrize("F,H,Fo", [(128, 256, 128), (64, 64, 64), (8, 1, 8), (40, 65, 104), (99, 130, 65), (128, 250, 24), (24, 200, 128)])
+@pytest.mark.parametrize("act,p", [("silu", 0.0), ("gelu", 0.3)])
+def test_gradients_of_many_rows_in_bfloat16(F, H, Fo, act, p):
+    """More tiles of rows than SMs, ragged and empty subgraphs; dx in a wider tensor, beside columns that keep their values; dx in
+    the place of x, where it may not be written before the weights' gradients have read x, gives the same bits."""
+    import torch
+    sizes = np.random.RandomState(F + H).randint(0, 1500, 40)
+    sizes[[3, 17]] = 0, 1
+    ptr = np.concatenate([[0], np.cumsum(sizes)])
+    rows = int(ptr[-1])
+    g, t = load(sizes), make(rows, len(sizes), F, H, Fo, "bf16")
+    drop = gnnco.Dropout(p, 5, layer=2) if p else None
+    mask = ref.keep(rows, Fo, p, 5, layer=2) / (1 - p) if p else None
+    d = check_backward(g, t, ptr, act, "bf16", drop, mask, slots=4)
+    wide = torch.full((rows, 136), 7.0, dtype=torch.bfloat16, device="cuda")
+    e = g.gated_ff_backward(*t, act=act, drop=drop, dx=wide[:, :F])
+    assert all(torch.equal(e[k], d[k]) for k in d) and bool((wide[:, F:] == 7.0).all())
+    e = g.gated_ff_backward(*t, act=act, drop=drop, want_dw=False, dx=wide[:, 1:F + 1])
+    assert torch.equal(e["dx"], d["dx"])
+    e = g.gated_ff_backward(*t, act=act, drop=drop, dx=t[0])
+    assert all(torch.equal(e[k], d[k]) for k in d)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,F,H,Fo", [(150, 99, 41, 51), (7000, 99, 200, 51), (7000, 30, 300, 201), (7000, 261, 40, 270)])
+def test_odd_columns_of_wider_tensors(single, dtype, rows, F, H, Fo):
+    """Rows start on 16 bytes but end inside 16: what lies behind them is neither read (it is NaN) nor written."""
+    import torch
+    x, dy, *w = make(rows, 1, F, H, Fo, dtype)
+
+    def wide(t):
+        full = torch.full((rows, 272), float("nan"), dtype=t.dtype, device="cuda")
+        full[:, :t.shape[1]] = t
+        return full, full[:, :t.shape[1]]
+    want, d = single.gated_ff(x, *w), single.gated_ff_backward(x, dy, *w)
+    fx, vx = wide(x)
+    fdy, vdy = wide(dy)
+    fy, vy = wide(torch.zeros_like(dy))
+    fdx, vdx = wide(torch.zeros_like(x))
+    single.gated_ff(vx, *w, out=vy)
+    e = single.gated_ff_backward(vx, vdy, *w, dx=vdx)
+    assert torch.equal(vy, want) and all(torch.equal(e[k], d[k]) for k in d)
+    for full, n in ((fx, F), (fdy, Fo), (fy, Fo), (fdx, F)):
+        assert bool(full[:, n:].isnan().all())

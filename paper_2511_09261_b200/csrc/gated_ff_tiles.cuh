@@ -566,14 +566,12 @@ __global__ void __launch_bounds__(kThreads, 1) tiles(const __grid_constant__ Map
             }
           }
           if constexpr (kAlongRows) if (valid < 64) {
-            // row k of a 64-column block is 128 bytes at 128 k, whatever the swizzle does inside it
+            // row k of a 64-column block is 128 bytes at 128 k, whatever the swizzle does inside it; the products take 16 rows at a time
             if (!(ok = __all_sync(0xffffffffu, wait_bar(tail, tails & 1, abort_flag)) != 0)) break;
             ++tails;
-            const int blocks = (2 + nt / kCtas / 64) * LIMBS, zero = 64 - valid;
-            for (int q = lane; q < blocks * zero * 8; q += 32) {
-              const int block = q / (zero * 8), rest = q % (zero * 8);
-              tc::st_shared_zero16(at + block * 8192 + (valid + rest / 8) * 128 + (rest & 7) * 16);
-            }
+            const uint32_t end = at + (2 + nt / kCtas / 64) * kBlock;
+            for (uint32_t block = at; block < end; block += 8192)
+              for (int b = valid * 128 + lane * 16; b < ((valid + 15) & ~15) * 128; b += 512) tc::st_shared_zero16(block + b);
             tc::fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) {

@@ -459,7 +459,8 @@ int32_t gnnco_dropout(gnnco_handle* h, int32_t feat_dtype, int64_t rows, int32_t
  * GELU a = g (1 + erf(g / sqrt 2)) / 2, or the rectifier (derivative 0 at 0).  drop == NULL: none; else the mask of
  * gnnco_dropout on [rows x F_out].
  * feat_dtype: x, y, dy, dx.  w_dtype: GNNCO_F32, or GNNCO_BF16 with bfloat16 features; contiguous.  float32 features are
- * multiplied as three bfloat16 limbs (24 bits, float32 sums); finite values of magnitude below 2^-110 lose bits there, and
+ * multiplied as three bfloat16 limbs (24 bits, float32 sums; few rows in all or per subgraph: as float32); finite values of
+ * magnitude below 2^-110 lose bits there, and
  * above 3.38e38 become infinite.  In bfloat16 features h, dg and du are rounded to bfloat16 once (not h of one to four rows), float32 weights too.
  * A row with an infinity or NaN spoils its own results and, in the backward pass, its subgraph's weight gradients.
  * gnnco_gated_ff_backward: dy -> dx [rows x F] (or NULL) and the weight gradients (all three or none; dw_dtype as asked, like the

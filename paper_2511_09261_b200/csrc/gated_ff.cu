@@ -1,7 +1,7 @@
 // The gated feed-forward block, forward and backward: entry points, work areas, copies of operands and the choice of kernels
 // (formulas and kinds of products: gated_ff.cuh; the products: gated_ff_tiles.cuh).
 //
-// Up to four rows with one set of weights: gated_ff_rows.cu.  Forward in bfloat16 with widths up to 256: gated_ff_fused.cu.  Else
+// Up to four rows with one set of weights: gated_ff_rows.cu.  Subgraphs of few rows in float32: gated_ff_sets.cu.  Forward in bfloat16 with widths up to 256: gated_ff_fused.cu.  Else
 // Forward:   [operands as limbs]   h = act(x Wg) .* (x Wu)   y = drop(h Wd)
 // Backward:  [operands as limbs]   h, dg, du (g and u are computed again: nothing but x is kept from the forward pass, which at
 //            widths up to some 400 is also faster than writing and reading them)   dx   the weight gradients   [their partial sums]
@@ -12,6 +12,7 @@
 // most, as much as the results are rounded by), in float32 features three limbs (24 bits); float32 weights of bfloat16
 // features are rounded to bfloat16.  All sums are float32, and none depends on timing.
 #include "gated_ff.cuh"
+#include "gated_ff_sets.cuh"
 #include "vec_io.cuh"
 
 namespace ff {
@@ -285,6 +286,11 @@ Work lay_out(const gnnco_handle* h, const gnnco_gated_ff_desc* d, bool backward)
     w.total = align_up((size_t)d->rows * d->H * 4);
     return w;
   }
+  if (!backward && ff::few_rows_per_set(h, d)) {           // (backward the weight gradients' type decides, which is not known here)
+    w.h = 0;
+    w.total = align_up((size_t)d->rows * d->H * 4);
+    return w;
+  }
   auto take = [&](bool needed, int64_t elements) {
     if (!needed) return kNone;
     const size_t at = w.total;
@@ -328,6 +334,19 @@ struct Call {
   PackJobs jobs;
   int n_jobs = 0;
 
+  ff::SetArgs set_args() const {
+    ff::SetArgs A = {};
+    A.x = static_cast<const float*>(d->x);
+    A.x_ld = d->x_ld;
+    A.wg = static_cast<const float*>(d->w_gate);
+    A.wu = static_cast<const float*>(d->w_up);
+    A.wd = static_cast<const float*>(d->w_down);
+    A.F = d->F; A.H = d->H; A.F_out = d->F_out;
+    A.act = d->act;
+    A.masked = drops;
+    A.mask = jobs.mask;
+    return A;
+  }
   Operand operand(const void* p, int64_t rows, int32_t cols, int64_t ld, int dtype, bool masked, char* copy) {
     Operand o;
     if (!masked && direct(p, ld, dtype)) {
@@ -647,6 +666,16 @@ extern "C" int32_t gnnco_gated_ff(gnnco_handle* h, const gnnco_gated_ff_desc* d,
     return GNNCO_OK;
   }
   const int64_t sets = d->sets;
+  if (ff::few_rows_per_set(h, d)) {
+    ff::SetArgs A = c.set_args();
+    A.h = reinterpret_cast<float*>(base + w.h);
+    A.out = static_cast<float*>(y);
+    A.out_ld = y_ld;
+    const int32_t r = ff::launch_sets(h, A, sets, false, c.st);
+    if (r != GNNCO_OK) return r;
+    GNNCO_LAUNCH_CHECK();
+    return GNNCO_OK;
+  }
   const Operand x = c.operand(d->x, d->rows, d->F, d->x_ld, d->feat_dtype, false, base + w.x);
   const Operand wg = c.operand(d->w_gate, sets * d->F, d->H, d->H, d->w_dtype, false, base + w.wg);
   const Operand wu = c.operand(d->w_up, sets * d->F, d->H, d->H, d->w_dtype, false, base + w.wu);
@@ -697,6 +726,24 @@ extern "C" int32_t gnnco_gated_ff_backward(gnnco_handle* h, const gnnco_gated_ff
   if (ws_bytes < w.total) return GNNCO_WORKSPACE_TOO_SMALL;
   ProfScope prof_(h, K_GATED_FF, c.st);
   char* const base = static_cast<char*>(ws);
+  if (ff::few_rows_per_set(h, d) && (!weights || g->dw_dtype == GNNCO_F32)) {
+    ff::SetArgs A = c.set_args();
+    A.dy = static_cast<const float*>(dy);
+    A.dy_ld = dy_ld;
+    if (g->dx) {                                           // (the tiled products' copies of h, dg and du take more)
+      A.dg = reinterpret_cast<float*>(base + w.h);
+      A.du = A.dg + d->rows * d->H;
+    }
+    A.dwg = static_cast<float*>(g->dw_gate);
+    A.dwu = static_cast<float*>(g->dw_up);
+    A.dwd = static_cast<float*>(g->dw_down);
+    A.out = static_cast<float*>(g->dx);
+    A.out_ld = g->dx_ld;
+    const int32_t r = ff::launch_sets(h, A, sets, true, c.st);
+    if (r != GNNCO_OK) return r;
+    GNNCO_LAUNCH_CHECK();
+    return GNNCO_OK;
+  }
   const Operand x = c.operand(d->x, d->rows, d->F, d->x_ld, d->feat_dtype, false, base + w.x);
   const Operand wg = c.operand(d->w_gate, sets * d->F, d->H, d->H, d->w_dtype, false, base + w.wg);
   const Operand wu = c.operand(d->w_up, sets * d->F, d->H, d->H, d->w_dtype, false, base + w.wu);

@@ -143,6 +143,7 @@ struct gnnco_handle {
   int32_t *wg_mpart = nullptr, *wg_mfirst = nullptr, *wg_mcount = nullptr;
   int32_t n_wg_chunks = 0, n_wg_slots = 0, n_wg_multi = 0;
   std::vector<int32_t> h_part_ptr;
+  int32_t longest_part = 0;
   // a step on the active subgraphs only: the rows it covers (nullptr: all), the plan built by
   // gnnco_active_plan and the device flags it was built from
   RowChunks row_chunks;

@@ -625,6 +625,10 @@ extern "C" int32_t gnnco_partition_load(const gnnco_graph_desc* g, void* persist
 
   // 5. host-built tables: dense-transform tiles, objective work items, weight-gradient chunks (from part_ptr)
   HostWorkTables tab;
+  for (int32_t s = 0; s < S; ++s) {
+    const int32_t rows = h->h_part_ptr[s + 1] - h->h_part_ptr[s];
+    if (rows > h->longest_part) h->longest_part = rows;
+  }
   build_work_tables(h->h_part_ptr, S, n, h->sm_count, nullptr, tab);
   const std::vector<int32_t>&t0 = tab.t0, &tr = tab.tr, &p0 = tab.p0, &pr = tab.pr, &i0 = tab.i0, &i1 = tab.i1, &pip = tab.pip,
                             &wb = tab.wb, &we = tab.we, &wsl = tab.wsl, &mp = tab.mp, &mf = tab.mf, &mc = tab.mc;

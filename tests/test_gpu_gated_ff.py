@@ -484,3 +484,42 @@ def test_odd_columns_of_wider_tensors(single, dtype, rows, F, H, Fo):
     assert torch.equal(vy, want) and all(torch.equal(e[k], d[k]) for k in d)
     for full, n in ((fx, F), (fdy, Fo), (fy, Fo), (fdx, F)):
         assert bool(full[:, n:].isnan().all())
+
+
+FEW = [0, 1, 8, 9, 2, 16, 17, 3, 0, 7, 60] + [1] * 12
+
+
+@pytest.mark.parametrize("F,H,Fo", [(1, 1, 1), (33, 19, 21), (64, 128, 40), (384, 40, 100), (20, 1024, 384), (32, 65, 33)])
+@pytest.mark.parametrize("act,p", [("silu", 0.0), ("gelu", 0.3)])
+def test_subgraphs_of_few_rows_in_float32(F, H, Fo, act, p):
+    """Sums of eight partial sums, K / 8 roundings each, are inside the bound of the tiled products for these lengths (18 + K / 64 on g
+    and u, three times over in the backward pass, from K = 384: 56)."""
+    import torch
+    ptr = np.concatenate([[0], np.cumsum(FEW)])
+    rows = int(ptr[-1])
+    g, t = load(FEW), make(rows, len(FEW), F, H, Fo, "f32")
+    drop = gnnco.Dropout(p, 5, layer=2) if p else None
+    mask = ref.keep(rows, Fo, p, 5, layer=2) / (1 - p) if p else None
+    y = check_forward(g, t, ptr, act, "f32", drop, mask)
+    d = check_backward(g, t, ptr, act, "f32", drop, mask, slots=8)
+    assert all(not d[k][s].any() for k in ("dw_gate", "dw_up", "dw_down") for s in (0, 8))
+    wide = torch.full((rows, 401), 7.0, device="cuda")
+    x = wide[:, 1:F + 1]
+    x.copy_(t[0])
+    assert torch.equal(g.gated_ff(x, *t[2:], act=act, drop=drop), y)
+    e = g.gated_ff_backward(x, t[1], *t[2:], act=act, drop=drop, dx=x)
+    assert all(torch.equal(e[k], d[k]) for k in d)
+    assert bool((wide[:, F + 1:] == 7.0).all()) and bool((wide[:, 0] == 7.0).all())
+    assert torch.equal(g.gated_ff_backward(*t, act=act, drop=drop, want_dw=False)["dx"], d["dx"])
+    assert torch.equal(g.gated_ff_backward(*t, act=act, drop=drop, want_dx=False)["dw_up"], d["dw_up"])
+    check_backward(g, t, ptr, act, "f32", drop, mask, slots=8, dw_dtype=torch.bfloat16)
+    bad = [v.clone() for v in t]
+    bad[0][int(ptr[3])] = float("nan")                      # a row of subgraph 3
+    bad[2][1] = float("inf")                                # the gate's weights of subgraph 1
+    y2, d2 = g.gated_ff(bad[0], *bad[2:], act=act), g.gated_ff_backward(*bad, act=act)
+    y, d = g.gated_ff(t[0], *t[2:], act=act), g.gated_ff_backward(*t, act=act)
+    keep = torch.ones(rows, dtype=torch.bool, device="cuda")
+    keep[int(ptr[3])] = keep[int(ptr[1])] = False
+    assert torch.equal(y2[keep], y[keep]) and torch.equal(d2["dx"][keep], d["dx"][keep])
+    sets = [s for s in range(len(FEW)) if s not in (1, 3)]
+    assert all(torch.equal(d2[k][sets], d[k][sets]) for k in ("dw_gate", "dw_up", "dw_down"))

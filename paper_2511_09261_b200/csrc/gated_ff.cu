@@ -1,7 +1,8 @@
 // The gated feed-forward block, forward and backward: entry points, work areas, copies of operands and the choice of kernels
 // (formulas and kinds of products: gated_ff.cuh; the products: gated_ff_tiles.cuh).
 //
-// Up to four rows with one set of weights: gated_ff_rows.cu.  Subgraphs of few rows in float32: gated_ff_sets.cu.  Forward in bfloat16 with widths up to 256: gated_ff_fused.cu.  Else
+// Up to four rows with one set of weights: gated_ff_rows.cu.  Subgraphs of few rows in float32: gated_ff_sets.cu.  Bfloat16 forward with
+// widths up to 256: gated_ff_fused.cu; backward, up to dx, with widths up to 128: gated_ff_fused_back.cu.  Else
 // Forward:   [operands as limbs]   h = act(x Wg) .* (x Wu)   y = drop(h Wd)
 // Backward:  [operands as limbs]   h, dg, du (g and u are computed again: nothing but x is kept from the forward pass, which at
 //            widths up to some 400 is also faster than writing and reading them)   dx   the weight gradients   [their partial sums]

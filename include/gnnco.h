@@ -25,6 +25,9 @@
  *     which every subgraph is a contiguous id range; `perm` (new -> original) and
  *     `inv_perm` (original -> new) from gnnco_graph_info map back to the caller's ids.
  *   - Dense matrices are row-major.
+ *   - Calls on one handle are issued by one thread at a time, but for gnnco_dropout, gnnco_block_norm*,
+ *     gnnco_gated_ff*: other threads may issue these at any time after the load, also while a training step is
+ *     being issued.
  */
 #ifndef GNNCO_H_
 #define GNNCO_H_

@@ -231,8 +231,8 @@ Chunks chunks_of(const gnnco_handle* h, const gnnco_gated_ff_desc* d) {
   Chunks c;
   if (d->sets > 1) {                                       // the handle's runs of rows: long subgraphs are cut
     c.table = true;
-    c.count = h->n_wg_chunks;
-    c.slots = h->n_wg_slots;
+    c.count = h->all_rows.n_wg_chunks;
+    c.slots = h->all_rows.n_wg_slots;
     return c;
   }
   // one set: enough runs that every SM has a tile of 128 x 128, none shorter than 512 rows -- and none longer than 65,536: the tensor
@@ -258,7 +258,7 @@ Chunks chunks_of(const gnnco_handle* h, const gnnco_gated_ff_desc* d) {
 // 86; 1,000 x 64 x 128 in 8 sets 9.0 and 13.1; but 4,000 x 256 x 512 16.3 and 14.3, 4,000 x 256 x 4,096 71 and 38.)
 bool fuses(const gnnco_handle* h, const gnnco_gated_ff_desc* d) {
   if (d->feat_dtype != GNNCO_BF16 || d->F > 256 || d->F_out > 256) return false;
-  const int64_t pairs = ff::resident_pairs(h->device, h->sm_count), tiles = d->sets > 1 ? h->n_pairs : blocks_of(d->rows, 256);
+  const int64_t pairs = ff::resident_pairs(h->device, h->sm_count), tiles = d->sets > 1 ? h->all_rows.n_pairs : blocks_of(d->rows, 256);
   return pairs > 0 && (2 * tiles >= pairs || d->H <= 256);
 }
 
@@ -275,7 +275,7 @@ bool fuses_back(const gnnco_handle* h, const gnnco_gated_ff_desc* d, const gnnco
     return a + ((d->rows - 1) * g->dx_ld + d->F) * 2 <= b || b + ((d->rows - 1) * o.ld + cols) * 2 <= a;
   };
   if (g->dw_gate && !(apart(x, d->F) && apart(dy, d->F_out))) return false;
-  const int64_t tiles = d->sets > 1 ? h->n_tiles : blocks_of(d->rows, 128);
+  const int64_t tiles = d->sets > 1 ? h->all_rows.n_tiles : blocks_of(d->rows, 128);
   return 4 * tiles >= h->sm_count || d->H <= 128;
 }
 
@@ -383,7 +383,7 @@ struct Call {
   }
   // tiles of rows
   int64_t row_tiles(bool pair) const {
-    if (d->sets > 1) return pair ? h->n_pairs : h->n_tiles;
+    if (d->sets > 1) return pair ? h->all_rows.n_pairs : h->all_rows.n_tiles;
     return blocks_of(d->rows, pair ? 256 : 128);
   }
   void rows_of(Args* a, bool pair) const {
@@ -391,8 +391,8 @@ struct Call {
     a->node_part = h->node_part;
     a->m_tiles = (int32_t)row_tiles(pair);
     if (d->sets > 1) {
-      a->tile_row0 = pair ? h->pair_row0 : h->tile_row0;
-      a->tile_rows = pair ? h->pair_rows : h->tile_rows;
+      a->tile_row0 = pair ? h->all_rows.pair_row0 : h->all_rows.tile_row0;
+      a->tile_rows = pair ? h->all_rows.pair_rows : h->all_rows.tile_rows;
     }
     a->status = h->status;
   }
@@ -588,9 +588,9 @@ struct Call {
     a.chunk_rows = c.rows;
     a.per_chunk = (int32_t)tiles_of(a.p);
     if (c.table) {
-      a.chunk_begin = h->wg_begin;
-      a.chunk_end = h->wg_end;
-      a.chunk_slot = h->wg_slot;
+      a.chunk_begin = h->all_rows.wg_begin;
+      a.chunk_end = h->all_rows.wg_end;
+      a.chunk_slot = h->all_rows.wg_slot;
     }
     for (int q = 0; q < 3; ++q) {
       ff::Problem& P = a.p[q];
@@ -616,10 +616,10 @@ struct Call {
         J.out[q] = outs[q];
         if (J.count[q] > most) most = J.count[q];
       }
-      if (c.table) { J.part = h->wg_mpart; J.first = h->wg_mfirst; J.slots = h->wg_mcount; }
+      if (c.table) { J.part = h->all_rows.wg_mpart; J.first = h->all_rows.wg_mfirst; J.slots = h->all_rows.wg_mcount; }
       J.all = c.slots;
       J.out_f32 = f32;
-      const int sets = c.table ? h->n_wg_multi : 1;
+      const int sets = c.table ? h->all_rows.n_wg_multi : 1;
       const int64_t blocks = blocks_of(most, 256);
       // (a split subgraph has over 2,048 rows: there are fewer than 2^20 of them, and a grid takes 65,535 at a time)
       for (int s0 = 0; s0 < sets; s0 += 65535) {

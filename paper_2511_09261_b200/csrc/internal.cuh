@@ -101,6 +101,15 @@ struct WorkSet {
   FuseSet fuse;
 };
 
+// The tables of all subgraphs as gnnco_partition_load built them.  A training step exchanges the handle's own fields while it issues its
+// launches (WorkSet, ranges of subgraphs, heavy double tiles); operators that another thread may issue meanwhile read these.
+struct RowTables {
+  const int32_t *tile_row0 = nullptr, *tile_rows = nullptr, *pair_row0 = nullptr, *pair_rows = nullptr;
+  const int32_t *wg_begin = nullptr, *wg_end = nullptr, *wg_slot = nullptr;
+  const int32_t *wg_mpart = nullptr, *wg_mfirst = nullptr, *wg_mcount = nullptr;
+  int32_t n_tiles = 0, n_pairs = 0, n_wg_chunks = 0, n_wg_slots = 0, n_wg_multi = 0;
+};
+
 // The host-buffer step lets layer 1 start on a range of subgraphs as soon as that range of X has been uploaded:
 // per range the event its copy records and where its tiles and double tiles start in the tables.
 constexpr int kArrivalGroups = 8;
@@ -144,13 +153,14 @@ struct gnnco_handle {
   int32_t n_wg_chunks = 0, n_wg_slots = 0, n_wg_multi = 0;
   std::vector<int32_t> h_part_ptr;
   int32_t longest_part = 0;
+  RowTables all_rows;                                        // not written after the load
   // a step on the active subgraphs only: the rows it covers (nullptr: all), the plan built by
   // gnnco_active_plan and the device flags it was built from
   RowChunks row_chunks;
   WorkSet plan;
   const uint8_t* plan_active = nullptr;
   int32_t plan_active_count = -1;                            // -1: no plan
-  int64_t launches = 0;
+  std::atomic<int64_t> launches{0};                          // (several threads may issue operators)
   Profiler prof;
   // bf16 copies of the weights that the last updating step left in its work area (GNNCO_WEIGHTS_UNTOUCHED):
   // which master weights and which copies they belong to; fresh[l] says whether layer l's copies are current

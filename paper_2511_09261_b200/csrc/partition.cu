@@ -640,6 +640,12 @@ extern "C" int32_t gnnco_partition_load(const gnnco_graph_desc* g, void* persist
   h->n_pairs = (int32_t)p0.size();
   h->n_items = (int32_t)i0.size();
   if (h->n_tiles > P.max_tiles || h->n_items > P.max_items) return GNNCO_INTERNAL;
+  RowTables& all = h->all_rows;
+  all.tile_row0 = P.tile_row0; all.tile_rows = P.tile_rows; all.pair_row0 = P.pair_row0; all.pair_rows = P.pair_rows;
+  all.wg_begin = P.wg_begin; all.wg_end = P.wg_end; all.wg_slot = P.wg_slot;
+  all.wg_mpart = P.wg_mpart; all.wg_mfirst = P.wg_mfirst; all.wg_mcount = P.wg_mcount;
+  all.n_tiles = h->n_tiles; all.n_pairs = h->n_pairs; all.n_wg_chunks = h->n_wg_chunks;
+  all.n_wg_slots = h->n_wg_slots; all.n_wg_multi = h->n_wg_multi;
   auto up = [&](int32_t* dst, const std::vector<int32_t>& v) {
     return v.empty() ? cudaSuccess
                      : cudaMemcpyAsync(dst, v.data(), v.size() * sizeof(int32_t), cudaMemcpyHostToDevice, st);
@@ -738,7 +744,7 @@ extern "C" int32_t gnnco_async_status(const gnnco_handle* h, void* stream, int32
   return GNNCO_OK;
 }
 
-extern "C" int64_t gnnco_launch_count(const gnnco_handle* h) { return h ? h->launches : 0; }
+extern "C" int64_t gnnco_launch_count(const gnnco_handle* h) { return h ? h->launches.load() : 0; }
 
 extern "C" int32_t gnnco_destroy(gnnco_handle* h) {
   if (h) {

@@ -229,15 +229,13 @@ int64_t slot_layout(const gnnco_gated_ff_desc* d, int64_t at[3]) {
 
 Chunks chunks_of(const gnnco_handle* h, const gnnco_gated_ff_desc* d) {
   Chunks c;
-  if (d->sets > 1) {                                       // the handle's runs of rows: long subgraphs are cut
+  if (d->sets > 1) {                                       // the handle's runs of rows, at most kMostRunRows long: long subgraphs are cut
     c.table = true;
     c.count = h->all_rows.n_wg_chunks;
     c.slots = h->all_rows.n_wg_slots;
     return c;
   }
-  // one set: enough runs that every SM has a tile of 128 x 128, none shorter than 512 rows -- and none longer than 65,536: the tensor
-  // core cuts off what does not fit when it adds 16 rows to an accumulator, up to 2^-23 of it each time (4,096 times here: 5e-4 at
-  // most, in bfloat16 features less than the stored dg's 2^-8; a million rows in one run would lose 1 %)
+  // one set: enough runs that every SM has a tile of 128 x 128, none shorter than 512 rows and none longer than kMostRunRows
   ff::Problem p[3];
   shape_problem(p, d->F, d->H, false, true);
   p[1] = p[0];
@@ -245,7 +243,7 @@ Chunks chunks_of(const gnnco_handle* h, const gnnco_gated_ff_desc* d) {
   const int64_t tiles = tiles_of(p);
   int64_t runs = tiles >= h->sm_count ? 1 : blocks_of(h->sm_count, tiles);
   if (runs > blocks_of(d->rows, 512)) runs = blocks_of(d->rows, 512);
-  if (runs < blocks_of(d->rows, 65536)) runs = blocks_of(d->rows, 65536);
+  if (runs < blocks_of(d->rows, kMostRunRows)) runs = blocks_of(d->rows, kMostRunRows);
   if (runs < 1) runs = 1;
   c.rows = (int32_t)((blocks_of(d->rows, runs) + 63) / 64 * 64);
   c.count = c.rows > 0 ? (int32_t)blocks_of(d->rows, c.rows) : 1;

@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "gnnco.h"
+#include "runs.cuh"
 
 #define GNNCO_CUDA_TRY(expr)                      \
   do {                                            \
@@ -24,7 +25,6 @@
 constexpr int kGemmTileRows = 128;   // rows of one dense-transform tile (never straddles a subgraph)
 constexpr int kLongRowDegree = 256;  // rows with more intra neighbours are aggregated by a whole block
 constexpr int kLongRowSegment = 2048; // ... and in segments of this many neighbours, one block each
-constexpr int kWgChunkMinRows = 2048; // a subgraph is split for the weight gradient only in runs at least this long
 constexpr int kItemRows = 1024;      // rows of one objective work item (never straddles a subgraph)
 
 // Kernel families, for launch accounting and per-kernel timing.
@@ -102,7 +102,8 @@ struct WorkSet {
 };
 
 // The tables of all subgraphs as gnnco_partition_load built them.  A training step exchanges the handle's own fields while it issues its
-// launches (WorkSet, ranges of subgraphs, heavy double tiles); operators that another thread may issue meanwhile read these.
+// launches (WorkSet, ranges of subgraphs, heavy double tiles); operators that another thread may issue meanwhile read these.  Their runs of
+// rows have at most kMostRunRows rows.
 struct RowTables {
   const int32_t *tile_row0 = nullptr, *tile_rows = nullptr, *pair_row0 = nullptr, *pair_rows = nullptr;
   const int32_t *wg_begin = nullptr, *wg_end = nullptr, *wg_slot = nullptr;
@@ -223,9 +224,8 @@ static inline int64_t linear_rows(const gnnco_handle* h) {
 
 // Host side of the work tables: what partition_load uploads for all subgraphs and what
 // gnnco_active_plan uploads for the active ones (active == nullptr: all).  Defined in partition.cu.
-struct HostWorkTables {
-  std::vector<int32_t> t0, tr, p0, pr, i0, i1, pip, wb, we, wsl, mp, mf, mc, c0, cr;
-  int32_t n_wg_slots = 0;
+struct HostWorkTables : HostRuns {
+  std::vector<int32_t> t0, tr, p0, pr, i0, i1, pip, c0, cr;
 };
 void build_work_tables(const std::vector<int32_t>& part_ptr, int32_t S, int64_t n, int sm_count, const uint8_t* active,
                        HostWorkTables& out);

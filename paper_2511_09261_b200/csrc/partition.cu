@@ -348,7 +348,8 @@ struct PersistentLayout {
   int32_t* src_list;
   FuseSet fuse;
   int32_t *wg_begin, *wg_end, *wg_slot, *wg_mpart, *wg_mfirst, *wg_mcount;
-  int64_t max_chunks;
+  int32_t *run_begin, *run_end, *run_slot, *run_mpart, *run_mfirst, *run_mcount;     // the same in runs of kMostRunRows rows
+  int64_t max_chunks, max_runs;
   int64_t max_tiles, max_items, max_long, max_segs;
   size_t bytes;
 };
@@ -392,6 +393,15 @@ PersistentLayout carve_persistent(void* base, int64_t n, int64_t E, int32_t S) {
   L.wg_mpart = c.take<int32_t>((size_t)S);
   L.wg_mfirst = c.take<int32_t>((size_t)S);
   L.wg_mcount = c.take<int32_t>((size_t)S);
+  // (needed where the runs above are longer, which hangs on the number of SMs, and only with subgraphs that are as long)
+  L.max_runs = n > kMostRunRows ? (int64_t)S + n / kMostRunRows + 1 : 0;
+  const size_t longer = n > kMostRunRows ? (size_t)(n / kMostRunRows + 1) : 0;       // subgraphs with more than kMostRunRows rows
+  L.run_begin = c.take<int32_t>(L.max_runs);
+  L.run_end = c.take<int32_t>(L.max_runs);
+  L.run_slot = c.take<int32_t>(L.max_runs);
+  L.run_mpart = c.take<int32_t>(longer);
+  L.run_mfirst = c.take<int32_t>(longer);
+  L.run_mcount = c.take<int32_t>(longer);
   L.bytes = c.off;
   return L;
 }
@@ -450,18 +460,11 @@ void build_work_tables(const std::vector<int32_t>& part_ptr, int32_t S, int64_t 
                        HostWorkTables& o) {
   o = HostWorkTables();
   o.pip.assign((size_t)S + 1, 0);
-  const int64_t sms = sm_count > 0 ? sm_count : 148;
-  const int64_t per = (n + 4 * sms - 1) / (4 * sms);
-  int64_t chunk_rows = (per + 63) / 64 * 64;
-  if (chunk_rows < kWgChunkMinRows) chunk_rows = kWgChunkMinRows;
-  int32_t slots = 0;
+  cut_runs(part_ptr, S, run_rows(n, sm_count), active, o);
   for (int32_t s = 0; s < S; ++s) {
     const int32_t a = part_ptr[s], b = part_ptr[s + 1];
     const bool on = !active || active[s];
     o.pip[s] = (int32_t)o.i0.size();
-    const bool split = b - a > chunk_rows;
-    int32_t first_slot = slots;
-    if (split) slots += (int32_t)((b - a + chunk_rows - 1) / chunk_rows);
     if (!on) continue;
     for (int32_t r = a; r < b; r += kGemmTileRows) {
       o.t0.push_back(r);
@@ -479,22 +482,8 @@ void build_work_tables(const std::vector<int32_t>& part_ptr, int32_t S, int64_t 
       o.i0.push_back(r);
       o.i1.push_back(b - r < kItemRows ? b : r + kItemRows);
     }
-    if (!split) {
-      o.wb.push_back(a); o.we.push_back(b); o.wsl.push_back(-(s + 1));
-    } else {
-      o.mp.push_back(s); o.mf.push_back(first_slot);
-      int32_t cnt = 0;
-      for (int64_t r = a; r < b; r += chunk_rows) {
-        o.wb.push_back((int32_t)r);
-        o.we.push_back((int32_t)(r + chunk_rows < b ? r + chunk_rows : b));
-        o.wsl.push_back(first_slot + cnt);
-        ++cnt;
-      }
-      o.mc.push_back(cnt);
-    }
   }
   o.pip[S] = (int32_t)o.i0.size();
-  o.n_wg_slots = slots;
 }
 
 extern "C" const char* gnnco_status_string(int32_t status) {
@@ -646,6 +635,14 @@ extern "C" int32_t gnnco_partition_load(const gnnco_graph_desc* g, void* persist
   all.wg_mpart = P.wg_mpart; all.wg_mfirst = P.wg_mfirst; all.wg_mcount = P.wg_mcount;
   all.n_tiles = h->n_tiles; all.n_pairs = h->n_pairs; all.n_wg_chunks = h->n_wg_chunks;
   all.n_wg_slots = h->n_wg_slots; all.n_wg_multi = h->n_wg_multi;
+  HostRuns runs;
+  if (run_rows(n, h->sm_count) > kMostRunRows && h->longest_part > kMostRunRows) {
+    cut_runs(h->h_part_ptr, S, kMostRunRows, nullptr, runs);
+    if ((int64_t)runs.wb.size() > P.max_runs) return GNNCO_INTERNAL;
+    all.wg_begin = P.run_begin; all.wg_end = P.run_end; all.wg_slot = P.run_slot;
+    all.wg_mpart = P.run_mpart; all.wg_mfirst = P.run_mfirst; all.wg_mcount = P.run_mcount;
+    all.n_wg_chunks = (int32_t)runs.wb.size(); all.n_wg_slots = runs.n_wg_slots; all.n_wg_multi = (int32_t)runs.mp.size();
+  }
   auto up = [&](int32_t* dst, const std::vector<int32_t>& v) {
     return v.empty() ? cudaSuccess
                      : cudaMemcpyAsync(dst, v.data(), v.size() * sizeof(int32_t), cudaMemcpyHostToDevice, st);
@@ -663,6 +660,12 @@ extern "C" int32_t gnnco_partition_load(const gnnco_graph_desc* g, void* persist
   GNNCO_CUDA_TRY(up(P.wg_mpart, mp));
   GNNCO_CUDA_TRY(up(P.wg_mfirst, mf));
   GNNCO_CUDA_TRY(up(P.wg_mcount, mc));
+  GNNCO_CUDA_TRY(up(P.run_begin, runs.wb));
+  GNNCO_CUDA_TRY(up(P.run_end, runs.we));
+  GNNCO_CUDA_TRY(up(P.run_slot, runs.wsl));
+  GNNCO_CUDA_TRY(up(P.run_mpart, runs.mp));
+  GNNCO_CUDA_TRY(up(P.run_mfirst, runs.mf));
+  GNNCO_CUDA_TRY(up(P.run_mcount, runs.mc));
   GNNCO_CUDA_TRY(cudaMemcpyAsync(hs, P.status, sizeof(hs), cudaMemcpyDeviceToHost, st));
   GNNCO_CUDA_TRY(cudaStreamSynchronize(st));
   if (hs[kStatus] != GNNCO_OK) return hs[kStatus];

@@ -136,7 +136,7 @@ void launch_drop(gnnco_handle* h, DropArgs A, cudaStream_t st) {
       return;
     }
   }
-  A.groups = (A.F + 3) / 4;
+  A.groups = A.F / 4 + (A.F % 4 != 0);                     // (F + 3 may not fit)
   drop_quads<T, kQuads><<<blocks(256 * kQuads), 256, 0, st>>>(A);
 }
 

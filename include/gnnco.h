@@ -443,8 +443,8 @@ int32_t gnnco_block_norm_backward(gnnco_handle* h, const gnnco_block_norm_desc* 
  * out.  A dropped element is 0 whatever it was (NaN included); p = 0 keeps all, p = 1 none.
  * step_dev (device, one uint32, or NULL) is read when the kernel runs, so that a recorded graph draws a new mask whenever the
  * caller advances it; advance it after the backward pass, which has to see the forward pass's value.
- * Rows are x_ld / out_ld elements apart; out may be x.  Any alignment works, 16-byte aligned rows are faster.  Asynchronous
- * on `stream`. */
+ * Rows are x_ld / out_ld elements apart; out may be x, with out_ld == x_ld.  Any alignment works, 16-byte aligned rows are
+ * faster.  Asynchronous on `stream`. */
 typedef struct {
   double p;                      /* probability of being dropped, in [0, 1] */
   uint64_t seed;

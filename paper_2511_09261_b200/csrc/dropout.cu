@@ -168,6 +168,7 @@ extern "C" int32_t gnnco_dropout(gnnco_handle* h, int32_t feat_dtype, int64_t ro
   if (feat_dtype != GNNCO_F32 && feat_dtype != GNNCO_BF16) return GNNCO_UNSUPPORTED;
   if (rows == 0) return GNNCO_OK;
   if (!x || !out || x_ld < F || out_ld < F || rows > ((int64_t)1 << 62) / F || !on_own_device(h)) return GNNCO_INVALID_ARGUMENT;
+  if (x == out && x_ld != out_ld && rows > 1) return GNNCO_INVALID_ARGUMENT;         // (a row of out would lie over other rows of x)
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   ProfScope prof_(h, K_DROPOUT, st);
   const size_t es = feat_dtype == GNNCO_F32 ? 4 : 2;

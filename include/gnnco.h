@@ -471,8 +471,9 @@ int32_t gnnco_dropout(gnnco_handle* h, int32_t feat_dtype, int64_t rows, int32_t
  * fixed order; with bfloat16 features the tensor cores sum runs of at most 65,536 rows (sets == S: and at most max(2,048, n / (4 SMs))
  * rows of a subgraph) and may lose 2^-27 of the terms' magnitudes per row of a run.  A subgraph without rows gets zero gradients.
  * x_ld, y_ld, dy_ld, dx_ld: elements between rows.  Any alignment works; 16-byte aligned rows and weights (widths that are
- * multiples of 8 in bfloat16) spare a copy.  dx may be x or dy, and y may be x.  ws: gnnco_gated_ff_workspace_bytes bytes for the same d (its
- * pointers included), 256-byte aligned, not shared by calls that may overlap.  rows < 2^31 - 256, widths <= 65536.
+ * multiples of 8 in bfloat16) spare a copy.  dx may be x or dy; y may be x, with y_ld == x_ld.
+ * ws: gnnco_gated_ff_workspace_bytes bytes for the same d (its pointers included), 256-byte aligned, not shared by calls that may
+ * overlap.  rows < 2^31 - 256, widths <= 65536.
  * Asynchronous on `stream`. */
 typedef enum { GNNCO_SILU = 0, GNNCO_GELU = 1, GNNCO_RELU = 2 } gnnco_activation;
 typedef struct {

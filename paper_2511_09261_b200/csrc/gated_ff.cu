@@ -650,6 +650,8 @@ extern "C" int32_t gnnco_gated_ff(gnnco_handle* h, const gnnco_gated_ff_desc* d,
   if (!d->x || d->x_ld < d->F || !d->w_gate || !d->w_up || !d->w_down || !y || y_ld < d->F_out || !ws || ((uintptr_t)ws & 255) ||
       !on_own_device(h))
     return GNNCO_INVALID_ARGUMENT;
+  // (a row of y would lie over other rows of x, which one of the kernels reads while it writes y)
+  if (y == d->x && y_ld != d->x_ld && d->rows > 1) return GNNCO_INVALID_ARGUMENT;
   const Work w = lay_out(h, d, false);
   if (ws_bytes < w.total) return GNNCO_WORKSPACE_TOO_SMALL;
   c.h = h;

@@ -264,7 +264,8 @@ bool fuses(const gnnco_handle* h, const gnnco_gated_ff_desc* d) {
 // rows, by pairs of CTAs for 256).  Backward passes, in one kernel and in two, in us: 1.13 M x 128 x 256 in 1,024 sets 1,220 and 1,320,
 // 300,000 x 32 x 64 in 512 113 and 125, 1,000 x 64 x 128 in 8 20.5 and 22.6, 4,000 x 128 x 256 32.7 and 32.8; but 60,000 x 64 x 600 in
 // 64 170 and 166, 20,000 x 128 x 1,024 133 and 117, and with few tiles 300 x 128 x 256 24.6 and 22.6.
-// dx is written before the weight gradients read x and dy there, so it must be neither of them.
+// dx is written there before the weight gradients read x and dy, so it must be neither of them; without weight gradients it may lie over
+// them row by row (a tile's rows are read before they are written, other tiles' rows at any time).
 bool fuses_back(const gnnco_handle* h, const gnnco_gated_ff_desc* d, const gnnco_gated_ff_grads* g, const Operand& x, const Operand& dy) {
   if (d->feat_dtype != GNNCO_BF16 || d->F > 128 || d->F_out > 128 || d->H > 256 || !g->dx || ((uintptr_t)g->dx & 15) || g->dx_ld % 8 || d->F % 8)
     return false;
@@ -272,7 +273,13 @@ bool fuses_back(const gnnco_handle* h, const gnnco_gated_ff_desc* d, const gnnco
     const uintptr_t a = (uintptr_t)g->dx, b = (uintptr_t)o.p;
     return a + ((d->rows - 1) * g->dx_ld + d->F) * 2 <= b || b + ((d->rows - 1) * o.ld + cols) * 2 <= a;
   };
-  if (g->dw_gate && !(apart(x, d->F) && apart(dy, d->F_out))) return false;
+  // row r of dx touches no row of o but r
+  auto by_rows = [&](const Operand& o, int cols) {
+    const int64_t off = (int64_t)((uintptr_t)g->dx - (uintptr_t)o.p), ld = g->dx_ld;
+    return d->rows == 1 || (o.ld == ld && off <= (ld - d->F) * 2 && off >= (cols - ld) * 2);
+  };
+  auto fits = [&](const Operand& o, int cols) { return apart(o, cols) || (!g->dw_gate && by_rows(o, cols)); };
+  if (!fits(x, d->F) || !fits(dy, d->F_out)) return false;
   const int64_t tiles = d->sets > 1 ? h->all_rows.n_tiles : blocks_of(d->rows, 128);
   return 4 * tiles >= h->sm_count || d->H <= 128;
 }

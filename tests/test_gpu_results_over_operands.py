@@ -36,3 +36,29 @@ def test_forward_refuses_rows_of_another_distance(graph, dtype, rows, F, Fo):
     want = graph.gated_ff(x, *w)
     graph.gated_ff(wide[:, :F], *w, out=wide[:, :Fo])
     assert torch.equal(wide[:, :Fo], want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("want_dw", [False, True])
+@pytest.mark.parametrize("F,Fo", [(64, 128), (128, 64), (128, 40), (64, 64)])
+def test_dx_over_operands(graph, dtype, want_dw, F, Fo):
+    """dx in the place of dy as rows of another distance, of x with gaps, of the same rows, and in columns beside x."""
+    import torch
+    rows = graph.n
+    x, dy, *w = make(rows, graph.S, F, 96, Fo, dtype)
+    want = graph.gated_ff_backward(x, dy, *w, want_dw=want_dw)
+
+    def check(x, dy, dx):
+        d = graph.gated_ff_backward(x, dy, *w, want_dw=want_dw, dx=dx)
+        torch.cuda.synchronize()
+        assert all((a is None) == (d[n] is None) and (a is None or torch.equal(d[n], a)) for n, a in want.items())
+    buffer = torch.zeros(rows, 2 * max(F, Fo), dtype=x.dtype, device="cuda")
+    over(buffer, Fo).copy_(dy)
+    check(x, over(buffer, Fo), over(buffer, F))
+    buffer[:, :F] = x
+    check(buffer[:, :F], dy, over(buffer, F))
+    buffer[:, :F] = x
+    check(buffer[:, :F], dy, buffer[:, :F])
+    buffer[:, :F] = x
+    check(buffer[:, :F], dy, buffer[:, F:2 * F])
+    assert torch.equal(buffer[:, :F], x)

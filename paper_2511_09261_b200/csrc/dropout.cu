@@ -4,7 +4,7 @@
 // A thread takes one vector of 16 bytes (two or four, loaded before the words are computed, took as long or longer: 2.5 M x 256 bfloat16
 // 583 us with one, 597 with two, 586 with four).  Elements whose word falls below the limit are set to 0 by selection, not by a
 // product: an infinity or NaN that is dropped is gone.
-// A quad takes 17 wide products and 19 logical instructions, a quarter of that per element.  In bfloat16, at 4 bytes moved per element,
+// A quad takes 18 wide products and 19 logical instructions, a quarter of that per element.  In bfloat16, at 4 bytes moved per element,
 // this is what bounds it: 4.4 TB/s, the pipe of the wide products 73 % busy, the one of logic and comparisons 55 %; as separate
 // high and low products the same work took 647 us.
 #include <math.h>

@@ -17,7 +17,8 @@
 // What bounds it: the products without dropout (400,000 x 256 x 512: 272 us, tensor pipe 63 % active, the special functions of SiLU 47 %),
 // products and the words' wide multiplications with it (331 us, tensor pipe 50 %).  DRAM carries 1.9 TB/s.
 //
-// Shared memory per CTA: x 64 KB, h 32 KB, blocks of Wg (even CTA) or Wu (odd) 4 x 16 KB, of Wd 2 x 16 KB, staging 32 KB.
+// Shared memory per CTA: x 64 KB, h 32 KB, blocks of Wg (even CTA) or Wu (odd) 4 x 16 KB, of Wd 2 x 16 KB, staging 16 KB, bits of the
+// mask 2 x 4 KB.
 // Roles of the warps: 0 products, 1 copies, 4-11 results; with dropout 2, 3 and 12-15 draw.  (Eight result warps with 168 registers
 // each hold nearly all of their g and u, so the accumulator is free soon; sixteen with 96 had to compute the first half before they
 // could take the second, and the products waited: 1,666 us against 1,590.  With dropout the launch has 128 registers a thread.)

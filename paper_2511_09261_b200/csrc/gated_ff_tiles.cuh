@@ -189,8 +189,8 @@ __device__ __forceinline__ Two inverse(Two x) {
 // a = act(g) and, for the backward pass, slope = act'(g).
 //   SiLU   s = 1 / (1 + 2^(-g log2 e)):  a = g s,  a' = s + a (1 - s)
 //   GELU   E = exp(-g^2 / 2), Phi(-|g|) = E t P(t) with t = 1 / (1 + 0.3 |g| / sqrt 2), P of degree 8 fitted to
-//          erfc(z) exp(z^2) / (2 t) over t (2e-8 of the value everywhere; in float32 4e-7 up to |g| = 2, 1.5e-6 up to 5, where Phi is
-//          3e-7):  a = g Phi(g),  a' = Phi(g) + g E / sqrt(2 pi)
+//          erfc(z) exp(z^2) / (2 t) over t (4.5e-8 of the value at most up to |g| = 14, where Phi is 8e-45; with E and the rest in
+//          float32, of a 4.8e-7 up to |g| = 2, 1.5e-6 up to 5 and 7.5e-6 up to 12, where Phi is 2e-33):  a = g Phi(g),  a' = Phi(g) + g E / sqrt(2 pi)
 template <int ACT, bool BACK>
 __device__ __forceinline__ void activate(Two g, Two& a, Two& slope) {
   if (ACT == GNNCO_SILU) {

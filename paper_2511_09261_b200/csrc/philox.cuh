@@ -27,7 +27,7 @@ inline void set_seed(Mask* m, uint64_t seed) {
 }
 
 // The part of the rounds that all counters of a launch share is computed once: the second product of round 1, and, while the upper
-// half of the quad's number stays the same, the first product of round 2 (17 products a quad instead of 20).
+// half of the quad's number stays the same, the first product of round 2 (18 products a quad instead of 20).
 struct Stream {
   uint32_t hi1, lo1, last_hi, hi2, lo2;
   __device__ __forceinline__ explicit Stream(const Mask& m) {

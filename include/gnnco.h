@@ -27,7 +27,7 @@
  *   - Dense matrices are row-major.
  *   - Calls on one handle are issued by one thread at a time, but for gnnco_dropout, gnnco_block_norm*,
  *     gnnco_gated_ff*: other threads may issue these at any time after the load, also while a training step is
- *     being issued.
+ *     being issued (but not while kernels are timed by gnnco_profile_begin).
  */
 #ifndef GNNCO_H_
 #define GNNCO_H_
